@@ -81,13 +81,17 @@ typedef enum {
   NGC_DEV_STRIP_FULL = 4,     /* append would exceed the sequence's row capacity */
   NGC_DEV_LISTS_DISAGREE = 5, /* lists of one sequence keep different token counts */
   NGC_DEV_TIMEOUT = 6,        /* a bounded wait inside a kernel ran out */
-  NGC_DEV_DEBUG_BOUNDS = 7    /* bounds-checking build only: a kernel computed an index outside its array */
+  NGC_DEV_DEBUG_BOUNDS = 7,   /* bounds-checking build only: a kernel computed an index outside its array */
+  NGC_DEV_BAD_TREE = 8,       /* a node count, parent link, drafted token or accepted path that is none */
+  NGC_DEV_BAD_PROBS = 9,      /* probabilities without a finite positive sum */
+  NGC_DEV_BAD_SOURCE = 10,    /* a fork's source is no sequence, or is itself a destination */
+  NGC_DEV_BAD_PAGE = 11       /* a page-table entry outside 0 .. pages_cap-1 */
 } ngc_dev_status;
 
 typedef enum { NGC_F32 = 0, NGC_BF16 = 1 } ngc_dtype;
 typedef enum { NGC_LISTS_SHARED = 0, NGC_LISTS_PER_LAYER = 1, NGC_LISTS_PER_LAYER_KVHEAD = 2 } ngc_lists;
 typedef enum { NGC_OP_SCORE = 0, NGC_OP_SAMPLE = 1, NGC_OP_LOGPROB = 2, NGC_OP_COMPACT = 3, NGC_OP_DECODE = 4,
-               NGC_OP_SCORE_BACKWARD = 5 } ngc_op;
+               NGC_OP_SCORE_BACKWARD = 5, NGC_OP_TREE_ATTN = 6 } ngc_op;
 
 /* Describes the cache; owns nothing.  `rows` and `max_len` are host copies the
  * launch geometry needs: rows = seq_off[B]; max_len >= every length at the
@@ -116,7 +120,9 @@ int ngc_last_cuda_error(void);
 /* Bytes of workspace `op` needs for this cache / list shape (0 = none).  For
  * NGC_OP_SAMPLE and NGC_OP_LOGPROB only c->B (sequences, times rounds for the
  * log-prob) is read from the cache descriptor; pass G, n_max, k_max as in the
- * call.  The workspace must be 256-byte aligned; its contents need not be
+ * call (NGC_OP_TREE_ATTN: n_max = nodes per tree; for a paged cache pass a
+ * contiguous descriptor with rows = B * pages_cap * page and max_len =
+ * pages_cap * page).  The workspace must be 256-byte aligned; its contents need not be
  * preserved between calls, and calls sharing a workspace must be stream-ordered. */
 size_t ngc_workspace_bytes(int op, const ngc_cache* c, int G, int n_max, int k_max);
 
@@ -431,6 +437,124 @@ int ngc_decode_attn_paged(ngc_paged_cache* c, const void* q, const void* new_k, 
 int ngc_decode_attn_ragged_static(ngc_cache* c, const void* q, const void* new_k, const void* new_v,
                                   int layer_begin, int layer_end, float scale,
                                   void* out, int out_dtype, int32_t* dev_status, ngc_stream stream);
+
+/*
+ * Drafted tokens.  (The paper decodes one token per pass; these calls let a
+ * rollout advance by several, and let the rollouts of one prompt -- Section 5.1
+ * samples a group per prompt -- share its prefill.)  A draft is a TREE of up to
+ * NGC_TREE_MAX_NODES tokens per sequence: node 0 is the pending token (the
+ * last one sampled, whose K/V is not in the cache yet), every other node
+ * continues its parent.  One step is
+ *   ngc_tree_attn (per layer or for all) -> the model's output probabilities
+ *   -> ngc_verify_draft -> ngc_commit_draft.
+ * Nothing of the draft is in the cache before the commit, so there is nothing
+ * to roll back.  Arguments shared by the calls:
+ *   parent  [B][N] int32: parent[b][0] = -1, 0 <= parent[b][i] < i for i >= 1
+ *   n_nodes [B] int32 or NULL (= N): nodes of each tree, 0 .. N; the others'
+ *           entries are ignored wherever they appear
+ * A sequence with a bad count or link is reported as NGC_DEV_BAD_TREE and
+ * skipped.
+ */
+#define NGC_TREE_MAX_NODES 128
+
+/*
+ * Attention for a tree of drafted tokens over a cache: node i attends to every
+ * alive cache row of its strip, to its ancestors and to itself,
+ *   out_i = softmax_j(scale * q_i . k_j) V,  j over alive rows and ancestors-or-self.
+ * For layers [layer_begin, layer_end); reads lens and the cache, changes neither.
+ *   q       [L][B][Hq][N][d] cache dtype;  tree_k, tree_v [L][B][Hkv][N][d] cache dtype
+ *   N       1 .. NGC_TREE_MAX_NODES (N = 1: the one-token decode without append)
+ *   scale   positive and finite
+ *   out     [L][B][Hq][N][d] of out_dtype (NGC_F32, or NGC_BF16 for a bf16
+ *           cache); only the layers of the range and the nodes of each tree
+ *           are written
+ * Masked and dead rows take no part whatever they hold (infinities, NaN).
+ * fp32 scores, softmax and accumulation; on bf16 caches the probabilities are
+ * rounded to bf16 for the P*V product.  A length outside 0 .. capacity is
+ * reported (NGC_DEV_BAD_COUNTS) and the sequence skipped.  q, tree_k, tree_v,
+ * out, k and v must be 16-byte aligned.  Workspace:
+ * ngc_workspace_bytes(NGC_OP_TREE_ATTN, c, 1, N, 0).
+ */
+int ngc_tree_attn(const ngc_cache* c, const void* q, const void* tree_k, const void* tree_v, const int32_t* parent,
+                  const int32_t* n_nodes, int N, int layer_begin, int layer_end, float scale, void* out, int out_dtype,
+                  void* ws, size_t ws_bytes, int32_t* dev_status, ngc_stream stream);
+
+/* Number of kernels one ngc_tree_attn call over `layers` layers of this cache enqueues (host-only planning query). */
+int ngc_tree_attn_launches(const ngc_cache* c, int layers, int N);
+
+/* ngc_tree_attn over a paged cache.  A page-table entry outside 0 .. pages_cap-1 is reported as
+ * NGC_DEV_BAD_PAGE; the outputs of that sequence are then unspecified. */
+int ngc_tree_attn_paged(const ngc_paged_cache* c, const void* q, const void* tree_k, const void* tree_v, const int32_t* parent,
+                        const int32_t* n_nodes, int N, int layer_begin, int layer_end, float scale, void* out, int out_dtype,
+                        void* ws, size_t ws_bytes, int32_t* dev_status, ngc_stream stream);
+
+/*
+ * Verification of a drafted tree against the target's probabilities from given
+ * random numbers (multi-round speculative sampling: the token sequence that
+ * comes out is distributed as if sampled from the target).  The walk starts
+ * at node 0 and tries the children of the current node in index order; at a
+ * node with target row p and draft row q, starting from w = p and S = 1, child
+ * i with token x = tokens[b][i] and u = uniforms[b][i]:
+ *   draft_probs given (children drawn independently from q):
+ *     accepted iff u * q(x) * S < w(x);  else w <- max(w - S q, 0), S <- sum w
+ *   draft_probs NULL (children picked without chance, e.g. the likeliest tokens):
+ *     accepted iff u * S < w(x);         else S <- S - w(x), w(x) <- 0
+ *   greedy != 0 (uniforms and draft_probs unused): accepted iff x is the
+ *     argmax of p (smallest index of equal ones)
+ * (a rejection that would leave no mass leaves w and S as they were).  An
+ * accepted child becomes the current node.  When no child is left the next
+ * token is drawn from what remains: the first x whose running sum of w exceeds
+ * uniforms[b][0] * sum w -- or the argmax, if greedy.
+ *   tokens       [B][N] int32 in 0 .. vocab-1 (entry 0 unused)
+ *   target_probs [B][N][vocab] fp32: row i follows node i.  Rows are taken as
+ *                normalised; only the rows the walk visits are read.
+ *   draft_probs  [B][N][vocab] fp32 or NULL: row i is what node i's children were drawn from
+ *   uniforms     [B][N] fp32 in [0, 1) (may be NULL if greedy)
+ *   path         [B][N] out: accepted nodes from node 0 on, -1 padded (ascending)
+ *   n_path       [B] out: their number (>= 1; 0 for an empty tree)
+ *   next_token   [B] out: the token that follows the path (-1 for an empty tree)
+ * Decisions and sums in fp64: the outcome does not depend on launch geometry
+ * beyond the last bits of an fp64 sum.  A bad tree or token (NGC_DEV_BAD_TREE)
+ * or a visited row without a finite positive sum (NGC_DEV_BAD_PROBS; a NaN, if
+ * greedy) gives path -1, n_path 0, next_token -1.
+ */
+int ngc_verify_draft(const int32_t* tokens, const int32_t* parent, const int32_t* n_nodes, const float* target_probs,
+                     const float* draft_probs, const float* uniforms, int B, int N, int vocab, int greedy,
+                     int32_t* path, int32_t* n_path, int32_t* next_token, int32_t* dev_status, ngc_stream stream);
+
+/*
+ * Appends the K/V rows of the accepted nodes: row path[b][j] of tree_k / tree_v
+ * goes to position len + j of every strip, for j < n_path[b], and the lengths
+ * grow by n_path[b].  Bit-exact row copies.
+ *   tree_k, tree_v [L][B][Hkv][N][d] as given to ngc_tree_attn, 16-byte aligned
+ *   path [B][N], n_path [B] as written by ngc_verify_draft
+ * A path that is not ascending within 0 .. N-1 (NGC_DEV_BAD_TREE) or does not
+ * fit the sequence's capacity in some list (NGC_DEV_STRIP_FULL) leaves the
+ * sequence as it was.
+ */
+int ngc_commit_draft(ngc_cache* c, const void* tree_k, const void* tree_v, const int32_t* path, const int32_t* n_path,
+                     int N, int32_t* dev_status, ngc_stream stream);
+
+/* ngc_commit_draft on a paged cache: the rows go to the pages that positions len + j fall into.  A bad
+ * page-table entry among them (NGC_DEV_BAD_PAGE) leaves the sequence as it was. */
+int ngc_commit_draft_paged(ngc_paged_cache* c, const void* tree_k, const void* tree_v, const int32_t* path,
+                           const int32_t* n_path, int N, int32_t* dev_status, ngc_stream stream);
+
+/*
+ * Forks sequences: sequence b becomes a copy of sequence src_of[b] (its alive
+ * rows in every strip and its lengths; rows beyond them stay as they were).
+ *   src_of [B] int32: -1 or b itself = sequence b is left alone.  A source must
+ *          be left alone itself; otherwise, or with a source outside 0 .. B-1,
+ *          b is reported (NGC_DEV_BAD_SOURCE) and left as it was, as is a b too
+ *          small for its source in some list (NGC_DEV_STRIP_FULL) or one whose
+ *          source has a length outside its capacity (NGC_DEV_BAD_COUNTS).
+ */
+int ngc_fork_kv(ngc_cache* c, const int32_t* src_of, int32_t* dev_status, ngc_stream stream);
+
+/* ngc_fork_kv on a paged cache: rows are copied page by page, from the pages the source's table names to the
+ * first pages of b's own table (the tables do not change).  A bad page-table entry among them
+ * (NGC_DEV_BAD_PAGE) leaves b as it was. */
+int ngc_fork_pages(ngc_paged_cache* c, const int32_t* src_of, int32_t* dev_status, ngc_stream stream);
 
 /*
  * Self-test of the bounded wait.  (The paper has no counterpart: this is a

@@ -20,15 +20,19 @@ LIB_PATH = os.path.join(_HERE, "libngc_b200.so")
 
 F32, BF16 = 0, 1
 LISTS_SHARED, LISTS_PER_LAYER, LISTS_PER_LAYER_KVHEAD = 0, 1, 2
-OP_SCORE, OP_SAMPLE, OP_LOGPROB, OP_COMPACT, OP_DECODE, OP_SCORE_BACKWARD = range(6)
+OP_SCORE, OP_SAMPLE, OP_LOGPROB, OP_COMPACT, OP_DECODE, OP_SCORE_BACKWARD, OP_TREE_ATTN = range(7)
 
 DEV_STATUS = {0: "ok", 1: "bad counts", 2: "NaN logit", 3: "bad kept list", 4: "strip full",
-              5: "lists disagree", 6: "timeout", 7: "index out of bounds (bounds-checking build)"}
+              5: "lists disagree", 6: "timeout", 7: "index out of bounds (bounds-checking build)", 8: "bad drafted tree or path",
+              9: "probabilities without a finite positive sum", 10: "bad fork source", 11: "bad page-table entry"}
 
 EXPORTS = ["ngc_version", "ngc_strerror", "ngc_last_cuda_error", "ngc_workspace_bytes", "ngc_decode_splits", "ngc_score_evict", "ngc_score_evict_launches",
            "ngc_sample_evict", "ngc_evict_logprob", "ngc_evict_logprob_backward", "ngc_compact_kv", "ngc_decode_attn_ragged",
-           "ngc_decode_attn_ragged_static", "ngc_evict_pages", "ngc_decode_attn_paged", "ngc_score_evict_paged", "ngc_replay_visibility", "ngc_score_evict_backward", "ngc_replay_attn", "ngc_replay_attn_variant", "ngc_selftest_bounded_wait"]
+           "ngc_decode_attn_ragged_static", "ngc_evict_pages", "ngc_decode_attn_paged", "ngc_score_evict_paged", "ngc_replay_visibility", "ngc_score_evict_backward", "ngc_replay_attn", "ngc_replay_attn_variant", "ngc_selftest_bounded_wait",
+           "ngc_tree_attn", "ngc_tree_attn_paged", "ngc_tree_attn_launches", "ngc_verify_draft", "ngc_commit_draft", "ngc_commit_draft_paged",
+           "ngc_fork_kv", "ngc_fork_pages"]
 STATIC_SCRATCH_BYTES = 8 << 20
+TREE_MAX_NODES = 128
 
 
 class NgcError(RuntimeError):
@@ -97,6 +101,23 @@ def _load(path: str = LIB_PATH):
     lib.ngc_evict_pages.argtypes = [C.POINTER(PagedCacheDesc), vp, vp, i32, vp, vp]
     lib.ngc_decode_attn_paged.restype = i32
     lib.ngc_decode_attn_paged.argtypes = [C.POINTER(PagedCacheDesc), vp, vp, vp, i32, i32, C.c_float, vp, i32, vp, sz, vp, vp]
+    tree = [vp, vp, vp, vp, vp, i32, i32, i32, C.c_float, vp, i32, vp, sz, vp, vp]
+    lib.ngc_tree_attn.restype = i32
+    lib.ngc_tree_attn.argtypes = [C.POINTER(CacheDesc)] + tree
+    lib.ngc_tree_attn_paged.restype = i32
+    lib.ngc_tree_attn_paged.argtypes = [C.POINTER(PagedCacheDesc)] + tree
+    lib.ngc_tree_attn_launches.restype = i32
+    lib.ngc_tree_attn_launches.argtypes = [C.POINTER(CacheDesc), i32, i32]
+    lib.ngc_verify_draft.restype = i32
+    lib.ngc_verify_draft.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.ngc_commit_draft.restype = i32
+    lib.ngc_commit_draft.argtypes = [C.POINTER(CacheDesc), vp, vp, vp, vp, i32, vp, vp]
+    lib.ngc_commit_draft_paged.restype = i32
+    lib.ngc_commit_draft_paged.argtypes = [C.POINTER(PagedCacheDesc), vp, vp, vp, vp, i32, vp, vp]
+    lib.ngc_fork_kv.restype = i32
+    lib.ngc_fork_kv.argtypes = [C.POINTER(CacheDesc), vp, vp, vp]
+    lib.ngc_fork_pages.restype = i32
+    lib.ngc_fork_pages.argtypes = [C.POINTER(PagedCacheDesc), vp, vp, vp]
     return lib
 
 
@@ -131,6 +152,26 @@ def _ptr(t: Optional[torch.Tensor]):
     if not t.is_contiguous():
         raise NgcError("contiguous tensors required")
     return t.data_ptr()
+
+
+def _expect(what: str, device: torch.device, *tensors):
+    """Checks of the drafted-token calls: every (name, tensor or None, shape, dtype) must have that shape and type, be
+    contiguous and live on ``device``, which must be the current one (the library launches there)."""
+    for name, t, shape, dtype in tensors:
+        if t is None:
+            continue
+        if t.shape != shape or t.dtype is not dtype:
+            raise NgcError(f"{what}: {name} must be {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+        if not t.is_contiguous():
+            raise NgcError(f"{what}: {name} must be contiguous")
+    if device.type != "cuda":
+        raise NgcError(f"{what}: device tensors required: the library has no CPU path")
+    index = device.index
+    for name, t, _, _ in tensors:
+        if t is not None and t.get_device() != index:
+            raise NgcError(f"{what}: {name} is on {t.device}, the call's other tensors on {device}")
+    if index != torch.cuda.current_device():
+        raise NgcError(f"{what}: tensors on {device}, but the current device is {torch.cuda.current_device()}")
 
 
 def _stream():
@@ -391,6 +432,115 @@ def ngc_score_evict_backward(cache: NgcCache, q_recent: torch.Tensor, block: int
                                       _ptr(grad_logits), grad_logits.shape[2], _ptr(grad_q_recent), _ptr(grad_k),
                                       _ptr(ws), 0 if ws is None else ws.numel(), _ptr(status), _stream())
     _check(rc, "ngc_score_evict_backward")
+
+
+def tree_attn_launches(cache: NgcCache, N: int, layers: Optional[int] = None) -> int:
+    """Kernels one ngc_tree_attn call over ``layers`` layers enqueues (launch counting)."""
+    d = cache.desc()
+    return int(lib.ngc_tree_attn_launches(C.byref(d), cache.L if layers is None else layers, N))
+
+
+def _cache_shape(cache):
+    """(L, B, Hkv, d) of a contiguous or paged cache."""
+    if isinstance(cache, NgcPagedCache):
+        return cache.k.shape[0], cache.page_table.shape[0], cache.k.shape[1], cache.k.shape[4]
+    return cache.L, cache.B, cache.Hkv, cache.d
+
+
+def _cache_tensors(cache):
+    """The cache's own tensors for _expect: types, and lengths of a shape the descriptor can name."""
+    k, i32 = cache.k, torch.int32
+    if isinstance(cache, NgcPagedCache):
+        B, G = cache.page_table.shape[:2]
+        per, tab = cache.lens.dim() == 2, ("page_table", cache.page_table, cache.page_table.shape, i32)
+    else:
+        B, per = cache.B, cache.lens_lists != 0
+        G, tab = lists_G(cache.lens_lists, k.shape[0], k.shape[1]), ("seq_off", cache.seq_off, (B + 1,), torch.int64)
+    return ("k", k, k.shape, k.dtype), ("v", cache.v, k.shape, k.dtype), ("lens", cache.lens, (B, G) if per else (B,), i32), tab
+
+
+def _tree_attn(what, call, cache, q, tree_k, tree_v, parent, out, n_nodes, layer_begin, layer_end, scale, ws, status):
+    L, B, Hkv, d = _cache_shape(cache)
+    N, dt, i32 = parent.shape[-1], cache.k.dtype, torch.int32
+    heads, rows = (L, B, cache.Hq, N, d), (L, B, Hkv, N, d)
+    _expect(what, cache.k.device, ("q", q, heads, dt), ("tree_k", tree_k, rows, dt), ("tree_v", tree_v, rows, dt), ("parent", parent, (B, N), i32),
+            ("n_nodes", n_nodes, (B,), i32), ("out", out, heads, out.dtype), ("ws", ws, ws.shape if ws is not None else (), torch.uint8),
+            ("status", status, (1,), i32), *_cache_tensors(cache))
+    desc = cache.desc()
+    rc = call(C.byref(desc), _ptr(q), _ptr(tree_k), _ptr(tree_v), _ptr(parent), _ptr(n_nodes), N, layer_begin,
+              L if layer_end is None else layer_end, 1.0 / (d ** 0.5) if scale is None else scale, _ptr(out), _dtype_code(out),
+              _ptr(ws), 0 if ws is None else ws.numel(), _ptr(status), _stream())
+    _check(rc, what)
+
+
+def ngc_tree_attn(cache: NgcCache, q: torch.Tensor, tree_k: torch.Tensor, tree_v: torch.Tensor, parent: torch.Tensor,
+                  out: torch.Tensor, n_nodes: Optional[torch.Tensor] = None, layer_begin: int = 0, layer_end: Optional[int] = None,
+                  scale: Optional[float] = None, ws: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """Attention for a tree of drafted tokens over the cache: q, out [L][B][Hq][N][d]; tree_k, tree_v [L][B][Hkv][N][d];
+    parent int32 [B][N]; n_nodes int32 [B] or None (= N).  ``ws``: workspace_bytes(OP_TREE_ATTN, cache, n_max=N)."""
+    _tree_attn("ngc_tree_attn", lib.ngc_tree_attn, cache, q, tree_k, tree_v, parent, out, n_nodes, layer_begin, layer_end, scale, ws, status)
+
+
+def ngc_tree_attn_paged(cache: NgcPagedCache, q: torch.Tensor, tree_k: torch.Tensor, tree_v: torch.Tensor, parent: torch.Tensor,
+                        out: torch.Tensor, n_nodes: Optional[torch.Tensor] = None, layer_begin: int = 0,
+                        layer_end: Optional[int] = None, scale: Optional[float] = None, ws: Optional[torch.Tensor] = None,
+                        status: Optional[torch.Tensor] = None):
+    """ngc_tree_attn over a paged cache (``ws``: workspace_bytes(OP_TREE_ATTN, cache.as_contiguous_desc(), n_max=N))."""
+    _tree_attn("ngc_tree_attn_paged", lib.ngc_tree_attn_paged, cache, q, tree_k, tree_v, parent, out, n_nodes, layer_begin, layer_end,
+               scale, ws, status)
+
+
+def ngc_verify_draft(tokens: torch.Tensor, parent: torch.Tensor, target_probs: torch.Tensor, uniforms: Optional[torch.Tensor],
+                     path: torch.Tensor, n_path: torch.Tensor, next_token: torch.Tensor, draft_probs: Optional[torch.Tensor] = None,
+                     n_nodes: Optional[torch.Tensor] = None, greedy: int = 0, status: Optional[torch.Tensor] = None):
+    """Walk of a drafted tree: target_probs, draft_probs fp32 [B][N][vocab]; tokens, parent, path int32 [B][N]; uniforms
+    fp32 [B][N] (entry 0: the final draw); n_path, next_token int32 [B]."""
+    B, N, V = target_probs.shape
+    i32, f32 = torch.int32, torch.float32
+    _expect("ngc_verify_draft", target_probs.device, ("tokens", tokens, (B, N), i32), ("parent", parent, (B, N), i32),
+            ("target_probs", target_probs, (B, N, V), f32), ("uniforms", uniforms, (B, N), f32), ("path", path, (B, N), i32),
+            ("n_path", n_path, (B,), i32), ("next_token", next_token, (B,), i32), ("draft_probs", draft_probs, (B, N, V), f32),
+            ("n_nodes", n_nodes, (B,), i32), ("status", status, (1,), i32))
+    rc = lib.ngc_verify_draft(_ptr(tokens), _ptr(parent), _ptr(n_nodes), _ptr(target_probs), _ptr(draft_probs), _ptr(uniforms), B, N, V,
+                              greedy, _ptr(path), _ptr(n_path), _ptr(next_token), _ptr(status), _stream())
+    _check(rc, "ngc_verify_draft")
+
+
+def _commit_draft(what, call, cache, tree_k, tree_v, path, n_path, status):
+    L, B, Hkv, d = _cache_shape(cache)
+    N, dt, i32 = path.shape[-1], cache.k.dtype, torch.int32
+    _expect(what, cache.k.device, ("tree_k", tree_k, (L, B, Hkv, N, d), dt), ("tree_v", tree_v, (L, B, Hkv, N, d), dt),
+            ("path", path, (B, N), i32), ("n_path", n_path, (B,), i32), ("status", status, (1,), i32), *_cache_tensors(cache))
+    desc = cache.desc()
+    _check(call(C.byref(desc), _ptr(tree_k), _ptr(tree_v), _ptr(path), _ptr(n_path), N, _ptr(status), _stream()), what)
+
+
+def ngc_commit_draft(cache: NgcCache, tree_k: torch.Tensor, tree_v: torch.Tensor, path: torch.Tensor, n_path: torch.Tensor,
+                     status: Optional[torch.Tensor] = None):
+    """Appends the accepted nodes' rows of tree_k / tree_v [L][B][Hkv][N][d] to the cache; lens grows by n_path."""
+    _commit_draft("ngc_commit_draft", lib.ngc_commit_draft, cache, tree_k, tree_v, path, n_path, status)
+
+
+def ngc_commit_draft_paged(cache: NgcPagedCache, tree_k: torch.Tensor, tree_v: torch.Tensor, path: torch.Tensor,
+                           n_path: torch.Tensor, status: Optional[torch.Tensor] = None):
+    _commit_draft("ngc_commit_draft_paged", lib.ngc_commit_draft_paged, cache, tree_k, tree_v, path, n_path, status)
+
+
+def _fork(what, call, cache, src_of, status):
+    _expect(what, cache.k.device, ("src_of", src_of, (_cache_shape(cache)[1],), torch.int32), ("status", status, (1,), torch.int32),
+            *_cache_tensors(cache))
+    desc = cache.desc()
+    _check(call(C.byref(desc), _ptr(src_of), _ptr(status), _stream()), what)
+
+
+def ngc_fork_kv(cache: NgcCache, src_of: torch.Tensor, status: Optional[torch.Tensor] = None):
+    """Sequence b becomes a copy of sequence src_of[b] (int32 [B]; -1 or b itself: left alone)."""
+    _fork("ngc_fork_kv", lib.ngc_fork_kv, cache, src_of, status)
+
+
+def ngc_fork_pages(cache: NgcPagedCache, src_of: torch.Tensor, status: Optional[torch.Tensor] = None):
+    """ngc_fork_kv on a paged cache: the source's pages are copied into b's own."""
+    _fork("ngc_fork_pages", lib.ngc_fork_pages, cache, src_of, status)
 
 
 REPLAY_ATTN_AUTO, REPLAY_ATTN_MMA_SYNC, REPLAY_ATTN_TCGEN05 = 0, 1, 2

@@ -76,6 +76,21 @@ __host__ __device__ inline int64_t len_index(int lens_lists, int L, int Hkv, int
   return (int64_t)b * lists_G(lens_lists, L, Hkv) + list_of(lens_lists, l, h, Hkv);
 }
 
+// A paged cache as a descriptor whose planes are the page pools (seq_off is null); false for one that is none.
+inline bool paged_as_cache(const ngc_paged_cache* pc, ngc_cache* c) {
+  if (!pc || !pc->k || !pc->v || !pc->page_table || !pc->lens || pc->L <= 0 || pc->B <= 0 || pc->Hq <= 0 || pc->Hkv <= 0 ||
+      pc->Hq % pc->Hkv != 0 || (pc->d != 64 && pc->d != 128) || (pc->dtype != NGC_F32 && pc->dtype != NGC_BF16) ||
+      pc->pages_cap <= 0 || (pc->page != 32 && pc->page != 64) || pc->lists < 0 || pc->lists > 2 ||
+      (int64_t)pc->pages_cap * pc->page > 0x7fffffffLL)
+    return false;
+  c->k = pc->k; c->v = pc->v; c->seq_off = nullptr; c->lens = pc->lens;
+  c->rows = (int64_t)pc->B * pc->pages_cap * pc->page;
+  c->L = pc->L; c->B = pc->B; c->Hq = pc->Hq; c->Hkv = pc->Hkv; c->d = pc->d; c->dtype = pc->dtype;
+  c->max_len = pc->pages_cap * pc->page;
+  c->lens_lists = pc->lens_per_list ? pc->lists : 0;
+  return true;
+}
+
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Set-up that CUDA keeps PER DEVICE (a kernel's opt-in to more than 48 KB of dynamic shared

@@ -22,4 +22,6 @@ size_t sample_workspace_bytes(int B, int G, int n_max);
 size_t score_workspace_bytes(const ngc_cache* c, int G, int n_max);
 size_t score_backward_workspace_bytes(const ngc_cache* c);
 
+size_t tree_workspace_bytes(const ngc_cache* c, int N);
+
 }  // namespace ngc

@@ -1,0 +1,392 @@
+// ngc_tree_attn: attention for a tree of drafted tokens over the pruned cache.
+//
+// The query rows of one KV head are the N nodes of each of its g query heads; in the layout
+// [Hq][N][d] they are g * N consecutive rows, so a work item is a block of those rows, all of which
+// see the alive cache rows and, of the tree, their ancestors.  Keys are numbered through: cache rows
+// first, then the nodes; a row's mask only matters in the node part, where it is a bit of the node's
+// ancestor set.
+//
+// FMA path (this file): tiles of 32 keys in shared memory as fp32, 4 rows x 2 keys of S and 4 rows x
+// 8 channels (d = 128) of O per thread, online softmax with the row statistics spread over 16 lanes.
+// One pass over K and V; with few items the key axis is split and a combine kernel joins the parts.
+#include <cuda_bf16.h>
+
+#include "ngc_plan.h"
+#include "tree_attn.cuh"
+
+namespace ngc {
+namespace {
+
+constexpr int kKeyTile = 32;                    // keys per tile, and the split granularity
+constexpr int kSplitMin = 8;                    // tiles a split has at least
+
+// (m, l) of a row that is not computed (a node beyond the tree, a refused sequence): the combine kernel leaves it alone.
+#define kNoPart make_float2(0.f, -1.f)
+
+__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
+  const uint2 t = *reinterpret_cast<const uint2*>(p);
+  const __nv_bfloat162 a = *reinterpret_cast<const __nv_bfloat162*>(&t.x), c = *reinterpret_cast<const __nv_bfloat162*>(&t.y);
+  return make_float4(__low2float(a), __high2float(a), __low2float(c), __high2float(c));
+}
+__device__ __forceinline__ bool finite4(float4 x) {
+  return isfinite(x.x) && isfinite(x.y) && isfinite(x.z) && isfinite(x.w);
+}
+__device__ __forceinline__ void store_out4(const TreeAttnParams& p, int64_t idx, float4 v) {
+  if (p.out_bf16)
+    *reinterpret_cast<uint2*>((__nv_bfloat16*)p.out + idx) = make_uint2(ptx::pack_bf16x2(v.x, v.y), ptx::pack_bf16x2(v.z, v.w));
+  else
+    *reinterpret_cast<float4*>((float*)p.out + idx) = v;
+}
+
+template <int D, int RB> struct FmaSmem {
+  float q[RB][D + 4], k[kKeyTile][D + 4], v[kKeyTile][D];
+  float p[kKeyTile][RB + 4];
+  uint32_t anc[kTreeMaxNodes][kTreeWords];
+  int jump[kTreeMaxNodes];
+  int odd;                                      // the tile's V rows hold an infinity or a NaN in its node part
+};
+
+// RB rows per item, 4 * RB threads: thread (ty, tx) of 16 lanes per row group owns rows 4 ty .. 4 ty + 3.
+template <typename T, int D, int RB>
+__global__ void __launch_bounds__(4 * RB) tree_fma_kernel(TreeAttnParams p) {
+  constexpr int NT = 4 * RB, CV = D / 64;       // CV float4 groups of channels per thread
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  FmaSmem<D, RB>& sm = *reinterpret_cast<FmaSmem<D, RB>*>(smem_raw);
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+
+  int item = blockIdx.x;
+  const int split = item % p.n_split; item /= p.n_split;
+  const int rb = item % p.row_blocks; item /= p.row_blocks;
+  const int h = item % p.Hkv; item /= p.Hkv;
+  const int b = item % p.B;
+  const int lr = item / p.B, l = p.layer_begin + lr;
+
+  ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
+  const int n = p.n_nodes ? p.n_nodes[b] : p.N;
+  const int rows = p.g * p.N, r0 = rb * RB;
+  const int64_t part0 = (((int64_t)lr * p.B + b) * p.Hq + (int64_t)h * p.g) * p.N;     // parts of the KV head's first row
+  const int len = p.lens[len_index(p.lens_lists, p.L, p.Hkv, b, l, h)];
+  const bool tree_ok = tree_masks<NT>(p.parent + (int64_t)b * p.N, n, p.N, sm.anc, sm.jump);
+  if (!tree_ok || len < 0 || len > tree_capacity(p, b)) {
+    if (tid == 0) set_dev_status(p.dev_status, tree_ok ? NGC_DEV_BAD_COUNTS : NGC_DEV_BAD_TREE);
+    if (p.n_split > 1)
+      for (int r = r0 + tid; r < min(rows, r0 + RB); r += NT) p.part_ml[(part0 + r) * p.n_split + split] = kNoPart;
+    return;
+  }
+  const int keys = len + n;
+  const int nt = (keys + kKeyTile - 1) / kKeyTile, tps = (nt + p.n_split - 1) / p.n_split;
+  const int tile_lo = min(nt, split * tps), tile_hi = min(nt, tile_lo + tps);
+  const int plane = l * p.Hkv + h;
+  const int32_t* table = p.page_table ? p.page_table + ((int64_t)b * p.G + list_of(p.lists, l, h, p.Hkv)) * p.pages_cap : nullptr;
+  const T* const kc = (const T*)p.k + (int64_t)plane * p.rows * D;
+  const T* const vc = (const T*)p.v + (int64_t)plane * p.rows * D;
+  const int64_t base = p.page_table ? (int64_t)b * p.pages_cap * p.page : p.seq_off[b];
+  const int64_t strip = ((int64_t)l * p.B + b) * p.Hkv + h;
+  const T* const kt = (const T*)p.tree_k + strip * p.N * D;
+  const T* const vt = (const T*)p.tree_v + strip * p.N * D;
+  const int64_t row0 = (((int64_t)l * p.B + b) * p.Hq + (int64_t)h * p.g) * p.N;       // first query row of the KV head
+
+  for (int i = tid; i < RB * (D / 4); i += NT) {
+    const int r = i / (D / 4), c = 4 * (i % (D / 4));
+    const float4 x = r0 + r < rows ? load4((const T*)p.q + (row0 + r0 + r) * D + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    *reinterpret_cast<float4*>(&sm.q[r][c]) = x;
+  }
+  int node[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int r = r0 + 4 * ty + e;
+    node[e] = r < rows && r % p.N < n ? r % p.N : -1;              // -1: a row that is not there, and not written
+  }
+  float m[4], lsum[4], acc[4][4 * CV];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    m[e] = -INFINITY; lsum[e] = 0.f;
+#pragma unroll
+    for (int c = 0; c < 4 * CV; ++c) acc[e][c] = 0.f;
+  }
+
+  for (int t = tile_lo; t < tile_hi; ++t) {
+    const int j0 = t * kKeyTile;
+    __syncthreads();                                               // the previous tile has been read
+    if (tid == 0) sm.odd = 0;
+    __syncthreads();
+    for (int i = tid; i < kKeyTile * (D / 4); i += NT) {
+      const int jj = i / (D / 4), c = 4 * (i % (D / 4)), j = j0 + jj;
+      float4 kx = make_float4(0.f, 0.f, 0.f, 0.f), vx = kx;        // dead keys: zeros, so that weight 0 x value is 0
+      if (j < len) {
+        int64_t row = base + j;
+        if (table) {
+          int pg = table[j / p.page];
+          if (pg < 0 || pg >= p.pages_cap) { set_dev_status(p.dev_status, NGC_DEV_BAD_PAGE); pg = 0; }
+          row = base + (int64_t)pg * p.page + j % p.page;
+        }
+        if (NGC_IN_BOUNDS(p.dev_status, row >= 0 && row < p.rows)) { kx = load4(kc + row * D + c); vx = load4(vc + row * D + c); }
+      } else if (j < keys) {
+        kx = load4(kt + (int64_t)(j - len) * D + c); vx = load4(vt + (int64_t)(j - len) * D + c);
+        if (!finite4(vx)) sm.odd = 1;
+      }
+      *reinterpret_cast<float4*>(&sm.k[jj][c]) = kx;
+      *reinterpret_cast<float4*>(&sm.v[jj][c]) = vx;
+    }
+    __syncthreads();
+    // S: rows 4 ty + e, keys tx and tx + 16
+    float s[4][2];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { s[e][0] = 0.f; s[e][1] = 0.f; }
+#pragma unroll 8
+    for (int c = 0; c < D; c += 4) {
+      const float4 k0 = *reinterpret_cast<const float4*>(&sm.k[tx][c]), k1 = *reinterpret_cast<const float4*>(&sm.k[tx + 16][c]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float4 x = *reinterpret_cast<const float4*>(&sm.q[4 * ty + e][c]);
+        s[e][0] = fmaf(x.x, k0.x, fmaf(x.y, k0.y, fmaf(x.z, k0.z, fmaf(x.w, k0.w, s[e][0]))));
+        s[e][1] = fmaf(x.x, k1.x, fmaf(x.y, k1.y, fmaf(x.z, k1.z, fmaf(x.w, k1.w, s[e][1]))));
+      }
+    }
+    uint32_t vis = 0;                                              // bit 2 e + u: row 4 ty + e sees key tx + 16 u
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int j = j0 + tx + 16 * u, i = j - len;
+        const bool see = j < len || (j < keys && node[e] >= 0 && ((sm.anc[node[e]][i >> 5] >> (i & 31)) & 1u));
+        vis |= (uint32_t)see << (2 * e + u);
+        s[e][u] = see ? s[e][u] * p.scale_log2 : -INFINITY;
+        mx = fmaxf(mx, s[e][u]);
+      }
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+      const float m_new = fmaxf(m[e], mx), m_eff = m_new == -INFINITY ? 0.f : m_new;    // nothing visible yet: weights 0
+      const float alpha = exp2f(m[e] - m_eff);
+      const float p0 = exp2f(s[e][0] - m_eff), p1 = exp2f(s[e][1] - m_eff);
+      lsum[e] = lsum[e] * alpha + (p0 + p1);                       // this lane's share; joined at the end
+      m[e] = m_new;
+      sm.p[tx][4 * ty + e] = p0;
+      sm.p[tx + 16][4 * ty + e] = p1;
+#pragma unroll
+      for (int c = 0; c < 4 * CV; ++c) acc[e][c] *= alpha;
+    }
+    __syncwarp();                                                  // P of a row group stays within its 16 lanes
+    if (!sm.odd) {
+#pragma unroll 4
+      for (int jj = 0; jj < kKeyTile; ++jj) {
+        const float4 w = *reinterpret_cast<const float4*>(&sm.p[jj][4 * ty]);
+#pragma unroll
+        for (int cv = 0; cv < CV; ++cv) {
+          const float4 x = *reinterpret_cast<const float4*>(&sm.v[jj][64 * cv + 4 * tx]);
+          const float we[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            acc[e][4 * cv] = fmaf(we[e], x.x, acc[e][4 * cv]);
+            acc[e][4 * cv + 1] = fmaf(we[e], x.y, acc[e][4 * cv + 1]);
+            acc[e][4 * cv + 2] = fmaf(we[e], x.z, acc[e][4 * cv + 2]);
+            acc[e][4 * cv + 3] = fmaf(we[e], x.w, acc[e][4 * cv + 3]);
+          }
+        }
+      }
+    } else {
+      // a node's V row holds an infinity or a NaN: it must not reach the rows that do not see the node (0 x inf)
+      for (int jj = 0; jj < kKeyTile; ++jj) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t see = __shfl_sync(0xffffffffu, vis, (tid & 16) + (jj & 15)) >> (2 * e + (jj >> 4)) & 1u;
+          if (!see) continue;
+          const float w = sm.p[jj][4 * ty + e];
+#pragma unroll
+          for (int cv = 0; cv < CV; ++cv)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) acc[e][4 * cv + c] = fmaf(w, sm.v[jj][64 * cv + 4 * tx + c], acc[e][4 * cv + c]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) lsum[e] += __shfl_xor_sync(0xffffffffu, lsum[e], o);
+    const int r = r0 + 4 * ty + e;
+    const int64_t pit = (part0 + r) * p.n_split + split;
+    if (node[e] < 0) {
+      if (p.n_split > 1 && r < rows && tx == 0) p.part_ml[pit] = kNoPart;
+      continue;
+    }
+    if (p.n_split == 1) {
+      const float inv = lsum[e] == 0.f ? 0.f : 1.f / lsum[e];     // a NaN stays one
+#pragma unroll
+      for (int cv = 0; cv < CV; ++cv)
+        store_out4(p, (row0 + r) * D + 64 * cv + 4 * tx, make_float4(acc[e][4 * cv] * inv, acc[e][4 * cv + 1] * inv,
+                                                                     acc[e][4 * cv + 2] * inv, acc[e][4 * cv + 3] * inv));
+    } else {
+      if (tx == 0) p.part_ml[pit] = make_float2(m[e], lsum[e]);
+#pragma unroll
+      for (int cv = 0; cv < CV; ++cv)
+        *reinterpret_cast<float4*>(p.part_o + pit * D + 64 * cv + 4 * tx) =
+            make_float4(acc[e][4 * cv], acc[e][4 * cv + 1], acc[e][4 * cv + 2], acc[e][4 * cv + 3]);
+    }
+  }
+}
+
+// Joins the splits of a query row: d / 4 threads per row, four channels each.
+__global__ void __launch_bounds__(128) tree_combine_kernel(TreeAttnParams p) {
+  ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
+  const int per_row = p.d / 4;
+  const int64_t row = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) / per_row;      // (lr, b, hq, node)
+  const int c = 4 * (int)(((int64_t)blockIdx.x * blockDim.x + threadIdx.x) % per_row);
+  const int64_t per_layer = (int64_t)p.B * p.Hq * p.N;
+  if (row >= p.n_layers * per_layer) return;
+  if (p.part_ml[row * p.n_split].y < 0.f) return;                  // kNoPart
+  float mg = -INFINITY;
+  for (int s = 0; s < p.n_split; ++s) mg = fmaxf(mg, p.part_ml[row * p.n_split + s].x);
+  float ls = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s = 0; s < p.n_split; ++s) {
+    const float2 ml = p.part_ml[row * p.n_split + s];
+    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - mg);
+    const float4 x = *reinterpret_cast<const float4*>(p.part_o + (row * p.n_split + s) * p.d + c);
+    o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
+    ls = fmaf(ml.y, f, ls);
+  }
+  const float inv = ls == 0.f ? 0.f : 1.f / ls;
+  store_out4(p, ((int64_t)p.layer_begin * per_layer + row) * p.d + c, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+}
+
+// Rows per item: small blocks keep the arithmetic near the rows there are.
+int fma_rows(const ngc_cache* c, int N) { return c->Hq / c->Hkv * N <= 16 ? 16 : 64; }
+
+template <typename T, int D> cudaError_t launch_fma(const TreeAttnParams& p, int rb, unsigned grid, cudaStream_t stream) {
+  if (rb == 16) return launch_pdl(tree_fma_kernel<T, D, 16>, dim3(grid), dim3(64), sizeof(FmaSmem<D, 16>), stream, p);
+  return launch_pdl(tree_fma_kernel<T, D, 64>, dim3(grid), dim3(256), sizeof(FmaSmem<D, 64>), stream, p);
+}
+template <typename T, int D> cudaError_t opt_in_fma() {
+  cudaError_t e = cudaFuncSetAttribute(tree_fma_kernel<T, D, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(FmaSmem<D, 16>));
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(tree_fma_kernel<T, D, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(FmaSmem<D, 64>));
+  return e;
+}
+
+constexpr int kTargetCtas = 148 * 2 * 2;
+
+// Row blocks per KV head and token splits of a call over `layers` layers.
+int tree_plan(const ngc_cache* c, int layers, int N, int* n_split) {
+  const int rows = c->Hq / c->Hkv * N, rb = fma_rows(c, N), blocks = (rows + rb - 1) / rb;
+  const int64_t items = (int64_t)layers * c->B * c->Hkv * blocks;
+  int64_t ns = (kTargetCtas + items - 1) / items;
+  const int64_t by_len = ((int64_t)c->max_len + N + kSplitMin * kKeyTile - 1) / (kSplitMin * kKeyTile);
+  if (ns > by_len) ns = by_len;
+  if (ns > 64) ns = 64;
+  *n_split = ns < 1 ? 1 : (int)ns;
+  return blocks;
+}
+
+size_t tree_call_scratch_bytes(const ngc_cache* c, int layers, int N, size_t* ml_offset) {
+  int ns = 1;
+  tree_plan(c, layers, N, &ns);
+  *ml_offset = 0;
+  if (ns <= 1) return 0;
+  const size_t parts = (size_t)layers * c->B * c->Hq * N * ns;
+  *ml_offset = align256(parts * c->d * 4);
+  return *ml_offset + align256(parts * 8);
+}
+
+int tree_impl(const ngc_cache* c, const PagedView& pv, const void* q, const void* tree_k, const void* tree_v, const int32_t* parent,
+              const int32_t* n_nodes, int N, int layer_begin, int layer_end, float scale, void* out, int out_dtype,
+              void* ws, size_t ws_bytes, int32_t* dev_status, cudaStream_t stream) {
+  if (!q || !tree_k || !tree_v || !parent || !out || N < 1 || layer_begin < 0 || layer_end > c->L || layer_begin >= layer_end)
+    return NGC_ERR_INVALID_ARG;
+  if (!(scale > 0.f) || scale > 3.0e38f) return NGC_ERR_INVALID_ARG;
+  if ((((uintptr_t)q | (uintptr_t)tree_k | (uintptr_t)tree_v | (uintptr_t)out | (uintptr_t)c->k | (uintptr_t)c->v) & 15) != 0)
+    return NGC_ERR_INVALID_ARG;      // rows are moved as 16-byte vectors
+  if (out_dtype != NGC_F32 && !(out_dtype == NGC_BF16 && c->dtype == NGC_BF16)) return NGC_ERR_INVALID_ARG;
+  if (N > kTreeMaxNodes) return NGC_ERR_UNSUPPORTED;
+  if (pv.table && (c->dtype != NGC_BF16 || c->d != 128)) return NGC_ERR_UNSUPPORTED;
+
+  TreeAttnParams p;
+  p.k = c->k; p.v = c->v; p.seq_off = c->seq_off; p.lens = c->lens;
+  p.q = q; p.tree_k = tree_k; p.tree_v = tree_v; p.parent = parent; p.n_nodes = n_nodes; p.out = out;
+  p.part_o = nullptr; p.part_ml = nullptr; p.dev_status = dev_status; p.rows = c->rows;
+  p.L = c->L; p.B = c->B; p.Hq = c->Hq; p.Hkv = c->Hkv; p.d = c->d; p.g = c->Hq / c->Hkv; p.N = N;
+  p.layer_begin = layer_begin; p.n_layers = layer_end - layer_begin;
+  p.out_bf16 = out_dtype == NGC_BF16; p.scale_log2 = scale * 1.4426950408889634f;
+  p.page_table = pv.table; p.page = pv.page; p.pages_cap = pv.pages_cap; p.lists = pv.lists;
+  p.G = lists_G(pv.lists, c->L, c->Hkv); p.lens_lists = c->lens_lists;
+  p.row_blocks = tree_plan(c, p.n_layers, N, &p.n_split);
+  if (p.n_split > 1) {
+    size_t ml_offset = 0;
+    const size_t need = tree_call_scratch_bytes(c, p.n_layers, N, &ml_offset);
+    if (!ws || ws_bytes < need || ((uintptr_t)ws & 255)) return NGC_ERR_WORKSPACE;
+    p.part_o = (float*)ws;
+    p.part_ml = (float2*)((char*)ws + ml_offset);
+  }
+  const int64_t items = (int64_t)p.n_layers * c->B * c->Hkv * p.row_blocks * p.n_split;
+  const int64_t out_threads = (int64_t)p.n_layers * c->B * c->Hq * N * (c->d / 4);
+  if (items > 0x7fffffffLL || out_threads / 128 > 0x7ffffff0LL) return NGC_ERR_UNSUPPORTED;
+
+  static PerDeviceOnce attr_once;
+  const int rc = attr_once.run([] {
+    cudaError_t e = opt_in_fma<float, 64>();
+    if (e == cudaSuccess) e = opt_in_fma<float, 128>();
+    if (e == cudaSuccess) e = opt_in_fma<__nv_bfloat16, 64>();
+    if (e == cudaSuccess) e = opt_in_fma<__nv_bfloat16, 128>();
+    return e;
+  });
+  if (rc != NGC_OK) return rc;
+  const int rb = fma_rows(c, N);
+  const unsigned grid = (unsigned)items;
+  if (c->dtype == NGC_F32 && c->d == 64) NGC_CUDA_TRY((launch_fma<float, 64>(p, rb, grid, stream)));
+  else if (c->dtype == NGC_F32) NGC_CUDA_TRY((launch_fma<float, 128>(p, rb, grid, stream)));
+  else if (c->d == 64) NGC_CUDA_TRY((launch_fma<__nv_bfloat16, 64>(p, rb, grid, stream)));
+  else NGC_CUDA_TRY((launch_fma<__nv_bfloat16, 128>(p, rb, grid, stream)));
+  if (p.n_split > 1)
+    NGC_CUDA_TRY(launch_pdl(tree_combine_kernel, dim3((unsigned)((out_threads + 127) / 128)), dim3(128), 0, stream, p));
+  return NGC_OK;
+}
+
+}  // namespace
+
+// Workspace that serves a call over any layer range.
+size_t tree_workspace_bytes(const ngc_cache* c, int N) {
+  if (N < 1 || N > kTreeMaxNodes) return 0;
+  size_t worst = 0, ml_offset;
+  for (int layers = 1; layers <= c->L; ++layers) {
+    const size_t bytes = tree_call_scratch_bytes(c, layers, N, &ml_offset);
+    if (bytes > worst) worst = bytes;
+  }
+  return worst;
+}
+
+}  // namespace ngc
+
+extern "C" int ngc_tree_attn_launches(const ngc_cache* c, int layers, int N) {
+  using namespace ngc;
+  if (!valid_cache(c) || layers < 1 || N < 1 || N > kTreeMaxNodes) return 0;
+  int ns = 1;
+  tree_plan(c, layers, N, &ns);
+  return ns > 1 ? 2 : 1;
+}
+
+extern "C" int ngc_tree_attn(const ngc_cache* c, const void* q, const void* tree_k, const void* tree_v, const int32_t* parent,
+                             const int32_t* n_nodes, int N, int layer_begin, int layer_end, float scale, void* out, int out_dtype,
+                             void* ws, size_t ws_bytes, int32_t* dev_status, ngc_stream stream) {
+  NGC_API_RANGE("ngc_tree_attn");
+  using namespace ngc;
+  if (!valid_cache(c)) return NGC_ERR_INVALID_ARG;
+  const PagedView none = {nullptr, 0, 0, NGC_LISTS_SHARED};
+  return tree_impl(c, none, q, tree_k, tree_v, parent, n_nodes, N, layer_begin, layer_end, scale, out, out_dtype, ws, ws_bytes,
+                   dev_status, (cudaStream_t)stream);
+}
+
+extern "C" int ngc_tree_attn_paged(const ngc_paged_cache* pc, const void* q, const void* tree_k, const void* tree_v,
+                                   const int32_t* parent, const int32_t* n_nodes, int N, int layer_begin, int layer_end, float scale,
+                                   void* out, int out_dtype, void* ws, size_t ws_bytes, int32_t* dev_status, ngc_stream stream) {
+  NGC_API_RANGE("ngc_tree_attn_paged");
+  using namespace ngc;
+  ngc_cache c;
+  if (!paged_as_cache(pc, &c)) return NGC_ERR_INVALID_ARG;
+  const PagedView pv = {pc->page_table, pc->page, pc->pages_cap, pc->lists};
+  return tree_impl(&c, pv, q, tree_k, tree_v, parent, n_nodes, N, layer_begin, layer_end, scale, out, out_dtype, ws, ws_bytes,
+                   dev_status, (cudaStream_t)stream);
+}

@@ -1,0 +1,99 @@
+// Launch parameters and device helpers shared by the paths of ngc_tree_attn.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "ngc_common.cuh"
+#include "ptx.cuh"
+
+namespace ngc {
+
+struct TreeAttnParams {
+  const void* k;                // [L][Hkv][rows][d]
+  const void* v;
+  const int64_t* seq_off;       // contiguous caches only
+  const int32_t* lens;
+  const void* q;                // [L][B][Hq][N][d]
+  const void* tree_k;           // [L][B][Hkv][N][d]
+  const void* tree_v;
+  const int32_t* parent;        // [B][N]
+  const int32_t* n_nodes;       // [B] or null
+  void* out;                    // [L][B][Hq][N][d]
+  float* part_o;                // [n_layers][B][Hq][N][n_split][d]
+  float2* part_ml;              // [n_layers][B][Hq][N][n_split]   (m in log2 units, l)
+  int32_t* dev_status;
+  int64_t rows;
+  int L, B, Hq, Hkv, d, g, N;
+  int layer_begin, n_layers, n_split, row_blocks, out_bf16;
+  float scale_log2;             // scale * log2(e)
+  const int32_t* page_table;    // [B][G][pages_cap] or null
+  int page, pages_cap, lists, G;
+  int lens_lists;
+};
+
+constexpr int kTreeMaxNodes = NGC_TREE_MAX_NODES;
+constexpr int kTreeWords = kTreeMaxNodes / 32;
+
+// Row capacity of sequence b.
+__device__ __forceinline__ int64_t tree_capacity(const TreeAttnParams& p, int b) {
+  return p.page_table ? (int64_t)p.pages_cap * p.page : p.seq_off[b + 1] - p.seq_off[b];
+}
+
+// Ancestor-or-self sets of a tree as bit masks, by pointer doubling: in every round a node takes over the set of the
+// node its jump link points at and jumps as far again, so a tree of depth D needs ceil(log2 D) rounds.  Called by all
+// NT threads of the CTA; `anc` [n][kTreeWords] and `jump` [n] are shared memory.  Returns (to every thread) false for
+// a node count or a link that is none; nothing may be read from anc then.
+template <int NT>
+__device__ __forceinline__ bool tree_masks(const int32_t* parent, int n, int N, uint32_t (*anc)[kTreeWords], int* jump) {
+  constexpr int kPer = (kTreeMaxNodes + NT - 1) / NT;         // nodes per thread
+  const int tid = threadIdx.x;
+  bool bad = n < 0 || n > N;
+  if (bad) n = 0;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    const int i = tid + e * NT;
+    if (i < n) {
+      const int pa = parent[i];
+      const bool wrong = i == 0 ? pa != -1 : (pa < 0 || pa >= i);
+      bad = bad || wrong;
+      jump[i] = wrong ? -1 : pa;
+#pragma unroll
+      for (int w = 0; w < kTreeWords; ++w) anc[i][w] = (i >> 5) == w ? 1u << (i & 31) : 0u;
+    }
+  }
+  if (__syncthreads_or(bad)) return false;
+  for (;;) {
+    uint32_t m[kPer][kTreeWords];
+    int nj[kPer];
+    bool more = false;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      const int i = tid + e * NT;
+      nj[e] = -1;
+#pragma unroll
+      for (int w = 0; w < kTreeWords; ++w) m[e][w] = 0;
+      if (i < n && jump[i] >= 0) {
+        const int j = jump[i];
+        nj[e] = jump[j];
+        more = true;
+#pragma unroll
+        for (int w = 0; w < kTreeWords; ++w) m[e][w] = anc[j][w];
+      }
+    }
+    if (!__syncthreads_or(more)) return true;                  // (also: every read of this round is done)
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      const int i = tid + e * NT;
+      if (i < n) {
+        jump[i] = nj[e];
+#pragma unroll
+        for (int w = 0; w < kTreeWords; ++w) anc[i][w] |= m[e][w];
+      }
+    }
+    __syncthreads();
+  }
+}
+
+}  // namespace ngc

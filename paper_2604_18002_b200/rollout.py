@@ -52,6 +52,7 @@ class NgcRollout:
         self.ws_sample = ngc.alloc_workspace(ngc.workspace_bytes(ngc.OP_SAMPLE, None, self.G, n_max, k_max, B=B), device)
         self.ws_score = ngc.alloc_workspace(ngc.workspace_bytes(ngc.OP_SCORE, self.cache, self.G, n_max), device) \
             if with_score else None
+        self.ws_tree = {}          # nodes per tree -> workspace of draft_attention
         self.launches = 0          # kernels enqueued so far (bookkeeping for the benchmark)
 
     # ---- one eviction round: score -> sample -> log-prob -> compact ----------------
@@ -95,6 +96,33 @@ class NgcRollout:
             for s in range(q.shape[0]):
                 self.decode_step(q[s], out[s], new_k[s], new_v[s])
         return graph
+
+    # ---- drafted tokens: several tokens of a rollout per pass over the cache ---------
+    def fork(self, src_of: torch.Tensor):
+        """Sequence b becomes a copy of sequence ``src_of[b]`` (int32 [B]; -1: left alone): the rollouts of one prompt
+        start from a single prefill."""
+        ngc.ngc_fork_kv(self.cache, src_of, status=self.status)
+        self.launches += 1
+
+    def draft_attention(self, q: torch.Tensor, tree_k: torch.Tensor, tree_v: torch.Tensor, parent: torch.Tensor, out: torch.Tensor,
+                        n_nodes: Optional[torch.Tensor] = None, layer_begin: int = 0, layer_end: Optional[int] = None):
+        """Attention of every node of the drafted trees over the cache, its ancestors and itself; the cache is not changed."""
+        N = parent.shape[1]
+        if N not in self.ws_tree:
+            self.ws_tree[N] = ngc.alloc_workspace(ngc.workspace_bytes(ngc.OP_TREE_ATTN, self.cache, n_max=N), self.device)
+        ngc.ngc_tree_attn(self.cache, q, tree_k, tree_v, parent, out, n_nodes, layer_begin, layer_end, ws=self.ws_tree[N],
+                          status=self.status)
+        self.launches += ngc.tree_attn_launches(self.cache, N, (self.L if layer_end is None else layer_end) - layer_begin)
+
+    def accept_draft(self, tokens: torch.Tensor, parent: torch.Tensor, target_probs: torch.Tensor, uniforms: Optional[torch.Tensor],
+                     tree_k: torch.Tensor, tree_v: torch.Tensor, path: torch.Tensor, n_path: torch.Tensor, next_token: torch.Tensor,
+                     draft_probs: Optional[torch.Tensor] = None, n_nodes: Optional[torch.Tensor] = None, greedy: int = 0):
+        """Verifies the drafted trees and appends the accepted nodes' K/V rows to the cache; ``next_token`` is the pending
+        token (node 0) of the next draft."""
+        ngc.ngc_verify_draft(tokens, parent, target_probs, uniforms, path, n_path, next_token, draft_probs, n_nodes, greedy,
+                             status=self.status)
+        ngc.ngc_commit_draft(self.cache, tree_k, tree_v, path, n_path, status=self.status)
+        self.launches += 3
 
     def check_status(self):
         code = int(self.status.item())
