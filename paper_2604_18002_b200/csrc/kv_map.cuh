@@ -27,27 +27,27 @@ inline EncodeTiledFn encode_tiled_fn() {
   return fn;
 }
 
-// K or V of a bf16, d = 128 cache as a 3-D tensor (channel, row in plane, plane);
+// K or V of a bf16 cache with d = 128 (or 64) as a 3-D tensor (channel, row in plane, plane);
 // box = 64 channels x `box_rows` rows, 128-byte swizzle.  A row of 128 channels
 // is fetched as two boxes (x = 0 and x = 64).
-inline bool make_kv_map(CUtensorMap* map, void* base, int64_t rows, int planes, int box_rows) {
+inline bool make_kv_map(CUtensorMap* map, const void* base, int64_t rows, int planes, int box_rows, int d = 128) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (!fn) return false;
-  cuuint64_t dims[3] = {128, (cuuint64_t)rows, (cuuint64_t)planes};
-  cuuint64_t strides[2] = {256, (cuuint64_t)rows * 256};
+  cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)rows, (cuuint64_t)planes};
+  cuuint64_t strides[2] = {(cuuint64_t)d * 2, (cuuint64_t)rows * d * 2};
   cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};
   cuuint32_t estr[3] = {1, 1, 1};
-  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// A bf16 matrix of `rows` rows of 128 channels as a 2-D tensor (channel, row); box = 64 channels x `box_rows`
+// A bf16 matrix of `rows` rows of 128 (or d = 64) channels as a 2-D tensor (channel, row); box = 64 channels x `box_rows`
 // rows, 128-byte swizzle.  box_rows = 1 is the shape the TMA row gather (tile::gather4) takes.
-inline bool make_rows_map(CUtensorMap* map, const void* base, int64_t rows, int box_rows) {
+inline bool make_rows_map(CUtensorMap* map, const void* base, int64_t rows, int box_rows, int d = 128) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (!fn || rows <= 0 || rows > 0x7fffffffLL) return false;
-  cuuint64_t dims[2] = {128, (cuuint64_t)rows};
-  cuuint64_t strides[1] = {256};
+  cuuint64_t dims[2] = {(cuuint64_t)d, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)d * 2};
   cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
   cuuint32_t estr[2] = {1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,

@@ -91,70 +91,22 @@ struct Shared {
   Plan plan[kPlanSlots];
 };
 
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
-// two floats in one 64-bit register for the packed fp32 instructions (fma / add on both halves at once)
-__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-
-// Bounded wait that also gives up as soon as another thread of the CTA has given up.
+// Bounded waits of one thread / of a whole warp (every lane gets the same answer).
 __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, Shared* sh, int32_t* dev_status) {
-  if (ptx::mbar_try_wait(bar, parity)) return true;
-  const uint64_t t0 = ptx::globaltimer_ns();
-  for (uint32_t spins = 0;; ++spins) {
-    if (ptx::mbar_try_wait(bar, parity)) return true;
-    if ((spins & 63u) == 63u) {
-      if (*(volatile int*)&sh->abort) return false;
-      if (ptx::globaltimer_ns() - t0 > ptx::kWaitLimitNs) {
-        *(volatile int*)&sh->abort = 1;
-        set_dev_status(dev_status, NGC_DEV_TIMEOUT);
-        return false;
-      }
-    }
-  }
+  return umma::wait_or_abort(bar, parity, &sh->abort, dev_status);
 }
-// The same for a whole warp: every lane gets the same answer.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, Shared* sh, int32_t* dev_status) {
-  return __all_sync(0xffffffffu, wait_or_abort(bar, parity, sh, dev_status));
+  return umma::warp_wait(bar, parity, &sh->abort, dev_status);
 }
 
 // Tensor maps of a launch: Q as a 2-D tensor (channel, row over all layers / sequences / heads), box = 64 channels x
 // 128 rows; the output over the same rows, box = 32 channels x 32 rows (one warp's chunk).
 struct Maps { CUtensorMap q, out; };
 
-__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, int x, int y, const void* src) {
-  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
-               ::"l"(map), "r"(x), "r"(y), "r"(ptx::smem_u32(src))
-               : "memory");
-}
-
 // swizzled byte offset of 16-byte piece c (0..15) of key row r inside a K or V tile
 __device__ __forceinline__ uint32_t tile_off(int r, int c) {
   return (uint32_t)((c >> 3) * kKBox + r * 128 + (((c & 7) ^ (r & 7)) << 4));
 }
-__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
-  asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-               ::"r"(ptx::smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(ptx::smem_u32(bar))
-               : "memory");
-}
-
 __global__ void __launch_bounds__(kThreads, 1)
 replay_attn_umma_kernel(const __grid_constant__ Maps maps, ReplayAttnParams p, int n_items) {
   extern __shared__ uint8_t smem_dyn[];
@@ -288,8 +240,8 @@ replay_attn_umma_kernel(const __grid_constant__ Maps maps, ReplayAttnParams p, i
         ptx::mbar_expect_tx(&sh.q_full, (uint32_t)(n_heads * kQBytes));
         for (int hh = 0; hh < n_heads; ++hh) {
           const int y = (int)((((int64_t)l * p.B + b) * p.Hq + hq0 + hh) * (int64_t)p.t_max + q0);
-          tma_load_2d(sQ + hh * kQBytes, &maps.q, 0, y, &sh.q_full);
-          tma_load_2d(sQ + hh * kQBytes + kQHalf, &maps.q, 64, y, &sh.q_full);
+          ptx::tma_load_2d(sQ + hh * kQBytes, &maps.q, 0, y, &sh.q_full);
+          ptx::tma_load_2d(sQ + hh * kQBytes + kQHalf, &maps.q, 64, y, &sh.q_full);
         }
       }
       __syncwarp();
@@ -500,7 +452,7 @@ replay_attn_umma_kernel(const __grid_constant__ Maps maps, ReplayAttnParams p, i
             for (int j = 0; j < 32; j += 8) {
 #pragma unroll
               for (int c = 0; c < 4; ++c)
-                mxc[c] = max3(mxc[c], __uint_as_float(zr[half][j + 2 * c]), __uint_as_float(zr[half][j + 2 * c + 1]));
+                mxc[c] = umma::max3(mxc[c], __uint_as_float(zr[half][j + 2 * c]), __uint_as_float(zr[half][j + 2 * c + 1]));
             }
           const float mx = fmaxf(fmaxf(mxc[0], mxc[1]), fmaxf(mxc[2], mxc[3])) * p.scale_log2;
           // the maximum used for the exponentials follows the true one lazily
@@ -529,7 +481,7 @@ replay_attn_umma_kernel(const __grid_constant__ Maps maps, ReplayAttnParams p, i
           const float m_eff = m_use == -INFINITY ? 0.f : m_use;               // nothing visible yet: every exponential is 0
           // p = 2^(z * scale - m): one packed fused multiply-add per pair of scores, then the exponentials; the row sum
           // in four independent packed chains
-          const uint64_t sc2 = pack2(p.scale_log2, p.scale_log2), nm2 = pack2(-m_eff, -m_eff);
+          const uint64_t sc2 = umma::pack2(p.scale_log2, p.scale_log2), nm2 = umma::pack2(-m_eff, -m_eff);
           uint64_t acc2[4] = {0ull, 0ull, 0ull, 0ull};
           uint32_t pk[32];
 #pragma unroll
@@ -537,14 +489,14 @@ replay_attn_umma_kernel(const __grid_constant__ Maps maps, ReplayAttnParams p, i
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {
               float x0, x1;
-              unpack2(fma2(pack2(__uint_as_float(zr[half][j]), __uint_as_float(zr[half][j + 1])), sc2, nm2), x0, x1);
+              umma::unpack2(umma::fma2(umma::pack2(__uint_as_float(zr[half][j]), __uint_as_float(zr[half][j + 1])), sc2, nm2), x0, x1);
               const float p0 = ptx::ex2_approx(x0), p1 = ptx::ex2_approx(x1);
-              acc2[(j >> 1) & 3] = add2(acc2[(j >> 1) & 3], pack2(p0, p1));
+              acc2[(j >> 1) & 3] = umma::add2(acc2[(j >> 1) & 3], umma::pack2(p0, p1));
               pk[16 * half + (j >> 1)] = ptx::pack_bf16x2(p0, p1);
             }
           {
             float s0, s1;
-            unpack2(add2(add2(acc2[0], acc2[1]), add2(acc2[2], acc2[3])), s0, s1);
+            umma::unpack2(umma::add2(umma::add2(acc2[0], acc2[1]), umma::add2(acc2[2], acc2[3])), s0, s1);
             l_run += s0 + s1;
           }
           // P over the first 32 columns of the S buffer this row was just read from (free: the row is in registers)
@@ -597,7 +549,7 @@ replay_attn_umma_kernel(const __grid_constant__ Maps maps, ReplayAttnParams p, i
             ptx::fence_proxy_async();
             __syncwarp();
             if (lane == 0) {
-              tma_store_2d(&maps.out, c0, (int)(o_row0 >> 7), so);
+              ptx::tma_store_2d(&maps.out, c0, (int)(o_row0 >> 7), so);
               ptx::bulk_commit();
             }
           } else if (p.out_bf16) {

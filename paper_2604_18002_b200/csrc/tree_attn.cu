@@ -6,6 +6,7 @@
 // first, then the nodes; a row's mask only matters in the node part, where it is a bit of the node's
 // ancestor set.
 //
+// bf16 caches run on the tensor cores (tree_attn_umma.cu); fp32 caches on the
 // FMA path (this file): tiles of 32 keys in shared memory as fp32, 4 rows x 2 keys of S and 4 rows x
 // 8 channels (d = 128) of O per thread, online softmax with the row statistics spread over 16 lanes.
 // One pass over K and V; with few items the key axis is split and a combine kernel joins the parts.
@@ -20,15 +21,7 @@ namespace {
 constexpr int kKeyTile = 32;                    // keys per tile, and the split granularity
 constexpr int kSplitMin = 8;                    // tiles a split has at least
 
-// (m, l) of a row that is not computed (a node beyond the tree, a refused sequence): the combine kernel leaves it alone.
-#define kNoPart make_float2(0.f, -1.f)
-
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
-  const uint2 t = *reinterpret_cast<const uint2*>(p);
-  const __nv_bfloat162 a = *reinterpret_cast<const __nv_bfloat162*>(&t.x), c = *reinterpret_cast<const __nv_bfloat162*>(&t.y);
-  return make_float4(__low2float(a), __high2float(a), __low2float(c), __high2float(c));
-}
 __device__ __forceinline__ bool finite4(float4 x) {
   return isfinite(x.x) && isfinite(x.y) && isfinite(x.z) && isfinite(x.w);
 }
@@ -48,7 +41,7 @@ template <int D, int RB> struct FmaSmem {
 };
 
 // RB rows per item, 4 * RB threads: thread (ty, tx) of 16 lanes per row group owns rows 4 ty .. 4 ty + 3.
-template <typename T, int D, int RB>
+template <int D, int RB>
 __global__ void __launch_bounds__(4 * RB) tree_fma_kernel(TreeAttnParams p) {
   constexpr int NT = 4 * RB, CV = D / 64;       // CV float4 groups of channels per thread
   extern __shared__ __align__(16) uint8_t smem_raw[];
@@ -80,17 +73,17 @@ __global__ void __launch_bounds__(4 * RB) tree_fma_kernel(TreeAttnParams p) {
   const int tile_lo = min(nt, split * tps), tile_hi = min(nt, tile_lo + tps);
   const int plane = l * p.Hkv + h;
   const int32_t* table = p.page_table ? p.page_table + ((int64_t)b * p.G + list_of(p.lists, l, h, p.Hkv)) * p.pages_cap : nullptr;
-  const T* const kc = (const T*)p.k + (int64_t)plane * p.rows * D;
-  const T* const vc = (const T*)p.v + (int64_t)plane * p.rows * D;
+  const float* const kc = (const float*)p.k + (int64_t)plane * p.rows * D;
+  const float* const vc = (const float*)p.v + (int64_t)plane * p.rows * D;
   const int64_t base = p.page_table ? (int64_t)b * p.pages_cap * p.page : p.seq_off[b];
   const int64_t strip = ((int64_t)l * p.B + b) * p.Hkv + h;
-  const T* const kt = (const T*)p.tree_k + strip * p.N * D;
-  const T* const vt = (const T*)p.tree_v + strip * p.N * D;
+  const float* const kt = (const float*)p.tree_k + strip * p.N * D;
+  const float* const vt = (const float*)p.tree_v + strip * p.N * D;
   const int64_t row0 = (((int64_t)l * p.B + b) * p.Hq + (int64_t)h * p.g) * p.N;       // first query row of the KV head
 
   for (int i = tid; i < RB * (D / 4); i += NT) {
     const int r = i / (D / 4), c = 4 * (i % (D / 4));
-    const float4 x = r0 + r < rows ? load4((const T*)p.q + (row0 + r0 + r) * D + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    const float4 x = r0 + r < rows ? load4((const float*)p.q + (row0 + r0 + r) * D + c) : make_float4(0.f, 0.f, 0.f, 0.f);
     *reinterpret_cast<float4*>(&sm.q[r][c]) = x;
   }
   int node[4];
@@ -245,7 +238,8 @@ __global__ void __launch_bounds__(128) tree_combine_kernel(TreeAttnParams p) {
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int s = 0; s < p.n_split; ++s) {
     const float2 ml = p.part_ml[row * p.n_split + s];
-    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - mg);
+    if (ml.x == -INFINITY) continue;                               // nothing visible in this part (it may hold no sums)
+    const float f = exp2f(ml.x - mg);
     const float4 x = *reinterpret_cast<const float4*>(p.part_o + (row * p.n_split + s) * p.d + c);
     o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
     ls = fmaf(ml.y, f, ls);
@@ -254,37 +248,44 @@ __global__ void __launch_bounds__(128) tree_combine_kernel(TreeAttnParams p) {
   store_out4(p, ((int64_t)p.layer_begin * per_layer + row) * p.d + c, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
 }
 
-// Rows per item: small blocks keep the arithmetic near the rows there are.
-int fma_rows(const ngc_cache* c, int N) { return c->Hq / c->Hkv * N <= 16 ? 16 : 64; }
-
-template <typename T, int D> cudaError_t launch_fma(const TreeAttnParams& p, int rb, unsigned grid, cudaStream_t stream) {
-  if (rb == 16) return launch_pdl(tree_fma_kernel<T, D, 16>, dim3(grid), dim3(64), sizeof(FmaSmem<D, 16>), stream, p);
-  return launch_pdl(tree_fma_kernel<T, D, 64>, dim3(grid), dim3(256), sizeof(FmaSmem<D, 64>), stream, p);
+template <int D> cudaError_t launch_fma(const TreeAttnParams& p, int rb, unsigned grid, cudaStream_t stream) {
+  if (rb == 16) return launch_pdl(tree_fma_kernel<D, 16>, dim3(grid), dim3(64), sizeof(FmaSmem<D, 16>), stream, p);
+  return launch_pdl(tree_fma_kernel<D, 64>, dim3(grid), dim3(256), sizeof(FmaSmem<D, 64>), stream, p);
 }
-template <typename T, int D> cudaError_t opt_in_fma() {
-  cudaError_t e = cudaFuncSetAttribute(tree_fma_kernel<T, D, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(FmaSmem<D, 16>));
+template <int D> cudaError_t opt_in_fma() {
+  cudaError_t e = cudaFuncSetAttribute(tree_fma_kernel<D, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(FmaSmem<D, 16>));
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(tree_fma_kernel<T, D, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(FmaSmem<D, 64>));
+    e = cudaFuncSetAttribute(tree_fma_kernel<D, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(FmaSmem<D, 64>));
   return e;
 }
 
-constexpr int kTargetCtas = 148 * 2 * 2;
-
-// Row blocks per KV head and token splits of a call over `layers` layers.
-int tree_plan(const ngc_cache* c, int layers, int N, int* n_split) {
-  const int rows = c->Hq / c->Hkv * N, rb = fma_rows(c, N), blocks = (rows + rb - 1) / rb;
-  const int64_t items = (int64_t)layers * c->B * c->Hkv * blocks;
-  int64_t ns = (kTargetCtas + items - 1) / items;
-  const int64_t by_len = ((int64_t)c->max_len + N + kSplitMin * kKeyTile - 1) / (kSplitMin * kKeyTile);
+// Rows per item, row blocks per KV head and token splits of a call over `layers` layers.
+struct TreePlan { int block_rows, blocks, n_split; };
+TreePlan tree_plan(const ngc_cache* c, int layers, int N) {
+  const int rows = c->Hq / c->Hkv * N;
+  TreePlan pl;
+  int target, split_keys;                       // CTAs worth having, keys a split has at least
+  if (c->dtype == NGC_BF16) {
+    pl.block_rows = 128 * tree_umma_tiles(rows);
+    target = rows <= 128 ? 148 * 2 * 2 : 148 * 2;
+    split_keys = 4 * 64;
+  } else {
+    pl.block_rows = rows <= 16 ? 16 : 64;       // small blocks keep the arithmetic near the rows there are
+    target = 148 * 2 * 2;
+    split_keys = kSplitMin * kKeyTile;
+  }
+  pl.blocks = (rows + pl.block_rows - 1) / pl.block_rows;
+  const int64_t items = (int64_t)layers * c->B * c->Hkv * pl.blocks;
+  int64_t ns = (target + items - 1) / items;
+  const int64_t by_len = ((int64_t)c->max_len + N + split_keys - 1) / split_keys;
   if (ns > by_len) ns = by_len;
   if (ns > 64) ns = 64;
-  *n_split = ns < 1 ? 1 : (int)ns;
-  return blocks;
+  pl.n_split = ns < 1 ? 1 : (int)ns;
+  return pl;
 }
 
 size_t tree_call_scratch_bytes(const ngc_cache* c, int layers, int N, size_t* ml_offset) {
-  int ns = 1;
-  tree_plan(c, layers, N, &ns);
+  const int ns = tree_plan(c, layers, N).n_split;
   *ml_offset = 0;
   if (ns <= 1) return 0;
   const size_t parts = (size_t)layers * c->B * c->Hq * N * ns;
@@ -313,7 +314,8 @@ int tree_impl(const ngc_cache* c, const PagedView& pv, const void* q, const void
   p.out_bf16 = out_dtype == NGC_BF16; p.scale_log2 = scale * 1.4426950408889634f;
   p.page_table = pv.table; p.page = pv.page; p.pages_cap = pv.pages_cap; p.lists = pv.lists;
   p.G = lists_G(pv.lists, c->L, c->Hkv); p.lens_lists = c->lens_lists;
-  p.row_blocks = tree_plan(c, p.n_layers, N, &p.n_split);
+  const TreePlan plan = tree_plan(c, p.n_layers, N);
+  p.row_blocks = plan.blocks; p.n_split = plan.n_split;
   if (p.n_split > 1) {
     size_t ml_offset = 0;
     const size_t need = tree_call_scratch_bytes(c, p.n_layers, N, &ml_offset);
@@ -325,21 +327,19 @@ int tree_impl(const ngc_cache* c, const PagedView& pv, const void* q, const void
   const int64_t out_threads = (int64_t)p.n_layers * c->B * c->Hq * N * (c->d / 4);
   if (items > 0x7fffffffLL || out_threads / 128 > 0x7ffffff0LL) return NGC_ERR_UNSUPPORTED;
 
-  static PerDeviceOnce attr_once;
-  const int rc = attr_once.run([] {
-    cudaError_t e = opt_in_fma<float, 64>();
-    if (e == cudaSuccess) e = opt_in_fma<float, 128>();
-    if (e == cudaSuccess) e = opt_in_fma<__nv_bfloat16, 64>();
-    if (e == cudaSuccess) e = opt_in_fma<__nv_bfloat16, 128>();
-    return e;
-  });
-  if (rc != NGC_OK) return rc;
-  const int rb = fma_rows(c, N);
-  const unsigned grid = (unsigned)items;
-  if (c->dtype == NGC_F32 && c->d == 64) NGC_CUDA_TRY((launch_fma<float, 64>(p, rb, grid, stream)));
-  else if (c->dtype == NGC_F32) NGC_CUDA_TRY((launch_fma<float, 128>(p, rb, grid, stream)));
-  else if (c->d == 64) NGC_CUDA_TRY((launch_fma<__nv_bfloat16, 64>(p, rb, grid, stream)));
-  else NGC_CUDA_TRY((launch_fma<__nv_bfloat16, 128>(p, rb, grid, stream)));
+  if (c->dtype == NGC_BF16) {
+    const int rc = launch_tree_umma(p, (unsigned)items, stream);
+    if (rc != NGC_OK) return rc;
+  } else {
+    static PerDeviceOnce attr_once;
+    const int rc = attr_once.run([] {
+      cudaError_t e = opt_in_fma<64>();
+      return e == cudaSuccess ? opt_in_fma<128>() : e;
+    });
+    if (rc != NGC_OK) return rc;
+    NGC_CUDA_TRY(c->d == 64 ? launch_fma<64>(p, plan.block_rows, (unsigned)items, stream)
+                            : launch_fma<128>(p, plan.block_rows, (unsigned)items, stream));
+  }
   if (p.n_split > 1)
     NGC_CUDA_TRY(launch_pdl(tree_combine_kernel, dim3((unsigned)((out_threads + 127) / 128)), dim3(128), 0, stream, p));
   return NGC_OK;
@@ -363,9 +363,7 @@ size_t tree_workspace_bytes(const ngc_cache* c, int N) {
 extern "C" int ngc_tree_attn_launches(const ngc_cache* c, int layers, int N) {
   using namespace ngc;
   if (!valid_cache(c) || layers < 1 || N < 1 || N > kTreeMaxNodes) return 0;
-  int ns = 1;
-  tree_plan(c, layers, N, &ns);
-  return ns > 1 ? 2 : 1;
+  return tree_plan(c, layers, N).n_split > 1 ? 2 : 1;
 }
 
 extern "C" int ngc_tree_attn(const ngc_cache* c, const void* q, const void* tree_k, const void* tree_v, const int32_t* parent,

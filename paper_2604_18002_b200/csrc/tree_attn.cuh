@@ -96,4 +96,12 @@ __device__ __forceinline__ bool tree_masks(const int32_t* parent, int n, int N, 
   }
 }
 
+// (m, l) of a row that is not computed (a node beyond the tree, a refused sequence): the combine kernel leaves it alone.
+#define kNoPart make_float2(0.f, -1.f)
+
+// Tensor-core path (bf16 caches, tree_attn_umma.cu): M tiles of 128 query rows per CTA for KV heads of `rows` rows.  One
+// tile per CTA lets two CTAs share an SM; more rows than that share their K and V tiles in pairs.
+inline int tree_umma_tiles(int rows) { return rows <= 128 ? 1 : 2; }
+int launch_tree_umma(const TreeAttnParams& p, unsigned grid, cudaStream_t stream);
+
 }  // namespace ngc

@@ -16,6 +16,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "ngc_common.cuh"
 #include "ptx.cuh"
 
 namespace ngc {
@@ -102,6 +103,51 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
                : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Arithmetic of the softmax warps.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// two floats in one 64-bit register for the packed fp32 instructions (fma / add on both halves at once)
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+// Bounded wait that also gives up as soon as another thread of the CTA has given up (*abort, in shared memory).
+__device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, int* abort, int32_t* dev_status) {
+  if (ptx::mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = ptx::globaltimer_ns();
+  for (uint32_t spins = 0;; ++spins) {
+    if (ptx::mbar_try_wait(bar, parity)) return true;
+    if ((spins & 63u) == 63u) {
+      if (*(volatile int*)abort) return false;
+      if (ptx::globaltimer_ns() - t0 > ptx::kWaitLimitNs) {
+        *(volatile int*)abort = 1;
+        set_dev_status(dev_status, NGC_DEV_TIMEOUT);
+        return false;
+      }
+    }
+  }
+}
+// The same for a whole warp: every lane gets the same answer.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int* abort, int32_t* dev_status) {
+  return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort, dev_status));
+}
 
 }  // namespace umma
 }  // namespace ngc

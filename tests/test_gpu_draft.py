@@ -34,7 +34,7 @@ def case(dtype, d, Hq, Hkv, L, lens, N, kind="tree", seed=0, capacity=None, n_no
     return c, q, tk, tv, trees(B, N, kind, seed), None if n_nodes is None else np.asarray(n_nodes, np.int32)
 
 
-def bound(c, q, tk, tv, parent, n_nodes, ref, lens_lists=0, out_bf16=False):
+def bound(c, q, tk, tv, parent, n_nodes, ref, lens_lists=0, out_bf16=False, scale=None):
     """How far a row may be off, element by element.  With weights w (sum 1) the output is sum w v.  A score is a dot
     product of d terms in fp32, so it is off by at most d 2^-24 sum |q k| scale =: ez, a weight by a factor
     1 + ez (+ 2^-22 of the exponential) above and below the line, hence 2 (ez + 2^-22) A in all, A = sum w |v|; the fp32
@@ -43,7 +43,7 @@ def bound(c, q, tk, tv, parent, n_nodes, ref, lens_lists=0, out_bf16=False):
     f = synth.as_f64
     args = (f(synth.to_numpy(c.k)), np.abs(f(synth.to_numpy(c.v))), c.seq_off.numpy(), c.lens.numpy(), f(synth.to_numpy(q)),
             f(synth.to_numpy(tk)), np.abs(f(synth.to_numpy(tv))), parent, n_nodes)
-    A = draft.tree_attn(*args, lens_lists=lens_lists)
+    A = draft.tree_attn(*args, scale=scale, lens_lists=lens_lists)         # (the weights are those of the call's own scale)
     L, B, Hq, N, d = q.shape
     aq, ak, at = np.abs(args[4]), np.abs(args[0]), np.abs(args[5])
     g, so, most = Hq // at.shape[2], args[2], 0.0
@@ -54,7 +54,7 @@ def bound(c, q, tk, tv, parent, n_nodes, ref, lens_lists=0, out_bf16=False):
                 T = min(max(0, draft.strip_len(args[3], lens_lists, b, l, h, at.shape[2])), int(so[b + 1] - so[b]))
                 for kk in (ak[l, h, so[b]:so[b] + T], at[l, b, h]):
                     most = max(most, float((rows @ kk.T).max()) if len(kk) else 0.0)
-    ez = d * 2.0 ** -24 * most / np.sqrt(d)
+    ez = d * 2.0 ** -24 * most * (1 / np.sqrt(d) if scale is None else scale)
     T = int(np.max(args[3])) + q.shape[3]
     b = (2 * (ez + 2.0 ** -22) + 2 * T * 2.0 ** -24 + (2.0 ** -8 if c.k.dtype == bf16 else 0)) * A + 1e-30
     return b + (2.0 ** -8 * np.abs(ref) if out_bf16 else 0)
@@ -79,7 +79,7 @@ def check_tree(c, q, tk, tv, parent, n_nodes, out_dtype=None, lens_lists=0, **kw
     n = [synth.to_numpy(x) for x in (q, tk, tv)]
     ref = draft.tree_attn(synth.to_numpy(c.k), synth.to_numpy(c.v), c.seq_off.numpy(), c.lens.numpy(), *n, parent, n_nodes,
                           lens_lists=lens_lists, fill=-7.0, scale=kw.get("scale"))
-    lim = bound(c, q, tk, tv, parent, n_nodes, ref, lens_lists, (out_dtype or f32) == bf16)
+    lim = bound(c, q, tk, tv, parent, n_nodes, ref, lens_lists, (out_dtype or f32) == bf16, kw.get("scale"))
     got = out.float().cpu().numpy().astype(np.float64)
     if n_nodes is not None:                       # rows of nodes that do not exist are left alone
         for bb, m in enumerate(n_nodes):
