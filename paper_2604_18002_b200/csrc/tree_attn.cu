@@ -25,13 +25,6 @@ __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_ca
 __device__ __forceinline__ bool finite4(float4 x) {
   return isfinite(x.x) && isfinite(x.y) && isfinite(x.z) && isfinite(x.w);
 }
-__device__ __forceinline__ void store_out4(const TreeAttnParams& p, int64_t idx, float4 v) {
-  if (p.out_bf16)
-    *reinterpret_cast<uint2*>((__nv_bfloat16*)p.out + idx) = make_uint2(ptx::pack_bf16x2(v.x, v.y), ptx::pack_bf16x2(v.z, v.w));
-  else
-    *reinterpret_cast<float4*>((float*)p.out + idx) = v;
-}
-
 template <int D, int RB> struct FmaSmem {
   float q[RB][D + 4], k[kKeyTile][D + 4], v[kKeyTile][D];
   float p[kKeyTile][RB + 4];
@@ -210,7 +203,7 @@ __global__ void __launch_bounds__(4 * RB) tree_fma_kernel(TreeAttnParams p) {
       const float inv = lsum[e] == 0.f ? 0.f : 1.f / lsum[e];     // a NaN stays one
 #pragma unroll
       for (int cv = 0; cv < CV; ++cv)
-        store_out4(p, (row0 + r) * D + 64 * cv + 4 * tx, make_float4(acc[e][4 * cv] * inv, acc[e][4 * cv + 1] * inv,
+        tree_store_out4(p, (row0 + r) * D + 64 * cv + 4 * tx, make_float4(acc[e][4 * cv] * inv, acc[e][4 * cv + 1] * inv,
                                                                      acc[e][4 * cv + 2] * inv, acc[e][4 * cv + 3] * inv));
     } else {
       if (tx == 0) p.part_ml[pit] = make_float2(m[e], lsum[e]);
@@ -245,7 +238,7 @@ __global__ void __launch_bounds__(128) tree_combine_kernel(TreeAttnParams p) {
     ls = fmaf(ml.y, f, ls);
   }
   const float inv = ls == 0.f ? 0.f : 1.f / ls;
-  store_out4(p, ((int64_t)p.layer_begin * per_layer + row) * p.d + c, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+  tree_store_out4(p, ((int64_t)p.layer_begin * per_layer + row) * p.d + c, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
 }
 
 template <int D> cudaError_t launch_fma(const TreeAttnParams& p, int rb, unsigned grid, cudaStream_t stream) {
@@ -259,38 +252,53 @@ template <int D> cudaError_t opt_in_fma() {
   return e;
 }
 
-// Rows per item, row blocks per KV head and token splits of a call over `layers` layers.
-struct TreePlan { int block_rows, blocks, n_split; };
+// How a call over `layers` layers is laid out.
+struct TreePlan {
+  int block_rows, blocks;       // query rows per item, blocks per KV head
+  int n_split;                  // FMA path: token splits
+  int even, grid, n_units;      // tensor cores: even split over `grid` CTAs, or a unit per CTA
+};
 TreePlan tree_plan(const ngc_cache* c, int layers, int N) {
   const int rows = c->Hq / c->Hkv * N;
-  TreePlan pl;
-  int target, split_keys;                       // CTAs worth having, keys a split has at least
+  TreePlan pl = {};
+  pl.n_split = 1;
   if (c->dtype == NGC_BF16) {
-    pl.block_rows = 128 * tree_umma_tiles(rows);
-    target = rows <= 128 ? 148 * 2 * 2 : 148 * 2;
-    split_keys = 4 * 64;
-  } else {
-    pl.block_rows = rows <= 16 ? 16 : 64;       // small blocks keep the arithmetic near the rows there are
-    target = 148 * 2 * 2;
-    split_keys = kSplitMin * kKeyTile;
+    const int tiles = tree_umma_tiles(rows), slots = tiles == 1 ? 2 * 148 : 148, keys = tree_umma_keys(tiles);
+    pl.blocks = (rows + 128 * tiles - 1) / (128 * tiles);
+    pl.block_rows = pl.blocks > 1 ? 128 * tiles : rows;
+    const int64_t units = (int64_t)layers * c->B * c->Hkv * pl.blocks;
+    const int64_t longest = ((int64_t)c->max_len + keys - 1) / keys + (N + keys - 1) / keys;
+    // Many units: the hardware deals them out one by one.  Short ones are not worth a second kernel.
+    pl.even = units < 4 * slots && longest > 2 * kTreeMinTiles;
+    pl.n_units = (int)(units > 0x7fffffffLL ? 0x7fffffffLL : units);
+    pl.grid = pl.n_units;
+    if (pl.even) {
+      const int64_t most = units * longest / kTreeMinTiles;
+      pl.grid = (int)(most < slots ? most : slots);
+    }
+    return pl;
   }
+  pl.block_rows = rows <= 16 ? 16 : 64;         // small blocks keep the arithmetic near the rows there are
   pl.blocks = (rows + pl.block_rows - 1) / pl.block_rows;
   const int64_t items = (int64_t)layers * c->B * c->Hkv * pl.blocks;
-  int64_t ns = (target + items - 1) / items;
-  const int64_t by_len = ((int64_t)c->max_len + N + split_keys - 1) / split_keys;
+  int64_t ns = (148 * 2 * 2 + items - 1) / items;
+  const int64_t by_len = ((int64_t)c->max_len + N + kSplitMin * kKeyTile - 1) / (kSplitMin * kKeyTile);
   if (ns > by_len) ns = by_len;
   if (ns > 64) ns = 64;
   pl.n_split = ns < 1 ? 1 : (int)ns;
   return pl;
 }
 
-size_t tree_call_scratch_bytes(const ngc_cache* c, int layers, int N, size_t* ml_offset) {
-  const int ns = tree_plan(c, layers, N).n_split;
-  *ml_offset = 0;
-  if (ns <= 1) return 0;
-  const size_t parts = (size_t)layers * c->B * c->Hq * N * ns;
-  *ml_offset = align256(parts * c->d * 4);
-  return *ml_offset + align256(parts * 8);
+// Scratch of one call: the parts' sums, their (m, l), the plan.
+struct TreeScratch { size_t ml, plan, bytes; };
+TreeScratch tree_scratch(const ngc_cache* c, const TreePlan& pl, int layers, int N) {
+  if (pl.n_split <= 1 && !pl.even) return {0, 0, 0};
+  const size_t parts = pl.even ? (size_t)pl.grid * 2 * pl.block_rows : (size_t)layers * c->B * c->Hq * N * pl.n_split;
+  TreeScratch s;
+  s.ml = align256(parts * c->d * 4);
+  s.plan = s.ml + align256(parts * 8);
+  s.bytes = s.plan + (pl.even ? align256(((size_t)pl.n_units + 2) * 4) : 0);
+  return s;
 }
 
 int tree_impl(const ngc_cache* c, const PagedView& pv, const void* q, const void* tree_k, const void* tree_v, const int32_t* parent,
@@ -315,21 +323,21 @@ int tree_impl(const ngc_cache* c, const PagedView& pv, const void* q, const void
   p.page_table = pv.table; p.page = pv.page; p.pages_cap = pv.pages_cap; p.lists = pv.lists;
   p.G = lists_G(pv.lists, c->L, c->Hkv); p.lens_lists = c->lens_lists;
   const TreePlan plan = tree_plan(c, p.n_layers, N);
-  p.row_blocks = plan.blocks; p.n_split = plan.n_split;
-  if (p.n_split > 1) {
-    size_t ml_offset = 0;
-    const size_t need = tree_call_scratch_bytes(c, p.n_layers, N, &ml_offset);
-    if (!ws || ws_bytes < need || ((uintptr_t)ws & 255)) return NGC_ERR_WORKSPACE;
+  p.row_blocks = plan.blocks; p.n_split = plan.n_split; p.block_rows = plan.block_rows;
+  p.even = plan.even; p.grid = plan.grid; p.n_units = plan.n_units; p.plan = nullptr;
+  const TreeScratch need = tree_scratch(c, plan, p.n_layers, N);
+  if (need.bytes > 0) {
+    if (!ws || ws_bytes < need.bytes || ((uintptr_t)ws & 255)) return NGC_ERR_WORKSPACE;
     p.part_o = (float*)ws;
-    p.part_ml = (float2*)((char*)ws + ml_offset);
+    p.part_ml = (float2*)((char*)ws + need.ml);
+    p.plan = (int32_t*)((char*)ws + need.plan);
   }
   const int64_t items = (int64_t)p.n_layers * c->B * c->Hkv * p.row_blocks * p.n_split;
   const int64_t out_threads = (int64_t)p.n_layers * c->B * c->Hq * N * (c->d / 4);
   if (items > 0x7fffffffLL || out_threads / 128 > 0x7ffffff0LL) return NGC_ERR_UNSUPPORTED;
 
   if (c->dtype == NGC_BF16) {
-    const int rc = launch_tree_umma(p, (unsigned)items, stream);
-    if (rc != NGC_OK) return rc;
+    return launch_tree_umma(p, stream);
   } else {
     static PerDeviceOnce attr_once;
     const int rc = attr_once.run([] {
@@ -350,9 +358,9 @@ int tree_impl(const ngc_cache* c, const PagedView& pv, const void* q, const void
 // Workspace that serves a call over any layer range.
 size_t tree_workspace_bytes(const ngc_cache* c, int N) {
   if (N < 1 || N > kTreeMaxNodes) return 0;
-  size_t worst = 0, ml_offset;
+  size_t worst = 0;
   for (int layers = 1; layers <= c->L; ++layers) {
-    const size_t bytes = tree_call_scratch_bytes(c, layers, N, &ml_offset);
+    const size_t bytes = tree_scratch(c, tree_plan(c, layers, N), layers, N).bytes;
     if (bytes > worst) worst = bytes;
   }
   return worst;
@@ -363,7 +371,8 @@ size_t tree_workspace_bytes(const ngc_cache* c, int N) {
 extern "C" int ngc_tree_attn_launches(const ngc_cache* c, int layers, int N) {
   using namespace ngc;
   if (!valid_cache(c) || layers < 1 || N < 1 || N > kTreeMaxNodes) return 0;
-  return tree_plan(c, layers, N).n_split > 1 ? 2 : 1;
+  const TreePlan pl = tree_plan(c, layers, N);
+  return pl.n_split > 1 || pl.even ? 2 : 1;
 }
 
 extern "C" int ngc_tree_attn(const ngc_cache* c, const void* q, const void* tree_k, const void* tree_v, const int32_t* parent,

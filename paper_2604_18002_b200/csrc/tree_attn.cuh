@@ -21,12 +21,15 @@ struct TreeAttnParams {
   const int32_t* parent;        // [B][N]
   const int32_t* n_nodes;       // [B] or null
   void* out;                    // [L][B][Hq][N][d]
-  float* part_o;                // [n_layers][B][Hq][N][n_split][d]
-  float2* part_ml;              // [n_layers][B][Hq][N][n_split]   (m in log2 units, l)
+  float* part_o;                // parts of split rows: sums, unnormalised ...
+  float2* part_ml;              // ... and (maximum in log2 units, sum of weights)
+                                //   FMA path: [n_layers][B][Hq][N][n_split]; tensor cores: [CTA][2][block_rows]
+  int32_t* plan;                // tensor cores: tiles before every unit [n_units + 1], CTAs that had work
   int32_t* dev_status;
   int64_t rows;
   int L, B, Hq, Hkv, d, g, N;
   int layer_begin, n_layers, n_split, row_blocks, out_bf16;
+  int even, grid, n_units, block_rows;    // tensor cores
   float scale_log2;             // scale * log2(e)
   const int32_t* page_table;    // [B][G][pages_cap] or null
   int page, pages_cap, lists, G;
@@ -99,9 +102,28 @@ __device__ __forceinline__ bool tree_masks(const int32_t* parent, int n, int N, 
 // (m, l) of a row that is not computed (a node beyond the tree, a refused sequence): the combine kernel leaves it alone.
 #define kNoPart make_float2(0.f, -1.f)
 
-// Tensor-core path (bf16 caches, tree_attn_umma.cu): M tiles of 128 query rows per CTA for KV heads of `rows` rows.  One
-// tile per CTA lets two CTAs share an SM; more rows than that share their K and V tiles in pairs.
-inline int tree_umma_tiles(int rows) { return rows <= 128 ? 1 : 2; }
-int launch_tree_umma(const TreeAttnParams& p, unsigned grid, cudaStream_t stream);
+// Four consecutive output channels from element idx on.
+__device__ __forceinline__ void tree_store_out4(const TreeAttnParams& p, int64_t idx, float4 v) {
+  if (p.out_bf16)
+    *reinterpret_cast<uint2*>((__nv_bfloat16*)p.out + idx) = make_uint2(ptx::pack_bf16x2(v.x, v.y), ptx::pack_bf16x2(v.z, v.w));
+  else
+    *reinterpret_cast<float4*>((float*)p.out + idx) = v;
+}
+
+// Tensor-core path (bf16 caches, tree_attn_umma.cu): M tiles of 128 query rows per CTA for KV heads of `rows` rows, and the
+// keys of a tile.
+__host__ __device__ constexpr int tree_umma_tiles(int rows) { return rows <= 128 ? 1 : 2; }
+__host__ __device__ constexpr int tree_umma_keys(int tiles) { return tiles == 1 ? 64 : 128; }
+int launch_tree_umma(const TreeAttnParams& p, cudaStream_t stream);
+
+// Even split of `total` tiles: how many of `grid` CTAs take part (each gets at least kTreeMinTiles tiles), the first tile
+// of CTA c, and the CTA that has tile g.
+constexpr int kTreeMaxUnits = 1184, kTreeMinTiles = 3;
+__host__ __device__ inline int tree_even_ctas(int total, int grid) {
+  const int most = total / kTreeMinTiles;
+  return most < 1 ? 1 : (most < grid ? most : grid);
+}
+__host__ __device__ inline int tree_even_first(int c, int total, int ctas) { return (int)((int64_t)total * c / ctas); }
+__host__ __device__ inline int tree_even_owner(int g, int total, int ctas) { return (int)((((int64_t)g + 1) * ctas - 1) / total); }
 
 }  // namespace ngc

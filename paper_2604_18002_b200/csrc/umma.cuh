@@ -34,6 +34,15 @@ __device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t saddr, uint32_t lbo
   return ((uint64_t)hi << 32) | lo;
 }
 
+// True in exactly one lane of a converged warp.  The compiler knows that the branch it guards runs in one thread: the
+// operands of the instructions inside stay in uniform registers (a plain `lane == 0` costs a move out of the vector
+// registers for every descriptor).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
+}
+
 // Tensor memory: `cols` columns (a power of two, 32..512) of 128 lanes x 32 bit.  Warp-collective; the
 // base address lands in *slot (shared memory).  The same warp frees it.
 __device__ __forceinline__ void tmem_alloc(uint32_t* slot, uint32_t cols) {

@@ -193,17 +193,26 @@ def test_tree_attn_skips_refused_sequences(dtype, d, T):
     c, q, tk, tv, parent, _ = case(dtype, d, 4, 2, 1, [T, T, T, T], N, "tree", seed=4)
     good, st = run_tree(c, q, tk, tv, parent, None)
     assert st == 0
+    # A long bf16 cache is cut into parts at places that depend on all the sequences' lengths, so the same row may come
+    # out of another grouping of the same sums: each of the two is within its bound of the exact value, hence they
+    # are within twice that of one another.  Everything else is the same to the bit.
+    ref = draft.tree_attn(synth.to_numpy(c.k), synth.to_numpy(c.v), c.seq_off.numpy(), c.lens.numpy(), synth.to_numpy(q), synth.to_numpy(tk),
+                          synth.to_numpy(tv), parent)
+    lim = torch.as_tensor(2 * bound(c, q, tk, tv, parent, None, ref)).cuda() * int(dtype == bf16 and T > 64)
+
+    def same(out, seqs):
+        return bool((torch.abs(out[:, seqs].double() - good[:, seqs].double()) <= lim[:, seqs]).all())
     for where, val in (((1, 0), 0), ((1, 4), 4), ((1, 4), 7), ((1, 8), -1), ((1, 3), -2)):
         p2 = parent.copy()
         p2[where] = val
         out, st = run_tree(c, q, tk, tv, p2, None)
-        assert st == 8 and (out[:, 1] == -7).all() and torch.equal(out[:, [0, 2, 3]], good[:, [0, 2, 3]])
+        assert st == 8 and (out[:, 1] == -7).all() and same(out, [0, 2, 3])
     out, st = run_tree(c, q, tk, tv, parent, np.array([N, -1, N + 1, N], np.int32))
-    assert st == 8 and (out[:, 1:3] == -7).all() and torch.equal(out[:, [0, 3]], good[:, [0, 3]])
+    assert st == 8 and (out[:, 1:3] == -7).all() and same(out, [0, 3])
     lens = c.lens.clone()
     lens[0], lens[2] = -1, T + 1
     out, st = run_tree(c, q, tk, tv, parent, None, lens=lens)
-    assert st == 1 and (out[:, [0, 2]] == -7).all() and torch.equal(out[:, [1, 3]], good[:, [1, 3]])
+    assert st == 1 and (out[:, [0, 2]] == -7).all() and same(out, [1, 3])
 
 
 def to_pages(c, page, lists, seed, per_list):
