@@ -41,6 +41,19 @@ inline bool make_kv_map(CUtensorMap* map, const void* base, int64_t rows, int pl
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The same rows as a 4-D tensor (channel in its group of 64, row, group, plane), so that ONE load fetches all d channels
+// of `box_rows` rows: groups one behind the other in shared memory, each 64 channels x box_rows rows.
+inline bool make_strip_map(CUtensorMap* map, const void* base, int64_t rows, int planes, int box_rows, int d) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  cuuint64_t dims[4] = {64, (cuuint64_t)rows, (cuuint64_t)(d / 64), (cuuint64_t)planes};
+  cuuint64_t strides[3] = {(cuuint64_t)d * 2, 128, (cuuint64_t)rows * d * 2};
+  cuuint32_t box[4] = {64, (cuuint32_t)box_rows, (cuuint32_t)(d / 64), 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // A bf16 matrix of `rows` rows of 128 (or d = 64) channels as a 2-D tensor (channel, row); box = 64 channels x `box_rows`
 // rows, 128-byte swizzle.  box_rows = 1 is the shape the TMA row gather (tile::gather4) takes.
 inline bool make_rows_map(CUtensorMap* map, const void* base, int64_t rows, int box_rows, int d = 128) {

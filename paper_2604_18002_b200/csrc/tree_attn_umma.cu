@@ -10,10 +10,12 @@
 //                    tiles serve both M tiles, whose softmax and products alternate on the tensor pipe.  (With 64 keys
 //                    S = Q K^T waits for shared memory: Q is read again for every 64 keys.)
 //
-//   producer warp    Q once per unit, then K and V of every tile by tiled TMA (128-byte swizzle), each in a ring of its
-//                    own (K is free as soon as S is computed, V only after P V): whole tiles or pages, the partly
-//                    filled last tile of the cache and the tree tiles in 16-row boxes; page-table entries are fetched
-//                    32 at a time, a batch ahead;
+//   producer warps   one for Q (once per unit) and K, one for V, by tiled TMA (128-byte swizzle), K and V each in a ring
+//                    of its own (K is free as soon as S is computed, V only after P V).  Issuing a load takes a warp
+//                    some 150 cycles, so a whole tile of a contiguous cache is ONE load (the groups of 64 channels are a
+//                    dimension of the tensor map); pages are a load per 64 channels, the partly filled last tile of the
+//                    cache and the tree tiles come in 16-row boxes.  Page-table entries are fetched 32 at a time, a
+//                    batch ahead;
 //   MMA warp         S = Q K^T into tensor memory, O += P V with P read from tensor memory;
 //   softmax warps    (4 MT) one thread per row: mask (only in tree tiles, a bit of the node's ancestor set, and in the
 //                    cache's last tile), online softmax in the log2 domain, P as bf16 over the S it came from, 64 keys
@@ -50,8 +52,8 @@ template <int D, int MT> struct Cfg {
   static constexpr int kHalves = kKeys / 64;               // P is handed over 64 keys at a time
   static constexpr int kStages = D == 64 ? 4 : 2;          // of K and of V
   static constexpr int kCtas = MT == 1 ? 2 : 1;
-  static constexpr int kThreads = (4 * MT + 2) * 32;
-  static constexpr int kMmaWarp = 4 * MT, kProducerWarp = 4 * MT + 1;
+  static constexpr int kThreads = (4 * MT + 3) * 32;
+  static constexpr int kMmaWarp = 4 * MT, kProducerWarp = 4 * MT + 1;      // K and Q; V in the warp behind
   static constexpr int kBox = kKeys * 128;                 // a tile's 64 channels
   static constexpr int kTile = kKeys * D * 2;              // K or V tile
   static constexpr int kQBytes = 128 * D * 2;              // Q of an M tile
@@ -60,9 +62,10 @@ template <int D, int MT> struct Cfg {
   static constexpr uint32_t kCols = MT == 1 ? 256 : 512;
 };
 
-// Tensor maps of a launch: K and V by 64 rows (or one page) and by 16 rows; the tree's K and V (16 rows, a plane
-// per strip); Q (128 rows).
-struct Maps { CUtensorMap k, v, k16, v16, tk, tv, q; };
+// Tensor maps of a launch.  K and V: whole tiles (contiguous caches, all channels in one box) or pages, and 16 rows; the
+// tree's K and V (16 rows, a plane per strip); Q (128 rows).
+struct KvMaps { CUtensorMap whole, part, tree; };
+struct Maps { KvMaps k, v; CUtensorMap q; };
 
 template <int D, int MT> struct Shared {
   using C = Cfg<D, MT>;
@@ -104,19 +107,22 @@ template <int KT> __device__ __forceinline__ int unit_tiles(const TreeAttnParams
   return counts_ok(p, w) && w.n > 0 ? (w.len + KT - 1) / KT + (w.n + KT - 1) / KT : 0;
 }
 
-// Page-table entries in order, 32 at a time in the lanes of the producer warp, the next batch on its way.
+// Page-table entries in order, 32 at a time in the lanes of a producer warp, the next batch on its way.  An entry that is
+// none is reported and read as page 0.
 struct PageWalk {
   const int32_t* table;
-  int cap, at, cur, next;
+  int cap, len, at, cur, next;                  // len: pages in use
   int32_t* dev_status;
   __device__ __forceinline__ int fetch(int first) const {
     const int j = first + (int)(threadIdx.x & 31);
-    if (j >= cap) return 0;
+    if (j >= len) return 0;
     const int pg = table[j];
-    return pg;
+    if (pg >= 0 && pg < cap) return pg;
+    set_dev_status(dev_status, NGC_DEV_BAD_PAGE);
+    return 0;
   }
-  __device__ __forceinline__ void start(const int32_t* t, int pages_cap, int first, int32_t* status) {
-    table = t; cap = pages_cap; at = first; dev_status = status;
+  __device__ __forceinline__ void start(const int32_t* t, int pages_cap, int pages, int first, int32_t* status) {
+    table = t; cap = pages_cap; len = pages; at = first; dev_status = status;
     cur = fetch(at);
     next = fetch(at + 32);
   }
@@ -127,45 +133,50 @@ struct PageWalk {
       cur = next;
       next = fetch(at + 32);
     }
-    int pg = __shfl_sync(0xffffffffu, cur, j - at);
-    if (pg < 0 || pg >= cap) {
-      set_dev_status(dev_status, NGC_DEV_BAD_PAGE);
-      pg = 0;
-    }
-    return pg;
+    return __shfl_sync(0xffffffffu, cur, j - at);
   }
 };
 
 // Issues the loads of K or V tile t (whole warp; one lane issues).  Rows that are not loaded keep old bytes: their scores
 // are masked and P V stops before them.
 template <int D, int KT>
-__device__ __forceinline__ void load_tile(const TreeAttnParams& p, const CUtensorMap* whole, const CUtensorMap* part, const CUtensorMap* tree,
-                                          PageWalk& pages, const Piece& w, int base, int t, uint8_t* dst, uint64_t* bar) {
+__device__ __forceinline__ void load_tile(const TreeAttnParams& p, const KvMaps& maps, PageWalk& pages, const Piece& w, int base, int t,
+                                          uint8_t* dst, uint64_t* bar) {
   constexpr int kBox = KT * 128;
   const bool in_tree = t >= w.n_ct;
   const int live = min(KT, in_tree ? w.n - (t - w.n_ct) * KT : w.len - t * KT);
-  const int n16 = (live + 15) >> 4, n64 = in_tree ? 0 : live >> 6;          // 64-row parts that are full
-  if (umma::elect_one()) ptx::mbar_expect_tx(bar, (uint32_t)n16 * 16 * D * 2);
-  __syncwarp();
-  const int step = p.page_table ? p.page : 64;
-  for (int r = 0; r < 64 * n64; r += step) {
-    int y = base + t * KT + r;
-    if (p.page_table) y = base + pages.get((t * KT + r) / p.page) * p.page;
-    if (!NGC_IN_BOUNDS(p.dev_status, y >= 0 && y + step <= p.rows)) y = 0;
+  if (!p.page_table && !in_tree && live == KT) {
+    int y = base + t * KT;
+    if (!NGC_IN_BOUNDS(p.dev_status, y >= 0 && y + KT <= p.rows)) y = 0;
     if (umma::elect_one()) {
-#pragma unroll
-      for (int c = 0; c < D / 64; ++c) ptx::tma_load_3d(dst + c * kBox + r * 128, whole, 64 * c, y, w.plane, bar);
+      ptx::mbar_expect_tx(bar, (uint32_t)KT * D * 2);
+      ptx::tma_load_4d(dst, &maps.whole, 0, y, 0, w.plane, bar);
     }
     __syncwarp();
+    return;
   }
-  for (int r = 64 * n64; r < 16 * n16; r += 16) {
+  const int n16 = (live + 15) >> 4;
+  if (umma::elect_one()) ptx::mbar_expect_tx(bar, (uint32_t)n16 * 16 * D * 2);
+  __syncwarp();
+  int r = 0;
+  if (p.page_table && !in_tree)
+    for (; r + p.page <= live; r += p.page) {
+      int y = base + pages.get((t * KT + r) / p.page) * p.page;
+      if (!NGC_IN_BOUNDS(p.dev_status, y >= 0 && y + p.page <= p.rows)) y = 0;
+      if (umma::elect_one()) {
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) ptx::tma_load_3d(dst + c * kBox + r * 128, &maps.whole, 64 * c, y, w.plane, bar);
+      }
+      __syncwarp();
+    }
+  for (; r < 16 * n16; r += 16) {
     int y = in_tree ? (t - w.n_ct) * KT + r : base + t * KT + r;
     if (!in_tree && p.page_table) y = base + pages.get((t * KT + r) / p.page) * p.page + (t * KT + r) % p.page;
     if (!NGC_IN_BOUNDS(p.dev_status, y >= 0 && y < (in_tree ? (int64_t)p.N : p.rows))) y = 0;
     if (umma::elect_one()) {
 #pragma unroll
       for (int c = 0; c < D / 64; ++c)
-        ptx::tma_load_3d(dst + c * kBox + r * 128, in_tree ? tree : part, 64 * c, y, in_tree ? w.strip : w.plane, bar);
+        ptx::tma_load_3d(dst + c * kBox + r * 128, in_tree ? &maps.tree : &maps.part, 64 * c, y, in_tree ? w.strip : w.plane, bar);
     }
     __syncwarp();
   }
@@ -209,8 +220,8 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     ptx::mbar_init(&sh.drain, 1);
     ptx::fence_barrier_init();
     sh.abort = 0;
-    ptx::prefetch_tensormap(&maps.k);
-    ptx::prefetch_tensormap(&maps.v);
+    ptx::prefetch_tensormap(&maps.k.whole);
+    ptx::prefetch_tensormap(&maps.v.whole);
     ptx::prefetch_tensormap(&maps.q);
   }
   if (warp == C::kMmaWarp) umma::tmem_alloc(&sh.tmem, C::kCols);
@@ -306,15 +317,15 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
         for (int r = tid; r < p.block_rows; r += NT) p.part_ml[part0 + r] = kNoPart;
     } else if (w.n_tiles <= 0) {
       // an empty tree
-    } else if (warp == C::kProducerWarp) {
-      // ------------------------------------------------------------------ producer
+    } else if (warp >= C::kProducerWarp) {
+      // ------------------------------------------------------------------ producers
+      const bool is_v = warp != C::kProducerWarp;
       const int base = (int)(p.page_table ? (int64_t)w.b * p.pages_cap * p.page : p.seq_off[w.b]);
       PageWalk pages;
       if (p.page_table)
         pages.start(p.page_table + ((int64_t)w.b * p.G + list_of(p.lists, w.l, w.h, p.Hkv)) * p.pages_cap, p.pages_cap,
-                    min(w.lo * KT, w.len) / p.page, p.dev_status);
-      PageWalk pages_v = pages;
-      if (umma::elect_one()) {
+                    (w.len + p.page - 1) / p.page, min(w.lo * KT, w.len) / p.page, p.dev_status);
+      if (!is_v && umma::elect_one()) {
         ptx::mbar_expect_tx(&sh.q_full, (uint32_t)(tiles_m * C::kQBytes));
         // rows beyond the KV head's belong to the next head (zeros past the end): they only feed rows that are never written
         for (int m = 0; m < tiles_m; ++m)
@@ -323,23 +334,19 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
             ptx::tma_load_2d(sQ + m * C::kQBytes + c * (128 * 128), &maps.q, 64 * c, (int)(row0 + r0 + 128 * m), &sh.q_full);
       }
       __syncwarp();
-      bool ok = true;
-      int i = 0, v_issued = 0;
+      uint8_t* ring = is_v ? sV : sK;
+      uint64_t* full = is_v ? sh.v_full : sh.k_full;
+      uint64_t* empty = is_v ? sh.v_empty : sh.k_empty;
+      const KvMaps& map = is_v ? maps.v : maps.k;
+      int i = 0;
       for (; i < w.n_tiles; ++i) {
         const int s = (kv + i) % ST;
-        const uint32_t ph = ((kv + i) / ST - 1) & 1;
-        ok = kv + i < ST || umma::warp_wait(&sh.k_empty[s], ph, &sh.abort, p.dev_status);
-        if (!ok) break;
-        load_tile<D, KT>(p, &maps.k, &maps.k16, &maps.tk, pages, w, base, w.lo + i, sK + s * C::kTile, &sh.k_full[s]);
-        ok = kv + i < ST || umma::warp_wait(&sh.v_empty[s], ph, &sh.abort, p.dev_status);
-        if (!ok) { ++i; break; }
-        load_tile<D, KT>(p, &maps.v, &maps.v16, &maps.tv, pages_v, w, base, w.lo + i, sV + s * C::kTile, &sh.v_full[s]);
-        ++v_issued;
+        if (kv + i >= ST && !umma::warp_wait(&empty[s], ((kv + i) / ST - 1) & 1, &sh.abort, p.dev_status)) break;
+        load_tile<D, KT>(p, map, pages, w, base, w.lo + i, ring + s * C::kTile, &full[s]);
       }
-      if (!ok) {                                // giving up: no copy may be in flight when the CTA ends
-        ptx::mbar_wait_bounded(&sh.q_full, n_q & 1);
-        for (int j = max(0, i - ST); j < i; ++j) ptx::mbar_wait_bounded(&sh.k_full[(kv + j) % ST], ((kv + j) / ST) & 1);
-        for (int j = max(0, v_issued - ST); j < v_issued; ++j) ptx::mbar_wait_bounded(&sh.v_full[(kv + j) % ST], ((kv + j) / ST) & 1);
+      if (i < w.n_tiles) {                      // giving up: no copy may be in flight when the CTA ends
+        if (!is_v) ptx::mbar_wait_bounded(&sh.q_full, n_q & 1);
+        for (int j = max(0, i - ST); j < i; ++j) ptx::mbar_wait_bounded(&full[(kv + j) % ST], ((kv + j) / ST) & 1);
       }
     } else if (warp == C::kMmaWarp) {
       // ------------------------------------------------------------------ MMA issue, one elected lane
@@ -383,6 +390,8 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
           issue_s(0, i + 1, true);
         }
         ok = umma::warp_wait(&sh.v_full[s], ((kv + i) / ST) & 1, &sh.abort, p.dev_status);
+        if (NB == 1 && ok && i + 1 < w.n_tiles)
+          ok = umma::warp_wait(&sh.k_full[(kv + i + 1) % ST], ((kv + i + 1) / ST) & 1, &sh.abort, p.dev_status);
         for (int m = 0; ok && m < tiles_m; ++m) {
           const int buf = (done[m] + i) % NB;
           const uint32_t ph = ((done[m] + i) / NB) & 1, o_tmem = tmem + C::kOCol + (uint32_t)(D * m);
@@ -405,10 +414,7 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
             }
             __syncwarp();
           }
-          if (NB == 1 && ok && i + 1 < w.n_tiles) {
-            if (m == 0) ok = umma::warp_wait(&sh.k_full[(kv + i + 1) % ST], ((kv + i + 1) / ST) & 1, &sh.abort, p.dev_status);
-            if (ok) issue_s(m, i + 1, m + 1 == tiles_m);
-          }
+          if (NB == 1 && ok && i + 1 < w.n_tiles) issue_s(m, i + 1, m + 1 == tiles_m);
         }
       }
     } else if (warp < 4 * tiles_m) {
@@ -684,16 +690,20 @@ int launch_tree_umma(const TreeAttnParams& p, cudaStream_t stream) {
   const int64_t strips = (int64_t)p.L * p.B * p.Hkv, q_rows = (int64_t)p.L * p.B * p.Hq * p.N;
   if (p.rows > 0x7fffffffLL || strips > 0x7fffffffLL) return NGC_ERR_UNSUPPORTED;      // TMA coordinates are 32-bit
   Maps maps;
-  bool ok = make_kv_map(&maps.tk, p.tree_k, p.N, (int)strips, 16, p.d) && make_kv_map(&maps.tv, p.tree_v, p.N, (int)strips, 16, p.d) &&
-            make_rows_map(&maps.q, p.q, q_rows, 128, p.d);
-  if (ok && p.rows > 0) {
-    const int box = p.page_table ? p.page : 64;
-    ok = make_kv_map(&maps.k, p.k, p.rows, planes, box, p.d) && make_kv_map(&maps.v, p.v, p.rows, planes, box, p.d) &&
-         make_kv_map(&maps.k16, p.k, p.rows, planes, 16, p.d) && make_kv_map(&maps.v16, p.v, p.rows, planes, 16, p.d);
-  } else {
-    maps.k = maps.k16 = maps.tk;                 // a cache without rows: never read
-    maps.v = maps.v16 = maps.tv;
-  }
+  const bool one = tree_umma_tiles(p.g * p.N) == 1;
+  bool ok = make_rows_map(&maps.q, p.q, q_rows, 128, p.d);
+  auto kv_maps = [&](KvMaps* m, const void* cache, const void* tree) {
+    ok = ok && make_kv_map(&m->tree, tree, p.N, (int)strips, 16, p.d);
+    if (p.rows == 0) {                           // a cache without rows: never read
+      m->whole = m->part = m->tree;
+      return;
+    }
+    ok = ok && make_kv_map(&m->part, cache, p.rows, planes, 16, p.d) &&
+         (p.page_table ? make_kv_map(&m->whole, cache, p.rows, planes, p.page, p.d)
+                       : make_strip_map(&m->whole, cache, p.rows, planes, tree_umma_keys(one ? 1 : 2), p.d));
+  };
+  kv_maps(&maps.k, p.k, p.tree_k);
+  kv_maps(&maps.v, p.v, p.tree_v);
   if (!ok) return NGC_ERR_UNSUPPORTED;
   static PerDeviceOnce attr_once;
   const int rc = attr_once.run([] {
@@ -704,7 +714,6 @@ int launch_tree_umma(const TreeAttnParams& p, cudaStream_t stream) {
     return e;
   });
   if (rc != NGC_OK) return rc;
-  const bool one = tree_umma_tiles(p.g * p.N) == 1;
   if (p.d == 64) NGC_CUDA_TRY(one ? (launch<64, 1>(maps, p, stream)) : (launch<64, 2>(maps, p, stream)));
   else NGC_CUDA_TRY(one ? (launch<128, 1>(maps, p, stream)) : (launch<128, 2>(maps, p, stream)));
   if (p.even) {

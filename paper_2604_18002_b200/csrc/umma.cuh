@@ -137,15 +137,17 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   return d;
 }
 
-// Bounded wait that also gives up as soon as another thread of the CTA has given up (*abort, in shared memory).
+// Bounded wait that also gives up as soon as another thread of the CTA has given up (*abort, in shared memory).  The
+// clock is first read after 64 tries: reading it takes longer than most waits last.
 __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, int* abort, int32_t* dev_status) {
-  if (ptx::mbar_try_wait(bar, parity)) return true;
-  const uint64_t t0 = ptx::globaltimer_ns();
+  uint64_t t0 = 0;
   for (uint32_t spins = 0;; ++spins) {
     if (ptx::mbar_try_wait(bar, parity)) return true;
     if ((spins & 63u) == 63u) {
       if (*(volatile int*)abort) return false;
-      if (ptx::globaltimer_ns() - t0 > ptx::kWaitLimitNs) {
+      const uint64_t t = ptx::globaltimer_ns();
+      if (t0 == 0) t0 = t;
+      if (t - t0 > ptx::kWaitLimitNs) {
         *(volatile int*)abort = 1;
         set_dev_status(dev_status, NGC_DEV_TIMEOUT);
         return false;
