@@ -552,8 +552,8 @@ int ngc_commit_draft_paged(ngc_paged_cache* c, const void* tree_k, const void* t
 int ngc_fork_kv(ngc_cache* c, const int32_t* src_of, int32_t* dev_status, ngc_stream stream);
 
 /* ngc_fork_kv on a paged cache: rows are copied page by page, from the pages the source's table names to the
- * first pages of b's own table (the tables do not change).  A bad page-table entry among them
- * (NGC_DEV_BAD_PAGE) leaves b as it was. */
+ * first pages of b's own table (the tables do not change).  A bad page-table entry among them (NGC_DEV_BAD_PAGE) leaves
+ * b's lengths as they were; the rows of the lists whose entries are good may have been copied. */
 int ngc_fork_pages(ngc_paged_cache* c, const int32_t* src_of, int32_t* dev_status, ngc_stream stream);
 
 /*

@@ -154,24 +154,36 @@ def _ptr(t: Optional[torch.Tensor]):
     return t.data_ptr()
 
 
-def _expect(what: str, device: torch.device, *tensors):
-    """Checks of the drafted-token calls: every (name, tensor or None, shape, dtype) must have that shape and type, be
-    contiguous and live on ``device``, which must be the current one (the library launches there)."""
-    for name, t, shape, dtype in tensors:
-        if t is None:
-            continue
-        if t.shape != shape or t.dtype is not dtype:
-            raise NgcError(f"{what}: {name} must be {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-        if not t.is_contiguous():
-            raise NgcError(f"{what}: {name} must be contiguous")
-    if device.type != "cuda":
+# Argument checks of the drafted-token calls.  A draft step is a handful of calls per layer, a few microseconds each on
+# the GPU, so the checks are written to cost little: one pass per tensor that ends in its address.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_I32, _F32, _I64, _U8 = torch.int32, torch.float32, torch.int64, torch.uint8
+
+
+def _refuse(what: str, name: str, t: torch.Tensor, shape, dtype, index: int):
+    if t.shape != shape or t.dtype is not dtype:
+        raise NgcError(f"{what}: {name} must be {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise NgcError(f"{what}: {name} must be contiguous")
+    raise NgcError(f"{what}: {name} is on {t.device}, the call's other tensors on " + ("the host" if index < 0 else f"cuda:{index}"))
+
+
+def _arg(what: str, name: str, t: Optional[torch.Tensor], shape, dtype, index: int):
+    """Address of a contiguous tensor of that shape and type on device ``index`` (-1: host); None for None."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
+        _refuse(what, name, t, shape, dtype, index)
+    return t.data_ptr()
+
+
+def _launch_stream(what: str, index: int):
+    """The current stream of the device that the tensors are on, which must be the current one (the library launches there)."""
+    if index < 0:
         raise NgcError(f"{what}: device tensors required: the library has no CPU path")
-    index = device.index
-    for name, t, _, _ in tensors:
-        if t is not None and t.get_device() != index:
-            raise NgcError(f"{what}: {name} is on {t.device}, the call's other tensors on {device}")
     if index != torch.cuda.current_device():
-        raise NgcError(f"{what}: tensors on {device}, but the current device is {torch.cuda.current_device()}")
+        raise NgcError(f"{what}: tensors on cuda:{index}, but the current device is {torch.cuda.current_device()}")
+    return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
 
 
 def _stream():
@@ -440,37 +452,40 @@ def tree_attn_launches(cache: NgcCache, N: int, layers: Optional[int] = None) ->
     return int(lib.ngc_tree_attn_launches(C.byref(d), cache.L if layers is None else layers, N))
 
 
-def _cache_shape(cache):
-    """(L, B, Hkv, d) of a contiguous or paged cache."""
+def _view(what: str, cache):
+    """Checks a cache's own tensors; (descriptor, L, B, Hkv, d, dtype, device index)."""
+    k, lens = cache.k, cache.lens
+    shape, dt, index = k.shape, k.dtype, k.get_device()
+    kp, vp = _arg(what, "k", k, shape, dt, index), _arg(what, "v", cache.v, shape, dt, index)
     if isinstance(cache, NgcPagedCache):
-        return cache.k.shape[0], cache.page_table.shape[0], cache.k.shape[1], cache.k.shape[4]
-    return cache.L, cache.B, cache.Hkv, cache.d
-
-
-def _cache_tensors(cache):
-    """The cache's own tensors for _expect: types, and lengths of a shape the descriptor can name."""
-    k, i32 = cache.k, torch.int32
-    if isinstance(cache, NgcPagedCache):
-        B, G = cache.page_table.shape[:2]
-        per, tab = cache.lens.dim() == 2, ("page_table", cache.page_table, cache.page_table.shape, i32)
+        L, Hkv, n_pages, page, d = shape
+        table = cache.page_table
+        B, G, cap = table.shape
+        if n_pages != B * cap or G != lists_G(cache.lists, L, Hkv):
+            raise NgcError(f"{what}: page_table {tuple(table.shape)} does not fit k {tuple(shape)} and the lists")
+        per = lens.dim() == 2
+        desc = PagedCacheDesc(kp, vp, _arg(what, "page_table", table, table.shape, _I32, index),
+                              _arg(what, "lens", lens, (B, G) if per else (B,), _I32, index), L, B, cache.Hq, Hkv, d, _dtype_code(k), page, cap,
+                              cache.lists, 1 if per else 0)
     else:
-        B, per = cache.B, cache.lens_lists != 0
-        G, tab = lists_G(cache.lens_lists, k.shape[0], k.shape[1]), ("seq_off", cache.seq_off, (B + 1,), torch.int64)
-    return ("k", k, k.shape, k.dtype), ("v", cache.v, k.shape, k.dtype), ("lens", cache.lens, (B, G) if per else (B,), i32), tab
+        L, Hkv, R, d = shape
+        B, per = cache.seq_off.shape[0] - 1, cache.lens_lists
+        desc = CacheDesc(kp, vp, _arg(what, "seq_off", cache.seq_off, (B + 1,), _I64, index),
+                         _arg(what, "lens", lens, (B, lists_G(per, L, Hkv)) if per else (B,), _I32, index), R, L, B, cache.Hq, Hkv, d,
+                         _dtype_code(k), cache.max_len, per)
+    return desc, L, B, Hkv, d, dt, index
 
 
 def _tree_attn(what, call, cache, q, tree_k, tree_v, parent, out, n_nodes, layer_begin, layer_end, scale, ws, status):
-    L, B, Hkv, d = _cache_shape(cache)
-    N, dt, i32 = parent.shape[-1], cache.k.dtype, torch.int32
+    desc, L, B, Hkv, d, dt, index = _view(what, cache)
+    N = parent.shape[-1]
     heads, rows = (L, B, cache.Hq, N, d), (L, B, Hkv, N, d)
-    _expect(what, cache.k.device, ("q", q, heads, dt), ("tree_k", tree_k, rows, dt), ("tree_v", tree_v, rows, dt), ("parent", parent, (B, N), i32),
-            ("n_nodes", n_nodes, (B,), i32), ("out", out, heads, out.dtype), ("ws", ws, ws.shape if ws is not None else (), torch.uint8),
-            ("status", status, (1,), i32), *_cache_tensors(cache))
-    desc = cache.desc()
-    rc = call(C.byref(desc), _ptr(q), _ptr(tree_k), _ptr(tree_v), _ptr(parent), _ptr(n_nodes), N, layer_begin,
-              L if layer_end is None else layer_end, 1.0 / (d ** 0.5) if scale is None else scale, _ptr(out), _dtype_code(out),
-              _ptr(ws), 0 if ws is None else ws.numel(), _ptr(status), _stream())
-    _check(rc, what)
+    args = (_arg(what, "q", q, heads, dt, index), _arg(what, "tree_k", tree_k, rows, dt, index), _arg(what, "tree_v", tree_v, rows, dt, index),
+            _arg(what, "parent", parent, (B, N), _I32, index), _arg(what, "n_nodes", n_nodes, (B,), _I32, index), N, layer_begin,
+            L if layer_end is None else layer_end, d ** -0.5 if scale is None else scale, _arg(what, "out", out, heads, out.dtype, index),
+            _dtype_code(out), None if ws is None else _arg(what, "ws", ws, ws.shape, _U8, index), 0 if ws is None else ws.numel(),
+            _arg(what, "status", status, (1,), _I32, index))
+    _check(call(C.byref(desc), *args, _launch_stream(what, index)), what)
 
 
 def ngc_tree_attn(cache: NgcCache, q: torch.Tensor, tree_k: torch.Tensor, tree_v: torch.Tensor, parent: torch.Tensor,
@@ -496,23 +511,23 @@ def ngc_verify_draft(tokens: torch.Tensor, parent: torch.Tensor, target_probs: t
     """Walk of a drafted tree: target_probs, draft_probs fp32 [B][N][vocab]; tokens, parent, path int32 [B][N]; uniforms
     fp32 [B][N] (entry 0: the final draw); n_path, next_token int32 [B]."""
     B, N, V = target_probs.shape
-    i32, f32 = torch.int32, torch.float32
-    _expect("ngc_verify_draft", target_probs.device, ("tokens", tokens, (B, N), i32), ("parent", parent, (B, N), i32),
-            ("target_probs", target_probs, (B, N, V), f32), ("uniforms", uniforms, (B, N), f32), ("path", path, (B, N), i32),
-            ("n_path", n_path, (B,), i32), ("next_token", next_token, (B,), i32), ("draft_probs", draft_probs, (B, N, V), f32),
-            ("n_nodes", n_nodes, (B,), i32), ("status", status, (1,), i32))
-    rc = lib.ngc_verify_draft(_ptr(tokens), _ptr(parent), _ptr(n_nodes), _ptr(target_probs), _ptr(draft_probs), _ptr(uniforms), B, N, V,
-                              greedy, _ptr(path), _ptr(n_path), _ptr(next_token), _ptr(status), _stream())
-    _check(rc, "ngc_verify_draft")
+    what, index, probs = "ngc_verify_draft", target_probs.get_device(), (B, N, V)
+    args = (_arg(what, "tokens", tokens, (B, N), _I32, index), _arg(what, "parent", parent, (B, N), _I32, index),
+            _arg(what, "n_nodes", n_nodes, (B,), _I32, index), _arg(what, "target_probs", target_probs, probs, _F32, index),
+            _arg(what, "draft_probs", draft_probs, probs, _F32, index), _arg(what, "uniforms", uniforms, (B, N), _F32, index), B, N, V, greedy,
+            _arg(what, "path", path, (B, N), _I32, index), _arg(what, "n_path", n_path, (B,), _I32, index),
+            _arg(what, "next_token", next_token, (B,), _I32, index), _arg(what, "status", status, (1,), _I32, index))
+    _check(lib.ngc_verify_draft(*args, _launch_stream(what, index)), what)
 
 
 def _commit_draft(what, call, cache, tree_k, tree_v, path, n_path, status):
-    L, B, Hkv, d = _cache_shape(cache)
-    N, dt, i32 = path.shape[-1], cache.k.dtype, torch.int32
-    _expect(what, cache.k.device, ("tree_k", tree_k, (L, B, Hkv, N, d), dt), ("tree_v", tree_v, (L, B, Hkv, N, d), dt),
-            ("path", path, (B, N), i32), ("n_path", n_path, (B,), i32), ("status", status, (1,), i32), *_cache_tensors(cache))
-    desc = cache.desc()
-    _check(call(C.byref(desc), _ptr(tree_k), _ptr(tree_v), _ptr(path), _ptr(n_path), N, _ptr(status), _stream()), what)
+    desc, L, B, Hkv, d, dt, index = _view(what, cache)
+    N = path.shape[-1]
+    rows = (L, B, Hkv, N, d)
+    args = (_arg(what, "tree_k", tree_k, rows, dt, index), _arg(what, "tree_v", tree_v, rows, dt, index),
+            _arg(what, "path", path, (B, N), _I32, index), _arg(what, "n_path", n_path, (B,), _I32, index), N,
+            _arg(what, "status", status, (1,), _I32, index))
+    _check(call(C.byref(desc), *args, _launch_stream(what, index)), what)
 
 
 def ngc_commit_draft(cache: NgcCache, tree_k: torch.Tensor, tree_v: torch.Tensor, path: torch.Tensor, n_path: torch.Tensor,
@@ -527,10 +542,9 @@ def ngc_commit_draft_paged(cache: NgcPagedCache, tree_k: torch.Tensor, tree_v: t
 
 
 def _fork(what, call, cache, src_of, status):
-    _expect(what, cache.k.device, ("src_of", src_of, (_cache_shape(cache)[1],), torch.int32), ("status", status, (1,), torch.int32),
-            *_cache_tensors(cache))
-    desc = cache.desc()
-    _check(call(C.byref(desc), _ptr(src_of), _ptr(status), _stream()), what)
+    desc, _, B, _, _, _, index = _view(what, cache)
+    args = (_arg(what, "src_of", src_of, (B,), _I32, index), _arg(what, "status", status, (1,), _I32, index))
+    _check(call(C.byref(desc), *args, _launch_stream(what, index)), what)
 
 
 def ngc_fork_kv(cache: NgcCache, src_of: torch.Tensor, status: Optional[torch.Tensor] = None):

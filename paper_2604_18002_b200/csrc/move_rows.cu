@@ -1,12 +1,16 @@
 // Row moves around a draft: ngc_commit_draft appends the K/V rows of the accepted nodes, ngc_fork_kv
 // copies a prefilled sequence to the sequences of its group.  Contiguous and paged caches.
 //
-// Both only move 16-byte vectors: HBM-bound for large batches, launch latency for small ones.
+// Both only move whole rows: HBM-bound for large batches, launch latency for small ones.
+#include <cooperative_groups.h>
+
 #include "ngc_common.cuh"
 #include "ptx.cuh"
 
 namespace ngc {
 namespace {
+
+namespace cg = cooperative_groups;
 
 constexpr int kMoveThreads = 256;
 
@@ -39,12 +43,12 @@ __device__ __forceinline__ int64_t move_row(const MoveParams& p, int b, int l, i
   const int32_t* row = p.page_table + ((int64_t)b * p.G + list_of(p.lists, l, h, p.Hkv)) * p.pages_cap;
   return ((int64_t)b * p.pages_cap + row[t / p.page]) * p.page + t % p.page;
 }
-// Whether pages [lo, hi) of every list of b are pages; all threads take part, each checks its share.
+// Whether an entry [lo, hi) of a list's table row is no page.
 __device__ __forceinline__ bool pages_bad(const MoveParams& p, int b, int gi, int lo, int hi) {
   const int32_t* row = p.page_table + ((int64_t)b * p.G + gi) * p.pages_cap;
-  for (int j = lo; j < hi; ++j)
-    if (row[j] < 0 || row[j] >= p.pages_cap) return true;
-  return false;
+  bool bad = false;
+  for (int j = lo; j < hi; ++j) bad |= (uint32_t)row[j] >= (uint32_t)p.pages_cap;
+  return bad;
 }
 // Length of list gi of b as the tables count lists (a length per sequence serves all of its lists).
 __device__ __forceinline__ int list_len(const MoveParams& p, int b, int gi, int n_lens) {
@@ -53,118 +57,210 @@ __device__ __forceinline__ int list_len(const MoveParams& p, int b, int gi, int 
 
 // ---------------------------------------------------------------- commit
 
-__global__ void __launch_bounds__(kMoveThreads) commit_rows_kernel(MoveParams p) {
-  const int b = blockIdx.y, tid = threadIdx.x;
+// A cluster of CTAs per sequence.  All of them check the path and the room (every list, since a sequence is committed
+// whole or not at all), copy their share of the rows, and meet at a cluster barrier: behind it nobody reads the lengths
+// any more and the first CTA writes the new ones.  One launch: for a single rollout the call is all latency.
+constexpr int kMoveVecs = 4;                    // 16-byte vectors a thread has in flight
+__global__ void __launch_bounds__(kMoveThreads) commit_kernel(MoveParams p) {
+  const cg::cluster_group cluster = cg::this_cluster();
+  __shared__ int s_path[NGC_TREE_MAX_NODES];
+  __shared__ int s_wrong;
+  const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int b = blockIdx.x / ctas, tid = threadIdx.x;
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
-  const int n = p.n_path[b];
-  const int32_t* path = p.path + (int64_t)b * p.N;
-  int status = NGC_DEV_OK;
-  if (n < 0 || n > p.N) status = NGC_DEV_BAD_TREE;
-  else
-    for (int j = tid; j < n; j += kMoveThreads)
-      if (path[j] < (j ? path[j - 1] + 1 : 0) || path[j] >= p.N) status = NGC_DEV_BAD_TREE;
-  if (__syncthreads_or(status != NGC_DEV_OK)) status = NGC_DEV_BAD_TREE;
-  const int n_lens = lists_G(p.lens_lists, p.L, p.Hkv);
-  if (status == NGC_DEV_OK) {
-    const int64_t cap = move_capacity(p, b);
-    bool full = false, bad_page = false;
-    const int lists = p.page_table ? p.G : n_lens;
-    for (int gi = tid; gi < lists; gi += kMoveThreads) {
-      const int len = list_len(p, b, gi, n_lens);
-      if (len < 0 || (int64_t)len + n > cap) full = true;
-      else if (p.page_table && n > 0) bad_page = bad_page || pages_bad(p, b, gi, len / p.page, (len + n - 1) / p.page + 1);
-    }
-    if (__syncthreads_or(full)) status = NGC_DEV_STRIP_FULL;
-    else if (__syncthreads_or(bad_page)) status = NGC_DEV_BAD_PAGE;
+  int n = p.n_path[b];
+  bool bad = n < 0 || n > p.N;
+  if (bad) n = 0;
+  if (tid < n) {
+    const int x = p.path[(int64_t)b * p.N + tid], before = tid ? p.path[(int64_t)b * p.N + tid - 1] : -1;
+    bad = x <= before || x < 0 || x >= p.N;
+    s_path[tid] = x;
   }
+  const int n_lens = lists_G(p.lens_lists, p.L, p.Hkv);
+  const int64_t cap = move_capacity(p, b);
+  bool full = false, bad_page = false;
+  const int lists = p.page_table ? p.G : n_lens;
+  for (int gi = tid; gi < lists; gi += kMoveThreads) {
+    const int len = list_len(p, b, gi, n_lens);
+    if (len < 0 || (int64_t)len + n > cap) full = true;
+    else if (p.page_table && n > 0) bad_page = bad_page || pages_bad(p, b, gi, len / p.page, (len + n - 1) / p.page + 1);
+  }
+  if (tid == 0) s_wrong = 0;
+  __syncthreads();
+  if (bad || full || bad_page) atomicOr(&s_wrong, (bad ? 1 : 0) | (full ? 2 : 0) | (bad_page ? 4 : 0));
+  __syncthreads();
+  const int wrong = s_wrong;
+  const int status = wrong & 1 ? NGC_DEV_BAD_TREE : wrong & 2 ? NGC_DEV_STRIP_FULL : wrong & 4 ? NGC_DEV_BAD_PAGE : NGC_DEV_OK;
   if (status != NGC_DEV_OK) {
     if (tid == 0) set_dev_status(p.dev_status, status);
-    return;
+    n = 0;
   }
-  // vectors of the sequence: (plane, K or V, row of the path, piece)
-  const int per_row = p.row_vecs, per_half = n * per_row;
-  const int64_t total = (int64_t)p.L * p.Hkv * 2 * per_half;
-  for (int64_t i = (int64_t)blockIdx.x * kMoveThreads + tid; i < total; i += (int64_t)gridDim.x * kMoveThreads) {
-    const int half = (int)(i / per_half), rest = (int)(i % per_half), j = rest / per_row, c = rest % per_row;
-    const int plane = half >> 1, l = plane / p.Hkv, h = plane % p.Hkv;
-    const uint4* src = (half & 1 ? p.tree_v : p.tree_k) + ((((int64_t)l * p.B + b) * p.Hkv + h) * p.N + path[j]) * per_row + c;
-    const int64_t row = move_row(p, b, l, h, move_len(p, b, l, h) + j);
-    if (NGC_IN_BOUNDS(p.dev_status, row >= 0 && row < p.rows))
-      (half & 1 ? p.v : p.k)[((int64_t)plane * p.rows + row) * per_row + c] = *src;
+  // vectors of the sequence: (plane, row of the path, piece), K and V of each
+  const int per_plane = n * p.row_vecs;
+  const int64_t total = (int64_t)p.L * p.Hkv * per_plane;
+  for (int64_t i0 = (int64_t)rank * kMoveThreads + tid; i0 < total; i0 += (int64_t)ctas * kMoveThreads * kMoveVecs) {
+    uint4 xk[kMoveVecs], xv[kMoveVecs];
+    int64_t to[kMoveVecs];
+#pragma unroll
+    for (int e = 0; e < kMoveVecs; ++e) {
+      const int64_t i = i0 + (int64_t)e * ctas * kMoveThreads;
+      to[e] = -1;
+      if (i >= total) continue;
+      const int plane = (int)(i / per_plane), rest = (int)(i % per_plane), j = rest / p.row_vecs, c = rest % p.row_vecs;
+      const int l = plane / p.Hkv, h = plane % p.Hkv;
+      const int64_t from = ((((int64_t)l * p.B + b) * p.Hkv + h) * p.N + s_path[j]) * p.row_vecs + c;
+      xk[e] = p.tree_k[from];
+      xv[e] = p.tree_v[from];
+      const int64_t row = move_row(p, b, l, h, move_len(p, b, l, h) + j);
+      if (NGC_IN_BOUNDS(p.dev_status, row >= 0 && row < p.rows)) to[e] = ((int64_t)plane * p.rows + row) * p.row_vecs + c;
+    }
+#pragma unroll
+    for (int e = 0; e < kMoveVecs; ++e)
+      if (to[e] >= 0) {
+        p.k[to[e]] = xk[e];
+        p.v[to[e]] = xv[e];
+      }
   }
-}
-
-// Lengths of the sequences that were committed: the same checks, one warp per sequence.
-__global__ void __launch_bounds__(kMoveThreads) commit_lens_kernel(MoveParams p) {
-  ptx::grid_dep_launch();
-  ptx::grid_dep_wait();          // every CTA of the copy has read the lengths
-  const int b = blockIdx.x * (kMoveThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (b >= p.B) return;
-  const int n = p.n_path[b];
-  const int32_t* path = p.path + (int64_t)b * p.N;
-  bool bad = n < 0 || n > p.N;
-  if (!bad)
-    for (int j = lane; j < n; j += 32) bad = bad || path[j] < (j ? path[j - 1] + 1 : 0) || path[j] >= p.N;
-  if (__any_sync(0xffffffffu, bad)) return;
-  const int n_lens = lists_G(p.lens_lists, p.L, p.Hkv), lists = p.page_table ? p.G : n_lens;
-  const int64_t cap = move_capacity(p, b);
-  for (int gi = lane; gi < lists; gi += 32) {
-    const int len = list_len(p, b, gi, n_lens);
-    if (len < 0 || (int64_t)len + n > cap) bad = true;
-    else if (p.page_table && n > 0) bad = bad || pages_bad(p, b, gi, len / p.page, (len + n - 1) / p.page + 1);
-  }
-  if (__any_sync(0xffffffffu, bad)) return;
-  for (int gi = lane; gi < n_lens; gi += 32) p.lens[(int64_t)b * n_lens + gi] += n;
+  cluster.sync();
+  if (rank == 0 && n > 0)
+    for (int gi = tid; gi < n_lens; gi += kMoveThreads) p.lens[(int64_t)b * n_lens + gi] += n;
 }
 
 // ---------------------------------------------------------------- fork
 
-// One CTA per (destination, plane, K or V); destinations vary fastest, so that the copies of one source strip run
-// side by side and read it from L2.
-__global__ void __launch_bounds__(kMoveThreads) fork_rows_kernel(MoveParams p) {
-  const int tid = threadIdx.x;
-  const int b = blockIdx.x % p.B, strip = blockIdx.x / p.B, isv = strip & 1, plane = strip >> 1;
-  const int l = plane / p.Hkv, h = plane % p.Hkv;
+// A source strip is read once for all of its copies: bulk copies bring up to 64 KB of it into shared memory, from where
+// bulk stores write it to every destination (a lane per destination).  No data passes through registers, and a CTA
+// of one busy warp keeps 64 KB in flight.  grid.x = (strip, chunk of its rows), chunks beyond the grid's follow in turns;
+// grid.y deals the destinations out, so that one prompt's group alone fills the GPU.
+constexpr int kForkThreads = 128;
+constexpr int kForkQuarter = 16384, kForkChunk = 4 * kForkQuarter;     // bytes
+constexpr int kForkMaxB = 65536;
+
+__global__ void __launch_bounds__(kForkThreads) fork_kernel(MoveParams p, int n_chunks) {
+  extern __shared__ __align__(128) uint8_t stage[];                    // [4][kForkQuarter]
+  __shared__ uint32_t is_source[kForkMaxB / 32];
+  __shared__ uint64_t full[4];
+  __shared__ int dst[kForkThreads], n_dst;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int strip = blockIdx.x / n_chunks, chunk0 = blockIdx.x % n_chunks, isv = strip & 1, plane = strip >> 1;
+  const int l = plane / p.Hkv, h = plane % p.Hkv, own_list = p.page_table ? list_of(p.lists, l, h, p.Hkv) : 0;
+  const bool reports = blockIdx.x == 0 && blockIdx.y == 0, sets_lens = blockIdx.x == 0;
+  const int n_lens = lists_G(p.lens_lists, p.L, p.Hkv);
+  const int row_bytes = p.row_vecs * 16, chunk_rows = kForkChunk / row_bytes, quarter_rows = kForkQuarter / row_bytes;
+  uint8_t* const buf = (uint8_t*)(isv ? p.v : p.k) + (int64_t)plane * p.rows * row_bytes;
+  if (tid == 0) {
+    for (int i = 0; i < 4; ++i) ptx::mbar_init(&full[i], 1);
+    ptx::fence_barrier_init();
+  }
+  for (int i = tid; i < (p.B + 31) / 32; i += kForkThreads) is_source[i] = 0;
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
-  const int s = p.src_of[b];
-  if (s == -1 || s == b) return;
-  int status = NGC_DEV_OK;
-  if (s < 0 || s >= p.B || (p.src_of[s] != -1 && p.src_of[s] != s)) status = NGC_DEV_BAD_SOURCE;
-  const int n_lens = lists_G(p.lens_lists, p.L, p.Hkv);
-  if (status == NGC_DEV_OK) {
-    const int64_t cap_s = move_capacity(p, s), cap_b = move_capacity(p, b);
-    bool counts = false, full = false, bad_page = false;
-    const int lists = p.page_table ? p.G : n_lens;
-    for (int gi = tid; gi < lists; gi += kMoveThreads) {
-      const int len = list_len(p, s, gi, n_lens);
-      if (len < 0 || len > cap_s) counts = true;
-      else if (len > cap_b) full = true;
-      else if (p.page_table) {
-        const int pages = (len + p.page - 1) / p.page;
-        bad_page = bad_page || pages_bad(p, s, gi, 0, pages) || pages_bad(p, b, gi, 0, pages);
+  __syncthreads();
+  for (int b = tid; b < p.B; b += kForkThreads) {
+    const int s = p.src_of[b];
+    if (s == -1 || s == b) continue;
+    if (s < 0 || s >= p.B || (p.src_of[s] != -1 && p.src_of[s] != s)) {
+      if (reports) set_dev_status(p.dev_status, NGC_DEV_BAD_SOURCE);
+    } else {
+      atomicOr(&is_source[s >> 5], 1u << (s & 31));
+    }
+  }
+  __syncthreads();
+  int turn = 0;                                 // chunks that went through the stage so far (phase of its barriers)
+  bool ok = true;
+  for (int word = 0; word < (p.B + 31) / 32; ++word)
+    for (uint32_t bits = is_source[word]; bits; bits &= bits - 1) {
+      const int s = 32 * word + __ffs(bits) - 1;
+      // the source's lengths, and its pages of this strip's list
+      const int64_t cap_s = move_capacity(p, s);
+      const int lists = p.page_table ? p.G : n_lens;
+      bool wrong = false;
+      for (int gi = tid; gi < lists; gi += kForkThreads) {
+        const int len = list_len(p, s, gi, n_lens);
+        wrong = wrong || len < 0 || len > cap_s;
+      }
+      if (__syncthreads_or(wrong)) {
+        if (reports && tid == 0) set_dev_status(p.dev_status, NGC_DEV_BAD_COUNTS);
+        continue;
+      }
+      const int len = move_len(p, s, l, h);
+      const int32_t* from = p.page_table ? p.page_table + ((int64_t)s * p.G + own_list) * p.pages_cap : nullptr;
+      const int pages = p.page_table ? (len + p.page - 1) / p.page : 0;
+      for (int j = tid; j < pages; j += kForkThreads) wrong = wrong || from[j] < 0 || from[j] >= p.pages_cap;
+      const bool bad_source_page = __syncthreads_or(wrong);
+      for (int b0 = 0; b0 < p.B; b0 += kForkThreads) {
+        // destinations among the next sequences: a thread each
+        const int b = b0 + tid;
+        if (tid == 0) n_dst = 0;
+        __syncthreads();
+        if (b < p.B && b != s && p.src_of[b] == s && (s + b) % gridDim.y == blockIdx.y) {
+          const int64_t cap_b = move_capacity(p, b);
+          bool small = false, bad_page = bad_source_page;
+          for (int gi = 0; gi < lists; ++gi) small = small || list_len(p, s, gi, n_lens) > cap_b;
+          const int32_t* to = p.page_table ? p.page_table + ((int64_t)b * p.G + own_list) * p.pages_cap : nullptr;
+          if (!small)
+            for (int j = 0; j < pages; ++j) bad_page |= (uint32_t)to[j] >= (uint32_t)p.pages_cap;
+          if (small || bad_page) set_dev_status(p.dev_status, small ? NGC_DEV_STRIP_FULL : NGC_DEV_BAD_PAGE);
+          else dst[atomicAdd(&n_dst, 1)] = b;
+          if (sets_lens && chunk0 == 0 && !small && !bad_page) {
+            // every list's pages; nobody reads a destination's lengths (a source is no destination)
+            for (int gi = 0; p.page_table && gi < p.G; ++gi) {
+              const int used = (list_len(p, s, gi, n_lens) + p.page - 1) / p.page;
+              bad_page = bad_page || pages_bad(p, s, gi, 0, used) || pages_bad(p, b, gi, 0, used);
+            }
+            if (bad_page) set_dev_status(p.dev_status, NGC_DEV_BAD_PAGE);
+            else
+              for (int gi = 0; gi < n_lens; ++gi) p.lens[(int64_t)b * n_lens + gi] = p.lens[(int64_t)s * n_lens + gi];
+          }
+        }
+        __syncthreads();
+        const int n = n_dst;
+        if (tid < 32 && n > 0) {
+          for (int r0 = chunk0 * chunk_rows; ok && r0 < len; r0 += n_chunks * chunk_rows) {
+            ptx::bulk_wait_read<0>();           // this lane's stores have read the stage
+            __syncwarp();
+            const int rows = min(chunk_rows, len - r0);
+            if (lane == 0) {
+              for (int i = 0; i * quarter_rows < rows; ++i) {
+                const int m = min(quarter_rows, rows - i * quarter_rows);
+                ptx::mbar_expect_tx(&full[i], (uint32_t)(m * row_bytes));
+                const int step = p.page_table ? p.page : m;
+                for (int r = 0; r < m; r += step) {
+                  const int t = r0 + i * quarter_rows + r;
+                  const int64_t row = p.page_table ? ((int64_t)s * p.pages_cap + from[t / p.page]) * p.page : p.seq_off[s] + t;
+                  ptx::bulk_load(stage + i * kForkQuarter + r * row_bytes, buf + row * row_bytes, (uint32_t)(min(step, m - r) * row_bytes), &full[i]);
+                }
+              }
+            }
+            __syncwarp();
+            for (int i = 0; i * quarter_rows < rows; ++i) {
+              // (a quarter that a short chunk did not use keeps its phase: it is only ever the last chunk of a strip that is
+              // short, and the phases are counted per quarter)
+              const int m = min(quarter_rows, rows - i * quarter_rows);
+              ok = ok && __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&full[i], (turn >> (8 * i)) & 1));
+              if (!ok) break;
+              for (int d = lane; d < n; d += 32) {
+                const int b2 = dst[d];
+                const int32_t* to = p.page_table ? p.page_table + ((int64_t)b2 * p.G + own_list) * p.pages_cap : nullptr;
+                const int step = p.page_table ? p.page : m;
+                for (int r = 0; r < m; r += step) {
+                  const int t = r0 + i * quarter_rows + r;
+                  const int64_t row = p.page_table ? ((int64_t)b2 * p.pages_cap + to[t / p.page]) * p.page : p.seq_off[b2] + t;
+                  if (NGC_IN_BOUNDS(p.dev_status, row >= 0 && row + min(step, m - r) <= p.rows))
+                    ptx::bulk_store(buf + row * row_bytes, stage + i * kForkQuarter + r * row_bytes, (uint32_t)(min(step, m - r) * row_bytes));
+                }
+              }
+              ptx::bulk_commit();
+              turn ^= 1 << (8 * i);
+            }
+            if (!ok && lane == 0) set_dev_status(p.dev_status, NGC_DEV_TIMEOUT);
+          }
+        }
+        __syncthreads();                        // the list may change
       }
     }
-    if (__syncthreads_or(counts)) status = NGC_DEV_BAD_COUNTS;
-    else if (__syncthreads_or(full)) status = NGC_DEV_STRIP_FULL;
-    else if (__syncthreads_or(bad_page)) status = NGC_DEV_BAD_PAGE;
-  }
-  if (status != NGC_DEV_OK) {
-    if (tid == 0) set_dev_status(p.dev_status, status);
-    return;
-  }
-  const int len = move_len(p, s, l, h);
-  uint4* buf = (isv ? p.v : p.k) + (int64_t)plane * p.rows * p.row_vecs;
-  for (int i = tid; i < len * p.row_vecs; i += kMoveThreads) {
-    const int t = i / p.row_vecs, c = i % p.row_vecs;
-    const int64_t from = move_row(p, s, l, h, t), to = move_row(p, b, l, h, t);
-    if (NGC_IN_BOUNDS(p.dev_status, from >= 0 && from < p.rows && to >= 0 && to < p.rows))
-      buf[to * p.row_vecs + c] = buf[from * p.row_vecs + c];
-  }
-  // nobody reads a destination's lengths (a source is no destination)
-  if (strip == 0)
-    for (int gi = tid; gi < n_lens; gi += kMoveThreads) p.lens[(int64_t)b * n_lens + gi] = p.lens[(int64_t)s * n_lens + gi];
+  if (tid < 32) ptx::bulk_wait<0>();            // every store has been written
 }
 
 // ---------------------------------------------------------------- host side
@@ -185,12 +281,12 @@ int commit_impl(const ngc_cache* c, const PagedView& pv, const void* tree_k, con
   if (N > NGC_TREE_MAX_NODES) return NGC_ERR_UNSUPPORTED;
   MoveParams p = move_params(c, pv, dev_status);
   p.tree_k = (const uint4*)tree_k; p.tree_v = (const uint4*)tree_v; p.path = path; p.n_path = n_path; p.N = N;
-  if (c->B > 65535) return NGC_ERR_UNSUPPORTED;
-  const int64_t most = (int64_t)c->L * c->Hkv * 2 * N * p.row_vecs;
-  int64_t per_seq = (most + kMoveThreads * 4 - 1) / (kMoveThreads * 4);
-  if (per_seq > 16) per_seq = 16;
-  NGC_CUDA_TRY(launch_pdl(commit_rows_kernel, dim3((unsigned)per_seq, (unsigned)c->B), dim3(kMoveThreads), 0, stream, p));
-  NGC_CUDA_TRY(launch_pdl(commit_lens_kernel, dim3((unsigned)((c->B + 7) / 8)), dim3(kMoveThreads), 0, stream, p));
+  // CTAs per sequence: enough for one round of vectors if every node were accepted, at most 8
+  const int64_t most = (int64_t)c->L * c->Hkv * N * p.row_vecs;
+  unsigned cluster = 1;
+  while (cluster < 8 && most > (int64_t)cluster * kMoveThreads * kMoveVecs) cluster *= 2;
+  if ((int64_t)c->B * cluster > 0x7fffffffLL) return NGC_ERR_UNSUPPORTED;
+  NGC_CUDA_TRY(launch_pdl_cluster(commit_kernel, dim3((unsigned)c->B * cluster), dim3(kMoveThreads), cluster, stream, p));
   return NGC_OK;
 }
 
@@ -199,9 +295,20 @@ int fork_impl(const ngc_cache* c, const PagedView& pv, const int32_t* src_of, in
   if ((((uintptr_t)c->k | (uintptr_t)c->v) & 15) != 0) return NGC_ERR_INVALID_ARG;
   MoveParams p = move_params(c, pv, dev_status);
   p.src_of = src_of;
-  const int64_t grid = (int64_t)c->B * c->L * c->Hkv * 2;
-  if (grid > 0x7fffffffLL) return NGC_ERR_UNSUPPORTED;
-  NGC_CUDA_TRY(launch_pdl(fork_rows_kernel, dim3((unsigned)grid), dim3(kMoveThreads), 0, stream, p));
+  if (c->B > kForkMaxB) return NGC_ERR_UNSUPPORTED;
+  static PerDeviceOnce attr_once;
+  const int rc = attr_once.run([] { return cudaFuncSetAttribute(fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kForkChunk); });
+  if (rc != NGC_OK) return rc;
+  // two rounds of CTAs (three fit an SM): first over the rows of the strips, then over the destinations
+  const int64_t strips = (int64_t)c->L * c->Hkv * 2, want = 2 * 3 * 148;
+  const int64_t most_chunks = ((int64_t)c->max_len * p.row_vecs * 16 + kForkChunk - 1) / kForkChunk;
+  int64_t chunks = (want + strips - 1) / strips;
+  if (chunks > most_chunks) chunks = most_chunks;
+  if (chunks < 1) chunks = 1;
+  int64_t deals = (want + strips * chunks - 1) / (strips * chunks);
+  if (deals > c->B) deals = c->B;
+  if (strips * chunks > 0x7fffffffLL) return NGC_ERR_UNSUPPORTED;
+  NGC_CUDA_TRY(launch_pdl(fork_kernel, dim3((unsigned)(strips * chunks), (unsigned)deals), dim3(kForkThreads), kForkChunk, stream, p, (int)chunks));
   return NGC_OK;
 }
 

@@ -86,6 +86,16 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int x, int 
                ::"l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(src))
                : "memory");
 }
+// Untiled bulk copies of `bytes` (a multiple of 16, both addresses 16-byte aligned): global -> shared with completion on an
+// mbarrier, shared -> global tracked by the issuing thread's bulk groups.
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
+__device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_u32(src)), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 // Wait until at most N of this thread's bulk groups still READ their shared-memory source.
 template <int N> __device__ __forceinline__ void bulk_wait_read() {

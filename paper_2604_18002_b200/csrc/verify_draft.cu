@@ -1,21 +1,33 @@
 // ngc_verify_draft: multi-round speculative sampling over a drafted tree.
 //
-// One CTA per sequence.  Nodes are numbered with parents before children, so one ascending sweep over
-// the nodes visits the children of the current node in index order.  With draft rows, k rejections at
-// a node leave w = max(p - c q, 0): the max of nested subtractions of non-negative multiples of q is the
-// subtraction of their sum, so one number c stands for the whole residual and nothing is stored.  All
-// decisions and sums are in fp64 (fp32 inputs are exact in it); multiplications and subtractions are
-// kept apart (no fused multiply-add), so that the arithmetic is the one written down.
-// The final draw is an inverse CDF: every warp owns a contiguous range of the vocabulary, the sums of the
-// ranges give the range that the target falls into, and its warp walks it.
+// A cluster of up to 8 CTAs per sequence; every CTA owns a slice of the vocabulary, every warp a contiguous range of
+// the slice.  All CTAs take the same walk from the same numbers, so only sums over the vocabulary are exchanged (one
+// number per CTA through distributed shared memory, added in rank order).
+//
+// Nodes are numbered with parents before children, so one ascending sweep over the nodes visits the children of
+// the current node in index order.  What a test needs of the big rows, p(x) and q(x) at the parent, is fetched for
+// all nodes at once before the walk: the walk itself reads shared memory only.  With draft rows, k rejections at
+// a node leave w = max(p - c q, 0): the max of nested subtractions of non-negative multiples of q is the subtraction
+// of their sum, so one number c stands for the whole residual and nothing is stored.  The sum after a rejection
+// is also the one that the final draw needs; a vocabulary row is read again only if a second child is rejected.
+//
+// All decisions and sums are in fp64 (fp32 inputs are exact in it); multiplications and subtractions are kept apart (no
+// fused multiply-add), so that the arithmetic is the one written down.  The final draw is an inverse CDF: the sums
+// per CTA and per warp lead to a range of about vocab / 128 tokens, which the CTA that owns it scans.
+#include <cooperative_groups.h>
+
 #include "ngc_common.cuh"
 #include "ptx.cuh"
 
 namespace ngc {
 namespace {
 
+namespace cg = cooperative_groups;
+
 enum { kModeDraft = 0, kModePoint = 1, kModeGreedy = 2 };
-constexpr int kVerifyThreads = 1024, kVerifyWarps = kVerifyThreads / 32;
+constexpr int kVerifyThreads = 512, kVerifyWarps = kVerifyThreads / 32;
+constexpr int kMaxCluster = 8;
+constexpr int kUnroll = 8;                           // loads a lane has in flight per row
 
 struct VerifyParams {
   const int32_t* tokens;
@@ -33,102 +45,159 @@ struct VerifyParams {
 
 struct VerifyShared {
   int parent[NGC_TREE_MAX_NODES], token[NGC_TREE_MAX_NODES], path[NGC_TREE_MAX_NODES], tried[NGC_TREE_MAX_NODES];
-  float u[NGC_TREE_MAX_NODES];
+  float u[NGC_TREE_MAX_NODES], p[NGC_TREE_MAX_NODES], q[NGC_TREE_MAX_NODES];     // p, q: of the node's token, at its parent
   double warp_sum[kVerifyWarps];
   float warp_max[kVerifyWarps];
   int warp_arg[kVerifyWarps];
-  int next;
+  // what the other CTAs read; two of each, so that one cluster barrier per exchange is enough
+  double cta_sum[2];
+  float cta_max[2];
+  int cta_arg[2];
+  int last;
 };
 
-// What is left of token x at the current node.
+// What is left of the current node's row after the rejections so far.
 template <int MODE> struct Residual {
   const float* p;
   const float* q;
   const int* tried;
   double c;
   int n_tried;
-  __device__ __forceinline__ double at(int x) const {
-    double w = (double)p[x];
+  __device__ __forceinline__ double of(int x, float pv, float qv) const {
+    double w = (double)pv;
     if (MODE == kModeDraft) {
-      w = __dsub_rn(w, __dmul_rn(c, (double)q[x]));
+      w = __dsub_rn(w, __dmul_rn(c, (double)qv));
       return w < 0.0 ? 0.0 : w;                      // a NaN stays one
     }
     for (int e = 0; e < n_tried; ++e)
       if (tried[e] == x) return 0.0;
     return w;
   }
+  __device__ __forceinline__ bool with_q() const { return MODE == kModeDraft && c != 0.0; }
+  __device__ __forceinline__ double at(int x) const { return of(x, p[x], with_q() ? q[x] : 0.f); }
 };
 
-// Sum over the vocabulary; the warps' shares stay in sh.warp_sum.  Every thread gets the same value.
-template <int MODE> __device__ double residual_sum(const Residual<MODE>& w, int lo, int hi, VerifyShared& sh) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+// Sum over this warp's range.
+template <int MODE> __device__ __forceinline__ double range_sum(const Residual<MODE>& w, int lo, int hi) {
+  const int lane = threadIdx.x & 31;
+  const bool with_q = w.with_q();
   double s = 0.0;
-  for (int x = lo + lane; x < hi; x += 32) s += w.at(x);
-  s = warp_sum(s);
-  __syncthreads();
-  if (lane == 0) sh.warp_sum[warp] = s;
-  __syncthreads();
-  s = 0.0;
-  for (int i = 0; i < kVerifyWarps; ++i) s += sh.warp_sum[i];
-  return s;
-}
-
-// argmax of a row (the smallest index of equal values), or -1 if the row holds a NaN.
-__device__ int row_argmax(const float* p, int lo, int hi, VerifyShared& sh) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  float best = -INFINITY;
-  int arg = 0x7fffffff;
-  bool nan = false;
-  for (int x = lo + lane; x < hi; x += 32) {
-    const float v = p[x];
-    nan = nan || v != v;
-    if (v > best || arg == 0x7fffffff) { best = v; arg = x; }
-  }
+  for (int x0 = lo + lane; x0 < hi; x0 += 32 * kUnroll) {
+    float pv[kUnroll], qv[kUnroll];
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float v = __shfl_xor_sync(0xffffffffu, best, o);
-    const int a = __shfl_xor_sync(0xffffffffu, arg, o);
-    if (v > best || (v == best && a < arg)) { best = v; arg = a; }
+    for (int e = 0; e < kUnroll; ++e) {
+      const int x = x0 + 32 * e;
+      pv[e] = x < hi ? w.p[x] : 0.f;
+      qv[e] = with_q && x < hi ? w.q[x] : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < kUnroll; ++e) s += w.of(x0 + 32 * e, pv[e], qv[e]);
   }
-  if (__syncthreads_or(nan)) return -1;
-  if (lane == 0) { sh.warp_max[warp] = best; sh.warp_arg[warp] = arg; }
-  __syncthreads();
-  best = sh.warp_max[0];
-  arg = sh.warp_arg[0];
-  for (int i = 1; i < kVerifyWarps; ++i) {
-    const float v = sh.warp_max[i];
-    const int a = sh.warp_arg[i];
-    if (v > best || (v == best && a < arg)) { best = v; arg = a; }
-  }
-  return arg;
+  return warp_sum(s);
 }
 
-template <int MODE> __global__ void __launch_bounds__(kVerifyThreads) verify_draft_kernel(VerifyParams p) {
+template <int MODE> __global__ void __launch_bounds__(kVerifyThreads, 2) verify_draft_kernel(VerifyParams p) {
   __shared__ VerifyShared sh;
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const cg::cluster_group cluster = cg::this_cluster();
+  const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int b = blockIdx.x / ctas, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
   int n = p.n_nodes ? p.n_nodes[b] : p.N;
   bool bad = n < 0 || n > p.N;
   if (bad) n = 0;
-  for (int i = tid; i < n; i += kVerifyThreads) {
-    const int pa = p.parent[(int64_t)b * p.N + i], x = p.tokens[(int64_t)b * p.N + i];
-    bad = bad || (i == 0 ? pa != -1 : (pa < 0 || pa >= i || x < 0 || x >= p.vocab));
-    sh.parent[i] = pa;
-    sh.token[i] = x;
-    if (MODE != kModeGreedy) sh.u[i] = p.uniforms[(int64_t)b * p.N + i];
+  const int64_t row0 = (int64_t)b * p.N * p.vocab;
+  if (tid < n) {
+    const int pa = p.parent[(int64_t)b * p.N + tid], x = p.tokens[(int64_t)b * p.N + tid];
+    if (tid == 0) bad = pa != -1;
+    else bad = pa < 0 || pa >= tid || x < 0 || x >= p.vocab;
+    sh.parent[tid] = pa;
+    sh.token[tid] = x;
+    if (MODE != kModeGreedy) {
+      sh.u[tid] = p.uniforms[(int64_t)b * p.N + tid];
+      if (tid > 0 && !bad) {
+        sh.p[tid] = p.target[row0 + (int64_t)pa * p.vocab + x];
+        if (MODE == kModeDraft) sh.q[tid] = p.draft[row0 + (int64_t)pa * p.vocab + x];
+      }
+    }
   }
   int status = __syncthreads_or(bad) ? NGC_DEV_BAD_TREE : NGC_DEV_OK;
 
-  const int per_warp = (p.vocab + kVerifyWarps - 1) / kVerifyWarps;
-  const int lo = min(p.vocab, warp * per_warp), hi = min(p.vocab, lo + per_warp);
+  // slices of the CTAs, ranges of the warps
+  const int per_cta = (p.vocab + ctas - 1) / ctas, cta_lo = min(p.vocab, rank * per_cta), cta_hi = min(p.vocab, cta_lo + per_cta);
+  const int per_warp = (per_cta + kVerifyWarps - 1) / kVerifyWarps;
+  const int lo = min(cta_hi, cta_lo + warp * per_warp), hi = min(cta_hi, lo + per_warp);
+  int exchange = 0;
+
+  // sum of a residual over the vocabulary: the same value in every thread of the cluster; the warps' and CTAs' shares stay
+  auto vocab_sum = [&](const Residual<MODE>& w) {
+    const double s = range_sum(w, lo, hi);
+    __syncthreads();
+    if (lane == 0) sh.warp_sum[warp] = s;
+    __syncthreads();
+    if (tid == 0) {
+      double t = 0.0;
+      for (int i = 0; i < kVerifyWarps; ++i) t += sh.warp_sum[i];
+      sh.cta_sum[exchange & 1] = t;
+    }
+    cluster.sync();
+    double total = 0.0;
+    for (int i = 0; i < ctas; ++i) total += cluster.map_shared_rank(sh.cta_sum, i)[exchange & 1];
+    ++exchange;
+    return total;
+  };
+  // argmax of a row (the smallest index of equal values), or -1 if the row holds a NaN
+  auto row_argmax = [&](const float* row) {
+    float best = -INFINITY;
+    int arg = 0x7fffffff;
+    bool nan = false;
+    for (int x0 = lo + lane; x0 < hi; x0 += 32 * kUnroll) {
+      float v[kUnroll];
+#pragma unroll
+      for (int e = 0; e < kUnroll; ++e) v[e] = x0 + 32 * e < hi ? row[x0 + 32 * e] : -INFINITY;
+#pragma unroll
+      for (int e = 0; e < kUnroll; ++e) {
+        nan = nan || v[e] != v[e];
+        if (x0 + 32 * e < hi && (v[e] > best || arg == 0x7fffffff)) { best = v[e]; arg = x0 + 32 * e; }
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const float v = __shfl_xor_sync(0xffffffffu, best, o);
+      const int a = __shfl_xor_sync(0xffffffffu, arg, o);
+      if (v > best || (v == best && a < arg)) { best = v; arg = a; }
+    }
+    nan = __syncthreads_or(nan);
+    if (lane == 0) { sh.warp_max[warp] = best; sh.warp_arg[warp] = arg; }
+    __syncthreads();
+    if (tid == 0) {
+      for (int i = 1; i < kVerifyWarps; ++i)
+        if (sh.warp_max[i] > best || (sh.warp_max[i] == best && sh.warp_arg[i] < arg)) { best = sh.warp_max[i]; arg = sh.warp_arg[i]; }
+      sh.cta_max[exchange & 1] = best;
+      sh.cta_arg[exchange & 1] = nan ? -1 : arg;
+    }
+    cluster.sync();
+    best = -INFINITY;
+    arg = 0x7fffffff;
+    nan = false;
+    for (int i = 0; i < ctas; ++i) {
+      const float v = cluster.map_shared_rank(sh.cta_max, i)[exchange & 1];
+      const int a = cluster.map_shared_rank(sh.cta_arg, i)[exchange & 1];
+      nan = nan || a < 0;
+      if (v > best || (v == best && a < arg)) { best = v; arg = a; }
+    }
+    ++exchange;
+    return nan ? -1 : arg;
+  };
+
   int n_path = 0, next = -1;
+  bool draws = false;                                // this CTA holds the token of the final draw
   if (status == NGC_DEV_OK && n > 0) {
-    const int64_t row0 = (int64_t)b * p.N * p.vocab;
     int cur = 0;
     double mass = 1.0;
+    bool summed = false;                             // mass is the sum of w as it stands, its shares are in shared memory
     Residual<MODE> w = {p.target + row0, MODE == kModeDraft ? p.draft + row0 : nullptr, sh.tried, 0.0, 0};
-    int best = MODE == kModeGreedy ? row_argmax(w.p, lo, hi, sh) : 0;
+    int best = MODE == kModeGreedy ? row_argmax(w.p) : 0;
     if (tid == 0) sh.path[0] = 0;
     n_path = 1;
     for (int i = 1; i < n && status == NGC_DEV_OK && best >= 0; ++i) {
@@ -138,12 +207,13 @@ template <int MODE> __global__ void __launch_bounds__(kVerifyThreads) verify_dra
       if (MODE == kModeGreedy) {
         ok = x == best;
       } else {
-        const double wx = w.at(x), u = (double)sh.u[i];
-        ok = MODE == kModeDraft ? __dmul_rn(__dmul_rn(u, (double)w.q[x]), mass) < wx : __dmul_rn(u, mass) < wx;
+        const double wx = w.of(x, sh.p[i], MODE == kModeDraft ? sh.q[i] : 0.f), u = (double)sh.u[i];
+        ok = MODE == kModeDraft ? __dmul_rn(__dmul_rn(u, (double)sh.q[i]), mass) < wx : __dmul_rn(u, mass) < wx;
         if (!ok && MODE == kModeDraft) {
           const double c = w.c;
           w.c = __dadd_rn(c, mass);
-          const double rest = residual_sum(w, lo, hi, sh);
+          const double rest = vocab_sum(w);
+          summed = rest > 0.0;
           if (!isfinite(rest)) status = NGC_DEV_BAD_PROBS;
           else if (rest > 0.0) mass = rest;
           else w.c = c;
@@ -151,7 +221,7 @@ template <int MODE> __global__ void __launch_bounds__(kVerifyThreads) verify_dra
           const double rest = __dsub_rn(mass, wx);
           if (rest > 0.0) {
             mass = rest;
-            __syncthreads();                         // (reads of the list by w.at above are done)
+            __syncthreads();                         // (reads of the list by w.of above are done)
             if (tid == 0) sh.tried[w.n_tried] = x;
             __syncthreads();
             ++w.n_tried;
@@ -167,57 +237,92 @@ template <int MODE> __global__ void __launch_bounds__(kVerifyThreads) verify_dra
         w.c = 0.0;
         w.n_tried = 0;
         mass = 1.0;
-        if (MODE == kModeGreedy) best = row_argmax(w.p, lo, hi, sh);
+        summed = false;
+        if (MODE == kModeGreedy) best = row_argmax(w.p);
       }
     }
     if (MODE == kModeGreedy) {
       next = best;
+      draws = rank == 0;
       if (best < 0) status = NGC_DEV_BAD_PROBS;
     } else if (status == NGC_DEV_OK) {
-      const double total = residual_sum(w, lo, hi, sh);
+      const double total = summed ? mass : vocab_sum(w);
       if (!isfinite(total) || !(total > 0.0)) {
         status = NGC_DEV_BAD_PROBS;
       } else {
+        // the CTA and the warp range that the target falls into; rounding may leave it at the very end: then the last
+        // token with mass
         double t = __dmul_rn((double)sh.u[0], total), before = 0.0;
-        int own = -1, last = 0;                      // the range the target falls into; the last one with mass
-        for (int i = 0; i < kVerifyWarps; ++i) {
-          const double s = sh.warp_sum[i];
-          if (s > 0.0) last = i;
+        int own = -1, last = 0;
+        double last_before = 0.0;
+        for (int i = 0; i < ctas; ++i) {
+          const double s = cluster.map_shared_rank(sh.cta_sum, i)[(exchange - 1) & 1];
+          if (s > 0.0) { last = i; last_before = before; }
           if (own < 0 && before + s > t) own = i;
           if (own < 0) before += s;
         }
-        if (own < 0) { own = last; t = INFINITY; }   // rounding left the target at the very end: the last token with mass
-        if (warp == own) {
-          int hit = -1, tail = lo;
-          double run = before;
-          for (int x0 = lo; x0 < hi; x0 += 32) {
-            const double wx = x0 + lane < hi ? w.at(x0 + lane) : 0.0;
-            double c = wx;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-              const double y = __shfl_up_sync(0xffffffffu, c, o);
-              if (lane >= o) c += y;
-            }
-            const uint32_t over = __ballot_sync(0xffffffffu, run + c > t), live = __ballot_sync(0xffffffffu, wx > 0.0);
-            if (over) { hit = x0 + __ffs(over) - 1; break; }
-            if (live) tail = x0 + 31 - __clz(live);
-            run += __shfl_sync(0xffffffffu, c, 31);
+        if (own < 0) { own = last; before = last_before; t = INFINITY; }
+        draws = rank == own;
+        if (draws) {
+          int range = -1;
+          last = 0;
+          for (int i = 0; i < kVerifyWarps; ++i) {
+            const double s = sh.warp_sum[i];
+            if (s > 0.0) { last = i; last_before = before; }
+            if (range < 0 && before + s > t) range = i;
+            if (range < 0) before += s;
           }
-          if (lane == 0) sh.next = hit >= 0 ? hit : tail;
+          if (range < 0) { range = last; before = last_before; t = INFINITY; }
+          // the whole CTA scans the range: a run of consecutive tokens per thread
+          const int r_lo = min(cta_hi, cta_lo + range * per_warp), r_hi = min(cta_hi, r_lo + per_warp);
+          const int run = (per_warp + kVerifyThreads - 1) / kVerifyThreads;
+          const int x0 = min(r_hi, r_lo + tid * run), x1 = min(r_hi, x0 + run);
+          double s = 0.0;
+          int tail = -1;
+          for (int x = x0; x < x1; ++x) {
+            const double wx = w.at(x);
+            s += wx;
+            if (wx > 0.0) tail = x;
+          }
+          double c = s;
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) {
+            const double y = __shfl_up_sync(0xffffffffu, c, o);
+            if (lane >= o) c += y;
+          }
+          __syncthreads();                           // (warp_sum has been read)
+          if (tid == 0) { sh.last = -1; sh.warp_arg[0] = 0x7fffffff; }
+          if (lane == 31) sh.warp_sum[warp] = c;
+          __syncthreads();
+          for (int i = 0; i < warp; ++i) before += sh.warp_sum[i];
+          double upto = before + (c - s);
+          int hit = -1;
+          if (upto + s > t)
+            for (int x = x0; x < x1 && hit < 0; ++x) {
+              upto += w.at(x);
+              if (upto > t) hit = x;
+            }
+          if (hit >= 0) atomicMin(&sh.warp_arg[0], hit);
+          if (tail >= 0) atomicMax(&sh.last, tail);
+          __syncthreads();
+          next = sh.warp_arg[0] != 0x7fffffff ? sh.warp_arg[0] : sh.last;
         }
-        __syncthreads();
-        next = sh.next;
       }
     }
   }
-  if (status != NGC_DEV_OK) {
-    if (tid == 0) set_dev_status(p.dev_status, status);
+  if (status != NGC_DEV_OK || n == 0) {
+    if (tid == 0 && status != NGC_DEV_OK) set_dev_status(p.dev_status, status);
     n_path = 0;
     next = -1;
+    draws = rank == 0;
   }
   __syncthreads();
-  for (int i = tid; i < p.N; i += kVerifyThreads) p.path[(int64_t)b * p.N + i] = i < n_path ? sh.path[i] : -1;
-  if (tid == 0) { p.n_path[b] = n_path; p.next_token[b] = next; }
+  if (rank == 0) {
+    for (int i = tid; i < p.N; i += kVerifyThreads) p.path[(int64_t)b * p.N + i] = i < n_path ? sh.path[i] : -1;
+    if (tid == 0) p.n_path[b] = n_path;
+  }
+  if (draws && tid == 0) p.next_token[b] = next;
+  cluster.sync();                                    // nobody leaves while its sums may still be read
 }
 
 }  // namespace
@@ -232,10 +337,14 @@ extern "C" int ngc_verify_draft(const int32_t* tokens, const int32_t* parent, co
     return NGC_ERR_INVALID_ARG;
   if (N > NGC_TREE_MAX_NODES) return NGC_ERR_UNSUPPORTED;
   const VerifyParams p = {tokens, parent, n_nodes, target_probs, draft_probs, uniforms, path, n_path, next_token, dev_status, N, vocab};
-  const dim3 grid((unsigned)B), block(kVerifyThreads);
+  // CTAs per sequence: a slice of at least 2048 tokens each, at most 8
+  int cluster = 1;
+  while (cluster < kMaxCluster && (int64_t)vocab >= 4096LL * cluster) cluster *= 2;
+  if ((int64_t)B * cluster > 0x7fffffffLL) return NGC_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)(B * cluster)), block(kVerifyThreads);
   cudaStream_t s = (cudaStream_t)stream;
-  if (greedy) NGC_CUDA_TRY(launch_pdl(verify_draft_kernel<kModeGreedy>, grid, block, 0, s, p));
-  else if (draft_probs) NGC_CUDA_TRY(launch_pdl(verify_draft_kernel<kModeDraft>, grid, block, 0, s, p));
-  else NGC_CUDA_TRY(launch_pdl(verify_draft_kernel<kModePoint>, grid, block, 0, s, p));
+  if (greedy) NGC_CUDA_TRY(launch_pdl_cluster(verify_draft_kernel<kModeGreedy>, grid, block, cluster, s, p));
+  else if (draft_probs) NGC_CUDA_TRY(launch_pdl_cluster(verify_draft_kernel<kModeDraft>, grid, block, cluster, s, p));
+  else NGC_CUDA_TRY(launch_pdl_cluster(verify_draft_kernel<kModePoint>, grid, block, cluster, s, p));
   return NGC_OK;
 }

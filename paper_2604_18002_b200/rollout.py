@@ -122,7 +122,7 @@ class NgcRollout:
         ngc.ngc_verify_draft(tokens, parent, target_probs, uniforms, path, n_path, next_token, draft_probs, n_nodes, greedy,
                              status=self.status)
         ngc.ngc_commit_draft(self.cache, tree_k, tree_v, path, n_path, status=self.status)
-        self.launches += 3
+        self.launches += 2
 
     def check_status(self):
         code = int(self.status.item())
