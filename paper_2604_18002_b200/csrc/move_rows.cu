@@ -69,20 +69,23 @@ __global__ void __launch_bounds__(kMoveThreads) commit_kernel(MoveParams p) {
   const int b = blockIdx.x / ctas, tid = threadIdx.x;
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
-  int n = p.n_path[b];
+  // path, lengths and path length in one round of loads, the pages in a second
+  const int n_lens = lists_G(p.lens_lists, p.L, p.Hkv), lists = p.page_table ? p.G : n_lens;
+  int n = p.n_path[b], x = 0, before = -1, len = tid < lists ? list_len(p, b, tid, n_lens) : 0;
+  if (tid < p.N) {
+    x = p.path[(int64_t)b * p.N + tid];
+    if (tid > 0) before = p.path[(int64_t)b * p.N + tid - 1];
+  }
+  const int64_t cap = move_capacity(p, b);
   bool bad = n < 0 || n > p.N;
   if (bad) n = 0;
   if (tid < n) {
-    const int x = p.path[(int64_t)b * p.N + tid], before = tid ? p.path[(int64_t)b * p.N + tid - 1] : -1;
     bad = x <= before || x < 0 || x >= p.N;
     s_path[tid] = x;
   }
-  const int n_lens = lists_G(p.lens_lists, p.L, p.Hkv);
-  const int64_t cap = move_capacity(p, b);
   bool full = false, bad_page = false;
-  const int lists = p.page_table ? p.G : n_lens;
   for (int gi = tid; gi < lists; gi += kMoveThreads) {
-    const int len = list_len(p, b, gi, n_lens);
+    if (gi != tid) len = list_len(p, b, gi, n_lens);
     if (len < 0 || (int64_t)len + n > cap) full = true;
     else if (p.page_table && n > 0) bad_page = bad_page || pages_bad(p, b, gi, len / p.page, (len + n - 1) / p.page + 1);
   }
@@ -197,24 +200,34 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(MoveParams p, int n_
         if (b < p.B && b != s && p.src_of[b] == s && (s + b) % gridDim.y == blockIdx.y) {
           const int64_t cap_b = move_capacity(p, b);
           bool small = false, bad_page = bad_source_page;
-          for (int gi = 0; gi < lists; ++gi) small = small || list_len(p, s, gi, n_lens) > cap_b;
+          for (int gi = 0; gi < n_lens; ++gi) small |= list_len(p, s, gi, n_lens) > cap_b;
           const int32_t* to = p.page_table ? p.page_table + ((int64_t)b * p.G + own_list) * p.pages_cap : nullptr;
           if (!small)
             for (int j = 0; j < pages; ++j) bad_page |= (uint32_t)to[j] >= (uint32_t)p.pages_cap;
           if (small || bad_page) set_dev_status(p.dev_status, small ? NGC_DEV_STRIP_FULL : NGC_DEV_BAD_PAGE);
           else dst[atomicAdd(&n_dst, 1)] = b;
-          if (sets_lens && chunk0 == 0 && !small && !bad_page) {
-            // every list's pages; nobody reads a destination's lengths (a source is no destination)
-            for (int gi = 0; p.page_table && gi < p.G; ++gi) {
-              const int used = (list_len(p, s, gi, n_lens) + p.page - 1) / p.page;
-              bad_page = bad_page || pages_bad(p, s, gi, 0, used) || pages_bad(p, b, gi, 0, used);
-            }
-            if (bad_page) set_dev_status(p.dev_status, NGC_DEV_BAD_PAGE);
-            else
-              for (int gi = 0; gi < n_lens; ++gi) p.lens[(int64_t)b * n_lens + gi] = p.lens[(int64_t)s * n_lens + gi];
-          }
         }
         __syncthreads();
+        if (sets_lens) {
+          // the lengths, if every list's pages are pages; nobody reads a destination's lengths (a source is no destination)
+          for (int d = 0; d < n_dst; ++d) {
+            const int b2 = dst[d];
+            bool bad_page = false;
+            if (p.page_table) {
+              const int64_t entries = (int64_t)p.G * p.pages_cap;
+              for (int64_t j = tid; j < entries; j += kForkThreads) {
+                const int gi = (int)(j / p.pages_cap), used = (list_len(p, s, gi, n_lens) + p.page - 1) / p.page;
+                bad_page |= j % p.pages_cap < used && ((uint32_t)p.page_table[s * entries + j] >= (uint32_t)p.pages_cap ||
+                                                       (uint32_t)p.page_table[b2 * entries + j] >= (uint32_t)p.pages_cap);
+              }
+            }
+            if (__syncthreads_or(bad_page)) {
+              if (tid == 0) set_dev_status(p.dev_status, NGC_DEV_BAD_PAGE);
+            } else {
+              for (int gi = tid; gi < n_lens; gi += kForkThreads) p.lens[(int64_t)b2 * n_lens + gi] = p.lens[(int64_t)s * n_lens + gi];
+            }
+          }
+        }
         const int n = n_dst;
         if (tid < 32 && n > 0) {
           for (int r0 = chunk0 * chunk_rows; ok && r0 < len; r0 += n_chunks * chunk_rows) {
@@ -281,10 +294,11 @@ int commit_impl(const ngc_cache* c, const PagedView& pv, const void* tree_k, con
   if (N > NGC_TREE_MAX_NODES) return NGC_ERR_UNSUPPORTED;
   MoveParams p = move_params(c, pv, dev_status);
   p.tree_k = (const uint4*)tree_k; p.tree_v = (const uint4*)tree_v; p.path = path; p.n_path = n_path; p.N = N;
-  // CTAs per sequence: enough for one round of vectors if every node were accepted, at most 8
+  // CTAs per sequence: at most 8, no more than a round of vectors would occupy if every node were accepted, nor than
+  // about one round of CTAs in all (each of them repeats the checks)
   const int64_t most = (int64_t)c->L * c->Hkv * N * p.row_vecs;
   unsigned cluster = 1;
-  while (cluster < 8 && most > (int64_t)cluster * kMoveThreads * kMoveVecs) cluster *= 2;
+  while (cluster < 8 && most > (int64_t)cluster * kMoveThreads * kMoveVecs && (int64_t)c->B * cluster * 2 <= 4 * 148) cluster *= 2;
   if ((int64_t)c->B * cluster > 0x7fffffffLL) return NGC_ERR_UNSUPPORTED;
   NGC_CUDA_TRY(launch_pdl_cluster(commit_kernel, dim3((unsigned)c->B * cluster), dim3(kMoveThreads), cluster, stream, p));
   return NGC_OK;

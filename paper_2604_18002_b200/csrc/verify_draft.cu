@@ -13,7 +13,7 @@
 //
 // All decisions and sums are in fp64 (fp32 inputs are exact in it); multiplications and subtractions are kept apart (no
 // fused multiply-add), so that the arithmetic is the one written down.  The final draw is an inverse CDF: the sums
-// per CTA and per warp lead to a range of about vocab / 128 tokens, which the CTA that owns it scans.
+// per CTA and per warp lead to a range of about vocab / 64 tokens, which the CTA that owns it scans.
 #include <cooperative_groups.h>
 
 #include "ngc_common.cuh"
@@ -25,7 +25,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 enum { kModeDraft = 0, kModePoint = 1, kModeGreedy = 2 };
-constexpr int kVerifyThreads = 512, kVerifyWarps = kVerifyThreads / 32;
+constexpr int kMaxWarps = 16;                        // per CTA
 constexpr int kMaxCluster = 8;
 constexpr int kUnroll = 8;                           // loads a lane has in flight per row
 
@@ -46,9 +46,9 @@ struct VerifyParams {
 struct VerifyShared {
   int parent[NGC_TREE_MAX_NODES], token[NGC_TREE_MAX_NODES], path[NGC_TREE_MAX_NODES], tried[NGC_TREE_MAX_NODES];
   float u[NGC_TREE_MAX_NODES], p[NGC_TREE_MAX_NODES], q[NGC_TREE_MAX_NODES];     // p, q: of the node's token, at its parent
-  double warp_sum[kVerifyWarps];
-  float warp_max[kVerifyWarps];
-  int warp_arg[kVerifyWarps];
+  double warp_sum[kMaxWarps];
+  float warp_max[kMaxWarps];
+  int warp_arg[kMaxWarps];
   // what the other CTAs read; two of each, so that one cluster barrier per exchange is enough
   double cta_sum[2];
   float cta_max[2];
@@ -64,14 +64,15 @@ template <int MODE> struct Residual {
   double c;
   int n_tried;
   __device__ __forceinline__ double of(int x, float pv, float qv) const {
-    double w = (double)pv;
-    if (MODE == kModeDraft) {
-      w = __dsub_rn(w, __dmul_rn(c, (double)qv));
-      return w < 0.0 ? 0.0 : w;                      // a NaN stays one
+    const double w = (double)pv;
+    if constexpr (MODE == kModeDraft) {
+      const double rest = __dsub_rn(w, __dmul_rn(c, (double)qv));
+      return rest < 0.0 ? 0.0 : rest;                // a NaN stays one
+    } else {
+      for (int e = 0; e < n_tried; ++e)
+        if (tried[e] == x) return 0.0;
+      return w;
     }
-    for (int e = 0; e < n_tried; ++e)
-      if (tried[e] == x) return 0.0;
-    return w;
   }
   __device__ __forceinline__ bool with_q() const { return MODE == kModeDraft && c != 0.0; }
   __device__ __forceinline__ double at(int x) const { return of(x, p[x], with_q() ? q[x] : 0.f); }
@@ -81,7 +82,7 @@ template <int MODE> struct Residual {
 template <int MODE> __device__ __forceinline__ double range_sum(const Residual<MODE>& w, int lo, int hi) {
   const int lane = threadIdx.x & 31;
   const bool with_q = w.with_q();
-  double s = 0.0;
+  double s[2] = {0.0, 0.0};
   for (int x0 = lo + lane; x0 < hi; x0 += 32 * kUnroll) {
     float pv[kUnroll], qv[kUnroll];
 #pragma unroll
@@ -91,34 +92,39 @@ template <int MODE> __device__ __forceinline__ double range_sum(const Residual<M
       qv[e] = with_q && x < hi ? w.q[x] : 0.f;
     }
 #pragma unroll
-    for (int e = 0; e < kUnroll; ++e) s += w.of(x0 + 32 * e, pv[e], qv[e]);
+    for (int e = 0; e < kUnroll; ++e) s[e & 1] += w.of(x0 + 32 * e, pv[e], qv[e]);
   }
-  return warp_sum(s);
+  return warp_sum(s[0] + s[1]);
 }
 
-template <int MODE> __global__ void __launch_bounds__(kVerifyThreads, 2) verify_draft_kernel(VerifyParams p) {
+template <int MODE, int kVerifyThreads>
+__global__ void __launch_bounds__(kVerifyThreads, 1024 / kVerifyThreads) verify_draft_kernel(VerifyParams p) {
+  constexpr int kVerifyWarps = kVerifyThreads / 32;
   __shared__ VerifyShared sh;
   const cg::cluster_group cluster = cg::this_cluster();
   const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int b = blockIdx.x / ctas, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
-  int n = p.n_nodes ? p.n_nodes[b] : p.N;
+  // the tree, and of the big rows what the tests need: two rounds of loads for all nodes at once
+  int n = p.N, pa = 0, x = 0;
+  if (p.n_nodes) n = p.n_nodes[b];
+  if (tid < p.N) {
+    pa = p.parent[(int64_t)b * p.N + tid];
+    x = p.tokens[(int64_t)b * p.N + tid];
+    if (MODE != kModeGreedy) sh.u[tid] = p.uniforms[(int64_t)b * p.N + tid];
+  }
   bool bad = n < 0 || n > p.N;
   if (bad) n = 0;
   const int64_t row0 = (int64_t)b * p.N * p.vocab;
   if (tid < n) {
-    const int pa = p.parent[(int64_t)b * p.N + tid], x = p.tokens[(int64_t)b * p.N + tid];
     if (tid == 0) bad = pa != -1;
     else bad = pa < 0 || pa >= tid || x < 0 || x >= p.vocab;
     sh.parent[tid] = pa;
     sh.token[tid] = x;
-    if (MODE != kModeGreedy) {
-      sh.u[tid] = p.uniforms[(int64_t)b * p.N + tid];
-      if (tid > 0 && !bad) {
-        sh.p[tid] = p.target[row0 + (int64_t)pa * p.vocab + x];
-        if (MODE == kModeDraft) sh.q[tid] = p.draft[row0 + (int64_t)pa * p.vocab + x];
-      }
+    if (MODE != kModeGreedy && tid > 0 && !bad) {
+      sh.p[tid] = p.target[row0 + (int64_t)pa * p.vocab + x];
+      if (MODE == kModeDraft) sh.q[tid] = p.draft[row0 + (int64_t)pa * p.vocab + x];
     }
   }
   int status = __syncthreads_or(bad) ? NGC_DEV_BAD_TREE : NGC_DEV_OK;
@@ -128,25 +134,35 @@ template <int MODE> __global__ void __launch_bounds__(kVerifyThreads, 2) verify_
   const int per_warp = (per_cta + kVerifyWarps - 1) / kVerifyWarps;
   const int lo = min(cta_hi, cta_lo + warp * per_warp), hi = min(cta_hi, lo + per_warp);
   int exchange = 0;
+  double share = 0.0;                                // lane i of every warp: the sum of CTA i's slice
 
-  // sum of a residual over the vocabulary: the same value in every thread of the cluster; the warps' and CTAs' shares stay
+  // sum of a residual over the vocabulary: the same value in every thread of the cluster; the shares of warps and CTAs stay
   auto vocab_sum = [&](const Residual<MODE>& w) {
     const double s = range_sum(w, lo, hi);
     __syncthreads();
     if (lane == 0) sh.warp_sum[warp] = s;
     __syncthreads();
-    if (tid == 0) {
-      double t = 0.0;
-      for (int i = 0; i < kVerifyWarps; ++i) t += sh.warp_sum[i];
-      sh.cta_sum[exchange & 1] = t;
+    if (warp == 0) {
+      const double t = warp_sum(lane < kVerifyWarps ? sh.warp_sum[lane] : 0.0);
+      if (lane == 0) sh.cta_sum[exchange & 1] = t;
     }
     cluster.sync();
-    double total = 0.0;
-    for (int i = 0; i < ctas; ++i) total += cluster.map_shared_rank(sh.cta_sum, i)[exchange & 1];
+    share = lane < ctas ? cluster.map_shared_rank(sh.cta_sum, lane)[exchange & 1] : 0.0;
     ++exchange;
-    return total;
+    return warp_sum(share);
   };
   // argmax of a row (the smallest index of equal values), or -1 if the row holds a NaN
+  auto better = [](float v, int a, float& best, int& arg) {
+    if (v > best || (v == best && a < arg)) { best = v; arg = a; }
+  };
+  auto warp_best = [&](float& best, int& arg) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const float v = __shfl_xor_sync(0xffffffffu, best, o);
+      const int a = __shfl_xor_sync(0xffffffffu, arg, o);
+      better(v, a, best, arg);
+    }
+  };
   auto row_argmax = [&](const float* row) {
     float best = -INFINITY;
     int arg = 0x7fffffff;
@@ -158,35 +174,25 @@ template <int MODE> __global__ void __launch_bounds__(kVerifyThreads, 2) verify_
 #pragma unroll
       for (int e = 0; e < kUnroll; ++e) {
         nan = nan || v[e] != v[e];
-        if (x0 + 32 * e < hi && (v[e] > best || arg == 0x7fffffff)) { best = v[e]; arg = x0 + 32 * e; }
+        if (x0 + 32 * e < hi) better(v[e], x0 + 32 * e, best, arg);
       }
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const float v = __shfl_xor_sync(0xffffffffu, best, o);
-      const int a = __shfl_xor_sync(0xffffffffu, arg, o);
-      if (v > best || (v == best && a < arg)) { best = v; arg = a; }
-    }
+    warp_best(best, arg);
     nan = __syncthreads_or(nan);
     if (lane == 0) { sh.warp_max[warp] = best; sh.warp_arg[warp] = arg; }
     __syncthreads();
-    if (tid == 0) {
-      for (int i = 1; i < kVerifyWarps; ++i)
-        if (sh.warp_max[i] > best || (sh.warp_max[i] == best && sh.warp_arg[i] < arg)) { best = sh.warp_max[i]; arg = sh.warp_arg[i]; }
-      sh.cta_max[exchange & 1] = best;
-      sh.cta_arg[exchange & 1] = nan ? -1 : arg;
+    if (warp == 0) {
+      best = lane < kVerifyWarps ? sh.warp_max[lane] : -INFINITY;
+      arg = lane < kVerifyWarps ? sh.warp_arg[lane] : 0x7fffffff;
+      warp_best(best, arg);
+      if (lane == 0) { sh.cta_max[exchange & 1] = best; sh.cta_arg[exchange & 1] = nan ? -1 : arg; }
     }
     cluster.sync();
-    best = -INFINITY;
-    arg = 0x7fffffff;
-    nan = false;
-    for (int i = 0; i < ctas; ++i) {
-      const float v = cluster.map_shared_rank(sh.cta_max, i)[exchange & 1];
-      const int a = cluster.map_shared_rank(sh.cta_arg, i)[exchange & 1];
-      nan = nan || a < 0;
-      if (v > best || (v == best && a < arg)) { best = v; arg = a; }
-    }
+    best = lane < ctas ? cluster.map_shared_rank(sh.cta_max, lane)[exchange & 1] : -INFINITY;
+    arg = lane < ctas ? cluster.map_shared_rank(sh.cta_arg, lane)[exchange & 1] : 0x7fffffff;
     ++exchange;
+    nan = __any_sync(0xffffffffu, arg < 0);
+    warp_best(best, arg);
     return nan ? -1 : arg;
   };
 
@@ -256,7 +262,7 @@ template <int MODE> __global__ void __launch_bounds__(kVerifyThreads, 2) verify_
         int own = -1, last = 0;
         double last_before = 0.0;
         for (int i = 0; i < ctas; ++i) {
-          const double s = cluster.map_shared_rank(sh.cta_sum, i)[(exchange - 1) & 1];
+          const double s = __shfl_sync(0xffffffffu, share, i);
           if (s > 0.0) { last = i; last_before = before; }
           if (own < 0 && before + s > t) own = i;
           if (own < 0) before += s;
@@ -266,8 +272,9 @@ template <int MODE> __global__ void __launch_bounds__(kVerifyThreads, 2) verify_
         if (draws) {
           int range = -1;
           last = 0;
+          const double shares = lane < kVerifyWarps ? sh.warp_sum[lane] : 0.0;
           for (int i = 0; i < kVerifyWarps; ++i) {
-            const double s = sh.warp_sum[i];
+            const double s = __shfl_sync(0xffffffffu, shares, i);
             if (s > 0.0) { last = i; last_before = before; }
             if (range < 0 && before + s > t) range = i;
             if (range < 0) before += s;
@@ -294,7 +301,8 @@ template <int MODE> __global__ void __launch_bounds__(kVerifyThreads, 2) verify_
           if (tid == 0) { sh.last = -1; sh.warp_arg[0] = 0x7fffffff; }
           if (lane == 31) sh.warp_sum[warp] = c;
           __syncthreads();
-          for (int i = 0; i < warp; ++i) before += sh.warp_sum[i];
+#pragma unroll
+          for (int i = 0; i < kVerifyWarps; ++i) before += i < warp ? sh.warp_sum[i] : 0.0;
           double upto = before + (c - s);
           int hit = -1;
           if (upto + s > t)
@@ -337,14 +345,20 @@ extern "C" int ngc_verify_draft(const int32_t* tokens, const int32_t* parent, co
     return NGC_ERR_INVALID_ARG;
   if (N > NGC_TREE_MAX_NODES) return NGC_ERR_UNSUPPORTED;
   const VerifyParams p = {tokens, parent, n_nodes, target_probs, draft_probs, uniforms, path, n_path, next_token, dev_status, N, vocab};
-  // CTAs per sequence: a slice of at least 2048 tokens each, at most 8
-  int cluster = 1;
-  while (cluster < kMaxCluster && (int64_t)vocab >= 4096LL * cluster) cluster *= 2;
+  // CTAs per sequence: a slice of at least 2048 tokens each, at most 8, and no more than one round of CTAs in all: a
+  // sequence that rejects many children takes many passes, which others should not queue behind.  Few sequences get
+  // twice the threads: then a pass is bound by each SM's conversions and latencies (4 rejections in 131072 tokens: 18.5 us
+  // with 512 threads, 24.8 us with 256), else by how many CTAs are there at once (64 sequences: 46.7 and 42.3 us).
+  const bool wide = (int64_t)B * kMaxCluster <= 2 * 148;
+  int cluster = vocab / 2048;
+  if (cluster > 4 * 148 / B) cluster = 4 * 148 / B;
+  if (cluster > kMaxCluster) cluster = kMaxCluster;
+  if (cluster < 1) cluster = 1;
   if ((int64_t)B * cluster > 0x7fffffffLL) return NGC_ERR_UNSUPPORTED;
-  const dim3 grid((unsigned)(B * cluster)), block(kVerifyThreads);
-  cudaStream_t s = (cudaStream_t)stream;
-  if (greedy) NGC_CUDA_TRY(launch_pdl_cluster(verify_draft_kernel<kModeGreedy>, grid, block, cluster, s, p));
-  else if (draft_probs) NGC_CUDA_TRY(launch_pdl_cluster(verify_draft_kernel<kModeDraft>, grid, block, cluster, s, p));
-  else NGC_CUDA_TRY(launch_pdl_cluster(verify_draft_kernel<kModePoint>, grid, block, cluster, s, p));
+  const dim3 grid((unsigned)(B * cluster)), block(wide ? 512 : 256);
+  auto kernel = greedy ? (wide ? verify_draft_kernel<kModeGreedy, 512> : verify_draft_kernel<kModeGreedy, 256>)
+              : draft_probs ? (wide ? verify_draft_kernel<kModeDraft, 512> : verify_draft_kernel<kModeDraft, 256>)
+                            : (wide ? verify_draft_kernel<kModePoint, 512> : verify_draft_kernel<kModePoint, 256>);
+  NGC_CUDA_TRY(launch_pdl_cluster(kernel, grid, block, (unsigned)cluster, (cudaStream_t)stream, p));
   return NGC_OK;
 }
