@@ -7,9 +7,12 @@
 // ancestor set.
 //
 // bf16 caches run on the tensor cores (tree_attn_umma.cu); fp32 caches on the
-// FMA path (this file): tiles of 32 keys in shared memory as fp32, 4 rows x 2 keys of S and 4 rows x
-// 8 channels (d = 128) of O per thread, online softmax with the row statistics spread over 16 lanes.
-// One pass over K and V; with few items the key axis is split and a combine kernel joins the parts.
+// FMA path (this file): tiles of 32 keys as fp32 in shared memory, the next one on its way by 16-byte asynchronous
+// copies; four query rows per group of lanes, online softmax with the row statistics spread over the group.  Blocks of
+// 64 rows use 16 lanes per group (4 rows x 2 keys of S, 4 rows x 8 channels of O per thread at d = 128: 32 multiply-adds
+// per 8 shared-memory wavefronts), blocks of at most 16 rows 32 lanes (twice the threads per row: those calls wait
+// for memory, not for arithmetic).  One pass over K and V; with few items the key axis is split and a second kernel
+// joins the parts.
 #include <cuda_bf16.h>
 
 #include "ngc_plan.h"
@@ -19,27 +22,46 @@ namespace ngc {
 namespace {
 
 constexpr int kKeyTile = 32;                    // keys per tile, and the split granularity
-constexpr int kSplitMin = 8;                    // tiles a split has at least
+constexpr int kSplitMin = 2;                    // tiles a split has at least
 
-__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
 __device__ __forceinline__ bool finite4(float4 x) {
   return isfinite(x.x) && isfinite(x.y) && isfinite(x.z) && isfinite(x.w);
 }
-template <int D, int RB> struct FmaSmem {
-  float q[RB][D + 4], k[kKeyTile][D + 4], v[kKeyTile][D];
-  float p[kKeyTile][RB + 4];
-  uint32_t anc[kTreeMaxNodes][kTreeWords];
-  int jump[kTreeMaxNodes];
-  int odd;                                      // the tile's V rows hold an infinity or a NaN in its node part
+// 16-byte asynchronous copy that writes zeros instead when `live` is false (nothing is read then).
+__device__ __forceinline__ void copy16_or_zero(void* dst, const void* src, bool live) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(dst)), "l"(src), "r"(live ? 16 : 0) : "memory");
+}
+template <int N> __device__ __forceinline__ void load_n(const float* p, float (&x)[N]) {
+  if constexpr (N == 2) {
+    const float2 t = *reinterpret_cast<const float2*>(p);
+    x[0] = t.x; x[1] = t.y;
+  } else {
+    const float4 t = *reinterpret_cast<const float4*>(p);
+    x[0] = t.x; x[1] = t.y; x[2] = t.z; x[3] = t.w;
+  }
+}
+
+template <int D, int RB> struct Fma {
+  static constexpr int kLanes = RB == 16 ? 32 : 16;          // per group of 4 rows
+  static constexpr int kThreads = RB / 4 * kLanes;
+  static constexpr int kKeys = kKeyTile / kLanes;            // keys of a tile per lane: tx + kLanes * u
+  static constexpr int kVec = D / kLanes < 4 ? D / kLanes : 4, kVecs = D / kLanes / kVec;   // channels per lane: kVecs runs of kVec
+  struct Smem {
+    float q[RB][D + 4], k[2][kKeyTile][D + 4], v[2][kKeyTile][D];
+    float p[kKeyTile][RB + 4];
+    uint32_t anc[kTreeMaxNodes][kTreeWords];
+    int jump[kTreeMaxNodes];
+    int odd[2];                                 // the tile's V rows hold an infinity or a NaN in its node part
+  };
 };
 
-// RB rows per item, 4 * RB threads: thread (ty, tx) of 16 lanes per row group owns rows 4 ty .. 4 ty + 3.
 template <int D, int RB>
-__global__ void __launch_bounds__(4 * RB) tree_fma_kernel(TreeAttnParams p) {
-  constexpr int NT = 4 * RB, CV = D / 64;       // CV float4 groups of channels per thread
+__global__ void __launch_bounds__(Fma<D, RB>::kThreads) tree_fma_kernel(TreeAttnParams p) {
+  using F = Fma<D, RB>;
+  constexpr int NT = F::kThreads, NL = F::kLanes, KL = F::kKeys, VW = F::kVec, VN = F::kVecs;
   extern __shared__ __align__(16) uint8_t smem_raw[];
-  FmaSmem<D, RB>& sm = *reinterpret_cast<FmaSmem<D, RB>*>(smem_raw);
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  typename F::Smem& sm = *reinterpret_cast<typename F::Smem*>(smem_raw);
+  const int tid = threadIdx.x, tx = tid % NL, ty = tid / NL;
 
   int item = blockIdx.x;
   const int split = item % p.n_split; item /= p.n_split;
@@ -54,30 +76,42 @@ __global__ void __launch_bounds__(4 * RB) tree_fma_kernel(TreeAttnParams p) {
   const int rows = p.g * p.N, r0 = rb * RB;
   const int64_t part0 = (((int64_t)lr * p.B + b) * p.Hq + (int64_t)h * p.g) * p.N;     // parts of the KV head's first row
   const int len = p.lens[len_index(p.lens_lists, p.L, p.Hkv, b, l, h)];
-  const bool tree_ok = tree_masks<NT>(p.parent + (int64_t)b * p.N, n, p.N, sm.anc, sm.jump);
-  if (!tree_ok || len < 0 || len > tree_capacity(p, b)) {
-    if (tid == 0) set_dev_status(p.dev_status, tree_ok ? NGC_DEV_BAD_COUNTS : NGC_DEV_BAD_TREE);
-    if (p.n_split > 1)
-      for (int r = r0 + tid; r < min(rows, r0 + RB); r += NT) p.part_ml[(part0 + r) * p.n_split + split] = kNoPart;
-    return;
-  }
-  const int keys = len + n;
+  const bool len_ok = len >= 0 && len <= tree_capacity(p, b), n_ok = n >= 0 && n <= p.N;
+  const int keys = len_ok && n_ok ? len + n : 0;
   const int nt = (keys + kKeyTile - 1) / kKeyTile, tps = (nt + p.n_split - 1) / p.n_split;
   const int tile_lo = min(nt, split * tps), tile_hi = min(nt, tile_lo + tps);
   const int plane = l * p.Hkv + h;
-  const int32_t* table = p.page_table ? p.page_table + ((int64_t)b * p.G + list_of(p.lists, l, h, p.Hkv)) * p.pages_cap : nullptr;
-  const float* const kc = (const float*)p.k + (int64_t)plane * p.rows * D;
-  const float* const vc = (const float*)p.v + (int64_t)plane * p.rows * D;
-  const int64_t base = p.page_table ? (int64_t)b * p.pages_cap * p.page : p.seq_off[b];
   const int64_t strip = ((int64_t)l * p.B + b) * p.Hkv + h;
+  const float* const kc = (const float*)p.k + ((int64_t)plane * p.rows + p.seq_off[b]) * D;
+  const float* const vc = (const float*)p.v + ((int64_t)plane * p.rows + p.seq_off[b]) * D;
   const float* const kt = (const float*)p.tree_k + strip * p.N * D;
   const float* const vt = (const float*)p.tree_v + strip * p.N * D;
   const int64_t row0 = (((int64_t)l * p.B + b) * p.Hq + (int64_t)h * p.g) * p.N;       // first query row of the KV head
 
+  auto fetch = [&](int t) {                                        // dead keys: zeros, so that weight 0 x value is 0
+    const int s = t & 1;
+    for (int i = tid; i < kKeyTile * (D / 4); i += NT) {
+      const int jj = i / (D / 4), c = 4 * (i % (D / 4)), j = t * kKeyTile + jj;
+      const bool live = j < keys;
+      const int64_t at = (int64_t)(j < len ? j : j - len) * D + c;
+      copy16_or_zero(&sm.k[s][jj][c], live ? (j < len ? kc : kt) + at : kt, live);
+      copy16_or_zero(&sm.v[s][jj][c], live ? (j < len ? vc : vt) + at : vt, live);
+    }
+    ptx::cp_async_commit();
+  };
   for (int i = tid; i < RB * (D / 4); i += NT) {
     const int r = i / (D / 4), c = 4 * (i % (D / 4));
-    const float4 x = r0 + r < rows ? load4((const float*)p.q + (row0 + r0 + r) * D + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-    *reinterpret_cast<float4*>(&sm.q[r][c]) = x;
+    const bool live = r0 + r < rows;
+    copy16_or_zero(&sm.q[r][c], (const float*)p.q + (row0 + (live ? r0 + r : 0)) * D + c, live);
+  }
+  if (tile_lo < tile_hi) fetch(tile_lo);
+  const bool tree_ok = tree_masks<NT>(p.parent + (int64_t)b * p.N, n, p.N, sm.anc, sm.jump);
+  if (!tree_ok || !len_ok) {
+    ptx::cp_async_wait_all();
+    if (tid == 0) set_dev_status(p.dev_status, tree_ok ? NGC_DEV_BAD_COUNTS : NGC_DEV_BAD_TREE);
+    if (p.n_split > 1)
+      for (int r = r0 + tid; r < min(rows, r0 + RB); r += NT) p.part_ml[(part0 + r) * p.n_split + split] = kNoPart;
+    return;
   }
   int node[4];
 #pragma unroll
@@ -85,92 +119,96 @@ __global__ void __launch_bounds__(4 * RB) tree_fma_kernel(TreeAttnParams p) {
     const int r = r0 + 4 * ty + e;
     node[e] = r < rows && r % p.N < n ? r % p.N : -1;              // -1: a row that is not there, and not written
   }
-  float m[4], lsum[4], acc[4][4 * CV];
+  float m[4], lsum[4], acc[4][VN][VW];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     m[e] = -INFINITY; lsum[e] = 0.f;
 #pragma unroll
-    for (int c = 0; c < 4 * CV; ++c) acc[e][c] = 0.f;
+    for (int cv = 0; cv < VN; ++cv)
+#pragma unroll
+      for (int c = 0; c < VW; ++c) acc[e][cv][c] = 0.f;
   }
+  if (tid < 2) sm.odd[tid] = 0;
 
   for (int t = tile_lo; t < tile_hi; ++t) {
-    const int j0 = t * kKeyTile;
-    __syncthreads();                                               // the previous tile has been read
-    if (tid == 0) sm.odd = 0;
-    __syncthreads();
-    for (int i = tid; i < kKeyTile * (D / 4); i += NT) {
-      const int jj = i / (D / 4), c = 4 * (i % (D / 4)), j = j0 + jj;
-      float4 kx = make_float4(0.f, 0.f, 0.f, 0.f), vx = kx;        // dead keys: zeros, so that weight 0 x value is 0
-      if (j < len) {
-        int64_t row = base + j;
-        if (table) {
-          int pg = table[j / p.page];
-          if (pg < 0 || pg >= p.pages_cap) { set_dev_status(p.dev_status, NGC_DEV_BAD_PAGE); pg = 0; }
-          row = base + (int64_t)pg * p.page + j % p.page;
-        }
-        if (NGC_IN_BOUNDS(p.dev_status, row >= 0 && row < p.rows)) { kx = load4(kc + row * D + c); vx = load4(vc + row * D + c); }
-      } else if (j < keys) {
-        kx = load4(kt + (int64_t)(j - len) * D + c); vx = load4(vt + (int64_t)(j - len) * D + c);
-        if (!finite4(vx)) sm.odd = 1;
-      }
-      *reinterpret_cast<float4*>(&sm.k[jj][c]) = kx;
-      *reinterpret_cast<float4*>(&sm.v[jj][c]) = vx;
+    const int j0 = t * kKeyTile, s = t & 1;
+    if (t + 1 < tile_hi) {
+      fetch(t + 1);
+      ptx::cp_async_wait_group<1>();
+    } else {
+      ptx::cp_async_wait_all();
     }
     __syncthreads();
-    // S: rows 4 ty + e, keys tx and tx + 16
-    float s[4][2];
+    if (j0 + kKeyTile > len) {
+      for (int i = tid; i < kKeyTile * (D / 4); i += NT) {
+        const int jj = i / (D / 4);
+        if (j0 + jj >= len && !finite4(*reinterpret_cast<const float4*>(&sm.v[s][jj][4 * (i % (D / 4))]))) sm.odd[s] = 1;
+      }
+      __syncthreads();
+    }
+    // S: rows 4 ty + e, keys tx + NL u
+    float z[4][KL];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) { s[e][0] = 0.f; s[e][1] = 0.f; }
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int u = 0; u < KL; ++u) z[e][u] = 0.f;
 #pragma unroll 8
     for (int c = 0; c < D; c += 4) {
-      const float4 k0 = *reinterpret_cast<const float4*>(&sm.k[tx][c]), k1 = *reinterpret_cast<const float4*>(&sm.k[tx + 16][c]);
+      float4 kx[KL];
+#pragma unroll
+      for (int u = 0; u < KL; ++u) kx[u] = *reinterpret_cast<const float4*>(&sm.k[s][tx + NL * u][c]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float4 x = *reinterpret_cast<const float4*>(&sm.q[4 * ty + e][c]);
-        s[e][0] = fmaf(x.x, k0.x, fmaf(x.y, k0.y, fmaf(x.z, k0.z, fmaf(x.w, k0.w, s[e][0]))));
-        s[e][1] = fmaf(x.x, k1.x, fmaf(x.y, k1.y, fmaf(x.z, k1.z, fmaf(x.w, k1.w, s[e][1]))));
+#pragma unroll
+        for (int u = 0; u < KL; ++u)
+          z[e][u] = fmaf(x.x, kx[u].x, fmaf(x.y, kx[u].y, fmaf(x.z, kx[u].z, fmaf(x.w, kx[u].w, z[e][u]))));
       }
     }
-    uint32_t vis = 0;                                              // bit 2 e + u: row 4 ty + e sees key tx + 16 u
+    uint32_t vis = 0;                                              // bit KL e + u: row 4 ty + e sees key tx + NL u
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       float mx = -INFINITY;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int j = j0 + tx + 16 * u, i = j - len;
+      for (int u = 0; u < KL; ++u) {
+        const int j = j0 + tx + NL * u, i = j - len;
         const bool see = j < len || (j < keys && node[e] >= 0 && ((sm.anc[node[e]][i >> 5] >> (i & 31)) & 1u));
-        vis |= (uint32_t)see << (2 * e + u);
-        s[e][u] = see ? s[e][u] * p.scale_log2 : -INFINITY;
-        mx = fmaxf(mx, s[e][u]);
+        vis |= (uint32_t)see << (KL * e + u);
+        z[e][u] = see ? z[e][u] * p.scale_log2 : -INFINITY;
+        mx = fmaxf(mx, z[e][u]);
       }
 #pragma unroll
-      for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+      for (int o = NL / 2; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
       const float m_new = fmaxf(m[e], mx), m_eff = m_new == -INFINITY ? 0.f : m_new;    // nothing visible yet: weights 0
       const float alpha = exp2f(m[e] - m_eff);
-      const float p0 = exp2f(s[e][0] - m_eff), p1 = exp2f(s[e][1] - m_eff);
-      lsum[e] = lsum[e] * alpha + (p0 + p1);                       // this lane's share; joined at the end
-      m[e] = m_new;
-      sm.p[tx][4 * ty + e] = p0;
-      sm.p[tx + 16][4 * ty + e] = p1;
+      float sum = 0.f;
 #pragma unroll
-      for (int c = 0; c < 4 * CV; ++c) acc[e][c] *= alpha;
+      for (int u = 0; u < KL; ++u) {
+        const float w = exp2f(z[e][u] - m_eff);
+        sm.p[tx + NL * u][4 * ty + e] = w;
+        sum += w;
+      }
+      lsum[e] = lsum[e] * alpha + sum;                             // this lane's share; joined at the end
+      m[e] = m_new;
+#pragma unroll
+      for (int cv = 0; cv < VN; ++cv)
+#pragma unroll
+        for (int c = 0; c < VW; ++c) acc[e][cv][c] *= alpha;
     }
-    __syncwarp();                                                  // P of a row group stays within its 16 lanes
-    if (!sm.odd) {
+    __syncwarp();                                                  // P of a row group stays within its lanes
+    if (!sm.odd[s]) {
 #pragma unroll 4
       for (int jj = 0; jj < kKeyTile; ++jj) {
-        const float4 w = *reinterpret_cast<const float4*>(&sm.p[jj][4 * ty]);
+        float w[4];
+        load_n(&sm.p[jj][4 * ty], w);
 #pragma unroll
-        for (int cv = 0; cv < CV; ++cv) {
-          const float4 x = *reinterpret_cast<const float4*>(&sm.v[jj][64 * cv + 4 * tx]);
-          const float we[4] = {w.x, w.y, w.z, w.w};
+        for (int cv = 0; cv < VN; ++cv) {
+          float x[VW];
+          load_n(&sm.v[s][jj][VW * (NL * cv + tx)], x);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            acc[e][4 * cv] = fmaf(we[e], x.x, acc[e][4 * cv]);
-            acc[e][4 * cv + 1] = fmaf(we[e], x.y, acc[e][4 * cv + 1]);
-            acc[e][4 * cv + 2] = fmaf(we[e], x.z, acc[e][4 * cv + 2]);
-            acc[e][4 * cv + 3] = fmaf(we[e], x.w, acc[e][4 * cv + 3]);
-          }
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int c = 0; c < VW; ++c) acc[e][cv][c] = fmaf(w[e], x[c], acc[e][cv][c]);
         }
       }
     } else {
@@ -178,39 +216,37 @@ __global__ void __launch_bounds__(4 * RB) tree_fma_kernel(TreeAttnParams p) {
       for (int jj = 0; jj < kKeyTile; ++jj) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const uint32_t see = __shfl_sync(0xffffffffu, vis, (tid & 16) + (jj & 15)) >> (2 * e + (jj >> 4)) & 1u;
-          if (!see) continue;
+          const uint32_t of = __shfl_sync(0xffffffffu, vis, (tid & 31 & ~(NL - 1)) + jj % NL);
+          if (!(of >> (KL * e + jj / NL) & 1u)) continue;
           const float w = sm.p[jj][4 * ty + e];
 #pragma unroll
-          for (int cv = 0; cv < CV; ++cv)
+          for (int cv = 0; cv < VN; ++cv)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) acc[e][4 * cv + c] = fmaf(w, sm.v[jj][64 * cv + 4 * tx + c], acc[e][4 * cv + c]);
+            for (int c = 0; c < VW; ++c) acc[e][cv][c] = fmaf(w, sm.v[s][jj][VW * (NL * cv + tx) + c], acc[e][cv][c]);
         }
       }
     }
+    __syncthreads();                                               // the stage may be overwritten
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) lsum[e] += __shfl_xor_sync(0xffffffffu, lsum[e], o);
+    for (int o = NL / 2; o > 0; o >>= 1) lsum[e] += __shfl_xor_sync(0xffffffffu, lsum[e], o);
     const int r = r0 + 4 * ty + e;
     const int64_t pit = (part0 + r) * p.n_split + split;
     if (node[e] < 0) {
       if (p.n_split > 1 && r < rows && tx == 0) p.part_ml[pit] = kNoPart;
       continue;
     }
-    if (p.n_split == 1) {
-      const float inv = lsum[e] == 0.f ? 0.f : 1.f / lsum[e];     // a NaN stays one
+    const bool whole = p.n_split == 1;
+    const float inv = !whole ? 1.f : lsum[e] == 0.f ? 0.f : 1.f / lsum[e];     // a NaN stays one
+    if (!whole && tx == 0) p.part_ml[pit] = make_float2(m[e], lsum[e]);
+    float* const to = whole ? (float*)p.out + (row0 + r) * D : p.part_o + pit * D;
 #pragma unroll
-      for (int cv = 0; cv < CV; ++cv)
-        tree_store_out4(p, (row0 + r) * D + 64 * cv + 4 * tx, make_float4(acc[e][4 * cv] * inv, acc[e][4 * cv + 1] * inv,
-                                                                     acc[e][4 * cv + 2] * inv, acc[e][4 * cv + 3] * inv));
-    } else {
-      if (tx == 0) p.part_ml[pit] = make_float2(m[e], lsum[e]);
-#pragma unroll
-      for (int cv = 0; cv < CV; ++cv)
-        *reinterpret_cast<float4*>(p.part_o + pit * D + 64 * cv + 4 * tx) =
-            make_float4(acc[e][4 * cv], acc[e][4 * cv + 1], acc[e][4 * cv + 2], acc[e][4 * cv + 3]);
+    for (int cv = 0; cv < VN; ++cv) {
+      float* const at = to + VW * (NL * cv + tx);
+      if constexpr (VW == 2) *reinterpret_cast<float2*>(at) = make_float2(acc[e][cv][0] * inv, acc[e][cv][1] * inv);
+      else *reinterpret_cast<float4*>(at) = make_float4(acc[e][cv][0] * inv, acc[e][cv][1] * inv, acc[e][cv][2] * inv, acc[e][cv][3] * inv);
     }
   }
 }
@@ -241,14 +277,17 @@ __global__ void __launch_bounds__(128) tree_combine_kernel(TreeAttnParams p) {
   tree_store_out4(p, ((int64_t)p.layer_begin * per_layer + row) * p.d + c, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
 }
 
-template <int D> cudaError_t launch_fma(const TreeAttnParams& p, int rb, unsigned grid, cudaStream_t stream) {
-  if (rb == 16) return launch_pdl(tree_fma_kernel<D, 16>, dim3(grid), dim3(64), sizeof(FmaSmem<D, 16>), stream, p);
-  return launch_pdl(tree_fma_kernel<D, 64>, dim3(grid), dim3(256), sizeof(FmaSmem<D, 64>), stream, p);
+template <int D, int RB> cudaError_t launch_fma_rows(const TreeAttnParams& p, unsigned grid, cudaStream_t stream) {
+  using F = Fma<D, RB>;
+  return launch_pdl(tree_fma_kernel<D, RB>, dim3(grid), dim3(F::kThreads), sizeof(typename F::Smem), stream, p);
+}
+template <int D> cudaError_t launch_fma(const TreeAttnParams& p, unsigned grid, cudaStream_t stream) {
+  return p.block_rows == 16 ? launch_fma_rows<D, 16>(p, grid, stream) : launch_fma_rows<D, 64>(p, grid, stream);
 }
 template <int D> cudaError_t opt_in_fma() {
-  cudaError_t e = cudaFuncSetAttribute(tree_fma_kernel<D, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(FmaSmem<D, 16>));
+  cudaError_t e = cudaFuncSetAttribute(tree_fma_kernel<D, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(typename Fma<D, 16>::Smem));
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(tree_fma_kernel<D, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(FmaSmem<D, 64>));
+    e = cudaFuncSetAttribute(tree_fma_kernel<D, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(typename Fma<D, 64>::Smem));
   return e;
 }
 
@@ -345,8 +384,7 @@ int tree_impl(const ngc_cache* c, const PagedView& pv, const void* q, const void
       return e == cudaSuccess ? opt_in_fma<128>() : e;
     });
     if (rc != NGC_OK) return rc;
-    NGC_CUDA_TRY(c->d == 64 ? launch_fma<64>(p, plan.block_rows, (unsigned)items, stream)
-                            : launch_fma<128>(p, plan.block_rows, (unsigned)items, stream));
+    NGC_CUDA_TRY(c->d == 64 ? launch_fma<64>(p, (unsigned)items, stream) : launch_fma<128>(p, (unsigned)items, stream));
   }
   if (p.n_split > 1)
     NGC_CUDA_TRY(launch_pdl(tree_combine_kernel, dim3((unsigned)((out_threads + 127) / 128)), dim3(128), 0, stream, p));
