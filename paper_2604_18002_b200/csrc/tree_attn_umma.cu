@@ -17,10 +17,15 @@
 //                    cache and the tree tiles come in 16-row boxes.  Page-table entries are fetched 32 at a time, a
 //                    batch ahead;
 //   MMA warp         S = Q K^T into tensor memory, O += P V with P read from tensor memory;
-//   softmax warps    (4 MT) one thread per row: mask (only in tree tiles, a bit of the node's ancestor set, and in the
-//                    cache's last tile), online softmax in the log2 domain, P as bf16 over the S it came from, 64 keys
-//                    at a time.  The maximum used only moves when the true one has grown by more than a factor 2^8, so
-//                    O in tensor memory is rarely rescaled.
+//   softmax warps    (4 MT) one thread per row: follows its node's links to the root for its mask (needed only in tree
+//                    tiles; the cache's last tile has a common one), online softmax in the log2 domain, P as bf16 over
+//                    the S it came from, 64 keys at a time.  The maximum used only moves when the true one has grown by
+//                    more than a factor 2^8, so O in tensor memory is rarely rescaled.  With two M tiles a part of
+//                    the exponentials is a polynomial on the FMA pipe: one exponential takes the special-function unit 8
+//                    cycles per warp, 128 x 128 of them as long as the tensor pipe needs for their products.
+//
+// The roles only meet at mbarriers, also from one unit to the next: loads and scores of the next unit run under the
+// end of the current one.
 //
 // Work is dealt out in one of two ways.  With many units (or short ones) a CTA takes one unit.  With few, the tiles of
 // all units form one line that is cut into equal pieces, a CTA per piece: rollouts of any lengths keep all SMs busy
@@ -58,6 +63,7 @@ template <int D, int MT> struct Cfg {
   static constexpr int kTile = kKeys * D * 2;              // K or V tile
   static constexpr int kQBytes = 128 * D * 2;              // Q of an M tile
   static constexpr int kSmem = MT * kQBytes + 2 * kStages * kTile + 1024;
+  static constexpr int kPolyPairs = MT == 1 ? 0 : 1;       // of four pairs of exponentials on the FMA pipe
   static constexpr uint32_t kOCol = 128 * MT;              // S[m][buf] at 128 m + 64 buf, O[m] behind
   static constexpr uint32_t kCols = MT == 1 ? 256 : 512;
 };
@@ -67,14 +73,17 @@ template <int D, int MT> struct Cfg {
 struct KvMaps { CUtensorMap whole, part, tree; };
 struct Maps { KvMaps k, v; CUtensorMap q; };
 
+template <int N> struct Int { static constexpr int value = N; };
+
 template <int D, int MT> struct Shared {
   using C = Cfg<D, MT>;
   uint64_t k_full[C::kStages], k_empty[C::kStages], v_full[C::kStages], v_empty[C::kStages];
   uint64_t s_full[MT][C::kBufs], p_full[MT][C::kBufs][C::kHalves], o_done[MT][C::kBufs];
-  uint64_t q_full, fixed[3], drain;
-  uint32_t anc[kTreeMaxNodes][kTreeWords];
-  int jump[kTreeMaxNodes];
-  uint32_t odd[kTreeWords];                     // nodes whose V row holds an infinity or a NaN
+  uint64_t q_full, q_empty, checked[MT], fixed[3], drain;
+  // by piece & 3 (no role is more than two pieces ahead of another): nodes whose V row holds an infinity or a NaN, and
+  // piece + 1 if the tree's links are no links
+  uint32_t odd[4][kTreeWords];
+  int refused[MT][4];
   uint32_t tmem;
   int abort;
   int warp_sum[C::kThreads / 32];
@@ -87,6 +96,8 @@ struct Piece {
   int plane, strip;                                    // of the cache; of the tree's K and V
   bool first, last;                                    // holds the unit's first / last tile
 };
+// This CTA's share: from tile `lo` of unit `u` on, n_left tiles in all; `seq` pieces so far.
+struct Walk { int u, lo, n_left, seq; };
 
 __device__ __forceinline__ void unit_of(const TreeAttnParams& p, int u, Piece& w) {
   w.rb = u % p.row_blocks; u /= p.row_blocks;
@@ -105,6 +116,27 @@ __device__ __forceinline__ bool counts_ok(const TreeAttnParams& p, const Piece& 
 }
 template <int KT> __device__ __forceinline__ int unit_tiles(const TreeAttnParams& p, const Piece& w) {
   return counts_ok(p, w) && w.n > 0 ? (w.len + KT - 1) / KT + (w.n + KT - 1) / KT : 0;
+}
+
+// The next piece of the walk; false at its end.  (A unit per CTA: also a unit without tiles.)
+template <int KT> __device__ __forceinline__ bool next_piece(const TreeAttnParams& p, Walk& k, Piece& w) {
+  if (k.n_left <= 0) return false;
+  int nt;
+  for (;; ++k.u, k.lo = 0) {
+    unit_of(p, k.u, w);
+    nt = unit_tiles<KT>(p, w);
+    if (nt > 0 || !p.even) break;
+  }
+  w.lo = k.lo;
+  w.n_tiles = min(nt - k.lo, k.n_left);
+  w.n_ct = (w.len + KT - 1) / KT;
+  w.first = w.lo == 0;
+  w.last = w.lo + w.n_tiles == nt;
+  k.n_left = p.even ? k.n_left - w.n_tiles : 0;
+  ++k.u;
+  k.lo = 0;
+  ++k.seq;
+  return true;
 }
 
 // Page-table entries in order, 32 at a time in the lanes of a producer warp, the next batch on its way.  An entry that is
@@ -182,6 +214,36 @@ __device__ __forceinline__ void load_tile(const TreeAttnParams& p, const KvMaps&
   }
 }
 
+// max that keeps a NaN
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// 2^x for a pair of finite x <= 100 on the FMA pipe: x = n + f with |f| <= 1/2, 2^f by its minimax polynomial of degree 4
+// (found with the Remez exchange; relative error 2.7e-6 in fp32), n added to the exponent.  Below 2^-126: 2^-126.
+__device__ __forceinline__ uint64_t exp2_poly2(uint64_t x2) {
+  float x0, x1, r0, r1;
+  umma::unpack2(x2, x0, x1);
+  x2 = umma::pack2(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
+  const uint64_t n2 = umma::add2(x2, umma::pack2(12582912.f, 12582912.f));             // 1.5 * 2^23: rounds to whole numbers
+  const uint64_t f2 = umma::fma2(umma::add2(n2, umma::pack2(-12582912.f, -12582912.f)), umma::pack2(-1.f, -1.f), x2);
+  uint64_t r2 = umma::fma2(umma::pack2(9.570101911e-03f, 9.570101911e-03f), f2, umma::pack2(5.591786032e-02f, 5.591786032e-02f));
+  r2 = umma::fma2(r2, f2, umma::pack2(2.402474483e-01f, 2.402474483e-01f));
+  r2 = umma::fma2(r2, f2, umma::pack2(6.931218147e-01f, 6.931218147e-01f));
+  r2 = umma::fma2(r2, f2, umma::pack2(9.999992614e-01f, 9.999992614e-01f));
+  umma::unpack2(r2, r0, r1);
+  umma::unpack2(n2, x0, x1);
+  return umma::pack2(__uint_as_float(__float_as_uint(r0) + (__float_as_uint(x0) << 23)),
+                     __uint_as_float(__float_as_uint(r1) + (__float_as_uint(x1) << 23)));
+}
+// 32 consecutive bytes, a whole sector, at once
+__device__ __forceinline__ void store_sector(float* p, const uint32_t* r) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+
 __device__ __forceinline__ uint32_t odd_half(uint32_t x) { return (x & 0x7f80u) == 0x7f80u ? 0xffffu : 0u; }
 // Bits of x (two bf16) that belong to infinities or NaN.
 __device__ __forceinline__ uint32_t odd_bits(uint32_t x) { return odd_half(x) | odd_half(x >> 16) << 16; }
@@ -215,6 +277,13 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
         for (int e = 0; e < NH; ++e) ptx::mbar_init(&sh.p_full[m][i][e], 128);
       }
     ptx::mbar_init(&sh.q_full, 1);
+    ptx::mbar_init(&sh.q_empty, 1);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      ptx::mbar_init(&sh.checked[m], 128);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sh.refused[m][i] = 0;
+    }
 #pragma unroll
     for (int i = 0; i < 3; ++i) ptx::mbar_init(&sh.fixed[i], 128);
     ptx::mbar_init(&sh.drain, 1);
@@ -232,8 +301,7 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
   ptx::grid_dep_launch();                       // from here on this CTA holds its tensor memory
   const uint32_t tmem = sh.tmem;
 
-  // ---- this CTA's share: unit u, tiles from g_lo of it on, n_left tiles in all
-  int u = blockIdx.x, g_lo = 0, n_left = 0x7fffffff;
+  Walk walk = {(int)blockIdx.x, 0, 0x7fffffff, 0};
   if (p.even) {
     const int per = (p.n_units + NT - 1) / NT, u0 = min(p.n_units, tid * per), u1 = min(p.n_units, u0 + per);
     int sum = 0;
@@ -267,15 +335,15 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
       if (tid == 0) p.plan[p.n_units + 1] = ctas;
     }
     const int g0 = tree_even_first(blockIdx.x, total, ctas), g1 = tree_even_first(blockIdx.x + 1, total, ctas);
-    n_left = (int)blockIdx.x < ctas ? g1 - g0 : 0;
+    walk.n_left = (int)blockIdx.x < ctas ? g1 - g0 : 0;
     // the unit that tile g0 belongs to
     int lo = 0, hi = p.n_units;
-    while (n_left > 0 && hi - lo > 1) {
+    while (walk.n_left > 0 && hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (sh.base[mid] <= g0) lo = mid; else hi = mid;
     }
-    u = lo;
-    g_lo = g0 - sh.base[u];
+    walk.u = lo;
+    walk.lo = g0 - sh.base[lo];
     // counts that cannot be worked with have no tiles: report them here
     if (blockIdx.x == 0)
       for (int i = u0; i < u1; ++i) {
@@ -285,80 +353,72 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
       }
   }
 
-  // Ring positions and barrier phases follow from running counters over all pieces: tiles -> K/V stage and, per M tile,
-  // S buffer and P / O phases.
-  int kv = 0, n_q = 0, fixes[3] = {0, 0, 0}, done[MT];
-#pragma unroll
-  for (int m = 0; m < MT; ++m) done[m] = 0;
-  for (; n_left > 0; ++u, g_lo = 0) {
-    Piece w;
-    unit_of(p, u, w);
-    const int nt = unit_tiles<KT>(p, w);
-    if (p.even ? nt == 0 : false) continue;
-    if (tid < kTreeWords) sh.odd[tid] = 0;
-    const bool counts = counts_ok(p, w);
-    const bool ok_unit = tree_masks<NT>(p.parent + (int64_t)w.b * p.N, counts ? w.n : 0, p.N, sh.anc, sh.jump) && counts;
-    w.lo = g_lo;
-    w.n_tiles = min(nt - g_lo, n_left);
-    w.n_ct = (w.len + KT - 1) / KT;
-    w.first = w.lo == 0;
-    w.last = w.lo + w.n_tiles == nt;
-    n_left = p.even ? n_left - w.n_tiles : 0;
-    const int r0 = w.rb * MT * 128;
-    const int tiles_m = min(MT, (rows - r0 + 127) >> 7);           // M tiles that have a row
-    const int64_t row0 = (((int64_t)w.l * p.B + w.b) * p.Hq + (int64_t)w.h * p.g) * p.N;   // first query row of the KV head
-    const bool whole = w.first && w.last;
-    const int64_t part0 = ((int64_t)blockIdx.x * 2 + (w.first ? 1 : 0)) * p.block_rows;    // this CTA's slot for the piece
-
-    if (!ok_unit) {
-      // bad links (every CTA with a piece of the unit sees them) or, a unit per CTA, bad counts
-      if (tid == 0) set_dev_status(p.dev_status, !counts && w.n >= 0 && w.n <= p.N ? NGC_DEV_BAD_COUNTS : NGC_DEV_BAD_TREE);
-      if (!whole && p.even)
-        for (int r = tid; r < p.block_rows; r += NT) p.part_ml[part0 + r] = kNoPart;
-    } else if (w.n_tiles <= 0) {
-      // an empty tree
-    } else if (warp >= C::kProducerWarp) {
-      // ------------------------------------------------------------------ producers
-      const bool is_v = warp != C::kProducerWarp;
+  // Every role takes the same walk.  Ring positions and barrier phases follow from running counters over its pieces: tiles
+  // -> K/V stage; per M tile, tiles -> S buffer and P / O phases.
+  Piece w;
+  int kv = 0;
+  if (warp >= C::kProducerWarp) {
+    // ------------------------------------------------------------------ producers
+    const bool is_v = warp != C::kProducerWarp;
+    uint8_t* ring = is_v ? sV : sK;
+    uint64_t* full = is_v ? sh.v_full : sh.k_full;
+    uint64_t* empty = is_v ? sh.v_empty : sh.k_empty;
+    const KvMaps& map = is_v ? maps.v : maps.k;
+    int n_q = 0;
+    bool ok = true;
+    while (ok && next_piece<KT>(p, walk, w)) {
+      if (w.n_tiles <= 0) continue;
       const int base = (int)(p.page_table ? (int64_t)w.b * p.pages_cap * p.page : p.seq_off[w.b]);
       PageWalk pages;
       if (p.page_table)
         pages.start(p.page_table + ((int64_t)w.b * p.G + list_of(p.lists, w.l, w.h, p.Hkv)) * p.pages_cap, p.pages_cap,
                     (w.len + p.page - 1) / p.page, min(w.lo * KT, w.len) / p.page, p.dev_status);
-      if (!is_v && umma::elect_one()) {
-        ptx::mbar_expect_tx(&sh.q_full, (uint32_t)(tiles_m * C::kQBytes));
-        // rows beyond the KV head's belong to the next head (zeros past the end): they only feed rows that are never written
-        for (int m = 0; m < tiles_m; ++m)
+      if (!is_v) {
+        const int r0 = w.rb * MT * 128, tiles_m = min(MT, (rows - r0 + 127) >> 7);
+        const int64_t row0 = (((int64_t)w.l * p.B + w.b) * p.Hq + (int64_t)w.h * p.g) * p.N;
+        ok = n_q == 0 || umma::warp_wait(&sh.q_empty, (n_q - 1) & 1, &sh.abort, p.dev_status);
+        if (!ok) break;
+        if (umma::elect_one()) {
+          ptx::mbar_expect_tx(&sh.q_full, (uint32_t)(tiles_m * C::kQBytes));
+          // rows beyond the KV head's belong to the next head (zeros past the end): they only feed rows that are never written
+          for (int m = 0; m < tiles_m; ++m)
 #pragma unroll
-          for (int c = 0; c < D / 64; ++c)
-            ptx::tma_load_2d(sQ + m * C::kQBytes + c * (128 * 128), &maps.q, 64 * c, (int)(row0 + r0 + 128 * m), &sh.q_full);
+            for (int c = 0; c < D / 64; ++c)
+              ptx::tma_load_2d(sQ + m * C::kQBytes + c * (128 * 128), &maps.q, 64 * c, (int)(row0 + r0 + 128 * m), &sh.q_full);
+        }
+        __syncwarp();
+        ++n_q;
       }
-      __syncwarp();
-      uint8_t* ring = is_v ? sV : sK;
-      uint64_t* full = is_v ? sh.v_full : sh.k_full;
-      uint64_t* empty = is_v ? sh.v_empty : sh.k_empty;
-      const KvMaps& map = is_v ? maps.v : maps.k;
-      int i = 0;
-      for (; i < w.n_tiles; ++i) {
-        const int s = (kv + i) % ST;
-        if (kv + i >= ST && !umma::warp_wait(&empty[s], ((kv + i) / ST - 1) & 1, &sh.abort, p.dev_status)) break;
+      for (int i = 0; ok && i < w.n_tiles; ++i) {
+        const int s = kv % ST;
+        ok = kv < ST || umma::warp_wait(&empty[s], (kv / ST - 1) & 1, &sh.abort, p.dev_status);
+        if (!ok) break;
         load_tile<D, KT>(p, map, pages, w, base, w.lo + i, ring + s * C::kTile, &full[s]);
+        ++kv;
       }
-      if (i < w.n_tiles) {                      // giving up: no copy may be in flight when the CTA ends
-        if (!is_v) ptx::mbar_wait_bounded(&sh.q_full, n_q & 1);
-        for (int j = max(0, i - ST); j < i; ++j) ptx::mbar_wait_bounded(&full[(kv + j) % ST], ((kv + j) / ST) & 1);
-      }
-    } else if (warp == C::kMmaWarp) {
-      // ------------------------------------------------------------------ MMA issue, one elected lane
-      // operand descriptors differ only in their low word (start address / 16)
-      const uint64_t desc_hi = (uint64_t)umma::smem_desc_sw128(0, 0, 1024) & 0xffffffff00000000ull;
-      const uint32_t q_base = (ptx::smem_u32(sQ) >> 4) | (1u << 16);
-      const uint32_t v_lbo = (uint32_t)(C::kBox >> 4) << 16;                     // V: the next 64 channels are one box on
+    }
+    if (!ok) {                                  // giving up: no copy may be in flight when the CTA ends
+      if (!is_v && n_q > 0) ptx::mbar_wait_bounded(&sh.q_full, (n_q - 1) & 1);
+      for (int j = max(0, kv - ST); j < kv; ++j) ptx::mbar_wait_bounded(&full[j % ST], (j / ST) & 1);
+    }
+  } else if (warp == C::kMmaWarp) {
+    // ------------------------------------------------------------------ MMA issue, one elected lane
+    // operand descriptors differ only in their low word (start address / 16)
+    const uint64_t desc_hi = (uint64_t)umma::smem_desc_sw128(0, 0, 1024) & 0xffffffff00000000ull;
+    const uint32_t q_base = (ptx::smem_u32(sQ) >> 4) | (1u << 16);
+    const uint32_t v_lbo = (uint32_t)(C::kBox >> 4) << 16;                       // V: the next 64 channels are one box on
+    int n_q = 0, done[MT];                      // tiles per M tile so far
+#pragma unroll
+    for (int m = 0; m < MT; ++m) done[m] = 0;
+    bool ok = true;
+    while (ok && next_piece<KT>(p, walk, w)) {
+      if (w.n_tiles <= 0) continue;
+      const int tiles_m = min(MT, (rows - w.rb * MT * 128 + 127) >> 7);          // M tiles that have a row
       auto steps_of = [&](int i) {              // 16-key steps of tile i that hold a live key
         const int t = w.lo + i;
         return min(KT / 16, (int)((t < w.n_ct ? w.len - t * KT : w.n - (t - w.n_ct) * KT) + 15) >> 4);
       };
-      auto issue_s = [&](int m, int i, bool release) {
+      auto issue_s = [&](int m, int i) {
         const int s = (kv + i) % ST, buf = (done[m] + i) % NB;
         const uint32_t k_lo = ((ptx::smem_u32(sK) + s * C::kTile) >> 4) | (1u << 16);
         const uint32_t q_lo = q_base + (uint32_t)((m * C::kQBytes) >> 4);
@@ -371,27 +431,29 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
             umma::mma_bf16(tmem + (uint32_t)(128 * m + 64 * buf), a, bd, idesc, ks > 0);
           }
           umma::commit(&sh.s_full[m][buf]);
-          if (release) umma::commit(&sh.k_empty[s]);
+          if (m + 1 == tiles_m) {
+            umma::commit(&sh.k_empty[s]);
+            if (i + 1 == w.n_tiles) umma::commit(&sh.q_empty);
+          }
         }
         __syncwarp();
       };
-      bool ok = umma::warp_wait(&sh.q_full, n_q & 1, &sh.abort, p.dev_status) &&
-                umma::warp_wait(&sh.k_full[kv % ST], (kv / ST) & 1, &sh.abort, p.dev_status);
-      if (ok)
-        for (int m = 0; m < tiles_m; ++m) issue_s(m, 0, m + 1 == tiles_m);
+      ok = umma::warp_wait(&sh.q_full, n_q & 1, &sh.abort, p.dev_status) &&
+           umma::warp_wait(&sh.k_full[kv % ST], (kv / ST) & 1, &sh.abort, p.dev_status);
+      ++n_q;
+      // (the S buffers: P of the tile that used one before was consumed by a product issued before, and the pipe runs them
+      // in issue order)
+      for (int m = 0; ok && m < tiles_m; ++m) issue_s(m, 0);
       for (int i = 0; ok && i < w.n_tiles; ++i) {
         const int s = (kv + i) % ST, steps = steps_of(i);
         const uint32_t v_lo = ((ptx::smem_u32(sV) + s * C::kTile) >> 4) | v_lbo;
-        // S of the next tile: before P V of this one where S has a second buffer (that one held S and P of two tiles ago,
-        // whose P V was issued before, and the pipe runs them in issue order), else right behind it
-        if (NB == 2 && i + 1 < w.n_tiles) {
+        // S of the next tile: before P V of this one where S has a second buffer, else right behind it
+        if (i + 1 < w.n_tiles) {
           ok = umma::warp_wait(&sh.k_full[(kv + i + 1) % ST], ((kv + i + 1) / ST) & 1, &sh.abort, p.dev_status);
           if (!ok) break;
-          issue_s(0, i + 1, true);
+          if (NB == 2) issue_s(0, i + 1);
         }
         ok = umma::warp_wait(&sh.v_full[s], ((kv + i) / ST) & 1, &sh.abort, p.dev_status);
-        if (NB == 1 && ok && i + 1 < w.n_tiles)
-          ok = umma::warp_wait(&sh.k_full[(kv + i + 1) % ST], ((kv + i + 1) / ST) & 1, &sh.abort, p.dev_status);
         for (int m = 0; ok && m < tiles_m; ++m) {
           const int buf = (done[m] + i) % NB;
           const uint32_t ph = ((done[m] + i) / NB) & 1, o_tmem = tmem + C::kOCol + (uint32_t)(D * m);
@@ -414,36 +476,63 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
             }
             __syncwarp();
           }
-          if (NB == 1 && ok && i + 1 < w.n_tiles) issue_s(m, i + 1, m + 1 == tiles_m);
+          if (NB == 1 && ok && i + 1 < w.n_tiles) issue_s(m, i + 1);
         }
       }
-    } else if (warp < 4 * tiles_m) {
-      // ------------------------------------------------------------------ softmax: one thread per query row
-      const int m = MT == 1 ? 0 : warp >> 2;
-      int tc = done[0];                         // tiles of this M tile before the piece
-      if (MT == 2 && m == 1) tc = done[MT - 1];
-      const int r = r0 + 128 * m + 32 * (warp & 3) + lane;
-      const int node = r % p.N;
-      const bool live_row = r < rows && node < w.n;
-      const bool live_warp = r0 + 128 * m + 32 * (warp & 3) < rows;
-      uint32_t aw[kTreeWords];
+      kv += w.n_tiles;
 #pragma unroll
-      for (int x = 0; x < kTreeWords; ++x) aw[x] = live_row ? sh.anc[node][x] : 0u;
-      const uint32_t lane_base = (uint32_t)(32 * (warp & 3)) << 16;
-      const uint32_t o_addr = tmem + lane_base + C::kOCol + (uint32_t)(D * m);
-      float m_use = -INFINITY, l_run = 0.f;
-      bool ok = true;
-      for (int i = 0; i < w.n_tiles; ++i) {
-        const int t = w.lo + i, buf = (tc + i) % NB;
-        const bool in_tree = t >= w.n_ct;
-        const int live = in_tree ? w.n - (t - w.n_ct) * KT : w.len - t * KT;
-        if (in_tree || live < KT) {
-          // V rows that must not meet a zero weight: by the warps of the first M tile, the others wait for them
+      for (int m = 0; m < MT; ++m) done[m] += m < tiles_m ? w.n_tiles : 0;
+    }
+  } else {
+    // ------------------------------------------------------------------ softmax: one thread per query row
+    const int m = warp >> 2, in_group = tid & 127;
+    const uint32_t lane_base = (uint32_t)(32 * (warp & 3)) << 16;
+    const uint32_t o_addr = tmem + lane_base + C::kOCol + (uint32_t)(D * m);
+    int tc = 0, pieces = 0, fixes[3] = {0, 0, 0};      // tiles and pieces of this M tile so far; uses of sh.fixed
+    bool ok = true;
+    while (ok && next_piece<KT>(p, walk, w)) {
+      if (w.n_tiles <= 0) {
+        if (tid == 0 && !counts_ok(p, w))
+          set_dev_status(p.dev_status, w.n < 0 || w.n > p.N ? NGC_DEV_BAD_TREE : NGC_DEV_BAD_COUNTS);
+        continue;
+      }
+      const int r0 = w.rb * MT * 128, slot = walk.seq & 3;
+      const bool in_tail = w.len % KT != 0 && w.lo < w.n_ct && w.lo + w.n_tiles >= w.n_ct;
+      const bool in_tree0 = w.lo <= w.n_ct && w.lo + w.n_tiles > w.n_ct, in_tree1 = w.lo <= w.n_ct + 1 && w.lo + w.n_tiles > w.n_ct + 1;
+      if (r0 + 128 * m < rows) {
+        const int r = r0 + 128 * m + 32 * (warp & 3) + lane;
+        const int node = r % p.N;
+        const bool live_row = r < rows && node < w.n;
+        const bool live_warp = r0 + 128 * m + 32 * (warp & 3) < rows;
+        // links: a node per thread is checked, and the row's own are followed
+        const int32_t* parent = p.parent + (int64_t)w.b * p.N;
+        if (in_group < w.n) {
+          const int pa = parent[in_group];
+          if (in_group == 0 ? pa != -1 : (pa < 0 || pa >= in_group)) sh.refused[m][slot] = walk.seq;
+        }
+        if (m == 0 && in_group < kTreeWords) sh.odd[slot][in_group] = 0;
+        ptx::mbar_arrive(&sh.checked[m]);
+        uint32_t aw[kTreeWords] = {0u, 0u, 0u, 0u};
+        for (int j = live_row && w.lo + w.n_tiles > w.n_ct ? node : -1; j >= 0;) {
+#pragma unroll
+          for (int x = 0; x < kTreeWords; ++x) aw[x] |= (j >> 5) == x ? 1u << (j & 31) : 0u;
+          const int pa = parent[j];
+          j = pa < j ? pa : -1;
+        }
+        if (m == 0 && (in_tree0 || in_tree1))    // the words above are zero before a tile's nodes are searched
+          ok = umma::warp_wait(&sh.checked[m], pieces & 1, &sh.abort, p.dev_status);
+        float m_use = -INFINITY, l_run = 0.f;
+        for (int i = 0; ok && i < w.n_tiles; ++i) {
+          const int t = w.lo + i, buf = (tc + i) % NB;
+          const bool in_tree = t >= w.n_ct;
+          const int live = in_tree ? w.n - (t - w.n_ct) * KT : w.len - t * KT;
+          const bool masked = in_tree || live < KT;
           const int f = in_tree ? 1 + t - w.n_ct : 0;
-          const int uses = f == 0 ? fixes[0] : f == 1 ? fixes[1] : fixes[2];
-          if (m == 0) {
+          if (masked && m == 0) {
+            // V rows that must not meet a zero weight: by the warps of the first M tile
             const int s = (kv + i) % ST;
-            if (!umma::warp_wait(&sh.v_full[s], ((kv + i) / ST) & 1, &sh.abort, p.dev_status)) { ok = false; break; }
+            ok = umma::warp_wait(&sh.v_full[s], ((kv + i) / ST) & 1, &sh.abort, p.dev_status);
+            if (!ok) break;
             const int n_rows = min(KT, ((live + 15) >> 4) << 4);
             for (int e = tid; e < n_rows * (D / 8); e += 128) {
               const int rr = e / (D / 8), c = e % (D / 8);               // (the swizzle permutes pieces within a row only)
@@ -456,178 +545,198 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
                 if (o.x | o.y | o.z | o.w) {
                   *at = make_uint4(x.x & ~o.x, x.y & ~o.y, x.z & ~o.z, x.w & ~o.w);
                   const int j = (t - w.n_ct) * KT + rr;
-                  atomicOr(&sh.odd[j >> 5], 1u << (j & 31));
+                  atomicOr(&sh.odd[slot][j >> 5], 1u << (j & 31));
                 }
               }
             }
             ptx::fence_proxy_async();
             ptx::mbar_arrive(&sh.fixed[f]);
-          } else if (!umma::warp_wait(&sh.fixed[f], uses & 1, &sh.abort, p.dev_status)) {
-            ok = false;
-            break;
           }
-        }
-        if (!umma::warp_wait(&sh.s_full[m][buf], ((tc + i) / NB) & 1, &sh.abort, p.dev_status)) { ok = false; break; }
-        umma::fence_after_sync();
-        if (!live_warp) {                       // rows that are not there: whatever P holds for them goes nowhere
-#pragma unroll
-          for (int e = 0; e < NH; ++e) ptx::mbar_arrive(&sh.p_full[m][buf][e]);
-          continue;
-        }
-        // 64 scores of the row at a time.  Of a 128-key tile the second half is read for the maximum, then the first half,
-        // which stays in registers for its exponentials; the second half is read again behind them (a read costs about
-        // 50 cycles; 128 scores in registers do not fit).
-        uint32_t zr[2][32];
-        const uint32_t s_addr = tmem + lane_base + (uint32_t)(128 * m + 64 * buf);
-        auto read_half = [&](int e) {
-          umma::tmem_ld32(s_addr + 64 * e, zr[0]);
-          umma::tmem_ld32(s_addr + 64 * e + 32, zr[1]);
-          umma::tmem_ld_wait();
-          if (in_tree || live < KT) {
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              uint32_t see;
-              if (!in_tree) see = live >= 64 * e + 32 * c + 32 ? 0xffffffffu : live > 64 * e + 32 * c ? (1u << (live - 64 * e - 32 * c)) - 1u : 0u;
-              else if (KT == 128) see = e == 0 ? aw[c] : aw[2 + c];
-              else see = t == w.n_ct ? aw[c] : aw[2 + c];
-#pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (!(see >> j & 1u)) zr[c][j] = 0xff800000u;            // -inf
-            }
-          }
-        };
-        float mxc[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int e = NH - 1; e >= 0; --e) {
-          read_half(e);
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int j = 0; j < 32; j += 8) {
-#pragma unroll
-              for (int x = 0; x < 4; ++x)
-                mxc[x] = umma::max3(mxc[x], __uint_as_float(zr[c][j + 2 * x]), __uint_as_float(zr[c][j + 2 * x + 1]));
-            }
-        }
-        const float mx = fmaxf(fmaxf(mxc[0], mxc[1]), fmaxf(mxc[2], mxc[3])) * p.scale_log2;
-        const bool grow = mx > m_use + kLazyRescale;                      // also the first visible key (m_use = -inf)
-        const bool rescale = grow && m_use != -INFINITY && i > 0;         // O already holds something for this row
-        if (__any_sync(0xffffffffu, rescale)) {
-          // P V of the tile before is complete (with one S buffer: S of this tile came behind it)
-          if (NB == 2 && !umma::warp_wait(&sh.o_done[m][(tc + i - 1) % NB], ((tc + i - 1) / NB) & 1, &sh.abort, p.dev_status)) { ok = false; break; }
+          ok = umma::warp_wait(&sh.s_full[m][buf], ((tc + i) / NB) & 1, &sh.abort, p.dev_status);
+          // (behind S of this tile every earlier use of the barrier is over, so its phase cannot be mistaken)
+          if (ok && masked && m != 0)
+            ok = umma::warp_wait(&sh.fixed[f], (f == 0 ? fixes[0] : f == 1 ? fixes[1] : fixes[2]) & 1, &sh.abort, p.dev_status);
+          if (!ok) break;
           umma::fence_after_sync();
-          const float alpha = rescale ? ptx::ex2_approx(m_use - mx) : 1.f;
-          l_run *= alpha;
-#pragma unroll 1
-          for (int c0 = 0; c0 < D; c0 += 16) {
-            uint32_t o[16];
-            umma::tmem_ld16(o_addr + c0, o);
-            umma::tmem_ld_wait();
+          if (!live_warp) {                     // rows that are not there: whatever P holds for them goes nowhere
 #pragma unroll
-            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
-            umma::tmem_st8(o_addr + c0, o);
-            umma::tmem_st8(o_addr + c0 + 8, o + 8);
+            for (int e = 0; e < NH; ++e) ptx::mbar_arrive(&sh.p_full[m][buf][e]);
+            continue;
           }
-          umma::tmem_st_wait();
-        }
-        if (grow) m_use = mx;
-        const float m_eff = m_use == -INFINITY ? 0.f : m_use;             // nothing visible yet: every exponential is 0
-        const uint64_t sc2 = umma::pack2(p.scale_log2, p.scale_log2), nm2 = umma::pack2(-m_eff, -m_eff);
-        uint64_t acc2[4] = {0ull, 0ull, 0ull, 0ull};
+          // 64 scores of the row at a time.  Of a 128-key tile the second half is read for the maximum, then the first half,
+          // which stays in registers for its exponentials; the second half is read again behind them (a read costs about
+          // 50 cycles; 128 scores in registers do not fit).
+          uint32_t zr[2][32];
+          const uint32_t s_addr = tmem + lane_base + (uint32_t)(128 * m + 64 * buf);
+          auto read_half = [&](int e) {
+            umma::tmem_ld32(s_addr + 64 * e, zr[0]);
+            umma::tmem_ld32(s_addr + 64 * e + 32, zr[1]);
+            umma::tmem_ld_wait();
+            if (masked) {
 #pragma unroll
-        for (int e = 0; e < NH; ++e) {
-          if (e > 0) read_half(e);
-          uint32_t pk[32];
+              for (int c = 0; c < 2; ++c) {
+                uint32_t see;
+                if (!in_tree) see = live >= 64 * e + 32 * c + 32 ? 0xffffffffu : live > 64 * e + 32 * c ? (1u << (live - 64 * e - 32 * c)) - 1u : 0u;
+                else if (KT == 128) see = e == 0 ? aw[c] : aw[2 + c];
+                else see = t == w.n_ct ? aw[c] : aw[2 + c];
 #pragma unroll
-          for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-              float x0, x1;
-              umma::unpack2(umma::fma2(umma::pack2(__uint_as_float(zr[c][j]), __uint_as_float(zr[c][j + 1])), sc2, nm2), x0, x1);
-              const float p0 = ptx::ex2_approx(x0), p1 = ptx::ex2_approx(x1);
-              acc2[(j >> 1) & 3] = umma::add2(acc2[(j >> 1) & 3], umma::pack2(p0, p1));
-              pk[16 * c + (j >> 1)] = ptx::pack_bf16x2(p0, p1);
-            }
-          umma::tmem_st32(s_addr + 32 * e, pk);                           // P over the S columns it came from, packed to half
-          umma::tmem_st_wait();
-          umma::fence_before_sync();
-          ptx::mbar_arrive(&sh.p_full[m][buf][e]);
-        }
-        float s0, s1;
-        umma::unpack2(umma::add2(umma::add2(acc2[0], acc2[1]), umma::add2(acc2[2], acc2[3])), s0, s1);
-        l_run += s0 + s1;
-      }
-      const int last = tc + w.n_tiles - 1;
-      if (ok) ok = umma::warp_wait(&sh.o_done[m][last % NB], (last / NB) & 1, &sh.abort, p.dev_status);
-      uint32_t odd[kTreeWords] = {0u, 0u, 0u, 0u};
-      for (int t = max(w.lo, w.n_ct); ok && t < w.lo + w.n_tiles; ++t)
-        ok = umma::warp_wait(&sh.fixed[1 + t - w.n_ct], (t == w.n_ct ? fixes[1] : fixes[2]) & 1, &sh.abort, p.dev_status);
-      if (ok && w.lo + w.n_tiles > w.n_ct) {
-#pragma unroll
-        for (int x = 0; x < kTreeWords; ++x) odd[x] = sh.odd[x] & aw[x];
-      }
-      if (ok && live_warp) {
-        umma::fence_after_sync();
-        const float inv = l_run == 0.f ? 0.f : 1.f / l_run;               // a NaN stays one
-        const int64_t pit = part0 + (r - r0);
-        if (!whole && r < rows) p.part_ml[pit] = live_row ? make_float2(m_use, l_run) : kNoPart;
-        const __nv_bfloat16* tv = (const __nv_bfloat16*)p.tree_v + (int64_t)w.strip * p.N * D;
-#pragma unroll 1
-        for (int c0 = 0; c0 < D; c0 += 32) {
-          uint32_t o[32];
-          __syncwarp();
-          umma::tmem_ld32(o_addr + c0, o);
-          umma::tmem_ld_wait();
-          if (odd[0] | odd[1] | odd[2] | odd[3]) {
-            for (int j = 0; j < w.n; ++j) {
-              const uint32_t word = j < 64 ? (j < 32 ? odd[0] : odd[1]) : (j < 96 ? odd[2] : odd[3]);
-              if (!(word >> (j & 31) & 1u)) continue;
-#pragma unroll
-              for (int c = 0; c < 32; ++c) {
-                const float v = __bfloat162float(tv[(int64_t)j * D + c0 + c]);
-                if (!isfinite(v)) o[c] = __float_as_uint(__uint_as_float(o[c]) + v);
+                for (int j = 0; j < 32; ++j)
+                  if (!(see >> j & 1u)) zr[c][j] = 0xff800000u;          // -inf
               }
             }
+          };
+          float mxc[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int e = NH - 1; e >= 0; --e) {
+            read_half(e);
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+              for (int j = 0; j < 32; j += 8) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                  mxc[x] = max3_nan(mxc[x], __uint_as_float(zr[c][j + 2 * x]), __uint_as_float(zr[c][j + 2 * x + 1]));
+              }
           }
-          if (!live_row) {
-            // nothing to write
-          } else if (!whole) {
+          const float mx = max3_nan(max3_nan(mxc[0], mxc[1], mxc[2]), mxc[3], mxc[3]) * p.scale_log2;
+          if (!(mx < INFINITY)) {               // a score of infinity or NaN: the row is NaN (also if it is all there is so far)
+            l_run = __int_as_float(0x7fffffff);
+            if (m_use == -INFINITY) m_use = 0.f;
+          }
+          const bool grow = mx > m_use + kLazyRescale;                    // also the first visible key (m_use = -inf)
+          const bool rescale = grow && m_use != -INFINITY && i > 0;       // O already holds something for this row
+          if (__any_sync(0xffffffffu, rescale)) {
+            // P V of the tile before is complete (with one S buffer: S of this tile came behind it)
+            if (NB == 2) {
+              ok = umma::warp_wait(&sh.o_done[m][(tc + i - 1) % NB], ((tc + i - 1) / NB) & 1, &sh.abort, p.dev_status);
+              if (!ok) break;
+              umma::fence_after_sync();
+            }
+            const float alpha = rescale ? ptx::ex2_approx(m_use - mx) : 1.f;
+            l_run *= alpha;
+#pragma unroll 1
+            for (int c0 = 0; c0 < D; c0 += 16) {
+              uint32_t o[16];
+              umma::tmem_ld16(o_addr + c0, o);
+              umma::tmem_ld_wait();
 #pragma unroll
-            for (int c = 0; c < 32; c += 4)
-              *reinterpret_cast<uint4*>(p.part_o + pit * D + c0 + c) = make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
-          } else if (p.out_bf16) {
+              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+              umma::tmem_st8(o_addr + c0, o);
+              umma::tmem_st8(o_addr + c0 + 8, o + 8);
+            }
+            umma::tmem_st_wait();
+          }
+          if (grow) m_use = mx;
+          const float m_eff = m_use == -INFINITY ? 0.f : m_use;           // nothing visible yet: every exponential is 0
+          const uint64_t sc2 = umma::pack2(p.scale_log2, p.scale_log2), nm2 = umma::pack2(-m_eff, -m_eff);
+          uint64_t acc2[4] = {0ull, 0ull, 0ull, 0ull};
+          // weights 2^(z * scale - m) of 64 keys as bf16 pairs; kPoly of every four pairs on the FMA pipe (not where scores
+          // are masked: their weight is exactly 0)
+          auto weights = [&](uint32_t (&pk)[32], auto kPoly) {
 #pragma unroll
-            for (int c = 0; c < 32; c += 8)
-              *reinterpret_cast<uint4*>((__nv_bfloat16*)p.out + (row0 + r) * D + c0 + c) =
-                  make_uint4(ptx::pack_bf16x2(__uint_as_float(o[c]) * inv, __uint_as_float(o[c + 1]) * inv),
-                             ptx::pack_bf16x2(__uint_as_float(o[c + 2]) * inv, __uint_as_float(o[c + 3]) * inv),
-                             ptx::pack_bf16x2(__uint_as_float(o[c + 4]) * inv, __uint_as_float(o[c + 5]) * inv),
-                             ptx::pack_bf16x2(__uint_as_float(o[c + 6]) * inv, __uint_as_float(o[c + 7]) * inv));
-          } else {
+            for (int c = 0; c < 2; ++c)
 #pragma unroll
-            for (int c = 0; c < 32; c += 4)
-              *reinterpret_cast<float4*>((float*)p.out + (row0 + r) * D + c0 + c) =
-                  make_float4(__uint_as_float(o[c]) * inv, __uint_as_float(o[c + 1]) * inv,
-                              __uint_as_float(o[c + 2]) * inv, __uint_as_float(o[c + 3]) * inv);
+              for (int j = 0; j < 32; j += 2) {
+                const uint64_t x2 = umma::fma2(umma::pack2(__uint_as_float(zr[c][j]), __uint_as_float(zr[c][j + 1])), sc2, nm2);
+                const int pair = (j >> 1) & 3;
+                float p0, p1;
+                if (pair < decltype(kPoly)::value) {
+                  umma::unpack2(exp2_poly2(x2), p0, p1);
+                } else {
+                  float x0, x1;
+                  umma::unpack2(x2, x0, x1);
+                  p0 = ptx::ex2_approx(x0);
+                  p1 = ptx::ex2_approx(x1);
+                }
+                acc2[pair] = umma::add2(acc2[pair], umma::pack2(p0, p1));
+                pk[16 * c + (j >> 1)] = ptx::pack_bf16x2(p0, p1);
+              }
+          };
+#pragma unroll
+          for (int e = 0; e < NH; ++e) {
+            if (e > 0) read_half(e);
+            uint32_t pk[32];
+            if (C::kPolyPairs == 0 || masked) weights(pk, Int<0>());
+            else weights(pk, Int<C::kPolyPairs>());
+            umma::tmem_st32(s_addr + 32 * e, pk);                         // P over the S columns it came from, packed to half
+            umma::tmem_st_wait();
+            umma::fence_before_sync();
+            ptx::mbar_arrive(&sh.p_full[m][buf][e]);
+          }
+          float s0, s1;
+          umma::unpack2(umma::add2(umma::add2(acc2[0], acc2[1]), umma::add2(acc2[2], acc2[3])), s0, s1);
+          l_run += s0 + s1;
+        }
+        // ---- the row's sums leave
+        const int last = tc + w.n_tiles - 1;
+        ok = ok && umma::warp_wait(&sh.o_done[m][last % NB], (last / NB) & 1, &sh.abort, p.dev_status) &&
+             umma::warp_wait(&sh.checked[m], pieces & 1, &sh.abort, p.dev_status) &&
+             (!in_tree0 || umma::warp_wait(&sh.fixed[1], fixes[1] & 1, &sh.abort, p.dev_status)) &&
+             (!in_tree1 || umma::warp_wait(&sh.fixed[2], fixes[2] & 1, &sh.abort, p.dev_status));
+        if (!ok) break;
+        umma::fence_after_sync();
+        const bool whole = w.first && w.last, refused = sh.refused[m][slot] == walk.seq;
+        const int64_t pit = ((int64_t)blockIdx.x * 2 + (w.first ? 1 : 0)) * p.block_rows + (r - r0);     // in this CTA's slots
+        if (refused && in_group == 0) set_dev_status(p.dev_status, NGC_DEV_BAD_TREE);
+        if (!whole && r < rows) p.part_ml[pit] = live_row && !refused ? make_float2(m_use, l_run) : kNoPart;
+        if (live_warp && !refused) {
+          uint32_t odd[kTreeWords];
+#pragma unroll
+          for (int x = 0; x < kTreeWords; ++x) odd[x] = in_tree0 || in_tree1 ? sh.odd[slot][x] & aw[x] : 0u;
+          const float inv = l_run == 0.f ? 0.f : 1.f / l_run;             // a NaN stays one
+          const int64_t out_row = (((int64_t)w.l * p.B + w.b) * p.Hq + (int64_t)w.h * p.g) * p.N + r;
+          const __nv_bfloat16* tv = (const __nv_bfloat16*)p.tree_v + (int64_t)w.strip * p.N * D;
+#pragma unroll 1
+          for (int c0 = 0; c0 < D; c0 += 32) {
+            uint32_t o[32];
+            __syncwarp();
+            umma::tmem_ld32(o_addr + c0, o);
+            umma::tmem_ld_wait();
+            if (odd[0] | odd[1] | odd[2] | odd[3]) {
+              for (int j = 0; j < w.n; ++j) {
+                const uint32_t word = j < 64 ? (j < 32 ? odd[0] : odd[1]) : (j < 96 ? odd[2] : odd[3]);
+                if (!(word >> (j & 31) & 1u)) continue;
+#pragma unroll
+                for (int c = 0; c < 32; ++c) {
+                  const float v = __bfloat162float(tv[(int64_t)j * D + c0 + c]);
+                  if (!isfinite(v)) o[c] = __float_as_uint(__uint_as_float(o[c]) + v);
+                }
+              }
+            }
+            if (!live_row) {
+              // nothing to write
+            } else if (!whole) {
+#pragma unroll
+              for (int c = 0; c < 32; c += 8) store_sector(p.part_o + pit * D + c0 + c, o + c);
+            } else if (p.out_bf16) {
+#pragma unroll
+              for (int c = 0; c < 32; c += 8)
+                *reinterpret_cast<uint4*>((__nv_bfloat16*)p.out + out_row * D + c0 + c) =
+                    make_uint4(ptx::pack_bf16x2(__uint_as_float(o[c]) * inv, __uint_as_float(o[c + 1]) * inv),
+                               ptx::pack_bf16x2(__uint_as_float(o[c + 2]) * inv, __uint_as_float(o[c + 3]) * inv),
+                               ptx::pack_bf16x2(__uint_as_float(o[c + 4]) * inv, __uint_as_float(o[c + 5]) * inv),
+                               ptx::pack_bf16x2(__uint_as_float(o[c + 6]) * inv, __uint_as_float(o[c + 7]) * inv));
+            } else {
+#pragma unroll
+              for (int c = 0; c < 32; c += 4)
+                *reinterpret_cast<float4*>((float*)p.out + out_row * D + c0 + c) =
+                    make_float4(__uint_as_float(o[c]) * inv, __uint_as_float(o[c + 1]) * inv,
+                                __uint_as_float(o[c + 2]) * inv, __uint_as_float(o[c + 3]) * inv);
+            }
           }
         }
+        umma::fence_before_sync();              // O may be overwritten once the next P of this thread is out
+        tc += w.n_tiles;
+        ++pieces;
       }
-    }
-    // ---- the piece is done in every role: masks, Q and O may change
-    umma::fence_before_sync();
-    if (__syncthreads_or(*(volatile int*)&sh.abort)) break;
-    umma::fence_after_sync();
-    if (ok_unit && w.n_tiles > 0) {
       kv += w.n_tiles;
-      ++n_q;
-#pragma unroll
-      for (int m = 0; m < MT; ++m) done[m] += m < tiles_m ? w.n_tiles : 0;
-      if (w.len % KT != 0 && w.lo < w.n_ct && w.lo + w.n_tiles >= w.n_ct) ++fixes[0];
-      if (w.lo <= w.n_ct && w.lo + w.n_tiles > w.n_ct) ++fixes[1];
-      if (w.lo <= w.n_ct + 1 && w.lo + w.n_tiles > w.n_ct + 1) ++fixes[2];
+      fixes[0] += in_tail;
+      fixes[1] += in_tree0;
+      fixes[2] += in_tree1;
     }
   }
-  // ---- teardown: every MMA has completed before tensor memory is released
+  __syncthreads();
+  // ---- teardown: every role has left its loops; every MMA has completed before tensor memory is released
   if (warp == C::kMmaWarp) {
     if (umma::elect_one()) umma::commit(&sh.drain);
     __syncwarp();
@@ -653,10 +762,11 @@ template <int D> __global__ void __launch_bounds__(256) tree_join_kernel(TreeAtt
   if (t1 == t0) return;                                                            // nothing of this unit is computed
   const int c0 = tree_even_owner(t0, total, ctas), c1 = tree_even_owner(t1 - 1, total, ctas);
   if (c0 == c1) return;                                                            // one CTA had all of it
-  Piece w;
-  unit_of(p, u, w);
-  const int r = w.rb * p.block_rows + rr;
+  int item = u;
+  const int r = item % p.row_blocks * p.block_rows + rr;
   if (r >= p.g * p.N) return;
+  item /= p.row_blocks;
+  const int h = item % p.Hkv, b = item / p.Hkv % p.B, l = p.layer_begin + item / p.Hkv / p.B;
   // part of CTA x: the unit begins in c0 (its second slot) and goes on through the others (their first)
   auto slot = [&](int x) { return ((int64_t)x * 2 + (x == c0 ? 1 : 0)) * p.block_rows + rr; };
   if (p.part_ml[slot(c0)].y < 0.f) return;                                         // kNoPart
@@ -672,7 +782,7 @@ template <int D> __global__ void __launch_bounds__(256) tree_join_kernel(TreeAtt
     ls = fmaf(ml.y, f, ls);
   }
   const float inv = ls == 0.f ? 0.f : 1.f / ls;
-  const int64_t row = (((int64_t)w.l * p.B + w.b) * p.Hq + (int64_t)w.h * p.g) * p.N + r;
+  const int64_t row = (((int64_t)l * p.B + b) * p.Hq + (int64_t)h * p.g) * p.N + r;
   tree_store_out4(p, row * D + c, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
 }
 
