@@ -336,7 +336,7 @@ TreeScratch tree_scratch(const ngc_cache* c, const TreePlan& pl, int layers, int
   TreeScratch s;
   s.ml = align256(parts * c->d * 4);
   s.plan = s.ml + align256(parts * 8);
-  s.bytes = s.plan + (pl.even ? align256(((size_t)pl.n_units + 2) * 4) : 0);
+  s.bytes = s.plan + (pl.even ? align256((size_t)pl.grid * 8) : 0);
   return s;
 }
 
@@ -369,7 +369,7 @@ int tree_impl(const ngc_cache* c, const PagedView& pv, const void* q, const void
     if (!ws || ws_bytes < need.bytes || ((uintptr_t)ws & 255)) return NGC_ERR_WORKSPACE;
     p.part_o = (float*)ws;
     p.part_ml = (float2*)((char*)ws + need.ml);
-    p.plan = (int32_t*)((char*)ws + need.plan);
+    p.plan = (int2*)((char*)ws + need.plan);
   }
   const int64_t items = (int64_t)p.n_layers * c->B * c->Hkv * p.row_blocks * p.n_split;
   const int64_t out_threads = (int64_t)p.n_layers * c->B * c->Hq * N * (c->d / 4);

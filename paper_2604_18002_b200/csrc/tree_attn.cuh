@@ -24,7 +24,7 @@ struct TreeAttnParams {
   float* part_o;                // parts of split rows: sums, unnormalised ...
   float2* part_ml;              // ... and (maximum in log2 units, sum of weights)
                                 //   FMA path: [n_layers][B][Hq][N][n_split]; tensor cores: [CTA][2][block_rows]
-  int32_t* plan;                // tensor cores: tiles before every unit [n_units + 1], CTAs that had work
+  int2* plan;                   // tensor cores, even split: per CTA, the unit that begins in it and goes on, the CTA it ends in or -1
   int32_t* dev_status;
   int64_t rows;
   int L, B, Hq, Hkv, d, g, N;
@@ -116,14 +116,21 @@ __host__ __device__ constexpr int tree_umma_tiles(int rows) { return rows <= 128
 __host__ __device__ constexpr int tree_umma_keys(int tiles) { return tiles == 1 ? 64 : 128; }
 int launch_tree_umma(const TreeAttnParams& p, cudaStream_t stream);
 
-// Even split of `total` tiles: how many of `grid` CTAs take part (each gets at least kTreeMinTiles tiles), the first tile
-// of CTA c, and the CTA that has tile g.
+// Even split of `total` tiles: how many of `grid` CTAs take part (each gets at least kTreeMinTiles tiles, so `per` below is
+// at least one), the first tile of CTA c, and the CTA that has tile g.
 constexpr int kTreeMaxUnits = 1184, kTreeMinTiles = 3;
 __host__ __device__ inline int tree_even_ctas(int total, int grid) {
   const int most = total / kTreeMinTiles;
   return most < 1 ? 1 : (most < grid ? most : grid);
 }
-__host__ __device__ inline int tree_even_first(int c, int total, int ctas) { return (int)((int64_t)total * c / ctas); }
-__host__ __device__ inline int tree_even_owner(int g, int total, int ctas) { return (int)((((int64_t)g + 1) * ctas - 1) / total); }
+struct TreeEven {
+  uint32_t per, more;           // tiles per CTA; the first `more` CTAs have one more
+  __device__ __forceinline__ TreeEven(int total, int ctas) : per((uint32_t)total / (uint32_t)ctas), more((uint32_t)total % (uint32_t)ctas) {}
+  __device__ __forceinline__ int first(uint32_t c) const { return (int)(c * per + min(c, more)); }
+  __device__ __forceinline__ int owner(uint32_t g) const {
+    const uint32_t split = more * (per + 1);
+    return (int)(g < split ? g / (per + 1) : more + (g - split) / per);
+  }
+};
 
 }  // namespace ngc

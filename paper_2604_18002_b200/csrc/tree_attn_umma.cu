@@ -20,9 +20,7 @@
 //   softmax warps    (4 MT) one thread per row: follows its node's links to the root for its mask (needed only in tree
 //                    tiles; the cache's last tile has a common one), online softmax in the log2 domain, P as bf16 over
 //                    the S it came from, 64 keys at a time.  The maximum used only moves when the true one has grown by
-//                    more than a factor 2^8, so O in tensor memory is rarely rescaled.  With two M tiles a part of
-//                    the exponentials is a polynomial on the FMA pipe: one exponential takes the special-function unit 8
-//                    cycles per warp, 128 x 128 of them as long as the tensor pipe needs for their products.
+//                    more than a factor 2^8, so O in tensor memory is rarely rescaled.
 //
 // The roles only meet at mbarriers, also from one unit to the next: loads and scores of the next unit run under the
 // end of the current one.
@@ -63,7 +61,6 @@ template <int D, int MT> struct Cfg {
   static constexpr int kTile = kKeys * D * 2;              // K or V tile
   static constexpr int kQBytes = 128 * D * 2;              // Q of an M tile
   static constexpr int kSmem = MT * kQBytes + 2 * kStages * kTile + 1024;
-  static constexpr int kPolyPairs = MT == 1 ? 0 : 1;       // of four pairs of exponentials on the FMA pipe
   static constexpr uint32_t kOCol = 128 * MT;              // S[m][buf] at 128 m + 64 buf, O[m] behind
   static constexpr uint32_t kCols = MT == 1 ? 256 : 512;
 };
@@ -72,8 +69,6 @@ template <int D, int MT> struct Cfg {
 // tree's K and V (16 rows, a plane per strip); Q (128 rows).
 struct KvMaps { CUtensorMap whole, part, tree; };
 struct Maps { KvMaps k, v; CUtensorMap q; };
-
-template <int N> struct Int { static constexpr int value = N; };
 
 template <int D, int MT> struct Shared {
   using C = Cfg<D, MT>;
@@ -94,28 +89,30 @@ template <int D, int MT> struct Shared {
 struct Piece {
   int b, h, l, lr, rb, n, len, lo, n_tiles, n_ct;      // tiles [lo, lo + n_tiles) of the unit; the first n_ct are the cache's
   int plane, strip;                                    // of the cache; of the tree's K and V
-  bool first, last;                                    // holds the unit's first / last tile
+  int64_t base;                                        // row of a plane at which the sequence (or its pages) begins
+  bool fits, first, last;                              // holds the unit's first / last tile
 };
 // This CTA's share: from tile `lo` of unit `u` on, n_left tiles in all; `seq` pieces so far.
 struct Walk { int u, lo, n_left, seq; };
 
-__device__ __forceinline__ void unit_of(const TreeAttnParams& p, int u, Piece& w) {
-  w.rb = u % p.row_blocks; u /= p.row_blocks;
-  w.h = u % p.Hkv; u /= p.Hkv;
-  w.b = u % p.B;
-  w.lr = u / p.B;
+// Decodes unit u.  All of its numbers are loaded at once; `fits` = node count and length can be worked with (links are checked
+// later); returns its key tiles, 0 for a unit that has nothing to do or does not fit.
+template <int KT> __device__ __forceinline__ int unit_of(const TreeAttnParams& p, uint32_t u, Piece& w) {
+  if (p.row_blocks > 1) { w.rb = u % (uint32_t)p.row_blocks; u /= (uint32_t)p.row_blocks; } else { w.rb = 0; }
+  w.h = u % (uint32_t)p.Hkv; u /= (uint32_t)p.Hkv;
+  w.lr = p.n_layers > 1 ? u / (uint32_t)p.B : 0;
+  w.b = u - w.lr * p.B;
   w.l = p.layer_begin + w.lr;
-  w.n = p.n_nodes ? p.n_nodes[w.b] : p.N;
-  w.len = p.lens[len_index(p.lens_lists, p.L, p.Hkv, w.b, w.l, w.h)];
+  const int n = p.n_nodes ? p.n_nodes[w.b] : p.N;
+  const int len = p.lens[p.lens_lists ? len_index(p.lens_lists, p.L, p.Hkv, w.b, w.l, w.h) : w.b];
+  w.base = p.page_table ? (int64_t)w.b * p.pages_cap * p.page : p.seq_off[w.b];
+  const int64_t cap = p.page_table ? (int64_t)p.pages_cap * p.page : p.seq_off[w.b + 1] - w.base;
+  w.n = n;
+  w.len = len;
   w.plane = w.l * p.Hkv + w.h;
   w.strip = (w.l * p.B + w.b) * p.Hkv + w.h;
-}
-// Whether node count and length can be worked with (links are checked later).
-__device__ __forceinline__ bool counts_ok(const TreeAttnParams& p, const Piece& w) {
-  return w.n >= 0 && w.n <= p.N && w.len >= 0 && w.len <= tree_capacity(p, w.b);
-}
-template <int KT> __device__ __forceinline__ int unit_tiles(const TreeAttnParams& p, const Piece& w) {
-  return counts_ok(p, w) && w.n > 0 ? (w.len + KT - 1) / KT + (w.n + KT - 1) / KT : 0;
+  w.fits = (n >= 0) & (n <= p.N) & (len >= 0) & (len <= cap);
+  return w.fits && n > 0 ? (int)((uint32_t)(len + KT - 1) / KT + (uint32_t)(n + KT - 1) / KT) : 0;
 }
 
 // The next piece of the walk; false at its end.  (A unit per CTA: also a unit without tiles.)
@@ -123,8 +120,7 @@ template <int KT> __device__ __forceinline__ bool next_piece(const TreeAttnParam
   if (k.n_left <= 0) return false;
   int nt;
   for (;; ++k.u, k.lo = 0) {
-    unit_of(p, k.u, w);
-    nt = unit_tiles<KT>(p, w);
+    nt = unit_of<KT>(p, (uint32_t)k.u, w);
     if (nt > 0 || !p.even) break;
   }
   w.lo = k.lo;
@@ -220,23 +216,6 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-// 2^x for a pair of finite x <= 100 on the FMA pipe: x = n + f with |f| <= 1/2, 2^f by its minimax polynomial of degree 4
-// (found with the Remez exchange; relative error 2.7e-6 in fp32), n added to the exponent.  Below 2^-126: 2^-126.
-__device__ __forceinline__ uint64_t exp2_poly2(uint64_t x2) {
-  float x0, x1, r0, r1;
-  umma::unpack2(x2, x0, x1);
-  x2 = umma::pack2(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
-  const uint64_t n2 = umma::add2(x2, umma::pack2(12582912.f, 12582912.f));             // 1.5 * 2^23: rounds to whole numbers
-  const uint64_t f2 = umma::fma2(umma::add2(n2, umma::pack2(-12582912.f, -12582912.f)), umma::pack2(-1.f, -1.f), x2);
-  uint64_t r2 = umma::fma2(umma::pack2(9.570101911e-03f, 9.570101911e-03f), f2, umma::pack2(5.591786032e-02f, 5.591786032e-02f));
-  r2 = umma::fma2(r2, f2, umma::pack2(2.402474483e-01f, 2.402474483e-01f));
-  r2 = umma::fma2(r2, f2, umma::pack2(6.931218147e-01f, 6.931218147e-01f));
-  r2 = umma::fma2(r2, f2, umma::pack2(9.999992614e-01f, 9.999992614e-01f));
-  umma::unpack2(r2, r0, r1);
-  umma::unpack2(n2, x0, x1);
-  return umma::pack2(__uint_as_float(__float_as_uint(r0) + (__float_as_uint(x0) << 23)),
-                     __uint_as_float(__float_as_uint(r1) + (__float_as_uint(x1) << 23)));
-}
 // 32 consecutive bytes, a whole sector, at once
 __device__ __forceinline__ void store_sector(float* p, const uint32_t* r) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
@@ -307,10 +286,11 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     int sum = 0;
     for (int i = u0; i < u1; ++i) {
       Piece w;
-      unit_of(p, i, w);
-      const int t = unit_tiles<KT>(p, w);
+      const int t = unit_of<KT>(p, (uint32_t)i, w);
       sh.base[i] = t;
       sum += t;
+      // counts that cannot be worked with have no tiles: reported here, by the first CTA
+      if (blockIdx.x == 0 && !w.fits) set_dev_status(p.dev_status, w.n < 0 || w.n > p.N ? NGC_DEV_BAD_TREE : NGC_DEV_BAD_COUNTS);
     }
     int incl = sum;
 #pragma unroll
@@ -330,11 +310,8 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     if (tid == NT - 1) sh.base[p.n_units] = before;
     __syncthreads();
     const int total = sh.base[p.n_units], ctas = tree_even_ctas(total, gridDim.x);
-    if (blockIdx.x == 0) {                      // for the kernel that joins the parts
-      for (int i = tid; i <= p.n_units; i += NT) p.plan[i] = sh.base[i];
-      if (tid == 0) p.plan[p.n_units + 1] = ctas;
-    }
-    const int g0 = tree_even_first(blockIdx.x, total, ctas), g1 = tree_even_first(blockIdx.x + 1, total, ctas);
+    const TreeEven even(total, ctas);
+    const int g0 = even.first(blockIdx.x), g1 = even.first(blockIdx.x + 1);
     walk.n_left = (int)blockIdx.x < ctas ? g1 - g0 : 0;
     // the unit that tile g0 belongs to
     int lo = 0, hi = p.n_units;
@@ -344,13 +321,14 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     }
     walk.u = lo;
     walk.lo = g0 - sh.base[lo];
-    // counts that cannot be worked with have no tiles: report them here
-    if (blockIdx.x == 0)
-      for (int i = u0; i < u1; ++i) {
-        Piece w;
-        unit_of(p, i, w);
-        if (!counts_ok(p, w)) set_dev_status(p.dev_status, w.n < 0 || w.n > p.N ? NGC_DEV_BAD_TREE : NGC_DEV_BAD_COUNTS);
-      }
+    // for the kernel that joins the parts: the unit that begins here and goes on elsewhere (at most the last one), and
+    // the CTA that it ends in
+    if (tid == 0) {
+      int last = lo, end = -1;
+      while (walk.n_left > 0 && sh.base[last + 1] < g1) ++last;
+      if (walk.n_left > 0 && sh.base[last] >= g0 && sh.base[last + 1] > g1) end = even.owner(sh.base[last + 1] - 1);
+      p.plan[blockIdx.x] = make_int2(last, end);
+    }
   }
 
   // Every role takes the same walk.  Ring positions and barrier phases follow from running counters over its pieces: tiles
@@ -368,7 +346,7 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     bool ok = true;
     while (ok && next_piece<KT>(p, walk, w)) {
       if (w.n_tiles <= 0) continue;
-      const int base = (int)(p.page_table ? (int64_t)w.b * p.pages_cap * p.page : p.seq_off[w.b]);
+      const int base = (int)w.base;
       PageWalk pages;
       if (p.page_table)
         pages.start(p.page_table + ((int64_t)w.b * p.G + list_of(p.lists, w.l, w.h, p.Hkv)) * p.pages_cap, p.pages_cap,
@@ -492,7 +470,7 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     bool ok = true;
     while (ok && next_piece<KT>(p, walk, w)) {
       if (w.n_tiles <= 0) {
-        if (tid == 0 && !counts_ok(p, w))
+        if (tid == 0 && !w.fits)
           set_dev_status(p.dev_status, w.n < 0 || w.n > p.N ? NGC_DEV_BAD_TREE : NGC_DEV_BAD_COUNTS);
         continue;
       }
@@ -630,34 +608,20 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
           const float m_eff = m_use == -INFINITY ? 0.f : m_use;           // nothing visible yet: every exponential is 0
           const uint64_t sc2 = umma::pack2(p.scale_log2, p.scale_log2), nm2 = umma::pack2(-m_eff, -m_eff);
           uint64_t acc2[4] = {0ull, 0ull, 0ull, 0ull};
-          // weights 2^(z * scale - m) of 64 keys as bf16 pairs; kPoly of every four pairs on the FMA pipe (not where scores
-          // are masked: their weight is exactly 0)
-          auto weights = [&](uint32_t (&pk)[32], auto kPoly) {
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-              for (int j = 0; j < 32; j += 2) {
-                const uint64_t x2 = umma::fma2(umma::pack2(__uint_as_float(zr[c][j]), __uint_as_float(zr[c][j + 1])), sc2, nm2);
-                const int pair = (j >> 1) & 3;
-                float p0, p1;
-                if (pair < decltype(kPoly)::value) {
-                  umma::unpack2(exp2_poly2(x2), p0, p1);
-                } else {
-                  float x0, x1;
-                  umma::unpack2(x2, x0, x1);
-                  p0 = ptx::ex2_approx(x0);
-                  p1 = ptx::ex2_approx(x1);
-                }
-                acc2[pair] = umma::add2(acc2[pair], umma::pack2(p0, p1));
-                pk[16 * c + (j >> 1)] = ptx::pack_bf16x2(p0, p1);
-              }
-          };
 #pragma unroll
           for (int e = 0; e < NH; ++e) {
             if (e > 0) read_half(e);
             uint32_t pk[32];
-            if (C::kPolyPairs == 0 || masked) weights(pk, Int<0>());
-            else weights(pk, Int<C::kPolyPairs>());
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+              for (int j = 0; j < 32; j += 2) {
+                float x0, x1;
+                umma::unpack2(umma::fma2(umma::pack2(__uint_as_float(zr[c][j]), __uint_as_float(zr[c][j + 1])), sc2, nm2), x0, x1);
+                const float p0 = ptx::ex2_approx(x0), p1 = ptx::ex2_approx(x1);
+                acc2[(j >> 1) & 3] = umma::add2(acc2[(j >> 1) & 3], umma::pack2(p0, p1));
+                pk[16 * c + (j >> 1)] = ptx::pack_bf16x2(p0, p1);
+              }
             umma::tmem_st32(s_addr + 32 * e, pk);                         // P over the S columns it came from, packed to half
             umma::tmem_st_wait();
             umma::fence_before_sync();
@@ -750,40 +714,76 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
   }
 }
 
-// Joins the parts of every unit that was cut: D / 4 threads per query row.
-template <int D> __global__ void __launch_bounds__(256) tree_join_kernel(TreeAttnParams p) {
-  constexpr int kPerRow = D / 4, kRows = 256 / kPerRow;
+// Joins the parts of the units that were cut.  blockIdx.x: the CTA of the main kernel that the unit began in, if one did;
+// 16 lanes per query row, D / 16 channels per lane.  The lanes fetch the parts' (m, l) together, then four parts' sums
+// are on their way at a time.
+constexpr int kJoinRows = 16;                   // rows per CTA
+template <int D> __global__ void __launch_bounds__(16 * kJoinRows) tree_join_kernel(TreeAttnParams p) {
+  constexpr int kPer = D / 16, kAhead = 4;
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
-  const int64_t at = (int64_t)blockIdx.x * kRows + threadIdx.x / kPerRow;          // (unit, row of the block)
-  const int u = (int)(at / p.block_rows), rr = (int)(at % p.block_rows), c = 4 * (threadIdx.x % kPerRow);
-  if (u >= p.n_units) return;
-  const int total = p.plan[p.n_units], ctas = p.plan[p.n_units + 1], t0 = p.plan[u], t1 = p.plan[u + 1];
-  if (t1 == t0) return;                                                            // nothing of this unit is computed
-  const int c0 = tree_even_owner(t0, total, ctas), c1 = tree_even_owner(t1 - 1, total, ctas);
-  if (c0 == c1) return;                                                            // one CTA had all of it
-  int item = u;
-  const int r = item % p.row_blocks * p.block_rows + rr;
-  if (r >= p.g * p.N) return;
-  item /= p.row_blocks;
-  const int h = item % p.Hkv, b = item / p.Hkv % p.B, l = p.layer_begin + item / p.Hkv / p.B;
+  const int c0 = blockIdx.x, lane = threadIdx.x & 15, rr = blockIdx.y * kJoinRows + (threadIdx.x >> 4);
+  const int2 cut = p.plan[c0];                  // (unit, CTA that it ends in)
+  const int c1 = cut.y;
+  if (c1 < 0) return;
+  const int r = (int)((uint32_t)cut.x % (uint32_t)p.row_blocks) * p.block_rows + rr;
+  const bool live_row = rr < p.block_rows && r < p.g * p.N;
   // part of CTA x: the unit begins in c0 (its second slot) and goes on through the others (their first)
-  auto slot = [&](int x) { return ((int64_t)x * 2 + (x == c0 ? 1 : 0)) * p.block_rows + rr; };
-  if (p.part_ml[slot(c0)].y < 0.f) return;                                         // kNoPart
-  float mg = -INFINITY, ls = 0.f;
-  for (int x = c0; x <= c1; ++x) mg = fmaxf(mg, p.part_ml[slot(x)].x);
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int x = c0; x <= c1; ++x) {
-    const float2 ml = p.part_ml[slot(x)];
-    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - mg);
-    const float4 y = *reinterpret_cast<const float4*>(p.part_o + slot(x) * D + c);
-    o.x = fmaf(y.x, f, o.x); o.y = fmaf(y.y, f, o.y); o.z = fmaf(y.z, f, o.z); o.w = fmaf(y.w, f, o.w);
-    ls = fmaf(ml.y, f, ls);
+  auto slot = [&](int x) { return ((int64_t)x * 2 + (x == c0 ? 1 : 0)) * p.block_rows + (live_row ? rr : 0); };
+  float mg = -INFINITY, ls = 0.f, o[kPer];
+  bool none = !live_row;
+#pragma unroll
+  for (int c = 0; c < kPer; ++c) o[c] = 0.f;
+  for (int x0 = c0; x0 <= c1; x0 += 16) {
+    const int n = min(16, c1 - x0 + 1);
+    const float2 ml = lane < n ? p.part_ml[slot(x0 + lane)] : make_float2(-INFINITY, 0.f);
+    const float l_first = __shfl_sync(0xffffffffu, ml.y, 0, 16);
+    if (x0 == c0 && l_first < 0.f) none = true;                                    // kNoPart (then all parts are)
+    float m_new = ml.x;
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) m_new = fmaxf(m_new, __shfl_xor_sync(0xffffffffu, m_new, d));
+    m_new = fmaxf(mg, m_new);
+    const float m_eff = m_new == -INFINITY ? 0.f : m_new;                          // nothing visible so far: weights 0
+    const float old = exp2f(mg - m_eff), f = exp2f(ml.x - m_eff);
+    float l = ml.x == -INFINITY ? 0.f : ml.y * f;
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+    ls = ls * old + l;
+#pragma unroll
+    for (int c = 0; c < kPer; ++c) o[c] *= old;
+    mg = m_new;
+    for (int i0 = 0; i0 < n; i0 += kAhead) {
+      float4 y[kAhead][kPer / 4];
+      float w[kAhead];
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e) {
+        w[e] = __shfl_sync(0xffffffffu, f, (i0 + e) & 15, 16);
+        // (a part in which the row saw nothing holds no sums)
+        const float m_part = __shfl_sync(0xffffffffu, ml.x, (i0 + e) & 15, 16);
+        const bool live = !none && i0 + e < n && m_part != -INFINITY;
+        const float4* from = reinterpret_cast<const float4*>(p.part_o + slot(live ? x0 + i0 + e : c0) * D + kPer * lane);
+#pragma unroll
+        for (int c = 0; c < kPer / 4; ++c) y[e][c] = live ? from[c] : make_float4(0.f, 0.f, 0.f, 0.f);
+        if (!live) w[e] = 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e)
+#pragma unroll
+        for (int c = 0; c < kPer / 4; ++c) {
+          o[4 * c] = fmaf(y[e][c].x, w[e], o[4 * c]); o[4 * c + 1] = fmaf(y[e][c].y, w[e], o[4 * c + 1]);
+          o[4 * c + 2] = fmaf(y[e][c].z, w[e], o[4 * c + 2]); o[4 * c + 3] = fmaf(y[e][c].w, w[e], o[4 * c + 3]);
+        }
+    }
   }
+  if (none) return;
+  uint32_t item = (uint32_t)cut.x / (uint32_t)p.row_blocks;
+  const int h = item % (uint32_t)p.Hkv;
+  item /= (uint32_t)p.Hkv;
+  const int b = item % (uint32_t)p.B, l = p.layer_begin + (int)(item / (uint32_t)p.B);
   const float inv = ls == 0.f ? 0.f : 1.f / ls;
-  const int64_t row = (((int64_t)l * p.B + b) * p.Hq + (int64_t)h * p.g) * p.N + r;
-  tree_store_out4(p, row * D + c, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+  const int64_t to = ((((int64_t)l * p.B + b) * p.Hq + (int64_t)h * p.g) * p.N + r) * D + kPer * lane;
+#pragma unroll
+  for (int c = 0; c < kPer; c += 4) tree_store_out4(p, to + c, make_float4(o[c] * inv, o[c + 1] * inv, o[c + 2] * inv, o[c + 3] * inv));
 }
 
 template <int D, int MT> cudaError_t opt_in() {
@@ -827,10 +827,9 @@ int launch_tree_umma(const TreeAttnParams& p, cudaStream_t stream) {
   if (p.d == 64) NGC_CUDA_TRY(one ? (launch<64, 1>(maps, p, stream)) : (launch<64, 2>(maps, p, stream)));
   else NGC_CUDA_TRY(one ? (launch<128, 1>(maps, p, stream)) : (launch<128, 2>(maps, p, stream)));
   if (p.even) {
-    const int64_t threads = (int64_t)p.n_units * p.block_rows * (p.d / 4);
-    const dim3 grid((unsigned)((threads + 255) / 256));
-    NGC_CUDA_TRY(p.d == 64 ? launch_pdl(tree_join_kernel<64>, grid, dim3(256), 0, stream, p)
-                           : launch_pdl(tree_join_kernel<128>, grid, dim3(256), 0, stream, p));
+    const dim3 grid((unsigned)p.grid, (unsigned)((p.block_rows + kJoinRows - 1) / kJoinRows)), block(16 * kJoinRows);
+    NGC_CUDA_TRY(p.d == 64 ? launch_pdl(tree_join_kernel<64>, grid, block, 0, stream, p)
+                           : launch_pdl(tree_join_kernel<128>, grid, block, 0, stream, p));
   }
   return NGC_OK;
 }
