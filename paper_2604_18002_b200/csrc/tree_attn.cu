@@ -302,7 +302,7 @@ TreePlan tree_plan(const ngc_cache* c, int layers, int N) {
   TreePlan pl = {};
   pl.n_split = 1;
   if (c->dtype == NGC_BF16) {
-    const int tiles = tree_umma_tiles(rows), slots = tiles == 1 ? 2 * 148 : 148, keys = tree_umma_keys(tiles);
+    const int tiles = tree_umma_tiles(rows), slots = 148, keys = tree_umma_keys(tiles);
     pl.blocks = (rows + 128 * tiles - 1) / (128 * tiles);
     pl.block_rows = pl.blocks > 1 ? 128 * tiles : rows;
     const int64_t units = (int64_t)layers * c->B * c->Hkv * pl.blocks;

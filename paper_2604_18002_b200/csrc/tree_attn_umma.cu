@@ -26,8 +26,8 @@
 // end of the current one.
 //
 // Work is dealt out in one of two ways.  With many units (or short ones) a CTA takes one unit.  With few, the tiles of
-// all units form one line that is cut into equal pieces, a CTA per piece: rollouts of any lengths keep all SMs busy
-// to the end.  A CTA then owns at most two unfinished units, the one it begins in and the one it ends in; their
+// all units form one line (with a gap before each unit that stands for the cost of beginning it) that is cut into equal
+// pieces, a CTA per piece: rollouts of any lengths keep all SMs busy to the end.  A CTA then owns at most two unfinished units, the one it begins in and the one it ends in; their
 // sums go to its two slots of the workspace and a second kernel joins the parts of every unit that was cut.
 //
 // bf16 P: one rounding per weight (2^-8), as in the decode and replay calls; the row sum takes the weights
@@ -53,14 +53,15 @@ template <int D, int MT> struct Cfg {
   static constexpr int kKeys = tree_umma_keys(MT);         // keys per tile
   static constexpr int kBufs = MT == 1 ? 2 : 1;            // S buffers per M tile
   static constexpr int kHalves = kKeys / 64;               // P is handed over 64 keys at a time
-  static constexpr int kStages = D == 64 ? 4 : 2;          // of K and of V
-  static constexpr int kCtas = MT == 1 ? 2 : 1;
+  static constexpr int kStages = (MT == 1 ? 5 : 2) * (128 / D);      // of K and of V
   static constexpr int kThreads = (4 * MT + 3) * 32;
   static constexpr int kMmaWarp = 4 * MT, kProducerWarp = 4 * MT + 1;      // K and Q; V in the warp behind
   static constexpr int kBox = kKeys * 128;                 // a tile's 64 channels
   static constexpr int kTile = kKeys * D * 2;              // K or V tile
   static constexpr int kQBytes = 128 * D * 2;              // Q of an M tile
   static constexpr int kSmem = MT * kQBytes + 2 * kStages * kTile + 1024;
+  // What beginning another unit costs a CTA, in tiles: the row sums leave, Q changes.
+  static constexpr int kUnitCost = MT == 1 ? 3 : 4;
   static constexpr uint32_t kOCol = 128 * MT;              // S[m][buf] at 128 m + 64 buf, O[m] behind
   static constexpr uint32_t kCols = MT == 1 ? 256 : 512;
 };
@@ -81,58 +82,80 @@ template <int D, int MT> struct Shared {
   int refused[MT][4];
   uint32_t tmem;
   int abort;
+  uint8_t parent[MT][4][kTreeMaxNodes];         // by piece & 3: links of the tree (node 0 and bad links: the node itself)
   int warp_sum[C::kThreads / 32];
-  int base[kTreeMaxUnits + 1];                  // tiles before every unit (even split)
+  // even split, by unit: where it begins on the line, its length and node count (loaded once: while every SM streams K and
+  // V a load from global memory takes microseconds)
+  int base[kTreeMaxUnits + 1], len[kTreeMaxUnits];
+  uint8_t n[kTreeMaxUnits];
 };
 
 // What every role needs to know about the piece of a unit that is being worked on.
 struct Piece {
   int b, h, l, lr, rb, n, len, lo, n_tiles, n_ct;      // tiles [lo, lo + n_tiles) of the unit; the first n_ct are the cache's
   int plane, strip;                                    // of the cache; of the tree's K and V
-  int64_t base;                                        // row of a plane at which the sequence (or its pages) begins
-  bool fits, first, last;                              // holds the unit's first / last tile
+  bool first, last;                                    // holds the unit's first / last tile
 };
-// This CTA's share: from tile `lo` of unit `u` on, n_left tiles in all; `seq` pieces so far.
-struct Walk { int u, lo, n_left, seq; };
+// This CTA's share of the line: from place `at` of unit `u` on, n_left places in all; `seq` pieces so far.  A unit's
+// first kUnitCost places hold no tile.
+struct Walk { int u, at, n_left, seq; };
 
-// Decodes unit u.  All of its numbers are loaded at once; `fits` = node count and length can be worked with (links are checked
-// later); returns its key tiles, 0 for a unit that has nothing to do or does not fit.
-template <int KT> __device__ __forceinline__ int unit_of(const TreeAttnParams& p, uint32_t u, Piece& w) {
+// Decodes unit u.
+__device__ __forceinline__ void unit_of(const TreeAttnParams& p, uint32_t u, Piece& w) {
   if (p.row_blocks > 1) { w.rb = u % (uint32_t)p.row_blocks; u /= (uint32_t)p.row_blocks; } else { w.rb = 0; }
   w.h = u % (uint32_t)p.Hkv; u /= (uint32_t)p.Hkv;
   w.lr = p.n_layers > 1 ? u / (uint32_t)p.B : 0;
   w.b = u - w.lr * p.B;
   w.l = p.layer_begin + w.lr;
-  const int n = p.n_nodes ? p.n_nodes[w.b] : p.N;
-  const int len = p.lens[p.lens_lists ? len_index(p.lens_lists, p.L, p.Hkv, w.b, w.l, w.h) : w.b];
-  w.base = p.page_table ? (int64_t)w.b * p.pages_cap * p.page : p.seq_off[w.b];
-  const int64_t cap = p.page_table ? (int64_t)p.pages_cap * p.page : p.seq_off[w.b + 1] - w.base;
-  w.n = n;
-  w.len = len;
   w.plane = w.l * p.Hkv + w.h;
   w.strip = (w.l * p.B + w.b) * p.Hkv + w.h;
-  w.fits = (n >= 0) & (n <= p.N) & (len >= 0) & (len <= cap);
-  return w.fits && n > 0 ? (int)((uint32_t)(len + KT - 1) / KT + (uint32_t)(n + KT - 1) / KT) : 0;
+}
+// Its node count and length, loaded at once.  False if they cannot be worked with (links are checked later).
+__device__ __forceinline__ bool load_counts(const TreeAttnParams& p, Piece& w) {
+  const int n = p.n_nodes ? p.n_nodes[w.b] : p.N;
+  const int len = p.lens[p.lens_lists ? len_index(p.lens_lists, p.L, p.Hkv, w.b, w.l, w.h) : w.b];
+  const int64_t cap = p.page_table ? (int64_t)p.pages_cap * p.page : p.seq_off[w.b + 1] - p.seq_off[w.b];
+  w.n = n;
+  w.len = len;
+  return (n >= 0) & (n <= p.N) & (len >= 0) & (len <= cap);
+}
+// Key tiles of a unit with these counts.
+template <int KT> __device__ __forceinline__ int unit_tiles(int n, int len) {
+  return n > 0 ? (int)((uint32_t)(len + KT - 1) / KT + (uint32_t)(n + KT - 1) / KT) : 0;
 }
 
 // The next piece of the walk; false at its end.  (A unit per CTA: also a unit without tiles.)
-template <int KT> __device__ __forceinline__ bool next_piece(const TreeAttnParams& p, Walk& k, Piece& w) {
-  if (k.n_left <= 0) return false;
-  int nt;
-  for (;; ++k.u, k.lo = 0) {
-    nt = unit_of<KT>(p, (uint32_t)k.u, w);
-    if (nt > 0 || !p.even) break;
+template <int KT, int kUnitCost, typename Sh> __device__ __forceinline__ bool next_piece(const TreeAttnParams& p, const Sh& sh, Walk& k, Piece& w) {
+  while (k.n_left > 0) {
+    unit_of(p, (uint32_t)k.u, w);
+    int nt;
+    if (!p.even) {
+      const bool fits = load_counts(p, w);
+      nt = fits ? unit_tiles<KT>(w.n, w.len) : 0;
+      if (!fits && threadIdx.x == 0) set_dev_status(p.dev_status, w.n < 0 || w.n > p.N ? NGC_DEV_BAD_TREE : NGC_DEV_BAD_COUNTS);
+      w.lo = 0;
+      w.n_tiles = nt;
+      k.n_left = 0;
+    } else {
+      w.n = sh.n[k.u];
+      w.len = sh.len[k.u];
+      nt = unit_tiles<KT>(w.n, w.len);
+      const int places = nt > 0 ? min(nt + kUnitCost - k.at, k.n_left) : 0;
+      w.lo = max(0, k.at - kUnitCost);
+      w.n_tiles = max(0, k.at + places - kUnitCost) - w.lo;
+      k.n_left -= places;
+    }
+    ++k.u;
+    k.at = 0;
+    if (w.n_tiles > 0 || !p.even) {
+      w.n_ct = (int)((uint32_t)(w.len + KT - 1) / KT);
+      w.first = w.lo == 0;
+      w.last = w.lo + w.n_tiles == nt;
+      ++k.seq;
+      return true;
+    }
   }
-  w.lo = k.lo;
-  w.n_tiles = min(nt - k.lo, k.n_left);
-  w.n_ct = (w.len + KT - 1) / KT;
-  w.first = w.lo == 0;
-  w.last = w.lo + w.n_tiles == nt;
-  k.n_left = p.even ? k.n_left - w.n_tiles : 0;
-  ++k.u;
-  k.lo = 0;
-  ++k.seq;
-  return true;
+  return false;
 }
 
 // Page-table entries in order, 32 at a time in the lanes of a producer warp, the next batch on its way.  An entry that is
@@ -223,12 +246,20 @@ __device__ __forceinline__ void store_sector(float* p, const uint32_t* r) {
                : "memory");
 }
 
+// 32 channels of an output row from element idx on, scaled.
+__device__ __forceinline__ void tree_store_row32(const TreeAttnParams& p, int64_t idx, const uint32_t* o, float inv) {
+#pragma unroll
+  for (int c = 0; c < 32; c += 4)
+    tree_store_out4(p, idx + c, make_float4(__uint_as_float(o[c]) * inv, __uint_as_float(o[c + 1]) * inv,
+                                            __uint_as_float(o[c + 2]) * inv, __uint_as_float(o[c + 3]) * inv));
+}
+
 __device__ __forceinline__ uint32_t odd_half(uint32_t x) { return (x & 0x7f80u) == 0x7f80u ? 0xffffu : 0u; }
 // Bits of x (two bf16) that belong to infinities or NaN.
 __device__ __forceinline__ uint32_t odd_bits(uint32_t x) { return odd_half(x) | odd_half(x >> 16) << 16; }
 
 template <int D, int MT>
-__global__ void __launch_bounds__(Cfg<D, MT>::kThreads, Cfg<D, MT>::kCtas)
+__global__ void __launch_bounds__(Cfg<D, MT>::kThreads, 1)
 tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
   using C = Cfg<D, MT>;
   constexpr int ST = C::kStages, NT = C::kThreads, KT = C::kKeys, NB = C::kBufs, NH = C::kHalves;
@@ -286,11 +317,15 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     int sum = 0;
     for (int i = u0; i < u1; ++i) {
       Piece w;
-      const int t = unit_of<KT>(p, (uint32_t)i, w);
+      unit_of(p, (uint32_t)i, w);
+      const bool fits = load_counts(p, w);
+      sh.len[i] = w.len;
+      sh.n[i] = (uint8_t)(fits ? w.n : 0);      // counts that cannot be worked with: no tiles
+      int t = fits ? unit_tiles<KT>(w.n, w.len) : 0;
+      if (t > 0) t += C::kUnitCost;
       sh.base[i] = t;
       sum += t;
-      // counts that cannot be worked with have no tiles: reported here, by the first CTA
-      if (blockIdx.x == 0 && !w.fits) set_dev_status(p.dev_status, w.n < 0 || w.n > p.N ? NGC_DEV_BAD_TREE : NGC_DEV_BAD_COUNTS);
+      if (blockIdx.x == 0 && !fits) set_dev_status(p.dev_status, w.n < 0 || w.n > p.N ? NGC_DEV_BAD_TREE : NGC_DEV_BAD_COUNTS);
     }
     int incl = sum;
 #pragma unroll
@@ -313,20 +348,21 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     const TreeEven even(total, ctas);
     const int g0 = even.first(blockIdx.x), g1 = even.first(blockIdx.x + 1);
     walk.n_left = (int)blockIdx.x < ctas ? g1 - g0 : 0;
-    // the unit that tile g0 belongs to
+    // the unit that place g0 belongs to
     int lo = 0, hi = p.n_units;
     while (walk.n_left > 0 && hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (sh.base[mid] <= g0) lo = mid; else hi = mid;
     }
     walk.u = lo;
-    walk.lo = g0 - sh.base[lo];
+    walk.at = g0 - sh.base[lo];
     // for the kernel that joins the parts: the unit that begins here and goes on elsewhere (at most the last one), and
     // the CTA that it ends in
     if (tid == 0) {
       int last = lo, end = -1;
       while (walk.n_left > 0 && sh.base[last + 1] < g1) ++last;
-      if (walk.n_left > 0 && sh.base[last] >= g0 && sh.base[last + 1] > g1) end = even.owner(sh.base[last + 1] - 1);
+      const int tile0 = sh.base[last] + C::kUnitCost;
+      if (walk.n_left > 0 && tile0 >= g0 && tile0 < g1 && sh.base[last + 1] > g1) end = even.owner(sh.base[last + 1] - 1);
       p.plan[blockIdx.x] = make_int2(last, end);
     }
   }
@@ -344,14 +380,21 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     const KvMaps& map = is_v ? maps.v : maps.k;
     int n_q = 0;
     bool ok = true;
-    while (ok && next_piece<KT>(p, walk, w)) {
+    while (ok && next_piece<KT, C::kUnitCost>(p, sh, walk, w)) {
       if (w.n_tiles <= 0) continue;
-      const int base = (int)w.base;
+      const int base = (int)(p.page_table ? (int64_t)w.b * p.pages_cap * p.page : p.seq_off[w.b]);
       PageWalk pages;
       if (p.page_table)
         pages.start(p.page_table + ((int64_t)w.b * p.G + list_of(p.lists, w.l, w.h, p.Hkv)) * p.pages_cap, p.pages_cap,
                     (w.len + p.page - 1) / p.page, min(w.lo * KT, w.len) / p.page, p.dev_status);
-      if (!is_v) {
+      for (int i = 0; ok && i < w.n_tiles; ++i) {
+        const int s = kv % ST;
+        ok = kv < ST || umma::warp_wait(&empty[s], (kv / ST - 1) & 1, &sh.abort, p.dev_status);
+        if (!ok) break;
+        load_tile<D, KT>(p, map, pages, w, base, w.lo + i, ring + s * C::kTile, &full[s]);
+        ++kv;
+        if (is_v || i > 0) continue;
+        // Q behind the first K tile: its buffer is free once the last S of the piece before is done, the ring earlier
         const int r0 = w.rb * MT * 128, tiles_m = min(MT, (rows - r0 + 127) >> 7);
         const int64_t row0 = (((int64_t)w.l * p.B + w.b) * p.Hq + (int64_t)w.h * p.g) * p.N;
         ok = n_q == 0 || umma::warp_wait(&sh.q_empty, (n_q - 1) & 1, &sh.abort, p.dev_status);
@@ -366,13 +409,6 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
         }
         __syncwarp();
         ++n_q;
-      }
-      for (int i = 0; ok && i < w.n_tiles; ++i) {
-        const int s = kv % ST;
-        ok = kv < ST || umma::warp_wait(&empty[s], (kv / ST - 1) & 1, &sh.abort, p.dev_status);
-        if (!ok) break;
-        load_tile<D, KT>(p, map, pages, w, base, w.lo + i, ring + s * C::kTile, &full[s]);
-        ++kv;
       }
     }
     if (!ok) {                                  // giving up: no copy may be in flight when the CTA ends
@@ -389,7 +425,7 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
 #pragma unroll
     for (int m = 0; m < MT; ++m) done[m] = 0;
     bool ok = true;
-    while (ok && next_piece<KT>(p, walk, w)) {
+    while (ok && next_piece<KT, C::kUnitCost>(p, sh, walk, w)) {
       if (w.n_tiles <= 0) continue;
       const int tiles_m = min(MT, (rows - w.rb * MT * 128 + 127) >> 7);          // M tiles that have a row
       auto steps_of = [&](int i) {              // 16-key steps of tile i that hold a live key
@@ -467,14 +503,14 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     const uint32_t lane_base = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t o_addr = tmem + lane_base + C::kOCol + (uint32_t)(D * m);
     int tc = 0, pieces = 0, fixes[3] = {0, 0, 0};      // tiles and pieces of this M tile so far; uses of sh.fixed
-    bool ok = true;
-    while (ok && next_piece<KT>(p, walk, w)) {
-      if (w.n_tiles <= 0) {
-        if (tid == 0 && !w.fits)
-          set_dev_status(p.dev_status, w.n < 0 || w.n > p.N ? NGC_DEV_BAD_TREE : NGC_DEV_BAD_COUNTS);
-        continue;
-      }
-      const int r0 = w.rb * MT * 128, slot = walk.seq & 3;
+    bool ok = true, more = next_piece<KT, C::kUnitCost>(p, sh, walk, w);
+    // this thread's node's link in the piece's tree: fetched a piece ahead, like the piece itself
+    auto fetch_link = [&](const Piece& x) { return more && x.n_tiles > 0 && in_group < x.n ? p.parent[(int64_t)x.b * p.N + in_group] : 0; };
+    int link = fetch_link(w), next_link = 0;
+    while (ok && more) {
+      if (w.n_tiles <= 0) break;                // (a unit per CTA that has none)
+      const int r0 = w.rb * MT * 128, seq = walk.seq, slot = seq & 3;
+      Piece next;                               // found out while the last product runs
       const bool in_tail = w.len % KT != 0 && w.lo < w.n_ct && w.lo + w.n_tiles >= w.n_ct;
       const bool in_tree0 = w.lo <= w.n_ct && w.lo + w.n_tiles > w.n_ct, in_tree1 = w.lo <= w.n_ct + 1 && w.lo + w.n_tiles > w.n_ct + 1;
       if (r0 + 128 * m < rows) {
@@ -482,23 +518,22 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
         const int node = r % p.N;
         const bool live_row = r < rows && node < w.n;
         const bool live_warp = r0 + 128 * m + 32 * (warp & 3) < rows;
-        // links: a node per thread is checked, and the row's own are followed
-        const int32_t* parent = p.parent + (int64_t)w.b * p.N;
+        // links: a node per thread is checked and laid out, then the row's own are followed
         if (in_group < w.n) {
-          const int pa = parent[in_group];
-          if (in_group == 0 ? pa != -1 : (pa < 0 || pa >= in_group)) sh.refused[m][slot] = walk.seq;
+          const bool wrong = in_group == 0 ? link != -1 : (link < 0 || link >= in_group);
+          if (wrong) sh.refused[m][slot] = seq;
+          sh.parent[m][slot][in_group] = (uint8_t)(wrong || in_group == 0 ? in_group : link);
         }
         if (m == 0 && in_group < kTreeWords) sh.odd[slot][in_group] = 0;
         ptx::mbar_arrive(&sh.checked[m]);
+        ok = umma::warp_wait(&sh.checked[m], pieces & 1, &sh.abort, p.dev_status);
         uint32_t aw[kTreeWords] = {0u, 0u, 0u, 0u};
-        for (int j = live_row && w.lo + w.n_tiles > w.n_ct ? node : -1; j >= 0;) {
+        for (int j = ok && live_row && w.lo + w.n_tiles > w.n_ct ? node : -1; j >= 0;) {
 #pragma unroll
           for (int x = 0; x < kTreeWords; ++x) aw[x] |= (j >> 5) == x ? 1u << (j & 31) : 0u;
-          const int pa = parent[j];
-          j = pa < j ? pa : -1;
+          const int up = sh.parent[m][slot][j];
+          j = up < j ? up : -1;
         }
-        if (m == 0 && (in_tree0 || in_tree1))    // the words above are zero before a tile's nodes are searched
-          ok = umma::warp_wait(&sh.checked[m], pieces & 1, &sh.abort, p.dev_status);
         float m_use = -INFINITY, l_run = 0.f;
         for (int i = 0; ok && i < w.n_tiles; ++i) {
           const int t = w.lo + i, buf = (tc + i) % NB;
@@ -632,6 +667,8 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
           l_run += s0 + s1;
         }
         // ---- the row's sums leave
+        if (ok) more = next_piece<KT, C::kUnitCost>(p, sh, walk, next);
+        next_link = fetch_link(next);
         const int last = tc + w.n_tiles - 1;
         ok = ok && umma::warp_wait(&sh.o_done[m][last % NB], (last / NB) & 1, &sh.abort, p.dev_status) &&
              umma::warp_wait(&sh.checked[m], pieces & 1, &sh.abort, p.dev_status) &&
@@ -639,7 +676,7 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
              (!in_tree1 || umma::warp_wait(&sh.fixed[2], fixes[2] & 1, &sh.abort, p.dev_status));
         if (!ok) break;
         umma::fence_after_sync();
-        const bool whole = w.first && w.last, refused = sh.refused[m][slot] == walk.seq;
+        const bool whole = w.first && w.last, refused = sh.refused[m][slot] == seq;
         const int64_t pit = ((int64_t)blockIdx.x * 2 + (w.first ? 1 : 0)) * p.block_rows + (r - r0);     // in this CTA's slots
         if (refused && in_group == 0) set_dev_status(p.dev_status, NGC_DEV_BAD_TREE);
         if (!whole && r < rows) p.part_ml[pit] = live_row && !refused ? make_float2(m_use, l_run) : kNoPart;
@@ -672,31 +709,24 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
             } else if (!whole) {
 #pragma unroll
               for (int c = 0; c < 32; c += 8) store_sector(p.part_o + pit * D + c0 + c, o + c);
-            } else if (p.out_bf16) {
-#pragma unroll
-              for (int c = 0; c < 32; c += 8)
-                *reinterpret_cast<uint4*>((__nv_bfloat16*)p.out + out_row * D + c0 + c) =
-                    make_uint4(ptx::pack_bf16x2(__uint_as_float(o[c]) * inv, __uint_as_float(o[c + 1]) * inv),
-                               ptx::pack_bf16x2(__uint_as_float(o[c + 2]) * inv, __uint_as_float(o[c + 3]) * inv),
-                               ptx::pack_bf16x2(__uint_as_float(o[c + 4]) * inv, __uint_as_float(o[c + 5]) * inv),
-                               ptx::pack_bf16x2(__uint_as_float(o[c + 6]) * inv, __uint_as_float(o[c + 7]) * inv));
             } else {
-#pragma unroll
-              for (int c = 0; c < 32; c += 4)
-                *reinterpret_cast<float4*>((float*)p.out + out_row * D + c0 + c) =
-                    make_float4(__uint_as_float(o[c]) * inv, __uint_as_float(o[c + 1]) * inv,
-                                __uint_as_float(o[c + 2]) * inv, __uint_as_float(o[c + 3]) * inv);
+              tree_store_row32(p, out_row * D + c0, o, inv);
             }
           }
         }
         umma::fence_before_sync();              // O may be overwritten once the next P of this thread is out
         tc += w.n_tiles;
         ++pieces;
+      } else {
+        more = next_piece<KT, C::kUnitCost>(p, sh, walk, next);
+        next_link = fetch_link(next);
       }
       kv += w.n_tiles;
       fixes[0] += in_tail;
       fixes[1] += in_tree0;
       fixes[2] += in_tree1;
+      w = next;
+      link = next_link;
     }
   }
   __syncthreads();
