@@ -17,9 +17,9 @@
 //                    cache and the tree tiles come in 16-row boxes.  Page-table entries are fetched 32 at a time, a
 //                    batch ahead;
 //   MMA warp         S = Q K^T into tensor memory, O += P V with P read from tensor memory;
-//   softmax warps    (4 MT) one thread per row: follows its node's links to the root for its mask (needed only in tree
-//                    tiles; the cache's last tile has a common one), online softmax in the log2 domain, P as bf16 over
-//                    the S it came from, 64 keys at a time.  The maximum used only moves when the true one has grown by
+//   mask warp        the ancestor sets of the next unit's tree, by pointer doubling;
+//   softmax warps    (4 MT) one thread per row: mask (in tree tiles, its node's ancestors; in the cache's last tile a common
+//                    one), online softmax in the log2 domain, P as bf16 over the S it came from, 64 keys at a time.  The maximum used only moves when the true one has grown by
 //                    more than a factor 2^8, so O in tensor memory is rarely rescaled.
 //
 // The roles only meet at mbarriers, also from one unit to the next: loads and scores of the next unit run under the
@@ -54,14 +54,14 @@ template <int D, int MT> struct Cfg {
   static constexpr int kBufs = MT == 1 ? 2 : 1;            // S buffers per M tile
   static constexpr int kHalves = kKeys / 64;               // P is handed over 64 keys at a time
   static constexpr int kStages = (MT == 1 ? 5 : 2) * (128 / D);      // of K and of V
-  static constexpr int kThreads = (4 * MT + 3) * 32;
-  static constexpr int kMmaWarp = 4 * MT, kProducerWarp = 4 * MT + 1;      // K and Q; V in the warp behind
+  static constexpr int kThreads = (4 * MT + 4) * 32;
+  static constexpr int kMmaWarp = 4 * MT, kMaskWarp = 4 * MT + 1, kProducerWarp = 4 * MT + 2;      // K and Q; V in the warp behind
   static constexpr int kBox = kKeys * 128;                 // a tile's 64 channels
   static constexpr int kTile = kKeys * D * 2;              // K or V tile
   static constexpr int kQBytes = 128 * D * 2;              // Q of an M tile
   static constexpr int kSmem = MT * kQBytes + 2 * kStages * kTile + 1024;
   // What beginning another unit costs a CTA, in tiles: the row sums leave, Q changes.
-  static constexpr int kUnitCost = MT == 1 ? 3 : 4;
+  static constexpr int kUnitCost = MT == 1 ? 4 : 5;
   static constexpr uint32_t kOCol = 128 * MT;              // S[m][buf] at 128 m + 64 buf, O[m] behind
   static constexpr uint32_t kCols = MT == 1 ? 256 : 512;
 };
@@ -75,14 +75,13 @@ template <int D, int MT> struct Shared {
   using C = Cfg<D, MT>;
   uint64_t k_full[C::kStages], k_empty[C::kStages], v_full[C::kStages], v_empty[C::kStages];
   uint64_t s_full[MT][C::kBufs], p_full[MT][C::kBufs][C::kHalves], o_done[MT][C::kBufs];
-  uint64_t q_full, q_empty, checked[MT], fixed[3], drain;
-  // by piece & 3 (no role is more than two pieces ahead of another): nodes whose V row holds an infinity or a NaN, and
-  // piece + 1 if the tree's links are no links
-  uint32_t odd[4][kTreeWords];
-  int refused[MT][4];
+  uint64_t q_full, q_empty, masks_full[2], masks_empty[2], fixed[3], drain;
+  // by piece & 1: ancestor-or-self sets of the nodes, and whether the links are none
+  alignas(16) uint32_t anc[2][kTreeMaxNodes][kTreeWords];
+  int refused[2], jump[kTreeMaxNodes];
+  uint32_t odd[4][kTreeWords];                  // by piece & 3: nodes whose V row holds an infinity or a NaN
   uint32_t tmem;
   int abort;
-  uint8_t parent[MT][4][kTreeMaxNodes];         // by piece & 3: links of the tree (node 0 and bad links: the node itself)
   int warp_sum[C::kThreads / 32];
   // even split, by unit: where it begins on the line, its length and node count (loaded once: while every SM streams K and
   // V a load from global memory takes microseconds)
@@ -289,11 +288,7 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     ptx::mbar_init(&sh.q_full, 1);
     ptx::mbar_init(&sh.q_empty, 1);
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      ptx::mbar_init(&sh.checked[m], 128);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sh.refused[m][i] = 0;
-    }
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(&sh.masks_full[i], 32); ptx::mbar_init(&sh.masks_empty[i], 128 * MT); }
 #pragma unroll
     for (int i = 0; i < 3; ++i) ptx::mbar_init(&sh.fixed[i], 128);
     ptx::mbar_init(&sh.drain, 1);
@@ -415,6 +410,53 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
       if (!is_v && n_q > 0) ptx::mbar_wait_bounded(&sh.q_full, (n_q - 1) & 1);
       for (int j = max(0, kv - ST); j < kv; ++j) ptx::mbar_wait_bounded(&full[j % ST], (j / ST) & 1);
     }
+  } else if (warp == C::kMaskWarp) {
+    // ------------------------------------------------------------------ ancestor sets, four nodes per lane
+    while (next_piece<KT, C::kUnitCost>(p, sh, walk, w) && w.n_tiles > 0) {
+      const int slot = walk.seq & 1, use = (walk.seq - 1) >> 1;
+      int link[kTreeWords];
+#pragma unroll
+      for (int x = 0; x < kTreeWords; ++x) link[x] = lane + 32 * x < w.n ? p.parent[(int64_t)w.b * p.N + lane + 32 * x] : -1;
+      // (all softmax threads have taken the sets of two pieces ago, hence left the piece before that one)
+      if (use > 0 && !umma::warp_wait(&sh.masks_empty[slot], (use - 1) & 1, &sh.abort, p.dev_status)) break;
+      bool wrong = false;
+#pragma unroll
+      for (int x = 0; x < kTreeWords; ++x) {
+        const int i = lane + 32 * x;
+        const bool bad = i < w.n && (i == 0 ? link[x] != -1 : (link[x] < 0 || link[x] >= i));
+        wrong = wrong || bad;
+        sh.jump[i] = bad ? -1 : link[x];
+#pragma unroll
+        for (int y = 0; y < kTreeWords; ++y) sh.anc[slot][i][y] = y == x ? 1u << lane : 0u;
+      }
+      wrong = __any_sync(0xffffffffu, wrong);
+      if (lane == 0) sh.refused[slot] = wrong;
+      if (lane < kTreeWords) sh.odd[walk.seq & 3][lane] = 0;
+      // in every round a node takes over the set of the node that its jump points at and jumps as far again
+      for (bool more = true; more;) {
+        more = false;
+        uint4 got[kTreeWords];
+        int far[kTreeWords];
+        __syncwarp();
+#pragma unroll
+        for (int x = 0; x < kTreeWords; ++x) {
+          const int j = sh.jump[lane + 32 * x];
+          far[x] = j >= 0 ? sh.jump[j] : -1;
+          got[x] = j >= 0 ? *reinterpret_cast<const uint4*>(sh.anc[slot][j]) : make_uint4(0, 0, 0, 0);
+          more = more || j >= 0;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int x = 0; x < kTreeWords; ++x) {
+          uint4* at = reinterpret_cast<uint4*>(sh.anc[slot][lane + 32 * x]);
+          const uint4 own = *at;
+          sh.jump[lane + 32 * x] = far[x];
+          *at = make_uint4(own.x | got[x].x, own.y | got[x].y, own.z | got[x].z, own.w | got[x].w);
+        }
+        more = __any_sync(0xffffffffu, more);
+      }
+      ptx::mbar_arrive(&sh.masks_full[slot]);
+    }
   } else if (warp == C::kMmaWarp) {
     // ------------------------------------------------------------------ MMA issue, one elected lane
     // operand descriptors differ only in their low word (start address / 16)
@@ -499,41 +541,27 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     }
   } else {
     // ------------------------------------------------------------------ softmax: one thread per query row
-    const int m = warp >> 2, in_group = tid & 127;
+    const int m = warp >> 2;
     const uint32_t lane_base = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t o_addr = tmem + lane_base + C::kOCol + (uint32_t)(D * m);
-    int tc = 0, pieces = 0, fixes[3] = {0, 0, 0};      // tiles and pieces of this M tile so far; uses of sh.fixed
+    int tc = 0, fixes[3] = {0, 0, 0};           // tiles of this M tile so far; uses of sh.fixed
     bool ok = true, more = next_piece<KT, C::kUnitCost>(p, sh, walk, w);
-    // this thread's node's link in the piece's tree: fetched a piece ahead, like the piece itself
-    auto fetch_link = [&](const Piece& x) { return more && x.n_tiles > 0 && in_group < x.n ? p.parent[(int64_t)x.b * p.N + in_group] : 0; };
-    int link = fetch_link(w), next_link = 0;
     while (ok && more) {
       if (w.n_tiles <= 0) break;                // (a unit per CTA that has none)
       const int r0 = w.rb * MT * 128, seq = walk.seq, slot = seq & 3;
       Piece next;                               // found out while the last product runs
+      const int r = r0 + 128 * m + 32 * (warp & 3) + lane;
+      const int node = (int)((uint32_t)r % (uint32_t)p.N);
+      const bool live_row = r < rows && node < w.n;
+      ok = umma::warp_wait(&sh.masks_full[seq & 1], ((seq - 1) >> 1) & 1, &sh.abort, p.dev_status);
+      const uint4 set = live_row ? *reinterpret_cast<const uint4*>(sh.anc[seq & 1][node]) : make_uint4(0, 0, 0, 0);
+      const uint32_t aw[kTreeWords] = {set.x, set.y, set.z, set.w};
+      const bool refused = sh.refused[seq & 1] != 0;
+      ptx::mbar_arrive(&sh.masks_empty[seq & 1]);
       const bool in_tail = w.len % KT != 0 && w.lo < w.n_ct && w.lo + w.n_tiles >= w.n_ct;
       const bool in_tree0 = w.lo <= w.n_ct && w.lo + w.n_tiles > w.n_ct, in_tree1 = w.lo <= w.n_ct + 1 && w.lo + w.n_tiles > w.n_ct + 1;
       if (r0 + 128 * m < rows) {
-        const int r = r0 + 128 * m + 32 * (warp & 3) + lane;
-        const int node = r % p.N;
-        const bool live_row = r < rows && node < w.n;
         const bool live_warp = r0 + 128 * m + 32 * (warp & 3) < rows;
-        // links: a node per thread is checked and laid out, then the row's own are followed
-        if (in_group < w.n) {
-          const bool wrong = in_group == 0 ? link != -1 : (link < 0 || link >= in_group);
-          if (wrong) sh.refused[m][slot] = seq;
-          sh.parent[m][slot][in_group] = (uint8_t)(wrong || in_group == 0 ? in_group : link);
-        }
-        if (m == 0 && in_group < kTreeWords) sh.odd[slot][in_group] = 0;
-        ptx::mbar_arrive(&sh.checked[m]);
-        ok = umma::warp_wait(&sh.checked[m], pieces & 1, &sh.abort, p.dev_status);
-        uint32_t aw[kTreeWords] = {0u, 0u, 0u, 0u};
-        for (int j = ok && live_row && w.lo + w.n_tiles > w.n_ct ? node : -1; j >= 0;) {
-#pragma unroll
-          for (int x = 0; x < kTreeWords; ++x) aw[x] |= (j >> 5) == x ? 1u << (j & 31) : 0u;
-          const int up = sh.parent[m][slot][j];
-          j = up < j ? up : -1;
-        }
         float m_use = -INFINITY, l_run = 0.f;
         for (int i = 0; ok && i < w.n_tiles; ++i) {
           const int t = w.lo + i, buf = (tc + i) % NB;
@@ -668,17 +696,15 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
         }
         // ---- the row's sums leave
         if (ok) more = next_piece<KT, C::kUnitCost>(p, sh, walk, next);
-        next_link = fetch_link(next);
         const int last = tc + w.n_tiles - 1;
         ok = ok && umma::warp_wait(&sh.o_done[m][last % NB], (last / NB) & 1, &sh.abort, p.dev_status) &&
-             umma::warp_wait(&sh.checked[m], pieces & 1, &sh.abort, p.dev_status) &&
              (!in_tree0 || umma::warp_wait(&sh.fixed[1], fixes[1] & 1, &sh.abort, p.dev_status)) &&
              (!in_tree1 || umma::warp_wait(&sh.fixed[2], fixes[2] & 1, &sh.abort, p.dev_status));
         if (!ok) break;
         umma::fence_after_sync();
-        const bool whole = w.first && w.last, refused = sh.refused[m][slot] == seq;
+        const bool whole = w.first && w.last;
         const int64_t pit = ((int64_t)blockIdx.x * 2 + (w.first ? 1 : 0)) * p.block_rows + (r - r0);     // in this CTA's slots
-        if (refused && in_group == 0) set_dev_status(p.dev_status, NGC_DEV_BAD_TREE);
+        if (refused && tid == 0) set_dev_status(p.dev_status, NGC_DEV_BAD_TREE);
         if (!whole && r < rows) p.part_ml[pit] = live_row && !refused ? make_float2(m_use, l_run) : kNoPart;
         if (live_warp && !refused) {
           uint32_t odd[kTreeWords];
@@ -716,17 +742,14 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
         }
         umma::fence_before_sync();              // O may be overwritten once the next P of this thread is out
         tc += w.n_tiles;
-        ++pieces;
       } else {
         more = next_piece<KT, C::kUnitCost>(p, sh, walk, next);
-        next_link = fetch_link(next);
       }
       kv += w.n_tiles;
       fixes[0] += in_tail;
       fixes[1] += in_tree0;
       fixes[2] += in_tree1;
       w = next;
-      link = next_link;
     }
   }
   __syncthreads();
