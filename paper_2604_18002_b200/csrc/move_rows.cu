@@ -60,7 +60,7 @@ __device__ __forceinline__ int list_len(const MoveParams& p, int b, int gi, int 
 // A cluster of CTAs per sequence.  All of them check the path and the room (every list, since a sequence is committed
 // whole or not at all), copy their share of the rows, and meet at a cluster barrier: behind it nobody reads the lengths
 // any more and the first CTA writes the new ones.  One launch: for a single rollout the call is all latency.
-constexpr int kMoveVecs = 4;                    // 16-byte vectors a thread has in flight
+constexpr int kMoveVecs = 2;                    // vectors of K, and of V, a thread has in flight
 __global__ void __launch_bounds__(kMoveThreads) commit_kernel(MoveParams p) {
   const cg::cluster_group cluster = cg::this_cluster();
   __shared__ int s_path[NGC_TREE_MAX_NODES];
@@ -99,24 +99,23 @@ __global__ void __launch_bounds__(kMoveThreads) commit_kernel(MoveParams p) {
     if (tid == 0) set_dev_status(p.dev_status, status);
     n = 0;
   }
-  // vectors of the sequence: (plane, row of the path, piece), K and V of each
-  const int per_plane = n * p.row_vecs;
-  const int64_t total = (int64_t)p.L * p.Hkv * per_plane;
-  for (int64_t i0 = (int64_t)rank * kMoveThreads + tid; i0 < total; i0 += (int64_t)ctas * kMoveThreads * kMoveVecs) {
+  // rows of the sequence: (plane, row of the path), K and V of each; a thread per 16-byte piece
+  const uint32_t piece = tid & (p.row_vecs - 1), per_round = kMoveThreads / p.row_vecs;        // (row_vecs: 8, 16 or 32)
+  const uint32_t total = (uint32_t)(p.L * p.Hkv) * n;
+  for (uint32_t i0 = rank * per_round + tid / p.row_vecs; i0 < total; i0 += ctas * per_round * kMoveVecs) {
     uint4 xk[kMoveVecs], xv[kMoveVecs];
     int64_t to[kMoveVecs];
 #pragma unroll
     for (int e = 0; e < kMoveVecs; ++e) {
-      const int64_t i = i0 + (int64_t)e * ctas * kMoveThreads;
+      const uint32_t i = i0 + e * ctas * per_round;
       to[e] = -1;
       if (i >= total) continue;
-      const int plane = (int)(i / per_plane), rest = (int)(i % per_plane), j = rest / p.row_vecs, c = rest % p.row_vecs;
-      const int l = plane / p.Hkv, h = plane % p.Hkv;
-      const int64_t from = ((((int64_t)l * p.B + b) * p.Hkv + h) * p.N + s_path[j]) * p.row_vecs + c;
+      const uint32_t plane = i / (uint32_t)n, j = i - plane * n, l = plane / (uint32_t)p.Hkv, h = plane - l * p.Hkv;
+      const int64_t from = ((((int64_t)l * p.B + b) * p.Hkv + h) * p.N + s_path[j]) * p.row_vecs + piece;
       xk[e] = p.tree_k[from];
       xv[e] = p.tree_v[from];
-      const int64_t row = move_row(p, b, l, h, move_len(p, b, l, h) + j);
-      if (NGC_IN_BOUNDS(p.dev_status, row >= 0 && row < p.rows)) to[e] = ((int64_t)plane * p.rows + row) * p.row_vecs + c;
+      const int64_t row = move_row(p, b, l, h, move_len(p, b, l, h) + (int)j);
+      if (NGC_IN_BOUNDS(p.dev_status, row >= 0 && row < p.rows)) to[e] = ((int64_t)plane * p.rows + row) * p.row_vecs + piece;
     }
 #pragma unroll
     for (int e = 0; e < kMoveVecs; ++e)
@@ -132,6 +131,11 @@ __global__ void __launch_bounds__(kMoveThreads) commit_kernel(MoveParams p) {
 
 // ---------------------------------------------------------------- fork
 
+// Barrier of `threads` threads of the CTA (whole warps).
+__device__ __forceinline__ void named_barrier(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
 // A source strip is read once for all of its copies: bulk copies bring up to 64 KB of it into shared memory, from where
 // bulk stores write it to every destination (a lane per destination).  No data passes through registers, and a CTA
 // of one busy warp keeps 64 KB in flight.  grid.x = (strip, chunk of its rows), chunks beyond the grid's follow in turns;
@@ -144,7 +148,7 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(MoveParams p, int n_
   extern __shared__ __align__(128) uint8_t stage[];                    // [4][kForkQuarter]
   __shared__ uint32_t is_source[kForkMaxB / 32];
   __shared__ uint64_t full[4];
-  __shared__ int dst[kForkThreads], n_dst;
+  __shared__ int dst[kForkThreads], bad_dst[kForkThreads], n_dst;
   const int tid = threadIdx.x, lane = tid & 31;
   const int strip = blockIdx.x / n_chunks, chunk0 = blockIdx.x % n_chunks, isv = strip & 1, plane = strip >> 1;
   const int l = plane / p.Hkv, h = plane % p.Hkv, own_list = p.page_table ? list_of(p.lists, l, h, p.Hkv) : 0;
@@ -208,26 +212,6 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(MoveParams p, int n_
           else dst[atomicAdd(&n_dst, 1)] = b;
         }
         __syncthreads();
-        if (sets_lens) {
-          // the lengths, if every list's pages are pages; nobody reads a destination's lengths (a source is no destination)
-          for (int d = 0; d < n_dst; ++d) {
-            const int b2 = dst[d];
-            bool bad_page = false;
-            if (p.page_table) {
-              const int64_t entries = (int64_t)p.G * p.pages_cap;
-              for (int64_t j = tid; j < entries; j += kForkThreads) {
-                const int gi = (int)(j / p.pages_cap), used = (list_len(p, s, gi, n_lens) + p.page - 1) / p.page;
-                bad_page |= j % p.pages_cap < used && ((uint32_t)p.page_table[s * entries + j] >= (uint32_t)p.pages_cap ||
-                                                       (uint32_t)p.page_table[b2 * entries + j] >= (uint32_t)p.pages_cap);
-              }
-            }
-            if (__syncthreads_or(bad_page)) {
-              if (tid == 0) set_dev_status(p.dev_status, NGC_DEV_BAD_PAGE);
-            } else {
-              for (int gi = tid; gi < n_lens; gi += kForkThreads) p.lens[(int64_t)b2 * n_lens + gi] = p.lens[(int64_t)s * n_lens + gi];
-            }
-          }
-        }
         const int n = n_dst;
         if (tid < 32 && n > 0) {
           for (int r0 = chunk0 * chunk_rows; ok && r0 < len; r0 += n_chunks * chunk_rows) {
@@ -248,11 +232,13 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(MoveParams p, int n_
             }
             __syncwarp();
             for (int i = 0; i * quarter_rows < rows; ++i) {
-              // (a quarter that a short chunk did not use keeps its phase: it is only ever the last chunk of a strip that is
-              // short, and the phases are counted per quarter)
+              // (phases are counted per quarter: a short chunk does not use them all)
               const int m = min(quarter_rows, rows - i * quarter_rows);
-              ok = ok && __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&full[i], (turn >> (8 * i)) & 1));
-              if (!ok) break;
+              ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&full[i], (turn >> (8 * i)) & 1));
+              if (!ok) {                        // giving up: no copy may be in flight when the CTA ends
+                for (int j = i + 1; j * quarter_rows < rows; ++j) ptx::mbar_wait_bounded(&full[j], (turn >> (8 * j)) & 1);
+                break;
+              }
               for (int d = lane; d < n; d += 32) {
                 const int b2 = dst[d];
                 const int32_t* to = p.page_table ? p.page_table + ((int64_t)b2 * p.G + own_list) * p.pages_cap : nullptr;
@@ -268,6 +254,29 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(MoveParams p, int n_
               turn ^= 1 << (8 * i);
             }
             if (!ok && lane == 0) set_dev_status(p.dev_status, NGC_DEV_TIMEOUT);
+          }
+        } else if (tid >= 32 && sets_lens) {
+          // meanwhile the other warps set the lengths of those whose lists all have good pages; nobody reads a destination's
+          // lengths (a source is no destination)
+          const int t = tid - 32, threads = kForkThreads - 32;
+          for (int d = t; d < n; d += threads) bad_dst[d] = 0;
+          named_barrier(1, threads);
+          if (p.page_table) {
+            const uint32_t entries = (uint32_t)p.G * p.pages_cap;
+            for (uint32_t j = t; j < entries; j += threads) {
+              const uint32_t gi = j / (uint32_t)p.pages_cap;
+              if ((int)(j - gi * p.pages_cap) >= (list_len(p, s, gi, n_lens) + p.page - 1) / p.page) continue;
+              const bool bad_source = (uint32_t)p.page_table[(int64_t)s * entries + j] >= (uint32_t)p.pages_cap;
+#pragma unroll 4
+              for (int d = 0; d < n; ++d)
+                if (bad_source | ((uint32_t)p.page_table[(int64_t)dst[d] * entries + j] >= (uint32_t)p.pages_cap)) bad_dst[d] = 1;
+            }
+            named_barrier(1, threads);
+          }
+          for (int i = t; i < n * n_lens; i += threads) {
+            const int d = i / n_lens, gi = i % n_lens;
+            if (!bad_dst[d]) p.lens[(int64_t)dst[d] * n_lens + gi] = p.lens[(int64_t)s * n_lens + gi];
+            else if (gi == 0) set_dev_status(p.dev_status, NGC_DEV_BAD_PAGE);
           }
         }
         __syncthreads();                        // the list may change
@@ -299,7 +308,7 @@ int commit_impl(const ngc_cache* c, const PagedView& pv, const void* tree_k, con
   const int64_t most = (int64_t)c->L * c->Hkv * N * p.row_vecs;
   unsigned cluster = 1;
   while (cluster < 8 && most > (int64_t)cluster * kMoveThreads * kMoveVecs && (int64_t)c->B * cluster * 2 <= 4 * 148) cluster *= 2;
-  if ((int64_t)c->B * cluster > 0x7fffffffLL) return NGC_ERR_UNSUPPORTED;
+  if ((int64_t)c->B * cluster > 0x7fffffffLL || most > 0x7fffffffLL) return NGC_ERR_UNSUPPORTED;
   NGC_CUDA_TRY(launch_pdl_cluster(commit_kernel, dim3((unsigned)c->B * cluster), dim3(kMoveThreads), cluster, stream, p));
   return NGC_OK;
 }
@@ -313,8 +322,9 @@ int fork_impl(const ngc_cache* c, const PagedView& pv, const int32_t* src_of, in
   static PerDeviceOnce attr_once;
   const int rc = attr_once.run([] { return cudaFuncSetAttribute(fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kForkChunk); });
   if (rc != NGC_OK) return rc;
-  // two rounds of CTAs (three fit an SM): first over the rows of the strips, then over the destinations
-  const int64_t strips = (int64_t)c->L * c->Hkv * 2, want = 2 * 3 * 148;
+  // one round of CTAs (three fit an SM; two rounds: 348 us instead of 333 us for four prompts to sixteen rollouts each),
+  // first over the rows of the strips, then over the destinations
+  const int64_t strips = (int64_t)c->L * c->Hkv * 2, want = 3 * 148;
   const int64_t most_chunks = ((int64_t)c->max_len * p.row_vecs * 16 + kForkChunk - 1) / kForkChunk;
   int64_t chunks = (want + strips - 1) / strips;
   if (chunks > most_chunks) chunks = most_chunks;
