@@ -44,10 +44,11 @@ template <int N> __device__ __forceinline__ void load_n(const float* p, float (&
 template <int D, int RB> struct Fma {
   static constexpr int kLanes = RB == 16 ? 32 : 16;          // per group of 4 rows
   static constexpr int kThreads = RB / 4 * kLanes;
+  static constexpr int kStages = RB == 16 ? 1 : 2;           // small blocks: more CTAs per SM hide the loads better
   static constexpr int kKeys = kKeyTile / kLanes;            // keys of a tile per lane: tx + kLanes * u
   static constexpr int kVec = D / kLanes < 4 ? D / kLanes : 4, kVecs = D / kLanes / kVec;   // channels per lane: kVecs runs of kVec
   struct Smem {
-    float q[RB][D + 4], k[2][kKeyTile][D + 4], v[2][kKeyTile][D];
+    float q[RB][D + 4], k[kStages][kKeyTile][D + 4], v[kStages][kKeyTile][D];
     float p[kKeyTile][RB + 4];
     uint32_t anc[kTreeMaxNodes][kTreeWords];
     int jump[kTreeMaxNodes];
@@ -58,7 +59,7 @@ template <int D, int RB> struct Fma {
 template <int D, int RB>
 __global__ void __launch_bounds__(Fma<D, RB>::kThreads) tree_fma_kernel(TreeAttnParams p) {
   using F = Fma<D, RB>;
-  constexpr int NT = F::kThreads, NL = F::kLanes, KL = F::kKeys, VW = F::kVec, VN = F::kVecs;
+  constexpr int NT = F::kThreads, ST = F::kStages, NL = F::kLanes, KL = F::kKeys, VW = F::kVec, VN = F::kVecs;
   extern __shared__ __align__(16) uint8_t smem_raw[];
   typename F::Smem& sm = *reinterpret_cast<typename F::Smem*>(smem_raw);
   const int tid = threadIdx.x, tx = tid % NL, ty = tid / NL;
@@ -89,7 +90,7 @@ __global__ void __launch_bounds__(Fma<D, RB>::kThreads) tree_fma_kernel(TreeAttn
   const int64_t row0 = (((int64_t)l * p.B + b) * p.Hq + (int64_t)h * p.g) * p.N;       // first query row of the KV head
 
   auto fetch = [&](int t) {                                        // dead keys: zeros, so that weight 0 x value is 0
-    const int s = t & 1;
+    const int s = t % ST;
     for (int i = tid; i < kKeyTile * (D / 4); i += NT) {
       const int jj = i / (D / 4), c = 4 * (i % (D / 4)), j = t * kKeyTile + jj;
       const bool live = j < keys;
@@ -104,7 +105,7 @@ __global__ void __launch_bounds__(Fma<D, RB>::kThreads) tree_fma_kernel(TreeAttn
     const bool live = r0 + r < rows;
     copy16_or_zero(&sm.q[r][c], (const float*)p.q + (row0 + (live ? r0 + r : 0)) * D + c, live);
   }
-  if (tile_lo < tile_hi) fetch(tile_lo);
+  if (ST == 2 && tile_lo < tile_hi) fetch(tile_lo);
   const bool tree_ok = tree_masks<NT>(p.parent + (int64_t)b * p.N, n, p.N, sm.anc, sm.jump);
   if (!tree_ok || !len_ok) {
     ptx::cp_async_wait_all();
@@ -129,10 +130,12 @@ __global__ void __launch_bounds__(Fma<D, RB>::kThreads) tree_fma_kernel(TreeAttn
       for (int c = 0; c < VW; ++c) acc[e][cv][c] = 0.f;
   }
   if (tid < 2) sm.odd[tid] = 0;
+  const bool works = r0 + 4 * (ty & ~(32 / NL - 1)) < rows;         // a warp without rows only helps to fetch
 
   for (int t = tile_lo; t < tile_hi; ++t) {
-    const int j0 = t * kKeyTile, s = t & 1;
-    if (t + 1 < tile_hi) {
+    const int j0 = t * kKeyTile, s = t % ST;
+    if (ST == 1) fetch(t);
+    if (ST == 2 && t + 1 < tile_hi) {
       fetch(t + 1);
       ptx::cp_async_wait_group<1>();
     } else {
@@ -145,6 +148,10 @@ __global__ void __launch_bounds__(Fma<D, RB>::kThreads) tree_fma_kernel(TreeAttn
         if (j0 + jj >= len && !finite4(*reinterpret_cast<const float4*>(&sm.v[s][jj][4 * (i % (D / 4))]))) sm.odd[s] = 1;
       }
       __syncthreads();
+    }
+    if (!works) {
+      __syncthreads();
+      continue;
     }
     // S: rows 4 ty + e, keys tx + NL u
     float z[4][KL];
@@ -320,7 +327,7 @@ TreePlan tree_plan(const ngc_cache* c, int layers, int N) {
   pl.block_rows = rows <= 16 ? 16 : 64;         // small blocks keep the arithmetic near the rows there are
   pl.blocks = (rows + pl.block_rows - 1) / pl.block_rows;
   const int64_t items = (int64_t)layers * c->B * c->Hkv * pl.blocks;
-  int64_t ns = (148 * 2 * 2 + items - 1) / items;
+  int64_t ns = 148 * (pl.block_rows == 16 ? 4 : 2) / items;      // one round of the CTAs that fit
   const int64_t by_len = ((int64_t)c->max_len + N + kSplitMin * kKeyTile - 1) / (kSplitMin * kKeyTile);
   if (ns > by_len) ns = by_len;
   if (ns > 64) ns = 64;
