@@ -22,6 +22,7 @@ namespace ngc {
 namespace {
 
 constexpr int kKeyTile = 32;                    // keys per tile, and the split granularity
+constexpr int kSms = 148;
 constexpr int kSplitMin = 2;                    // tiles a split has at least
 
 __device__ __forceinline__ bool finite4(float4 x) {
@@ -302,35 +303,35 @@ template <int D> cudaError_t opt_in_fma() {
 struct TreePlan {
   int block_rows, blocks;       // query rows per item, blocks per KV head
   int n_split;                  // FMA path: token splits
-  int even, grid, n_units;      // tensor cores: even split over `grid` CTAs, or a unit per CTA
+  int even, cut, grid, n_units; // tensor cores: tiles dealt to `grid` CTAs, units cut where that falls; or a unit per CTA
 };
 TreePlan tree_plan(const ngc_cache* c, int layers, int N) {
   const int rows = c->Hq / c->Hkv * N;
   TreePlan pl = {};
   pl.n_split = 1;
   if (c->dtype == NGC_BF16) {
-    const int tiles = tree_umma_tiles(rows), slots = 148, keys = tree_umma_keys(tiles);
+    const int tiles = tree_umma_tiles(rows), keys = tree_umma_keys(tiles);
     pl.blocks = (rows + 128 * tiles - 1) / (128 * tiles);
     pl.block_rows = pl.blocks > 1 ? 128 * tiles : rows;
     const int64_t units = (int64_t)layers * c->B * c->Hkv * pl.blocks;
     const int64_t longest = ((int64_t)c->max_len + keys - 1) / keys + (N + keys - 1) / keys;
-    // Many units: the hardware deals them out one by one.  Short ones are not worth a second kernel.
-    pl.even = units < 4 * slots && longest > 2 * kTreeMinTiles;
     pl.n_units = (int)(units > 0x7fffffffLL ? 0x7fffffffLL : units);
+    pl.even = units > kSms || longest > 2 * kTreeMinTiles;
+    pl.cut = pl.even && units < 8 * kSms;
     pl.grid = pl.n_units;
     if (pl.even) {
       const int64_t most = units * longest / kTreeMinTiles;
-      pl.grid = (int)(most < slots ? most : slots);
+      pl.grid = (int)(most < kSms ? most : kSms);
     }
     return pl;
   }
   pl.block_rows = rows <= 16 ? 16 : 64;         // small blocks keep the arithmetic near the rows there are
   pl.blocks = (rows + pl.block_rows - 1) / pl.block_rows;
   const int64_t items = (int64_t)layers * c->B * c->Hkv * pl.blocks;
-  int64_t ns = 148 * (pl.block_rows == 16 ? 4 : 2) / items;      // one round of the CTAs that fit
+  int64_t ns = kSms * (pl.block_rows == 16 ? 4 : 2) / items;      // one round of the CTAs that fit
   const int64_t by_len = ((int64_t)c->max_len + N + kSplitMin * kKeyTile - 1) / (kSplitMin * kKeyTile);
   if (ns > by_len) ns = by_len;
-  if (ns > 64) ns = 64;
+  if (ns > kSms) ns = kSms;
   pl.n_split = ns < 1 ? 1 : (int)ns;
   return pl;
 }
@@ -338,12 +339,12 @@ TreePlan tree_plan(const ngc_cache* c, int layers, int N) {
 // Scratch of one call: the parts' sums, their (m, l), the plan.
 struct TreeScratch { size_t ml, plan, bytes; };
 TreeScratch tree_scratch(const ngc_cache* c, const TreePlan& pl, int layers, int N) {
-  if (pl.n_split <= 1 && !pl.even) return {0, 0, 0};
-  const size_t parts = pl.even ? (size_t)pl.grid * 2 * pl.block_rows : (size_t)layers * c->B * c->Hq * N * pl.n_split;
+  if (pl.n_split <= 1 && !pl.cut) return {0, 0, 0};
+  const size_t parts = pl.cut ? (size_t)pl.grid * 2 * pl.block_rows : (size_t)layers * c->B * c->Hq * N * pl.n_split;
   TreeScratch s;
   s.ml = align256(parts * c->d * 4);
   s.plan = s.ml + align256(parts * 8);
-  s.bytes = s.plan + (pl.even ? align256((size_t)pl.grid * 8) : 0);
+  s.bytes = s.plan + (pl.cut ? align256((size_t)pl.grid * 8) : 0);
   return s;
 }
 
@@ -370,7 +371,7 @@ int tree_impl(const ngc_cache* c, const PagedView& pv, const void* q, const void
   p.G = lists_G(pv.lists, c->L, c->Hkv); p.lens_lists = c->lens_lists;
   const TreePlan plan = tree_plan(c, p.n_layers, N);
   p.row_blocks = plan.blocks; p.n_split = plan.n_split; p.block_rows = plan.block_rows;
-  p.even = plan.even; p.grid = plan.grid; p.n_units = plan.n_units; p.plan = nullptr;
+  p.even = plan.even; p.cut = plan.cut; p.grid = plan.grid; p.n_units = plan.n_units; p.plan = nullptr;
   const TreeScratch need = tree_scratch(c, plan, p.n_layers, N);
   if (need.bytes > 0) {
     if (!ws || ws_bytes < need.bytes || ((uintptr_t)ws & 255)) return NGC_ERR_WORKSPACE;
@@ -417,7 +418,7 @@ extern "C" int ngc_tree_attn_launches(const ngc_cache* c, int layers, int N) {
   using namespace ngc;
   if (!valid_cache(c) || layers < 1 || N < 1 || N > kTreeMaxNodes) return 0;
   const TreePlan pl = tree_plan(c, layers, N);
-  return pl.n_split > 1 || pl.even ? 2 : 1;
+  return pl.n_split > 1 || pl.cut ? 2 : 1;
 }
 
 extern "C" int ngc_tree_attn(const ngc_cache* c, const void* q, const void* tree_k, const void* tree_v, const int32_t* parent,

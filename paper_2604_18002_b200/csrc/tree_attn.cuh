@@ -24,12 +24,12 @@ struct TreeAttnParams {
   float* part_o;                // parts of split rows: sums, unnormalised ...
   float2* part_ml;              // ... and (maximum in log2 units, sum of weights)
                                 //   FMA path: [n_layers][B][Hq][N][n_split]; tensor cores: [CTA][2][block_rows]
-  int2* plan;                   // tensor cores, even split: per CTA, the unit that begins in it and goes on, the CTA it ends in or -1
+  int2* plan;                   // tensor cores, cut units: per CTA, the unit that begins in it and goes on, the CTA it ends in or -1
   int32_t* dev_status;
   int64_t rows;
   int L, B, Hq, Hkv, d, g, N;
   int layer_begin, n_layers, n_split, row_blocks, out_bf16;
-  int even, grid, n_units, block_rows;    // tensor cores
+  int even, cut, grid, n_units, block_rows;    // tensor cores
   float scale_log2;             // scale * log2(e)
   const int32_t* page_table;    // [B][G][pages_cap] or null
   int page, pages_cap, lists, G;
@@ -118,7 +118,7 @@ int launch_tree_umma(const TreeAttnParams& p, cudaStream_t stream);
 
 // Even split of `total` tiles: how many of `grid` CTAs take part (each gets at least kTreeMinTiles tiles, so `per` below is
 // at least one), the first tile of CTA c, and the CTA that has tile g.
-constexpr int kTreeMaxUnits = 1184, kTreeMinTiles = 3;
+constexpr int kTreeMinTiles = 3;
 __host__ __device__ inline int tree_even_ctas(int total, int grid) {
   const int most = total / kTreeMinTiles;
   return most < 1 ? 1 : (most < grid ? most : grid);

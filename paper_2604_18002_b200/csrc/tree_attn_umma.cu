@@ -25,10 +25,12 @@
 // The roles only meet at mbarriers, also from one unit to the next: loads and scores of the next unit run under the
 // end of the current one.
 //
-// Work is dealt out in one of two ways.  With many units (or short ones) a CTA takes one unit.  With few, the tiles of
-// all units form one line (with a gap before each unit that stands for the cost of beginning it) that is cut into equal
-// pieces, a CTA per piece: rollouts of any lengths keep all SMs busy to the end.  A CTA then owns at most two unfinished units, the one it begins in and the one it ends in; their
-// sums go to its two slots of the workspace and a second kernel joins the parts of every unit that was cut.
+// Work is dealt out by tiles: the tiles of all units form one line (with a gap before each unit that stands for the cost
+// of beginning it) that is cut into a piece per CTA, one CTA per SM.  With many units a piece ends at the next unit's
+// beginning.  With few (fewer than 8 per SM) the pieces are equal, so that rollouts of any lengths keep all SMs busy to the
+// end: a CTA then has at most two unfinished units, the one it begins in and the one it ends in; their sums go to its two
+// slots of the workspace and a second kernel joins the parts of every unit that was cut.  Where a handful of short units
+// leaves nothing to deal, a CTA takes one.
 //
 // bf16 P: one rounding per weight (2^-8), as in the decode and replay calls; the row sum takes the weights
 // before it.  0 x V must be 0 whatever a dead V row holds: rows of the last 16-row box beyond the live ones are
@@ -71,6 +73,9 @@ template <int D, int MT> struct Cfg {
 struct KvMaps { CUtensorMap whole, part, tree; };
 struct Maps { KvMaps k, v; CUtensorMap q; };
 
+// A unit and where it begins on the line.
+struct Found { int u, base, places; };
+
 template <int D, int MT> struct Shared {
   using C = Cfg<D, MT>;
   uint64_t k_full[C::kStages], k_empty[C::kStages], v_full[C::kStages], v_empty[C::kStages];
@@ -82,11 +87,8 @@ template <int D, int MT> struct Shared {
   uint32_t odd[4][kTreeWords];                  // by piece & 3: nodes whose V row holds an infinity or a NaN
   uint32_t tmem;
   int abort;
-  int warp_sum[C::kThreads / 32];
-  // even split, by unit: where it begins on the line, its length and node count (loaded once: while every SM streams K and
-  // V a load from global memory takes microseconds)
-  int base[kTreeMaxUnits + 1], len[kTreeMaxUnits];
-  uint8_t n[kTreeMaxUnits];
+  int warp_sum[C::kThreads / 32], chunk[C::kThreads], total;         // places of the line before each thread's units
+  Found found[2];
 };
 
 // What every role needs to know about the piece of a unit that is being worked on.
@@ -124,21 +126,17 @@ template <int KT> __device__ __forceinline__ int unit_tiles(int n, int len) {
 }
 
 // The next piece of the walk; false at its end.  (A unit per CTA: also a unit without tiles.)
-template <int KT, int kUnitCost, typename Sh> __device__ __forceinline__ bool next_piece(const TreeAttnParams& p, const Sh& sh, Walk& k, Piece& w) {
+template <int KT, int kUnitCost> __device__ __forceinline__ bool next_piece(const TreeAttnParams& p, Walk& k, Piece& w) {
   while (k.n_left > 0) {
     unit_of(p, (uint32_t)k.u, w);
-    int nt;
+    const bool fits = load_counts(p, w);
+    const int nt = fits ? unit_tiles<KT>(w.n, w.len) : 0;
     if (!p.even) {
-      const bool fits = load_counts(p, w);
-      nt = fits ? unit_tiles<KT>(w.n, w.len) : 0;
       if (!fits && threadIdx.x == 0) set_dev_status(p.dev_status, w.n < 0 || w.n > p.N ? NGC_DEV_BAD_TREE : NGC_DEV_BAD_COUNTS);
       w.lo = 0;
       w.n_tiles = nt;
       k.n_left = 0;
     } else {
-      w.n = sh.n[k.u];
-      w.len = sh.len[k.u];
-      nt = unit_tiles<KT>(w.n, w.len);
       const int places = nt > 0 ? min(nt + kUnitCost - k.at, k.n_left) : 0;
       w.lo = max(0, k.at - kUnitCost);
       w.n_tiles = max(0, k.at + places - kUnitCost) - w.lo;
@@ -155,6 +153,43 @@ template <int KT, int kUnitCost, typename Sh> __device__ __forceinline__ bool ne
     }
   }
   return false;
+}
+
+// Places of unit u on the line.
+template <int KT, int kUnitCost> __device__ __forceinline__ int unit_places(const TreeAttnParams& p, int u, bool reports) {
+  Piece w;
+  unit_of(p, (uint32_t)u, w);
+  const bool fits = load_counts(p, w);
+  // counts that cannot be worked with have no tiles
+  if (reports && !fits) set_dev_status(p.dev_status, w.n < 0 || w.n > p.N ? NGC_DEV_BAD_TREE : NGC_DEV_BAD_COUNTS);
+  const int t = fits ? unit_tiles<KT>(w.n, w.len) : 0;
+  return t > 0 ? t + kUnitCost : 0;
+}
+// The unit that place g lies in (whole warp): first the thread whose units it lies in, then 32 of them at a time.
+template <int KT, int kUnitCost>
+__device__ __forceinline__ Found find_unit(const TreeAttnParams& p, const int* chunk, int threads, int per, int g) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, hi = threads;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (chunk[mid] <= g) lo = mid; else hi = mid;
+  }
+  int run = chunk[lo];
+  for (int u0 = lo * per;; u0 += 32) {
+    const int mine = u0 + lane < min(p.n_units, lo * per + per) ? unit_places<KT, kUnitCost>(p, u0 + lane, false) : 0;
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += y;
+    }
+    const uint32_t over = __ballot_sync(0xffffffffu, run + incl > g);
+    if (over || u0 + 32 >= lo * per + per) {
+      const int at = over ? __ffs(over) - 1 : 31;
+      return {u0 + at, __shfl_sync(0xffffffffu, run + incl - mine, at), __shfl_sync(0xffffffffu, mine, at)};
+    }
+    run += __shfl_sync(0xffffffffu, incl, 31);
+  }
 }
 
 // Page-table entries in order, 32 at a time in the lanes of a producer warp, the next batch on its way.  An entry that is
@@ -310,18 +345,8 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
   if (p.even) {
     const int per = (p.n_units + NT - 1) / NT, u0 = min(p.n_units, tid * per), u1 = min(p.n_units, u0 + per);
     int sum = 0;
-    for (int i = u0; i < u1; ++i) {
-      Piece w;
-      unit_of(p, (uint32_t)i, w);
-      const bool fits = load_counts(p, w);
-      sh.len[i] = w.len;
-      sh.n[i] = (uint8_t)(fits ? w.n : 0);      // counts that cannot be worked with: no tiles
-      int t = fits ? unit_tiles<KT>(w.n, w.len) : 0;
-      if (t > 0) t += C::kUnitCost;
-      sh.base[i] = t;
-      sum += t;
-      if (blockIdx.x == 0 && !fits) set_dev_status(p.dev_status, w.n < 0 || w.n > p.N ? NGC_DEV_BAD_TREE : NGC_DEV_BAD_COUNTS);
-    }
+#pragma unroll 2
+    for (int i = u0; i < u1; ++i) sum += unit_places<KT, C::kUnitCost>(p, i, blockIdx.x == 0);
     int incl = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -332,34 +357,36 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     __syncthreads();
     int before = incl - sum;
     for (int i = 0; i < warp; ++i) before += sh.warp_sum[i];
-    for (int i = u0; i < u1; ++i) {
-      const int t = sh.base[i];
-      sh.base[i] = before;
-      before += t;
-    }
-    if (tid == NT - 1) sh.base[p.n_units] = before;
+    sh.chunk[tid] = before;
+    if (tid == NT - 1) sh.total = before + sum;
     __syncthreads();
-    const int total = sh.base[p.n_units], ctas = tree_even_ctas(total, gridDim.x);
+    const int total = sh.total, ctas = tree_even_ctas(total, gridDim.x);
     const TreeEven even(total, ctas);
     const int g0 = even.first(blockIdx.x), g1 = even.first(blockIdx.x + 1);
-    walk.n_left = (int)blockIdx.x < ctas ? g1 - g0 : 0;
-    // the unit that place g0 belongs to
-    int lo = 0, hi = p.n_units;
-    while (walk.n_left > 0 && hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (sh.base[mid] <= g0) lo = mid; else hi = mid;
+    const bool busy = (int)blockIdx.x < ctas && total > 0;
+    // the units in which this CTA's piece begins and ends (of whole units: in which the next piece begins)
+    if (busy && warp < 2) {
+      const int g = warp == 0 ? g0 : p.cut ? g1 - 1 : min(g1, total - 1);
+      const Found f = find_unit<KT, C::kUnitCost>(p, sh.chunk, NT, per, g);
+      if (lane == 0) sh.found[warp] = f;
     }
-    walk.u = lo;
-    walk.at = g0 - sh.base[lo];
-    // for the kernel that joins the parts: the unit that begins here and goes on elsewhere (at most the last one), and
-    // the CTA that it ends in
-    if (tid == 0) {
-      int last = lo, end = -1;
-      while (walk.n_left > 0 && sh.base[last + 1] < g1) ++last;
-      const int tile0 = sh.base[last] + C::kUnitCost;
-      if (walk.n_left > 0 && tile0 >= g0 && tile0 < g1 && sh.base[last + 1] > g1) end = even.owner(sh.base[last + 1] - 1);
-      p.plan[blockIdx.x] = make_int2(last, end);
+    __syncthreads();
+    const Found a = sh.found[0], z = sh.found[1];
+    if (!busy) {
+      walk.n_left = 0;
+    } else if (p.cut) {
+      walk = {a.u, g0 - a.base, g1 - g0, 0};
+      // for the kernel that joins the parts: the unit that begins here and goes on elsewhere (at most the last one), and
+      // the CTA that it ends in
+      const int tile0 = z.base + C::kUnitCost, end = z.base + z.places;
+      if (tid == 0) p.plan[blockIdx.x] = make_int2(z.u, tile0 >= g0 && tile0 < g1 && end > g1 ? even.owner(end - 1) : -1);
+    } else {
+      // units that begin at a place of the piece, to their ends
+      const bool here = a.base == g0;
+      const int begin = here ? g0 : a.base + a.places, end = g1 >= total ? total : z.base == g1 ? g1 : z.base + z.places;
+      walk = {here ? a.u : a.u + 1, 0, max(0, end - begin), 0};
     }
+    if (!busy && p.cut && tid == 0) p.plan[blockIdx.x] = make_int2(0, -1);
   }
 
   // Every role takes the same walk.  Ring positions and barrier phases follow from running counters over its pieces: tiles
@@ -374,9 +401,8 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     uint64_t* empty = is_v ? sh.v_empty : sh.k_empty;
     const KvMaps& map = is_v ? maps.v : maps.k;
     int n_q = 0;
-    bool ok = true;
-    while (ok && next_piece<KT, C::kUnitCost>(p, sh, walk, w)) {
-      if (w.n_tiles <= 0) continue;
+    bool ok = true, more = next_piece<KT, C::kUnitCost>(p, walk, w);
+    for (Piece next; ok && more && w.n_tiles > 0; w = next) {
       const int base = (int)(p.page_table ? (int64_t)w.b * p.pages_cap * p.page : p.seq_off[w.b]);
       PageWalk pages;
       if (p.page_table)
@@ -388,6 +414,7 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
         if (!ok) break;
         load_tile<D, KT>(p, map, pages, w, base, w.lo + i, ring + s * C::kTile, &full[s]);
         ++kv;
+        if (i == 0 && is_v) more = next_piece<KT, C::kUnitCost>(p, walk, next);      // (found out while this piece runs)
         if (is_v || i > 0) continue;
         // Q behind the first K tile: its buffer is free once the last S of the piece before is done, the ring earlier
         const int r0 = w.rb * MT * 128, tiles_m = min(MT, (rows - r0 + 127) >> 7);
@@ -404,6 +431,7 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
         }
         __syncwarp();
         ++n_q;
+        more = next_piece<KT, C::kUnitCost>(p, walk, next);
       }
     }
     if (!ok) {                                  // giving up: no copy may be in flight when the CTA ends
@@ -412,7 +440,7 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     }
   } else if (warp == C::kMaskWarp) {
     // ------------------------------------------------------------------ ancestor sets, four nodes per lane
-    while (next_piece<KT, C::kUnitCost>(p, sh, walk, w) && w.n_tiles > 0) {
+    while (next_piece<KT, C::kUnitCost>(p, walk, w) && w.n_tiles > 0) {        // (a piece ahead of the others)
       const int slot = walk.seq & 1, use = (walk.seq - 1) >> 1;
       int link[kTreeWords];
 #pragma unroll
@@ -466,9 +494,8 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     int n_q = 0, done[MT];                      // tiles per M tile so far
 #pragma unroll
     for (int m = 0; m < MT; ++m) done[m] = 0;
-    bool ok = true;
-    while (ok && next_piece<KT, C::kUnitCost>(p, sh, walk, w)) {
-      if (w.n_tiles <= 0) continue;
+    bool ok = true, more = next_piece<KT, C::kUnitCost>(p, walk, w);
+    for (Piece next; ok && more && w.n_tiles > 0; w = next) {
       const int tiles_m = min(MT, (rows - w.rb * MT * 128 + 127) >> 7);          // M tiles that have a row
       auto steps_of = [&](int i) {              // 16-key steps of tile i that hold a live key
         const int t = w.lo + i;
@@ -500,6 +527,7 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
       // (the S buffers: P of the tile that used one before was consumed by a product issued before, and the pipe runs them
       // in issue order)
       for (int m = 0; ok && m < tiles_m; ++m) issue_s(m, 0);
+      more = next_piece<KT, C::kUnitCost>(p, walk, next);
       for (int i = 0; ok && i < w.n_tiles; ++i) {
         const int s = (kv + i) % ST, steps = steps_of(i);
         const uint32_t v_lo = ((ptx::smem_u32(sV) + s * C::kTile) >> 4) | v_lbo;
@@ -545,11 +573,12 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     const uint32_t lane_base = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t o_addr = tmem + lane_base + C::kOCol + (uint32_t)(D * m);
     int tc = 0, fixes[3] = {0, 0, 0};           // tiles of this M tile so far; uses of sh.fixed
-    bool ok = true, more = next_piece<KT, C::kUnitCost>(p, sh, walk, w);
+    bool ok = true, more = next_piece<KT, C::kUnitCost>(p, walk, w);
     while (ok && more) {
       if (w.n_tiles <= 0) break;                // (a unit per CTA that has none)
       const int r0 = w.rb * MT * 128, seq = walk.seq, slot = seq & 3;
-      Piece next;                               // found out while the last product runs
+      Piece next;
+      more = next_piece<KT, C::kUnitCost>(p, walk, next);
       const int r = r0 + 128 * m + 32 * (warp & 3) + lane;
       const int node = (int)((uint32_t)r % (uint32_t)p.N);
       const bool live_row = r < rows && node < w.n;
@@ -695,7 +724,6 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
           l_run += s0 + s1;
         }
         // ---- the row's sums leave
-        if (ok) more = next_piece<KT, C::kUnitCost>(p, sh, walk, next);
         const int last = tc + w.n_tiles - 1;
         ok = ok && umma::warp_wait(&sh.o_done[m][last % NB], (last / NB) & 1, &sh.abort, p.dev_status) &&
              (!in_tree0 || umma::warp_wait(&sh.fixed[1], fixes[1] & 1, &sh.abort, p.dev_status)) &&
@@ -742,8 +770,6 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
         }
         umma::fence_before_sync();              // O may be overwritten once the next P of this thread is out
         tc += w.n_tiles;
-      } else {
-        more = next_piece<KT, C::kUnitCost>(p, sh, walk, next);
       }
       kv += w.n_tiles;
       fixes[0] += in_tail;
@@ -879,7 +905,7 @@ int launch_tree_umma(const TreeAttnParams& p, cudaStream_t stream) {
   if (rc != NGC_OK) return rc;
   if (p.d == 64) NGC_CUDA_TRY(one ? (launch<64, 1>(maps, p, stream)) : (launch<64, 2>(maps, p, stream)));
   else NGC_CUDA_TRY(one ? (launch<128, 1>(maps, p, stream)) : (launch<128, 2>(maps, p, stream)));
-  if (p.even) {
+  if (p.cut) {
     const dim3 grid((unsigned)p.grid, (unsigned)((p.block_rows + kJoinRows - 1) / kJoinRows)), block(16 * kJoinRows);
     NGC_CUDA_TRY(p.d == 64 ? launch_pdl(tree_join_kernel<64>, grid, block, 0, stream, p)
                            : launch_pdl(tree_join_kernel<128>, grid, block, 0, stream, p));

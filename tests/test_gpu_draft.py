@@ -125,6 +125,24 @@ def test_tree_attn_splits_a_long_cache(dtype, d, Hq, Hkv, N, T):
     check_tree(c, q, tk, tv, parent, n_nodes)
 
 
+@pytest.mark.parametrize("d,L,B,Hq,Hkv,N,T", [(128, 2, 330, 2, 2, 3, 150), (64, 1, 700, 2, 2, 2, 70), (128, 1, 80, 2, 2, 130 // 2, 300),
+                                              (128, 1, 310, 130, 1, 2, 40), (128, 3, 100, 2, 1, 1, 700)])
+def test_tree_attn_deals_out_many_units(d, L, B, Hq, Hkv, N, T):
+    """More (layer, sequence, KV head, row block) units than SMs: whole units dealt out (1320, 1400 and 930 units), or a few
+    units per SM cut where the deal falls; ragged lengths with empty caches, full ones and empty trees among them."""
+    rng = np.random.default_rng(B)
+    lens = rng.integers(0, T + 1, B)
+    lens[:4] = [0, T, 0, T]
+    nodes = rng.integers(0, N + 1, B)
+    nodes[:4] = [N, N, 0, 0]
+    c, q, tk, tv, parent, n_nodes = case(bf16, d, Hq, Hkv, L, lens.tolist(), N, "tree", seed=B, capacity=T, n_nodes=nodes)
+    b = ngc()
+    units = L * B * Hkv * -(-Hq // Hkv * N // (128 if Hq // Hkv * N <= 128 else 256))
+    dc = b.NgcCache(c.k.cuda(), c.v.cuda(), c.seq_off.cuda(), c.lens.cuda(), Hq, T)
+    assert units > 148 and b.tree_attn_launches(dc, N) == (1 if units >= 8 * 148 else 2)
+    check_tree(c, q, tk, tv, parent, n_nodes)
+
+
 @pytest.mark.parametrize("dtype,d", [(f32, 64), (bf16, 128), (bf16, 64)])
 def test_tree_attn_takes_nothing_from_dead_rows_and_other_branches(dtype, d):
     """Cache rows beyond the length, nodes beyond the tree and (for the rows that do not see them) nodes of other
