@@ -23,6 +23,7 @@ namespace {
 
 constexpr int kKeyTile = 32;                    // keys per tile, and the split granularity
 constexpr int kSms = 148;
+constexpr int kShortTiles = 48;                 // tensor cores: key tiles up to which a unit is a short one
 constexpr int kSplitMin = 2;                    // tiles a split has at least
 
 __device__ __forceinline__ bool finite4(float4 x) {
@@ -303,6 +304,7 @@ template <int D> cudaError_t opt_in_fma() {
 struct TreePlan {
   int block_rows, blocks;       // query rows per item, blocks per KV head
   int n_split;                  // FMA path: token splits
+  int tiles_m, ctas_sm;         // tensor cores: M tiles per CTA, CTAs per SM
   int even, cut, grid, n_units; // tensor cores: tiles dealt to `grid` CTAs, units cut where that falls; or a unit per CTA
 };
 TreePlan tree_plan(const ngc_cache* c, int layers, int N) {
@@ -316,12 +318,15 @@ TreePlan tree_plan(const ngc_cache* c, int layers, int N) {
     const int64_t units = (int64_t)layers * c->B * c->Hkv * pl.blocks;
     const int64_t longest = ((int64_t)c->max_len + keys - 1) / keys + (N + keys - 1) / keys;
     pl.n_units = (int)(units > 0x7fffffffLL ? 0x7fffffffLL : units);
-    pl.even = units > kSms || longest > 2 * kTreeMinTiles;
-    pl.cut = pl.even && units < 8 * kSms;
+    pl.tiles_m = tiles;
+    pl.ctas_sm = tiles == 1 && longest <= kShortTiles && units >= 4 * kSms ? 2 : 1;
+    const int64_t slots = kSms * pl.ctas_sm;
+    pl.even = units > slots || longest > 2 * kTreeMinTiles;
+    pl.cut = pl.even && units < 2 * slots;
     pl.grid = pl.n_units;
     if (pl.even) {
       const int64_t most = units * longest / kTreeMinTiles;
-      pl.grid = (int)(most < kSms ? most : kSms);
+      pl.grid = (int)(most < slots ? most : slots);
     }
     return pl;
   }
@@ -371,7 +376,7 @@ int tree_impl(const ngc_cache* c, const PagedView& pv, const void* q, const void
   p.G = lists_G(pv.lists, c->L, c->Hkv); p.lens_lists = c->lens_lists;
   const TreePlan plan = tree_plan(c, p.n_layers, N);
   p.row_blocks = plan.blocks; p.n_split = plan.n_split; p.block_rows = plan.block_rows;
-  p.even = plan.even; p.cut = plan.cut; p.grid = plan.grid; p.n_units = plan.n_units; p.plan = nullptr;
+  p.tiles_m = plan.tiles_m; p.ctas_sm = plan.ctas_sm; p.even = plan.even; p.cut = plan.cut; p.grid = plan.grid; p.n_units = plan.n_units; p.plan = nullptr;
   const TreeScratch need = tree_scratch(c, plan, p.n_layers, N);
   if (need.bytes > 0) {
     if (!ws || ws_bytes < need.bytes || ((uintptr_t)ws & 255)) return NGC_ERR_WORKSPACE;

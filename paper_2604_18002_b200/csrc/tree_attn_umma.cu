@@ -4,8 +4,9 @@
 // one after the other) with all of its key tiles: the cache rows, then the nodes of the tree.  The 128 rows of an M
 // tile are the 128 lanes of tensor memory.
 //
-//   up to 128 rows   MT = 1, tiles of 64 keys, S double-buffered, two CTAs per SM: these calls are bound by the cache
-//                    that they read, and the second CTA covers the first one's latencies;
+//   up to 128 rows   MT = 1, tiles of 64 keys, S double-buffered: these calls are bound by the cache that they read.  One
+//                    CTA per SM with five stages of K and V, or, where units are so short that their beginnings and ends
+//                    count, two CTAs with two stages each that cover one another's;
 //   more rows        MT = 2, tiles of 128 keys, one CTA per SM: bound by the tensor pipe and the exponentials.  K and V
 //                    tiles serve both M tiles, whose softmax and products alternate on the tensor pipe.  (With 64 keys
 //                    S = Q K^T waits for shared memory: Q is read again for every 64 keys.)
@@ -26,8 +27,8 @@
 // end of the current one.
 //
 // Work is dealt out by tiles: the tiles of all units form one line (with a gap before each unit that stands for the cost
-// of beginning it) that is cut into a piece per CTA, one CTA per SM.  With many units a piece ends at the next unit's
-// beginning.  With few (fewer than 8 per SM) the pieces are equal, so that rollouts of any lengths keep all SMs busy to the
+// of beginning it) that is cut into a piece per CTA.  With many units a piece ends at the next unit's
+// beginning.  With few (fewer than two per CTA) the pieces are equal, so that rollouts of any lengths keep all SMs busy to the
 // end: a CTA then has at most two unfinished units, the one it begins in and the one it ends in; their sums go to its two
 // slots of the workspace and a second kernel joins the parts of every unit that was cut.  Where a handful of short units
 // leaves nothing to deal, a CTA takes one.
@@ -51,11 +52,11 @@ namespace {
 
 constexpr float kLazyRescale = 8.f;             // log2 units the row maximum may grow before O is rescaled
 
-template <int D, int MT> struct Cfg {
+template <int D, int MT, int CT> struct Cfg {
   static constexpr int kKeys = tree_umma_keys(MT);         // keys per tile
   static constexpr int kBufs = MT == 1 ? 2 : 1;            // S buffers per M tile
   static constexpr int kHalves = kKeys / 64;               // P is handed over 64 keys at a time
-  static constexpr int kStages = (MT == 1 ? 5 : 2) * (128 / D);      // of K and of V
+  static constexpr int kStages = (MT == 1 && CT == 1 ? 5 : 2) * (128 / D);      // of K and of V
   static constexpr int kThreads = (4 * MT + 4) * 32;
   static constexpr int kMmaWarp = 4 * MT, kMaskWarp = 4 * MT + 1, kProducerWarp = 4 * MT + 2;      // K and Q; V in the warp behind
   static constexpr int kBox = kKeys * 128;                 // a tile's 64 channels
@@ -76,8 +77,8 @@ struct Maps { KvMaps k, v; CUtensorMap q; };
 // A unit and where it begins on the line.
 struct Found { int u, base, places; };
 
-template <int D, int MT> struct Shared {
-  using C = Cfg<D, MT>;
+template <int D, int MT, int CT> struct Shared {
+  using C = Cfg<D, MT, CT>;
   uint64_t k_full[C::kStages], k_empty[C::kStages], v_full[C::kStages], v_empty[C::kStages];
   uint64_t s_full[MT][C::kBufs], p_full[MT][C::kBufs][C::kHalves], o_done[MT][C::kBufs];
   uint64_t q_full, q_empty, masks_full[2], masks_empty[2], fixed[3], drain;
@@ -292,13 +293,13 @@ __device__ __forceinline__ uint32_t odd_half(uint32_t x) { return (x & 0x7f80u) 
 // Bits of x (two bf16) that belong to infinities or NaN.
 __device__ __forceinline__ uint32_t odd_bits(uint32_t x) { return odd_half(x) | odd_half(x >> 16) << 16; }
 
-template <int D, int MT>
-__global__ void __launch_bounds__(Cfg<D, MT>::kThreads, 1)
+template <int D, int MT, int CT>
+__global__ void __launch_bounds__(Cfg<D, MT, CT>::kThreads, CT)
 tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
-  using C = Cfg<D, MT>;
+  using C = Cfg<D, MT, CT>;
   constexpr int ST = C::kStages, NT = C::kThreads, KT = C::kKeys, NB = C::kBufs, NH = C::kHalves;
   extern __shared__ uint8_t smem_dyn[];
-  __shared__ Shared<D, MT> sh;
+  __shared__ Shared<D, MT, CT> sh;
   uint8_t* sQ = (uint8_t*)(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);     // [MT][128 rows]
   uint8_t* sK = sQ + MT * C::kQBytes;                                            // [ST]
   uint8_t* sV = sK + ST * C::kTile;                                              // [ST]
@@ -865,11 +866,21 @@ template <int D> __global__ void __launch_bounds__(16 * kJoinRows) tree_join_ker
   for (int c = 0; c < kPer; c += 4) tree_store_out4(p, to + c, make_float4(o[c] * inv, o[c + 1] * inv, o[c + 2] * inv, o[c + 3] * inv));
 }
 
-template <int D, int MT> cudaError_t opt_in() {
-  return cudaFuncSetAttribute(tree_umma_kernel<D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, MT>::kSmem);
+template <int D, int MT, int CT> cudaError_t opt_in() {
+  return cudaFuncSetAttribute(tree_umma_kernel<D, MT, CT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, MT, CT>::kSmem);
 }
-template <int D, int MT> cudaError_t launch(const Maps& maps, const TreeAttnParams& p, cudaStream_t stream) {
-  return launch_pdl(tree_umma_kernel<D, MT>, dim3(p.grid), dim3(Cfg<D, MT>::kThreads), Cfg<D, MT>::kSmem, stream, maps, p);
+template <int D, int MT, int CT> cudaError_t launch(const Maps& maps, const TreeAttnParams& p, cudaStream_t stream) {
+  using C = Cfg<D, MT, CT>;
+  return launch_pdl(tree_umma_kernel<D, MT, CT>, dim3(p.grid), dim3(C::kThreads), C::kSmem, stream, maps, p);
+}
+template <int D> cudaError_t launch_d(const Maps& maps, const TreeAttnParams& p, cudaStream_t stream) {
+  if (p.tiles_m == 2) return launch<D, 2, 1>(maps, p, stream);
+  return p.ctas_sm == 1 ? launch<D, 1, 1>(maps, p, stream) : launch<D, 1, 2>(maps, p, stream);
+}
+template <int D> cudaError_t opt_in_d() {
+  cudaError_t e = opt_in<D, 1, 1>();
+  if (e == cudaSuccess) e = opt_in<D, 1, 2>();
+  return e == cudaSuccess ? opt_in<D, 2, 1>() : e;
 }
 
 }  // namespace
@@ -879,7 +890,6 @@ int launch_tree_umma(const TreeAttnParams& p, cudaStream_t stream) {
   const int64_t strips = (int64_t)p.L * p.B * p.Hkv, q_rows = (int64_t)p.L * p.B * p.Hq * p.N;
   if (p.rows > 0x7fffffffLL || strips > 0x7fffffffLL) return NGC_ERR_UNSUPPORTED;      // TMA coordinates are 32-bit
   Maps maps;
-  const bool one = tree_umma_tiles(p.g * p.N) == 1;
   bool ok = make_rows_map(&maps.q, p.q, q_rows, 128, p.d);
   auto kv_maps = [&](KvMaps* m, const void* cache, const void* tree) {
     ok = ok && make_kv_map(&m->tree, tree, p.N, (int)strips, 16, p.d);
@@ -889,22 +899,18 @@ int launch_tree_umma(const TreeAttnParams& p, cudaStream_t stream) {
     }
     ok = ok && make_kv_map(&m->part, cache, p.rows, planes, 16, p.d) &&
          (p.page_table ? make_kv_map(&m->whole, cache, p.rows, planes, p.page, p.d)
-                       : make_strip_map(&m->whole, cache, p.rows, planes, tree_umma_keys(one ? 1 : 2), p.d));
+                       : make_strip_map(&m->whole, cache, p.rows, planes, tree_umma_keys(p.tiles_m), p.d));
   };
   kv_maps(&maps.k, p.k, p.tree_k);
   kv_maps(&maps.v, p.v, p.tree_v);
   if (!ok) return NGC_ERR_UNSUPPORTED;
   static PerDeviceOnce attr_once;
   const int rc = attr_once.run([] {
-    cudaError_t e = opt_in<64, 1>();
-    if (e == cudaSuccess) e = opt_in<64, 2>();
-    if (e == cudaSuccess) e = opt_in<128, 1>();
-    if (e == cudaSuccess) e = opt_in<128, 2>();
-    return e;
+    cudaError_t e = opt_in_d<64>();
+    return e == cudaSuccess ? opt_in_d<128>() : e;
   });
   if (rc != NGC_OK) return rc;
-  if (p.d == 64) NGC_CUDA_TRY(one ? (launch<64, 1>(maps, p, stream)) : (launch<64, 2>(maps, p, stream)));
-  else NGC_CUDA_TRY(one ? (launch<128, 1>(maps, p, stream)) : (launch<128, 2>(maps, p, stream)));
+  NGC_CUDA_TRY(p.d == 64 ? launch_d<64>(maps, p, stream) : launch_d<128>(maps, p, stream));
   if (p.cut) {
     const dim3 grid((unsigned)p.grid, (unsigned)((p.block_rows + kJoinRows - 1) / kJoinRows)), block(16 * kJoinRows);
     NGC_CUDA_TRY(p.d == 64 ? launch_pdl(tree_join_kernel<64>, grid, block, 0, stream, p)

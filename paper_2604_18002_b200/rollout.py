@@ -109,6 +109,9 @@ class NgcRollout:
         """Attention of every node of the drafted trees over the cache, its ancestors and itself; the cache is not changed."""
         N = parent.shape[1]
         if N not in self.ws_tree:
+            if torch.cuda.is_current_stream_capturing():
+                # (memory allocated during a capture belongs to the graph, later eager calls would share it)
+                raise ngc.NgcError(f"call draft_attention once with {N} nodes before capturing it")
             self.ws_tree[N] = ngc.alloc_workspace(ngc.workspace_bytes(ngc.OP_TREE_ATTN, self.cache, n_max=N), self.device)
         ngc.ngc_tree_attn(self.cache, q, tree_k, tree_v, parent, out, n_nodes, layer_begin, layer_end, ws=self.ws_tree[N],
                           status=self.status)

@@ -125,11 +125,11 @@ def test_tree_attn_splits_a_long_cache(dtype, d, Hq, Hkv, N, T):
     check_tree(c, q, tk, tv, parent, n_nodes)
 
 
-@pytest.mark.parametrize("d,L,B,Hq,Hkv,N,T", [(128, 2, 330, 2, 2, 3, 150), (64, 1, 700, 2, 2, 2, 70), (128, 1, 80, 2, 2, 130 // 2, 300),
-                                              (128, 1, 310, 130, 1, 2, 40), (128, 3, 100, 2, 1, 1, 700)])
-def test_tree_attn_deals_out_many_units(d, L, B, Hq, Hkv, N, T):
-    """More (layer, sequence, KV head, row block) units than SMs: whole units dealt out (1320, 1400 and 930 units), or a few
-    units per SM cut where the deal falls; ragged lengths with empty caches, full ones and empty trees among them."""
+@pytest.mark.parametrize("d,L,B,Hq,Hkv,N,T,launches", [(128, 2, 330, 2, 2, 3, 150, 1), (64, 1, 700, 2, 2, 2, 70, 1), (128, 1, 80, 2, 2, 65, 300, 2),
+                                                       (128, 1, 310, 130, 1, 2, 40, 1), (128, 3, 90, 2, 1, 1, 700, 2), (128, 1, 60, 8, 4, 90, 130, 2)])
+def test_tree_attn_deals_out_many_units(d, L, B, Hq, Hkv, N, T, launches):
+    """More (layer, sequence, KV head, row block) units than SMs: whole units dealt out (one launch), or units cut where the
+    deal falls and joined (two); ragged lengths with empty caches, full ones and empty trees among them."""
     rng = np.random.default_rng(B)
     lens = rng.integers(0, T + 1, B)
     lens[:4] = [0, T, 0, T]
@@ -137,9 +137,8 @@ def test_tree_attn_deals_out_many_units(d, L, B, Hq, Hkv, N, T):
     nodes[:4] = [N, N, 0, 0]
     c, q, tk, tv, parent, n_nodes = case(bf16, d, Hq, Hkv, L, lens.tolist(), N, "tree", seed=B, capacity=T, n_nodes=nodes)
     b = ngc()
-    units = L * B * Hkv * -(-Hq // Hkv * N // (128 if Hq // Hkv * N <= 128 else 256))
     dc = b.NgcCache(c.k.cuda(), c.v.cuda(), c.seq_off.cuda(), c.lens.cuda(), Hq, T)
-    assert units > 148 and b.tree_attn_launches(dc, N) == (1 if units >= 8 * 148 else 2)
+    assert b.tree_attn_launches(dc, N) == launches
     check_tree(c, q, tk, tv, parent, n_nodes)
 
 
@@ -703,3 +702,30 @@ def test_draft_step_in_a_graph_and_on_another_stream():
             assert torch.equal(x, w)
         restore()
     assert status_value(st) == 0
+
+
+def test_rollout_refuses_to_allocate_while_capturing():
+    """The first draft_attention with a node count allocates its workspace: inside a capture that is refused, and the capture
+    of a call made before works."""
+    from paper_2604_18002_b200.rollout import NgcRollout
+    b = ngc()
+    L, B, Hq, Hkv, d, N, T = 1, 2, 4, 2, 128, 4, 2000
+    ro = NgcRollout(L, B, Hq, Hkv, d, bf16, T, n_max=T, k_max=8)
+    ro.cache.k.normal_()
+    ro.cache.v.normal_()
+    ro.cache.lens.fill_(T)
+    q, tk, tv = (torch.randn((L, B, H, N, d), device="cuda").to(bf16) for H in (Hq, Hkv, Hkv))
+    parent = torch.as_tensor(trees(B, N, "tree", 1)).cuda()
+    out = torch.empty((L, B, Hq, N, d), dtype=f32, device="cuda")
+    q3, parent3 = q[:, :, :, :3].contiguous(), parent[:, :3].contiguous()
+    ro.draft_attention(q, tk, tv, parent, out)
+    ref = out.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ro.draft_attention(q, tk, tv, parent, out)
+        with pytest.raises(b.NgcError, match="before capturing"):
+            ro.draft_attention(q3, tk[:, :, :, :3].contiguous(), tv[:, :, :, :3].contiguous(), parent3, out[:, :, :, :3].contiguous())
+    out.zero_()
+    graph.replay()
+    assert torch.equal(out, ref)
+    ro.check_status()
