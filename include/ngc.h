@@ -464,14 +464,19 @@ int ngc_decode_attn_ragged_static(ngc_cache* c, const void* q, const void* new_k
  * For layers [layer_begin, layer_end); reads lens and the cache, changes neither.
  *   q       [L][B][Hq][N][d] cache dtype;  tree_k, tree_v [L][B][Hkv][N][d] cache dtype
  *   N       1 .. NGC_TREE_MAX_NODES (N = 1: the one-token decode without append)
- *   scale   positive and finite
+ *   scale   positive, at most 2e38
  *   out     [L][B][Hq][N][d] of out_dtype (NGC_F32, or NGC_BF16 for a bf16
  *           cache); only the layers of the range and the nodes of each tree
  *           are written
- * Masked and dead rows take no part whatever they hold (infinities, NaN).
- * fp32 scores, softmax and accumulation; on bf16 caches the probabilities are
- * rounded to bf16 for the P*V product.  A length outside 0 .. capacity is
- * reported (NGC_DEV_BAD_COUNTS) and the sequence skipped.  q, tree_k, tree_v,
+ * Masked and dead rows take no part whatever they hold (infinities, NaN); a
+ * row that sees a NaN or an infinite score is NaN, and so may be one with scores
+ * of 2^30 and more.  fp32 scores, softmax and accumulation; on bf16 caches the
+ * probabilities are rounded to bf16 for the P*V product.  Results are the same
+ * in every run; where one lies in its last bits may depend on the lengths of
+ * the call's other sequences (they decide how the work is cut).  A length
+ * outside 0 .. capacity is reported (NGC_DEV_BAD_COUNTS) and the sequence
+ * skipped.  The workspace is free again when the call has run: calls that may
+ * run at the same time (other streams, graphs) need one each.  q, tree_k, tree_v,
  * out, k and v must be 16-byte aligned.  Workspace:
  * ngc_workspace_bytes(NGC_OP_TREE_ATTN, c, 1, N, 0).
  */
@@ -507,7 +512,8 @@ int ngc_tree_attn_paged(const ngc_paged_cache* c, const void* q, const void* tre
  * uniforms[b][0] * sum w -- or the argmax, if greedy.
  *   tokens       [B][N] int32 in 0 .. vocab-1 (entry 0 unused)
  *   target_probs [B][N][vocab] fp32: row i follows node i.  Rows are taken as
- *                normalised; only the rows the walk visits are read.
+ *                normalised; whole rows are read only where the walk comes.
+ *                vocab <= 2^30
  *   draft_probs  [B][N][vocab] fp32 or NULL: row i is what node i's children were drawn from
  *   uniforms     [B][N] fp32 in [0, 1) (may be NULL if greedy)
  *   path         [B][N] out: accepted nodes from node 0 on, -1 padded (ascending)
@@ -548,6 +554,7 @@ int ngc_commit_draft_paged(ngc_paged_cache* c, const void* tree_k, const void* t
  *          b is reported (NGC_DEV_BAD_SOURCE) and left as it was, as is a b too
  *          small for its source in some list (NGC_DEV_STRIP_FULL) or one whose
  *          source has a length outside its capacity (NGC_DEV_BAD_COUNTS).
+ *          B <= 65536
  */
 int ngc_fork_kv(ngc_cache* c, const int32_t* src_of, int32_t* dev_status, ngc_stream stream);
 

@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(Fma<D, RB>::kThreads) tree_fma_kernel(TreeAttn
       continue;
     }
     const bool whole = p.n_split == 1;
-    const float inv = !whole ? 1.f : lsum[e] == 0.f ? 0.f : 1.f / lsum[e];     // a NaN stays one
+    const float inv = whole ? 1.f / lsum[e] : 1.f;                 // (a sum of 0: every score is -inf, the row is NaN)
     if (!whole && tx == 0) p.part_ml[pit] = make_float2(m[e], lsum[e]);
     float* const to = whole ? (float*)p.out + (row0 + r) * D : p.part_o + pit * D;
 #pragma unroll
@@ -276,13 +276,13 @@ __global__ void __launch_bounds__(128) tree_combine_kernel(TreeAttnParams p) {
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int s = 0; s < p.n_split; ++s) {
     const float2 ml = p.part_ml[row * p.n_split + s];
-    if (ml.x == -INFINITY) continue;                               // nothing visible in this part (it may hold no sums)
+    if (ml.x == -INFINITY && ml.y == 0.f) continue;                // nothing visible in this part; a NaN sum stays one
     const float f = exp2f(ml.x - mg);
     const float4 x = *reinterpret_cast<const float4*>(p.part_o + (row * p.n_split + s) * p.d + c);
     o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
     ls = fmaf(ml.y, f, ls);
   }
-  const float inv = ls == 0.f ? 0.f : 1.f / ls;
+  const float inv = 1.f / ls;
   tree_store_out4(p, ((int64_t)p.layer_begin * per_layer + row) * p.d + c, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
 }
 
@@ -362,7 +362,7 @@ int tree_impl(const ngc_cache* c, const PagedView& pv, const void* q, const void
               void* ws, size_t ws_bytes, int32_t* dev_status, cudaStream_t stream) {
   if (!q || !tree_k || !tree_v || !parent || !out || N < 1 || layer_begin < 0 || layer_end > c->L || layer_begin >= layer_end)
     return NGC_ERR_INVALID_ARG;
-  if (!(scale > 0.f) || scale > 3.0e38f) return NGC_ERR_INVALID_ARG;
+  if (!(scale > 0.f) || scale > 2.0e38f) return NGC_ERR_INVALID_ARG;      // (times log2 e it is still finite)
   if ((((uintptr_t)q | (uintptr_t)tree_k | (uintptr_t)tree_v | (uintptr_t)out | (uintptr_t)c->k | (uintptr_t)c->v) & 15) != 0)
     return NGC_ERR_INVALID_ARG;      // rows are moved as 16-byte vectors
   if (out_dtype != NGC_F32 && !(out_dtype == NGC_BF16 && c->dtype == NGC_BF16)) return NGC_ERR_INVALID_ARG;

@@ -20,8 +20,9 @@
 //   MMA warp         S = Q K^T into tensor memory, O += P V with P read from tensor memory;
 //   mask warp        the ancestor sets of the next unit's tree, by pointer doubling;
 //   softmax warps    (4 MT) one thread per row: mask (in tree tiles, its node's ancestors; in the cache's last tile a common
-//                    one), online softmax in the log2 domain, P as bf16 over the S it came from, 64 keys at a time.  The maximum used only moves when the true one has grown by
-//                    more than a factor 2^8, so O in tensor memory is rarely rescaled.
+//                    one), online softmax in the log2 domain, P as bf16 over the S it came from, 64 keys at a time.  The
+//                    maximum used only moves when the true one has grown by more than a factor 2^8, so O in tensor
+//                    memory is rarely rescaled.
 //
 // The roles only meet at mbarriers, also from one unit to the next: loads and scores of the next unit run under the
 // end of the current one.
@@ -739,7 +740,7 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
           uint32_t odd[kTreeWords];
 #pragma unroll
           for (int x = 0; x < kTreeWords; ++x) odd[x] = in_tree0 || in_tree1 ? sh.odd[slot][x] & aw[x] : 0u;
-          const float inv = l_run == 0.f ? 0.f : 1.f / l_run;             // a NaN stays one
+          const float inv = 1.f / l_run;        // (a sum of 0: every score is -inf, the row is NaN)
           const int64_t out_row = (((int64_t)w.l * p.B + w.b) * p.Hq + (int64_t)w.h * p.g) * p.N + r;
           const __nv_bfloat16* tv = (const __nv_bfloat16*)p.tree_v + (int64_t)w.strip * p.N * D;
 #pragma unroll 1
@@ -860,7 +861,7 @@ template <int D> __global__ void __launch_bounds__(16 * kJoinRows) tree_join_ker
   const int h = item % (uint32_t)p.Hkv;
   item /= (uint32_t)p.Hkv;
   const int b = item % (uint32_t)p.B, l = p.layer_begin + (int)(item / (uint32_t)p.B);
-  const float inv = ls == 0.f ? 0.f : 1.f / ls;
+  const float inv = 1.f / ls;
   const int64_t to = ((((int64_t)l * p.B + b) * p.Hq + (int64_t)h * p.g) * p.N + r) * D + kPer * lane;
 #pragma unroll
   for (int c = 0; c < kPer; c += 4) tree_store_out4(p, to + c, make_float4(o[c] * inv, o[c + 1] * inv, o[c + 2] * inv, o[c + 3] * inv));

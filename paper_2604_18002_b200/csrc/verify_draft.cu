@@ -13,7 +13,8 @@
 //
 // All decisions and sums are in fp64 (fp32 inputs are exact in it); multiplications and subtractions are kept apart (no
 // fused multiply-add), so that the arithmetic is the one written down.  The final draw is an inverse CDF: the sums
-// per CTA and per warp lead to a range of about vocab / 64 tokens, which the CTA that owns it scans.
+// per CTA and per warp lead to a range of 1 / 64 or 1 / 128 of the vocabulary (8 CTAs of 8 or 16 warps), which the CTA
+// that owns it scans.
 #include <cooperative_groups.h>
 
 #include "ngc_common.cuh"
@@ -343,7 +344,7 @@ extern "C" int ngc_verify_draft(const int32_t* tokens, const int32_t* parent, co
   using namespace ngc;
   if (!tokens || !parent || !target_probs || !path || !n_path || !next_token || (!greedy && !uniforms) || B < 1 || N < 1 || vocab < 1)
     return NGC_ERR_INVALID_ARG;
-  if (N > NGC_TREE_MAX_NODES) return NGC_ERR_UNSUPPORTED;
+  if (N > NGC_TREE_MAX_NODES || vocab > 1 << 30) return NGC_ERR_UNSUPPORTED;      // (indices a round ahead stay in 32 bits)
   const VerifyParams p = {tokens, parent, n_nodes, target_probs, draft_probs, uniforms, path, n_path, next_token, dev_status, N, vocab};
   // CTAs per sequence: a slice of at least 2048 tokens each, at most 8, and no more than one round of CTAs in all: a
   // sequence that rejects many children takes many passes, which others should not queue behind.  Few sequences get

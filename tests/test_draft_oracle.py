@@ -147,3 +147,11 @@ def test_binding_refuses_wrong_shapes_types_and_host_tensors(ngc):
     with pytest.raises(ngc.NgcError, match="contiguous"):
         ngc.ngc_verify_draft(parent, parent, p.transpose(0, 1).contiguous().transpose(0, 1), torch.zeros((B, N)), parent,
                              torch.zeros(B, dtype=torch.int32), torch.zeros(B, dtype=torch.int32))
+
+
+def test_limits_of_scale_and_vocabulary(ngc):
+    """scale * log2(e) has to stay finite, and token indices a round of loads ahead of the last one have to stay in 32 bits."""
+    lib = ngc.lib
+    c = ngc.CacheDesc(16, 16, 16, 16, 64, 2, 1, 12, 2, 128, ngc.BF16, 64)
+    assert lib.ngc_tree_attn(C.byref(c), 16, 16, 16, 16, None, 4, 0, 2, 2.5e38, 16, ngc.F32, None, 0, None, None) == -1
+    assert lib.ngc_verify_draft(16, 16, None, 16, 16, 16, 2, 4, (1 << 30) + 1, 0, 16, 16, 16, None, None) == -2

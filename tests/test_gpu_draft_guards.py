@@ -1,0 +1,198 @@
+"""What the drafted-token calls must not touch, and rows at the edge of the number range.
+
+(1) A spread of the calls' small parity cases on the bounds-checking build.  (2) Canaries: guard planes around K and V,
+spare rows behind every sequence, guard elements behind outputs and workspaces.  (3) Two calls at once on two streams.
+(4) Rows whose scores are NaN, all minus infinity, or huge."""
+import numpy as np
+import pytest
+import torch
+
+import test_gpu_draft as t_draft
+from helpers import ngc, status_value
+from oracle import draft
+from paper_2604_18002_b200 import synth
+from test_gpu_debug_build import PATTERN, assert_guards, debug_library, guarded, guarded_cache, planes_i16      # noqa: F401
+from test_gpu_draft import bound, case, device_cache, draft_case, run_tree, trees
+
+pytestmark = pytest.mark.gpu
+
+bf16, f32 = torch.bfloat16, torch.float32
+
+CASES = [(t_draft.test_tree_attn_matches_oracle, (i,)) for i in (0, 1, 4, 5, 7, 9, 12)] + [
+    (t_draft.test_tree_attn_splits_a_long_cache, (bf16, 128, 12, 2, 64, 3001)),
+    (t_draft.test_tree_attn_splits_a_long_cache, (f32, 64, 2, 2, 40, 1500)),
+    (t_draft.test_tree_attn_deals_out_many_units, (128, 2, 330, 2, 2, 3, 150, 1)),
+    (t_draft.test_paged_tree_attn_matches_oracle, (32, 1, True, 28, 4, 33, [96, 31])),
+    (t_draft.test_paged_bad_page_entry_is_reported_and_stays_with_its_sequence, ()),
+    (t_draft.test_verify_matches_oracle, (5, 128, 257, "star", "draft")),
+    (t_draft.test_commit_matches_oracle_bit_for_bit, (bf16, 64, 3, 2, 128, [300, 200, 130], 1)),
+    (t_draft.test_paged_commit_and_fork_match_oracle, (32, 1, True)),
+    (t_draft.test_fork_matches_oracle_bit_for_bit, (f32, 64, 1)),
+]
+
+
+@pytest.mark.parametrize("i", range(len(CASES)), ids=[f"{f.__name__}-{i}" for i, (f, _) in enumerate(CASES)])
+def test_small_draft_case_on_the_bounds_checking_build(i, debug_library):      # noqa: F811
+    fn, args = CASES[i]
+    fn(*args)
+
+
+# ------------------------------------------------------------------ canaries
+
+def guarded_workspace(need, extra=4096):
+    whole = torch.full((need + extra,), 0xAB, dtype=torch.uint8, device="cuda")
+    return whole[:need], whole
+
+
+@pytest.mark.parametrize("Hq,N,lens", [(12, 9, [700, 33, 257]), (12, 50, [300, 64, 1]), (2, 1, [5000, 2, 90])])
+def test_canaries_survive_tree_attention_commit_and_fork(Hq, N, lens):
+    b = ngc()
+    L, B, Hkv, d = 2, 3, 2, 128
+    cap = [max(lens) + N + 2] * B                              # 2 rows behind everything a sequence will hold
+    host, dc, bufs, so = guarded_cache(L, B, Hq, Hkv, d, lens, cap, seed=41)
+    q, tk, tv = (synth.normal((L, B, H, N, d), 50 + s, bf16) for H, s in ((Hq, 2), (Hkv, 3), (Hkv, 4)))
+    parent, n_nodes = trees(B, N, "tree", 3), np.array([N, max(N - 4, 0), 1], np.int32)
+    out, out_whole, out_fill = guarded((L, B, Hq, N, d), f32)
+    ws, ws_whole = guarded_workspace(b.workspace_bytes(b.OP_TREE_ATTN, dc, n_max=N))
+    st = b.new_status()
+    k0, v0 = planes_i16(dc)
+    dev = [x.cuda() for x in (q, tk, tv)]
+    b.ngc_tree_attn(dc, *dev, torch.as_tensor(parent).cuda(), out, torch.as_tensor(n_nodes).cuda(), ws=ws, status=st)
+    k1, v1 = planes_i16(dc)
+    assert status_value(st) == 0 and np.array_equal(k0, k1) and np.array_equal(v0, v1) and dc.lens.tolist() == lens
+    assert bool((out_whole[out.numel():] == out_fill).all()) and bool((ws_whole[ws.numel():] == 0xAB).all())
+    ref = draft.tree_attn(synth.to_numpy(host.k), synth.to_numpy(host.v), so, host.lens.numpy(), *[synth.to_numpy(x) for x in (q, tk, tv)],
+                          parent, n_nodes, fill=out_fill)
+    got = out.cpu().numpy().astype(np.float64)
+    assert (np.abs(got - ref) <= bound(host, q, tk, tv, parent, n_nodes, ref)).all()
+    # the append: its rows and nothing else
+    path = np.full((B, N), -1, np.int32)
+    n_path = np.array([min(N, 3), 1, 0], np.int32)
+    for bb in range(B):
+        path[bb, :n_path[bb]] = np.arange(n_path[bb])
+    b.ngc_commit_draft(dc, dev[1], dev[2], torch.as_tensor(path).cuda(), torch.as_tensor(n_path).cuda(), status=st)
+    k2, v2 = planes_i16(dc)
+    for bb in range(B):
+        new = slice(so[bb] + lens[bb], so[bb] + lens[bb] + n_path[bb])
+        for a, before, tree in ((k2, k1, tk), (v2, v1, tv)):
+            want = before.copy()[:, :, so[bb]:so[bb + 1]]
+            want[:, :, lens[bb]:lens[bb] + n_path[bb]] = tree[:, bb, :, :n_path[bb]].view(torch.int16).numpy()
+            assert np.array_equal(a[:, :, so[bb]:so[bb + 1]], want), (bb, new)
+    assert_guards(bufs)
+    # the fork: alive rows of sequence 0 to the others, rows behind them as they were
+    b.ngc_fork_kv(dc, torch.tensor([-1, 0, 0], dtype=torch.int32).cuda(), status=st)
+    k3, v3 = planes_i16(dc)
+    n0 = lens[0] + int(n_path[0])
+    assert status_value(st) == 0 and dc.lens.tolist() == [n0] * 3
+    for a, before in ((k3, k2), (v3, v2)):
+        for bb in range(B):
+            assert np.array_equal(a[:, :, so[bb]:so[bb] + n0], before[:, :, so[0]:so[0] + n0])
+            assert np.array_equal(a[:, :, so[bb] + n0:so[bb + 1]], before[:, :, so[bb] + n0:so[bb + 1]])
+    assert_guards(bufs)
+
+
+@pytest.mark.parametrize("T", [40, 3000])
+def test_canaries_behind_the_outputs_of_fp32_trees_and_of_the_verification(T):
+    b = ngc()
+    c, q, tk, tv, parent, _ = case(f32, 64, 4, 2, 1, [T], 5, "tree", seed=6)
+    dc = device_cache(c)
+    out, whole, fill = guarded(q.shape, f32)
+    ws, ws_whole = guarded_workspace(b.workspace_bytes(b.OP_TREE_ATTN, dc, n_max=5))
+    st = b.new_status()
+    b.ngc_tree_attn(dc, q.cuda(), tk.cuda(), tv.cuda(), torch.as_tensor(parent).cuda(), out, ws=ws, status=st)
+    assert status_value(st) == 0 and bool((whole[out.numel():] == fill).all()) and bool((ws_whole[ws.numel():] == 0xAB).all())
+    tokens, par, p, q_d, u = draft_case(3, 7, 501, "tree", "draft", 2)
+    outs = [guarded(s, torch.int32) for s in ((3, 7), (3,), (3,))]
+    b.ngc_verify_draft(*[torch.as_tensor(x).cuda() for x in (tokens, par, p, u)], *[o[0] for o in outs], torch.as_tensor(q_d).cuda(), status=st)
+    ref = draft.verify_draft(tokens, par, p, u, q_d)
+    for (a, w, f), r in zip(outs, ref):
+        assert np.array_equal(a.cpu().numpy(), r) and bool((w[a.numel():] == f).all())
+    assert status_value(st) == 0
+
+
+# ------------------------------------------------------------------ two calls at once
+
+def test_calls_on_two_streams_at_once():
+    """Each stream has its outputs, workspace and status: ten rounds of both at once give what each gives alone."""
+    b = ngc()
+    jobs = []
+    for seed, (dtype, d, Hq, N, lens) in enumerate([(bf16, 128, 12, 40, [4000, 100, 900]), (bf16, 128, 12, 6, [2000] * 70), (f32, 64, 4, 6, [900, 1500])]):
+        c, q, tk, tv, parent, _ = case(dtype, d, Hq, 2, 1, lens, N, "tree", seed=seed)
+        dc, st = device_cache(c), b.new_status()
+        dev = [x.cuda() for x in (q, tk, tv, torch.as_tensor(parent))]
+        out = torch.zeros(q.shape, dtype=f32, device="cuda")
+        ws = b.alloc_workspace(b.workspace_bytes(b.OP_TREE_ATTN, dc, n_max=N))
+        v = [torch.as_tensor(x).cuda() for x in draft_case(20, 9, 5000, "tree", "draft", seed)]
+        res = [torch.empty(s, dtype=torch.int32, device="cuda") for s in ((20, 9), (20,), (20,))]
+
+        def run(dc=dc, dev=dev, out=out, ws=ws, st=st, v=v, res=res):
+            b.ngc_tree_attn(dc, *dev, out, ws=ws, status=st)
+            b.ngc_verify_draft(v[0], v[1], v[2], v[4], *res, v[3], status=st)
+        run()
+        jobs.append((run, torch.cuda.Stream(), [out] + res, [x.clone() for x in [out] + res], st))
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for _, _, got, _, _ in jobs:
+            for x in got:
+                x.zero_()
+        for _, s, _, _, _ in jobs:
+            s.wait_stream(torch.cuda.current_stream())
+        for run, s, _, _, _ in jobs:
+            with torch.cuda.stream(s):
+                run()
+        for _, s, _, _, _ in jobs:
+            torch.cuda.current_stream().wait_stream(s)
+        for _, _, got, want, st in jobs:
+            assert status_value(st) == 0 and all(torch.equal(x, w) for x, w in zip(got, want))
+
+
+# ------------------------------------------------------------------ edges of the number range
+
+KINDS = [(f32, 64, 5, 40), (f32, 64, 5, 3000), (f32, 128, 40, 3000), (bf16, 128, 5, 40), (bf16, 128, 5, 4000), (bf16, 128, 100, 4000), (bf16, 64, 5, 4000)]
+
+
+@pytest.mark.parametrize("dtype,d,N,T", KINDS)      # with one part per row and with several
+def test_a_query_of_nan_gives_nan_and_changes_no_other_row(dtype, d, N, T):
+    c, q, tk, tv, parent, _ = case(dtype, d, 4, 2, 1, [T, T], N, "tree", seed=7)
+    clean, _ = run_tree(c, q, tk, tv, parent, None)
+    q2 = q.clone()
+    q2[0, 1, 2, 1, 3] = float("nan")
+    out, st = run_tree(c, q2, tk, tv, parent, None)
+    assert st == 0 and torch.isnan(out[0, 1, 2, 1]).all()
+    out[0, 1, 2, 1] = clean[0, 1, 2, 1]
+    assert torch.equal(out, clean)
+
+
+@pytest.mark.parametrize("dtype,d,N,T", KINDS)
+def test_scores_of_minus_infinity(dtype, d, N, T):
+    """Where all that a row sees scores minus infinity its softmax is 0 / 0, a NaN; where some of it does, that has weight 0."""
+    c, q, tk, tv, parent, _ = case(dtype, d, 4, 2, 1, [T], N, "tree", seed=9)
+    q[..., 0] = 1.0
+    c.k[..., 0] = float("-inf")
+    empty = c.clone()
+    empty.lens = torch.zeros_like(c.lens)
+    ref = draft.tree_attn(synth.to_numpy(empty.k), synth.to_numpy(empty.v), c.seq_off.numpy(), empty.lens.numpy(), synth.to_numpy(q),
+                          synth.to_numpy(tk), synth.to_numpy(tv), parent)
+    out, st = run_tree(c, q, tk, tv, parent, None)
+    assert st == 0 and (np.abs(out.cpu().numpy() - ref) <= bound(empty, q, tk, tv, parent, None, ref)).all()
+    tk[..., 0] = float("-inf")
+    out, st = run_tree(c, q, tk, tv, parent, None)
+    assert st == 0 and torch.isnan(out).all()
+
+
+@pytest.mark.parametrize("dtype,d,N,T", KINDS)
+def test_scores_up_to_the_documented_size(dtype, d, N, T):
+    """One cache row scores 2^29, everything else at most 2^28: its weight is 1, all others are 0.  Its weight is rounded once
+    before the product (2^-8 on bf16 caches), the sum it is divided by is not; 1 / sum and the product are rounded in fp32
+    (the two together, and an exponential that is the same on both sides, below 2^-20)."""
+    c, q, tk, tv, _, _ = case(dtype, d, 4, 2, 1, [T], N, "tree", seed=11)
+    parent = trees(1, N, "star", 0)
+    q.zero_(); c.k.zero_(); tk.zero_()
+    q[..., 0] = 2.0 ** 15
+    c.k[..., 0] = torch.as_tensor(np.random.default_rng(0).integers(-128, 129, tuple(c.k.shape[:3]))).to(dtype) * 64      # exact, up to 2^13
+    tk[..., 0] = 2.0 ** 13
+    top = T // 2 + 1
+    c.k[:, :, top, 0] = 2.0 ** 14
+    out, st = run_tree(c, q, tk, tv, parent, None, scale=1.0)
+    want = c.v[0, :, top].double().numpy()[None, None, :, None, None].repeat(2, 3).repeat(N, 4).reshape(1, 1, 4, N, d)
+    assert st == 0 and (np.abs(out.double().cpu().numpy() - want) <= (2.0 ** -8 if dtype == bf16 else 2.0 ** -20) * np.abs(want) + 1e-30).all()
