@@ -1,8 +1,8 @@
 // ngc_verify_draft: multi-round speculative sampling over a drafted tree.
 //
 // A cluster of up to 8 CTAs per sequence; every CTA owns a slice of the vocabulary, every warp a contiguous range of
-// the slice.  All CTAs take the same walk from the same numbers, so only sums over the vocabulary are exchanged (one
-// number per CTA through distributed shared memory, added in rank order).
+// the slice.  All CTAs take the same walk from the same numbers, so only sums over the vocabulary are exchanged: each
+// warp writes its own into the shared memory of all CTAs, one cluster barrier later everyone adds them in one order.
 //
 // Nodes are numbered with parents before children, so one ascending sweep over the nodes visits the children of
 // the current node in index order.  What a test needs of the big rows, p(x) and q(x) at the parent, is fetched for
@@ -13,8 +13,11 @@
 //
 // All decisions and sums are in fp64 (fp32 inputs are exact in it); multiplications and subtractions are kept apart (no
 // fused multiply-add), so that the arithmetic is the one written down.  The final draw is an inverse CDF: the sums
-// per CTA and per warp lead to a range of 1 / 64 or 1 / 128 of the vocabulary (8 CTAs of 8 or 16 warps), which the CTA
-// that owns it scans.
+// per CTA and per warp lead to a range of 1 / 64 of a large vocabulary, which the CTA that owns it scans.
+//
+// What bounds it: a rejection is a pass over two rows that waits for the one before.  One sequence, 131072 tokens: 9.6 us
+// with none (launch, tree, one pass, draw), then 2.2 us each.  64 sequences: 15 us with none (a row each, 34 MB), 31 us
+// with up to five, whose rows come from L2 after the first time.
 #include <cooperative_groups.h>
 
 #include "ngc_common.cuh"
@@ -26,9 +29,9 @@ namespace {
 namespace cg = cooperative_groups;
 
 enum { kModeDraft = 0, kModePoint = 1, kModeGreedy = 2 };
-constexpr int kMaxWarps = 16;                        // per CTA
+constexpr int kVerifyThreads = 256, kVerifyWarps = kVerifyThreads / 32;
 constexpr int kMaxCluster = 8;
-constexpr int kUnroll = 8;                           // loads a lane has in flight per row
+constexpr int kUnroll = 4;                           // 16-byte loads a lane has in flight per row
 
 struct VerifyParams {
   const int32_t* tokens;
@@ -47,11 +50,11 @@ struct VerifyParams {
 struct VerifyShared {
   int parent[NGC_TREE_MAX_NODES], token[NGC_TREE_MAX_NODES], path[NGC_TREE_MAX_NODES], tried[NGC_TREE_MAX_NODES];
   float u[NGC_TREE_MAX_NODES], p[NGC_TREE_MAX_NODES], q[NGC_TREE_MAX_NODES];     // p, q: of the node's token, at its parent
-  double warp_sum[kMaxWarps];
-  float warp_max[kMaxWarps];
-  int warp_arg[kMaxWarps];
-  // what the other CTAs read; two of each, so that one cluster barrier per exchange is enough
-  double cta_sum[2];
+  double scan[kVerifyWarps];
+  float warp_max[kVerifyWarps];
+  int warp_arg[kVerifyWarps];
+  // what the CTAs tell one another; two of each, so that one cluster barrier per exchange is enough
+  double sums[2][kMaxCluster][kVerifyWarps];            // of all CTAs' warps, written by them
   float cta_max[2];
   int cta_arg[2];
   int last;
@@ -79,32 +82,51 @@ template <int MODE> struct Residual {
   __device__ __forceinline__ double at(int x) const { return of(x, p[x], with_q() ? q[x] : 0.f); }
 };
 
+// Four tokens of a row from x0 on, with `fill` in place of those outside [lo, hi).  One load where `vec` says that x0 is
+// 16-byte aligned and all four are asked for.
+__device__ __forceinline__ float4 load4(const float* row, int x0, int lo, int hi, bool vec, float fill) {
+  if (vec && x0 >= lo && x0 + 4 <= hi) return *reinterpret_cast<const float4*>(row + x0);
+  float4 v;
+  v.x = x0 >= lo && x0 < hi ? row[x0] : fill;
+  v.y = x0 + 1 >= lo && x0 + 1 < hi ? row[x0 + 1] : fill;
+  v.z = x0 + 2 >= lo && x0 + 2 < hi ? row[x0 + 2] : fill;
+  v.w = x0 + 3 >= lo && x0 + 3 < hi ? row[x0 + 3] : fill;
+  return v;
+}
+// Places of a row that are 16-byte aligned: x with (x + phase) % 4 == 0.
+__device__ __forceinline__ int row_phase(const float* row) { return (int)((uintptr_t)row >> 2) & 3; }
+
 // Sum over this warp's range.
 template <int MODE> __device__ __forceinline__ double range_sum(const Residual<MODE>& w, int lo, int hi) {
-  const int lane = threadIdx.x & 31;
-  const bool with_q = w.with_q();
-  double s[2] = {0.0, 0.0};
-  for (int x0 = lo + lane; x0 < hi; x0 += 32 * kUnroll) {
-    float pv[kUnroll], qv[kUnroll];
+  const int lane = threadIdx.x & 31, phase = row_phase(w.p);
+  const bool with_q = w.with_q(), q_vec = with_q && row_phase(w.q) == phase;
+  double s[4] = {0.0, 0.0, 0.0, 0.0};
+  for (int x0 = ((lo + phase) & ~3) - phase + 4 * lane; x0 < hi; x0 += 128 * kUnroll) {
+    float4 pv[kUnroll], qv[kUnroll];
 #pragma unroll
     for (int e = 0; e < kUnroll; ++e) {
-      const int x = x0 + 32 * e;
-      pv[e] = x < hi ? w.p[x] : 0.f;
-      qv[e] = with_q && x < hi ? w.q[x] : 0.f;
+      pv[e] = load4(w.p, x0 + 128 * e, lo, hi, true, 0.f);
+      qv[e] = with_q ? load4(w.q, x0 + 128 * e, lo, hi, q_vec, 0.f) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
 #pragma unroll
-    for (int e = 0; e < kUnroll; ++e) s[e & 1] += w.of(x0 + 32 * e, pv[e], qv[e]);
+    for (int e = 0; e < kUnroll; ++e) {
+      const int x = x0 + 128 * e;
+      s[0] += w.of(x, pv[e].x, qv[e].x);
+      s[1] += w.of(x + 1, pv[e].y, qv[e].y);
+      s[2] += w.of(x + 2, pv[e].z, qv[e].z);
+      s[3] += w.of(x + 3, pv[e].w, qv[e].w);
+    }
   }
-  return warp_sum(s[0] + s[1]);
+  return warp_sum((s[0] + s[1]) + (s[2] + s[3]));
 }
 
-template <int MODE, int kVerifyThreads>
-__global__ void __launch_bounds__(kVerifyThreads, 1024 / kVerifyThreads) verify_draft_kernel(VerifyParams p) {
-  constexpr int kVerifyWarps = kVerifyThreads / 32;
+template <int MODE>
+__global__ void __launch_bounds__(kVerifyThreads, 4) verify_draft_kernel(VerifyParams p) {
   __shared__ VerifyShared sh;
   const cg::cluster_group cluster = cg::this_cluster();
   const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int b = blockIdx.x / ctas, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  cluster.barrier_arrive();                          // (shared memory of a CTA may be written from outside once it runs)
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
   // the tree, and of the big rows what the tests need: two rounds of loads for all nodes at once
@@ -129,28 +151,23 @@ __global__ void __launch_bounds__(kVerifyThreads, 1024 / kVerifyThreads) verify_
     }
   }
   int status = __syncthreads_or(bad) ? NGC_DEV_BAD_TREE : NGC_DEV_OK;
+  cluster.barrier_wait();
 
   // slices of the CTAs, ranges of the warps
   const int per_cta = (p.vocab + ctas - 1) / ctas, cta_lo = min(p.vocab, rank * per_cta), cta_hi = min(p.vocab, cta_lo + per_cta);
   const int per_warp = (per_cta + kVerifyWarps - 1) / kVerifyWarps;
   const int lo = min(cta_hi, cta_lo + warp * per_warp), hi = min(cta_hi, lo + per_warp);
   int exchange = 0;
-  double share = 0.0;                                // lane i of every warp: the sum of CTA i's slice
 
-  // sum of a residual over the vocabulary: the same value in every thread of the cluster; the shares of warps and CTAs stay
+  // sum of a residual over the vocabulary: the same value in every thread of the cluster; every CTA has all warps' sums
   auto vocab_sum = [&](const Residual<MODE>& w) {
     const double s = range_sum(w, lo, hi);
-    __syncthreads();
-    if (lane == 0) sh.warp_sum[warp] = s;
-    __syncthreads();
-    if (warp == 0) {
-      const double t = warp_sum(lane < kVerifyWarps ? sh.warp_sum[lane] : 0.0);
-      if (lane == 0) sh.cta_sum[exchange & 1] = t;
-    }
+    if (lane < ctas) cluster.map_shared_rank(&sh, lane)->sums[exchange & 1][rank][warp] = s;
     cluster.sync();
-    share = lane < ctas ? cluster.map_shared_rank(sh.cta_sum, lane)[exchange & 1] : 0.0;
+    double t = 0.0;
+    for (int i = lane; i < ctas * kVerifyWarps; i += 32) t += sh.sums[exchange & 1][i / kVerifyWarps][i % kVerifyWarps];
     ++exchange;
-    return warp_sum(share);
+    return warp_sum(t);
   };
   // argmax of a row (the smallest index of equal values), or -1 if the row holds a NaN
   auto better = [](float v, int a, float& best, int& arg) {
@@ -168,14 +185,20 @@ __global__ void __launch_bounds__(kVerifyThreads, 1024 / kVerifyThreads) verify_
     float best = -INFINITY;
     int arg = 0x7fffffff;
     bool nan = false;
-    for (int x0 = lo + lane; x0 < hi; x0 += 32 * kUnroll) {
-      float v[kUnroll];
+    const int phase = row_phase(row);
+    for (int x0 = ((lo + phase) & ~3) - phase + 4 * lane; x0 < hi; x0 += 128 * kUnroll) {
+      float4 v[kUnroll];
 #pragma unroll
-      for (int e = 0; e < kUnroll; ++e) v[e] = x0 + 32 * e < hi ? row[x0 + 32 * e] : -INFINITY;
+      for (int e = 0; e < kUnroll; ++e) v[e] = load4(row, x0 + 128 * e, lo, hi, true, -INFINITY);
 #pragma unroll
       for (int e = 0; e < kUnroll; ++e) {
-        nan = nan || v[e] != v[e];
-        if (x0 + 32 * e < hi) better(v[e], x0 + 32 * e, best, arg);
+        const float at[4] = {v[e].x, v[e].y, v[e].z, v[e].w};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int x = x0 + 128 * e + c;
+          nan = nan || at[c] != at[c];
+          if (x >= lo && x < hi) better(at[c], x, best, arg);
+        }
       }
     }
     warp_best(best, arg);
@@ -260,6 +283,10 @@ __global__ void __launch_bounds__(kVerifyThreads, 1024 / kVerifyThreads) verify_
         // the CTA and the warp range that the target falls into; rounding may leave it at the very end: then the last
         // token with mass
         double t = __dmul_rn((double)sh.u[0], total), before = 0.0;
+        const int slot = (exchange - 1) & 1;         // of the sums of w as it stands
+        double share = 0.0;                          // lane i: CTA i
+        if (lane < ctas)
+          for (int i = 0; i < kVerifyWarps; ++i) share += sh.sums[slot][lane][i];
         int own = -1, last = 0;
         double last_before = 0.0;
         for (int i = 0; i < ctas; ++i) {
@@ -273,7 +300,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 1024 / kVerifyThreads) verify_
         if (draws) {
           int range = -1;
           last = 0;
-          const double shares = lane < kVerifyWarps ? sh.warp_sum[lane] : 0.0;
+          const double shares = lane < kVerifyWarps ? sh.sums[slot][rank][lane] : 0.0;
           for (int i = 0; i < kVerifyWarps; ++i) {
             const double s = __shfl_sync(0xffffffffu, shares, i);
             if (s > 0.0) { last = i; last_before = before; }
@@ -298,12 +325,11 @@ __global__ void __launch_bounds__(kVerifyThreads, 1024 / kVerifyThreads) verify_
             const double y = __shfl_up_sync(0xffffffffu, c, o);
             if (lane >= o) c += y;
           }
-          __syncthreads();                           // (warp_sum has been read)
           if (tid == 0) { sh.last = -1; sh.warp_arg[0] = 0x7fffffff; }
-          if (lane == 31) sh.warp_sum[warp] = c;
+          if (lane == 31) sh.scan[warp] = c;
           __syncthreads();
 #pragma unroll
-          for (int i = 0; i < kVerifyWarps; ++i) before += i < warp ? sh.warp_sum[i] : 0.0;
+          for (int i = 0; i < kVerifyWarps; ++i) before += i < warp ? sh.scan[i] : 0.0;
           double upto = before + (c - s);
           int hit = -1;
           if (upto + s > t)
@@ -347,19 +373,16 @@ extern "C" int ngc_verify_draft(const int32_t* tokens, const int32_t* parent, co
   if (N > NGC_TREE_MAX_NODES || vocab > 1 << 30) return NGC_ERR_UNSUPPORTED;      // (indices a round ahead stay in 32 bits)
   const VerifyParams p = {tokens, parent, n_nodes, target_probs, draft_probs, uniforms, path, n_path, next_token, dev_status, N, vocab};
   // CTAs per sequence: a slice of at least 2048 tokens each, at most 8, and no more than one round of CTAs in all: a
-  // sequence that rejects many children takes many passes, which others should not queue behind.  Few sequences get
-  // twice the threads: then a pass is bound by each SM's conversions and latencies (4 rejections in 131072 tokens: 18.5 us
-  // with 512 threads, 24.8 us with 256), else by how many CTAs are there at once (64 sequences: 46.7 and 42.3 us).
-  const bool wide = (int64_t)B * kMaxCluster <= 2 * 148;
+  // sequence that rejects many children takes many passes, which others should not queue behind.  256 threads each: with
+  // 512 a pass over 131072 tokens of one sequence is shorter (4 rejections: 16.7 instead of 18.5 us), the rest longer (no
+  // rejection, 37 sequences: 21.4 and 14.4 us; 64 sequences of 16 drafted tokens: 38.6 and 31.0 us).
   int cluster = vocab / 2048;
   if (cluster > 4 * 148 / B) cluster = 4 * 148 / B;
   if (cluster > kMaxCluster) cluster = kMaxCluster;
   if (cluster < 1) cluster = 1;
   if ((int64_t)B * cluster > 0x7fffffffLL) return NGC_ERR_UNSUPPORTED;
-  const dim3 grid((unsigned)(B * cluster)), block(wide ? 512 : 256);
-  auto kernel = greedy ? (wide ? verify_draft_kernel<kModeGreedy, 512> : verify_draft_kernel<kModeGreedy, 256>)
-              : draft_probs ? (wide ? verify_draft_kernel<kModeDraft, 512> : verify_draft_kernel<kModeDraft, 256>)
-                            : (wide ? verify_draft_kernel<kModePoint, 512> : verify_draft_kernel<kModePoint, 256>);
+  const dim3 grid((unsigned)(B * cluster)), block(kVerifyThreads);
+  auto kernel = greedy ? verify_draft_kernel<kModeGreedy> : draft_probs ? verify_draft_kernel<kModeDraft> : verify_draft_kernel<kModePoint>;
   NGC_CUDA_TRY(launch_pdl_cluster(kernel, grid, block, (unsigned)cluster, (cudaStream_t)stream, p));
   return NGC_OK;
 }

@@ -110,6 +110,31 @@ def test_canaries_behind_the_outputs_of_fp32_trees_and_of_the_verification(T):
     assert status_value(st) == 0
 
 
+@pytest.mark.parametrize("mode", ["draft", "point", "greedy"])
+@pytest.mark.parametrize("V", [1, 3, 130, 4099, 20000])
+def test_verification_of_rows_at_any_alignment(V, mode):
+    """Rows of 4-byte numbers that begin anywhere within 16 bytes, the draft's elsewhere than the target's; what lies before
+    and behind them is NaN."""
+    b = ngc()
+    for seed, (a, e) in enumerate([(0, 0), (1, 1), (2, 3), (3, 0), (0, 2)]):
+        tokens, par, p, q_d, u = draft_case(2, 6, V, "tree", mode, seed)
+        ref = draft.verify_draft(tokens, par, p, u, q_d, greedy=mode == "greedy")
+
+        def shifted(x, off):
+            if x is None:
+                return None
+            whole = torch.full((x.size + 8,), float("nan"), device="cuda")
+            whole[off:off + x.size] = torch.as_tensor(x).cuda().view(-1)
+            return whole[off:off + x.size].view(x.shape)
+        res = [torch.empty(s, dtype=torch.int32, device="cuda") for s in ((2, 6), (2,), (2,))]
+        st = b.new_status()
+        b.ngc_verify_draft(torch.as_tensor(tokens).cuda(), torch.as_tensor(par).cuda(), shifted(p, a), torch.as_tensor(u).cuda(), *res,
+                           shifted(q_d, e), greedy=int(mode == "greedy"), status=st)
+        assert status_value(st) == 0 and not ref[3].any()
+        for x, r in zip(res, ref):
+            assert np.array_equal(x.cpu().numpy(), r)
+
+
 # ------------------------------------------------------------------ two calls at once
 
 def test_calls_on_two_streams_at_once():
