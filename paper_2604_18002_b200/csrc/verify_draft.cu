@@ -4,8 +4,7 @@
 // the slice.  All CTAs take the same walk from the same numbers, so only sums over the vocabulary are exchanged: each
 // warp writes its own into the shared memory of all CTAs, one cluster barrier later everyone adds them in one order.
 //
-// Nodes are numbered with parents before children, so one ascending sweep over the nodes visits the children of
-// the current node in index order.  What a test needs of the big rows, p(x) and q(x) at the parent, is fetched for
+// The children of the current node are a ballot over the parents that the lanes of each warp hold.  What a test needs of the big rows, p(x) and q(x) at the parent, is fetched for
 // all nodes at once before the walk: the walk itself reads shared memory only.  With draft rows, k rejections at
 // a node leave w = max(p - c q, 0): the max of nested subtractions of non-negative multiples of q is the subtraction
 // of their sum, so one number c stands for the whole residual and nothing is stored.  The sum after a rejection
@@ -15,9 +14,11 @@
 // fused multiply-add), so that the arithmetic is the one written down.  The final draw is an inverse CDF: the sums
 // per CTA and per warp lead to a range of 1 / 64 of a large vocabulary, which the CTA that owns it scans.
 //
-// What bounds it: a rejection is a pass over two rows that waits for the one before.  One sequence, 131072 tokens: 9.6 us
-// with none (launch, tree, one pass, draw), then 2.2 us each.  64 sequences: 15 us with none (a row each, 34 MB), 31 us
-// with up to five, whose rows come from L2 after the first time.
+// What bounds it: a rejection is a pass over two rows that waits for the one before.  One sequence, 131072 tokens: 9.3 us
+// with none (launch, tree, one pass, draw), then 1.8 us each.  64 sequences: 15 us with none (a row each, 34 MB), 31 us
+// with up to five, whose rows come from L2 after the first time.  Without draft rows there is one pass, the last: 48
+// sequences of 50001 tokens and 33 nodes take 9.8 us (19.5 us when tried tokens were a list that every thread searched for
+// every token).
 #include <cooperative_groups.h>
 
 #include "ngc_common.cuh"
@@ -31,6 +32,7 @@ namespace cg = cooperative_groups;
 enum { kModeDraft = 0, kModePoint = 1, kModeGreedy = 2 };
 constexpr int kVerifyThreads = 256, kVerifyWarps = kVerifyThreads / 32;
 constexpr int kMaxCluster = 8;
+constexpr int kWords = NGC_TREE_MAX_NODES / 32;
 constexpr int kUnroll = 4;                           // 16-byte loads a lane has in flight per row
 
 struct VerifyParams {
@@ -48,7 +50,7 @@ struct VerifyParams {
 };
 
 struct VerifyShared {
-  int parent[NGC_TREE_MAX_NODES], token[NGC_TREE_MAX_NODES], path[NGC_TREE_MAX_NODES], tried[NGC_TREE_MAX_NODES];
+  int parent[NGC_TREE_MAX_NODES], token[NGC_TREE_MAX_NODES], path[NGC_TREE_MAX_NODES];
   float u[NGC_TREE_MAX_NODES], p[NGC_TREE_MAX_NODES], q[NGC_TREE_MAX_NODES];     // p, q: of the node's token, at its parent
   double scan[kVerifyWarps];
   float warp_max[kVerifyWarps];
@@ -64,22 +66,43 @@ struct VerifyShared {
 template <int MODE> struct Residual {
   const float* p;
   const float* q;
-  const int* tried;
-  double c;
-  int n_tried;
-  __device__ __forceinline__ double of(int x, float pv, float qv) const {
+  const int* token;                                  // of the nodes
+  double c;                                          // with draft rows
+  uint32_t tried[kWords];                            // without: children whose token has no mass left
+  // of a token that has not been tried
+  __device__ __forceinline__ double of(float pv, float qv) const {
     const double w = (double)pv;
-    if constexpr (MODE == kModeDraft) {
-      const double rest = __dsub_rn(w, __dmul_rn(c, (double)qv));
-      return rest < 0.0 ? 0.0 : rest;                // a NaN stays one
-    } else {
-      for (int e = 0; e < n_tried; ++e)
-        if (tried[e] == x) return 0.0;
-      return w;
-    }
+    if constexpr (MODE != kModeDraft) return w;
+    const double rest = __dsub_rn(w, __dmul_rn(c, (double)qv));
+    return rest < 0.0 ? 0.0 : rest;                  // a NaN stays one
   }
   __device__ __forceinline__ bool with_q() const { return MODE == kModeDraft && c != 0.0; }
-  __device__ __forceinline__ double at(int x) const { return of(x, p[x], with_q() ? q[x] : 0.f); }
+  // f(token) for all tried ones
+  template <typename F> __device__ __forceinline__ void for_tried(F f) const {
+    if constexpr (MODE == kModePoint) {
+#pragma unroll
+      for (int k = 0; k < kWords; ++k)
+        for (uint32_t bits = tried[k]; bits; bits &= bits - 1) f(token[32 * k + __ffs(bits) - 1]);
+    }
+  }
+  // the same as far as tokens [lo, hi) are concerned: hardly any of them has been tried (whole warp)
+  __device__ __forceinline__ Residual within(int lo, int hi) const {
+    Residual r = *this;
+    if constexpr (MODE == kModePoint) {
+#pragma unroll
+      for (int k = 0; k < kWords; ++k)
+        if (tried[k]) {
+          const int x = tried[k] >> (threadIdx.x & 31) & 1u ? token[32 * k + (threadIdx.x & 31)] : -1;
+          r.tried[k] = __ballot_sync(0xffffffffu, x >= lo && x < hi);
+        }
+    }
+    return r;
+  }
+  __device__ __forceinline__ double at(int x) const {
+    float pv = p[x];
+    for_tried([&](int y) { if (x == y) pv = 0.f; });
+    return of(pv, with_q() ? q[x] : 0.f);
+  }
 };
 
 // Four tokens of a row from x0 on, with `fill` in place of those outside [lo, hi).  One load where `vec` says that x0 is
@@ -97,7 +120,8 @@ __device__ __forceinline__ float4 load4(const float* row, int x0, int lo, int hi
 __device__ __forceinline__ int row_phase(const float* row) { return (int)((uintptr_t)row >> 2) & 3; }
 
 // Sum over this warp's range.
-template <int MODE> __device__ __forceinline__ double range_sum(const Residual<MODE>& w, int lo, int hi) {
+template <int MODE> __device__ __forceinline__ double range_sum(const Residual<MODE>& all, int lo, int hi) {
+  const Residual<MODE> w = all.within(lo, hi);
   const int lane = threadIdx.x & 31, phase = row_phase(w.p);
   const bool with_q = w.with_q(), q_vec = with_q && row_phase(w.q) == phase;
   double s[4] = {0.0, 0.0, 0.0, 0.0};
@@ -108,20 +132,29 @@ template <int MODE> __device__ __forceinline__ double range_sum(const Residual<M
       pv[e] = load4(w.p, x0 + 128 * e, lo, hi, true, 0.f);
       qv[e] = with_q ? load4(w.q, x0 + 128 * e, lo, hi, q_vec, 0.f) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
+    w.for_tried([&](int y) {
+#pragma unroll
+      for (int e = 0; e < kUnroll; ++e) {
+        const int c = y - (x0 + 128 * e);
+        if (c == 0) pv[e].x = 0.f;
+        if (c == 1) pv[e].y = 0.f;
+        if (c == 2) pv[e].z = 0.f;
+        if (c == 3) pv[e].w = 0.f;
+      }
+    });
 #pragma unroll
     for (int e = 0; e < kUnroll; ++e) {
-      const int x = x0 + 128 * e;
-      s[0] += w.of(x, pv[e].x, qv[e].x);
-      s[1] += w.of(x + 1, pv[e].y, qv[e].y);
-      s[2] += w.of(x + 2, pv[e].z, qv[e].z);
-      s[3] += w.of(x + 3, pv[e].w, qv[e].w);
+      s[0] += w.of(pv[e].x, qv[e].x);
+      s[1] += w.of(pv[e].y, qv[e].y);
+      s[2] += w.of(pv[e].z, qv[e].z);
+      s[3] += w.of(pv[e].w, qv[e].w);
     }
   }
   return warp_sum((s[0] + s[1]) + (s[2] + s[3]));
 }
 
-template <int MODE>
-__global__ void __launch_bounds__(kVerifyThreads, 4) verify_draft_kernel(VerifyParams p) {
+template <int MODE, int kCtasSm>
+__global__ void __launch_bounds__(kVerifyThreads, kCtasSm) verify_draft_kernel(VerifyParams p) {
   __shared__ VerifyShared sh;
   const cg::cluster_group cluster = cg::this_cluster();
   const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -223,21 +256,42 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_draft_kernel(VerifyP
   int n_path = 0, next = -1;
   bool draws = false;                                // this CTA holds the token of the final draw
   if (status == NGC_DEV_OK && n > 0) {
-    int cur = 0;
     double mass = 1.0;
     bool summed = false;                             // mass is the sum of w as it stands, its shares are in shared memory
-    Residual<MODE> w = {p.target + row0, MODE == kModeDraft ? p.draft + row0 : nullptr, sh.tried, 0.0, 0};
+    Residual<MODE> w = {p.target + row0, MODE == kModeDraft ? p.draft + row0 : nullptr, sh.token, 0.0, {}};
+    // parents and tokens of the nodes, spread over the lanes: children and tokens are found by ballots
+    int par[kWords], tok[kWords];
+    uint32_t kids[kWords];                           // children of the current node that have not been tested
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) {
+      par[k] = lane + 32 * k < n ? sh.parent[lane + 32 * k] : -2;
+      tok[k] = MODE == kModePoint && lane + 32 * k < n ? sh.token[lane + 32 * k] : -1;
+      kids[k] = 32 * k < n ? __ballot_sync(0xffffffffu, par[k] == 0) : 0u;
+    }
     int best = MODE == kModeGreedy ? row_argmax(w.p) : 0;
     if (tid == 0) sh.path[0] = 0;
     n_path = 1;
-    for (int i = 1; i < n && status == NGC_DEV_OK && best >= 0; ++i) {
-      if (sh.parent[i] != cur) continue;
+    while (status == NGC_DEV_OK && best >= 0) {
+      int i = 0;
+#pragma unroll
+      for (int k = 0; k < kWords; ++k)
+        if (i == 0 && kids[k]) {
+          i = 32 * k + __ffs(kids[k]) - 1;
+          kids[k] &= kids[k] - 1;
+        }
+      if (i == 0) break;
       const int x = sh.token[i];
       bool ok;
       if (MODE == kModeGreedy) {
         ok = x == best;
       } else {
-        const double wx = w.of(x, sh.p[i], MODE == kModeDraft ? sh.q[i] : 0.f), u = (double)sh.u[i];
+        uint32_t again = 0;                          // children with the same token that were tried before
+        if constexpr (MODE == kModePoint) {
+#pragma unroll
+          for (int k = 0; k < kWords; ++k)
+            if (w.tried[k]) again |= __ballot_sync(0xffffffffu, tok[k] == x) & w.tried[k];
+        }
+        const double wx = again ? 0.0 : w.of(sh.p[i], MODE == kModeDraft ? sh.q[i] : 0.f), u = (double)sh.u[i];
         ok = MODE == kModeDraft ? __dmul_rn(__dmul_rn(u, (double)sh.q[i]), mass) < wx : __dmul_rn(u, mass) < wx;
         if (!ok && MODE == kModeDraft) {
           const double c = w.c;
@@ -251,21 +305,22 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_draft_kernel(VerifyP
           const double rest = __dsub_rn(mass, wx);
           if (rest > 0.0) {
             mass = rest;
-            __syncthreads();                         // (reads of the list by w.of above are done)
-            if (tid == 0) sh.tried[w.n_tried] = x;
-            __syncthreads();
-            ++w.n_tried;
+#pragma unroll
+            for (int k = 0; k < kWords; ++k) w.tried[k] |= i >> 5 == k ? 1u << (i & 31) : 0u;
           }
         }
       }
       if (ok) {
-        cur = i;
         if (tid == 0) sh.path[n_path] = i;
         ++n_path;
         w.p = p.target + row0 + (int64_t)i * p.vocab;
         if (MODE == kModeDraft) w.q = p.draft + row0 + (int64_t)i * p.vocab;
         w.c = 0.0;
-        w.n_tried = 0;
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) {
+          w.tried[k] = 0;
+          kids[k] = 32 * k < n ? __ballot_sync(0xffffffffu, par[k] == i) : 0u;
+        }
         mass = 1.0;
         summed = false;
         if (MODE == kModeGreedy) best = row_argmax(w.p);
@@ -312,10 +367,11 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_draft_kernel(VerifyP
           const int r_lo = min(cta_hi, cta_lo + range * per_warp), r_hi = min(cta_hi, r_lo + per_warp);
           const int run = (per_warp + kVerifyThreads - 1) / kVerifyThreads;
           const int x0 = min(r_hi, r_lo + tid * run), x1 = min(r_hi, x0 + run);
+          const Residual<MODE> part = w.within(r_lo, r_hi);
           double s = 0.0;
           int tail = -1;
           for (int x = x0; x < x1; ++x) {
-            const double wx = w.at(x);
+            const double wx = part.at(x);
             s += wx;
             if (wx > 0.0) tail = x;
           }
@@ -334,7 +390,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_draft_kernel(VerifyP
           int hit = -1;
           if (upto + s > t)
             for (int x = x0; x < x1 && hit < 0; ++x) {
-              upto += w.at(x);
+              upto += part.at(x);
               if (upto > t) hit = x;
             }
           if (hit >= 0) atomicMin(&sh.warp_arg[0], hit);
@@ -372,17 +428,21 @@ extern "C" int ngc_verify_draft(const int32_t* tokens, const int32_t* parent, co
     return NGC_ERR_INVALID_ARG;
   if (N > NGC_TREE_MAX_NODES || vocab > 1 << 30) return NGC_ERR_UNSUPPORTED;      // (indices a round ahead stay in 32 bits)
   const VerifyParams p = {tokens, parent, n_nodes, target_probs, draft_probs, uniforms, path, n_path, next_token, dev_status, N, vocab};
-  // CTAs per sequence: a slice of at least 2048 tokens each, at most 8, and no more than one round of CTAs in all: a
-  // sequence that rejects many children takes many passes, which others should not queue behind.  256 threads each: with
-  // 512 a pass over 131072 tokens of one sequence is shorter (4 rejections: 16.7 instead of 18.5 us), the rest longer (no
-  // rejection, 37 sequences: 21.4 and 14.4 us; 64 sequences of 16 drafted tokens: 38.6 and 31.0 us).
+  // CTAs per sequence: a slice of at least 2048 tokens each, at most 8, and no more than one round of CTAs in all (four fit
+  // an SM): a sequence that rejects many children takes many passes, which others should not queue behind.  256 threads each:
+  // with 512 a sequence that rejects nothing takes longer (37 sequences: 21.4 instead of 14.4 us).
   int cluster = vocab / 2048;
   if (cluster > 4 * 148 / B) cluster = 4 * 148 / B;
   if (cluster > kMaxCluster) cluster = kMaxCluster;
   if (cluster < 1) cluster = 1;
   if ((int64_t)B * cluster > 0x7fffffffLL) return NGC_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)(B * cluster)), block(kVerifyThreads);
-  auto kernel = greedy ? verify_draft_kernel<kModeGreedy> : draft_probs ? verify_draft_kernel<kModeDraft> : verify_draft_kernel<kModePoint>;
+  // With draft rows a thread has use for more registers than four CTAs per SM leave it (4 rejections, 131072 tokens, one
+  // sequence: 18.5 us with 64 registers, 16.5 us with 80); where three per SM do not hold all CTAs at once, four are
+  // better (64 sequences without a rejection: 21.2 us with three, 15.3 us with four).
+  const bool three = (int64_t)B * cluster <= 3 * 148;
+  auto kernel = greedy ? verify_draft_kernel<kModeGreedy, 4> : !draft_probs ? verify_draft_kernel<kModePoint, 4>
+              : three  ? verify_draft_kernel<kModeDraft, 3> : verify_draft_kernel<kModeDraft, 4>;
   NGC_CUDA_TRY(launch_pdl_cluster(kernel, grid, block, (unsigned)cluster, (cudaStream_t)stream, p));
   return NGC_OK;
 }
