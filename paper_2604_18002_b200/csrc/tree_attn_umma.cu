@@ -14,9 +14,8 @@
 //   producer warps   one for Q (once per unit) and K, one for V, by tiled TMA (128-byte swizzle), K and V each in a ring
 //                    of its own (K is free as soon as S is computed, V only after P V).  Issuing a load takes a warp
 //                    some 150 cycles, so a whole tile of a contiguous cache is ONE load (the groups of 64 channels are a
-//                    dimension of the tensor map); pages are a load per 64 channels, the partly filled last tile of the
-//                    cache and the tree tiles come in 16-row boxes.  Page-table entries are fetched 32 at a time, a
-//                    batch ahead;
+//                    dimension of the tensor map); pages are a load per 64 channels, the tree's rows come in
+//                    16-row boxes.  Page-table entries are fetched 32 at a time, a batch ahead;
 //   MMA warp         S = Q K^T into tensor memory, O += P V with P read from tensor memory;
 //   mask warp        the ancestor sets of the next unit's tree, by pointer doubling;
 //   softmax warps    (4 MT) one thread per row: mask (in tree tiles, its node's ancestors; in the cache's last tile a common
@@ -70,9 +69,9 @@ template <int D, int MT, int CT> struct Cfg {
   static constexpr uint32_t kCols = MT == 1 ? 256 : 512;
 };
 
-// Tensor maps of a launch.  K and V: whole tiles (contiguous caches, all channels in one box) or pages, and 16 rows; the
-// tree's K and V (16 rows, a plane per strip); Q (128 rows).
-struct KvMaps { CUtensorMap whole, part, tree; };
+// Tensor maps of a launch.  K and V: whole tiles (contiguous caches, all channels in one box) or pages; the tree's K and V
+// (16 rows, a plane per strip); Q (128 rows).
+struct KvMaps { CUtensorMap cache, tree; };
 struct Maps { KvMaps k, v; CUtensorMap q; };
 
 // A unit and where it begins on the line.
@@ -224,46 +223,42 @@ struct PageWalk {
   }
 };
 
-// Issues the loads of K or V tile t (whole warp; one lane issues).  Rows that are not loaded keep old bytes: their scores
-// are masked and P V stops before them.
+// Issues the loads of K or V tile t (whole warp; one lane issues).  The cache's last tile or page is fetched whole: its dead
+// rows, and rows that are not loaded and keep old bytes, are masked and P V stops before them.
 template <int D, int KT>
 __device__ __forceinline__ void load_tile(const TreeAttnParams& p, const KvMaps& maps, PageWalk& pages, const Piece& w, int base, int t,
                                           uint8_t* dst, uint64_t* bar) {
   constexpr int kBox = KT * 128;
-  const bool in_tree = t >= w.n_ct;
-  const int live = min(KT, in_tree ? w.n - (t - w.n_ct) * KT : w.len - t * KT);
-  if (!p.page_table && !in_tree && live == KT) {
-    int y = base + t * KT;
-    if (!NGC_IN_BOUNDS(p.dev_status, y >= 0 && y + KT <= p.rows)) y = 0;
+  if (t >= w.n_ct) {
+    const int row0 = (t - w.n_ct) * KT, n16 = (min(KT, w.n - row0) + 15) >> 4;
     if (umma::elect_one()) {
-      ptx::mbar_expect_tx(bar, (uint32_t)KT * D * 2);
-      ptx::tma_load_4d(dst, &maps.whole, 0, y, 0, w.plane, bar);
+      ptx::mbar_expect_tx(bar, (uint32_t)n16 * 16 * D * 2);
+      for (int r = 0; r < 16 * n16; r += 16)
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) ptx::tma_load_3d(dst + c * kBox + r * 128, &maps.tree, 64 * c, row0 + r, w.strip, bar);
     }
     __syncwarp();
     return;
   }
-  const int n16 = (live + 15) >> 4;
-  if (umma::elect_one()) ptx::mbar_expect_tx(bar, (uint32_t)n16 * 16 * D * 2);
-  __syncwarp();
-  int r = 0;
-  if (p.page_table && !in_tree)
-    for (; r + p.page <= live; r += p.page) {
-      int y = base + pages.get((t * KT + r) / p.page) * p.page;
-      if (!NGC_IN_BOUNDS(p.dev_status, y >= 0 && y + p.page <= p.rows)) y = 0;
-      if (umma::elect_one()) {
-#pragma unroll
-        for (int c = 0; c < D / 64; ++c) ptx::tma_load_3d(dst + c * kBox + r * 128, &maps.whole, 64 * c, y, w.plane, bar);
-      }
-      __syncwarp();
+  if (!p.page_table) {
+    int y = base + t * KT;                      // (beyond the plane's last row the tile is filled with zeros)
+    if (!NGC_IN_BOUNDS(p.dev_status, y >= 0 && y < p.rows)) y = 0;
+    if (umma::elect_one()) {
+      ptx::mbar_expect_tx(bar, (uint32_t)KT * D * 2);
+      ptx::tma_load_4d(dst, &maps.cache, 0, y, 0, w.plane, bar);
     }
-  for (; r < 16 * n16; r += 16) {
-    int y = in_tree ? (t - w.n_ct) * KT + r : base + t * KT + r;
-    if (!in_tree && p.page_table) y = base + pages.get((t * KT + r) / p.page) * p.page + (t * KT + r) % p.page;
-    if (!NGC_IN_BOUNDS(p.dev_status, y >= 0 && y < (in_tree ? (int64_t)p.N : p.rows))) y = 0;
+    __syncwarp();
+    return;
+  }
+  const int live = min(KT, w.len - t * KT), n_pages = (live + p.page - 1) / p.page;
+  if (umma::elect_one()) ptx::mbar_expect_tx(bar, (uint32_t)(n_pages * p.page) * D * 2);
+  __syncwarp();
+  for (int i = 0; i < n_pages; ++i) {
+    int y = base + pages.get(t * KT / p.page + i) * p.page;
+    if (!NGC_IN_BOUNDS(p.dev_status, y >= 0 && y + p.page <= p.rows)) y = 0;
     if (umma::elect_one()) {
 #pragma unroll
-      for (int c = 0; c < D / 64; ++c)
-        ptx::tma_load_3d(dst + c * kBox + r * 128, in_tree ? &maps.tree : &maps.part, 64 * c, y, in_tree ? w.strip : w.plane, bar);
+      for (int c = 0; c < D / 64; ++c) ptx::tma_load_3d(dst + c * kBox + i * p.page * 128, &maps.cache, 64 * c, y, w.plane, bar);
     }
     __syncwarp();
   }
@@ -331,8 +326,8 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     ptx::mbar_init(&sh.drain, 1);
     ptx::fence_barrier_init();
     sh.abort = 0;
-    ptx::prefetch_tensormap(&maps.k.whole);
-    ptx::prefetch_tensormap(&maps.v.whole);
+    ptx::prefetch_tensormap(&maps.k.cache);
+    ptx::prefetch_tensormap(&maps.v.cache);
     ptx::prefetch_tensormap(&maps.q);
   }
   if (warp == C::kMmaWarp) umma::tmem_alloc(&sh.tmem, C::kCols);
@@ -894,13 +889,9 @@ int launch_tree_umma(const TreeAttnParams& p, cudaStream_t stream) {
   bool ok = make_rows_map(&maps.q, p.q, q_rows, 128, p.d);
   auto kv_maps = [&](KvMaps* m, const void* cache, const void* tree) {
     ok = ok && make_kv_map(&m->tree, tree, p.N, (int)strips, 16, p.d);
-    if (p.rows == 0) {                           // a cache without rows: never read
-      m->whole = m->part = m->tree;
-      return;
-    }
-    ok = ok && make_kv_map(&m->part, cache, p.rows, planes, 16, p.d) &&
-         (p.page_table ? make_kv_map(&m->whole, cache, p.rows, planes, p.page, p.d)
-                       : make_strip_map(&m->whole, cache, p.rows, planes, tree_umma_keys(p.tiles_m), p.d));
+    if (p.rows == 0) m->cache = m->tree;         // a cache without rows: never read
+    else ok = ok && (p.page_table ? make_kv_map(&m->cache, cache, p.rows, planes, p.page, p.d)
+                                  : make_strip_map(&m->cache, cache, p.rows, planes, tree_umma_keys(p.tiles_m), p.d));
   };
   kv_maps(&maps.k, p.k, p.tree_k);
   kv_maps(&maps.v, p.v, p.tree_v);
