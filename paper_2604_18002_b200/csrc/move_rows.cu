@@ -309,7 +309,7 @@ int commit_impl(const ngc_cache* c, const PagedView& pv, const void* tree_k, con
   unsigned cluster = 1;
   while (cluster < 8 && most > (int64_t)cluster * kMoveThreads * kMoveVecs && (int64_t)c->B * cluster * 2 <= 4 * 148) cluster *= 2;
   if ((int64_t)c->B * cluster > 0x7fffffffLL || most > 0x7fffffffLL) return NGC_ERR_UNSUPPORTED;
-  NGC_CUDA_TRY(launch_pdl_cluster(commit_kernel, dim3((unsigned)c->B * cluster), dim3(kMoveThreads), cluster, stream, p));
+  NGC_CUDA_TRY(launch_pdl_cluster(commit_kernel, dim3((unsigned)c->B * cluster), dim3(kMoveThreads), cluster, 0, stream, p));
   return NGC_OK;
 }
 

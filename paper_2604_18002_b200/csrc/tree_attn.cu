@@ -24,6 +24,7 @@ namespace {
 constexpr int kKeyTile = 32;                    // keys per tile, and the split granularity
 constexpr int kSms = 148;
 constexpr int kShortTiles = 48;                 // tensor cores: key tiles up to which a unit is a short one
+constexpr int kClusterJoin = 3;                 // tensor cores: what joining in a cluster costs, in tiles
 constexpr int kSplitMin = 2;                    // tiles a split has at least
 
 __device__ __forceinline__ bool finite4(float4 x) {
@@ -305,7 +306,8 @@ struct TreePlan {
   int block_rows, blocks;       // query rows per item, blocks per KV head
   int n_split;                  // FMA path: token splits
   int tiles_m, ctas_sm;         // tensor cores: M tiles per CTA, CTAs per SM
-  int even, cut, grid, n_units; // tensor cores: tiles dealt to `grid` CTAs, units cut where that falls; or a unit per CTA
+  int even, cut, grid, n_units; // tensor cores: tiles dealt to `grid` CTAs, units cut where that falls; or
+  int cluster;                  //   a unit per cluster of so many CTAs
 };
 TreePlan tree_plan(const ngc_cache* c, int layers, int N) {
   const int rows = c->Hq / c->Hkv * N;
@@ -321,16 +323,28 @@ TreePlan tree_plan(const ngc_cache* c, int layers, int N) {
     pl.tiles_m = tiles;
     pl.ctas_sm = tiles == 1 && longest <= kShortTiles && units >= 4 * kSms ? 2 : 1;
     const int64_t slots = kSms * pl.ctas_sm;
-    // Cutting units costs a second kernel, some 8 us or join_tiles tiles, and saves what the longest unit takes beyond an
-    // equal share (lengths taken to be three quarters of the longest on average).  64 sequences of 512 / 1024 tokens: 17 / 23 us
-    // uncut, 23 / 27 us cut; one sequence of 512 tokens: 13.6 us and 15.4 us.
-    const int64_t join_tiles = tiles == 1 ? 10 : 5;
-    pl.even = units > slots || 4 * longest * slots - 3 * units * longest > 4 * join_tiles * slots;
+    // Clusters: so many CTAs per unit as make its tiles and the join shortest, as long as all clusters run at once: 14 of
+    // eight CTAs, 32 of four, 74 of two (16 of eight: 18.7 us instead of 11.0 us for 14, units of 1024 tokens).  One sequence of
+    // 512 / 1024 / 2048 tokens, 2 KV heads: 9.3 / 9.5 / 11.0 us; a CTA per unit 12.0 us, cut units 12.7 / 14.3 us.
+    pl.cluster = 1;
+    int64_t alone = longest;
+    for (int c = 2; c <= kTreeMaxCluster; c *= 2)
+      if (units <= (c == 8 ? 14 : c == 4 ? 32 : 74) && (longest + c - 1) / c + kClusterJoin < (pl.cluster > 1 ? alone + kClusterJoin : alone)) {
+        pl.cluster = c;
+        alone = (longest + c - 1) / c;
+      }
+    // Cutting units costs a second kernel, some 8 us or join_tiles tiles, and saves what a CTA's share of a unit takes beyond
+    // an equal share of all (lengths taken to be three quarters of the longest on average).  64 sequences of 1024 / 2048
+    // tokens: 21 / 34 us uncut, 27 / 41 us cut; 8 of 4096 tokens in clusters of four: 21.0 us, cut 19.4 us.
+    const int64_t join_tiles = tiles == 1 ? 12 : 5;
+    pl.even = units > slots || 4 * (alone - join_tiles) * slots > 3 * units * longest;
     pl.cut = pl.even && units < 2 * slots;
-    pl.grid = pl.n_units;
     if (pl.even) {
+      pl.cluster = 1;
       const int64_t most = units * longest / kTreeMinTiles;
       pl.grid = (int)(most < slots ? most : slots);
+    } else {
+      pl.grid = pl.n_units * pl.cluster;
     }
     return pl;
   }
@@ -380,7 +394,7 @@ int tree_impl(const ngc_cache* c, const PagedView& pv, const void* q, const void
   p.G = lists_G(pv.lists, c->L, c->Hkv); p.lens_lists = c->lens_lists;
   const TreePlan plan = tree_plan(c, p.n_layers, N);
   p.row_blocks = plan.blocks; p.n_split = plan.n_split; p.block_rows = plan.block_rows;
-  p.tiles_m = plan.tiles_m; p.ctas_sm = plan.ctas_sm; p.even = plan.even; p.cut = plan.cut; p.grid = plan.grid; p.n_units = plan.n_units; p.plan = nullptr;
+  p.tiles_m = plan.tiles_m; p.ctas_sm = plan.ctas_sm; p.even = plan.even; p.cut = plan.cut; p.cluster = plan.cluster; p.grid = plan.grid; p.n_units = plan.n_units; p.plan = nullptr;
   const TreeScratch need = tree_scratch(c, plan, p.n_layers, N);
   if (need.bytes > 0) {
     if (!ws || ws_bytes < need.bytes || ((uintptr_t)ws & 255)) return NGC_ERR_WORKSPACE;

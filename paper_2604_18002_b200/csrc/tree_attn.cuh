@@ -29,7 +29,7 @@ struct TreeAttnParams {
   int64_t rows;
   int L, B, Hq, Hkv, d, g, N;
   int layer_begin, n_layers, n_split, row_blocks, out_bf16;
-  int even, cut, grid, n_units, block_rows, tiles_m, ctas_sm;    // tensor cores
+  int even, cut, cluster, grid, n_units, block_rows, tiles_m, ctas_sm;    // tensor cores
   float scale_log2;             // scale * log2(e)
   const int32_t* page_table;    // [B][G][pages_cap] or null
   int page, pages_cap, lists, G;
@@ -114,6 +114,7 @@ __device__ __forceinline__ void tree_store_out4(const TreeAttnParams& p, int64_t
 // keys of a tile.
 __host__ __device__ constexpr int tree_umma_tiles(int rows) { return rows <= 128 ? 1 : 2; }
 __host__ __device__ constexpr int tree_umma_keys(int tiles) { return tiles == 1 ? 64 : 128; }
+constexpr int kTreeMaxCluster = 8;
 int launch_tree_umma(const TreeAttnParams& p, cudaStream_t stream);
 
 // Even split of `total` tiles: how many of `grid` CTAs take part (each gets at least kTreeMinTiles tiles, so `per` below is

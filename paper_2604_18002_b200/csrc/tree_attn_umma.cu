@@ -30,8 +30,9 @@
 // of beginning it) that is cut into a piece per CTA.  With many units a piece ends at the next unit's
 // beginning.  With few (fewer than two per CTA) the pieces are equal, so that rollouts of any lengths keep all SMs busy to the
 // end: a CTA then has at most two unfinished units, the one it begins in and the one it ends in; their sums go to its two
-// slots of the workspace and a second kernel joins the parts of every unit that was cut.  Where a handful of short units
-// leaves nothing to deal, a CTA takes one.
+// slots of the workspace and a second kernel joins the parts of every unit that was cut.  Where
+// that does not pay (few short units), a cluster of up to 8 CTAs takes a unit, each an equal part of its tiles, and joins the
+// parts through distributed shared memory.
 //
 // bf16 P: one rounding per weight (2^-8), as in the decode and replay calls; the row sum takes the weights
 // before it.  0 x V must be 0 whatever a dead V row holds: rows of the last 16-row box beyond the live ones are
@@ -40,6 +41,7 @@
 //
 // Every wait is bounded; a wait that runs out raises the CTA's abort flag, all roles leave, copies and MMAs
 // in flight are drained (bounded), tensor memory is freed and NGC_DEV_TIMEOUT is reported.
+#include <cooperative_groups.h>
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -49,6 +51,8 @@
 
 namespace ngc {
 namespace {
+
+namespace cg = cooperative_groups;
 
 constexpr float kLazyRescale = 8.f;             // log2 units the row maximum may grow before O is rescaled
 
@@ -65,6 +69,7 @@ template <int D, int MT, int CT> struct Cfg {
   static constexpr int kSmem = MT * kQBytes + 2 * kStages * kTile + 1024;
   // What beginning another unit costs a CTA, in tiles: the row sums leave, Q changes.
   static constexpr int kUnitCost = MT == 1 ? 4 : 5;
+  static_assert(128 * MT * D * 4 <= 2 * kStages * kTile);  // a part of a cluster lies over the rings
   static constexpr uint32_t kOCol = 128 * MT;              // S[m][buf] at 128 m + 64 buf, O[m] behind
   static constexpr uint32_t kCols = MT == 1 ? 256 : 512;
 };
@@ -88,6 +93,7 @@ template <int D, int MT, int CT> struct Shared {
   uint32_t odd[4][kTreeWords];                  // by piece & 3: nodes whose V row holds an infinity or a NaN
   uint32_t tmem;
   int abort;
+  float2 ml[128 * MT];                          // clusters: (maximum, sum) of this CTA's part of the rows
   int warp_sum[C::kThreads / 32], chunk[C::kThreads], total;         // places of the line before each thread's units
   Found found[2];
 };
@@ -126,16 +132,17 @@ template <int KT> __device__ __forceinline__ int unit_tiles(int n, int len) {
   return n > 0 ? (int)((uint32_t)(len + KT - 1) / KT + (uint32_t)(n + KT - 1) / KT) : 0;
 }
 
-// The next piece of the walk; false at its end.  (A unit per CTA: also a unit without tiles.)
+// The next piece of the walk; false at its end.  (A unit per cluster: also a piece without tiles.)
 template <int KT, int kUnitCost> __device__ __forceinline__ bool next_piece(const TreeAttnParams& p, Walk& k, Piece& w) {
   while (k.n_left > 0) {
     unit_of(p, (uint32_t)k.u, w);
     const bool fits = load_counts(p, w);
     const int nt = fits ? unit_tiles<KT>(w.n, w.len) : 0;
-    if (!p.even) {
+    if (!p.even) {                              // a unit per cluster
+      const int rank = (int)(blockIdx.x % (uint32_t)p.cluster);
       if (!fits && threadIdx.x == 0) set_dev_status(p.dev_status, w.n < 0 || w.n > p.N ? NGC_DEV_BAD_TREE : NGC_DEV_BAD_COUNTS);
-      w.lo = 0;
-      w.n_tiles = nt;
+      w.lo = nt * rank / p.cluster;
+      w.n_tiles = nt * (rank + 1) / p.cluster - w.lo;
       k.n_left = 0;
     } else {
       const int places = nt > 0 ? min(nt + kUnitCost - k.at, k.n_left) : 0;
@@ -289,6 +296,55 @@ __device__ __forceinline__ uint32_t odd_half(uint32_t x) { return (x & 0x7f80u) 
 // Bits of x (two bf16) that belong to infinities or NaN.
 __device__ __forceinline__ uint32_t odd_bits(uint32_t x) { return odd_half(x) | odd_half(x >> 16) << 16; }
 
+// (m, l) of a row of a part that has no tiles.
+#define kNoTiles make_float2(-INFINITY, -2.f)
+
+// Four channels of a row of a CTA's part, in shared memory (over the rings); rows are rotated so that neither the rows of a
+// warp nor the channels of a row meet in a bank.
+template <int D> __device__ __forceinline__ uint4* cluster_part(uint8_t* base, int row, int quad) {
+  return reinterpret_cast<uint4*>(base) + row * (D / 4) + (quad ^ (row & (D / 4 - 1)));
+}
+
+// Joins the parts of a unit that the CTAs of a cluster have in their shared memory: rows dealt out to the CTAs and their
+// warps, four channels per lane (with d = 64: two rows per warp).
+template <int D, int MT, typename Sh>
+__device__ __forceinline__ void cluster_join(const TreeAttnParams& p, Sh& sh, uint8_t* parts) {
+  constexpr int kLanes = D / 4;
+  const cg::cluster_group cluster = cg::this_cluster();
+  const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  cluster.sync();
+  Piece w;
+  unit_of(p, blockIdx.x / (uint32_t)p.cluster, w);
+  const int r0 = w.rb * MT * 128, rows = min(128 * MT, p.g * p.N - r0), quad = threadIdx.x % kLanes;
+  const int64_t row0 = (((int64_t)w.l * p.B + w.b) * p.Hq + (int64_t)w.h * p.g) * p.N + r0;
+  for (int r = rank + ctas * (threadIdx.x / kLanes); r < rows; r += ctas * (blockDim.x / kLanes)) {
+    float2 ml[kTreeMaxCluster];
+    float mg = -INFINITY;
+    bool none = false, some = false;
+#pragma unroll
+    for (int i = 0; i < kTreeMaxCluster; ++i) {
+      ml[i] = i < ctas ? *cluster.map_shared_rank(&sh.ml[r], i) : kNoTiles;
+      none = none || ml[i].y == -1.f;           // kNoPart
+      some = some || ml[i].y != -2.f;
+      mg = fmaxf(mg, ml[i].x);
+    }
+    if (none || !some) continue;
+    float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kTreeMaxCluster; ++i) {
+      if (ml[i].y == -2.f || (ml[i].x == -INFINITY && ml[i].y == 0.f)) continue;       // nothing visible in this part
+      const float f = exp2f(ml[i].x - mg);
+      const uint4 x = *cluster.map_shared_rank(cluster_part<D>(parts, r, quad), i);
+      l = fmaf(ml[i].y, f, l);
+      o[0] = fmaf(__uint_as_float(x.x), f, o[0]); o[1] = fmaf(__uint_as_float(x.y), f, o[1]);
+      o[2] = fmaf(__uint_as_float(x.z), f, o[2]); o[3] = fmaf(__uint_as_float(x.w), f, o[3]);
+    }
+    const float inv = 1.f / l;
+    tree_store_out4(p, (row0 + r) * D + 4 * quad, make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv));
+  }
+  cluster.sync();                               // nobody leaves while its part may still be read
+}
+
 template <int D, int MT, int CT>
 __global__ void __launch_bounds__(Cfg<D, MT, CT>::kThreads, CT)
 tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
@@ -338,7 +394,9 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
   ptx::grid_dep_launch();                       // from here on this CTA holds its tensor memory
   const uint32_t tmem = sh.tmem;
 
-  Walk walk = {(int)blockIdx.x, 0, 0x7fffffff, 0};
+  if (p.cluster > 1)
+    for (int i = tid; i < 128 * MT; i += NT) sh.ml[i] = kNoTiles;
+  Walk walk = {(int)(blockIdx.x / (uint32_t)p.cluster), 0, 0x7fffffff, 0};
   if (p.even) {
     const int per = (p.n_units + NT - 1) / NT, u0 = min(p.n_units, tid * per), u1 = min(p.n_units, u0 + per);
     int sum = 0;
@@ -484,9 +542,11 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     }
   } else if (warp == C::kMmaWarp) {
     // ------------------------------------------------------------------ MMA issue, one elected lane
-    // operand descriptors differ only in their low word (start address / 16)
+    // operand descriptors differ only in their low word (start address / 16, of which 14 bits: in a cluster, shared-memory
+    // addresses hold the CTA's rank above them)
+    const uint32_t k_base = (ptx::smem_u32(sK) >> 4) & 0x3fff, v_base = (ptx::smem_u32(sV) >> 4) & 0x3fff;
     const uint64_t desc_hi = (uint64_t)umma::smem_desc_sw128(0, 0, 1024) & 0xffffffff00000000ull;
-    const uint32_t q_base = (ptx::smem_u32(sQ) >> 4) | (1u << 16);
+    const uint32_t q_base = ((ptx::smem_u32(sQ) >> 4) & 0x3fff) | (1u << 16);
     const uint32_t v_lbo = (uint32_t)(C::kBox >> 4) << 16;                       // V: the next 64 channels are one box on
     int n_q = 0, done[MT];                      // tiles per M tile so far
 #pragma unroll
@@ -500,7 +560,7 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
       };
       auto issue_s = [&](int m, int i) {
         const int s = (kv + i) % ST, buf = (done[m] + i) % NB;
-        const uint32_t k_lo = ((ptx::smem_u32(sK) + s * C::kTile) >> 4) | (1u << 16);
+        const uint32_t k_lo = (k_base + (uint32_t)(s * C::kTile >> 4)) | (1u << 16);
         const uint32_t q_lo = q_base + (uint32_t)((m * C::kQBytes) >> 4);
         const uint32_t idesc = umma::instr_desc(128, 0, false) | ((uint32_t)steps_of(i) * 2) << 17;      // N = 16 per step
         if (umma::elect_one()) {
@@ -527,7 +587,7 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
       more = next_piece<KT, C::kUnitCost>(p, walk, next);
       for (int i = 0; ok && i < w.n_tiles; ++i) {
         const int s = (kv + i) % ST, steps = steps_of(i);
-        const uint32_t v_lo = ((ptx::smem_u32(sV) + s * C::kTile) >> 4) | v_lbo;
+        const uint32_t v_lo = (v_base + (uint32_t)(s * C::kTile >> 4)) | v_lbo;
         // S of the next tile: before P V of this one where S has a second buffer, else right behind it
         if (i + 1 < w.n_tiles) {
           ok = umma::warp_wait(&sh.k_full[(kv + i + 1) % ST], ((kv + i + 1) / ST) & 1, &sh.abort, p.dev_status);
@@ -572,7 +632,7 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     int tc = 0, fixes[3] = {0, 0, 0};           // tiles of this M tile so far; uses of sh.fixed
     bool ok = true, more = next_piece<KT, C::kUnitCost>(p, walk, w);
     while (ok && more) {
-      if (w.n_tiles <= 0) break;                // (a unit per CTA that has none)
+      if (w.n_tiles <= 0) break;                // (a unit per cluster: no tile of it is this CTA's)
       const int r0 = w.rb * MT * 128, seq = walk.seq, slot = seq & 3;
       Piece next;
       more = next_piece<KT, C::kUnitCost>(p, walk, next);
@@ -730,7 +790,9 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
         const bool whole = w.first && w.last;
         const int64_t pit = ((int64_t)blockIdx.x * 2 + (w.first ? 1 : 0)) * p.block_rows + (r - r0);     // in this CTA's slots
         if (refused && tid == 0) set_dev_status(p.dev_status, NGC_DEV_BAD_TREE);
-        if (!whole && r < rows) p.part_ml[pit] = live_row && !refused ? make_float2(m_use, l_run) : kNoPart;
+        const float2 ml = live_row && !refused ? make_float2(m_use, l_run) : kNoPart;
+        if (p.cluster > 1) sh.ml[r - r0] = ml;
+        else if (!whole && r < rows) p.part_ml[pit] = ml;
         if (live_warp && !refused) {
           uint32_t odd[kTreeWords];
 #pragma unroll
@@ -757,6 +819,10 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
             }
             if (!live_row) {
               // nothing to write
+            } else if (p.cluster > 1) {         // (every product of this CTA has been taken: the rings are free)
+#pragma unroll
+              for (int c = 0; c < 32; c += 4)
+                *cluster_part<D>(sK, r - r0, (c0 + c) / 4) = make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
             } else if (!whole) {
 #pragma unroll
               for (int c = 0; c < 32; c += 8) store_sector(p.part_o + pit * D + c0 + c, o + c);
@@ -788,6 +854,7 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     umma::fence_after_sync();
     umma::tmem_dealloc(tmem, C::kCols);
   }
+  if (p.cluster > 1) cluster_join<D, MT>(p, sh, sK);
 }
 
 // Joins the parts of the units that were cut.  blockIdx.x: the CTA of the main kernel that the unit began in, if one did;
@@ -867,7 +934,7 @@ template <int D, int MT, int CT> cudaError_t opt_in() {
 }
 template <int D, int MT, int CT> cudaError_t launch(const Maps& maps, const TreeAttnParams& p, cudaStream_t stream) {
   using C = Cfg<D, MT, CT>;
-  return launch_pdl(tree_umma_kernel<D, MT, CT>, dim3(p.grid), dim3(C::kThreads), C::kSmem, stream, maps, p);
+  return launch_pdl_cluster(tree_umma_kernel<D, MT, CT>, dim3(p.grid), dim3(C::kThreads), (unsigned)p.cluster, C::kSmem, stream, maps, p);
 }
 template <int D> cudaError_t launch_d(const Maps& maps, const TreeAttnParams& p, cudaStream_t stream) {
   if (p.tiles_m == 2) return launch<D, 2, 1>(maps, p, stream);

@@ -443,6 +443,6 @@ extern "C" int ngc_verify_draft(const int32_t* tokens, const int32_t* parent, co
   const bool three = (int64_t)B * cluster <= 3 * 148;
   auto kernel = greedy ? verify_draft_kernel<kModeGreedy, 4> : !draft_probs ? verify_draft_kernel<kModePoint, 4>
               : three  ? verify_draft_kernel<kModeDraft, 3> : verify_draft_kernel<kModeDraft, 4>;
-  NGC_CUDA_TRY(launch_pdl_cluster(kernel, grid, block, (unsigned)cluster, (cudaStream_t)stream, p));
+  NGC_CUDA_TRY(launch_pdl_cluster(kernel, grid, block, (unsigned)cluster, 0, (cudaStream_t)stream, p));
   return NGC_OK;
 }

@@ -19,8 +19,9 @@ pytestmark = pytest.mark.gpu
 bf16, f32 = torch.bfloat16, torch.float32
 
 CASES = [(t_draft.test_tree_attn_matches_oracle, (i,)) for i in (0, 1, 4, 5, 7, 9, 12)] + [
-    (t_draft.test_tree_attn_splits_a_long_cache, (bf16, 128, 12, 2, 64, 3001)),
-    (t_draft.test_tree_attn_splits_a_long_cache, (f32, 64, 2, 2, 40, 1500)),
+    (t_draft.test_tree_attn_splits_a_long_cache, (bf16, 128, 12, 2, 64, 3001, 1)),
+    (t_draft.test_tree_attn_splits_a_long_cache, (bf16, 128, 12, 2, 64, 12000, 2)),
+    (t_draft.test_tree_attn_splits_a_long_cache, (f32, 64, 2, 2, 40, 1500, 2)),
     (t_draft.test_tree_attn_deals_out_many_units, (128, 2, 330, 2, 2, 3, 150, 1)),
     (t_draft.test_paged_tree_attn_matches_oracle, (32, 1, True, 28, 4, 33, [96, 31])),
     (t_draft.test_paged_bad_page_entry_is_reported_and_stays_with_its_sequence, ()),
@@ -44,7 +45,7 @@ def guarded_workspace(need, extra=4096):
     return whole[:need], whole
 
 
-@pytest.mark.parametrize("Hq,N,lens", [(12, 9, [700, 33, 257]), (12, 50, [300, 64, 1]), (2, 1, [5000, 2, 90])])
+@pytest.mark.parametrize("Hq,N,lens", [(12, 9, [700, 33, 257]), (12, 50, [300, 64, 1]), (2, 1, [5000, 2, 90]), (2, 3, [13000, 70, 1])])
 def test_canaries_survive_tree_attention_commit_and_fork(Hq, N, lens):
     b = ngc()
     L, B, Hkv, d = 2, 3, 2, 128
@@ -135,6 +136,40 @@ def test_verification_of_rows_at_any_alignment(V, mode):
             assert np.array_equal(x.cpu().numpy(), r)
 
 
+CLUSTERS = [  # d, Hq, Hkv, N, lens, nodes per tree: units of at most 128 and of more rows, joined in clusters of 2, 4 and 8
+    (128, 12, 2, 1, [512], None), (128, 12, 2, 16, [1900], None), (128, 2, 2, 128, [700, 64], [128, 3]), (64, 8, 2, 12, [500, 1, 0], [12, 7, 1]),
+    (128, 12, 2, 40, [600], None), (128, 28, 4, 33, [1000, 130], [33, 0]), (64, 4, 1, 70, [900], None), (128, 16, 1, 50, [1000], [49]),
+    (128, 40, 2, 20, [257], None), (128, 1, 1, 1, [449, 0, 63, 64, 65], None)]
+
+
+@pytest.mark.parametrize("d,Hq,Hkv,N,lens,nodes", CLUSTERS)
+def test_short_units_joined_in_clusters(d, Hq, Hkv, N, lens, nodes):
+    b = ngc()
+    c, q, tk, tv, parent, n_nodes = case(bf16, d, Hq, Hkv, 1, lens, N, "tree", seed=N, n_nodes=nodes)
+    assert b.tree_attn_launches(device_cache(c), N) == 1
+    t_draft.check_tree(c, q, tk, tv, parent, n_nodes)
+    t_draft.check_tree(c, q, tk, tv, parent, n_nodes, out_dtype=bf16)
+    # a bad link and a bad length are reported and leave their sequence's rows alone, whichever CTA of the cluster meets them
+    B = len(lens)
+    bad = np.concatenate([parent, parent]), torch.cat([q, q], 1), torch.cat([tk, tk], 1), torch.cat([tv, tv], 1)
+    two = synth.make_cache(1, 2 * B, Hq, Hkv, d, bf16, list(lens) * 2, capacity=max(lens), seed=3)
+    n2 = None if nodes is None else np.concatenate([n_nodes, n_nodes])
+    good, st = run_tree(two, *bad[1:], bad[0], n2)
+    assert st == 0
+    p2 = bad[0].copy()
+    p2[B, 0] = 0
+    out, st = run_tree(two, *bad[1:], p2, n2)
+    assert st == 8 and (out[:, B] == -7).all()
+    out[:, B] = good[:, B]
+    assert torch.equal(out, good)
+    ln = two.lens.clone()
+    ln[0] = max(lens) + 1
+    out, st = run_tree(two, *bad[1:], bad[0], n2, lens=ln)
+    assert st == 1 and (out[:, 0] == -7).all()
+    out[:, 0] = good[:, 0]
+    assert torch.equal(out, good)
+
+
 # ------------------------------------------------------------------ two calls at once
 
 def test_calls_on_two_streams_at_once():
@@ -173,7 +208,8 @@ def test_calls_on_two_streams_at_once():
 
 # ------------------------------------------------------------------ edges of the number range
 
-KINDS = [(f32, 64, 5, 40), (f32, 64, 5, 3000), (f32, 128, 40, 3000), (bf16, 128, 5, 40), (bf16, 128, 5, 4000), (bf16, 128, 100, 4000), (bf16, 64, 5, 4000)]
+KINDS = [(bf16, 128, 5, 600), (bf16, 128, 100, 900), (f32, 64, 5, 40), (f32, 64, 5, 3000), (f32, 128, 40, 3000), (bf16, 128, 5, 40), (bf16, 128, 5, 4000), (bf16, 128, 100, 4000), (bf16, 64, 5, 4000),
+         (bf16, 128, 5, 14000), (bf16, 128, 100, 14000), (bf16, 64, 5, 14000)]
 
 
 @pytest.mark.parametrize("dtype,d,N,T", KINDS)      # with one part per row and with several
