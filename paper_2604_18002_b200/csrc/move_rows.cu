@@ -59,7 +59,9 @@ __device__ __forceinline__ int list_len(const MoveParams& p, int b, int gi, int 
 
 // A cluster of CTAs per sequence.  All of them check the path and the room (every list, since a sequence is committed
 // whole or not at all), copy their share of the rows, and meet at a cluster barrier: behind it nobody reads the lengths
-// any more and the first CTA writes the new ones.  One launch: for a single rollout the call is all latency.
+// any more and the first CTA writes the new ones.  One launch: for a single rollout the call is all latency (28 layers x 2
+// heads, 4 of 8 nodes: 4.5 us).  256 sequences, 7 of 16 nodes, pages of 32: 25 us, 103 MB; three rounds of dependent loads
+// (lengths, table entries, rows) stand before the stores.
 constexpr int kMoveVecs = 2;                    // vectors of K, and of V, a thread has in flight
 __global__ void __launch_bounds__(kMoveThreads) commit_kernel(MoveParams p) {
   const cg::cluster_group cluster = cg::this_cluster();
@@ -139,7 +141,8 @@ __device__ __forceinline__ void named_barrier(int id, int threads) {
 // A source strip is read once for all of its copies: bulk copies bring up to 64 KB of it into shared memory, from where
 // bulk stores write it to every destination (a lane per destination).  No data passes through registers, and a CTA
 // of one busy warp keeps 64 KB in flight.  grid.x = (strip, chunk of its rows), chunks beyond the grid's follow in turns;
-// grid.y deals the destinations out, so that one prompt's group alone fills the GPU.
+// grid.y deals the destinations out, so that one prompt's group alone fills the GPU.  Bound by DRAM writes: 4 prompts of 900
+// to 1100 tokens to 16 sequences each, 28 layers x 2 heads, 1.8 GB: 330 us, 5.5 TB/s; a prompt of 350 to 8, paged: 19 us.
 constexpr int kForkThreads = 128;
 constexpr int kForkQuarter = 16384, kForkChunk = 4 * kForkQuarter;     // bytes
 constexpr int kForkMaxB = 65536;

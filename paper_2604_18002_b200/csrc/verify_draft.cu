@@ -4,11 +4,12 @@
 // the slice.  All CTAs take the same walk from the same numbers, so only sums over the vocabulary are exchanged: each
 // warp writes its own into the shared memory of all CTAs, one cluster barrier later everyone adds them in one order.
 //
-// The children of the current node are a ballot over the parents that the lanes of each warp hold.  What a test needs of the big rows, p(x) and q(x) at the parent, is fetched for
-// all nodes at once before the walk: the walk itself reads shared memory only.  With draft rows, k rejections at
-// a node leave w = max(p - c q, 0): the max of nested subtractions of non-negative multiples of q is the subtraction
-// of their sum, so one number c stands for the whole residual and nothing is stored.  The sum after a rejection
-// is also the one that the final draw needs; a vocabulary row is read again only if a second child is rejected.
+// The children of the current node are a ballot over the parents that the lanes of each warp hold.  What a test needs of
+// the big rows, p(x) and q(x) at the parent, is fetched for all nodes at once before the walk: the walk itself reads shared
+// memory only.  With draft rows, k rejections at a node leave w = max(p - c q, 0): the max of nested subtractions of
+// non-negative multiples of q is the subtraction of their sum, so one number c stands for the whole residual and nothing is
+// stored.  The sum after a rejection is also the one that the final draw needs; a vocabulary row is read again only if a
+// second child is rejected.
 //
 // All decisions and sums are in fp64 (fp32 inputs are exact in it); multiplications and subtractions are kept apart (no
 // fused multiply-add), so that the arithmetic is the one written down.  The final draw is an inverse CDF: the sums
