@@ -65,10 +65,13 @@ constexpr float kLazyRescale = 8.f;             // log2 units the row maximum ma
 template <int D, int MT, int CT> struct Cfg {
   static constexpr int kKeys = tree_umma_keys(MT);         // keys per tile
   static constexpr int kBufs = MT == 1 ? 2 : 1;            // S buffers per M tile
+  static constexpr int kSplit = MT == 1 && CT == 1 ? 2 : 1;                     // softmax groups that take turns at an M tile's key tiles
+  static constexpr int kAhead = kBufs * kSplit;            // tiles whose S an M tile has room for
   static constexpr int kHalves = kKeys / 64;               // P is handed over 64 keys at a time
+  static constexpr int kGroups = MT * kSplit;              // softmax groups: 128 threads, S buffers and O of their own
   static constexpr int kStages = (MT == 1 && CT == 1 ? 5 : 2) * (128 / D);      // of K and of V
-  static constexpr int kThreads = (4 * MT + 4) * 32;
-  static constexpr int kMmaWarp = 4 * MT, kMaskWarp = 4 * MT + 1, kProducerWarp = 4 * MT + 2;      // K and Q; V in the warp behind
+  static constexpr int kThreads = (4 * kGroups + 4) * 32;
+  static constexpr int kMmaWarp = 4 * kGroups, kMaskWarp = kMmaWarp + 1, kProducerWarp = kMmaWarp + 2;      // K and Q; V in the warp behind
   static constexpr int kBox = kKeys * 128;                 // a tile's 64 channels
   static constexpr int kTile = kKeys * D * 2;              // K or V tile
   static constexpr int kQBytes = 128 * D * 2;              // Q of an M tile
@@ -76,8 +79,8 @@ template <int D, int MT, int CT> struct Cfg {
   // What beginning another unit costs a CTA, in tiles: the row sums leave, Q changes.
   static constexpr int kUnitCost = MT == 1 ? 4 : 5;
   static_assert(128 * MT * D * 4 <= 2 * kStages * kTile);  // a part of a cluster lies over the rings
-  static constexpr uint32_t kOCol = 128 * MT;              // S[m][buf] at 128 m + 64 buf, O[m] behind
-  static constexpr uint32_t kCols = MT == 1 ? 256 : 512;
+  static constexpr uint32_t kOCol = 128 * kGroups;         // S[group][buf] at 128 group + 64 buf, O[group] behind
+  static constexpr uint32_t kCols = 256 * kGroups;
 };
 
 // Tensor maps of a launch.  K and V: whole tiles (contiguous caches, all channels in one box) or pages; the tree's K and V
@@ -91,7 +94,9 @@ struct Found { int u, base, places; };
 template <int D, int MT, int CT> struct Shared {
   using C = Cfg<D, MT, CT>;
   uint64_t k_full[C::kStages], k_empty[C::kStages], v_full[C::kStages], v_empty[C::kStages];
-  uint64_t s_full[MT][C::kBufs], p_full[MT][C::kBufs][C::kHalves], o_done[MT][C::kBufs];
+  uint64_t s_full[C::kGroups][C::kBufs], p_full[C::kGroups][C::kBufs][C::kHalves], o_done[C::kGroups][C::kBufs];
+  uint64_t sums_full, sums_empty;               // two groups per M tile: the rows' (maximum, sum) in `sums`; O has been read
+  float2 sums[C::kSplit][128];
   uint64_t q_full, q_empty, masks_full[2], masks_empty[2], fixed[3], drain;
   // by piece & 1: ancestor-or-self sets of the nodes, and whether the links are none
   alignas(16) uint32_t anc[2][kTreeMaxNodes][kTreeWords];
@@ -355,7 +360,7 @@ template <int D, int MT, int CT>
 __global__ void __launch_bounds__(Cfg<D, MT, CT>::kThreads, CT)
 tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
   using C = Cfg<D, MT, CT>;
-  constexpr int ST = C::kStages, NT = C::kThreads, KT = C::kKeys, NB = C::kBufs, NH = C::kHalves;
+  constexpr int ST = C::kStages, NT = C::kThreads, KT = C::kKeys, NB = C::kBufs, NH = C::kHalves, SP = C::kSplit;
   extern __shared__ uint8_t smem_dyn[];
   __shared__ Shared<D, MT, CT> sh;
   uint8_t* sQ = (uint8_t*)(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);     // [MT][128 rows]
@@ -371,7 +376,7 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
       ptx::mbar_init(&sh.k_empty[s], 1); ptx::mbar_init(&sh.v_empty[s], 1);
     }
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < C::kGroups; ++m)
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
         ptx::mbar_init(&sh.s_full[m][i], 1);
@@ -382,9 +387,11 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     ptx::mbar_init(&sh.q_full, 1);
     ptx::mbar_init(&sh.q_empty, 1);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) { ptx::mbar_init(&sh.masks_full[i], 32); ptx::mbar_init(&sh.masks_empty[i], 128 * MT); }
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(&sh.masks_full[i], 32); ptx::mbar_init(&sh.masks_empty[i], 128 * C::kGroups); }
 #pragma unroll
     for (int i = 0; i < 3; ++i) ptx::mbar_init(&sh.fixed[i], 128);
+    ptx::mbar_init(&sh.sums_full, 128 * C::kGroups);
+    ptx::mbar_init(&sh.sums_empty, 128 * C::kGroups);
     ptx::mbar_init(&sh.drain, 1);
     ptx::fence_barrier_init();
     sh.abort = 0;
@@ -547,95 +554,105 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
       ptx::mbar_arrive(&sh.masks_full[slot]);
     }
   } else if (warp == C::kMmaWarp) {
-    // ------------------------------------------------------------------ MMA issue, one elected lane
-    // operand descriptors differ only in their low word (start address / 16, of which 14 bits: in a cluster, shared-memory
-    // addresses hold the CTA's rank above them)
-    const uint32_t k_base = (ptx::smem_u32(sK) >> 4) & 0x3fff, v_base = (ptx::smem_u32(sV) >> 4) & 0x3fff;
-    const uint64_t desc_hi = (uint64_t)umma::smem_desc_sw128(0, 0, 1024) & 0xffffffff00000000ull;
-    const uint32_t q_base = ((ptx::smem_u32(sQ) >> 4) & 0x3fff) | (1u << 16);
-    const uint32_t v_lbo = (uint32_t)(C::kBox >> 4) << 16;                       // V: the next 64 channels are one box on
-    int n_q = 0, done[MT];                      // tiles per M tile so far
+    // ------------------------------------------------------------------ MMA issue
+    // One thread does it all: a wait of the whole warp takes about 150 cycles even if it is over, and the tensor pipe runs dry
+    // meanwhile (64 sequences of 2048 tokens: 28.5 us, 34 us with the warp at it).
+    if (umma::elect_one()) {
+      // Operand descriptors differ only in their low word (start address / 16, of which 14 bits: in a cluster, shared-memory
+      // addresses hold the CTA's rank above them).
+      const uint64_t desc_hi = (uint64_t)umma::smem_desc_sw128(0, 0, 1024) & 0xffffffff00000000ull;
+      const uint32_t q_base = ((ptx::smem_u32(sQ) >> 4) & 0x3fff) | (1u << 16);
+      const uint32_t k_base = (ptx::smem_u32(sK) >> 4) & 0x3fff, v_base = (ptx::smem_u32(sV) >> 4) & 0x3fff;
+      const uint32_t v_lbo = (uint32_t)(C::kBox >> 4) << 16;                     // V: the next 64 channels are one box on
+      int n_q = 0, done[C::kGroups];            // tiles per softmax group so far
+      int k_at = 0, k_ph = 0, v_at = 0, v_ph = 0;           // stages of the next K and V tile, and their barriers' phases
 #pragma unroll
-    for (int m = 0; m < MT; ++m) done[m] = 0;
-    bool ok = true, more = next_piece<KT, C::kUnitCost>(p, walk, w);
-    for (Piece next; ok && more && w.n_tiles > 0; w = next) {
-      const int tiles_m = min(MT, (rows - w.rb * MT * 128 + 127) >> 7);          // M tiles that have a row
-      auto steps_of = [&](int i) {              // 16-key steps of tile i that hold a live key
-        const int t = w.lo + i;
-        return min(KT / 16, (int)((t < w.n_ct ? w.len - t * KT : w.n - (t - w.n_ct) * KT) + 15) >> 4);
-      };
-      auto issue_s = [&](int m, int i) {
-        const int s = (kv + i) % ST, buf = (done[m] + i) % NB;
-        const uint32_t k_lo = (k_base + (uint32_t)(s * C::kTile >> 4)) | (1u << 16);
-        const uint32_t q_lo = q_base + (uint32_t)((m * C::kQBytes) >> 4);
-        const uint32_t idesc = umma::instr_desc(128, 0, false) | ((uint32_t)steps_of(i) * 2) << 17;      // N = 16 per step
-        if (umma::elect_one()) {
+      for (int g = 0; g < C::kGroups; ++g) done[g] = 0;
+      auto wait = [&](uint64_t* bar, int phase) { return umma::wait_or_abort(bar, phase, &sh.abort, p.dev_status); };
+      bool ok = true, more = next_piece<KT, C::kUnitCost>(p, walk, w);
+      for (Piece next; ok && more && w.n_tiles > 0; w = next) {
+        const int tiles_m = min(MT, (rows - w.rb * MT * 128 + 127) >> 7);        // M tiles that have a row
+        auto steps_of = [&](int i) {            // 16-key steps of tile i that hold a live key
+          const int t = w.lo + i;
+          return min(KT / 16, (int)((t < w.n_ct ? w.len - t * KT : w.n - (t - w.n_ct) * KT) + 15) >> 4);
+        };
+        // softmax group of tile i of M tile m, and the tile's place in the group's order
+        auto group_of = [&](int m, int i) { return SP == 2 ? i & 1 : m; };
+        auto place_of = [&](int m, int i) { return SP == 2 ? (i & 1 ? done[C::kGroups - 1] : done[0]) + (i >> 1) : done[m] + i; };
+        // S of tile i, from the next K stage
+        auto issue_s = [&](int m, int i) {
+          const int grp = group_of(m, i), buf = place_of(m, i) % NB;
+          const uint32_t k_lo = (k_base + (uint32_t)(k_at * C::kTile >> 4)) | (1u << 16);
+          const uint32_t q_lo = q_base + (uint32_t)((m * C::kQBytes) >> 4);
+          const uint32_t idesc = umma::instr_desc(128, 0, false) | ((uint32_t)steps_of(i) * 2) << 17;    // N = 16 per step
 #pragma unroll
           for (int ks = 0; ks < D / 16; ++ks) {
             const uint64_t a = desc_hi | (uint64_t)(q_lo + (uint32_t)(((ks >> 2) * (128 * 128) + (ks & 3) * 32) >> 4));
             const uint64_t bd = desc_hi | (uint64_t)(k_lo + (uint32_t)(((ks >> 2) * C::kBox + (ks & 3) * 32) >> 4));
-            umma::mma_bf16(tmem + (uint32_t)(128 * m + 64 * buf), a, bd, idesc, ks > 0);
+            umma::mma_bf16(tmem + (uint32_t)(128 * grp + 64 * buf), a, bd, idesc, ks > 0);
           }
-          umma::commit(&sh.s_full[m][buf]);
+          umma::commit(&sh.s_full[grp][buf]);
           if (m + 1 == tiles_m) {
-            umma::commit(&sh.k_empty[s]);
+            umma::commit(&sh.k_empty[k_at]);
             if (i + 1 == w.n_tiles) umma::commit(&sh.q_empty);
           }
-        }
-        __syncwarp();
-      };
-      ok = umma::warp_wait(&sh.q_full, n_q & 1, &sh.abort, p.dev_status) &&
-           umma::warp_wait(&sh.k_full[kv % ST], (kv / ST) & 1, &sh.abort, p.dev_status);
-      ++n_q;
-      // (the S buffers: P of the tile that used one before was consumed by a product issued before, and the pipe runs them
-      // in issue order)
-      for (int m = 0; ok && m < tiles_m; ++m) issue_s(m, 0);
-      more = next_piece<KT, C::kUnitCost>(p, walk, next);
-      for (int i = 0; ok && i < w.n_tiles; ++i) {
-        const int s = (kv + i) % ST, steps = steps_of(i);
-        const uint32_t v_lo = (v_base + (uint32_t)(s * C::kTile >> 4)) | v_lbo;
-        // S of the next tile: before P V of this one where S has a second buffer, else right behind it
-        if (i + 1 < w.n_tiles) {
-          ok = umma::warp_wait(&sh.k_full[(kv + i + 1) % ST], ((kv + i + 1) / ST) & 1, &sh.abort, p.dev_status);
+        };
+        auto k_used = [&]() { if (++k_at == ST) { k_at = 0; k_ph ^= 1; } };
+        // S into all buffers.  (P of the tile that used one before was consumed by a product issued before, and the pipe runs
+        // them in issue order.)
+        ok = wait(&sh.q_full, n_q & 1);
+        ++n_q;
+        for (int i = 0; ok && i < min(C::kAhead, w.n_tiles); ++i) {
+          ok = wait(&sh.k_full[k_at], k_ph);
           if (!ok) break;
-          if (NB == 2) issue_s(0, i + 1);
+          for (int m = 0; m < tiles_m; ++m) issue_s(m, i);
+          k_used();
         }
-        ok = umma::warp_wait(&sh.v_full[s], ((kv + i) / ST) & 1, &sh.abort, p.dev_status);
-        for (int m = 0; ok && m < tiles_m; ++m) {
-          const int buf = (done[m] + i) % NB;
-          const uint32_t ph = ((done[m] + i) / NB) & 1, o_tmem = tmem + C::kOCol + (uint32_t)(D * m);
-          const uint32_t p_tmem = tmem + (uint32_t)(128 * m + 64 * buf);
-#pragma unroll
-          for (int e = 0; e < NH; ++e) {
-            ok = ok && umma::warp_wait(&sh.p_full[m][buf][e], ph, &sh.abort, p.dev_status);
+        more = next_piece<KT, C::kUnitCost>(p, walk, next);
+        for (int i = 0; ok && i < w.n_tiles; ++i) {
+          const bool s_next = i + C::kAhead < w.n_tiles;     // S of the tile that follows in this one's buffer
+          const int steps = steps_of(i);
+          if (MT == 2 && s_next) {
+            ok = wait(&sh.k_full[k_at], k_ph);
             if (!ok) break;
-            umma::fence_after_sync();           // P was written with tcgen05.st by the softmax threads
-            if (umma::elect_one()) {
+          }
+          ok = wait(&sh.v_full[v_at], v_ph);
+          const uint32_t v_lo = (v_base + (uint32_t)(v_at * C::kTile >> 4)) | v_lbo;
+          for (int m = 0; ok && m < tiles_m; ++m) {
+            const int grp = group_of(m, i), place = place_of(m, i), buf = place % NB;
+            const uint32_t o_tmem = tmem + C::kOCol + (uint32_t)(D * grp), p_tmem = tmem + (uint32_t)(128 * grp + 64 * buf);
+#pragma unroll
+            for (int e = 0; e < NH; ++e) {
+              ok = ok && wait(&sh.p_full[grp][buf][e], (place / NB) & 1);
+              if (!ok) break;
+              umma::fence_after_sync();         // P was written with tcgen05.st by the softmax threads
 #pragma unroll
               for (int kk = 4 * e; kk < 4 * e + 4; ++kk)
                 if (kk < steps)
                   umma::mma_bf16_a_tmem(o_tmem, p_tmem + 8 * kk, desc_hi | (uint64_t)(v_lo + (uint32_t)((kk * 2048) >> 4)),
-                                        umma::instr_desc(128, D, true), (i > 0 || kk > 0) ? 1u : 0u);
-              if (e == NH - 1) {
-                umma::commit(&sh.o_done[m][buf]);
-                if (m + 1 == tiles_m) umma::commit(&sh.v_empty[s]);
-              }
+                                        umma::instr_desc(128, D, true), (i >= SP || kk > 0) ? 1u : 0u);
             }
-            __syncwarp();
+            if (!ok) break;
+            umma::commit(&sh.o_done[grp][buf]);
+            if (m + 1 == tiles_m) umma::commit(&sh.v_empty[v_at]);
+            if (!s_next) continue;
+            if (MT == 1) ok = wait(&sh.k_full[k_at], k_ph);
+            if (ok) issue_s(m, i + C::kAhead);
           }
-          if (NB == 1 && ok && i + 1 < w.n_tiles) issue_s(m, i + 1);
+          if (s_next) k_used();
+          if (++v_at == ST) { v_at = 0; v_ph ^= 1; }
         }
-      }
-      kv += w.n_tiles;
 #pragma unroll
-      for (int m = 0; m < MT; ++m) done[m] += m < tiles_m ? w.n_tiles : 0;
+        for (int g = 0; g < C::kGroups; ++g) done[g] += SP == 2 ? (w.n_tiles + 1 - g) / 2 : g < tiles_m ? w.n_tiles : 0;
+      }
     }
+    __syncwarp();
   } else {
     // ------------------------------------------------------------------ softmax: one thread per query row
-    const int m = warp >> 2;
+    const int grp = warp >> 2, m = SP == 2 ? 0 : grp, turn = SP == 2 ? grp : 0;
     const uint32_t lane_base = (uint32_t)(32 * (warp & 3)) << 16;
-    const uint32_t o_addr = tmem + lane_base + C::kOCol + (uint32_t)(D * m);
-    int tc = 0, fixes[3] = {0, 0, 0};           // tiles of this M tile so far; uses of sh.fixed
+    const uint32_t o_addr = tmem + lane_base + C::kOCol + (uint32_t)(D * grp);
+    int tc = 0, fixes[3] = {0, 0, 0};           // tiles of this group so far; uses of sh.fixed
     bool ok = true, more = next_piece<KT, C::kUnitCost>(p, walk, w);
     while (ok && more) {
       if (w.n_tiles <= 0) break;                // (a unit per cluster: no tile of it is this CTA's)
@@ -655,19 +672,25 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
       if (r0 + 128 * m < rows) {
         const bool live_warp = r0 + 128 * m + 32 * (warp & 3) < rows;
         float m_use = -INFINITY, l_run = 0.f;
-        for (int i = 0; ok && i < w.n_tiles; ++i) {
-          const int t = w.lo + i, buf = (tc + i) % NB;
+        for (int i = turn; ok && i < w.n_tiles; i += SP) {
+          const int t = w.lo + i, place = tc + i / SP, buf = place % NB;
           const bool in_tree = t >= w.n_ct;
           const int live = in_tree ? w.n - (t - w.n_ct) * KT : w.len - t * KT;
           const bool masked = in_tree || live < KT;
           const int f = in_tree ? 1 + t - w.n_ct : 0;
+          auto wait_s = [&] { return umma::warp_wait(&sh.s_full[grp][buf], (place / NB) & 1, &sh.abort, p.dev_status); };
+          // A V stage's barrier may be asked for this tile once the stage's last tile was loaded, or its phase would be mistaken.
+          // S runs kAhead tiles ahead of P V; it is there once P V of the tile kAhead before was issued: as many stages or more.
+          // (MT = 2: S of the tile before, which is behind us, says the same, and the rows are mended under S of this one.)
+          if (MT == 1) ok = wait_s();
+          if (!ok) break;
           if (masked && m == 0) {
-            // V rows that must not meet a zero weight: by the warps of the first M tile
+            // V rows that must not meet a zero weight: by the tile's group, or the first M tile's
             const int s = (kv + i) % ST;
             ok = umma::warp_wait(&sh.v_full[s], ((kv + i) / ST) & 1, &sh.abort, p.dev_status);
             if (!ok) break;
             const int n_rows = min(KT, ((live + 15) >> 4) << 4);
-            for (int e = tid; e < n_rows * (D / 8); e += 128) {
+            for (int e = tid & 127; e < n_rows * (D / 8); e += 128) {
               const int rr = e / (D / 8), c = e % (D / 8);               // (the swizzle permutes pieces within a row only)
               uint4* at = reinterpret_cast<uint4*>(sV + s * C::kTile + (c >> 3) * C::kBox + rr * 128 + (c & 7) * 16);
               if (rr >= live) {
@@ -685,22 +708,22 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
             ptx::fence_proxy_async();
             ptx::mbar_arrive(&sh.fixed[f]);
           }
-          ok = umma::warp_wait(&sh.s_full[m][buf], ((tc + i) / NB) & 1, &sh.abort, p.dev_status);
-          // (behind S of this tile every earlier use of the barrier is over, so its phase cannot be mistaken)
+          if (MT == 2) ok = wait_s();
+          // (behind S of this tile every earlier use of the barrier is over)
           if (ok && masked && m != 0)
             ok = umma::warp_wait(&sh.fixed[f], (f == 0 ? fixes[0] : f == 1 ? fixes[1] : fixes[2]) & 1, &sh.abort, p.dev_status);
           if (!ok) break;
           umma::fence_after_sync();
           if (!live_warp) {                     // rows that are not there: whatever P holds for them goes nowhere
 #pragma unroll
-            for (int e = 0; e < NH; ++e) ptx::mbar_arrive(&sh.p_full[m][buf][e]);
+            for (int e = 0; e < NH; ++e) ptx::mbar_arrive(&sh.p_full[grp][buf][e]);
             continue;
           }
           // 64 scores of the row at a time.  Of a 128-key tile the second half is read for the maximum, then the first half,
           // which stays in registers for its exponentials; the second half is read again behind them (a read costs about
           // 50 cycles; 128 scores in registers do not fit).
           uint32_t zr[2][32];
-          const uint32_t s_addr = tmem + lane_base + (uint32_t)(128 * m + 64 * buf);
+          const uint32_t s_addr = tmem + lane_base + (uint32_t)(128 * grp + 64 * buf);
           auto read_half = [&](int e) {
             umma::tmem_ld32(s_addr + 64 * e, zr[0]);
             umma::tmem_ld32(s_addr + 64 * e + 32, zr[1]);
@@ -737,11 +760,11 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
             if (m_use == -INFINITY) m_use = 0.f;
           }
           const bool grow = mx > m_use + kLazyRescale;                    // also the first visible key (m_use = -inf)
-          const bool rescale = grow && m_use != -INFINITY && i > 0;       // O already holds something for this row
+          const bool rescale = grow && m_use != -INFINITY && i >= SP;       // O already holds something for this row
           if (__any_sync(0xffffffffu, rescale)) {
             // P V of the tile before is complete (with one S buffer: S of this tile came behind it)
             if (NB == 2) {
-              ok = umma::warp_wait(&sh.o_done[m][(tc + i - 1) % NB], ((tc + i - 1) / NB) & 1, &sh.abort, p.dev_status);
+              ok = umma::warp_wait(&sh.o_done[grp][(place - 1) % NB], ((place - 1) / NB) & 1, &sh.abort, p.dev_status);
               if (!ok) break;
               umma::fence_after_sync();
             }
@@ -780,25 +803,41 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
             umma::tmem_st32(s_addr + 32 * e, pk);                         // P over the S columns it came from, packed to half
             umma::tmem_st_wait();
             umma::fence_before_sync();
-            ptx::mbar_arrive(&sh.p_full[m][buf][e]);
+            ptx::mbar_arrive(&sh.p_full[grp][buf][e]);
           }
           float s0, s1;
           umma::unpack2(umma::add2(umma::add2(acc2[0], acc2[1]), umma::add2(acc2[2], acc2[3])), s0, s1);
           l_run += s0 + s1;
         }
         // ---- the row's sums leave
-        const int last = tc + w.n_tiles - 1;
-        ok = ok && umma::warp_wait(&sh.o_done[m][last % NB], (last / NB) & 1, &sh.abort, p.dev_status) &&
+        const int mine = (w.n_tiles - turn + SP - 1) / SP, last = tc + mine - 1;
+        ok = ok && (mine == 0 || umma::warp_wait(&sh.o_done[grp][last % NB], (last / NB) & 1, &sh.abort, p.dev_status)) &&
              (!in_tree0 || umma::warp_wait(&sh.fixed[1], fixes[1] & 1, &sh.abort, p.dev_status)) &&
              (!in_tree1 || umma::warp_wait(&sh.fixed[2], fixes[2] & 1, &sh.abort, p.dev_status));
         if (!ok) break;
         umma::fence_after_sync();
+        // two groups: their sums meet, and each takes half of the channels from here on
+        float f0 = 1.f, f1 = 0.f;
+        if constexpr (SP == 2) {
+          sh.sums[turn][tid & 127] = make_float2(m_use, l_run);
+          umma::fence_before_sync();
+          ptx::mbar_arrive(&sh.sums_full);
+          ok = umma::warp_wait(&sh.sums_full, (seq - 1) & 1, &sh.abort, p.dev_status);
+          if (!ok) break;
+          umma::fence_after_sync();
+          const float2 a = sh.sums[0][tid & 127], b = sh.sums[SP - 1][tid & 127];
+          m_use = fmaxf(a.x, b.x);
+          const float m_eff = m_use == -INFINITY ? 0.f : m_use;
+          f0 = exp2f(a.x - m_eff);
+          f1 = exp2f(b.x - m_eff);
+          l_run = a.y * f0 + b.y * f1;
+        }
         const bool whole = w.first && w.last;
         const int64_t pit = ((int64_t)blockIdx.x * 2 + (w.first ? 1 : 0)) * p.block_rows + (r - r0);     // in this CTA's slots
         if (refused && tid == 0) set_dev_status(p.dev_status, NGC_DEV_BAD_TREE);
         const float2 ml = live_row && !refused ? make_float2(m_use, l_run) : kNoPart;
-        if (p.cluster > 1) sh.ml[r - r0] = ml;
-        else if (!whole && r < rows) p.part_ml[pit] = ml;
+        if (turn == 0 && p.cluster > 1) sh.ml[r - r0] = ml;
+        else if (turn == 0 && !whole && r < rows) p.part_ml[pit] = ml;
         if (live_warp && !refused) {
           uint32_t odd[kTreeWords];
 #pragma unroll
@@ -807,11 +846,24 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
           const int64_t out_row = (((int64_t)w.l * p.B + w.b) * p.Hq + (int64_t)w.h * p.g) * p.N + r;
           const __nv_bfloat16* tv = (const __nv_bfloat16*)p.tree_v + (int64_t)w.strip * p.N * D;
 #pragma unroll 1
-          for (int c0 = 0; c0 < D; c0 += 32) {
+          for (int c0 = turn * (D / SP); c0 < (turn + 1) * (D / SP); c0 += 32) {
             uint32_t o[32];
             __syncwarp();
-            umma::tmem_ld32(o_addr + c0, o);
-            umma::tmem_ld_wait();
+            if constexpr (SP == 1) {
+              umma::tmem_ld32(o_addr + c0, o);
+              umma::tmem_ld_wait();
+            } else {
+              const uint32_t from = tmem + lane_base + C::kOCol + c0;
+              uint32_t o1[32];
+              umma::tmem_ld32(from, o);
+              if (w.n_tiles > 1) umma::tmem_ld32(from + D, o1);
+              umma::tmem_ld_wait();
+#pragma unroll
+              for (int c = 0; c < 32; ++c) {
+                const float x = __uint_as_float(o[c]) * f0;
+                o[c] = __float_as_uint(w.n_tiles > 1 ? fmaf(__uint_as_float(o1[c]), f1, x) : x);
+              }
+            }
             if (odd[0] | odd[1] | odd[2] | odd[3]) {
               for (int j = 0; j < w.n; ++j) {
                 const uint32_t word = j < 64 ? (j < 32 ? odd[0] : odd[1]) : (j < 96 ? odd[2] : odd[3]);
@@ -837,8 +889,12 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
             }
           }
         }
-        umma::fence_before_sync();              // O may be overwritten once the next P of this thread is out
-        tc += w.n_tiles;
+        umma::fence_before_sync();              // O may be overwritten once the next P of this thread is out ...
+        if constexpr (SP == 2) {                // ... which has to wait for both readers
+          ptx::mbar_arrive(&sh.sums_empty);
+          ok = umma::warp_wait(&sh.sums_empty, (seq - 1) & 1, &sh.abort, p.dev_status);
+        }
+        tc += mine;
       }
       kv += w.n_tiles;
       fixes[0] += in_tail;

@@ -206,6 +206,34 @@ def test_calls_on_two_streams_at_once():
             assert status_value(st) == 0 and all(torch.equal(x, w) for x, w in zip(got, want))
 
 
+@pytest.mark.parametrize("d,Hq,Hkv,N,B,T", [(128, 12, 2, 6, 70, 2000), (64, 12, 2, 6, 70, 2000), (128, 12, 2, 40, 30, 2010), (128, 2, 2, 3, 400, 450)])
+def test_rows_are_the_same_whether_the_cache_comes_from_memory_or_l2(d, Hq, Hkv, N, B, T):
+    """Late loads change the order in which the kernel's warps meet, not the result: runs behind a flushed L2 and warm ones agree
+    to the bit, with one another and, within the bound, with the oracle (first and last sequence)."""
+    b = ngc()
+    lens = [T - i % 7 for i in range(B)]
+    c, q, tk, tv, parent, _ = case(bf16, d, Hq, Hkv, 1, lens, N, "tree", seed=13)
+    dc, st = device_cache(c), b.new_status()
+    dev = [x.cuda() for x in (q, tk, tv, torch.as_tensor(parent))]
+    ws = b.alloc_workspace(b.workspace_bytes(b.OP_TREE_ATTN, dc, n_max=N))
+    flush = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    outs = []
+    for i in range(16):
+        out = torch.zeros(q.shape, dtype=f32, device="cuda")
+        if i % 4 < 3:
+            flush.fill_(i)
+        b.ngc_tree_attn(dc, *dev, out, ws=ws, status=st)
+        outs.append(out)
+    assert status_value(st) == 0 and all(torch.equal(x, outs[0]) for x in outs)
+    for s in (0, B - 1):
+        so = c.seq_off.numpy()
+        one = synth.Cache(c.k[:, :, so[s]:so[s + 1]].contiguous(), c.v[:, :, so[s]:so[s + 1]].contiguous(), torch.tensor([0, int(so[s + 1] - so[s])]),
+                          c.lens[s:s + 1], 1, 1, Hq, Hkv, d)
+        x = [t[:, s:s + 1].contiguous() for t in (q, tk, tv)]
+        ref = draft.tree_attn(synth.to_numpy(one.k), synth.to_numpy(one.v), one.seq_off.numpy(), one.lens.numpy(), *[synth.to_numpy(t) for t in x], parent[s:s + 1])
+        assert (np.abs(outs[0][:, s:s + 1].cpu().numpy() - ref) <= bound(one, *x, parent[s:s + 1], None, ref)).all()
+
+
 # ------------------------------------------------------------------ edges of the number range
 
 KINDS = [(bf16, 128, 5, 600), (bf16, 128, 100, 900), (f32, 64, 5, 40), (f32, 64, 5, 3000), (f32, 128, 40, 3000), (bf16, 128, 5, 40), (bf16, 128, 5, 4000), (bf16, 128, 100, 4000), (bf16, 64, 5, 4000),
