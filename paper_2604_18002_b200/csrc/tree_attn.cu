@@ -24,6 +24,8 @@ namespace {
 constexpr int kKeyTile = 32;                    // keys per tile, and the split granularity
 constexpr int kSms = 148;
 constexpr int kShortTiles = 48;                 // tensor cores: key tiles up to which a unit is a short one
+// Tensor cores: what a second kernel costs, in tiles; no call with so few tiles per unit cuts units.
+constexpr int join_tiles(int tiles_m) { return tiles_m == 1 ? 23 : 5; }
 constexpr int kClusterJoin = 3;                 // tensor cores: what joining in a cluster costs, in tiles
 constexpr int kSplitMin = 2;                    // tiles a split has at least
 
@@ -333,15 +335,15 @@ TreePlan tree_plan(const ngc_cache* c, int layers, int N) {
         pl.cluster = c;
         alone = (longest + c - 1) / c;
       }
-    // Cutting units costs a second kernel, some 8 us or join_tiles tiles, and saves what a CTA's share of a unit takes beyond
-    // an equal share of all (lengths taken to be three quarters of the longest on average).  64 sequences of 1024 / 2048
-    // tokens: 21 / 34 us uncut, 27 / 41 us cut; 8 of 4096 tokens in clusters of four: 21.0 us, cut 19.4 us.
-    const int64_t join_tiles = tiles == 1 ? 12 : 5;
-    pl.even = units > slots || 4 * (alone - join_tiles) * slots > 3 * units * longest;
+    // Cutting units costs a second kernel and the parts' way through memory, in all join_tiles() tiles, and saves what a CTA's
+    // share of a unit takes beyond an equal share of all (lengths taken to be three quarters of the longest on average).  64
+    // sequences of 4096 tokens: 50 us uncut, 61 us cut; 32 of 1024 to 8192: 43 us cut, 53 us in clusters of two; one of 131072:
+    // 55 us cut, 149 us in clusters of eight.
+    pl.even = units > slots || 4 * (alone - join_tiles(tiles)) * slots > 3 * units * longest;
     pl.cut = pl.even && units < 2 * slots;
     if (pl.even) {
       pl.cluster = 1;
-      const int64_t most = units * longest / kTreeMinTiles;
+      const int64_t most = units * longest / tree_min_tiles(tiles);
       pl.grid = (int)(most < slots ? most : slots);
     } else {
       pl.grid = pl.n_units * pl.cluster;
@@ -425,12 +427,20 @@ int tree_impl(const ngc_cache* c, const PagedView& pv, const void* q, const void
 
 }  // namespace
 
-// Workspace that serves a call over any layer range.
+// Workspace that serves a call over any layer range, and one that gives a smaller max_len (which may cut its units where
+// this one does not).
 size_t tree_workspace_bytes(const ngc_cache* c, int N) {
   if (N < 1 || N > kTreeMaxNodes) return 0;
   size_t worst = 0;
   for (int layers = 1; layers <= c->L; ++layers) {
-    const size_t bytes = tree_scratch(c, tree_plan(c, layers, N), layers, N).bytes;
+    TreePlan pl = tree_plan(c, layers, N);
+    if (c->dtype == NGC_BF16) {
+      const int keys = tree_umma_keys(pl.tiles_m);
+      const int64_t longest = ((int64_t)c->max_len + keys - 1) / keys + (N + keys - 1) / keys;
+      pl.cut = pl.n_units < 2 * kSms && (pl.n_units > kSms || longest > join_tiles(pl.tiles_m));
+      pl.grid = kSms;
+    }
+    const size_t bytes = tree_scratch(c, pl, layers, N).bytes;
     if (bytes > worst) worst = bytes;
   }
   return worst;

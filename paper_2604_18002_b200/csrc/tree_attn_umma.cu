@@ -77,7 +77,7 @@ template <int D, int MT, int CT> struct Cfg {
   static constexpr int kQBytes = 128 * D * 2;              // Q of an M tile
   static constexpr int kSmem = MT * kQBytes + 2 * kStages * kTile + 1024;
   // What beginning another unit costs a CTA, in tiles: the row sums leave, Q changes.
-  static constexpr int kUnitCost = MT == 1 ? 4 : 5;
+  static constexpr int kUnitCost = MT == 1 ? 9 : 5;
   static_assert(128 * MT * D * 4 <= 2 * kStages * kTile);  // a part of a cluster lies over the rings
   static constexpr uint32_t kOCol = 128 * kGroups;         // S[group][buf] at 128 group + 64 buf, O[group] behind
   static constexpr uint32_t kCols = 256 * kGroups;
@@ -428,7 +428,7 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
     sh.chunk[tid] = before;
     if (tid == NT - 1) sh.total = before + sum;
     __syncthreads();
-    const int total = sh.total, ctas = tree_even_ctas(total, gridDim.x);
+    const int total = sh.total, ctas = tree_even_ctas(total, gridDim.x, MT);
     const TreeEven even(total, ctas);
     const int g0 = even.first(blockIdx.x), g1 = even.first(blockIdx.x + 1);
     const bool busy = (int)blockIdx.x < ctas && total > 0;

@@ -155,3 +155,19 @@ def test_limits_of_scale_and_vocabulary(ngc):
     c = ngc.CacheDesc(16, 16, 16, 16, 64, 2, 1, 12, 2, 128, ngc.BF16, 64)
     assert lib.ngc_tree_attn(C.byref(c), 16, 16, 16, 16, None, 4, 0, 2, 2.5e38, 16, ngc.F32, None, 0, None, None) == -1
     assert lib.ngc_verify_draft(16, 16, None, 16, 16, 16, 2, 4, (1 << 30) + 1, 0, 16, 16, 16, None, None) == -2
+
+
+@pytest.mark.parametrize("dtype,d,N", [("BF16", 128, 16), ("BF16", 128, 40), ("BF16", 64, 1), ("F32", 64, 4)])
+def test_workspace_serves_every_smaller_max_len(ngc, dtype, d, N):
+    """How a call is laid out depends on max_len in steps, its workspace must not: one sized for a cache serves the call that
+    gives a smaller max_len (a call is refused with NGC_ERR_WORKSPACE, before anything is launched, if it has too little)."""
+    import itertools
+    for layers, B in itertools.product((1, 3), (1, 2, 7, 16, 20, 32, 48, 64, 150)):
+        last = 0
+        for T in range(0, 12000, 97):
+            c = ngc.CacheDesc(16, 16, 16, 16, B * T, layers, B, 12, 2, d, getattr(ngc, dtype), T)
+            need = ngc.lib.ngc_workspace_bytes(ngc.OP_TREE_ATTN, C.byref(c), 1, N, 0)
+            assert need >= last, (layers, B, T)
+            for n in range(1, layers + 1):
+                assert ngc.lib.ngc_tree_attn_launches(C.byref(c), n, N) == 1 or need > 0
+            last = need

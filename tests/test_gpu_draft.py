@@ -116,9 +116,10 @@ def test_tree_attn_matches_oracle(i):
 
 
 # launches: 1 where a cluster of CTAs shares a unit, 2 where units are cut and joined by a second kernel
-@pytest.mark.parametrize("dtype,d,Hq,Hkv,N,T,launches", [(bf16, 128, 12, 2, 16, 5000, 1), (bf16, 128, 12, 2, 64, 3001, 1), (bf16, 128, 2, 2, 1, 9000, 2),
+@pytest.mark.parametrize("dtype,d,Hq,Hkv,N,T,launches", [(bf16, 128, 12, 2, 16, 5000, 1), (bf16, 128, 12, 2, 64, 3001, 1), (bf16, 128, 2, 2, 1, 9000, 1),
                                                          (bf16, 64, 4, 1, 9, 4096, 1), (f32, 128, 4, 2, 7, 2500, 2), (f32, 64, 2, 2, 40, 1500, 2),
-                                                         (bf16, 128, 12, 2, 16, 9001, 2), (bf16, 128, 12, 2, 64, 12000, 2), (bf16, 64, 4, 1, 9, 10000, 2)])
+                                                         (bf16, 128, 12, 2, 16, 9001, 1), (bf16, 128, 12, 2, 64, 12000, 2), (bf16, 64, 4, 1, 9, 10000, 1),
+                                                         (bf16, 128, 12, 2, 16, 16001, 2), (bf16, 64, 4, 1, 9, 20000, 2), (bf16, 128, 2, 2, 1, 16100, 2)])
 def test_tree_attn_splits_a_long_cache(dtype, d, Hq, Hkv, N, T, launches):
     c, q, tk, tv, parent, n_nodes = case(dtype, d, Hq, Hkv, 1, [T, T // 3], N, "tree", seed=T, n_nodes=[N, max(1, N // 2)])
     b = ngc()
@@ -205,7 +206,7 @@ def test_tree_attn_layer_ranges_scale_and_lengths_per_list(dtype, d, N):
         check_tree(c, q, tk, tv, parent, n_nodes, lens_lists=lists)
 
 
-@pytest.mark.parametrize("T", [64, 4000, 9000])    # one part, a cluster, several parts
+@pytest.mark.parametrize("T", [64, 4000, 16000])   # one part, a cluster, several parts
 @pytest.mark.parametrize("dtype,d", [(f32, 64), (bf16, 128)])
 def test_tree_attn_skips_refused_sequences(dtype, d, T):
     N = 9

@@ -45,7 +45,7 @@ def guarded_workspace(need, extra=4096):
     return whole[:need], whole
 
 
-@pytest.mark.parametrize("Hq,N,lens", [(12, 9, [700, 33, 257]), (12, 50, [300, 64, 1]), (2, 1, [5000, 2, 90]), (2, 3, [13000, 70, 1])])
+@pytest.mark.parametrize("Hq,N,lens", [(12, 9, [700, 33, 257]), (12, 50, [300, 64, 1]), (2, 1, [5000, 2, 90]), (2, 3, [13000, 70, 1]), (2, 3, [20000, 70, 1])])
 def test_canaries_survive_tree_attention_commit_and_fork(Hq, N, lens):
     b = ngc()
     L, B, Hkv, d = 2, 3, 2, 128
