@@ -23,7 +23,6 @@ namespace {
 
 constexpr int kKeyTile = 32;                    // keys per tile, and the split granularity
 constexpr int kSms = 148;
-constexpr int kShortTiles = 48;                 // tensor cores: key tiles up to which a unit is a short one
 // Tensor cores: what a second kernel costs, in tiles; no call with so few tiles per unit cuts units.
 constexpr int join_tiles(int tiles_m) { return tiles_m == 1 ? 23 : 5; }
 constexpr int kClusterJoin = 3;                 // tensor cores: what joining in a cluster costs, in tiles
@@ -307,7 +306,7 @@ template <int D> cudaError_t opt_in_fma() {
 struct TreePlan {
   int block_rows, blocks;       // query rows per item, blocks per KV head
   int n_split;                  // FMA path: token splits
-  int tiles_m, ctas_sm;         // tensor cores: M tiles per CTA, CTAs per SM
+  int tiles_m;                  // tensor cores: M tiles per CTA
   int even, cut, grid, n_units; // tensor cores: tiles dealt to `grid` CTAs, units cut where that falls; or
   int cluster;                  //   a unit per cluster of so many CTAs
 };
@@ -323,8 +322,6 @@ TreePlan tree_plan(const ngc_cache* c, int layers, int N) {
     const int64_t longest = ((int64_t)c->max_len + keys - 1) / keys + (N + keys - 1) / keys;
     pl.n_units = (int)(units > 0x7fffffffLL ? 0x7fffffffLL : units);
     pl.tiles_m = tiles;
-    pl.ctas_sm = tiles == 1 && longest <= kShortTiles && units >= 4 * kSms ? 2 : 1;
-    const int64_t slots = kSms * pl.ctas_sm;
     // Clusters: so many CTAs per unit as make its tiles and the join shortest, as long as all clusters run at once: 14 of
     // eight CTAs, 32 of four, 74 of two (16 of eight: 18.7 us instead of 11.0 us for 14, units of 1024 tokens).  One sequence of
     // 512 / 1024 / 2048 tokens, 2 KV heads: 9.3 / 9.5 / 11.0 us; a CTA per unit 12.0 us, cut units 12.7 / 14.3 us.
@@ -339,12 +336,12 @@ TreePlan tree_plan(const ngc_cache* c, int layers, int N) {
     // share of a unit takes beyond an equal share of all (lengths taken to be three quarters of the longest on average).  64
     // sequences of 4096 tokens: 50 us uncut, 61 us cut; 32 of 1024 to 8192: 43 us cut, 53 us in clusters of two; one of 131072:
     // 55 us cut, 149 us in clusters of eight.
-    pl.even = units > slots || 4 * (alone - join_tiles(tiles)) * slots > 3 * units * longest;
-    pl.cut = pl.even && units < 2 * slots;
+    pl.even = units > kSms || 4 * (alone - join_tiles(tiles)) * kSms > 3 * units * longest;
+    pl.cut = pl.even && units < 2 * kSms;
     if (pl.even) {
       pl.cluster = 1;
       const int64_t most = units * longest / tree_min_tiles(tiles);
-      pl.grid = (int)(most < slots ? most : slots);
+      pl.grid = (int)(most < kSms ? most : kSms);
     } else {
       pl.grid = pl.n_units * pl.cluster;
     }
@@ -396,7 +393,7 @@ int tree_impl(const ngc_cache* c, const PagedView& pv, const void* q, const void
   p.G = lists_G(pv.lists, c->L, c->Hkv); p.lens_lists = c->lens_lists;
   const TreePlan plan = tree_plan(c, p.n_layers, N);
   p.row_blocks = plan.blocks; p.n_split = plan.n_split; p.block_rows = plan.block_rows;
-  p.tiles_m = plan.tiles_m; p.ctas_sm = plan.ctas_sm;
+  p.tiles_m = plan.tiles_m;
   p.even = plan.even; p.cut = plan.cut; p.cluster = plan.cluster; p.grid = plan.grid; p.n_units = plan.n_units; p.plan = nullptr;
   const TreeScratch need = tree_scratch(c, plan, p.n_layers, N);
   if (need.bytes > 0) {

@@ -29,7 +29,7 @@ struct TreeAttnParams {
   int64_t rows;
   int L, B, Hq, Hkv, d, g, N;
   int layer_begin, n_layers, n_split, row_blocks, out_bf16;
-  int even, cut, cluster, grid, n_units, block_rows, tiles_m, ctas_sm;    // tensor cores
+  int even, cut, cluster, grid, n_units, block_rows, tiles_m;    // tensor cores
   float scale_log2;             // scale * log2(e)
   const int32_t* page_table;    // [B][G][pages_cap] or null
   int page, pages_cap, lists, G;

@@ -4,21 +4,21 @@
 // one after the other) with all of its key tiles: the cache rows, then the nodes of the tree.  The 128 rows of an M
 // tile are the 128 lanes of tensor memory.
 //
-//   up to 128 rows   MT = 1, tiles of 64 keys, S double-buffered: these calls are bound by the cache that they read.  One
-//                    CTA per SM with five stages of K and V, or, where units are so short that their beginnings and ends
-//                    count, two CTAs with two stages each that cover one another's;
-//   more rows        MT = 2, tiles of 128 keys, one CTA per SM: bound by the tensor pipe and the exponentials.  K and V
-//                    tiles serve both M tiles, whose softmax and products alternate on the tensor pipe.  (With 64 keys
-//                    S = Q K^T waits for shared memory: Q is read again for every 64 keys.)
+//   up to 128 rows   MT = 1, tiles of 64 keys, five stages of K and V.  Two softmax groups take turns at the tiles, each with
+//                    an O of its own and two S buffers, so that S is there four tiles ahead of P V; their sums meet at the
+//                    end of a unit;
+//   more rows        MT = 2, tiles of 128 keys, two stages: K and V tiles serve both M tiles, whose softmax and products
+//                    alternate on the tensor pipe.  (With 64 keys S = Q K^T waits for shared memory: Q is read again for
+//                    every 64 keys.)
 //
 //   producer warps   one for Q (once per unit) and K, one for V, by tiled TMA (128-byte swizzle), K and V each in a ring
 //                    of its own (K is free as soon as S is computed, V only after P V).  Issuing a load takes a warp
 //                    some 150 cycles, so a whole tile of a contiguous cache is ONE load (the groups of 64 channels are a
 //                    dimension of the tensor map); pages are a load per 64 channels, the tree's rows come in
 //                    16-row boxes.  Page-table entries are fetched 32 at a time, a batch ahead;
-//   MMA warp         S = Q K^T into tensor memory, O += P V with P read from tensor memory;
+//   MMA thread       S = Q K^T into tensor memory, O += P V with P read from tensor memory;
 //   mask warp        the ancestor sets of the next unit's tree, by pointer doubling;
-//   softmax warps    (4 MT) one thread per row: mask (in tree tiles, its node's ancestors; in the cache's last tile a common
+//   softmax warps    (two groups of four) one thread per row: mask (in tree tiles, its node's ancestors; in the cache's last tile a common
 //                    one), online softmax in the log2 domain, P as bf16 over the S it came from, 64 keys at a time.  The
 //                    maximum used only moves when the true one has grown by more than a factor 2^8, so O in tensor
 //                    memory is rarely rescaled.
@@ -34,11 +34,12 @@
 // that does not pay (few short units), a cluster of up to 8 CTAs takes a unit, each an equal part of its tiles, and joins the
 // parts through distributed shared memory.
 //
-// What bounds it: up to 128 rows, DRAM in the steady state (6.0 TB/s from 4096 to 8192 tokens of 64 sequences) and some 20 us
-// around it where units are cut (64 sequences of 1024 to 4096 tokens, 173 MB: 48 us); a tile of 64 keys takes its CTA
-// some 1450 cycles, which is what few sequences see.  More rows: no pipe, but the chain S -> softmax -> P -> O of a tile (3100
-// cycles per 128 keys and 256 rows, 2550 of them without any softmax arithmetic): 131072 tokens under 64 nodes, 12 heads, two
-// layers in 140 us, 740 TFLOP/s.
+// What bounds it: up to 128 rows, DRAM in the steady state (6.9 TB/s from 2048 to 8192 tokens of 64 sequences) and some 20 us
+// around it (64 sequences of 1024 to 4096 tokens, 173 MB: 47 us); few sequences see what a tile takes its CTA, some 800 cycles.
+// (One softmax group and S one tile ahead: 1450 cycles.  Two CTAs per SM of two stages and one group each: 2 to 10 % slower
+// from 320 sequences on but for short ragged ones, 81 and 84 us for 512 of 200 to 500 tokens.)  More rows: no pipe, but the chain
+// S -> softmax -> P -> O of a tile (3100 cycles per 128 keys and 256 rows, 2550 of them without any softmax arithmetic): 131072
+// tokens under 64 nodes, 12 heads, two layers in 143 us, 720 TFLOP/s.
 //
 // bf16 P: one rounding per weight (2^-8), as in the decode and replay calls; the row sum takes the weights
 // before it.  0 x V must be 0 whatever a dead V row holds: rows of the last 16-row box beyond the live ones are
@@ -62,14 +63,14 @@ namespace cg = cooperative_groups;
 
 constexpr float kLazyRescale = 8.f;             // log2 units the row maximum may grow before O is rescaled
 
-template <int D, int MT, int CT> struct Cfg {
+template <int D, int MT> struct Cfg {
   static constexpr int kKeys = tree_umma_keys(MT);         // keys per tile
   static constexpr int kBufs = MT == 1 ? 2 : 1;            // S buffers per M tile
-  static constexpr int kSplit = MT == 1 && CT == 1 ? 2 : 1;                     // softmax groups that take turns at an M tile's key tiles
+  static constexpr int kSplit = MT == 1 ? 2 : 1;           // softmax groups that take turns at an M tile's key tiles
   static constexpr int kAhead = kBufs * kSplit;            // tiles whose S an M tile has room for
   static constexpr int kHalves = kKeys / 64;               // P is handed over 64 keys at a time
   static constexpr int kGroups = MT * kSplit;              // softmax groups: 128 threads, S buffers and O of their own
-  static constexpr int kStages = (MT == 1 && CT == 1 ? 5 : 2) * (128 / D);      // of K and of V
+  static constexpr int kStages = (MT == 1 ? 5 : 2) * (128 / D);                 // of K and of V
   static constexpr int kThreads = (4 * kGroups + 4) * 32;
   static constexpr int kMmaWarp = 4 * kGroups, kMaskWarp = kMmaWarp + 1, kProducerWarp = kMmaWarp + 2;      // K and Q; V in the warp behind
   static constexpr int kBox = kKeys * 128;                 // a tile's 64 channels
@@ -80,7 +81,7 @@ template <int D, int MT, int CT> struct Cfg {
   static constexpr int kUnitCost = MT == 1 ? 9 : 5;
   static_assert(128 * MT * D * 4 <= 2 * kStages * kTile);  // a part of a cluster lies over the rings
   static constexpr uint32_t kOCol = 128 * kGroups;         // S[group][buf] at 128 group + 64 buf, O[group] behind
-  static constexpr uint32_t kCols = 256 * kGroups;
+  static constexpr uint32_t kCols = 512;                   // of tensor memory: all
 };
 
 // Tensor maps of a launch.  K and V: whole tiles (contiguous caches, all channels in one box) or pages; the tree's K and V
@@ -91,8 +92,8 @@ struct Maps { KvMaps k, v; CUtensorMap q; };
 // A unit and where it begins on the line.
 struct Found { int u, base, places; };
 
-template <int D, int MT, int CT> struct Shared {
-  using C = Cfg<D, MT, CT>;
+template <int D, int MT> struct Shared {
+  using C = Cfg<D, MT>;
   uint64_t k_full[C::kStages], k_empty[C::kStages], v_full[C::kStages], v_empty[C::kStages];
   uint64_t s_full[C::kGroups][C::kBufs], p_full[C::kGroups][C::kBufs][C::kHalves], o_done[C::kGroups][C::kBufs];
   uint64_t sums_full, sums_empty;               // two groups per M tile: the rows' (maximum, sum) in `sums`; O has been read
@@ -356,13 +357,13 @@ __device__ __forceinline__ void cluster_join(const TreeAttnParams& p, Sh& sh, ui
   cluster.sync();                               // nobody leaves while its part may still be read
 }
 
-template <int D, int MT, int CT>
-__global__ void __launch_bounds__(Cfg<D, MT, CT>::kThreads, CT)
+template <int D, int MT>
+__global__ void __launch_bounds__(Cfg<D, MT>::kThreads, 1)
 tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
-  using C = Cfg<D, MT, CT>;
+  using C = Cfg<D, MT>;
   constexpr int ST = C::kStages, NT = C::kThreads, KT = C::kKeys, NB = C::kBufs, NH = C::kHalves, SP = C::kSplit;
   extern __shared__ uint8_t smem_dyn[];
-  __shared__ Shared<D, MT, CT> sh;
+  __shared__ Shared<D, MT> sh;
   uint8_t* sQ = (uint8_t*)(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);     // [MT][128 rows]
   uint8_t* sK = sQ + MT * C::kQBytes;                                            // [ST]
   uint8_t* sV = sK + ST * C::kTile;                                              // [ST]
@@ -991,21 +992,19 @@ template <int D> __global__ void __launch_bounds__(16 * kJoinRows) tree_join_ker
   for (int c = 0; c < kPer; c += 4) tree_store_out4(p, to + c, make_float4(o[c] * inv, o[c + 1] * inv, o[c + 2] * inv, o[c + 3] * inv));
 }
 
-template <int D, int MT, int CT> cudaError_t opt_in() {
-  return cudaFuncSetAttribute(tree_umma_kernel<D, MT, CT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, MT, CT>::kSmem);
+template <int D, int MT> cudaError_t opt_in() {
+  return cudaFuncSetAttribute(tree_umma_kernel<D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, MT>::kSmem);
 }
-template <int D, int MT, int CT> cudaError_t launch(const Maps& maps, const TreeAttnParams& p, cudaStream_t stream) {
-  using C = Cfg<D, MT, CT>;
-  return launch_pdl_cluster(tree_umma_kernel<D, MT, CT>, dim3(p.grid), dim3(C::kThreads), (unsigned)p.cluster, C::kSmem, stream, maps, p);
+template <int D, int MT> cudaError_t launch(const Maps& maps, const TreeAttnParams& p, cudaStream_t stream) {
+  using C = Cfg<D, MT>;
+  return launch_pdl_cluster(tree_umma_kernel<D, MT>, dim3(p.grid), dim3(C::kThreads), (unsigned)p.cluster, C::kSmem, stream, maps, p);
 }
 template <int D> cudaError_t launch_d(const Maps& maps, const TreeAttnParams& p, cudaStream_t stream) {
-  if (p.tiles_m == 2) return launch<D, 2, 1>(maps, p, stream);
-  return p.ctas_sm == 1 ? launch<D, 1, 1>(maps, p, stream) : launch<D, 1, 2>(maps, p, stream);
+  return p.tiles_m == 1 ? launch<D, 1>(maps, p, stream) : launch<D, 2>(maps, p, stream);
 }
 template <int D> cudaError_t opt_in_d() {
-  cudaError_t e = opt_in<D, 1, 1>();
-  if (e == cudaSuccess) e = opt_in<D, 1, 2>();
-  return e == cudaSuccess ? opt_in<D, 2, 1>() : e;
+  const cudaError_t e = opt_in<D, 1>();
+  return e == cudaSuccess ? opt_in<D, 2>() : e;
 }
 
 }  // namespace
