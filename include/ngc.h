@@ -478,7 +478,8 @@ int ngc_decode_attn_ragged_static(ngc_cache* c, const void* q, const void* new_k
  * skipped.  The workspace is free again when the call has run: calls that may
  * run at the same time (other streams, graphs) need one each.  q, tree_k, tree_v,
  * out, k and v must be 16-byte aligned.  Workspace:
- * ngc_workspace_bytes(NGC_OP_TREE_ATTN, c, 1, N, 0).
+ * ngc_workspace_bytes(NGC_OP_TREE_ATTN, c, 1, N, 0), which also serves calls
+ * that give a smaller max_len.
  */
 int ngc_tree_attn(const ngc_cache* c, const void* q, const void* tree_k, const void* tree_v, const int32_t* parent,
                   const int32_t* n_nodes, int N, int layer_begin, int layer_end, float scale, void* out, int out_dtype,
