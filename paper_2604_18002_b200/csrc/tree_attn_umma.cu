@@ -682,8 +682,11 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
           auto wait_s = [&] { return umma::warp_wait(&sh.s_full[grp][buf], (place / NB) & 1, &sh.abort, p.dev_status); };
           // A V stage's barrier may be asked for this tile once the stage's last tile was loaded, or its phase would be mistaken.
           // S runs kAhead tiles ahead of P V; it is there once P V of the tile kAhead before was issued: as many stages or more.
-          // (MT = 2: S of the tile before, which is behind us, says the same, and the rows are mended under S of this one.)
-          if (MT == 1) ok = wait_s();
+          // (MT = 2: S of the tile before, which is behind us, says the same, and the rows are mended under S of this one.  But
+          // not of a piece's first tile: its S says that the second group has left the last wait for `fixed` of the piece before,
+          // which an arrival at the same barrier would make it miss.)
+          const bool s_first = MT == 1 || i == 0;
+          if (s_first) ok = wait_s();
           if (!ok) break;
           if (masked && m == 0) {
             // V rows that must not meet a zero weight: by the tile's group, or the first M tile's
@@ -709,8 +712,9 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
             ptx::fence_proxy_async();
             ptx::mbar_arrive(&sh.fixed[f]);
           }
-          if (MT == 2) ok = wait_s();
-          // (behind S of this tile every earlier use of the barrier is over)
+          if (!s_first) ok = wait_s();
+          // (behind S of this tile every earlier use of the barrier is over, and the first group cannot come to its next use
+          // before this group's P of the tile)
           if (ok && masked && m != 0)
             ok = umma::warp_wait(&sh.fixed[f], (f == 0 ? fixes[0] : f == 1 ? fixes[1] : fixes[2]) & 1, &sh.abort, p.dev_status);
           if (!ok) break;
@@ -812,9 +816,12 @@ tree_umma_kernel(const __grid_constant__ Maps maps, TreeAttnParams p) {
         }
         // ---- the row's sums leave
         const int mine = (w.n_tiles - turn + SP - 1) / SP, last = tc + mine - 1;
+        // (sh.odd is complete once `fixed` is.  Of two M tiles, the second's group asked in the tile, and must not ask again: the
+        // first group may have used the barrier for the next piece by now.  Two groups of one M tile leave a piece together.)
+        const bool ask = SP == 2 || m == 0;
         ok = ok && (mine == 0 || umma::warp_wait(&sh.o_done[grp][last % NB], (last / NB) & 1, &sh.abort, p.dev_status)) &&
-             (!in_tree0 || umma::warp_wait(&sh.fixed[1], fixes[1] & 1, &sh.abort, p.dev_status)) &&
-             (!in_tree1 || umma::warp_wait(&sh.fixed[2], fixes[2] & 1, &sh.abort, p.dev_status));
+             (!ask || !in_tree0 || umma::warp_wait(&sh.fixed[1], fixes[1] & 1, &sh.abort, p.dev_status)) &&
+             (!ask || !in_tree1 || umma::warp_wait(&sh.fixed[2], fixes[2] & 1, &sh.abort, p.dev_status));
         if (!ok) break;
         umma::fence_after_sync();
         // two groups: their sums meet, and each takes half of the channels from here on

@@ -1,0 +1,55 @@
+"""Drafted-token calls where their parts meet: units that follow one another in a CTA, parts that a second kernel joins,
+draws and rows at the edge of what counts as a probability."""
+import numpy as np
+import pytest
+import torch
+
+from helpers import ngc, status_value
+from oracle import draft
+from paper_2604_18002_b200 import synth
+from test_gpu_draft import bound, case, device_cache, run_tree
+
+pytestmark = pytest.mark.gpu
+
+bf16, f32 = torch.bfloat16, torch.float32
+
+
+# ------------------------------------------------------------------ tree attention: from one unit to the next
+
+@pytest.mark.parametrize("d,Hq,Hkv,N,B,first,launches", [
+    (128, 2, 1, 80, 600, "refused", 1), (128, 2, 1, 80, 600, "one node", 1), (64, 2, 1, 80, 600, "refused", 1), (128, 4, 1, 96, 400, "refused", 1),
+    (128, 4, 2, 70, 300, "refused", 1), (128, 2, 1, 128, 600, "one node", 1), (128, 3, 1, 100, 250, "refused", 1), (128, 2, 1, 80, 200, "refused", 2),
+    (128, 2, 1, 80, 200, "one node", 2)])
+def test_empty_caches_behind_trees_that_leave_early(d, Hq, Hkv, N, B, first, launches):
+    """More than 128 query rows per KV head, units dealt out whole (one launch) or cut (two): every other sequence leaves its unit
+    early (its tree is refused, or has one node), the one behind it has an empty cache, so that its first tile is a tree tile whose
+    V rows are mended at once.  The softmax groups of the two M tiles are then as far apart as they get.  Runs behind a flushed L2
+    and warm ones agree to the bit, and with the oracle within the bound."""
+    b = ngc()
+    lens = [0 if i % 2 else (300, 129, 0, 260)[i // 2 % 4] for i in range(B)]
+    n_nodes = np.full(B, N, np.int32)
+    c, q, tk, tv, parent, _ = case(bf16, d, Hq, Hkv, 1, lens, N, "tree", seed=N, capacity=300)
+    if first == "refused":
+        parent[::2, N - 1] = N - 1
+    else:
+        n_nodes[::2] = 1
+    dc, st = device_cache(c), b.new_status()
+    assert b.tree_attn_launches(dc, N) == launches
+    dev = [x.cuda() for x in (q, tk, tv, torch.as_tensor(parent))]
+    dn = torch.as_tensor(n_nodes).cuda()
+    ws = b.alloc_workspace(b.workspace_bytes(b.OP_TREE_ATTN, dc, n_max=N))
+    flush = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    outs = []
+    for i in range(12):
+        out = torch.full(q.shape, -7.0, dtype=f32, device="cuda")
+        if i % 2:
+            flush.fill_(i)
+        st.zero_()
+        b.ngc_tree_attn(dc, *dev, out, dn, ws=ws, status=st)
+        assert status_value(st) == (8 if first == "refused" else 0)
+        outs.append(out)
+    assert all(torch.equal(x, outs[0]) for x in outs)
+    ref = draft.tree_attn(synth.to_numpy(c.k), synth.to_numpy(c.v), c.seq_off.numpy(), c.lens.numpy(), *[synth.to_numpy(x) for x in (q, tk, tv)],
+                          parent, n_nodes, fill=-7.0)
+    got = outs[0].cpu().numpy().astype(np.float64)
+    assert (got[ref == -7.0] == -7.0).all() and (np.abs(got - ref) <= bound(c, q, tk, tv, parent, n_nodes, ref)).all()
