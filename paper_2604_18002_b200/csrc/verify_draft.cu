@@ -387,12 +387,14 @@ __global__ void __launch_bounds__(kVerifyThreads, kCtasSm) verify_draft_kernel(V
           __syncthreads();
 #pragma unroll
           for (int i = 0; i < kVerifyWarps; ++i) before += i < warp ? sh.scan[i] : 0.0;
+          // (rounding may begin a run beyond the target already: a token without mass is passed over all the same)
           double upto = before + (c - s);
           int hit = -1;
           if (upto + s > t)
             for (int x = x0; x < x1 && hit < 0; ++x) {
-              upto += part.at(x);
-              if (upto > t) hit = x;
+              const double wx = part.at(x);
+              upto += wx;
+              if (wx > 0.0 && upto > t) hit = x;
             }
           if (hit >= 0) atomicMin(&sh.warp_arg[0], hit);
           if (tail >= 0) atomicMax(&sh.last, tail);

@@ -7,7 +7,7 @@ import torch
 from helpers import ngc, status_value
 from oracle import draft
 from paper_2604_18002_b200 import synth
-from test_gpu_draft import bound, case, device_cache, run_tree
+from test_gpu_draft import bound, case, device_cache, run_verify
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +53,21 @@ def test_empty_caches_behind_trees_that_leave_early(d, Hq, Hkv, N, B, first, lau
                           parent, n_nodes, fill=-7.0)
     got = outs[0].cpu().numpy().astype(np.float64)
     assert (got[ref == -7.0] == -7.0).all() and (np.abs(got - ref) <= bound(c, q, tk, tv, parent, n_nodes, ref)).all()
+
+
+# ------------------------------------------------------------------ verification: the final draw
+
+@pytest.mark.parametrize("o", [0, 3 * 16384 + 5 * 2048])
+@pytest.mark.parametrize("drafted", [False, True])
+def test_a_token_without_mass_is_never_drawn(o, drafted):
+    """The draw's target, 1 / 8, is exactly the sum of the tokens before a run of the scan (token o), and the run's own sum is the
+    double before its exact tie with that: 1 / 8 + (1 / 8 + 3 * 2^-55) rounds up, so that the run seems to begin 2^-55 beyond
+    the target.  Its first token has no mass; the token drawn is the first one that has."""
+    V, b = 131072, ngc()
+    p = np.zeros((1, 1, V), np.float32)
+    p[0, 0, [o, o + 9, o + 10, 131000]] = 0.125, 0.125, 3 * 2.0 ** -55, 0.75
+    u, none = np.full((1, 1), 0.125, np.float32), np.array([[-1]], np.int32)
+    ref = draft.verify_draft(none, none, p, u, p if drafted else None)
+    assert ref[2].tolist() == [o + 9] and not ref[3].any()
+    path, n_path, nxt, st = run_verify(none, none, p, u, p if drafted else None)
+    assert st == 0 and path.tolist() == [[0]] and n_path.tolist() == [1] and nxt.tolist() == [o + 9]
