@@ -83,7 +83,7 @@ typedef enum {
   NGC_DEV_TIMEOUT = 6,        /* a bounded wait inside a kernel ran out */
   NGC_DEV_DEBUG_BOUNDS = 7,   /* bounds-checking build only: a kernel computed an index outside its array */
   NGC_DEV_BAD_TREE = 8,       /* a node count, parent link, drafted token or accepted path that is none */
-  NGC_DEV_BAD_PROBS = 9,      /* probabilities without a finite positive sum */
+  NGC_DEV_BAD_PROBS = 9,      /* numbers that are no probabilities, or have no finite positive sum */
   NGC_DEV_BAD_SOURCE = 10,    /* a fork's source is no sequence, or is itself a destination */
   NGC_DEV_BAD_PAGE = 11       /* a page-table entry outside 0 .. pages_cap-1 */
 } ngc_dev_status;
@@ -522,8 +522,12 @@ int ngc_tree_attn_paged(const ngc_paged_cache* c, const void* q, const void* tre
  *   next_token   [B] out: the token that follows the path (-1 for an empty tree)
  * Decisions and sums in fp64: the outcome does not depend on launch geometry
  * beyond the last bits of an fp64 sum.  A bad tree or token (NGC_DEV_BAD_TREE)
- * or a visited row without a finite positive sum (NGC_DEV_BAD_PROBS; a NaN, if
- * greedy) gives path -1, n_path 0, next_token -1.
+ * or numbers that are no probabilities (NGC_DEV_BAD_PROBS) give path -1,
+ * n_path 0, next_token -1.  The latter are looked for where the walk reads: a
+ * tested child's p(x) or q(x) that is negative, infinite or NaN; a node where a
+ * child drawn from q is rejected, if what is left has no finite sum; the last
+ * node, if what is left has no finite positive sum; greedy: a NaN in any row that
+ * the walk visits.
  */
 int ngc_verify_draft(const int32_t* tokens, const int32_t* parent, const int32_t* n_nodes, const float* target_probs,
                      const float* draft_probs, const float* uniforms, int B, int N, int vocab, int greedy,

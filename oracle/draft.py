@@ -89,6 +89,9 @@ def verify_draft(tokens, parent, target, uniforms, draft=None, n_nodes=None, gre
                 if greedy:
                     ok = x == int(np.argmax(w))
                 else:
+                    if not all(0 <= float(r[b, cur, x]) < np.inf for r in (target, draft) if r is not None):
+                        status[b] = 9
+                        break
                     u = float(uniforms[b, i])
                     ok = u * mass < w[x] if q is None else u * q[x] * mass < w[x]
                 if ok:

@@ -24,7 +24,7 @@ OP_SCORE, OP_SAMPLE, OP_LOGPROB, OP_COMPACT, OP_DECODE, OP_SCORE_BACKWARD, OP_TR
 
 DEV_STATUS = {0: "ok", 1: "bad counts", 2: "NaN logit", 3: "bad kept list", 4: "strip full",
               5: "lists disagree", 6: "timeout", 7: "index out of bounds (bounds-checking build)", 8: "bad drafted tree or path",
-              9: "probabilities without a finite positive sum", 10: "bad fork source", 11: "bad page-table entry"}
+              9: "numbers that are no probabilities, or have no finite positive sum", 10: "bad fork source", 11: "bad page-table entry"}
 
 EXPORTS = ["ngc_version", "ngc_strerror", "ngc_last_cuda_error", "ngc_workspace_bytes", "ngc_decode_splits", "ngc_score_evict", "ngc_score_evict_launches",
            "ngc_sample_evict", "ngc_evict_logprob", "ngc_evict_logprob_backward", "ngc_compact_kv", "ngc_decode_attn_ragged",

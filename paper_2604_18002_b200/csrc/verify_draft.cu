@@ -180,8 +180,11 @@ __global__ void __launch_bounds__(kVerifyThreads, kCtasSm) verify_draft_kernel(V
     sh.parent[tid] = pa;
     sh.token[tid] = x;
     if (MODE != kModeGreedy && tid > 0 && !bad) {
-      sh.p[tid] = p.target[row0 + (int64_t)pa * p.vocab + x];
-      if (MODE == kModeDraft) sh.q[tid] = p.draft[row0 + (int64_t)pa * p.vocab + x];
+      const float px = p.target[row0 + (int64_t)pa * p.vocab + x];
+      const float qx = MODE == kModeDraft ? p.draft[row0 + (int64_t)pa * p.vocab + x] : 0.f;
+      // NaN: one of the two is no probability, which counts if the child is tested
+      sh.p[tid] = px < INFINITY && qx >= 0.f && qx < INFINITY ? px : NAN;
+      if (MODE == kModeDraft) sh.q[tid] = qx;
     }
   }
   int status = __syncthreads_or(bad) ? NGC_DEV_BAD_TREE : NGC_DEV_OK;
@@ -291,6 +294,10 @@ __global__ void __launch_bounds__(kVerifyThreads, kCtasSm) verify_draft_kernel(V
 #pragma unroll
           for (int k = 0; k < kWords; ++k)
             if (w.tried[k]) again |= __ballot_sync(0xffffffffu, tok[k] == x) & w.tried[k];
+        }
+        if (!(sh.p[i] >= 0.f)) {                     // (marked above; nothing else would notice in a row that is not summed)
+          status = NGC_DEV_BAD_PROBS;
+          break;
         }
         const double wx = again ? 0.0 : w.of(sh.p[i], MODE == kModeDraft ? sh.q[i] : 0.f), u = (double)sh.u[i];
         ok = MODE == kModeDraft ? __dmul_rn(__dmul_rn(u, (double)sh.q[i]), mass) < wx : __dmul_rn(u, mass) < wx;

@@ -7,7 +7,7 @@ import torch
 from helpers import ngc, status_value
 from oracle import draft
 from paper_2604_18002_b200 import synth
-from test_gpu_draft import bound, case, device_cache, run_verify
+from test_gpu_draft import bound, case, check_verify, device_cache, draft_case, run_verify
 
 pytestmark = pytest.mark.gpu
 
@@ -71,3 +71,37 @@ def test_a_token_without_mass_is_never_drawn(o, drafted):
     assert ref[2].tolist() == [o + 9] and not ref[3].any()
     path, n_path, nxt, st = run_verify(none, none, p, u, p if drafted else None)
     assert st == 0 and path.tolist() == [[0]] and n_path.tolist() == [1] and nxt.tolist() == [o + 9]
+
+
+# ------------------------------------------------------------------ verification: probabilities that are none
+
+@pytest.mark.parametrize("mode", ["draft", "point"])
+def test_a_tested_child_needs_probabilities(mode):
+    """A tree whose walk tests children at two nodes and leaves both behind; in the second sequence one of the numbers that a test
+    needs is negative, infinite or NaN, at nodes whose rows are not summed (or, where a drawn child is refused, not all of them).
+    Elsewhere in the first node's row nobody looks."""
+    V, N = 300, 6
+    tokens, _, p, q, u = draft_case(3, N, V, "chain", mode, 5)
+    parent = np.tile(np.array([-1, 0, 0, 1, 1, 4], np.int32), (3, 1))      # walk: 0, 1 (2 is not tested), 4 (behind 3), 5
+    tokens[:] = np.arange(N) + 7
+    p[:, 1, tokens[0, 3]] = 0.0                                           # node 3 is refused, node 4 taken
+    u[:, 1:] = 0.0
+    u[:, 3] = 0.5
+    if mode == "point":
+        q = None
+    else:
+        q[:, 1] = p[:, 1]                                                 # what is left after node 3: p - q would be nothing, so it stays
+        q[:, 1, tokens[0, 3]] = 0.25
+    good = check_verify(tokens, parent, p, q, u)
+    assert good[0][0].tolist() == [0, 1, 4, 5, -1, -1]
+    for at, child in ((0, 1), (1, 3), (1, 4)):
+        for rows in ("p", "q") if mode == "draft" else ("p",):
+            for x in (-0.25, np.inf, -np.inf, np.nan):
+                p2, q2 = p.copy(), None if q is None else q.copy()
+                (p2 if rows == "p" else q2)[1, at, tokens[1, child]] = x
+                ref = check_verify(tokens, parent, p2, q2, u)
+                assert ref[3].tolist() == [0, 9, 0] and ref[2][1] == -1 and ref[1][1] == 0, (at, child, rows, x)
+    p2 = p.copy()
+    p2[1, 0, 200] = np.nan                                                # node 0's row is read at one token only
+    ref = check_verify(tokens, parent, p2, q, u)
+    assert not ref[3].any() and np.array_equal(ref[0], good[0])
