@@ -23,7 +23,7 @@ namespace {
 
 constexpr int kKeyTile = 32;                    // keys per tile, and the split granularity
 constexpr int kSms = 148;
-// Tensor cores: what a second kernel costs, in tiles; no call with so few tiles per unit cuts units.
+// Tensor cores: what a second kernel costs, in tiles; up to a unit per SM, no call with so few tiles per unit cuts units.
 constexpr int join_tiles(int tiles_m) { return tiles_m == 1 ? 23 : 5; }
 constexpr int kClusterJoin = 3;                 // tensor cores: what joining in a cluster costs, in tiles
 constexpr int kSplitMin = 2;                    // tiles a split has at least
@@ -340,7 +340,9 @@ TreePlan tree_plan(const ngc_cache* c, int layers, int N) {
     pl.cut = pl.even && units < 2 * kSms;
     if (pl.even) {
       pl.cluster = 1;
-      const int64_t most = units * longest / tree_min_tiles(tiles);
+      // More units than SMs fill all SMs, however short they are: beginning one costs a CTA more than the least it gets.  (150 sequences
+      // of 64 tokens, one node and KV head: 15.9 us; 26.3 us on the 37 CTAs that a share of their 300 tiles would give.)
+      const int64_t most = units > kSms ? kSms : units * longest / tree_min_tiles(tiles);
       pl.grid = (int)(most < kSms ? most : kSms);
     } else {
       pl.grid = pl.n_units * pl.cluster;

@@ -105,3 +105,39 @@ def test_a_tested_child_needs_probabilities(mode):
     p2[1, 0, 200] = np.nan                                                # node 0's row is read at one token only
     ref = check_verify(tokens, parent, p2, q, u)
     assert not ref[3].any() and np.array_equal(ref[0], good[0])
+
+
+# ------------------------------------------------------------------ tree attention: CTAs of a call
+
+def kernel_grids(call):
+    """Grid sizes of the kernels that a call enqueues, from its capture."""
+    from cuda.bindings import driver
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        call()
+
+    def good(res):
+        assert res[0] == driver.CUresult.CUDA_SUCCESS
+        return res[1:]
+    raw = driver.CUgraph(graph.raw_cuda_graph())
+    nodes = good(driver.cuGraphGetNodes(raw, good(driver.cuGraphGetNodes(raw))[1]))[0]
+    params = [good(driver.cuGraphKernelNodeGetParams(x))[0] for x in nodes]
+    return [x.gridDimX * x.gridDimY * x.gridDimZ for x in params]
+
+
+@pytest.mark.parametrize("N,T", [(1, 64), (16, 128), (1, 1), (70, 130)])
+@pytest.mark.parametrize("B", [148, 149, 200, 296, 600])
+def test_many_short_units_use_every_sm(B, N, T):
+    """A unit (one KV head of a sequence) is work for a CTA however short it is: with 148 units and more all 148 SMs get some."""
+    b = ngc()
+    c, q, tk, tv, parent, _ = case(bf16, 128, 2, 1, 1, [T] * B, N, "tree", seed=1)
+    dc, st = device_cache(c), b.new_status()
+    dev = [x.cuda() for x in (q, tk, tv, torch.as_tensor(parent))]
+    out = torch.zeros(q.shape, dtype=f32, device="cuda")
+    ws = b.alloc_workspace(b.workspace_bytes(b.OP_TREE_ATTN, dc, n_max=N))
+
+    def call():
+        b.ngc_tree_attn(dc, *dev, out, ws=ws, status=st)
+    call()
+    grids = kernel_grids(call)
+    assert len(grids) == b.tree_attn_launches(dc, N) and grids[0] >= 148 and status_value(st) == 0
