@@ -475,17 +475,19 @@ int ngc_decode_attn_ragged_static(ngc_cache* c, const void* q, const void* new_k
  * in every run; where one lies in its last bits may depend on the lengths of
  * the call's other sequences (they decide how the work is cut).  A length
  * outside 0 .. capacity is reported (NGC_DEV_BAD_COUNTS) and the sequence
- * skipped.  The workspace is free again when the call has run: calls that may
- * run at the same time (other streams, graphs) need one each.  q, tree_k, tree_v,
- * out, k and v must be 16-byte aligned.  Workspace:
- * ngc_workspace_bytes(NGC_OP_TREE_ATTN, c, 1, N, 0), which also serves calls
- * that give a smaller max_len.
+ * skipped.  A bf16 call is refused (NGC_ERR_UNSUPPORTED) if its layers, KV heads
+ * and sequences make some 190 million strips or more.  The workspace is free
+ * again when the call has run: calls that may run at the same time (other
+ * streams, graphs) need one each.  q, tree_k, tree_v, out, k and v must be 16-byte
+ * aligned.  Workspace: ngc_workspace_bytes(NGC_OP_TREE_ATTN, c, 1, N, 0), which
+ * also serves calls that give a smaller max_len.
  */
 int ngc_tree_attn(const ngc_cache* c, const void* q, const void* tree_k, const void* tree_v, const int32_t* parent,
                   const int32_t* n_nodes, int N, int layer_begin, int layer_end, float scale, void* out, int out_dtype,
                   void* ws, size_t ws_bytes, int32_t* dev_status, ngc_stream stream);
 
-/* Number of kernels one ngc_tree_attn call over `layers` layers of this cache enqueues (host-only planning query). */
+/* Number of kernels one ngc_tree_attn call over `layers` layers of this cache enqueues (host-only planning query; 0: none, the
+ * call would be refused). */
 int ngc_tree_attn_launches(const ngc_cache* c, int layers, int N);
 
 /* ngc_tree_attn over a paged cache.  A page-table entry outside 0 .. pages_cap-1 is reported as

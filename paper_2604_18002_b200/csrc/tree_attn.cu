@@ -360,6 +360,15 @@ TreePlan tree_plan(const ngc_cache* c, int layers, int N) {
   return pl;
 }
 
+// Whether the line of tiles of a call on the tensor cores can be counted in 32 bits: each unit has its beginning, its tree's tiles and
+// the cache tile that it shares with nobody; all other cache tiles are full.
+bool tree_line_fits(const ngc_cache* c, const TreePlan& pl, int layers, int N) {
+  if (c->dtype != NGC_BF16) return true;
+  const int keys = tree_umma_keys(pl.tiles_m);
+  const double strips = (double)layers * c->Hkv * pl.blocks;
+  return strips * ((double)c->B * (tree_unit_cost(pl.tiles_m) + 1 + (N + keys - 1) / keys) + (double)c->rows / keys) < 2147483647.0;
+}
+
 // Scratch of one call: the parts' sums, their (m, l), the plan.
 struct TreeScratch { size_t ml, plan, bytes; };
 TreeScratch tree_scratch(const ngc_cache* c, const TreePlan& pl, int layers, int N) {
@@ -394,6 +403,7 @@ int tree_impl(const ngc_cache* c, const PagedView& pv, const void* q, const void
   p.page_table = pv.table; p.page = pv.page; p.pages_cap = pv.pages_cap; p.lists = pv.lists;
   p.G = lists_G(pv.lists, c->L, c->Hkv); p.lens_lists = c->lens_lists;
   const TreePlan plan = tree_plan(c, p.n_layers, N);
+  if (!tree_line_fits(c, plan, p.n_layers, N)) return NGC_ERR_UNSUPPORTED;
   p.row_blocks = plan.blocks; p.n_split = plan.n_split; p.block_rows = plan.block_rows;
   p.tiles_m = plan.tiles_m;
   p.even = plan.even; p.cut = plan.cut; p.cluster = plan.cluster; p.grid = plan.grid; p.n_units = plan.n_units; p.plan = nullptr;
@@ -451,6 +461,7 @@ extern "C" int ngc_tree_attn_launches(const ngc_cache* c, int layers, int N) {
   using namespace ngc;
   if (!valid_cache(c) || layers < 1 || N < 1 || N > kTreeMaxNodes) return 0;
   const TreePlan pl = tree_plan(c, layers, N);
+  if (!tree_line_fits(c, pl, layers, N)) return 0;
   return pl.n_split > 1 || pl.cut ? 2 : 1;
 }
 

@@ -114,6 +114,8 @@ __device__ __forceinline__ void tree_store_out4(const TreeAttnParams& p, int64_t
 // keys of a tile.
 __host__ __device__ constexpr int tree_umma_tiles(int rows) { return rows <= 128 ? 1 : 2; }
 __host__ __device__ constexpr int tree_umma_keys(int tiles) { return tiles == 1 ? 64 : 128; }
+// What beginning another unit costs a CTA, in tiles: the row sums leave, Q changes.
+__host__ __device__ constexpr int tree_unit_cost(int tiles_m) { return tiles_m == 1 ? 9 : 5; }
 constexpr int kTreeMaxCluster = 8;
 int launch_tree_umma(const TreeAttnParams& p, cudaStream_t stream);
 

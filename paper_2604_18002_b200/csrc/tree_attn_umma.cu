@@ -77,8 +77,7 @@ template <int D, int MT> struct Cfg {
   static constexpr int kTile = kKeys * D * 2;              // K or V tile
   static constexpr int kQBytes = 128 * D * 2;              // Q of an M tile
   static constexpr int kSmem = MT * kQBytes + 2 * kStages * kTile + 1024;
-  // What beginning another unit costs a CTA, in tiles: the row sums leave, Q changes.
-  static constexpr int kUnitCost = MT == 1 ? 9 : 5;
+  static constexpr int kUnitCost = tree_unit_cost(MT);
   static_assert(kUnitCost >= tree_min_tiles(MT));          // a unit is enough for a CTA
   static_assert(128 * MT * D * 4 <= 2 * kStages * kTile);  // a part of a cluster lies over the rings
   static constexpr uint32_t kOCol = 128 * kGroups;         // S[group][buf] at 128 group + 64 buf, O[group] behind
