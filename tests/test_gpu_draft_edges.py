@@ -7,7 +7,7 @@ import torch
 from helpers import ngc, status_value
 from oracle import draft
 from paper_2604_18002_b200 import synth
-from test_gpu_draft import bound, case, check_verify, device_cache, draft_case, run_verify
+from test_gpu_draft import bound, case, check_verify, device_cache, draft_case, run_tree, run_verify
 
 pytestmark = pytest.mark.gpu
 
@@ -141,3 +141,118 @@ def test_many_short_units_use_every_sm(B, N, T):
     call()
     grids = kernel_grids(call)
     assert len(grids) == b.tree_attn_launches(dc, N) and grids[0] >= 148 and status_value(st) == 0
+
+
+# ------------------------------------------------------------------ tree attention: units that are cut and joined by a second kernel
+
+CUT = [  # d, Hq, Hkv, N, lens: few long sequences, many units, one and two M tiles
+    (128, 12, 2, 6, [16100, 900]), (64, 12, 2, 6, [20000]), (128, 12, 2, 40, [13000, 70]), (128, 4, 2, 16, [700 - 7 * i % 300 for i in range(80)]),
+    (128, 4, 2, 70, [300 - 11 * i % 300 for i in range(80)])]
+
+
+def cut_job(d, Hq, Hkv, N, lens, seed=0):
+    """A call that cuts its units, with outputs, workspace and status of its own."""
+    b = ngc()
+    c, q, tk, tv, parent, _ = case(bf16, d, Hq, Hkv, 1, lens, N, "tree", seed=seed)
+    dc, st = device_cache(c), b.new_status()
+    assert b.tree_attn_launches(dc, N) == 2
+    dev = [x.cuda() for x in (q, tk, tv, torch.as_tensor(parent))]
+    out = torch.zeros(q.shape, dtype=f32, device="cuda")
+    ws = b.alloc_workspace(b.workspace_bytes(b.OP_TREE_ATTN, dc, n_max=N))
+
+    def run(ws=ws):
+        b.ngc_tree_attn(dc, *dev, out, ws=ws, status=st)
+    return run, out, st, dev, ws, (c, q, tk, tv, parent)
+
+
+def within_bound(out, c, q, tk, tv, parent, n_nodes=None):
+    ref = draft.tree_attn(synth.to_numpy(c.k), synth.to_numpy(c.v), c.seq_off.numpy(), c.lens.numpy(), *[synth.to_numpy(x) for x in (q, tk, tv)],
+                          parent, n_nodes)
+    return bool((np.abs(out.cpu().numpy() - ref) <= bound(c, q, tk, tv, parent, n_nodes, ref)).all())
+
+
+def test_cut_calls_on_two_streams_at_once():
+    jobs = [(cut_job(*x, seed=i), torch.cuda.Stream()) for i, x in enumerate(CUT)]
+    want = []
+    for (run, out, st, *_), _ in jobs:
+        run()
+        want.append(out.clone())
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for (run, out, *_), s in jobs:
+            out.zero_()
+            s.wait_stream(torch.cuda.current_stream())
+        for (run, *_), s in jobs:
+            with torch.cuda.stream(s):
+                run()
+                run()
+        for _, s in jobs:
+            torch.cuda.current_stream().wait_stream(s)
+        for ((_, out, st, *_), _), w in zip(jobs, want):
+            assert status_value(st) == 0 and torch.equal(out, w)
+
+
+@pytest.mark.parametrize("i", range(len(CUT)))
+def test_cut_calls_from_memory_and_from_l2(i):
+    run, out, st, _, _, host = cut_job(*CUT[i], seed=20 + i)
+    flush = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    first = None
+    for r in range(12):
+        out.zero_()
+        if r % 4 < 3:
+            flush.fill_(r)
+        run()
+        first = out.clone() if first is None else first
+        assert torch.equal(out, first)
+    assert status_value(st) == 0 and within_bound(out, *host)
+
+
+def test_cut_calls_in_graphs():
+    """Two captured calls replay on new inputs: at once on two streams, each with its workspace; and, captured with one workspace
+    between them, one after the other."""
+    b = ngc()
+    jobs = [cut_job(*CUT[i], seed=40 + i) for i in (0, 2)]
+    shared = max((x[4] for x in jobs), key=lambda w: w.numel())
+    graphs = []
+    for run, *_ in jobs:
+        run()
+        for kw in ({}, dict(ws=shared)):
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1]):
+                run(**kw)
+    side = torch.cuda.Stream()
+    for seed in (1, 2):
+        want = []
+        for run, out, st, dev, _, _ in jobs:
+            dev[0].copy_(synth.normal(dev[0].shape, seed, bf16))
+            run()
+            want.append(out.clone())
+            out.zero_()
+        side.wait_stream(torch.cuda.current_stream())
+        graphs[0].replay()
+        with torch.cuda.stream(side):
+            graphs[2].replay()
+        torch.cuda.current_stream().wait_stream(side)
+        for (_, out, st, *_), w in zip(jobs, want):
+            assert status_value(st) == 0 and torch.equal(out, w)
+            out.zero_()
+        graphs[1].replay()
+        graphs[3].replay()
+        for (_, out, st, *_), w in zip(jobs, want):
+            assert status_value(st) == 0 and torch.equal(out, w)
+
+
+@pytest.mark.parametrize("N,lens,max_len", [(16, [250, 0, 1, 64, 129, 300], 32768), (16, [250, 0, 1, 64, 129, 300] * 12, 8192), (70, [250, 0, 1, 64], 1 << 20),
+                                            (1, [1], 1 << 20), (1, [0], 1 << 30), (40, [300] * 30, 8192)])
+def test_lengths_far_below_max_len(N, lens, max_len):
+    """A pruned cache: max_len says nothing about the lengths.  The plan cuts units that turn out to be short; most CTAs get none."""
+    b = ngc()
+    c, q, tk, tv, parent, _ = case(bf16, 128, 12, 2, 1, lens, N, "tree", seed=N)
+    dc = device_cache(c)
+    dc.max_len = max_len
+    assert b.tree_attn_launches(dc, N) == 2
+    out, st = run_tree(c, q, tk, tv, parent, None, max_len=max_len)
+    assert st == 0 and within_bound(out, c, q, tk, tv, parent)
+    none = np.zeros(len(lens), np.int32)
+    out, st = run_tree(c, q, tk, tv, parent, none, max_len=max_len)                      # no tree has a node: no work at all
+    assert st == 0 and (out == -7).all()
