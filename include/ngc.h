@@ -501,8 +501,8 @@ int ngc_tree_attn_paged(const ngc_paged_cache* c, const void* q, const void* tre
  * random numbers (multi-round speculative sampling: the token sequence that
  * comes out is distributed as if sampled from the target).  The walk starts
  * at node 0 and tries the children of the current node in index order; at a
- * node with target row p and draft row q, starting from w = p and S = 1, child
- * i with token x = tokens[b][i] and u = uniforms[b][i]:
+ * node with target row p and draft row q, starting from w = max(p, 0) and S = 1,
+ * child i with token x = tokens[b][i] and u = uniforms[b][i]:
  *   draft_probs given (children drawn independently from q):
  *     accepted iff u * q(x) * S < w(x);  else w <- max(w - S q, 0), S <- sum w
  *   draft_probs NULL (children picked without chance, e.g. the likeliest tokens):

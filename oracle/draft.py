@@ -80,6 +80,8 @@ def verify_draft(tokens, parent, target, uniforms, draft=None, n_nodes=None, gre
         while True:
             w, mass = target[b, cur].astype(np.float64), 1.0
             q = None if draft is None else draft[b, cur].astype(np.float64)
+            if not greedy:
+                w[w < 0] = 0.0
             if greedy and np.isnan(w).any():
                 status[b] = 9
                 break

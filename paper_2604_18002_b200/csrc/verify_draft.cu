@@ -63,6 +63,13 @@ struct VerifyShared {
   int last;
 };
 
+// max that keeps a NaN
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+
 // What is left of the current node's row after the rejections so far.
 template <int MODE> struct Residual {
   const float* p;
@@ -72,8 +79,8 @@ template <int MODE> struct Residual {
   uint32_t tried[kWords];                            // without: children whose token has no mass left
   // of a token that has not been tried
   __device__ __forceinline__ double of(float pv, float qv) const {
+    if constexpr (MODE != kModeDraft) return (double)max_nan(pv, 0.f);
     const double w = (double)pv;
-    if constexpr (MODE != kModeDraft) return w;
     const double rest = __dsub_rn(w, __dmul_rn(c, (double)qv));
     return rest < 0.0 ? 0.0 : rest;                  // a NaN stays one
   }

@@ -256,3 +256,26 @@ def test_lengths_far_below_max_len(N, lens, max_len):
     none = np.zeros(len(lens), np.int32)
     out, st = run_tree(c, q, tk, tv, parent, none, max_len=max_len)                      # no tree has a node: no work at all
     assert st == 0 and (out == -7).all()
+
+
+@pytest.mark.parametrize("drafted", [False, True])
+@pytest.mark.parametrize("V", [5, 1000, 50001])
+def test_negative_numbers_of_a_summed_row_count_as_zeros(V, drafted):
+    """In the last node's row, of an only node and behind a refused child.  A row of nothing else has no positive sum."""
+    for seed, (N, x) in enumerate([(1, -1e-6), (1, -3.0), (3, -1e-6), (3, -3.0), (3, -0.0)]):
+        tokens, parent, p, q, u = draft_case(4, N, V, "star", "draft", 10 * V + seed)
+        tokens[:, 1:] = 1
+        u[:, 1:] = 1.0 - 2.0 ** -24
+        q[:, :, 1] = 1.0                                      # u q(1) stays above p(1): every child is refused
+        dr = q if drafted else None
+        p[2, 0, V // 2:] = 0.0
+        good = check_verify(tokens, parent, p, dr, u)
+        assert (good[1] == 1).all() and not good[3].any()
+        p2 = p.copy()
+        p2[2, 0, V // 2:] = x
+        ref = check_verify(tokens, parent, p2, dr, u)
+        assert all(np.array_equal(a, r) for a, r in zip(ref, good))
+        p2[2, 0] = x
+        p2[2, 0, 1] = 0.0                                     # (of the refused child's token: it is tested)
+        ref = check_verify(tokens, parent, p2, dr, u)
+        assert ref[3].tolist() == [0, 0, 9, 0]
