@@ -12,7 +12,8 @@
 // rows x 8 channels of O per thread at d = 128: 32 multiply-adds per 8 shared-memory wavefronts), blocks of at most 16 rows
 // 32 lanes (twice the threads per row: those calls wait for memory, not for arithmetic).  One pass over K and V; with few
 // items the key axis is split and a second kernel joins the parts.  32 sequences of 4096 tokens, 8 nodes, 4 heads, d = 128:
-// 158 us (537 MB: 3.4 TB/s; shared memory feeds the multiply-adds); 4 sequences of 300 to 512 tokens: 14 us, all latency.
+// 154 us (539 MB: 3.5 TB/s; shared memory feeds the multiply-adds); 4 sequences of 300 to 512 tokens: 14 us, all latency; one of
+// 8192 / 32768 tokens, one node: 51 / 78 us, most of it the join, which takes the parts of a row one after the other.
 #include <cuda_bf16.h>
 
 #include "ngc_plan.h"

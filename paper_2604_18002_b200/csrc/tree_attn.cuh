@@ -119,7 +119,7 @@ __host__ __device__ constexpr int tree_unit_cost(int tiles_m) { return tiles_m =
 constexpr int kTreeMaxCluster = 8;
 int launch_tree_umma(const TreeAttnParams& p, cudaStream_t stream);
 
-// Even split of `total` tiles: how many of `grid` CTAs take part (each gets so many tiles at least that joining its part costs
+// Even split of `total` tiles, beginnings of units counted in: how many of `grid` CTAs take part (each gets so many tiles at least that joining its part costs
 // less than it saves: one sequence of 16384 tokens under one node, 64-key tiles: 35 us with three), the first tile of CTA c, and the
 // CTA that has tile g.
 __host__ __device__ constexpr int tree_min_tiles(int tiles_m) { return tiles_m == 1 ? 8 : 3; }

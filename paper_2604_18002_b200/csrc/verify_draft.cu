@@ -18,7 +18,7 @@
 // What bounds it: a rejection is a pass over two rows that waits for the one before.  One sequence, 131072 tokens: 9.3 us
 // with none (launch, tree, one pass, draw), then 1.8 us each.  64 sequences: 15 us with none (a row each, 34 MB), 31 us
 // with up to five, whose rows come from L2 after the first time.  Without draft rows there is one pass, the last: 48
-// sequences of 50001 tokens and 33 nodes take 9.8 us (19.5 us when tried tokens were a list that every thread searched for
+// sequences of 50001 tokens and 33 nodes take 9.9 us (19.5 us when tried tokens were a list that every thread searched for
 // every token).
 #include <cooperative_groups.h>
 

@@ -106,7 +106,9 @@ class NgcRollout:
 
     def draft_attention(self, q: torch.Tensor, tree_k: torch.Tensor, tree_v: torch.Tensor, parent: torch.Tensor, out: torch.Tensor,
                         n_nodes: Optional[torch.Tensor] = None, layer_begin: int = 0, layer_end: Optional[int] = None):
-        """Attention of every node of the drafted trees over the cache, its ancestors and itself; the cache is not changed."""
+        """Attention of every node of the drafted trees over the cache, its ancestors and itself; the cache is not changed.  The
+        calls of one rollout with the same node count share a workspace, captured ones included: let one end before the next
+        begins (on one stream they do)."""
         N = parent.shape[1]
         if N not in self.ws_tree:
             if torch.cuda.is_current_stream_capturing():
