@@ -517,7 +517,8 @@ int ngc_tree_attn_paged(const ngc_paged_cache* c, const void* q, const void* tre
  *   target_probs [B][N][vocab] fp32: row i follows node i.  Rows are taken as
  *                normalised; whole rows are read only where the walk comes.
  *                vocab <= 2^30
- *   draft_probs  [B][N][vocab] fp32 or NULL: row i is what node i's children were drawn from
+ *   draft_probs  [B][N][vocab] fp32 or NULL: row i is what node i's children were drawn from; no
+ *                negative numbers (looked at for tested children only)
  *   uniforms     [B][N] fp32 in [0, 1) (may be NULL if greedy)
  *   path         [B][N] out: accepted nodes from node 0 on, -1 padded (ascending)
  *   n_path       [B] out: their number (>= 1; 0 for an empty tree)

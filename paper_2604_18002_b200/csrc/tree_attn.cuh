@@ -119,9 +119,9 @@ __host__ __device__ constexpr int tree_unit_cost(int tiles_m) { return tiles_m =
 constexpr int kTreeMaxCluster = 8;
 int launch_tree_umma(const TreeAttnParams& p, cudaStream_t stream);
 
-// Even split of `total` tiles, beginnings of units counted in: how many of `grid` CTAs take part (each gets so many tiles at least that joining its part costs
-// less than it saves: one sequence of 16384 tokens under one node, 64-key tiles: 35 us with three), the first tile of CTA c, and the
-// CTA that has tile g.
+// Even split of `total` tiles, beginnings of units counted in: how many of `grid` CTAs take part (each gets so many tiles at
+// least that joining its part costs less than it saves: one sequence of 16384 tokens under one node, 64-key tiles: 25 us, 35 us
+// with three), the first tile of CTA c, and the CTA that has tile g.
 __host__ __device__ constexpr int tree_min_tiles(int tiles_m) { return tiles_m == 1 ? 8 : 3; }
 __host__ __device__ inline int tree_even_ctas(int total, int grid, int tiles_m) {
   const int most = total / tree_min_tiles(tiles_m);

@@ -35,14 +35,14 @@
 // parts through distributed shared memory.
 //
 // What bounds it: up to 128 rows, DRAM in the steady state and some 12 us around it (64 sequences of 2048 / 4096 tokens, 142 /
-// 276 MB: 31.7 / 50.6 us, the difference at 7.1 TB/s; of 8192, cut: 102 us, 5.2 TB/s more), and the longest unit where lengths differ
-// (1024 to 4096 tokens, 173 MB: 47 us); few sequences see what a tile takes its CTA, some 800 cycles.
+// 276 MB: 31.7 / 50.6 us, the difference at 7.1 TB/s; of 8192, cut: 102 us, the difference at 5.2 TB/s), and the longest unit where
+// lengths differ (1024 to 4096 tokens, 173 MB: 47 us); few sequences see what a tile takes its CTA, some 800 cycles.
 // (One softmax group and S one tile ahead: 1450 cycles.  Two CTAs per SM of two stages and one group each: 2 to 10 % slower
 // from 320 sequences on but for short ragged ones, 81 and 84 us for 512 of 200 to 500 tokens.)  More rows: the chain
 // S -> softmax -> P -> O of a tile (3100 cycles per 128 keys and 256 rows, 2550 of them without any softmax arithmetic; the products
 // alone are 2048 cycles of the tensor pipe), the beginnings of units, and M tiles without rows: 131072
 // tokens under 64 nodes, 12 heads (384 rows: three of four M tiles), two layers in 129 us, 800 TFLOP/s, for the first 60 ms of a row of
-// calls and 152 to 156 us, 670 TFLOP/s, from then on, under the power limit.
+// calls and 152 to 156 us, 670 TFLOP/s, from then on (1000 W, 1650 of 1965 MHz).
 //
 // bf16 P: one rounding per weight (2^-8), as in the decode and replay calls; the row sum takes the weights
 // before it.  0 x V must be 0 whatever a dead V row holds: rows of the last 16-row box beyond the live ones are
