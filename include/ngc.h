@@ -85,7 +85,9 @@ typedef enum {
   NGC_DEV_BAD_TREE = 8,       /* a node count, parent link, drafted token or accepted path that is none */
   NGC_DEV_BAD_PROBS = 9,      /* numbers that are no probabilities, or have no finite positive sum */
   NGC_DEV_BAD_SOURCE = 10,    /* a fork's source is no sequence, or is itself a destination */
-  NGC_DEV_BAD_PAGE = 11       /* a page-table entry outside 0 .. pages_cap-1 */
+  NGC_DEV_BAD_PAGE = 11,      /* a page-table entry outside 0 .. pages_cap-1 (of a pool: 0 .. n_pages-1) */
+  NGC_DEV_POOL_FULL = 12,     /* a pool has fewer free pages than a sequence needs */
+  NGC_DEV_BAD_SLOT = 13       /* a slot outside the pool */
 } ngc_dev_status;
 
 typedef enum { NGC_F32 = 0, NGC_BF16 = 1 } ngc_dtype;
@@ -570,6 +572,145 @@ int ngc_fork_kv(ngc_cache* c, const int32_t* src_of, int32_t* dev_status, ngc_st
  * first pages of b's own table (the tables do not change).  A bad page-table entry among them (NGC_DEV_BAD_PAGE) leaves
  * b's lengths as they were; the rows of the lists whose entries are good may have been copied. */
 int ngc_fork_pages(ngc_paged_cache* c, const int32_t* src_of, int32_t* dev_status, ngc_stream stream);
+
+/*
+ * Latent attention.  (The paper's models give every KV head rows of its own;
+ * these calls serve models whose heads share ONE row per token and layer: a
+ * latent vector c_j that every head's key and value are projections of, and a
+ * rotary part r_j.)  With qn, qr the two parts of a head's query and U_h, W_h
+ * its projections of the latent to a key and a value, the EXPANDED form is
+ *   z_hj = scale * (qn_h . (U_h c_j) + qr_h . r_j),   out_h = sum_j softmax(z)_hj W_h c_j;
+ * taking U_h into the query, ql_h = U_h^T qn_h, and W_h behind the sum gives
+ * the ABSORBED form, which reads nothing but the shared rows:
+ *   z_hj = scale * (ql_h . c_j + qr_h . r_j),         o_h = sum_j softmax(z)_hj c_j,   out_h = W_h o_h.
+ * Generation uses the absorbed form over a pool of pages (ngc_pool_update ->
+ * ngc_latent_write -> ngc_latent_decode per step), prompts and training the
+ * expanded one over whole sequences (ngc_latent_replay_attn and its gradient).
+ * The projections themselves are the caller's matrix products.  Built for bf16.
+ */
+
+/* Rows in pages of a COMMON pool: any page may serve any sequence, so pages that
+ * eviction or a finished sequence frees go on to others.  As everywhere a
+ * sequence has G eviction lists (`lists`, with one KV head: SHARED: G = 1,
+ * otherwise G = L); list gi has its own free pages, the same n_pages in every
+ * layer it covers.  Owns nothing. */
+typedef struct {
+  void* rows;            /* [L][n_pages][page][d_latent + d_rope] bf16, 16-byte aligned */
+  int32_t* page_table;   /* [B][G][pages_cap]: page j of list gi of sequence b; entries at and beyond ceil(len / page) are -1 */
+  uint8_t* page_used;    /* [G][n_pages]: 0 = free */
+  int32_t* lens;         /* [B][G] alive tokens */
+  int32_t L, B;
+  int32_t d_latent;      /* 128, 256, 384 or 512 */
+  int32_t d_rope;        /* 16, 32, 48 or 64 */
+  int32_t dtype;         /* NGC_BF16 */
+  int32_t page;          /* tokens per page, 32 or 64 */
+  int32_t pages_cap, n_pages, lists;   /* L * n_pages * page < 2^31 */
+} ngc_latent_pool;
+
+/*
+ * The pool's books for the next step, in one launch and for every list on its
+ * own: what an eviction round keeps, what finished sequences give back, pages
+ * for the new tokens and where each of them goes.  For sequence b:
+ *   budget[b] >= 0:  only the units (= pages) kept_sorted[b][gi][0 .. budget[b]) stay: they move to the front of the table
+ *                    row in that order, the others return to the pool, the length becomes what was kept (a short last page
+ *                    stays last); budget[b] = -1, or kept_sorted NULL: no eviction
+ *   n_new[b] >= 0:   the sequence grows by n_new[b] tokens;  n_new[b] = -1: it is finished, its pages return to the pool, its
+ *                    length becomes 0
+ * All returns come before all growth; growth takes the lowest free page numbers
+ * in order of sequences.  Token t of sequence b's new ones is number first[b] + t.
+ *   n_new [B];  kept_sorted [B][G][k_max] as written by ngc_sample_evict, budget [B], or both NULL
+ *   slots [G][n_slots] out: page * (tokens per page) + place in the page of every new token; -1 from first[B] on
+ *   first [B+1] out: new tokens of the sequences before
+ * Per list, a sequence with counts that are none (NGC_DEV_BAD_COUNTS: also more
+ * new tokens than n_slots holds), a bad kept list (NGC_DEV_BAD_KEPT) or page-table entry
+ * (NGC_DEV_BAD_PAGE) is left as it was; one that outgrows pages_cap
+ * (NGC_DEV_STRIP_FULL) or the free pages (NGC_DEV_POOL_FULL) evicts but does
+ * not grow.  Their new tokens get slot -1.  B <= 8192.
+ */
+int ngc_pool_update(ngc_latent_pool* c, const int32_t* kept_sorted, const int32_t* budget, int k_max, const int32_t* n_new,
+                    int32_t* slots, int n_slots, int32_t* first, int32_t* dev_status, ngc_stream stream);
+
+/*
+ * Writes the rows of new tokens to their slots, for layers [layer_begin, layer_end): bit-exact copies.
+ *   latent [L][n_slots][d_latent], rope [L][n_slots][d_rope] bf16, 16-byte aligned; slots [G][n_slots] as written by ngc_pool_update
+ * Slot -1: no row; a slot beyond the pool is reported (NGC_DEV_BAD_SLOT) and skipped.  A slot that occurs twice gets one of its
+ * rows, or pieces of both.
+ */
+int ngc_latent_write(ngc_latent_pool* c, const int32_t* slots, int n_slots, const void* latent, const void* rope,
+                     int layer_begin, int layer_end, int32_t* dev_status, ngc_stream stream);
+
+/*
+ * Absorbed form for one token per sequence, over the alive rows of the pool (the
+ * token's own row among them: written before), for layers [layer_begin, layer_end):
+ *   q_latent [L][B][H][d_latent], q_rope [L][B][H][d_rope] bf16, 16-byte aligned;  H 1 .. 128
+ *   scale    positive, at most 2e38
+ *   out      [L][B][H][d_latent] of out_dtype (NGC_F32 or NGC_BF16), 16-byte aligned; an empty sequence gives zeros
+ * fp32 scores, softmax and sums; the probabilities are rounded to bf16 for the
+ * second product.  Rows of a page behind the length take no part whatever they
+ * hold.  A length outside 0 .. pages_cap * page is reported (NGC_DEV_BAD_COUNTS) and the
+ * sequence skipped; a bad page-table entry is reported (NGC_DEV_BAD_PAGE) and the
+ * outputs of its sequence are unspecified.  Results are the same in every run; where one lies in its
+ * last bits may depend on the call's other lengths (they decide how the work is
+ * cut).  Calls that may run at the same time need a workspace each.
+ * Workspace: ngc_latent_decode_workspace_bytes (reads L, B, d_latent only).
+ */
+int ngc_latent_decode(const ngc_latent_pool* c, const void* q_latent, const void* q_rope, int H, int layer_begin, int layer_end,
+                      float scale, void* out, int out_dtype, void* ws, size_t ws_bytes, int32_t* dev_status, ngc_stream stream);
+size_t ngc_latent_decode_workspace_bytes(const ngc_latent_pool* c, int H);
+
+/* Whole sequences in token-major rows, as projections write them: sequence b owns rows seq_off[b] .. seq_off[b+1], the first
+ * lens[b] of which are tokens.  Rows that are no tokens are neither read into results nor written. */
+typedef struct {
+  const int64_t* seq_off;    /* [B+1], seq_off[0] = 0, seq_off[B] = rows */
+  const int32_t* lens;       /* [B] */
+  int64_t rows;              /* host copy; L * rows < 2^31 */
+  int32_t L, B, H;
+  int32_t d_nope, d_v;       /* 128 */
+  int32_t d_rope;            /* 16, 32, 48 or 64 */
+  int32_t dtype;             /* NGC_BF16 */
+  int32_t max_len;           /* host bound on lens */
+} ngc_latent_seqs;
+
+/*
+ * Expanded form for whole sequences under their history of evictions, the
+ * counterpart of ngc_replay_attn: the query at position t sees key j iff j <= t
+ * and no round at or before t has evicted j.
+ *   q      [L][rows][H][d_nope + d_rope];  kv [L][rows][H][d_nope + d_v]: every head's key part and value;
+ *   k_rope [L][rows][d_rope]: one rotary key part for all heads; all bf16, 16-byte aligned
+ *   alive_pos [n_rounds][B][G][kt_max], alive_count [n_rounds][B][G], total_before [n_rounds][B] as for ngc_replay_attn
+ *          (ascending per sequence; G by `lists` with one KV head); n_rounds = 0: causal attention (prompts).  A position that
+ *          a round has evicted does not come back: a later round's list that names it again makes it count as never evicted
+ *          in between.  A bad count or position is reported (NGC_DEV_BAD_KEPT) and ignored.
+ *   scale  positive, at most 2e38
+ *   out    [L][rows][H][d_v] of out_dtype (NGC_F32 or NGC_BF16), 16-byte aligned
+ *   lse    [L][H][rows] fp32 or NULL: log of the sum of exp(z) of every query, for the gradient (-inf for a query that sees nothing,
+ *          whose output is zero)
+ * fp32 scores, softmax and sums; probabilities rounded to bf16 for the second
+ * product.  Infinities or NaN in a sequence's rows leave its results
+ * unspecified, other sequences' untouched.  A length outside its sequence's rows or above max_len is
+ * reported (NGC_DEV_BAD_COUNTS) and the sequence skipped.
+ * Workspace: ngc_latent_replay_workspace_bytes(s, lists, n_rounds, 0).
+ */
+int ngc_latent_replay_attn(const ngc_latent_seqs* s, const void* q, const void* kv, const void* k_rope,
+                           const int32_t* alive_pos, const int32_t* alive_count, const int32_t* total_before, int n_rounds,
+                           int kt_max, int lists, float scale, void* out, int out_dtype, float* lse,
+                           void* ws, size_t ws_bytes, int32_t* dev_status, ngc_stream stream);
+
+/*
+ * Gradient of ngc_latent_replay_attn with respect to q, kv and k_rope (for the latter summed over the heads that share it):
+ *   P = exp(z - lse),  D = sum_c grad_out * out,  dV = P^T grad_out,  dz = scale P (grad_out V^T - D),
+ *   dQ = dz K,  dK = dz^T Q.
+ *   out, lse as the forward call wrote them; grad_out [L][rows][H][d_v] bf16
+ *   grad_q, grad_kv, grad_k_rope: bf16 in the shapes of q, kv, k_rope; rows of tokens are written, no others
+ * P and dz are rounded to bf16 for the products, every sum is held in fp32 and rounded once.  Results are the same in every run.
+ * Workspace: ngc_latent_replay_workspace_bytes(s, lists, n_rounds, 1); its contents need not be those of the forward call.
+ */
+int ngc_latent_replay_attn_backward(const ngc_latent_seqs* s, const void* q, const void* kv, const void* k_rope,
+                                    const int32_t* alive_pos, const int32_t* alive_count, const int32_t* total_before,
+                                    int n_rounds, int kt_max, int lists, float scale, const void* out, int out_dtype,
+                                    const float* lse, const void* grad_out, void* grad_q, void* grad_kv, void* grad_k_rope,
+                                    void* ws, size_t ws_bytes, int32_t* dev_status, ngc_stream stream);
+size_t ngc_latent_replay_workspace_bytes(const ngc_latent_seqs* s, int lists, int n_rounds, int backward);
 
 /*
  * Self-test of the bounded wait.  (The paper has no counterpart: this is a

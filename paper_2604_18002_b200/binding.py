@@ -24,13 +24,15 @@ OP_SCORE, OP_SAMPLE, OP_LOGPROB, OP_COMPACT, OP_DECODE, OP_SCORE_BACKWARD, OP_TR
 
 DEV_STATUS = {0: "ok", 1: "bad counts", 2: "NaN logit", 3: "bad kept list", 4: "strip full",
               5: "lists disagree", 6: "timeout", 7: "index out of bounds (bounds-checking build)", 8: "bad drafted tree or path",
-              9: "numbers that are no probabilities, or have no finite positive sum", 10: "bad fork source", 11: "bad page-table entry"}
+              9: "numbers that are no probabilities, or have no finite positive sum", 10: "bad fork source", 11: "bad page-table entry",
+              12: "pool has too few free pages", 13: "slot outside the pool"}
 
 EXPORTS = ["ngc_version", "ngc_strerror", "ngc_last_cuda_error", "ngc_workspace_bytes", "ngc_decode_splits", "ngc_score_evict", "ngc_score_evict_launches",
            "ngc_sample_evict", "ngc_evict_logprob", "ngc_evict_logprob_backward", "ngc_compact_kv", "ngc_decode_attn_ragged",
            "ngc_decode_attn_ragged_static", "ngc_evict_pages", "ngc_decode_attn_paged", "ngc_score_evict_paged", "ngc_replay_visibility", "ngc_score_evict_backward", "ngc_replay_attn", "ngc_replay_attn_variant", "ngc_selftest_bounded_wait",
            "ngc_tree_attn", "ngc_tree_attn_paged", "ngc_tree_attn_launches", "ngc_verify_draft", "ngc_commit_draft", "ngc_commit_draft_paged",
-           "ngc_fork_kv", "ngc_fork_pages"]
+           "ngc_fork_kv", "ngc_fork_pages", "ngc_pool_update", "ngc_latent_write", "ngc_latent_decode", "ngc_latent_decode_workspace_bytes",
+           "ngc_latent_replay_attn", "ngc_latent_replay_attn_backward", "ngc_latent_replay_workspace_bytes"]
 STATIC_SCRATCH_BYTES = 8 << 20
 TREE_MAX_NODES = 128
 
@@ -52,6 +54,20 @@ class PagedCacheDesc(C.Structure):
                 ("L", C.c_int32), ("B", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("d", C.c_int32),
                 ("dtype", C.c_int32), ("page", C.c_int32), ("pages_cap", C.c_int32), ("lists", C.c_int32),
                 ("lens_per_list", C.c_int32)]
+
+
+class LatentPoolDesc(C.Structure):
+    """Mirror of ``ngc_latent_pool``."""
+    _fields_ = [("rows", C.c_void_p), ("page_table", C.c_void_p), ("page_used", C.c_void_p), ("lens", C.c_void_p),
+                ("L", C.c_int32), ("B", C.c_int32), ("d_latent", C.c_int32), ("d_rope", C.c_int32), ("dtype", C.c_int32),
+                ("page", C.c_int32), ("pages_cap", C.c_int32), ("n_pages", C.c_int32), ("lists", C.c_int32)]
+
+
+class LatentSeqsDesc(C.Structure):
+    """Mirror of ``ngc_latent_seqs``."""
+    _fields_ = [("seq_off", C.c_void_p), ("lens", C.c_void_p), ("rows", C.c_int64), ("L", C.c_int32), ("B", C.c_int32),
+                ("H", C.c_int32), ("d_nope", C.c_int32), ("d_v", C.c_int32), ("d_rope", C.c_int32), ("dtype", C.c_int32),
+                ("max_len", C.c_int32)]
 
 
 def _load(path: str = LIB_PATH):
@@ -118,6 +134,21 @@ def _load(path: str = LIB_PATH):
     lib.ngc_fork_kv.argtypes = [C.POINTER(CacheDesc), vp, vp, vp]
     lib.ngc_fork_pages.restype = i32
     lib.ngc_fork_pages.argtypes = [C.POINTER(PagedCacheDesc), vp, vp, vp]
+    lib.ngc_pool_update.restype = i32
+    lib.ngc_pool_update.argtypes = [C.POINTER(LatentPoolDesc), vp, vp, i32, vp, vp, i32, vp, vp, vp]
+    lib.ngc_latent_write.restype = i32
+    lib.ngc_latent_write.argtypes = [C.POINTER(LatentPoolDesc), vp, i32, vp, vp, i32, i32, vp, vp]
+    lib.ngc_latent_decode.restype = i32
+    lib.ngc_latent_decode.argtypes = [C.POINTER(LatentPoolDesc), vp, vp, i32, i32, i32, C.c_float, vp, i32, vp, sz, vp, vp]
+    lib.ngc_latent_decode_workspace_bytes.restype = sz
+    lib.ngc_latent_decode_workspace_bytes.argtypes = [C.POINTER(LatentPoolDesc), i32]
+    replay = [C.POINTER(LatentSeqsDesc), vp, vp, vp, vp, vp, vp, i32, i32, i32, C.c_float, vp, i32, vp]
+    lib.ngc_latent_replay_attn.restype = i32
+    lib.ngc_latent_replay_attn.argtypes = replay + [vp, sz, vp, vp]
+    lib.ngc_latent_replay_attn_backward.restype = i32
+    lib.ngc_latent_replay_attn_backward.argtypes = replay + [vp, vp, vp, vp, vp, sz, vp, vp]
+    lib.ngc_latent_replay_workspace_bytes.restype = sz
+    lib.ngc_latent_replay_workspace_bytes.argtypes = [C.POINTER(LatentSeqsDesc), i32, i32, i32]
     return lib
 
 
@@ -555,6 +586,170 @@ def ngc_fork_kv(cache: NgcCache, src_of: torch.Tensor, status: Optional[torch.Te
 def ngc_fork_pages(cache: NgcPagedCache, src_of: torch.Tensor, status: Optional[torch.Tensor] = None):
     """ngc_fork_kv on a paged cache: the source's pages are copied into b's own."""
     _fork("ngc_fork_pages", lib.ngc_fork_pages, cache, src_of, status)
+
+
+# ---------------------------------------------------------------- latent attention
+
+@dataclass
+class NgcLatentPool:
+    """Rows of a latent cache in pages of a common pool (any page may serve any sequence) and the pool's books."""
+    rows: torch.Tensor        # [L][n_pages][page][d_latent + d_rope] bf16
+    page_table: torch.Tensor  # int32 [B][G][pages_cap], -1: no page
+    page_used: torch.Tensor   # uint8 [G][n_pages], 0: free
+    lens: torch.Tensor        # int32 [B][G]
+    d_latent: int
+    lists: int = LISTS_SHARED
+
+    @property
+    def L(self):
+        return self.rows.shape[0]
+
+    @property
+    def B(self):
+        return self.page_table.shape[0]
+
+    @property
+    def d_rope(self):
+        return self.rows.shape[3] - self.d_latent
+
+
+def new_latent_pool(L: int, B: int, d_latent: int, d_rope: int, n_pages: int, pages_cap: int, page: int = 64, lists: int = LISTS_SHARED,
+                    device="cuda") -> NgcLatentPool:
+    """An empty pool: ``n_pages`` pages in every layer for ``B`` sequences of up to ``pages_cap`` pages."""
+    G = lists_G(lists, L, 1)
+    return NgcLatentPool(torch.empty((L, n_pages, page, d_latent + d_rope), dtype=torch.bfloat16, device=device),
+                         torch.full((B, G, pages_cap), -1, dtype=_I32, device=device), torch.zeros((G, n_pages), dtype=_U8, device=device),
+                         torch.zeros((B, G), dtype=_I32, device=device), d_latent, lists)
+
+
+def _pool_view(what: str, pool: NgcLatentPool):
+    """Checks a pool's own tensors; (descriptor, L, B, G, d_rope, device index)."""
+    rows, table = pool.rows, pool.page_table
+    index = rows.get_device()
+    L, n_pages, page, width = rows.shape
+    B, G, cap = table.shape
+    if G != lists_G(pool.lists, L, 1):
+        raise NgcError(f"{what}: page_table {tuple(table.shape)} does not fit rows {tuple(rows.shape)} and the lists")
+    desc = LatentPoolDesc(_arg(what, "rows", rows, rows.shape, torch.bfloat16, index), _arg(what, "page_table", table, table.shape, _I32, index),
+                          _arg(what, "page_used", pool.page_used, (G, n_pages), _U8, index), _arg(what, "lens", pool.lens, (B, G), _I32, index),
+                          L, B, pool.d_latent, width - pool.d_latent, BF16, page, cap, n_pages, pool.lists)
+    return desc, L, B, G, width - pool.d_latent, index
+
+
+def ngc_pool_update(pool: NgcLatentPool, n_new: torch.Tensor, slots: torch.Tensor, first: torch.Tensor, kept_sorted: Optional[torch.Tensor] = None,
+                    budget: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """The pool's books for the next step: eviction (``kept_sorted`` int32 [B][G][k_max], ``budget`` int32 [B], -1: none), finished
+    sequences (``n_new[b]`` = -1), pages for ``n_new[b]`` tokens each, and their ``slots`` int32 [G][n_slots]; ``first`` int32 [B+1]."""
+    what = "ngc_pool_update"
+    desc, _, B, G, _, index = _pool_view(what, pool)
+    k_max = 0 if kept_sorted is None else kept_sorted.shape[-1]
+    args = (_arg(what, "kept_sorted", kept_sorted, (B, G, k_max), _I32, index), _arg(what, "budget", budget, (B,), _I32, index), k_max,
+            _arg(what, "n_new", n_new, (B,), _I32, index), _arg(what, "slots", slots, (G, slots.shape[-1]), _I32, index), slots.shape[-1],
+            _arg(what, "first", first, (B + 1,), _I32, index), _arg(what, "status", status, (1,), _I32, index))
+    _check(lib.ngc_pool_update(C.byref(desc), *args, _launch_stream(what, index)), what)
+
+
+def ngc_latent_write(pool: NgcLatentPool, slots: torch.Tensor, latent: torch.Tensor, rope: torch.Tensor, layer_begin: int = 0,
+                     layer_end: Optional[int] = None, status: Optional[torch.Tensor] = None):
+    """Rows (latent [L][n_slots][d_latent] | rope [L][n_slots][d_rope]) to their ``slots`` [G][n_slots]; slot -1: no row."""
+    what = "ngc_latent_write"
+    desc, L, _, G, d_rope, index = _pool_view(what, pool)
+    n = slots.shape[-1]
+    args = (_arg(what, "slots", slots, (G, n), _I32, index), n, _arg(what, "latent", latent, (L, n, pool.d_latent), torch.bfloat16, index),
+            _arg(what, "rope", rope, (L, n, d_rope), torch.bfloat16, index), layer_begin, L if layer_end is None else layer_end,
+            _arg(what, "status", status, (1,), _I32, index))
+    _check(lib.ngc_latent_write(C.byref(desc), *args, _launch_stream(what, index)), what)
+
+
+def latent_decode_workspace_bytes(pool: NgcLatentPool, H: int) -> int:
+    desc = _pool_view("latent_decode_workspace_bytes", pool)[0]
+    return int(lib.ngc_latent_decode_workspace_bytes(C.byref(desc), H))
+
+
+def ngc_latent_decode(pool: NgcLatentPool, q_latent: torch.Tensor, q_rope: torch.Tensor, out: torch.Tensor, scale: float, layer_begin: int = 0,
+                      layer_end: Optional[int] = None, ws: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """Absorbed latent attention of one token per sequence: q_latent, out [L][B][H][d_latent]; q_rope [L][B][H][d_rope].  ``scale``:
+    one over the root of the EXPANDED key's width.  ``ws``: latent_decode_workspace_bytes(pool, H)."""
+    what = "ngc_latent_decode"
+    desc, L, B, _, d_rope, index = _pool_view(what, pool)
+    H = q_latent.shape[2]
+    heads = (L, B, H, pool.d_latent)
+    args = (_arg(what, "q_latent", q_latent, heads, torch.bfloat16, index), _arg(what, "q_rope", q_rope, (L, B, H, d_rope), torch.bfloat16, index), H,
+            layer_begin, L if layer_end is None else layer_end, scale, _arg(what, "out", out, heads, out.dtype, index), _dtype_code(out),
+            None if ws is None else _arg(what, "ws", ws, ws.shape, _U8, index), 0 if ws is None else ws.numel(),
+            _arg(what, "status", status, (1,), _I32, index))
+    _check(lib.ngc_latent_decode(C.byref(desc), *args, _launch_stream(what, index)), what)
+
+
+@dataclass
+class NgcLatentSeqs:
+    """Whole sequences in token-major rows: sequence b owns rows seq_off[b] .. seq_off[b+1], the first lens[b] are tokens."""
+    seq_off: torch.Tensor  # int64 [B+1], device; seq_off[B] = rows
+    lens: torch.Tensor     # int32 [B], device
+    max_len: int           # host bound on lens
+
+
+def _seqs_view(what: str, seqs: NgcLatentSeqs, q: torch.Tensor, kv: torch.Tensor):
+    """Descriptor of a call on whole sequences; (descriptor, L, rows, H, d_rope, B, device index)."""
+    index = q.get_device()
+    L, rows, H, width = q.shape
+    B = seqs.lens.shape[0]
+    desc = LatentSeqsDesc(_arg(what, "seq_off", seqs.seq_off, (B + 1,), _I64, index), _arg(what, "lens", seqs.lens, (B,), _I32, index), rows, L, B, H,
+                          128, 128, width - 128, BF16, seqs.max_len)
+    return desc, L, rows, H, width - 128, B, index
+
+
+def latent_replay_workspace_bytes(seqs: NgcLatentSeqs, q: torch.Tensor, kv: torch.Tensor, lists: int = LISTS_SHARED, n_rounds: int = 1,
+                                  backward: bool = False) -> int:
+    """Workspace of ngc_latent_replay_attn (or its gradient) for queries and keys of these shapes; ``n_rounds`` 0: causal."""
+    desc = _seqs_view("latent_replay_workspace_bytes", seqs, q, kv)[0]
+    return int(lib.ngc_latent_replay_workspace_bytes(C.byref(desc), lists, n_rounds, int(backward)))
+
+
+def _replay_args(what, seqs, q, kv, k_rope, out, lse, alive_pos, alive_count, total_before, lists, scale):
+    desc, L, rows, H, d_rope, B, index = _seqs_view(what, seqs, q, kv)
+    bf16, G = torch.bfloat16, lists_G(lists, L, 1)
+    R, kt = (0, 0) if alive_pos is None else (alive_pos.shape[0], alive_pos.shape[-1])
+    args = (_arg(what, "q", q, (L, rows, H, 128 + d_rope), bf16, index), _arg(what, "kv", kv, (L, rows, H, 256), bf16, index),
+            _arg(what, "k_rope", k_rope, (L, rows, d_rope), bf16, index), _arg(what, "alive_pos", alive_pos, (R, B, G, kt), _I32, index),
+            _arg(what, "alive_count", alive_count, (R, B, G), _I32, index), _arg(what, "total_before", total_before, (R, B), _I32, index), R, kt,
+            lists, (128 + d_rope) ** -0.5 if scale is None else scale, _arg(what, "out", out, (L, rows, H, 128), out.dtype, index),
+            _dtype_code(out), _arg(what, "lse", lse, (L, H, rows), _F32, index))
+    return desc, args, index
+
+
+def _ws(what, ws, index):
+    return (None, 0) if ws is None else (_arg(what, "ws", ws, ws.shape, _U8, index), ws.numel())
+
+
+def ngc_latent_replay_attn(seqs: NgcLatentSeqs, q: torch.Tensor, kv: torch.Tensor, k_rope: torch.Tensor, out: torch.Tensor,
+                           lse: Optional[torch.Tensor] = None, alive_pos: Optional[torch.Tensor] = None, alive_count: Optional[torch.Tensor] = None,
+                           total_before: Optional[torch.Tensor] = None, lists: int = LISTS_SHARED, scale: Optional[float] = None,
+                           ws: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """Expanded latent attention of whole sequences under their history of evictions (none: causal).  q [L][rows][H][128 + d_rope],
+    kv [L][rows][H][128 + 128], k_rope [L][rows][d_rope] (shared by the heads), out [L][rows][H][128], lse fp32 [L][H][rows]."""
+    what = "ngc_latent_replay_attn"
+    desc, args, index = _replay_args(what, seqs, q, kv, k_rope, out, lse, alive_pos, alive_count, total_before, lists, scale)
+    rc = lib.ngc_latent_replay_attn(C.byref(desc), *args, *_ws(what, ws, index), _arg(what, "status", status, (1,), _I32, index),
+                                    _launch_stream(what, index))
+    _check(rc, what)
+
+
+def ngc_latent_replay_attn_backward(seqs: NgcLatentSeqs, q: torch.Tensor, kv: torch.Tensor, k_rope: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                                    grad_out: torch.Tensor, grad_q: torch.Tensor, grad_kv: torch.Tensor, grad_k_rope: torch.Tensor,
+                                    alive_pos: Optional[torch.Tensor] = None, alive_count: Optional[torch.Tensor] = None,
+                                    total_before: Optional[torch.Tensor] = None, lists: int = LISTS_SHARED, scale: Optional[float] = None,
+                                    ws: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """Gradient of ngc_latent_replay_attn from grad_out (bf16, shape of out): grad_q, grad_kv, grad_k_rope in shape and type of q, kv,
+    k_rope; ``out`` and ``lse`` are the forward call's."""
+    what = "ngc_latent_replay_attn_backward"
+    desc, args, index = _replay_args(what, seqs, q, kv, k_rope, out, lse, alive_pos, alive_count, total_before, lists, scale)
+    bf16 = torch.bfloat16
+    grads = (_arg(what, "grad_out", grad_out, out.shape, bf16, index), _arg(what, "grad_q", grad_q, q.shape, bf16, index),
+             _arg(what, "grad_kv", grad_kv, kv.shape, bf16, index), _arg(what, "grad_k_rope", grad_k_rope, k_rope.shape, bf16, index))
+    rc = lib.ngc_latent_replay_attn_backward(C.byref(desc), *args, *grads, *_ws(what, ws, index), _arg(what, "status", status, (1,), _I32, index),
+                                             _launch_stream(what, index))
+    _check(rc, what)
 
 
 REPLAY_ATTN_AUTO, REPLAY_ATTN_MMA_SYNC, REPLAY_ATTN_TCGEN05 = 0, 1, 2

@@ -1,0 +1,247 @@
+// ngc_latent_replay_attn and its gradient: entries, argument checks, and the kernels that prepare the masks.
+#include "latent_pool.cuh"
+#include "latent_replay.cuh"
+#include "ptx.cuh"
+
+namespace ngc {
+namespace {
+
+// When each token was evicted.  Kept lists of all rounds become one number per token: the sequence length at the first
+// round that fired after the token was there and did not keep it.  (Entries are marked with the last round that names
+// them; a token named by none goes at the first round that it was there for.)  One CTA per (list, sequence).
+__global__ void __launch_bounds__(1024) latent_gone_kernel(LatentReplayParams p) {
+  const int gi = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  int64_t row0;
+  const int T = latent_seq(p, b, row0);
+  const int64_t list = (int64_t)b * p.G + gi;
+  int32_t* gone = p.gone + list * p.gone_cap;
+  int2* tiles = p.tile_gone + list * (p.gone_cap / kLatTile);
+  const int T_up = (T + kLatTile - 1) / kLatTile * kLatTile;
+  for (int t = tid; t < T_up; t += 1024) gone[t] = -1;
+  __syncthreads();
+  for (int r = 0; r < p.n_rounds; ++r) {
+    const int64_t at = ((int64_t)r * p.B + b) * p.G + gi;
+    const int n = p.alive_count[at], fired = min(p.total_before[r * p.B + b], T);
+    if (n < 0 || n > p.kt_max) {
+      // (a list that failed has count -1 from its round on: that its rollout went on all the same is what is reported)
+      if (tid == 0 && p.total_before[r * p.B + b] < T) set_dev_status(p.dev_status, NGC_DEV_BAD_KEPT);
+      continue;
+    }
+    if (p.total_before[r * p.B + b] >= T) break;       // no query of the sequence comes after this round
+    for (int i = tid; i < n; i += 1024) {
+      const int t = p.alive_pos[at * p.kt_max + i];
+      if (t < 0 || t >= fired) set_dev_status(p.dev_status, NGC_DEV_BAD_KEPT);
+      else atomicMax(&gone[t], r);
+    }
+  }
+  __syncthreads();
+  for (int t = tid; t < T_up; t += 1024) {
+    int r = gone[t] + 1;                               // the first round that does not name it ...
+    while (r < p.n_rounds && p.total_before[r * p.B + b] <= t) ++r;      // ... among those that it was there for
+    gone[t] = t >= T ? 0 : (r < p.n_rounds ? p.total_before[r * p.B + b] : kNeverGone);
+  }
+  __syncthreads();
+  for (int i = tid >> 5; i < T_up / kLatTile; i += 32) {
+    int lo = kNeverGone, hi = 0;
+    for (int t = i * kLatTile + (tid & 31); t < min((i + 1) * kLatTile, T); t += 32) { lo = min(lo, gone[t]); hi = max(hi, gone[t]); }
+    for (int o = 16; o > 0; o >>= 1) { lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o)); hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o)); }
+    if ((tid & 31) == 0) tiles[i] = make_int2(lo, hi);
+  }
+}
+
+struct Row { float v[8]; };
+__device__ __forceinline__ float at(const __nv_bfloat16* x) { return __bfloat162float(*x); }
+
+__device__ __forceinline__ float score(const LatentReplayParams& p, const float* q, const __nv_bfloat16* k, const __nv_bfloat16* r, int lane) {
+  float z = 0.f;
+  for (int i = 0; i < 4; ++i) z += q[i] * at(k + 32 * i + lane);
+  for (int i = 0; i < 2; ++i) if (32 * i + lane < p.dr) z += q[4 + i] * at(r + 32 * i + lane);
+  return warp_sum(z);
+}
+__device__ __forceinline__ void load_q(const LatentReplayParams& p, const __nv_bfloat16* x, float* q, int lane) {
+  for (int i = 0; i < 4; ++i) q[i] = at(x + 32 * i + lane);
+  for (int i = 0; i < 2; ++i) q[4 + i] = 32 * i + lane < p.dr ? at(x + 128 + 32 * i + lane) : 0.f;
+}
+
+// A warp per (token, head).
+__global__ void __launch_bounds__(256) latent_fwd_kernel(LatentReplayParams p) {
+  const int lane = threadIdx.x & 31, h = blockIdx.y, b = blockIdx.z % p.B, l = blockIdx.z / p.B;
+  int64_t row0;
+  const int T = latent_seq(p, b, row0), t = blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (t >= T) return;
+  const int32_t* gone = p.gone ? p.gone + ((int64_t)b * p.G + list_of(p.lists, l, 0, 1)) * p.gone_cap : nullptr;
+  const int64_t base = (int64_t)l * p.rows + row0;
+  float q[6], acc[4] = {0, 0, 0, 0}, m = -INFINITY, sum = 0.f;
+  load_q(p, p.q + ((base + t) * p.H + h) * (128 + p.dr), q, lane);
+  for (int j = 0; j <= t; ++j) {
+    if (gone && gone[j] <= t) continue;
+    const __nv_bfloat16* kv = p.kv + ((base + j) * p.H + h) * 256;
+    const float z = score(p, q, kv, p.kr + (base + j) * p.dr, lane) * p.scale;
+    const float mn = fmaxf(m, z), a = expf(m - mn), w = expf(z - mn);
+    sum = sum * a + w;
+    for (int i = 0; i < 4; ++i) acc[i] = acc[i] * a + w * at(kv + 128 + 32 * i + lane);
+    m = mn;
+  }
+  for (int i = 0; i < 4; ++i) {
+    const float o = sum > 0.f ? acc[i] / sum : 0.f;
+    const int64_t x = ((base + t) * p.H + h) * 128 + 32 * i + lane;
+    if (p.out_bf16) ((__nv_bfloat16*)p.out)[x] = __float2bfloat16(o); else ((float*)p.out)[x] = o;
+  }
+  if (p.lse && lane == 0) p.lse[((int64_t)l * p.H + h) * p.rows + row0 + t] = m + logf(sum);
+}
+
+// A warp per token; the heads one after the other, so that the shared rotary rows' gradient is one warp's sum.
+__global__ void __launch_bounds__(256) latent_bwd_kernel(LatentReplayParams p) {
+  const int lane = threadIdx.x & 31, b = blockIdx.z % p.B, l = blockIdx.z / p.B;
+  int64_t row0;
+  const int T = latent_seq(p, b, row0), t = blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (t >= T) return;
+  const int32_t* gone = p.gone ? p.gone + ((int64_t)b * p.G + list_of(p.lists, l, 0, 1)) * p.gone_cap : nullptr;
+  const int64_t base = (int64_t)l * p.rows + row0;
+  auto weight = [&](const float* q, const float* go, int tq, int j, int h, float delta, float& pr) {
+    const __nv_bfloat16* kv = p.kv + ((base + j) * p.H + h) * 256;
+    const float z = score(p, q, kv, p.kr + (base + j) * p.dr, lane) * p.scale;
+    pr = expf(z - p.lse[((int64_t)l * p.H + h) * p.rows + row0 + tq]);
+    float dp = 0.f;
+    for (int i = 0; i < 4; ++i) dp += go[i] * at(kv + 128 + 32 * i + lane);
+    return pr * (warp_sum(dp) - delta) * p.scale;
+  };
+  float gkr[2] = {0, 0};
+  for (int h = 0; h < p.H; ++h) {
+    float q[6], go[4], gq[6] = {0, 0, 0, 0, 0, 0}, gk[6] = {0, 0, 0, 0, 0, 0}, gv[4] = {0, 0, 0, 0};
+    load_q(p, p.q + ((base + t) * p.H + h) * (128 + p.dr), q, lane);
+    for (int i = 0; i < 4; ++i) go[i] = at(p.go + ((base + t) * p.H + h) * 128 + 32 * i + lane);
+    float delta = p.delta[((int64_t)l * p.H + h) * p.rows + row0 + t], pr;
+    for (int j = 0; j <= t; ++j) {                     // as a query
+      if (gone && gone[j] <= t) continue;
+      const float dz = weight(q, go, t, j, h, delta, pr);
+      const __nv_bfloat16* kv = p.kv + ((base + j) * p.H + h) * 256;
+      for (int i = 0; i < 4; ++i) gq[i] += dz * at(kv + 32 * i + lane);
+      for (int i = 0; i < 2; ++i) if (32 * i + lane < p.dr) gq[4 + i] += dz * at(p.kr + (base + j) * p.dr + 32 * i + lane);
+    }
+    const int end = gone ? min(gone[t], T) : T;
+    for (int tq = t; tq < end; ++tq) {                 // as a key
+      load_q(p, p.q + ((base + tq) * p.H + h) * (128 + p.dr), q, lane);
+      for (int i = 0; i < 4; ++i) go[i] = at(p.go + ((base + tq) * p.H + h) * 128 + 32 * i + lane);
+      const float dz = weight(q, go, tq, t, h, p.delta[((int64_t)l * p.H + h) * p.rows + row0 + tq], pr);
+      for (int i = 0; i < 6; ++i) gk[i] += dz * q[i];
+      for (int i = 0; i < 4; ++i) gv[i] += pr * go[i];
+    }
+    for (int i = 0; i < 4; ++i) {
+      p.gq[((base + t) * p.H + h) * (128 + p.dr) + 32 * i + lane] = __float2bfloat16(gq[i]);
+      p.gkv[((base + t) * p.H + h) * 256 + 32 * i + lane] = __float2bfloat16(gk[i]);
+      p.gkv[((base + t) * p.H + h) * 256 + 128 + 32 * i + lane] = __float2bfloat16(gv[i]);
+    }
+    for (int i = 0; i < 2; ++i) if (32 * i + lane < p.dr) {
+      p.gq[((base + t) * p.H + h) * (128 + p.dr) + 128 + 32 * i + lane] = __float2bfloat16(gq[4 + i]);
+      gkr[i] += gk[4 + i];
+    }
+  }
+  for (int i = 0; i < 2; ++i) if (32 * i + lane < p.dr) p.gkr[(base + t) * p.dr + 32 * i + lane] = __float2bfloat16(gkr[i]);
+}
+
+// delta = sum over channels of out * grad_out: 16 lanes per (token, head).
+__global__ void __launch_bounds__(256) latent_delta_kernel(LatentReplayParams p) {
+  const int lane = threadIdx.x & 31, h = blockIdx.y, b = blockIdx.z % p.B, l = blockIdx.z / p.B;
+  int64_t row0;
+  const int T = latent_seq(p, b, row0), t = blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (t >= T) return;
+  const int64_t x = (((int64_t)l * p.rows + row0 + t) * p.H + h) * 128;
+  float s = 0.f;
+  for (int i = 0; i < 4; ++i)
+    s += at(p.go + x + 32 * i + lane) * (p.out_bf16 ? at((const __nv_bfloat16*)p.out + x + 32 * i + lane) : ((const float*)p.out)[x + 32 * i + lane]);
+  s = warp_sum(s);
+  if (lane == 0) p.delta[((int64_t)l * p.H + h) * p.rows + row0 + t] = s;
+}
+
+bool valid_seqs(const ngc_latent_seqs* s) {
+  return s && s->seq_off && s->lens && s->rows >= 0 && s->L > 0 && s->B > 0 && s->H > 0 && s->d_nope > 0 && s->d_v > 0 && s->d_rope > 0 &&
+         s->max_len >= 0 && (s->dtype == NGC_F32 || s->dtype == NGC_BF16);
+}
+
+struct Space { size_t gone, tiles, delta, dkr, all; };
+int gone_cap(const ngc_latent_seqs* s) { return (int)(((int64_t)s->max_len + kLatTile - 1) / kLatTile * kLatTile); }
+Space space_of(const ngc_latent_seqs* s, int lists, int n_rounds, int backward) {
+  Space w = {0, 0, 0, 0, 0};
+  const size_t BG = (size_t)s->B * lists_G(lists, s->L, 1);
+  size_t at = 0;
+  if (n_rounds > 0) {
+    w.gone = at; at += align256(BG * gone_cap(s) * 4);
+    w.tiles = at; at += align256(BG * (gone_cap(s) / kLatTile) * 8);
+  }
+  if (backward) {
+    w.delta = at; at += align256((size_t)s->L * s->H * s->rows * 4);
+    w.dkr = at; at += align256((size_t)s->L * s->H * s->rows * s->d_rope * 4);
+  }
+  w.all = at;
+  return w;
+}
+
+int prepare(const ngc_latent_seqs* s, const void* q, const void* kv, const void* k_rope, const int32_t* alive_pos, const int32_t* alive_count,
+            const int32_t* total_before, int n_rounds, int kt_max, int lists, float scale, int out_dtype, void* ws, size_t ws_bytes,
+            int32_t* dev_status, int backward, LatentReplayParams* p) {
+  if (!valid_seqs(s) || !q || !kv || !k_rope || n_rounds < 0 || lists < 0 || lists > 2 || (out_dtype != NGC_F32 && out_dtype != NGC_BF16) ||
+      (n_rounds > 0 && (!alive_pos || !alive_count || !total_before || kt_max < 1)) || !(scale > 0.f && scale <= 2e38f) || !aligned16(q) ||
+      !aligned16(kv) || !aligned16(k_rope))
+    return NGC_ERR_INVALID_ARG;
+  if (s->dtype != NGC_BF16 || s->d_nope != kLatNope || s->d_v != kLatV || s->d_rope % 16 != 0 || s->d_rope > 64 ||
+      s->rows * s->L > 0x7fffffffLL || s->max_len > 0x7fffff00 || (int64_t)s->L * s->B > 65535 || s->H > 65535)
+    return NGC_ERR_UNSUPPORTED;
+  const Space w = space_of(s, lists, n_rounds, backward);
+  if (w.all > 0 && (!ws || ws_bytes < w.all || ((uintptr_t)ws & 255))) return NGC_ERR_WORKSPACE;
+  *p = LatentReplayParams{};
+  uint8_t* base = (uint8_t*)ws;
+  p->seq_off = s->seq_off; p->lens = s->lens; p->rows = s->rows;
+  p->q = (const __nv_bfloat16*)q; p->kv = (const __nv_bfloat16*)kv; p->kr = (const __nv_bfloat16*)k_rope;
+  p->alive_pos = alive_pos; p->alive_count = alive_count; p->total_before = total_before;
+  if (n_rounds > 0) { p->gone = (int32_t*)(base + w.gone); p->tile_gone = (int2*)(base + w.tiles); }
+  if (backward) { p->delta = (float*)(base + w.delta); p->dkr_part = (float*)(base + w.dkr); }
+  p->L = s->L; p->B = s->B; p->H = s->H; p->G = lists_G(lists, s->L, 1); p->dr = s->d_rope; p->lists = lists; p->n_rounds = n_rounds;
+  p->kt_max = kt_max; p->max_len = s->max_len; p->gone_cap = gone_cap(s); p->out_bf16 = out_dtype == NGC_BF16;
+  p->scale = scale; p->scale_log2 = scale * 1.4426950408889634f; p->dev_status = dev_status;
+  return NGC_OK;
+}
+
+}  // namespace
+}  // namespace ngc
+
+extern "C" size_t ngc_latent_replay_workspace_bytes(const ngc_latent_seqs* s, int lists, int n_rounds, int backward) {
+  return s && lists >= 0 && lists <= 2 ? ngc::space_of(s, lists, n_rounds, backward).all : 0;
+}
+
+extern "C" int ngc_latent_replay_attn(const ngc_latent_seqs* s, const void* q, const void* kv, const void* k_rope, const int32_t* alive_pos,
+                                      const int32_t* alive_count, const int32_t* total_before, int n_rounds, int kt_max, int lists, float scale,
+                                      void* out, int out_dtype, float* lse, void* ws, size_t ws_bytes, int32_t* dev_status, ngc_stream stream) {
+  using namespace ngc;
+  NGC_API_RANGE("ngc_latent_replay_attn");
+  LatentReplayParams p;
+  const int rc = prepare(s, q, kv, k_rope, alive_pos, alive_count, total_before, n_rounds, kt_max, lists, scale, out_dtype, ws, ws_bytes, dev_status, 0, &p);
+  if (rc != NGC_OK) return rc;
+  if (!out || !aligned16(out)) return NGC_ERR_INVALID_ARG;
+  if (s->rows == 0 || s->max_len == 0) return NGC_OK;
+  p.out = out; p.lse = lse;
+  if (n_rounds > 0) latent_gone_kernel<<<dim3(p.G, p.B), 1024, 0, stream>>>(p);
+  latent_fwd_kernel<<<dim3((p.max_len + 7) / 8, p.H, p.L * p.B), 256, 0, stream>>>(p);
+  return launch_status();
+}
+
+extern "C" int ngc_latent_replay_attn_backward(const ngc_latent_seqs* s, const void* q, const void* kv, const void* k_rope, const int32_t* alive_pos,
+                                               const int32_t* alive_count, const int32_t* total_before, int n_rounds, int kt_max, int lists,
+                                               float scale, const void* out, int out_dtype, const float* lse, const void* grad_out, void* grad_q,
+                                               void* grad_kv, void* grad_k_rope, void* ws, size_t ws_bytes, int32_t* dev_status, ngc_stream stream) {
+  using namespace ngc;
+  NGC_API_RANGE("ngc_latent_replay_attn_backward");
+  LatentReplayParams p;
+  const int rc = prepare(s, q, kv, k_rope, alive_pos, alive_count, total_before, n_rounds, kt_max, lists, scale, out_dtype, ws, ws_bytes, dev_status, 1, &p);
+  if (rc != NGC_OK) return rc;
+  if (!out || !lse || !grad_out || !grad_q || !grad_kv || !grad_k_rope || !aligned16(out) || !aligned16(grad_out) || !aligned16(grad_q) ||
+      !aligned16(grad_kv) || !aligned16(grad_k_rope))
+    return NGC_ERR_INVALID_ARG;
+  if (s->rows == 0 || s->max_len == 0) return NGC_OK;
+  p.out = const_cast<void*>(out); p.lse = const_cast<float*>(lse); p.go = (const __nv_bfloat16*)grad_out;
+  p.gq = (__nv_bfloat16*)grad_q; p.gkv = (__nv_bfloat16*)grad_kv; p.gkr = (__nv_bfloat16*)grad_k_rope;
+  if (n_rounds > 0) latent_gone_kernel<<<dim3(p.G, p.B), 1024, 0, stream>>>(p);
+  latent_delta_kernel<<<dim3((p.max_len + 7) / 8, p.H, p.L * p.B), 256, 0, stream>>>(p);
+  latent_bwd_kernel<<<dim3((p.max_len + 7) / 8, 1, p.L * p.B), 256, 0, stream>>>(p);
+  return launch_status();
+}

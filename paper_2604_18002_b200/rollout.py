@@ -135,6 +135,47 @@ class NgcRollout:
             raise ngc.NgcError(f"device status {code}: {ngc.DEV_STATUS.get(code, '?')}")
 
 
+class NgcLatentRollout:
+    """A batch of rollouts of a model with latent attention: its rows lie in a common pool of pages, so what one rollout evicts or
+    gives back when it ends serves the others.  One decode step is ``update`` (books and slots, once), then per layer ``write`` and
+    ``decode``; an eviction round is ``evict`` in the place of ``update``."""
+
+    def __init__(self, L, B, H, d_latent, d_rope, n_pages, pages_cap, max_new, scale, page=64, lists=ngc.LISTS_SHARED, list_base=0, device="cuda"):
+        """``max_new``: new tokens of all rollouts that one ``update`` may bring; ``scale``: of the scores (one over the root of the
+        expanded key's width)."""
+        self.L, self.B, self.H, self.lists, self.scale, self.list_base, self.device = L, B, H, lists, scale, list_base, device
+        self.G = ngc.lists_G(lists, L, 1)
+        self.pool = ngc.new_latent_pool(L, B, d_latent, d_rope, n_pages, pages_cap, page, lists, device)
+        self.slots = torch.empty((self.G, max_new), dtype=torch.int32, device=device)
+        self.first = torch.empty((B + 1,), dtype=torch.int32, device=device)
+        self.kept_order = torch.empty((B, self.G, pages_cap), dtype=torch.int32, device=device)
+        self.kept_sorted = torch.empty_like(self.kept_order)
+        self.status = ngc.new_status(device)
+        self.ws_sample = ngc.alloc_workspace(ngc.workspace_bytes(ngc.OP_SAMPLE, None, self.G, pages_cap, pages_cap, B=B), device)
+        self.ws_decode = ngc.alloc_workspace(ngc.latent_decode_workspace_bytes(self.pool, H), device)
+
+    def update(self, n_new: torch.Tensor):
+        """Pages and ``slots`` for ``n_new[b]`` new tokens per rollout (int32 [B]; -1: the rollout is finished)."""
+        ngc.ngc_pool_update(self.pool, n_new, self.slots, self.first, status=self.status)
+
+    def evict(self, logits: torch.Tensor, n: torch.Tensor, n_protect: Optional[torch.Tensor], budget: torch.Tensor, seed: int, rnd: int,
+              n_new: torch.Tensor, greedy: int = 0):
+        """An eviction round over whole pages and the next tokens' pages in one: draws ``budget[b]`` of ``n[b]`` pages by ``logits``
+        [B][G][pages_cap] fp32.  (With a length per list, lists may be a page short of ``n``: give the missing unit the logit -inf.)"""
+        ngc.ngc_sample_evict(logits, n, n_protect, budget, seed, rnd, self.kept_order, self.kept_sorted, None, greedy=greedy,
+                             list_base=self.list_base, ws=self.ws_sample, status=self.status)
+        ngc.ngc_pool_update(self.pool, n_new, self.slots, self.first, kept_sorted=self.kept_sorted, budget=budget, status=self.status)
+
+    def write(self, latent: torch.Tensor, rope: torch.Tensor, layer_begin: int = 0, layer_end: Optional[int] = None):
+        """Rows of the new tokens, in the order of ``first``: latent [L][max_new][d_latent], rope [L][max_new][d_rope]."""
+        ngc.ngc_latent_write(self.pool, self.slots, latent, rope, layer_begin, layer_end, status=self.status)
+
+    def decode(self, q_latent: torch.Tensor, q_rope: torch.Tensor, out: torch.Tensor, layer_begin: int = 0, layer_end: Optional[int] = None):
+        ngc.ngc_latent_decode(self.pool, q_latent, q_rope, out, self.scale, layer_begin, layer_end, ws=self.ws_decode, status=self.status)
+
+    check_status = NgcRollout.check_status
+
+
 class HostStep:
     """Host-buffer driver for one whole step (eviction round + decode steps): pinned host
     inputs in, attention outputs and eviction results out, copies overlapped with compute.
