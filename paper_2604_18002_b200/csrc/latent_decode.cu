@@ -1,75 +1,676 @@
-// ngc_latent_decode: absorbed latent attention of one token per sequence over a pool of pages.
+// ngc_latent_decode: absorbed latent attention of one token per sequence over a pool of pages, on the 5th-generation
+// tensor cores.
+//
+// All heads share the rows (c_j | r_j), so both products are tall: with X the rows of a tile of 64 tokens and Q the heads'
+// queries, scores are S^T = X Q^T and the sums O^T += C^T P^T, C the latent part of the same rows.  Tokens, then latent
+// channels are the M dimension of the tensor core (64 and 128 rows per product), the heads its N (16, 32 or 64 per CTA):
+// few heads cost few columns, where heads as M would cost 128 rows for 16 heads.  One copy of a tile in shared memory serves
+// as K-major A operand of the first product and as MN-major A operand of the second.  Every row is read from HBM once, which
+// bounds the call up to some 100 heads; the products of 128 heads take as long (36 + 16 steps per tile and 64 heads).
+//
+// Work is dealt out by tiles: the tiles of all (layer, sequence) units in one line, cut into equal pieces, one per CTA (per
+// group of heads).  A unit that lies in several pieces leaves unnormalised sums, maxima and weights per piece in the
+// workspace, and a second kernel joins them.  Roles of a CTA, which meet at mbarriers only:
+//   producer (1 thread)   the tile's rows by TMA, a box of 64 channels per page, into a ring of stages
+//   mender (1 warp)       rows behind a unit's last token: zeros (they may hold anything; a NaN times a zero weight is NaN)
+//   queries (1 thread)    the heads' queries of the next unit, when the last unit's scores are done
+//   MMA (1 thread)        S^T of tile i + 1 is issued before the sums of tile i, so it runs under the softmax of tile i
+//   softmax (4 warps)     16 tokens each.  A thread holds two tokens of a quarter of the heads; weights go to shared memory
+//                         by transposing matrix stores, as the K-major B operand.  The maximum that the exponentials refer to
+//                         moves only when a score exceeds it by 2^8 (exact in bf16 and fp32), which is one vote per tile.
+// Every wait is bounded; one that runs out makes all roles leave and is reported.
+#include <cuda.h>
 #include <cuda_bf16.h>
 
+#include "kv_map.cuh"
 #include "latent_pool.cuh"
 #include "ptx.cuh"
+#include "umma.cuh"
 
 namespace ngc {
 namespace {
 
+constexpr int kTile = 64;                      // tokens per tile
+constexpr int kBox = kTile * 128;              // 64 tokens x 64 channels
+constexpr int kMaxStages = 8;
+constexpr int kMaxGroups = 20;                 // groups of all stages: channels whose arrival is waited for together
+constexpr int kThreads = 256;                  // warps 0-3 softmax, 4 MMA, 5 producer, 6 mender, 7 queries
+constexpr int kMmaWarp = 4, kProducerWarp = 5, kMenderWarp = 6, kQueryWarp = 7;
+constexpr int kSmemLimit = 227 * 1024;
+constexpr int kStaticReserve = 2048;           // barriers and exchange buffers (static shared memory)
+constexpr float kLazy = 8.f;
+constexpr int kMinTiles = 1;                   // tiles per piece, at least
+constexpr int kMaxCtas = 148;                  // one per SM
+
 struct LatentDecodeParams {
-  const __nv_bfloat16* rows;
   const int32_t* table;
   const int32_t* lens;
-  const __nv_bfloat16* ql;
-  const __nv_bfloat16* qr;
   void* out;
+  float* part_o;                // [piece][2][H padded to the groups][dc] sums, unnormalised
+  float2* part_ml;              // [piece][2][H padded] (maximum in log2 units, sum of weights)
+  int2* plan;                   // [piece] the unit that begins in the piece and goes on behind it, the piece it ends in; or -1
   int32_t* dev_status;
-  int B, H, G, dc, dr, page, cap, n_pages, lists, layer_begin, out_bf16;
+  int B, H, G, dc, dr, page, cap, n_pages, lists, layer_begin, n_layers, out_bf16;
+  int stages, pieces, groups, heads_pad;
   float scale_log2;
 };
 
-// One CTA per (head, sequence, layer), its warps take tokens in turn; online softmax per warp, joined at the end.
-__global__ void __launch_bounds__(256) latent_decode_kernel(LatentDecodeParams p) {
-  __shared__ float so[8][512];
-  __shared__ float sm[8], sl[8];
-  const int h = blockIdx.x, b = blockIdx.y, l = p.layer_begin + blockIdx.z;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int gi = list_of(p.lists, l, 0, 1);
-  const int64_t list = (int64_t)b * p.G + gi;
-  const int len = p.lens[list];
-  if (len < 0 || len > p.cap * p.page) {
-    if (threadIdx.x == 0) set_dev_status(p.dev_status, NGC_DEV_BAD_COUNTS);
-    return;
+struct Maps { CUtensorMap rows, ql, qr; };
+
+template <int NH> struct Shared {
+  uint64_t full[kMaxGroups], empty[kMaxStages], raw[kMaxStages];
+  uint64_t s_full[2], p_full, o_done, q_full, q_empty, drain;
+  uint32_t tmem;
+  int abort;
+  int u0, t0, g0, n_tiles, total;              // where this CTA's piece begins, how many tiles it has, tiles of the call
+  int warp_sum[kThreads / 32];
+  float ex[4][NH];                             // per warp: column maxima, later sums of weights
+  float m[NH], alpha[NH];                      // the maximum that the exponentials refer to (log2 units), and what its last move costs
+};
+
+__device__ __forceinline__ int unit_len(const LatentDecodeParams& p, int u) {
+  const int n = p.lens[(int64_t)(u % p.B) * p.G + list_of(p.lists, p.layer_begin + u / p.B, 0, 1)];
+  return n < 0 || n > p.cap * p.page ? -1 : n;
+}
+
+// The pieces: how many there are (so few tiles that joining them would cost more than it saves stay together), which tile of
+// the line piece i begins at, and which piece has tile g.
+__device__ __forceinline__ int pieces_used(int total, int pieces) { return max(1, min(pieces, total / kMinTiles)); }
+__device__ __forceinline__ int piece_first(int total, int pieces, int i) { return (int)((int64_t)total * i / pieces); }
+__device__ __forceinline__ int piece_of(int total, int pieces, int g) {
+  int i = (int)(((int64_t)g * pieces) / total);
+  while (i + 1 < pieces && piece_first(total, pieces, i + 1) <= g) ++i;
+  while (i > 0 && piece_first(total, pieces, i) > g) --i;
+  return i;
+}
+
+// The parts of units that make up a piece, in order.
+struct Walk {
+  int u, t, left;               // next unit, its next tile, tiles left in the piece
+  int unit, t_begin, t_end, n, len;            // the current part: tiles t_begin .. t_end of the n of unit
+  template <int NH> __device__ __forceinline__ explicit Walk(const Shared<NH>& sh) : u(sh.u0), t(sh.t0), left(sh.n_tiles) {}
+  __device__ __forceinline__ bool next(const LatentDecodeParams& p) {
+    if (left <= 0) return false;
+    do {
+      if (u >= p.n_layers * p.B) return false;           // (the lengths changed under the call)
+      len = unit_len(p, u);
+      n = len > 0 ? (len + kTile - 1) / kTile : 0;
+      unit = u++;
+    } while (n == 0);           // (left > 0: a unit with tiles follows)
+    t_begin = t;
+    t_end = min(n, t + left);
+    left -= t_end - t_begin;
+    t = 0;
+    return true;
   }
-  const int D = p.dc + p.dr, per = p.dc / 32;
-  const int64_t qi = ((int64_t)l * p.B + b) * p.H + h;
-  float q[18], acc[16];
-  for (int i = 0; i < 16; ++i) { acc[i] = 0.f; q[i] = i < per ? __bfloat162float(p.ql[qi * p.dc + 32 * i + lane]) : 0.f; }
-  for (int i = 0; i < 2; ++i) q[16 + i] = 32 * i + lane < p.dr ? __bfloat162float(p.qr[qi * p.dr + 32 * i + lane]) : 0.f;
-  float m = -INFINITY, sum = 0.f;
-  for (int t = warp; t < len; t += 8) {
-    int pg = p.table[list * p.cap + t / p.page];
-    if ((uint32_t)pg >= (uint32_t)p.n_pages) { if (lane == 0) set_dev_status(p.dev_status, NGC_DEV_BAD_PAGE); pg = 0; }
-    const __nv_bfloat16* x = p.rows + (((int64_t)l * p.n_pages + pg) * p.page + t % p.page) * D;
-    float v[16], z = 0.f;
-    for (int i = 0; i < 16; ++i) if (i < per) { v[i] = __bfloat162float(x[32 * i + lane]); z += v[i] * q[i]; }
-    for (int i = 0; i < 2; ++i) if (32 * i + lane < p.dr) z += __bfloat162float(x[p.dc + 32 * i + lane]) * q[16 + i];
-    z = warp_sum(z) * p.scale_log2;
-    const float mn = fmaxf(m, z), a = exp2f(m - mn), w = exp2f(z - mn);
-    sum = sum * a + w;
-    for (int i = 0; i < 16; ++i) if (i < per) acc[i] = acc[i] * a + w * v[i];
-    m = mn;
+};
+
+// 16 lanes x 8 columns per matrix fragment: register 4 j + {0, 1}: row lane / 4, columns 8 j + 2 (lane % 4) + {0, 1}; 4 j + {2, 3}: row + 8.
+template <int NH> __device__ __forceinline__ void ld_frags(uint32_t taddr, uint32_t* r);
+template <> __device__ __forceinline__ void ld_frags<16>(uint32_t taddr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr));
+}
+template <> __device__ __forceinline__ void ld_frags<32>(uint32_t taddr, uint32_t* r) { ld_frags<16>(taddr, r); ld_frags<16>(taddr + 16, r + 8); }
+template <> __device__ __forceinline__ void ld_frags<64>(uint32_t taddr, uint32_t* r) { ld_frags<32>(taddr, r); ld_frags<32>(taddr + 32, r + 16); }
+
+__device__ __forceinline__ void stmatrix_x4_trans(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r0), "r"(r1), "r"(r2), "r"(r3) : "memory");
+}
+
+// Barrier of the four softmax warps; true to all where `mine` is true to one.
+__device__ __forceinline__ bool softmax_any(bool mine) {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\tbarrier.cta.red.or.pred p, 1, 128, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(r) : "r"((uint32_t)mine) : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ void softmax_sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
+
+template <int NH, int DC>
+__global__ void __launch_bounds__(kThreads, 1) latent_decode_kernel(const __grid_constant__ Maps maps, LatentDecodeParams p) {
+  extern __shared__ uint8_t smem_dyn[];
+  __shared__ Shared<NH> sh;
+  uint8_t* sQ = (uint8_t*)(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);     // [chunks][NH rows x 128 B]
+  constexpr int kChunks = DC / 64 + 1, kStage = kChunks * kBox;                  // the last chunk: rotary part, zeros behind it
+  constexpr int kGroups = DC / 128 + 1;                                          // group 0: the last chunk; group g: chunks 2 g - 2, 2 g - 1
+  uint8_t* sP = sQ + kChunks * NH * 128;                                         // [NH rows x 64 tokens]
+  uint8_t* stage0 = sP + NH * 128;                                               // [stages][chunks][64 tokens x 128 B]
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int piece = blockIdx.x / p.groups, hg = blockIdx.x % p.groups;
+  constexpr uint32_t kCols = NH == 64 ? 512 : (NH == 32 ? 256 : 128);            // O^T: 4 x NH, S^T: 2 x NH
+  const int U = p.n_layers * p.B;
+
+  if (tid == 0) {
+    for (int s = 0; s < p.stages; ++s) { ptx::mbar_init(&sh.raw[s], 1); ptx::mbar_init(&sh.empty[s], 1); }
+    for (int s = 0; s < p.stages * kGroups; ++s) ptx::mbar_init(&sh.full[s], 1);
+    ptx::mbar_init(&sh.s_full[0], 1); ptx::mbar_init(&sh.s_full[1], 1);
+    ptx::mbar_init(&sh.p_full, 128);
+    ptx::mbar_init(&sh.o_done, 1);
+    ptx::mbar_init(&sh.q_full, 1); ptx::mbar_init(&sh.q_empty, 1); ptx::mbar_init(&sh.drain, 1);
+    ptx::fence_barrier_init();
+    sh.abort = 0; sh.u0 = 0; sh.t0 = 0;
+    ptx::prefetch_tensormap(&maps.rows); ptx::prefetch_tensormap(&maps.ql); ptx::prefetch_tensormap(&maps.qr);
   }
-  for (int i = 0; i < 16; ++i) if (i < per) so[warp][32 * i + lane] = acc[i];
-  if (lane == 0) { sm[warp] = m; sl[warp] = sum; }
+  if (warp == kMmaWarp) umma::tmem_alloc(&sh.tmem, kCols);
+  ptx::grid_dep_wait();
+  // ---- the line of tiles, and where this piece begins: every thread sums a run of units
+  {
+    const int per = (U + kThreads - 1) / kThreads, u_lo = min(tid * per, U), u_hi = min(u_lo + per, U);
+    int mine = 0;
+    for (int u = u_lo; u < u_hi; ++u) {
+      const int n = unit_len(p, u);
+      if (n < 0) set_dev_status(p.dev_status, NGC_DEV_BAD_COUNTS);
+      mine += (max(n, 0) + kTile - 1) / kTile;
+    }
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += v; }
+    if (lane == 31) sh.warp_sum[warp] = incl;
+    __syncthreads();
+    int before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) { const int v = sh.warp_sum[w]; if (w < warp) before += v; total += v; }
+    const int used = pieces_used(total, p.pieces);
+    const int g0 = piece < used ? piece_first(total, used, piece) : 0, g1 = piece < used ? piece_first(total, used, piece + 1) : 0;
+    int at = before + incl - mine;                       // first tile of this thread's run
+    if (g0 < g1 && g0 >= at && g0 < at + mine) {
+      for (int u = u_lo; u < u_hi; ++u) {
+        const int n = (max(unit_len(p, u), 0) + kTile - 1) / kTile;
+        if (g0 < at + n) { sh.u0 = u; sh.t0 = g0 - at; break; }
+        at += n;
+      }
+    }
+    if (tid == 0) {
+      sh.n_tiles = g1 - g0; sh.total = total; sh.g0 = g0;
+      if (hg == 0) p.plan[piece] = make_int2(-1, -1);
+    }
+  }
+  umma::fence_before_sync();
   __syncthreads();
-  float mm = -INFINITY, ll = 0.f;
-  for (int w = 0; w < 8; ++w) if (sl[w] > 0.f || sl[w] != sl[w]) mm = fmaxf(mm, sm[w]);
-  for (int w = 0; w < 8; ++w) if (sm[w] != -INFINITY) ll += sl[w] * exp2f(sm[w] - mm);
-  for (int c = threadIdx.x; c < p.dc; c += 256) {
-    float o = 0.f;
-    for (int w = 0; w < 8; ++w) if (sm[w] != -INFINITY) o += so[w][c] * exp2f(sm[w] - mm);
-    o = len == 0 ? 0.f : o / ll;
-    if (p.out_bf16) ((__nv_bfloat16*)p.out)[qi * p.dc + c] = __float2bfloat16(o);
-    else ((float*)p.out)[qi * p.dc + c] = o;
+  umma::fence_after_sync();
+  const uint32_t tmem = sh.tmem;
+  const int n_tiles = sh.n_tiles;
+  const uint32_t s_tmem = tmem + 4 * NH;
+  ptx::grid_dep_launch();                                // (all CTAs are resident: the second kernel's can wait beside them)
+
+  if (warp == kProducerWarp) {
+    // ------------------------------------------------------------------ rows of the tiles
+    int t = 0;
+    uint32_t raw_last = 0, raw_phase = 0;                // bit s: stage s was last filled through raw / parity of raw's next use
+    int st = 0, phase = 0;                               // stage of tile t, parity of its uses
+    bool ok = true;
+    Walk w(sh);
+    while (ok && w.next(p)) {
+      const int l = p.layer_begin + w.unit / p.B, b = w.unit % p.B;
+      const int32_t* row = p.table + ((int64_t)b * p.G + list_of(p.lists, l, 0, 1)) * p.cap;
+      const int n_pages = (w.len + p.page - 1) / p.page, per = kTile / p.page;
+      int have = w.t_begin * per, pages = 0;             // lane j holds page `have - 32 + j` of the sequence
+      auto page_row = [&](int j) {                       // first row of the sequence's page j
+        const int y = (l * p.n_pages + __shfl_sync(0xffffffffu, pages, j - (have - 32))) * p.page;
+        return NGC_IN_BOUNDS(p.dev_status, y >= 0 && y / p.page < (p.layer_begin + p.n_layers) * p.n_pages) ? y : 0;
+      };
+      for (int i = w.t_begin; i < w.t_end; ++i, ++t) {
+        if (i * per >= have || i == w.t_begin) {
+          int pg = i * per + lane < n_pages ? row[i * per + lane] : 0;
+          if ((uint32_t)pg >= (uint32_t)p.n_pages) {
+            if (i * per + lane < w.t_end * per) set_dev_status(p.dev_status, NGC_DEV_BAD_PAGE);
+            pg = 0;
+          }
+          pages = pg;
+          have = i * per + 32;
+        }
+        const int n = min(kTile, w.len - i * kTile);
+        const bool tail = n < kTile;                     // the mender hands it on
+        const int boxes = min(per, (n + p.page - 1) / p.page);
+        const int y0 = page_row(i * per), y1 = boxes > 1 ? page_row(i * per + 1) : 0;
+        if (t >= p.stages && !umma::warp_wait(&sh.empty[st], phase ^ 1, &sh.abort, p.dev_status)) { ok = false; break; }
+        if (umma::elect_one()) {
+          uint8_t* dst = stage0 + st * kStage;
+          const uint32_t bytes = (uint32_t)(boxes * p.page * 128);
+          ptx::mbar_expect_tx(&sh.full[st * kGroups], bytes);
+          if (tail) ptx::mbar_expect_tx(&sh.raw[st], bytes * (DC / 64));
+          ptx::tma_load_2d(dst + (kChunks - 1) * kBox, &maps.rows, DC, y0, &sh.full[st * kGroups]);
+          if (boxes > 1) ptx::tma_load_2d(dst + (kChunks - 1) * kBox + 32 * 128, &maps.rows, DC, y1, &sh.full[st * kGroups]);
+#pragma unroll
+          for (int g = 1; g < kGroups; ++g) {
+            uint64_t* bar = tail ? &sh.raw[st] : &sh.full[st * kGroups + g];
+            if (!tail) ptx::mbar_expect_tx(bar, 2 * bytes);
+#pragma unroll
+            for (int c = 2 * g - 2; c < 2 * g; ++c) {
+              ptx::tma_load_2d(dst + c * kBox, &maps.rows, 64 * c, y0, bar);
+              if (boxes > 1) ptx::tma_load_2d(dst + c * kBox + 32 * 128, &maps.rows, 64 * c, y1, bar);
+            }
+          }
+        }
+        __syncwarp();
+        raw_last = tail ? raw_last | 1u << st : raw_last & ~(1u << st);
+        if (tail) raw_phase ^= 1u << st;
+        if (++st == p.stages) { st = 0; phase ^= 1; }
+      }
+    }
+    // nothing is in flight when the CTA ends: the last use of every stage
+    for (int s = 0; s < p.stages; ++s) {
+      const int n = (t - s + p.stages - 1) / p.stages;   // tiles that went through the stage
+      const bool through_raw = raw_last >> s & 1;
+      if (n > 0)
+        for (int g = 0; g < kGroups; ++g)
+          if (!(through_raw && g > 0)) ptx::mbar_wait_bounded(&sh.full[s * kGroups + g], (n - 1) & 1);
+      if (through_raw) ptx::mbar_wait_bounded(&sh.raw[s], ((raw_phase >> s) & 1) ^ 1);
+    }
+    __syncwarp();
+  } else if (warp == kMenderWarp) {
+    // ------------------------------------------------------------------ rows behind the last token
+    int t = 0;
+    uint32_t raw_phase = 0;
+    Walk w(sh);
+    while (w.next(p)) {
+      t += w.t_end - w.t_begin;
+      const int n = w.len - (w.n - 1) * kTile;
+      if (w.t_end < w.n || n == kTile) continue;
+      const int s = (t - 1) % p.stages;
+      if (!umma::warp_wait(&sh.raw[s], (raw_phase >> s) & 1, &sh.abort, p.dev_status)) break;
+      raw_phase ^= 1u << s;
+      uint8_t* st = stage0 + s * kStage;
+      for (int c = 0; c < DC / 64; ++c)
+        for (int x = n * 8 + lane; x < kTile * 8; x += 32) *reinterpret_cast<uint4*>(st + c * kBox + x * 16) = make_uint4(0, 0, 0, 0);
+      ptx::fence_proxy_async();
+      __syncwarp();
+      if (lane >= 1 && lane < kGroups) ptx::mbar_arrive(&sh.full[s * kGroups + lane]);
+    }
+  } else if (warp == kQueryWarp) {
+    // ------------------------------------------------------------------ queries of the units
+    int k = 0;
+    Walk w(sh);
+    for (; w.next(p); ++k) {
+      if (k > 0 && !umma::warp_wait(&sh.q_empty, (k - 1) & 1, &sh.abort, p.dev_status)) break;
+      const int z = (p.layer_begin + w.unit / p.B) * p.B + w.unit % p.B;
+      if (umma::elect_one()) {
+        ptx::mbar_expect_tx(&sh.q_full, (uint32_t)(kChunks * NH * 128));
+#pragma unroll
+        for (int c = 0; c < DC / 64; ++c) ptx::tma_load_3d(sQ + c * NH * 128, &maps.ql, 64 * c, hg * NH, z, &sh.q_full);
+        ptx::tma_load_3d(sQ + DC / 64 * NH * 128, &maps.qr, 0, hg * NH, z, &sh.q_full);
+      }
+      __syncwarp();
+    }
+    if (k > 0) ptx::mbar_wait_bounded(&sh.q_full, (k - 1) & 1);
+    __syncwarp();
+  } else if (warp == kMmaWarp) {
+    // ------------------------------------------------------------------ products
+    // (One elected thread issues: the compiler then keeps descriptors in uniform registers; with `lane == 0` a product took 90
+    // cycles to issue and the CTA 4500 per tile.)
+    if (n_tiles > 0) {
+      constexpr uint32_t idesc_s = umma::instr_desc(64, NH, false);
+      constexpr uint32_t idesc_o = umma::instr_desc(128, NH, false, true);
+      const uint64_t hi = (uint64_t)umma::smem_desc_sw128(0, 0, 1024) & 0xffffffff00000000ull;
+      const uint32_t st = ptx::smem_u32(stage0), q_lo = (ptx::smem_u32(sQ) >> 4) | 1u << 16, p_lo = (ptx::smem_u32(sP) >> 4) | 1u << 16;
+      const int steps_r = p.dr / 16;
+      Walk ws(sh), wp(sh);                               // the parts that scores and sums are at
+      int s_at = 0, p_at = 0, n_q = 0;                   // tile within the walk's part; units begun
+      ws.t_end = ws.t_begin = wp.t_end = wp.t_begin = 0;
+      // The warp looks at what is there, a tile for the next scores or weights for the next sums, and issues that: sums that
+      // waited behind the scores of a tile still on its way would hold their own tile's stage meanwhile.
+      int s_next = 0, p_next = 0, s_stage = 0, p_stage = 0, s_phase = 0;
+      uint64_t t0 = 0;
+      for (uint32_t spins = 0; p_next < n_tiles;) {
+        bool moved = false;
+        if (p_next < s_next && __all_sync(0xffffffffu, ptx::mbar_test_wait(&sh.p_full, p_next & 1))) {
+          umma::fence_after_sync();
+          bool fresh = false;
+          if (p_at == wp.t_end) { wp.next(p); p_at = wp.t_begin; fresh = true; }
+          const uint32_t a_lo = ((st + p_stage * kStage) >> 4) | (uint32_t)(kBox >> 4) << 16;
+          if (umma::elect_one()) {
+#pragma unroll
+            for (int m = 0; m < DC / 128; ++m)
+#pragma unroll
+            {
+#pragma unroll
+              for (int kk = 0; kk < 4; ++kk)
+                umma::mma_bf16(tmem + (uint32_t)(m * NH), hi | (a_lo + ((2 * m * kBox + kk * 2048) >> 4)), hi | (p_lo + 2 * kk), idesc_o,
+                               (!fresh || kk > 0) ? 1u : 0u);
+            }
+            umma::commit(&sh.o_done);
+            umma::commit(&sh.empty[p_stage]);
+          }
+          __syncwarp();
+          ++p_at;
+          ++p_next;
+          if (++p_stage == p.stages) p_stage = 0;
+          moved = true;
+        }
+        if (s_next < n_tiles && s_next <= p_next + 1) {  // (its buffer held the scores of s_next - 2, read before their weights were published)
+          if (s_at == ws.t_end) { ws.next(p); s_at = ws.t_begin; ++n_q; }
+          uint64_t* full = &sh.full[s_stage * kGroups];
+          if (__all_sync(0xffffffffu, ptx::mbar_test_wait(full + 1, s_phase) && ptx::mbar_test_wait(&sh.q_full, (n_q - 1) & 1))) {
+            // the first channels are there, the others on their way
+            umma::fence_after_sync();
+            const uint32_t d = s_tmem + (uint32_t)((s_next & 1) * NH);
+            const uint32_t a_lo = ((st + s_stage * kStage) >> 4) | 1u << 16;
+            ++s_at;
+            bool ok = true;
+#pragma unroll
+            for (int g = 1; g <= kGroups; ++g) {         // the rotary chunk last
+              ok = ok && umma::warp_wait(g < kGroups ? full + g : full, s_phase, &sh.abort, p.dev_status);
+              if (ok && umma::elect_one()) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                  const int c = g < kGroups ? 2 * g - 2 + (k >> 2) : kChunks - 1 + (k >> 2), ks = k & 3;
+                  if (c < kChunks - 1 || (k < 4 && ks < steps_r))
+                    umma::mma_bf16(d, hi | (a_lo + ((c * kBox + ks * 32) >> 4)), hi | (q_lo + ((c * NH * 128 + ks * 32) >> 4)), idesc_s,
+                                   (g > 1 || k > 0) ? 1u : 0u);
+                }
+                if (g == kGroups) {
+                  umma::commit(&sh.s_full[s_next & 1]);
+                  if (s_at == ws.t_end) umma::commit(&sh.q_empty);
+                }
+              }
+              __syncwarp();
+            }
+            if (!ok) break;
+            ++s_next;
+            if (++s_stage == p.stages) { s_stage = 0; s_phase ^= 1; }
+            moved = true;
+          }
+        }
+        if (moved) { t0 = 0; continue; }
+        if ((++spins & 255u) == 0) {
+          const uint64_t now = ptx::globaltimer_ns();
+          if (t0 == 0) t0 = now;
+          const bool late = now - t0 > ptx::kWaitLimitNs;
+          if (__any_sync(0xffffffffu, late || *(volatile int*)&sh.abort)) {
+            if (late) set_dev_status(p.dev_status, NGC_DEV_TIMEOUT);
+            *(volatile int*)&sh.abort = 1;
+            break;
+          }
+        }
+      }
+      if (umma::elect_one()) umma::commit(&sh.drain);    // everything issued has completed before tensor memory is released
+      __syncwarp();
+      ptx::mbar_wait_bounded(&sh.drain, 0);
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------------ softmax
+    const int nh = min(NH, p.H - hg * NH);               // heads of this CTA
+    for (int u = piece; u < U; u += p.pieces)            // empty sequences
+      if (unit_len(p, u) == 0) {
+        const int64_t o = (((int64_t)p.layer_begin * p.B + u) * p.H + hg * NH) * DC;
+        for (int x = tid; x < nh * DC; x += 128)
+          if (p.out_bf16) ((__nv_bfloat16*)p.out)[o + x] = __float2bfloat16(0.f); else ((float*)p.out)[o + x] = 0.f;
+      }
+    const uint32_t lane_base = (uint32_t)(32 * warp) << 16;
+    const int row_lo = 16 * warp + (lane >> 2);          // tokens row_lo and row_lo + 8 of the tile, heads 8 j + 2 (lane % 4) + {0, 1}
+    const uint32_t p_addr = ptx::smem_u32(sP);
+    // matrix stores: lane i gives the address of row i % 8 of matrix i / 8: heads 8 (j + i / 16) + i % 8, token octet 2 warp + (i / 8) % 2
+    const int st_head = 8 * (lane >> 4) + (lane & 7), st_piece = 2 * warp + ((lane >> 3) & 1);
+    const uint32_t st_addr = p_addr + st_head * 128 + ((st_piece ^ (st_head & 7)) << 4);
+    constexpr int NC = NH / 4;                           // columns per thread
+    int t = 0;
+    bool gone = false, ok = true;                        // ok: this warp's waits have ended well; the four leave together, at a vote
+    Walk w(sh);
+    while (!gone && w.next(p)) {
+      float m[NC], l[NC];
+#pragma unroll
+      for (int j = 0; j < NC; ++j) { m[j] = -INFINITY; l[j] = 0.f; }
+      for (int i = w.t_begin; i < w.t_end; ++i, ++t) {
+        ok = umma::warp_wait(&sh.s_full[t & 1], (t >> 1) & 1, &sh.abort, p.dev_status) && ok;
+        umma::fence_after_sync();
+        uint32_t z[NH / 2];
+        ld_frags<NH>(s_tmem + lane_base + (uint32_t)((t & 1) * NH), z);
+        umma::tmem_ld_wait();
+        const int n = w.len - i * kTile;
+        if (n < kTile) {
+#pragma unroll
+          for (int j = 0; j < NH / 2; ++j)
+            if (row_lo + ((j & 2) ? 8 : 0) >= n) z[j] = 0xff800000u;
+        }
+        bool grow = false;
+#pragma unroll
+        for (int j = 0; j < NH / 2; ++j) {
+          const int c = (j >> 2) * 2 + (j & 1);
+          grow = grow || __uint_as_float(z[j]) * p.scale_log2 > m[c] + kLazy;
+        }
+        if (softmax_any(grow || !ok || i == w.t_begin)) {
+          if (i > w.t_begin) ok = umma::warp_wait(&sh.o_done, (t - 1) & 1, &sh.abort, p.dev_status) && ok;
+          if (softmax_any(!ok)) { gone = true; break; }
+          // new maxima: columns over this warp's 16 tokens, then over the warps
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            const int j = (c >> 1) * 4 + (c & 1);
+            float x = fmaxf(__uint_as_float(z[j]), __uint_as_float(z[j + 2]));
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+            if (lane < 4) sh.ex[warp][8 * (c >> 1) + 2 * lane + (c & 1)] = x;
+          }
+          softmax_sync();
+          if (tid < NH) {
+            const float x = fmaxf(fmaxf(sh.ex[0][tid], sh.ex[1][tid]), fmaxf(sh.ex[2][tid], sh.ex[3][tid])) * p.scale_log2;
+            const float was = i == w.t_begin ? -INFINITY : sh.m[tid], now = fmaxf(was, x);
+            sh.m[tid] = now;
+            sh.alpha[tid] = now == -INFINITY ? 1.f : ptx::ex2_approx(was - now);
+          }
+          softmax_sync();
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            const int col = 8 * (c >> 1) + 2 * (lane & 3) + (c & 1);
+            m[c] = sh.m[col];
+            l[c] *= sh.alpha[col];
+          }
+          if (i > w.t_begin) {                           // the sums so far follow
+            umma::fence_after_sync();
+#pragma unroll 1
+            for (int mt = 0; mt < DC / 128; ++mt)
+#pragma unroll 1
+              for (int c0 = 0; c0 < NH; c0 += 16) {
+                uint32_t o[16];
+                const uint32_t a = tmem + lane_base + (uint32_t)(mt * NH + c0);
+                umma::tmem_ld16(a, o);
+                umma::tmem_ld_wait();
+#pragma unroll
+                for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * sh.alpha[c0 + c]);
+                umma::tmem_st8(a, o);
+                umma::tmem_st8(a + 8, o + 8);
+              }
+            umma::tmem_st_wait();
+          }
+        }
+        // weights: rounded to bf16 for the second product, summed before that
+        float m_eff[NC];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) m_eff[c] = m[c] == -INFINITY ? 0.f : m[c];
+        uint32_t pk[NH / 4];
+#pragma unroll
+        for (int j = 0; j < NH / 8; ++j)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {                  // column group j, token octet k
+            const float p0 = ptx::ex2_approx(fmaf(__uint_as_float(z[4 * j + 2 * k]), p.scale_log2, -m_eff[2 * j]));
+            const float p1 = ptx::ex2_approx(fmaf(__uint_as_float(z[4 * j + 2 * k + 1]), p.scale_log2, -m_eff[2 * j + 1]));
+            l[2 * j] += p0;
+            l[2 * j + 1] += p1;
+            pk[2 * j + k] = ptx::pack_bf16x2(p0, p1);
+          }
+        if (t > 0) ok = umma::warp_wait(&sh.o_done, (t - 1) & 1, &sh.abort, p.dev_status) && ok;     // the weights' buffer is free again
+#pragma unroll
+        for (int j = 0; j < NH / 16; ++j)                // 16 heads per matrix store
+          stmatrix_x4_trans(st_addr + j * 16 * 128, pk[4 * j], pk[4 * j + 1], pk[4 * j + 2], pk[4 * j + 3]);
+        ptx::fence_proxy_async();
+        umma::fence_before_sync();
+        ptx::mbar_arrive(&sh.p_full);
+      }
+      if (gone) break;
+      // ---- end of the part: sums of weights over all tokens, then the rows leave
+      ok = umma::warp_wait(&sh.o_done, (t - 1) & 1, &sh.abort, p.dev_status) && ok;
+      if (softmax_any(!ok)) break;
+      umma::fence_after_sync();
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) l[c] += __shfl_xor_sync(0xffffffffu, l[c], o);
+        if (lane < 4) sh.ex[warp][8 * (c >> 1) + 2 * lane + (c & 1)] = l[c];
+      }
+      softmax_sync();
+      const bool whole = w.t_begin == 0 && w.t_end == w.n;
+      const int64_t slot = ((int64_t)piece * 2 + (w.t_begin > 0 ? 0 : 1)) * p.heads_pad + hg * NH;
+      if (tid < NH) {
+        const float sum = sh.ex[0][tid] + sh.ex[1][tid] + sh.ex[2][tid] + sh.ex[3][tid];
+        if (whole) sh.alpha[tid] = 1.f / sum;
+        else p.part_ml[slot + tid] = make_float2(sh.m[tid], sum);
+      }
+      if (tid == 0 && hg == 0 && w.t_begin == 0 && !whole) {
+        const int used = pieces_used(sh.total, p.pieces), at = sh.g0 + t - (w.t_end - w.t_begin);      // first tile of the unit
+        p.plan[piece] = make_int2(w.unit, piece_of(sh.total, used, at + w.n - 1));
+      }
+      softmax_sync();
+      const int64_t out_row = ((int64_t)p.layer_begin * p.B + w.unit) * p.H + hg * NH;
+#pragma unroll 1
+      for (int mt = 0; mt < DC / 128; ++mt) {
+        const int d = 128 * mt + 32 * warp + lane;       // this thread's channel
+#pragma unroll 1
+        for (int c0 = 0; c0 < nh; c0 += 16) {
+          uint32_t o[16];
+          umma::tmem_ld16(tmem + lane_base + (uint32_t)(mt * NH + c0), o);
+          umma::tmem_ld_wait();
+          if (!whole) {
+#pragma unroll
+            for (int c = 0; c < 16; ++c)
+              if (c0 + c < nh) p.part_o[(slot + c0 + c) * DC + d] = __uint_as_float(o[c]);
+          } else if (!p.out_bf16) {
+#pragma unroll
+            for (int c = 0; c < 16; ++c)
+              if (c0 + c < nh) ((float*)p.out)[(out_row + c0 + c) * DC + d] = __uint_as_float(o[c]) * sh.alpha[c0 + c];
+          } else {
+            // two heads at a time: even lanes take the first head's channels d, d + 1, odd lanes the second's d - 1, d
+#pragma unroll
+            for (int c = 0; c < 16; c += 2) {
+              const float v0 = __uint_as_float(o[c]) * sh.alpha[c0 + c], v1 = __uint_as_float(o[c + 1]) * sh.alpha[c0 + c + 1];
+              const float far = __shfl_xor_sync(0xffffffffu, (lane & 1) ? v0 : v1, 1);
+              const int h = c0 + c + (lane & 1);
+              if (h < nh)
+                *reinterpret_cast<uint32_t*>((__nv_bfloat16*)p.out + (out_row + h) * DC + (d & ~1)) =
+                    (lane & 1) ? ptx::pack_bf16x2(far, v1) : ptx::pack_bf16x2(v0, far);
+            }
+          }
+        }
+      }
+      umma::fence_before_sync();                         // (the next unit's first sums overwrite O once its weights are published)
+    }
+  }
+  // ---- every role has left its loops; nothing of this CTA is in flight any more
+  umma::fence_before_sync();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    umma::fence_after_sync();
+    umma::tmem_dealloc(tmem, kCols);
+  }
+}
+
+// Joins the parts of the unit that begins in piece blockIdx.x and goes on behind it: four heads per CTA, 128 threads each, four
+// channels per thread.  Bound by latency: plan -> maxima -> sums.
+__global__ void __launch_bounds__(512) latent_join_kernel(LatentDecodeParams p) {
+  __shared__ float weight[4][kMaxCtas];
+  ptx::grid_dep_wait();
+  const int i0 = blockIdx.x;
+  const int2 plan = p.plan[i0];
+  if (plan.x < 0) return;
+  const int hh = threadIdx.x >> 7, h = 4 * blockIdx.y + hh, lane = threadIdx.x & 31, n = plan.y - i0 + 1;
+  auto slot = [&](int i) { return ((int64_t)(i0 + i) * 2 + (i == 0 ? 1 : 0)) * p.heads_pad + h; };
+  float total = 0.f;
+  if (h < p.H) {                                         // (every warp of a head for itself: lanes take parts)
+    float2 ml[(kMaxCtas + 31) / 32];
+    float m = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < (kMaxCtas + 31) / 32; ++k) {
+      ml[k] = 32 * k + lane < n ? p.part_ml[slot(32 * k + lane)] : make_float2(-INFINITY, 0.f);
+      m = fmaxf(m, ml[k].x);
+    }
+    m = warp_max(m);
+    if (m == -INFINITY) m = 0.f;
+#pragma unroll
+    for (int k = 0; k < (kMaxCtas + 31) / 32; ++k) {
+      const float f = ptx::ex2_approx(ml[k].x - m);
+      total += ml[k].y * f;
+      if ((threadIdx.x & 96) == 0 && 32 * k + lane < n) weight[hh][32 * k + lane] = f;
+    }
+    total = warp_sum(total);
+  }
+  __syncthreads();
+  const int c = 4 * (threadIdx.x & 127);
+  if (h >= p.H || c >= p.dc) return;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (int i = 0; i < n; ++i) {
+    const float4 v = *reinterpret_cast<const float4*>(p.part_o + slot(i) * p.dc + c);
+    const float f = weight[hh][i];
+    o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f;
+  }
+  const float inv = 1.f / total;
+  const int64_t at = (((int64_t)p.layer_begin * p.B + plan.x) * p.H + h) * p.dc + c;
+  if (p.out_bf16)
+    *reinterpret_cast<uint2*>((__nv_bfloat16*)p.out + at) = make_uint2(ptx::pack_bf16x2(o.x * inv, o.y * inv), ptx::pack_bf16x2(o.z * inv, o.w * inv));
+  else
+    *reinterpret_cast<float4*>((float*)p.out + at) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+}
+
+// bf16 rows of `d` channels, `mid` x `outer` of them, as a 3-D tensor; box = 64 channels x `box` rows of the middle axis.
+// Channels and rows of a box that the tensor does not have read as zeros.
+bool make_box_map(CUtensorMap* map, const void* base, int d, int64_t mid, int64_t outer, int box) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)mid, (cuuint64_t)outer};
+  cuuint64_t strides[2] = {(cuuint64_t)d * 2, (cuuint64_t)mid * d * 2};
+  cuuint32_t size[3] = {64, (cuuint32_t)box, 1}, step[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, size, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Heads per CTA: as many columns of the products as the heads need, 64 at most.
+int heads_per_cta(int H) { return H <= 16 ? 16 : (H <= 32 ? 32 : 64); }
+
+struct Space { int nh, groups, pieces; size_t ml, plan, all; };
+Space space_of(const ngc_latent_pool* c, int H) {
+  Space w;
+  w.nh = heads_per_cta(H);
+  w.groups = (H + w.nh - 1) / w.nh;
+  w.pieces = kMaxCtas / w.groups;
+  const size_t rows = (size_t)w.pieces * 2 * w.groups * w.nh;
+  w.ml = align256(rows * c->d_latent * 4);
+  w.plan = w.ml + align256(rows * 8);
+  w.all = w.plan + align256((size_t)w.pieces * 8);
+  return w;
+}
+
+template <int NH, int DC> int launch(const Maps& maps, LatentDecodeParams& p, cudaStream_t stream) {
+  constexpr int kChunks = DC / 64 + 1, kFixed = kStaticReserve + 1024 + kChunks * NH * 128 + NH * 128;
+  p.stages = (kSmemLimit - kFixed) / (kChunks * kBox);
+  if (p.stages > kMaxStages) p.stages = kMaxStages;
+  if (p.stages * (DC / 128 + 1) > kMaxGroups) p.stages = kMaxGroups / (DC / 128 + 1);
+  static_assert(sizeof(Shared<NH>) <= kStaticReserve, "static shared memory");
+  static PerDeviceOnce once;
+  const int rc = once.run([] {
+    return cudaFuncSetAttribute(latent_decode_kernel<NH, DC>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit - kStaticReserve);
+  });
+  if (rc != NGC_OK) return rc;
+  // (all of it, however little the ring takes: two CTAs of an SM would fight for its tensor memory)
+  NGC_CUDA_TRY(launch_pdl(latent_decode_kernel<NH, DC>, dim3(p.pieces * p.groups), dim3(kThreads), kSmemLimit - kStaticReserve, stream, maps, p));
+  NGC_CUDA_TRY(launch_pdl(latent_join_kernel, dim3(p.pieces, (p.H + 3) / 4), dim3(512), 0, stream, p));
+  return launch_status();
+}
+
+template <int NH> int launch_heads(const Maps& maps, LatentDecodeParams& p, cudaStream_t stream) {
+  switch (p.dc) {
+    case 128: return launch<NH, 128>(maps, p, stream);
+    case 256: return launch<NH, 256>(maps, p, stream);
+    case 384: return launch<NH, 384>(maps, p, stream);
+    default: return launch<NH, 512>(maps, p, stream);
   }
 }
 
 }  // namespace
 }  // namespace ngc
 
-extern "C" size_t ngc_latent_decode_workspace_bytes(const ngc_latent_pool* c, int H) { return c && H > 0 ? 256 : 0; }
+extern "C" size_t ngc_latent_decode_workspace_bytes(const ngc_latent_pool* c, int H) {
+  return c && c->d_latent > 0 && H > 0 ? ngc::space_of(c, H).all : 0;
+}
 
 extern "C" int ngc_latent_decode(const ngc_latent_pool* c, const void* q_latent, const void* q_rope, int H, int layer_begin, int layer_end,
                                  float scale, void* out, int out_dtype, void* ws, size_t ws_bytes, int32_t* dev_status, ngc_stream stream) {
@@ -79,14 +680,22 @@ extern "C" int ngc_latent_decode(const ngc_latent_pool* c, const void* q_latent,
       !(scale > 0.f && scale <= 2e38f) || (out_dtype != NGC_F32 && out_dtype != NGC_BF16) || !aligned16(c->rows) || !aligned16(q_latent) ||
       !aligned16(q_rope) || !aligned16(out))
     return NGC_ERR_INVALID_ARG;
-  if (c->dtype != NGC_BF16 || !built_latent_dims(c->d_latent, c->d_rope) || H > 128) return NGC_ERR_UNSUPPORTED;
-  if (ws_bytes < ngc_latent_decode_workspace_bytes(c, H) || !ws || ((uintptr_t)ws & 255)) return NGC_ERR_WORKSPACE;
+  if (c->dtype != NGC_BF16 || !built_latent_dims(c->d_latent, c->d_rope) || H > 128 || (int64_t)c->L * c->B > 0x7fffffffLL ||
+      (int64_t)(layer_end - layer_begin) * c->B * (((int64_t)c->pages_cap * c->page + kTile - 1) / kTile) > 0x7fffffffLL)
+    return NGC_ERR_UNSUPPORTED;
+  const Space w = space_of(c, H);
+  if (!ws || ws_bytes < w.all || ((uintptr_t)ws & 255)) return NGC_ERR_WORKSPACE;
   LatentDecodeParams p;
-  p.rows = (const __nv_bfloat16*)c->rows; p.table = c->page_table; p.lens = c->lens;
-  p.ql = (const __nv_bfloat16*)q_latent; p.qr = (const __nv_bfloat16*)q_rope; p.out = out; p.dev_status = dev_status;
+  p.table = c->page_table; p.lens = c->lens; p.out = out; p.dev_status = dev_status;
+  p.part_o = (float*)ws; p.part_ml = (float2*)((uint8_t*)ws + w.ml); p.plan = (int2*)((uint8_t*)ws + w.plan);
   p.B = c->B; p.H = H; p.G = lists_G(c->lists, c->L, 1); p.dc = c->d_latent; p.dr = c->d_rope; p.page = c->page; p.cap = c->pages_cap;
-  p.n_pages = c->n_pages; p.lists = c->lists; p.layer_begin = layer_begin; p.out_bf16 = out_dtype == NGC_BF16;
-  p.scale_log2 = scale * 1.4426950408889634f;
-  latent_decode_kernel<<<dim3(H, c->B, layer_end - layer_begin), 256, 0, stream>>>(p);
-  return launch_status();
+  p.n_pages = c->n_pages; p.lists = c->lists; p.layer_begin = layer_begin; p.n_layers = layer_end - layer_begin;
+  p.out_bf16 = out_dtype == NGC_BF16; p.stages = 0; p.pieces = w.pieces; p.groups = w.groups;
+  p.heads_pad = w.groups * w.nh; p.scale_log2 = scale * 1.4426950408889634f;
+  Maps maps;
+  const int64_t LB = (int64_t)c->L * c->B;
+  if (!make_rows_map(&maps.rows, c->rows, (int64_t)c->L * c->n_pages * c->page, c->page, c->d_latent + c->d_rope) ||
+      !make_box_map(&maps.ql, q_latent, c->d_latent, H, LB, w.nh) || !make_box_map(&maps.qr, q_rope, c->d_rope, H, LB, w.nh))
+    return NGC_ERR_UNSUPPORTED;
+  return w.nh == 16 ? launch_heads<16>(maps, p, stream) : w.nh == 32 ? launch_heads<32>(maps, p, stream) : launch_heads<64>(maps, p, stream);
 }
