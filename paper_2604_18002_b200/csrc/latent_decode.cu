@@ -15,7 +15,7 @@
 //   mender (1 warp)       rows behind a unit's last token: zeros (they may hold anything; a NaN times a zero weight is NaN)
 //   queries (1 thread)    the heads' queries of the next unit, when the last unit's scores are done
 //   MMA (1 thread)        S^T of tile i + 1 is issued before the sums of tile i, so it runs under the softmax of tile i
-//   softmax (4 warps)     16 tokens each.  A thread holds two tokens of a quarter of the heads; weights go to shared memory
+//   softmax (4 warps per 16 heads)  16 tokens each.  A thread holds two tokens of four heads; weights go to shared memory
 //                         by transposing matrix stores, as the K-major B operand.  The maximum that the exponentials refer to
 //                         moves only when a score exceeds it by 2^8 (exact in bf16 and fp32), which is one vote per tile.
 // Every wait is bounded; one that runs out makes all roles leave and is reported.
@@ -32,10 +32,13 @@ namespace {
 
 constexpr int kTile = 64;                      // tokens per tile
 constexpr int kBox = kTile * 128;              // 64 tokens x 64 channels
-constexpr int kMaxStages = 8;
-constexpr int kMaxGroups = 20;                 // groups of all stages: channels whose arrival is waited for together
-constexpr int kThreads = 256;                  // warps 0-3 softmax, 4 MMA, 5 producer, 6 mender, 7 queries
-constexpr int kMmaWarp = 4, kProducerWarp = 5, kMenderWarp = 6, kQueryWarp = 7;
+constexpr int kPair = 2 * kBox;                // 128 channels of the latent part: what arrives, is used and makes room together
+constexpr int kMaxPairs = 9, kMaxStages = 4;  // in shared memory, at most
+// Warps: softmax, four for 16 heads, else eight (a warp reaches a quarter of tensor memory's lanes; 16 for 64 heads: 147 -> 157 us
+// for 24 sequences of two layers, 128 heads), then one each for the MMAs, the first and
+// the second page of a tile, the mender, the queries.
+__host__ __device__ constexpr int softmax_warps(int nh) { return nh < 32 ? 4 : 8; }
+__host__ __device__ constexpr int cta_threads(int nh) { return (softmax_warps(nh) + 5) * 32; }
 constexpr int kSmemLimit = 227 * 1024;
 constexpr int kStaticReserve = 2048;           // barriers and exchange buffers (static shared memory)
 constexpr float kLazy = 8.f;
@@ -58,12 +61,12 @@ struct LatentDecodeParams {
 struct Maps { CUtensorMap rows, ql, qr; };
 
 template <int NH> struct Shared {
-  uint64_t full[kMaxGroups], empty[kMaxStages], raw[kMaxStages];
+  uint64_t full[kMaxPairs], empty[kMaxPairs], raw[kMaxPairs], r_full[kMaxStages], r_empty[kMaxStages];
   uint64_t s_full[2], p_full, o_done, q_full, q_empty, drain;
   uint32_t tmem;
   int abort;
-  int u0, t0, g0, n_tiles, total;              // where this CTA's piece begins, how many tiles it has, tiles of the call
-  int warp_sum[kThreads / 32];
+  int u0, t0, len0, g0, n_tiles, total;        // where this CTA's piece begins, how many tiles it has, tiles of the call
+  int warp_sum[cta_threads(NH) / 32];
   float ex[4][NH];                             // per warp: column maxima, later sums of weights
   float m[NH], alpha[NH];                      // the maximum that the exponentials refer to (log2 units), and what its last move costs
 };
@@ -84,16 +87,26 @@ __device__ __forceinline__ int piece_of(int total, int pieces, int g) {
   return i;
 }
 
+// Position in a ring: the slot to fill or use next, and the parity of its use.
+struct Ring {
+  int n, slot, phase;
+  bool first;                   // no slot has been used twice
+  __device__ __forceinline__ explicit Ring(int slots) : n(slots), slot(0), phase(0), first(true) {}
+  __device__ __forceinline__ bool fresh() const { return first; }
+  __device__ __forceinline__ void next() { if (++slot == n) { slot = 0; phase ^= 1; first = false; } }
+};
+
 // The parts of units that make up a piece, in order.
 struct Walk {
-  int u, t, left;               // next unit, its next tile, tiles left in the piece
+  int u, t, left, first;        // next unit, its next tile, tiles left in the piece; length of the piece's first unit
   int unit, t_begin, t_end, n, len;            // the current part: tiles t_begin .. t_end of the n of unit
-  template <int NH> __device__ __forceinline__ explicit Walk(const Shared<NH>& sh) : u(sh.u0), t(sh.t0), left(sh.n_tiles) {}
+  template <int NH> __device__ __forceinline__ explicit Walk(const Shared<NH>& sh) : u(sh.u0), t(sh.t0), left(sh.n_tiles), first(sh.len0) {}
   __device__ __forceinline__ bool next(const LatentDecodeParams& p) {
     if (left <= 0) return false;
     do {
       if (u >= p.n_layers * p.B) return false;           // (the lengths changed under the call)
-      len = unit_len(p, u);
+      len = first > 0 ? first : unit_len(p, u);
+      first = 0;
       n = len > 0 ? (len + kTile - 1) / kTile : 0;
       unit = u++;
     } while (n == 0);           // (left > 0: a unit with tiles follows)
@@ -106,50 +119,52 @@ struct Walk {
 };
 
 // 16 lanes x 8 columns per matrix fragment: register 4 j + {0, 1}: row lane / 4, columns 8 j + 2 (lane % 4) + {0, 1}; 4 j + {2, 3}: row + 8.
-template <int NH> __device__ __forceinline__ void ld_frags(uint32_t taddr, uint32_t* r);
-template <> __device__ __forceinline__ void ld_frags<16>(uint32_t taddr, uint32_t* r) {
+__device__ __forceinline__ void ld_frags(uint32_t taddr, uint32_t* r) {
   asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr));
 }
-template <> __device__ __forceinline__ void ld_frags<32>(uint32_t taddr, uint32_t* r) { ld_frags<16>(taddr, r); ld_frags<16>(taddr + 16, r + 8); }
-template <> __device__ __forceinline__ void ld_frags<64>(uint32_t taddr, uint32_t* r) { ld_frags<32>(taddr, r); ld_frags<32>(taddr + 32, r + 16); }
 
 __device__ __forceinline__ void stmatrix_x4_trans(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
   asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r0), "r"(r1), "r"(r2), "r"(r3) : "memory");
 }
 
-// Barrier of the four softmax warps; true to all where `mine` is true to one.
-__device__ __forceinline__ bool softmax_any(bool mine) {
+// Barrier of the softmax warps; true to all where `mine` is true to one.
+template <int N> __device__ __forceinline__ bool softmax_any(bool mine) {
   uint32_t r;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\tbarrier.cta.red.or.pred p, 1, 128, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(r) : "r"((uint32_t)mine) : "memory");
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\tbarrier.cta.red.or.pred p, 1, %2, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(r) : "r"((uint32_t)mine), "n"(N) : "memory");
   return r != 0;
 }
-__device__ __forceinline__ void softmax_sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void softmax_sync() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(N) : "memory"); }
 
 template <int NH, int DC>
-__global__ void __launch_bounds__(kThreads, 1) latent_decode_kernel(const __grid_constant__ Maps maps, LatentDecodeParams p) {
+__global__ void __launch_bounds__(cta_threads(NH), 1) latent_decode_kernel(const __grid_constant__ Maps maps, LatentDecodeParams p) {
+  constexpr int kSoft = softmax_warps(NH), kThreads = cta_threads(NH);
+  constexpr int kMmaWarp = kSoft, kProducerWarp = kSoft + 1, kMenderWarp = kSoft + 3, kQueryWarp = kSoft + 4;
   extern __shared__ uint8_t smem_dyn[];
   __shared__ Shared<NH> sh;
   uint8_t* sQ = (uint8_t*)(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);     // [chunks][NH rows x 128 B]
-  constexpr int kChunks = DC / 64 + 1, kStage = kChunks * kBox;                  // the last chunk: rotary part, zeros behind it
-  constexpr int kGroups = DC / 128 + 1;                                          // group 0: the last chunk; group g: chunks 2 g - 2, 2 g - 1
+  constexpr int kChunks = DC / 64 + 1, kM = DC / 128;                            // 64-channel chunks of a row (the last: rotary part, then zeros), pairs
+  constexpr int kStage = kChunks * kBox;
   uint8_t* sP = sQ + kChunks * NH * 128;                                         // [NH rows x 64 tokens]
-  uint8_t* stage0 = sP + NH * 128;                                               // [stages][chunks][64 tokens x 128 B]
+  uint8_t* sK = sP + NH * 128;                                                   // [stages][chunks][64 tokens x 128 B]
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int piece = blockIdx.x / p.groups, hg = blockIdx.x % p.groups;
   constexpr uint32_t kCols = NH == 64 ? 512 : (NH == 32 ? 256 : 128);            // O^T: 4 x NH, S^T: 2 x NH
   const int U = p.n_layers * p.B;
 
-  if (tid == 0) {
-    for (int s = 0; s < p.stages; ++s) { ptx::mbar_init(&sh.raw[s], 1); ptx::mbar_init(&sh.empty[s], 1); }
-    for (int s = 0; s < p.stages * kGroups; ++s) ptx::mbar_init(&sh.full[s], 1);
-    ptx::mbar_init(&sh.s_full[0], 1); ptx::mbar_init(&sh.s_full[1], 1);
-    ptx::mbar_init(&sh.p_full, 128);
-    ptx::mbar_init(&sh.o_done, 1);
-    ptx::mbar_init(&sh.q_full, 1); ptx::mbar_init(&sh.q_empty, 1); ptx::mbar_init(&sh.drain, 1);
+  if (warp == 0) {
+    if (lane < p.stages * kM) { ptx::mbar_init(&sh.full[lane], kTile / p.page); ptx::mbar_init(&sh.empty[lane], 1); ptx::mbar_init(&sh.raw[lane], kTile / p.page); }
+    if (lane < p.stages) { ptx::mbar_init(&sh.r_full[lane], kTile / p.page); ptx::mbar_init(&sh.r_empty[lane], 1); }
+    if (lane == 31) {
+      ptx::mbar_init(&sh.s_full[0], 1); ptx::mbar_init(&sh.s_full[1], 1);
+      ptx::mbar_init(&sh.p_full, kSoft * 32);
+      ptx::mbar_init(&sh.o_done, 1);
+      ptx::mbar_init(&sh.q_full, 1); ptx::mbar_init(&sh.q_empty, 1); ptx::mbar_init(&sh.drain, 1);
+      sh.abort = 0; sh.u0 = 0; sh.t0 = 0; sh.len0 = 0;
+    }
     ptx::fence_barrier_init();
-    sh.abort = 0; sh.u0 = 0; sh.t0 = 0;
+  } else if (warp == kProducerWarp && lane == 0) {
     ptx::prefetch_tensormap(&maps.rows); ptx::prefetch_tensormap(&maps.ql); ptx::prefetch_tensormap(&maps.qr);
   }
   if (warp == kMmaWarp) umma::tmem_alloc(&sh.tmem, kCols);
@@ -157,11 +172,11 @@ __global__ void __launch_bounds__(kThreads, 1) latent_decode_kernel(const __grid
   // ---- the line of tiles, and where this piece begins: every thread sums a run of units
   {
     const int per = (U + kThreads - 1) / kThreads, u_lo = min(tid * per, U), u_hi = min(u_lo + per, U);
-    int mine = 0;
+    int mine = 0, len = 0;
     for (int u = u_lo; u < u_hi; ++u) {
-      const int n = unit_len(p, u);
-      if (n < 0) set_dev_status(p.dev_status, NGC_DEV_BAD_COUNTS);
-      mine += (max(n, 0) + kTile - 1) / kTile;
+      len = unit_len(p, u);
+      if (len < 0) set_dev_status(p.dev_status, NGC_DEV_BAD_COUNTS);
+      mine += (max(len, 0) + kTile - 1) / kTile;
     }
     int incl = mine;
 #pragma unroll
@@ -176,8 +191,9 @@ __global__ void __launch_bounds__(kThreads, 1) latent_decode_kernel(const __grid
     int at = before + incl - mine;                       // first tile of this thread's run
     if (g0 < g1 && g0 >= at && g0 < at + mine) {
       for (int u = u_lo; u < u_hi; ++u) {
-        const int n = (max(unit_len(p, u), 0) + kTile - 1) / kTile;
-        if (g0 < at + n) { sh.u0 = u; sh.t0 = g0 - at; break; }
+        if (per > 1) len = unit_len(p, u);
+        const int n = (max(len, 0) + kTile - 1) / kTile;
+        if (g0 < at + n) { sh.u0 = u; sh.t0 = g0 - at; sh.len0 = len; break; }
         at += n;
       }
     }
@@ -194,89 +210,103 @@ __global__ void __launch_bounds__(kThreads, 1) latent_decode_kernel(const __grid
   const uint32_t s_tmem = tmem + 4 * NH;
   ptx::grid_dep_launch();                                // (all CTAs are resident: the second kernel's can wait beside them)
 
-  if (warp == kProducerWarp) {
-    // ------------------------------------------------------------------ rows of the tiles
-    int t = 0;
-    uint32_t raw_last = 0, raw_phase = 0;                // bit s: stage s was last filled through raw / parity of raw's next use
-    int st = 0, phase = 0;                               // stage of tile t, parity of its uses
-    bool ok = true;
-    Walk w(sh);
-    while (ok && w.next(p)) {
-      const int l = p.layer_begin + w.unit / p.B, b = w.unit % p.B;
-      const int32_t* row = p.table + ((int64_t)b * p.G + list_of(p.lists, l, 0, 1)) * p.cap;
-      const int n_pages = (w.len + p.page - 1) / p.page, per = kTile / p.page;
-      int have = w.t_begin * per, pages = 0;             // lane j holds page `have - 32 + j` of the sequence
-      auto page_row = [&](int j) {                       // first row of the sequence's page j
-        const int y = (l * p.n_pages + __shfl_sync(0xffffffffu, pages, j - (have - 32))) * p.page;
-        return NGC_IN_BOUNDS(p.dev_status, y >= 0 && y / p.page < (p.layer_begin + p.n_layers) * p.n_pages) ? y : 0;
-      };
-      for (int i = w.t_begin; i < w.t_end; ++i, ++t) {
-        if (i * per >= have || i == w.t_begin) {
-          int pg = i * per + lane < n_pages ? row[i * per + lane] : 0;
-          if ((uint32_t)pg >= (uint32_t)p.n_pages) {
-            if (i * per + lane < w.t_end * per) set_dev_status(p.dev_status, NGC_DEV_BAD_PAGE);
-            pg = 0;
+  if (warp == kProducerWarp || warp == kProducerWarp + 1) {
+    // ------------------------------------------------------------------ rows of the tiles: a warp per page of a tile
+    const int k = warp - kProducerWarp, per = kTile / p.page;
+    if (k < per) {
+      uint32_t raw_last = 0, raw_phase = 0;              // bit s: pair s was last filled through raw / parity of raw's next use
+      Ring at(p.stages);
+      int issued = 0, done = 0;                          // pairs and rotary parts loaded
+      bool ok = true;
+      Walk w(sh);
+      while (ok && w.next(p)) {
+        const int l = p.layer_begin + w.unit / p.B, b = w.unit % p.B;
+        const int32_t* row = p.table + ((int64_t)b * p.G + list_of(p.lists, l, 0, 1)) * p.cap;
+        const int n_pages = (w.len + p.page - 1) / p.page;
+        int have = 0, pages = 0;                         // lane j holds the page of tile have - 32 + j
+        for (int i = w.t_begin; ok && i < w.t_end; ++i) {
+          if (i >= have) {
+            const int j = (i + lane) * per + k;
+            pages = j < n_pages ? row[j] : 0;
+            if ((uint32_t)pages >= (uint32_t)p.n_pages) {
+              if (i + lane < w.t_end) set_dev_status(p.dev_status, NGC_DEV_BAD_PAGE);
+              pages = 0;
+            }
+            have = i + 32;
           }
-          pages = pg;
-          have = i * per + 32;
-        }
-        const int n = min(kTile, w.len - i * kTile);
-        const bool tail = n < kTile;                     // the mender hands it on
-        const int boxes = min(per, (n + p.page - 1) / p.page);
-        const int y0 = page_row(i * per), y1 = boxes > 1 ? page_row(i * per + 1) : 0;
-        if (t >= p.stages && !umma::warp_wait(&sh.empty[st], phase ^ 1, &sh.abort, p.dev_status)) { ok = false; break; }
-        if (umma::elect_one()) {
-          uint8_t* dst = stage0 + st * kStage;
-          const uint32_t bytes = (uint32_t)(boxes * p.page * 128);
-          ptx::mbar_expect_tx(&sh.full[st * kGroups], bytes);
-          if (tail) ptx::mbar_expect_tx(&sh.raw[st], bytes * (DC / 64));
-          ptx::tma_load_2d(dst + (kChunks - 1) * kBox, &maps.rows, DC, y0, &sh.full[st * kGroups]);
-          if (boxes > 1) ptx::tma_load_2d(dst + (kChunks - 1) * kBox + 32 * 128, &maps.rows, DC, y1, &sh.full[st * kGroups]);
+          const int n = min(kTile, w.len - i * kTile);
+          const bool tail = n < kTile;                   // the mender hands it on
+          const bool mine = k * p.page < n;              // (a short last tile may have no second page)
+          int y = (l * p.n_pages + __shfl_sync(0xffffffffu, pages, i - (have - 32))) * p.page;
+          if (!NGC_IN_BOUNDS(p.dev_status, y >= 0 && y / p.page < (p.layer_begin + p.n_layers) * p.n_pages)) y = 0;
+          const uint32_t bytes = (uint32_t)(p.page * 128);
 #pragma unroll
-          for (int g = 1; g < kGroups; ++g) {
-            uint64_t* bar = tail ? &sh.raw[st] : &sh.full[st * kGroups + g];
-            if (!tail) ptx::mbar_expect_tx(bar, 2 * bytes);
-#pragma unroll
-            for (int c = 2 * g - 2; c < 2 * g; ++c) {
-              ptx::tma_load_2d(dst + c * kBox, &maps.rows, 64 * c, y0, bar);
-              if (boxes > 1) ptx::tma_load_2d(dst + c * kBox + 32 * 128, &maps.rows, 64 * c, y1, bar);
+          for (int m = 0; m < kM; ++m) {
+            const int slot = at.slot * kM + m;
+            ok = ok && (at.fresh() || umma::warp_wait(&sh.empty[slot], at.phase ^ 1, &sh.abort, p.dev_status));
+            if (!ok) break;
+            if (umma::elect_one()) {
+              uint64_t* bar = tail ? &sh.raw[slot] : &sh.full[slot];
+              uint8_t* dst = sK + at.slot * kStage + m * kPair + k * (kBox / 2);
+              if (mine) {
+                ptx::mbar_expect_tx(bar, 2 * bytes);
+                ptx::tma_load_2d(dst, &maps.rows, 128 * m, y, bar);
+                ptx::tma_load_2d(dst + kBox, &maps.rows, 128 * m + 64, y, bar);
+              } else {
+                ptx::mbar_arrive(bar);
+              }
+            }
+            __syncwarp();
+            raw_last = tail ? raw_last | 1u << slot : raw_last & ~(1u << slot);
+            if (tail) raw_phase ^= 1u << slot;
+            ++issued;
+          }
+          ok = ok && (at.fresh() || umma::warp_wait(&sh.r_empty[at.slot], at.phase ^ 1, &sh.abort, p.dev_status));
+          if (!ok) break;
+          if (umma::elect_one()) {
+            if (mine) {
+              ptx::mbar_expect_tx(&sh.r_full[at.slot], bytes);
+              ptx::tma_load_2d(sK + at.slot * kStage + kM * kPair + k * (kBox / 2), &maps.rows, DC, y, &sh.r_full[at.slot]);
+            } else {
+              ptx::mbar_arrive(&sh.r_full[at.slot]);
             }
           }
+          __syncwarp();
+          at.next();
+          ++done;
         }
-        __syncwarp();
-        raw_last = tail ? raw_last | 1u << st : raw_last & ~(1u << st);
-        if (tail) raw_phase ^= 1u << st;
-        if (++st == p.stages) { st = 0; phase ^= 1; }
       }
-    }
-    // nothing is in flight when the CTA ends: the last use of every stage
-    for (int s = 0; s < p.stages; ++s) {
-      const int n = (t - s + p.stages - 1) / p.stages;   // tiles that went through the stage
-      const bool through_raw = raw_last >> s & 1;
-      if (n > 0)
-        for (int g = 0; g < kGroups; ++g)
-          if (!(through_raw && g > 0)) ptx::mbar_wait_bounded(&sh.full[s * kGroups + g], (n - 1) & 1);
-      if (through_raw) ptx::mbar_wait_bounded(&sh.raw[s], ((raw_phase >> s) & 1) ^ 1);
+      // nothing is in flight when the CTA ends: the last use of every barrier
+      for (int x = max(0, issued - p.stages * kM); x < issued; ++x) {
+        const int use = x / (p.stages * kM), slot = x - use * p.stages * kM;
+        if (raw_last >> slot & 1) ptx::mbar_wait_bounded(&sh.raw[slot], ((raw_phase >> slot) & 1) ^ 1);
+        else ptx::mbar_wait_bounded(&sh.full[slot], use & 1);
+      }
+      for (int x = max(0, done - p.stages); x < done; ++x) ptx::mbar_wait_bounded(&sh.r_full[x % p.stages], (x / p.stages) & 1);
     }
     __syncwarp();
   } else if (warp == kMenderWarp) {
     // ------------------------------------------------------------------ rows behind the last token
     int t = 0;
     uint32_t raw_phase = 0;
+    bool ok = true;
     Walk w(sh);
-    while (w.next(p)) {
+    while (ok && w.next(p)) {
       t += w.t_end - w.t_begin;
       const int n = w.len - (w.n - 1) * kTile;
       if (w.t_end < w.n || n == kTile) continue;
-      const int s = (t - 1) % p.stages;
-      if (!umma::warp_wait(&sh.raw[s], (raw_phase >> s) & 1, &sh.abort, p.dev_status)) break;
-      raw_phase ^= 1u << s;
-      uint8_t* st = stage0 + s * kStage;
-      for (int c = 0; c < DC / 64; ++c)
-        for (int x = n * 8 + lane; x < kTile * 8; x += 32) *reinterpret_cast<uint4*>(st + c * kBox + x * 16) = make_uint4(0, 0, 0, 0);
-      ptx::fence_proxy_async();
-      __syncwarp();
-      if (lane >= 1 && lane < kGroups) ptx::mbar_arrive(&sh.full[s * kGroups + lane]);
+      for (int m = 0; m < kM && ok; ++m) {
+        const int s = (t - 1) % p.stages * kM + m;
+        ok = umma::warp_wait(&sh.raw[s], (raw_phase >> s) & 1, &sh.abort, p.dev_status);
+        if (!ok) break;
+        raw_phase ^= 1u << s;
+        uint8_t* dst = sK + (t - 1) % p.stages * kStage + m * kPair;
+        for (int c = 0; c < 2; ++c)
+          for (int x = n * 8 + lane; x < kTile * 8; x += 32) *reinterpret_cast<uint4*>(dst + c * kBox + x * 16) = make_uint4(0, 0, 0, 0);
+        ptx::fence_proxy_async();
+        __syncwarp();
+        if (lane < kTile / p.page) ptx::mbar_arrive(&sh.full[s]);
+      }
     }
   } else if (warp == kQueryWarp) {
     // ------------------------------------------------------------------ queries of the units
@@ -303,74 +333,81 @@ __global__ void __launch_bounds__(kThreads, 1) latent_decode_kernel(const __grid
       constexpr uint32_t idesc_s = umma::instr_desc(64, NH, false);
       constexpr uint32_t idesc_o = umma::instr_desc(128, NH, false, true);
       const uint64_t hi = (uint64_t)umma::smem_desc_sw128(0, 0, 1024) & 0xffffffff00000000ull;
-      const uint32_t st = ptx::smem_u32(stage0), q_lo = (ptx::smem_u32(sQ) >> 4) | 1u << 16, p_lo = (ptx::smem_u32(sP) >> 4) | 1u << 16;
+      const uint32_t k_lo = ptx::smem_u32(sK) >> 4, q_lo = (ptx::smem_u32(sQ) >> 4) | 1u << 16, p_lo = (ptx::smem_u32(sP) >> 4) | 1u << 16;
       const int steps_r = p.dr / 16;
       Walk ws(sh), wp(sh);                               // the parts that scores and sums are at
       int s_at = 0, p_at = 0, n_q = 0;                   // tile within the walk's part; units begun
       ws.t_end = ws.t_begin = wp.t_end = wp.t_begin = 0;
       // The warp looks at what is there, a tile for the next scores or weights for the next sums, and issues that: sums that
       // waited behind the scores of a tile still on its way would hold their own tile's stage meanwhile.
-      int s_next = 0, p_next = 0, s_stage = 0, p_stage = 0, s_phase = 0;
+      int s_next = 0, p_next = 0;
+      Ring sp(p.stages), pp(p.stages);                   // the stages that scores and sums are at
       uint64_t t0 = 0;
       for (uint32_t spins = 0; p_next < n_tiles;) {
         bool moved = false;
-        if (p_next < s_next && __all_sync(0xffffffffu, ptx::mbar_test_wait(&sh.p_full, p_next & 1))) {
+        if (s_next < n_tiles && s_at == ws.t_end) { ws.next(p); s_at = ws.t_begin; ++n_q; }
+        // one look at everything that could be waited for, a barrier per lane: the next tile's pairs, its rotary part, the queries,
+        // the next weights
+        uint64_t* bar = &sh.p_full;
+        uint32_t parity = p_next & 1;
+        if (lane < kM) {
+          bar = &sh.full[sp.slot * kM + lane];
+          parity = sp.phase;
+        } else if (lane == kM) { bar = &sh.r_full[sp.slot]; parity = sp.phase; }
+        else if (lane == kM + 1) { bar = &sh.q_full; parity = (n_q - 1) & 1; }
+        const uint32_t seen = __ballot_sync(0xffffffffu, ptx::mbar_test_wait(bar, parity));
+        if (p_next < s_next && (seen >> 31)) {
           umma::fence_after_sync();
           bool fresh = false;
           if (p_at == wp.t_end) { wp.next(p); p_at = wp.t_begin; fresh = true; }
-          const uint32_t a_lo = ((st + p_stage * kStage) >> 4) | (uint32_t)(kBox >> 4) << 16;
+          const uint32_t a_lo = (k_lo + pp.slot * (kStage >> 4)) | (uint32_t)(kBox >> 4) << 16;
           if (umma::elect_one()) {
 #pragma unroll
-            for (int m = 0; m < DC / 128; ++m)
-#pragma unroll
-            {
+            for (int m = 0; m < kM; ++m) {
 #pragma unroll
               for (int kk = 0; kk < 4; ++kk)
-                umma::mma_bf16(tmem + (uint32_t)(m * NH), hi | (a_lo + ((2 * m * kBox + kk * 2048) >> 4)), hi | (p_lo + 2 * kk), idesc_o,
+                umma::mma_bf16(tmem + (uint32_t)(m * NH), hi | (a_lo + ((m * kPair + kk * 2048) >> 4)), hi | (p_lo + 2 * kk), idesc_o,
                                (!fresh || kk > 0) ? 1u : 0u);
+              umma::commit(&sh.empty[pp.slot * kM + m]);
             }
             umma::commit(&sh.o_done);
-            umma::commit(&sh.empty[p_stage]);
           }
           __syncwarp();
+          pp.next();
           ++p_at;
           ++p_next;
-          if (++p_stage == p.stages) p_stage = 0;
           moved = true;
         }
-        if (s_next < n_tiles && s_next <= p_next + 1) {  // (its buffer held the scores of s_next - 2, read before their weights were published)
-          if (s_at == ws.t_end) { ws.next(p); s_at = ws.t_begin; ++n_q; }
-          uint64_t* full = &sh.full[s_stage * kGroups];
-          if (__all_sync(0xffffffffu, ptx::mbar_test_wait(full + 1, s_phase) && ptx::mbar_test_wait(&sh.q_full, (n_q - 1) & 1))) {
-            // the first channels are there, the others on their way
+        // scores from the first channels' arrival on, while the others are on their way (the scores' buffer held those of
+        // s_next - 2, read before their weights were published)
+        constexpr uint32_t kFirst = 1u | 1u << (kM + 1);
+        if (s_next < n_tiles && s_next <= p_next + 1 && (seen & kFirst) == kFirst) {
+          const uint32_t d = s_tmem + (uint32_t)((s_next & 1) * NH);
+          const uint32_t a_lo = (k_lo + sp.slot * (kStage >> 4)) | 1u << 16;
+          bool ok = true;
+          ++s_at;
+#pragma unroll
+          for (int m = 0; m <= kM; ++m) {                // the rotary part last
+            ok = ok && ((seen >> m & 1) || umma::warp_wait(m < kM ? &sh.full[sp.slot * kM + m] : &sh.r_full[sp.slot], sp.phase, &sh.abort, p.dev_status));
             umma::fence_after_sync();
-            const uint32_t d = s_tmem + (uint32_t)((s_next & 1) * NH);
-            const uint32_t a_lo = ((st + s_stage * kStage) >> 4) | 1u << 16;
-            ++s_at;
-            bool ok = true;
+            if (ok && umma::elect_one()) {
 #pragma unroll
-            for (int g = 1; g <= kGroups; ++g) {         // the rotary chunk last
-              ok = ok && umma::warp_wait(g < kGroups ? full + g : full, s_phase, &sh.abort, p.dev_status);
-              if (ok && umma::elect_one()) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                  const int c = g < kGroups ? 2 * g - 2 + (k >> 2) : kChunks - 1 + (k >> 2), ks = k & 3;
-                  if (c < kChunks - 1 || (k < 4 && ks < steps_r))
-                    umma::mma_bf16(d, hi | (a_lo + ((c * kBox + ks * 32) >> 4)), hi | (q_lo + ((c * NH * 128 + ks * 32) >> 4)), idesc_s,
-                                   (g > 1 || k > 0) ? 1u : 0u);
-                }
-                if (g == kGroups) {
-                  umma::commit(&sh.s_full[s_next & 1]);
-                  if (s_at == ws.t_end) umma::commit(&sh.q_empty);
-                }
+              for (int k = 0; k < (m < kM ? 8 : 4); ++k)
+                if (m < kM || k < steps_r)
+                  umma::mma_bf16(d, hi | (a_lo + ((m * kPair + (k >> 2) * kBox + (k & 3) * 32) >> 4)),
+                                 hi | (q_lo + (((2 * m + (k >> 2)) * NH * 128 + (k & 3) * 32) >> 4)), idesc_s, (m > 0 || k > 0) ? 1u : 0u);
+              if (m == kM) {
+                umma::commit(&sh.s_full[s_next & 1]);
+                umma::commit(&sh.r_empty[sp.slot]);
+                if (s_at == ws.t_end) umma::commit(&sh.q_empty);
               }
-              __syncwarp();
             }
-            if (!ok) break;
-            ++s_next;
-            if (++s_stage == p.stages) { s_stage = 0; s_phase ^= 1; }
-            moved = true;
+            __syncwarp();
           }
+          if (!ok) break;
+          sp.next();
+          ++s_next;
+          moved = true;
         }
         if (moved) { t0 = 0; continue; }
         if ((++spins & 255u) == 0) {
@@ -395,16 +432,18 @@ __global__ void __launch_bounds__(kThreads, 1) latent_decode_kernel(const __grid
     for (int u = piece; u < U; u += p.pieces)            // empty sequences
       if (unit_len(p, u) == 0) {
         const int64_t o = (((int64_t)p.layer_begin * p.B + u) * p.H + hg * NH) * DC;
-        for (int x = tid; x < nh * DC; x += 128)
+        for (int x = tid; x < nh * DC; x += kSoft * 32)
           if (p.out_bf16) ((__nv_bfloat16*)p.out)[o + x] = __float2bfloat16(0.f); else ((float*)p.out)[o + x] = 0.f;
       }
-    const uint32_t lane_base = (uint32_t)(32 * warp) << 16;
-    const int row_lo = 16 * warp + (lane >> 2);          // tokens row_lo and row_lo + 8 of the tile, heads 8 j + 2 (lane % 4) + {0, 1}
-    const uint32_t p_addr = ptx::smem_u32(sP);
-    // matrix stores: lane i gives the address of row i % 8 of matrix i / 8: heads 8 (j + i / 16) + i % 8, token octet 2 warp + (i / 8) % 2
-    const int st_head = 8 * (lane >> 4) + (lane & 7), st_piece = 2 * warp + ((lane >> 3) & 1);
-    const uint32_t st_addr = p_addr + st_head * 128 + ((st_piece ^ (st_head & 7)) << 4);
-    constexpr int NC = NH / 4;                           // columns per thread
+    constexpr int kBlocks = NH / 4 / kSoft;              // of 16 heads per warp
+    const int quad = warp & 3, col0 = 16 * kBlocks * (warp >> 2);        // 16 tokens
+    const uint32_t lane_base = (uint32_t)(32 * quad) << 16;
+    const int row_lo = 16 * quad + (lane >> 2);          // tokens row_lo and row_lo + 8 of the tile, heads col0 + 8 j + 2 (lane % 4) + {0, 1}
+    // matrix stores: lane i gives the address of row i % 8 of matrix i / 8: heads col0 + 8 (i / 16) + i % 8, token octet 2 quad + (i / 8) % 2
+    const int st_head = col0 + 8 * (lane >> 4) + (lane & 7), st_piece = 2 * quad + ((lane >> 3) & 1);
+    const uint32_t st_addr = ptx::smem_u32(sP) + st_head * 128 + ((st_piece ^ (st_head & 7)) << 4);
+    constexpr int NC = 4 * kBlocks;                      // columns per thread
+    const int col = col0 + 2 * (lane & 3);               // columns col + 8 j + {0, 1}
     int t = 0;
     bool gone = false, ok = true;                        // ok: this warp's waits have ended well; the four leave together, at a vote
     Walk w(sh);
@@ -415,24 +454,25 @@ __global__ void __launch_bounds__(kThreads, 1) latent_decode_kernel(const __grid
       for (int i = w.t_begin; i < w.t_end; ++i, ++t) {
         ok = umma::warp_wait(&sh.s_full[t & 1], (t >> 1) & 1, &sh.abort, p.dev_status) && ok;
         umma::fence_after_sync();
-        uint32_t z[NH / 2];
-        ld_frags<NH>(s_tmem + lane_base + (uint32_t)((t & 1) * NH), z);
+        uint32_t z[8 * kBlocks];
+#pragma unroll
+        for (int k = 0; k < kBlocks; ++k) ld_frags(s_tmem + lane_base + (uint32_t)((t & 1) * NH + col0 + 16 * k), z + 8 * k);
         umma::tmem_ld_wait();
         const int n = w.len - i * kTile;
         if (n < kTile) {
 #pragma unroll
-          for (int j = 0; j < NH / 2; ++j)
+          for (int j = 0; j < 8 * kBlocks; ++j)
             if (row_lo + ((j & 2) ? 8 : 0) >= n) z[j] = 0xff800000u;
         }
         bool grow = false;
 #pragma unroll
-        for (int j = 0; j < NH / 2; ++j) {
+        for (int j = 0; j < 8 * kBlocks; ++j) {
           const int c = (j >> 2) * 2 + (j & 1);
           grow = grow || __uint_as_float(z[j]) * p.scale_log2 > m[c] + kLazy;
         }
-        if (softmax_any(grow || !ok || i == w.t_begin)) {
+        if (softmax_any<kSoft * 32>(grow || !ok || i == w.t_begin)) {
           if (i > w.t_begin) ok = umma::warp_wait(&sh.o_done, (t - 1) & 1, &sh.abort, p.dev_status) && ok;
-          if (softmax_any(!ok)) { gone = true; break; }
+          if (softmax_any<kSoft * 32>(!ok)) { gone = true; break; }
           // new maxima: columns over this warp's 16 tokens, then over the warps
 #pragma unroll
           for (int c = 0; c < NC; ++c) {
@@ -440,26 +480,25 @@ __global__ void __launch_bounds__(kThreads, 1) latent_decode_kernel(const __grid
             float x = fmaxf(__uint_as_float(z[j]), __uint_as_float(z[j + 2]));
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-            if (lane < 4) sh.ex[warp][8 * (c >> 1) + 2 * lane + (c & 1)] = x;
+            if (lane < 4) sh.ex[quad][col + 8 * (c >> 1) + (c & 1)] = x;
           }
-          softmax_sync();
+          softmax_sync<kSoft * 32>();
           if (tid < NH) {
             const float x = fmaxf(fmaxf(sh.ex[0][tid], sh.ex[1][tid]), fmaxf(sh.ex[2][tid], sh.ex[3][tid])) * p.scale_log2;
             const float was = i == w.t_begin ? -INFINITY : sh.m[tid], now = fmaxf(was, x);
             sh.m[tid] = now;
             sh.alpha[tid] = now == -INFINITY ? 1.f : ptx::ex2_approx(was - now);
           }
-          softmax_sync();
+          softmax_sync<kSoft * 32>();
 #pragma unroll
           for (int c = 0; c < NC; ++c) {
-            const int col = 8 * (c >> 1) + 2 * (lane & 3) + (c & 1);
-            m[c] = sh.m[col];
-            l[c] *= sh.alpha[col];
+            m[c] = sh.m[col + 8 * (c >> 1) + (c & 1)];
+            l[c] *= sh.alpha[col + 8 * (c >> 1) + (c & 1)];
           }
           if (i > w.t_begin) {                           // the sums so far follow
             umma::fence_after_sync();
 #pragma unroll 1
-            for (int mt = 0; mt < DC / 128; ++mt)
+            for (int mt = warp >> 2; mt < DC / 128; mt += kSoft / 4)
 #pragma unroll 1
               for (int c0 = 0; c0 < NH; c0 += 16) {
                 uint32_t o[16];
@@ -478,21 +517,19 @@ __global__ void __launch_bounds__(kThreads, 1) latent_decode_kernel(const __grid
         float m_eff[NC];
 #pragma unroll
         for (int c = 0; c < NC; ++c) m_eff[c] = m[c] == -INFINITY ? 0.f : m[c];
-        uint32_t pk[NH / 4];
+        uint32_t pk[4 * kBlocks];
 #pragma unroll
-        for (int j = 0; j < NH / 8; ++j)
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {                  // column group j, token octet k
-            const float p0 = ptx::ex2_approx(fmaf(__uint_as_float(z[4 * j + 2 * k]), p.scale_log2, -m_eff[2 * j]));
-            const float p1 = ptx::ex2_approx(fmaf(__uint_as_float(z[4 * j + 2 * k + 1]), p.scale_log2, -m_eff[2 * j + 1]));
-            l[2 * j] += p0;
-            l[2 * j + 1] += p1;
-            pk[2 * j + k] = ptx::pack_bf16x2(p0, p1);
-          }
+        for (int k = 0; k < 4 * kBlocks; ++k) {          // column group k / 2, token octet k % 2
+          const float p0 = ptx::ex2_approx(fmaf(__uint_as_float(z[2 * k]), p.scale_log2, -m_eff[2 * (k >> 1)]));
+          const float p1 = ptx::ex2_approx(fmaf(__uint_as_float(z[2 * k + 1]), p.scale_log2, -m_eff[2 * (k >> 1) + 1]));
+          l[2 * (k >> 1)] += p0;
+          l[2 * (k >> 1) + 1] += p1;
+          pk[k] = ptx::pack_bf16x2(p0, p1);
+        }
         if (t > 0) ok = umma::warp_wait(&sh.o_done, (t - 1) & 1, &sh.abort, p.dev_status) && ok;     // the weights' buffer is free again
 #pragma unroll
-        for (int j = 0; j < NH / 16; ++j)                // 16 heads per matrix store
-          stmatrix_x4_trans(st_addr + j * 16 * 128, pk[4 * j], pk[4 * j + 1], pk[4 * j + 2], pk[4 * j + 3]);
+        for (int k = 0; k < kBlocks; ++k)
+          stmatrix_x4_trans(st_addr + k * 16 * 128, pk[4 * k], pk[4 * k + 1], pk[4 * k + 2], pk[4 * k + 3]);
         ptx::fence_proxy_async();
         umma::fence_before_sync();
         ptx::mbar_arrive(&sh.p_full);
@@ -500,15 +537,15 @@ __global__ void __launch_bounds__(kThreads, 1) latent_decode_kernel(const __grid
       if (gone) break;
       // ---- end of the part: sums of weights over all tokens, then the rows leave
       ok = umma::warp_wait(&sh.o_done, (t - 1) & 1, &sh.abort, p.dev_status) && ok;
-      if (softmax_any(!ok)) break;
+      if (softmax_any<kSoft * 32>(!ok)) break;
       umma::fence_after_sync();
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) l[c] += __shfl_xor_sync(0xffffffffu, l[c], o);
-        if (lane < 4) sh.ex[warp][8 * (c >> 1) + 2 * lane + (c & 1)] = l[c];
+        if (lane < 4) sh.ex[quad][col + 8 * (c >> 1) + (c & 1)] = l[c];
       }
-      softmax_sync();
+      softmax_sync<kSoft * 32>();
       const bool whole = w.t_begin == 0 && w.t_end == w.n;
       const int64_t slot = ((int64_t)piece * 2 + (w.t_begin > 0 ? 0 : 1)) * p.heads_pad + hg * NH;
       if (tid < NH) {
@@ -516,15 +553,11 @@ __global__ void __launch_bounds__(kThreads, 1) latent_decode_kernel(const __grid
         if (whole) sh.alpha[tid] = 1.f / sum;
         else p.part_ml[slot + tid] = make_float2(sh.m[tid], sum);
       }
-      if (tid == 0 && hg == 0 && w.t_begin == 0 && !whole) {
-        const int used = pieces_used(sh.total, p.pieces), at = sh.g0 + t - (w.t_end - w.t_begin);      // first tile of the unit
-        p.plan[piece] = make_int2(w.unit, piece_of(sh.total, used, at + w.n - 1));
-      }
-      softmax_sync();
+      softmax_sync<kSoft * 32>();
       const int64_t out_row = ((int64_t)p.layer_begin * p.B + w.unit) * p.H + hg * NH;
 #pragma unroll 1
-      for (int mt = 0; mt < DC / 128; ++mt) {
-        const int d = 128 * mt + 32 * warp + lane;       // this thread's channel
+      for (int mt = warp >> 2; mt < DC / 128; mt += kSoft / 4) {
+        const int d = 128 * mt + 32 * quad + lane;       // this thread's channel
 #pragma unroll 1
         for (int c0 = 0; c0 < nh; c0 += 16) {
           uint32_t o[16];
@@ -552,6 +585,10 @@ __global__ void __launch_bounds__(kThreads, 1) latent_decode_kernel(const __grid
           }
         }
       }
+      if (tid == 0 && hg == 0 && w.t_begin == 0 && !whole) {
+        const int used = pieces_used(sh.total, p.pieces), at = sh.g0 + t - (w.t_end - w.t_begin);      // first tile of the unit
+        p.plan[piece] = make_int2(w.unit, piece_of(sh.total, used, at + w.n - 1));
+      }
       umma::fence_before_sync();                         // (the next unit's first sums overwrite O once its weights are published)
     }
   }
@@ -564,51 +601,65 @@ __global__ void __launch_bounds__(kThreads, 1) latent_decode_kernel(const __grid
   }
 }
 
-// Joins the parts of the unit that begins in piece blockIdx.x and goes on behind it: four heads per CTA, 128 threads each, four
-// channels per thread.  Bound by latency: plan -> maxima -> sums.
-__global__ void __launch_bounds__(512) latent_join_kernel(LatentDecodeParams p) {
-  __shared__ float weight[4][kMaxCtas];
+// Joins the parts of the unit that begins in piece blockIdx.x and goes on behind it.  A CTA of 128 threads takes four
+// heads: each warp works out the weights of one head's parts, then a thread sums four channels of all four.  Bound by latency, plan ->
+// maxima -> sums, so the CTAs are small enough to be resident all at once.
+constexpr int kJoin = 4;
+__global__ void __launch_bounds__(128) latent_join_kernel(LatentDecodeParams p) {
+  __shared__ float weight[kJoin][kMaxCtas];
+  ptx::grid_dep_launch();
   ptx::grid_dep_wait();
   const int i0 = blockIdx.x;
   const int2 plan = p.plan[i0];
   if (plan.x < 0) return;
-  const int hh = threadIdx.x >> 7, h = 4 * blockIdx.y + hh, lane = threadIdx.x & 31, n = plan.y - i0 + 1;
-  auto slot = [&](int i) { return ((int64_t)(i0 + i) * 2 + (i == 0 ? 1 : 0)) * p.heads_pad + h; };
-  float total = 0.f;
-  if (h < p.H) {                                         // (every warp of a head for itself: lanes take parts)
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = plan.y - i0 + 1, h0 = kJoin * blockIdx.y;
+  auto slot = [&](int i, int h) { return ((int64_t)(i0 + i) * 2 + (i == 0 ? 1 : 0)) * p.heads_pad + h; };
+  if (h0 + warp < p.H) {                                 // a warp per head: lanes take parts
     float2 ml[(kMaxCtas + 31) / 32];
-    float m = -INFINITY;
+    float m = -INFINITY, total = 0.f;
 #pragma unroll
     for (int k = 0; k < (kMaxCtas + 31) / 32; ++k) {
-      ml[k] = 32 * k + lane < n ? p.part_ml[slot(32 * k + lane)] : make_float2(-INFINITY, 0.f);
+      ml[k] = 32 * k + lane < n ? p.part_ml[slot(32 * k + lane, h0 + warp)] : make_float2(-INFINITY, 0.f);
       m = fmaxf(m, ml[k].x);
     }
     m = warp_max(m);
     if (m == -INFINITY) m = 0.f;
 #pragma unroll
     for (int k = 0; k < (kMaxCtas + 31) / 32; ++k) {
-      const float f = ptx::ex2_approx(ml[k].x - m);
-      total += ml[k].y * f;
-      if ((threadIdx.x & 96) == 0 && 32 * k + lane < n) weight[hh][32 * k + lane] = f;
+      ml[k].x = ptx::ex2_approx(ml[k].x - m);
+      total += ml[k].y * ml[k].x;
     }
-    total = warp_sum(total);
+    const float inv = 1.f / warp_sum(total);
+#pragma unroll
+    for (int k = 0; k < (kMaxCtas + 31) / 32; ++k)
+      if (32 * k + lane < n) weight[warp][32 * k + lane] = ml[k].x * inv;
   }
   __syncthreads();
-  const int c = 4 * (threadIdx.x & 127);
-  if (h >= p.H || c >= p.dc) return;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-  for (int i = 0; i < n; ++i) {
-    const float4 v = *reinterpret_cast<const float4*>(p.part_o + slot(i) * p.dc + c);
-    const float f = weight[hh][i];
-    o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f;
+  const int c = 4 * threadIdx.x;
+  if (c >= p.dc) return;
+  float4 o[kJoin];
+#pragma unroll
+  for (int k = 0; k < kJoin; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+  for (int i = 0; i < n; ++i)
+#pragma unroll
+    for (int k = 0; k < kJoin; ++k) {
+      if (h0 + k < p.H) {
+        const float4 v = *reinterpret_cast<const float4*>(p.part_o + slot(i, h0 + k) * p.dc + c);
+        const float f = weight[k][i];
+        o[k].x += v.x * f; o[k].y += v.y * f; o[k].z += v.z * f; o[k].w += v.w * f;
+      }
+    }
+#pragma unroll
+  for (int k = 0; k < kJoin; ++k) {
+    const int h = h0 + k;
+    const int64_t at = (((int64_t)p.layer_begin * p.B + plan.x) * p.H + h) * p.dc + c;
+    if (h >= p.H) break;
+    if (p.out_bf16)
+      *reinterpret_cast<uint2*>((__nv_bfloat16*)p.out + at) = make_uint2(ptx::pack_bf16x2(o[k].x, o[k].y), ptx::pack_bf16x2(o[k].z, o[k].w));
+    else
+      *reinterpret_cast<float4*>((float*)p.out + at) = o[k];
   }
-  const float inv = 1.f / total;
-  const int64_t at = (((int64_t)p.layer_begin * p.B + plan.x) * p.H + h) * p.dc + c;
-  if (p.out_bf16)
-    *reinterpret_cast<uint2*>((__nv_bfloat16*)p.out + at) = make_uint2(ptx::pack_bf16x2(o.x * inv, o.y * inv), ptx::pack_bf16x2(o.z * inv, o.w * inv));
-  else
-    *reinterpret_cast<float4*>((float*)p.out + at) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
 }
 
 // bf16 rows of `d` channels, `mid` x `outer` of them, as a 3-D tensor; box = 64 channels x `box` rows of the middle axis.
@@ -640,10 +691,10 @@ Space space_of(const ngc_latent_pool* c, int H) {
 }
 
 template <int NH, int DC> int launch(const Maps& maps, LatentDecodeParams& p, cudaStream_t stream) {
-  constexpr int kChunks = DC / 64 + 1, kFixed = kStaticReserve + 1024 + kChunks * NH * 128 + NH * 128;
-  p.stages = (kSmemLimit - kFixed) / (kChunks * kBox);
+  constexpr int kChunks = DC / 64 + 1, kFree = kSmemLimit - kStaticReserve - 1024 - kChunks * NH * 128 - NH * 128;
+  p.stages = kFree / (kChunks * kBox);
   if (p.stages > kMaxStages) p.stages = kMaxStages;
-  if (p.stages * (DC / 128 + 1) > kMaxGroups) p.stages = kMaxGroups / (DC / 128 + 1);
+  if (p.stages * (DC / 128) > kMaxPairs) p.stages = kMaxPairs / (DC / 128);
   static_assert(sizeof(Shared<NH>) <= kStaticReserve, "static shared memory");
   static PerDeviceOnce once;
   const int rc = once.run([] {
@@ -651,8 +702,8 @@ template <int NH, int DC> int launch(const Maps& maps, LatentDecodeParams& p, cu
   });
   if (rc != NGC_OK) return rc;
   // (all of it, however little the ring takes: two CTAs of an SM would fight for its tensor memory)
-  NGC_CUDA_TRY(launch_pdl(latent_decode_kernel<NH, DC>, dim3(p.pieces * p.groups), dim3(kThreads), kSmemLimit - kStaticReserve, stream, maps, p));
-  NGC_CUDA_TRY(launch_pdl(latent_join_kernel, dim3(p.pieces, (p.H + 3) / 4), dim3(512), 0, stream, p));
+  NGC_CUDA_TRY(launch_pdl(latent_decode_kernel<NH, DC>, dim3(p.pieces * p.groups), dim3(cta_threads(NH)), kSmemLimit - kStaticReserve, stream, maps, p));
+  NGC_CUDA_TRY(launch_pdl(latent_join_kernel, dim3(p.pieces, (p.H + kJoin - 1) / kJoin), dim3(128), 0, stream, p));
   return launch_status();
 }
 
