@@ -63,33 +63,6 @@ __device__ __forceinline__ void load_q(const LatentReplayParams& p, const __nv_b
   for (int i = 0; i < 2; ++i) q[4 + i] = 32 * i + lane < p.dr ? at(x + 128 + 32 * i + lane) : 0.f;
 }
 
-// A warp per (token, head).
-__global__ void __launch_bounds__(256) latent_fwd_kernel(LatentReplayParams p) {
-  const int lane = threadIdx.x & 31, h = blockIdx.y, b = blockIdx.z % p.B, l = blockIdx.z / p.B;
-  int64_t row0;
-  const int T = latent_seq(p, b, row0), t = blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (t >= T) return;
-  const int32_t* gone = p.gone ? p.gone + ((int64_t)b * p.G + list_of(p.lists, l, 0, 1)) * p.gone_cap : nullptr;
-  const int64_t base = (int64_t)l * p.rows + row0;
-  float q[6], acc[4] = {0, 0, 0, 0}, m = -INFINITY, sum = 0.f;
-  load_q(p, p.q + ((base + t) * p.H + h) * (128 + p.dr), q, lane);
-  for (int j = 0; j <= t; ++j) {
-    if (gone && gone[j] <= t) continue;
-    const __nv_bfloat16* kv = p.kv + ((base + j) * p.H + h) * 256;
-    const float z = score(p, q, kv, p.kr + (base + j) * p.dr, lane) * p.scale;
-    const float mn = fmaxf(m, z), a = expf(m - mn), w = expf(z - mn);
-    sum = sum * a + w;
-    for (int i = 0; i < 4; ++i) acc[i] = acc[i] * a + w * at(kv + 128 + 32 * i + lane);
-    m = mn;
-  }
-  for (int i = 0; i < 4; ++i) {
-    const float o = sum > 0.f ? acc[i] / sum : 0.f;
-    const int64_t x = ((base + t) * p.H + h) * 128 + 32 * i + lane;
-    if (p.out_bf16) ((__nv_bfloat16*)p.out)[x] = __float2bfloat16(o); else ((float*)p.out)[x] = o;
-  }
-  if (p.lse && lane == 0) p.lse[((int64_t)l * p.H + h) * p.rows + row0 + t] = m + logf(sum);
-}
-
 // A warp per token; the heads one after the other, so that the shared rotary rows' gradient is one warp's sum.
 __global__ void __launch_bounds__(256) latent_bwd_kernel(LatentReplayParams p) {
   const int lane = threadIdx.x & 31, b = blockIdx.z % p.B, l = blockIdx.z / p.B;
@@ -221,8 +194,7 @@ extern "C" int ngc_latent_replay_attn(const ngc_latent_seqs* s, const void* q, c
   if (s->rows == 0 || s->max_len == 0) return NGC_OK;
   p.out = out; p.lse = lse;
   if (n_rounds > 0) latent_gone_kernel<<<dim3(p.G, p.B), 1024, 0, stream>>>(p);
-  latent_fwd_kernel<<<dim3((p.max_len + 7) / 8, p.H, p.L * p.B), 256, 0, stream>>>(p);
-  return launch_status();
+  return launch_latent_fwd(p, stream);
 }
 
 extern "C" int ngc_latent_replay_attn_backward(const ngc_latent_seqs* s, const void* q, const void* kv, const void* k_rope, const int32_t* alive_pos,

@@ -50,4 +50,6 @@ __device__ __forceinline__ int latent_seq(const LatentReplayParams& p, int b, in
   return n;
 }
 
+int launch_latent_fwd(const LatentReplayParams& p, cudaStream_t stream);
+
 }  // namespace ngc
