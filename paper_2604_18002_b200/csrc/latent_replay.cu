@@ -49,69 +49,7 @@ __global__ void __launch_bounds__(1024) latent_gone_kernel(LatentReplayParams p)
   }
 }
 
-struct Row { float v[8]; };
 __device__ __forceinline__ float at(const __nv_bfloat16* x) { return __bfloat162float(*x); }
-
-__device__ __forceinline__ float score(const LatentReplayParams& p, const float* q, const __nv_bfloat16* k, const __nv_bfloat16* r, int lane) {
-  float z = 0.f;
-  for (int i = 0; i < 4; ++i) z += q[i] * at(k + 32 * i + lane);
-  for (int i = 0; i < 2; ++i) if (32 * i + lane < p.dr) z += q[4 + i] * at(r + 32 * i + lane);
-  return warp_sum(z);
-}
-__device__ __forceinline__ void load_q(const LatentReplayParams& p, const __nv_bfloat16* x, float* q, int lane) {
-  for (int i = 0; i < 4; ++i) q[i] = at(x + 32 * i + lane);
-  for (int i = 0; i < 2; ++i) q[4 + i] = 32 * i + lane < p.dr ? at(x + 128 + 32 * i + lane) : 0.f;
-}
-
-// A warp per token; the heads one after the other, so that the shared rotary rows' gradient is one warp's sum.
-__global__ void __launch_bounds__(256) latent_bwd_kernel(LatentReplayParams p) {
-  const int lane = threadIdx.x & 31, b = blockIdx.z % p.B, l = blockIdx.z / p.B;
-  int64_t row0;
-  const int T = latent_seq(p, b, row0), t = blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (t >= T) return;
-  const int32_t* gone = p.gone ? p.gone + ((int64_t)b * p.G + list_of(p.lists, l, 0, 1)) * p.gone_cap : nullptr;
-  const int64_t base = (int64_t)l * p.rows + row0;
-  auto weight = [&](const float* q, const float* go, int tq, int j, int h, float delta, float& pr) {
-    const __nv_bfloat16* kv = p.kv + ((base + j) * p.H + h) * 256;
-    const float z = score(p, q, kv, p.kr + (base + j) * p.dr, lane) * p.scale;
-    pr = expf(z - p.lse[((int64_t)l * p.H + h) * p.rows + row0 + tq]);
-    float dp = 0.f;
-    for (int i = 0; i < 4; ++i) dp += go[i] * at(kv + 128 + 32 * i + lane);
-    return pr * (warp_sum(dp) - delta) * p.scale;
-  };
-  float gkr[2] = {0, 0};
-  for (int h = 0; h < p.H; ++h) {
-    float q[6], go[4], gq[6] = {0, 0, 0, 0, 0, 0}, gk[6] = {0, 0, 0, 0, 0, 0}, gv[4] = {0, 0, 0, 0};
-    load_q(p, p.q + ((base + t) * p.H + h) * (128 + p.dr), q, lane);
-    for (int i = 0; i < 4; ++i) go[i] = at(p.go + ((base + t) * p.H + h) * 128 + 32 * i + lane);
-    float delta = p.delta[((int64_t)l * p.H + h) * p.rows + row0 + t], pr;
-    for (int j = 0; j <= t; ++j) {                     // as a query
-      if (gone && gone[j] <= t) continue;
-      const float dz = weight(q, go, t, j, h, delta, pr);
-      const __nv_bfloat16* kv = p.kv + ((base + j) * p.H + h) * 256;
-      for (int i = 0; i < 4; ++i) gq[i] += dz * at(kv + 32 * i + lane);
-      for (int i = 0; i < 2; ++i) if (32 * i + lane < p.dr) gq[4 + i] += dz * at(p.kr + (base + j) * p.dr + 32 * i + lane);
-    }
-    const int end = gone ? min(gone[t], T) : T;
-    for (int tq = t; tq < end; ++tq) {                 // as a key
-      load_q(p, p.q + ((base + tq) * p.H + h) * (128 + p.dr), q, lane);
-      for (int i = 0; i < 4; ++i) go[i] = at(p.go + ((base + tq) * p.H + h) * 128 + 32 * i + lane);
-      const float dz = weight(q, go, tq, t, h, p.delta[((int64_t)l * p.H + h) * p.rows + row0 + tq], pr);
-      for (int i = 0; i < 6; ++i) gk[i] += dz * q[i];
-      for (int i = 0; i < 4; ++i) gv[i] += pr * go[i];
-    }
-    for (int i = 0; i < 4; ++i) {
-      p.gq[((base + t) * p.H + h) * (128 + p.dr) + 32 * i + lane] = __float2bfloat16(gq[i]);
-      p.gkv[((base + t) * p.H + h) * 256 + 32 * i + lane] = __float2bfloat16(gk[i]);
-      p.gkv[((base + t) * p.H + h) * 256 + 128 + 32 * i + lane] = __float2bfloat16(gv[i]);
-    }
-    for (int i = 0; i < 2; ++i) if (32 * i + lane < p.dr) {
-      p.gq[((base + t) * p.H + h) * (128 + p.dr) + 128 + 32 * i + lane] = __float2bfloat16(gq[4 + i]);
-      gkr[i] += gk[4 + i];
-    }
-  }
-  for (int i = 0; i < 2; ++i) if (32 * i + lane < p.dr) p.gkr[(base + t) * p.dr + 32 * i + lane] = __float2bfloat16(gkr[i]);
-}
 
 // delta = sum over channels of out * grad_out: 16 lanes per (token, head).
 __global__ void __launch_bounds__(256) latent_delta_kernel(LatentReplayParams p) {
@@ -214,6 +152,5 @@ extern "C" int ngc_latent_replay_attn_backward(const ngc_latent_seqs* s, const v
   p.gq = (__nv_bfloat16*)grad_q; p.gkv = (__nv_bfloat16*)grad_kv; p.gkr = (__nv_bfloat16*)grad_k_rope;
   if (n_rounds > 0) latent_gone_kernel<<<dim3(p.G, p.B), 1024, 0, stream>>>(p);
   latent_delta_kernel<<<dim3((p.max_len + 7) / 8, p.H, p.L * p.B), 256, 0, stream>>>(p);
-  latent_bwd_kernel<<<dim3((p.max_len + 7) / 8, 1, p.L * p.B), 256, 0, stream>>>(p);
-  return launch_status();
+  return launch_latent_bwd(p, stream);
 }

@@ -51,5 +51,6 @@ __device__ __forceinline__ int latent_seq(const LatentReplayParams& p, int b, in
 }
 
 int launch_latent_fwd(const LatentReplayParams& p, cudaStream_t stream);
+int launch_latent_bwd(const LatentReplayParams& p, cudaStream_t stream);
 
 }  // namespace ngc

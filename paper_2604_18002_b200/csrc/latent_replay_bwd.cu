@@ -1,0 +1,613 @@
+// The gradient of ngc_latent_replay_attn on the 5th-generation tensor cores.
+//
+// With the forward pass's lse and D = sum over channels of out * grad_out, P = exp(z - lse) and dz = P (dP - D), dP = dO V^T
+// (the scale of z is applied to the finished sums).  Two kernels, each of which computes S and dP again, so that every sum lies in one
+// CTA's tensor memory: no atomics, the same bits in every run.
+//   queries   an item is 128 queries of a head; over its tiles of 128 keys: S = Q K^T, dP = dO V^T, dQ += dZ K
+//   keys      an item is 128 keys of a head; over the tiles of 64 queries that see them: S^T = K Q^T, dP^T = V dO^T,
+//             dV += P^T dO, dK += dZ^T Q.  Keys are the lanes of tensor memory, so what a query sees is one range of columns per
+//             thread.  64 queries because dV, dK (320 columns), S^T, dP^T and the bf16 P^T, dZ^T fill tensor memory
+// P and dZ are A operands in tensor memory, in columns of their own: the scores of the next tile are computed while the softmax
+// warps work on this one.  The head's share of the rotary keys' gradient goes to the workspace in fp32; a last kernel sums the heads
+// in order.  Roles as in the forward pass: producers by TMA, a mender (rows behind a sequence's end are zeroed where they are
+// summed over), the MMA warp, eight softmax warps (two per quarter of the lanes, half of the columns each).
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include "latent_replay_umma.cuh"
+#include "ptx.cuh"
+
+namespace ngc {
+namespace {
+
+constexpr int kMmaWarp = 8, kProducerWarp = 9, kMenderWarp = 10, kItemWarp = 11;
+constexpr int kThreads = 12 * 32;
+constexpr uint32_t kTmemCols = 512;
+constexpr int kQBytes = 3 * kLatChunk, kVBytes = 2 * kLatChunk;          // 128 rows of 192 and of 128 channels
+
+struct Maps { CUtensorMap q, kv, kr, go; };
+
+// The row of 128 (or fewer) fp32 sums of this thread as bf16, `n` of them from column taddr on, times `f`.
+__device__ __forceinline__ void store_bf16(uint32_t taddr, int n, float f, __nv_bfloat16* dst, bool mine) {
+#pragma unroll 1
+  for (int c0 = 0; c0 < n; c0 += 16) {
+    uint32_t o[16];
+    umma::tmem_ld16(taddr + c0, o);
+    umma::tmem_ld_wait();
+    if (!mine) continue;
+#pragma unroll
+    for (int c = 0; c < 16; c += 8)
+      *reinterpret_cast<uint4*>(dst + c0 + c) =
+          make_uint4(ptx::pack_bf16x2(__uint_as_float(o[c]) * f, __uint_as_float(o[c + 1]) * f),
+                     ptx::pack_bf16x2(__uint_as_float(o[c + 2]) * f, __uint_as_float(o[c + 3]) * f),
+                     ptx::pack_bf16x2(__uint_as_float(o[c + 4]) * f, __uint_as_float(o[c + 5]) * f),
+                     ptx::pack_bf16x2(__uint_as_float(o[c + 6]) * f, __uint_as_float(o[c + 7]) * f));
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------ queries
+
+constexpr int kSmemQ = kQBytes + kVBytes + 2 * kQBytes + kVBytes + 1024;         // Q, dO; two stages of K; V
+
+struct SharedQ {
+  uint64_t k_full[2], k_raw[2], k_empty[2], v_full, v_empty, q_full, q_empty, sp_full, sp_free, z_full, z_empty, dq_done, drain;
+  uint32_t tmem;
+  int abort;
+};
+
+__global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid_constant__ Maps maps, LatentReplayParams p, int n_items) {
+  extern __shared__ uint8_t smem_dyn[];
+  __shared__ SharedQ sh;
+  uint8_t* sQ = (uint8_t*)(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);
+  uint8_t* sG = sQ + kQBytes;
+  uint8_t* sK = sG + kVBytes;                            // [2]
+  uint8_t* sV = sK + 2 * kQBytes;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (warp == 0) {
+    if (lane < 2) { ptx::mbar_init(&sh.k_full[lane], 1); ptx::mbar_init(&sh.k_raw[lane], 1); ptx::mbar_init(&sh.k_empty[lane], 1); }
+    if (lane == 2) {
+      ptx::mbar_init(&sh.v_full, 1); ptx::mbar_init(&sh.v_empty, 1); ptx::mbar_init(&sh.q_full, 1); ptx::mbar_init(&sh.q_empty, 1);
+      ptx::mbar_init(&sh.sp_full, 1); ptx::mbar_init(&sh.sp_free, 256); ptx::mbar_init(&sh.z_full, 256); ptx::mbar_init(&sh.z_empty, 1);
+      ptx::mbar_init(&sh.dq_done, 1); ptx::mbar_init(&sh.drain, 1);
+      sh.abort = 0;
+    }
+    ptx::fence_barrier_init();
+  } else if (warp == kProducerWarp && lane == 0) {
+    ptx::prefetch_tensormap(&maps.q); ptx::prefetch_tensormap(&maps.kv); ptx::prefetch_tensormap(&maps.kr); ptx::prefetch_tensormap(&maps.go);
+  }
+  if (warp == kMmaWarp) umma::tmem_alloc(&sh.tmem, kTmemCols);
+  umma::fence_before_sync();
+  __syncthreads();
+  umma::fence_after_sync();
+  const uint32_t tmem = sh.tmem;
+  constexpr uint32_t kS = 0, kP = 128, kO = 256, kZ = 448;               // columns of S, dP, dQ, dZ
+  ptx::grid_dep_wait();
+  auto wait = [&](uint64_t* bar, uint32_t parity) { return umma::warp_wait(bar, parity, &sh.abort, p.dev_status); };
+
+  if (warp == kProducerWarp) {
+    QueryWalk<1> w(n_items);
+    int t = 0, n_raw[2] = {0, 0};
+    uint32_t through_raw = 0;
+    bool ok = true;
+    while (ok && w.next(p)) {
+      const int y = (int)((int64_t)w.l * p.rows + w.row0 + w.i * kLatTile), s = t & 1;
+      const bool tail = (w.i + 1) * kLatTile > w.T;
+      if (t > 1) ok = wait(&sh.k_empty[s], ((t >> 1) - 1) & 1);
+      if (!ok) break;
+      if (umma::elect_one()) {
+        uint64_t* bar = tail ? &sh.k_raw[s] : &sh.k_full[s];
+        ptx::mbar_expect_tx(bar, kQBytes);
+        for (int c = 0; c < 2; ++c) ptx::tma_load_3d(sK + s * kQBytes + c * kLatChunk, &maps.kv, 64 * c, w.h, y, bar);
+        ptx::tma_load_2d(sK + s * kQBytes + 2 * kLatChunk, &maps.kr, 0, y, bar);
+      }
+      __syncwarp();
+      through_raw = tail ? through_raw | 1u << s : through_raw & ~(1u << s);
+      n_raw[0] += tail && !s; n_raw[1] += tail && s;
+      if (t > 0) ok = wait(&sh.v_empty, (t - 1) & 1);
+      ++t;
+      if (!ok) { --t; break; }
+      if (umma::elect_one()) {
+        ptx::mbar_expect_tx(&sh.v_full, kVBytes);
+        for (int c = 0; c < 2; ++c) ptx::tma_load_3d(sV + c * kLatChunk, &maps.kv, kLatNope + 64 * c, w.h, y, &sh.v_full);
+      }
+      __syncwarp();
+    }
+    // nothing is in flight when the CTA ends (after a wait that ran out: K of tile t may be, V of it is not)
+    const int tk = ok ? t : t + 1;
+    for (int x = max(0, tk - 2); x < tk; ++x) {
+      if (through_raw >> (x & 1) & 1) ptx::mbar_wait_bounded(&sh.k_raw[x & 1], (n_raw[x & 1] - 1) & 1);
+      else ptx::mbar_wait_bounded(&sh.k_full[x & 1], (x >> 1) & 1);
+    }
+    if (t > 0) ptx::mbar_wait_bounded(&sh.v_full, (t - 1) & 1);
+    __syncwarp();
+  } else if (warp == kMenderWarp) {
+    // keys behind the sequence's end: dQ sums over them
+    QueryWalk<1> w(n_items);
+    uint32_t phase = 0;
+    for (int t = 0; w.next(p); ++t) {
+      if ((w.i + 1) * kLatTile <= w.T) continue;
+      const int s = t & 1, n = w.T - w.i * kLatTile;
+      if (!wait(&sh.k_raw[s], (phase >> s) & 1)) break;
+      phase ^= 1u << s;
+      for (int c = 0; c < 3; ++c)
+        for (int x = n * 8 + lane; x < kLatTile * 8; x += 32)
+          *reinterpret_cast<uint4*>(sK + s * kQBytes + c * kLatChunk + x * 16) = make_uint4(0, 0, 0, 0);
+      ptx::fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(&sh.k_full[s]);
+    }
+  } else if (warp == kItemWarp) {
+    QueryWalk<1> w(n_items);
+    int n = 0;
+    while (w.next(p)) {
+      if (!w.first) continue;
+      if (n > 0 && !wait(&sh.q_empty, (n - 1) & 1)) break;
+      if (umma::elect_one()) {
+        const int y = (int)((int64_t)w.l * p.rows + w.row0 + w.q0);
+        ptx::mbar_expect_tx(&sh.q_full, kQBytes + kVBytes);
+        for (int c = 0; c < 3; ++c) ptx::tma_load_3d(sQ + c * kLatChunk, &maps.q, 64 * c, w.h, y, &sh.q_full);
+        for (int c = 0; c < 2; ++c) ptx::tma_load_3d(sG + c * kLatChunk, &maps.go, 64 * c, w.h, y, &sh.q_full);
+      }
+      __syncwarp();
+      ++n;
+    }
+    if (n > 0) ptx::mbar_wait_bounded(&sh.q_full, (n - 1) & 1);
+    __syncwarp();
+  } else if (warp == kMmaWarp) {
+    constexpr uint32_t idesc = umma::instr_desc(kLatTile, kLatTile, false), idesc_q = umma::instr_desc(kLatTile, 192, true);
+    const uint64_t hi = (uint64_t)umma::smem_desc_sw128(0, 0, 1024) & 0xffffffff00000000ull;
+    const uint32_t q_lo = (ptx::smem_u32(sQ) >> 4) | 1u << 16, g_lo = (ptx::smem_u32(sG) >> 4) | 1u << 16, v_lo = (ptx::smem_u32(sV) >> 4) | 1u << 16,
+                   k_lo = ptx::smem_u32(sK) >> 4;
+    const int steps_r = p.dr / 16;
+    QueryWalk<1> cur(n_items), nxt(n_items);
+    int n_q = 0;
+    bool ok = true;
+    auto scores = [&](const QueryWalk<1>& w, int t) {
+      if (w.first) ok = ok && wait(&sh.q_full, n_q++ & 1);
+      ok = ok && (t == 0 || wait(&sh.sp_free, (t - 1) & 1)) && wait(&sh.k_full[t & 1], (t >> 1) & 1);
+      if (!ok) return;
+      umma::fence_after_sync();
+      if (umma::elect_one()) {
+        const uint32_t b = (k_lo + (t & 1) * (kQBytes >> 4)) | 1u << 16;
+#pragma unroll
+        for (int k = 0; k < 12; ++k)
+          if (k < 8 || k - 8 < steps_r) {
+            const uint32_t o = ((k >> 2) * kLatChunk + (k & 3) * 32) >> 4;
+            umma::mma_bf16(tmem + kS, hi | (q_lo + o), hi | (b + o), idesc, k > 0 ? 1u : 0u);
+          }
+      }
+      __syncwarp();
+      ok = wait(&sh.v_full, t & 1);
+      if (!ok) return;
+      umma::fence_after_sync();
+      const bool last = w.last();
+      if (umma::elect_one()) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const uint32_t o = ((k >> 2) * kLatChunk + (k & 3) * 32) >> 4;
+          umma::mma_bf16(tmem + kP, hi | (g_lo + o), hi | (v_lo + o), idesc, k > 0 ? 1u : 0u);
+        }
+        umma::commit(&sh.sp_full);
+        umma::commit(&sh.v_empty);
+        if (last) umma::commit(&sh.q_empty);
+      }
+      __syncwarp();
+    };
+    auto sums = [&](const QueryWalk<1>& w, int t) {
+      ok = ok && wait(&sh.z_full, t & 1);
+      if (!ok) return;
+      umma::fence_after_sync();
+      const bool first = w.first, last = w.last();
+      if (umma::elect_one()) {
+        const uint32_t b = (k_lo + (t & 1) * (kQBytes >> 4)) | (uint32_t)(kLatChunk >> 4) << 16;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          umma::mma_bf16_a_tmem(tmem + kO, tmem + kZ + 8 * k, hi | (b + ((k * 2048) >> 4)), idesc_q, (!first || k > 0) ? 1u : 0u);
+        umma::commit(&sh.k_empty[t & 1]);
+        umma::commit(&sh.z_empty);
+        if (last) umma::commit(&sh.dq_done);
+      }
+      __syncwarp();
+    };
+    bool more = nxt.next(p);
+    if (more) scores(nxt, 0);
+    for (int t = 0; ok && more; ++t) {
+      cur = nxt;
+      more = nxt.next(p);
+      // the next tile's scores first; at an item's end the sums, since the next queries are still on their way
+      if (more && !nxt.first) scores(nxt, t + 1);
+      if (ok) sums(cur, t);
+      if (ok && more && nxt.first) scores(nxt, t + 1);
+    }
+    if (umma::elect_one()) umma::commit(&sh.drain);
+    __syncwarp();
+    ptx::mbar_wait_bounded(&sh.drain, 0);
+    __syncwarp();
+  } else {
+    const int half = warp >> 2, row = 32 * (warp & 3) + lane;
+    const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
+    QueryWalk<1> w(n_items);
+    float lse2 = 0.f, delta = 0.f;
+    int n_items_done = 0;
+    for (int t = 0; w.next(p); ++t) {
+      const int t_q = w.q0 + row;
+      const bool mine = t_q < w.T;
+      if (w.first) {
+        const int64_t at = ((int64_t)w.l * p.H + w.h) * p.rows + w.row0 + t_q;
+        lse2 = mine ? p.lse[at] * 1.4426950408889634f : 0.f;
+        delta = mine ? p.delta[at] : 0.f;
+      }
+      if (!wait(&sh.sp_full, t & 1)) break;
+      umma::fence_after_sync();
+      uint32_t z[2][32], d[2][32];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) umma::tmem_ld32(lanes + kS + 64 * half + 32 * k, z[k]);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) umma::tmem_ld32(lanes + kP + 64 * half + 32 * k, d[k]);
+      umma::tmem_ld_wait();
+      umma::fence_before_sync();
+      ptx::mbar_arrive(&sh.sp_free);
+      const int j0 = w.i * kLatTile + 64 * half;
+      const bool plain = !w.tiles || (w.plain_a >> (w.i - w.window) & 1);
+      const int32_t* gone = plain ? nullptr : p.gone + ((int64_t)w.b * p.G + list_of(p.lists, w.l, 0, 1)) * p.gone_cap + j0;
+      uint32_t pk[32];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        uint32_t seen = 0xffffffffu;                     // bit j: this query sees key j0 + 32 k + j
+        const int behind = t_q - (j0 + 32 * k);          // keys behind the query do not count
+        if (behind < 31) seen = behind < 0 ? 0u : (2u << behind) - 1u;
+        if (!plain) {
+          const int g = gone[32 * k + lane];
+          const uint32_t lo = __ballot_sync(0xffffffffu, g > w.q0 + kLatTile - 1);
+          if (lo == __ballot_sync(0xffffffffu, g > w.q0)) {
+            seen &= lo;
+          } else {
+            uint32_t m = 0;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) m |= __shfl_sync(0xffffffffu, g, j) > t_q ? 1u << j : 0u;
+            seen &= m;
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+          float e[2];
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const float pr = ptx::ex2_approx(fmaf(__uint_as_float(z[k][j + c]), p.scale_log2, -lse2));
+            e[c] = (seen >> (j + c) & 1) ? pr * (__uint_as_float(d[k][j + c]) - delta) : 0.f;
+          }
+          pk[16 * k + (j >> 1)] = ptx::pack_bf16x2(e[0], e[1]);
+        }
+      }
+      if (t > 0 && !wait(&sh.z_empty, (t - 1) & 1)) break;
+      umma::tmem_st32(lanes + kZ + 32 * half, pk);
+      umma::tmem_st_wait();
+      umma::fence_before_sync();
+      ptx::mbar_arrive(&sh.z_full);
+      if (!w.last()) continue;
+      if (!wait(&sh.dq_done, n_items_done++ & 1)) break;
+      umma::fence_after_sync();
+      __nv_bfloat16* dst = p.gq + (((int64_t)w.l * p.rows + w.row0 + t_q) * p.H + w.h) * (kLatNope + p.dr);
+      // the first half of the warps: channels 0 .. 95, the others the rest
+      if (half == 0) store_bf16(lanes + kO, 96, p.scale, dst, mine);
+      else store_bf16(lanes + kO + 96, 32 + p.dr, p.scale, dst + 96, mine);
+      umma::fence_before_sync();
+    }
+  }
+  umma::fence_before_sync();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    umma::fence_after_sync();
+    umma::tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+// --------------------------------------------------------------------------------------------------------------- keys
+
+constexpr int kQTile = KeyWalk::kQ;
+constexpr int kQChunk = kQTile * 128;          // 64 queries x 64 channels
+constexpr int kStageK = 5 * kQChunk;           // Q: 3 chunks, dO: 2
+constexpr int kStagesK = 3;
+constexpr int kSmemK = kQBytes + kVBytes + kStagesK * kStageK + 1024;
+
+struct SharedK {
+  uint64_t full[kStagesK], raw[kStagesK], empty[kStagesK], kv_full, kv_empty, sp_full, sp_free, z_full, z_empty, done, drain;
+  uint32_t tmem;
+  int abort;
+  float2 rows[8][2][32];                       // per warp, two buffers: (lse in log2 units, D) of its columns' queries
+};
+
+__global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __grid_constant__ Maps maps, LatentReplayParams p, int n_items) {
+  extern __shared__ uint8_t smem_dyn[];
+  __shared__ SharedK sh;
+  uint8_t* sK = (uint8_t*)(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);
+  uint8_t* sV = sK + kQBytes;
+  uint8_t* stage = sV + kVBytes;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (warp == 0) {
+    if (lane < kStagesK) { ptx::mbar_init(&sh.full[lane], 1); ptx::mbar_init(&sh.raw[lane], 1); ptx::mbar_init(&sh.empty[lane], 1); }
+    if (lane == 31) {
+      ptx::mbar_init(&sh.kv_full, 1); ptx::mbar_init(&sh.kv_empty, 1); ptx::mbar_init(&sh.sp_full, 1); ptx::mbar_init(&sh.sp_free, 256);
+      ptx::mbar_init(&sh.z_full, 256); ptx::mbar_init(&sh.z_empty, 1); ptx::mbar_init(&sh.done, 1); ptx::mbar_init(&sh.drain, 1);
+      sh.abort = 0;
+    }
+    ptx::fence_barrier_init();
+  } else if (warp == kProducerWarp && lane == 0) {
+    ptx::prefetch_tensormap(&maps.q); ptx::prefetch_tensormap(&maps.kv); ptx::prefetch_tensormap(&maps.kr); ptx::prefetch_tensormap(&maps.go);
+  }
+  if (warp == kMmaWarp) umma::tmem_alloc(&sh.tmem, kTmemCols);
+  umma::fence_before_sync();
+  __syncthreads();
+  umma::fence_after_sync();
+  const uint32_t tmem = sh.tmem;
+  constexpr uint32_t kDv = 0, kDk = 128, kS = 320, kDp = 384, kP = 448, kZ = 480;        // columns
+  ptx::grid_dep_wait();
+  auto wait = [&](uint64_t* bar, uint32_t parity) { return umma::warp_wait(bar, parity, &sh.abort, p.dev_status); };
+
+  if (warp == kProducerWarp) {
+    KeyWalk w(n_items);
+    int t = 0, s = 0, phase = 0;
+    uint32_t through_raw = 0, raw_phase = 0;
+    while (w.next(p)) {
+      if (t >= kStagesK && !wait(&sh.empty[s], phase ^ 1)) break;
+      const bool tail = (w.i + 1) * kQTile > w.T;
+      const int y = (int)((int64_t)w.l * p.rows + w.row0 + w.i * kQTile);
+      if (umma::elect_one()) {
+        uint64_t* bar = tail ? &sh.raw[s] : &sh.full[s];
+        uint8_t* dst = stage + s * kStageK;
+        ptx::mbar_expect_tx(bar, kStageK);
+        for (int c = 0; c < 3; ++c) ptx::tma_load_3d(dst + c * kQChunk, &maps.q, 64 * c, w.h, y, bar);
+        for (int c = 0; c < 2; ++c) ptx::tma_load_3d(dst + (3 + c) * kQChunk, &maps.go, 64 * c, w.h, y, bar);
+      }
+      __syncwarp();
+      through_raw = tail ? through_raw | 1u << s : through_raw & ~(1u << s);
+      if (tail) raw_phase ^= 1u << s;
+      ++t;
+      if (++s == kStagesK) { s = 0; phase ^= 1; }
+    }
+    for (int x = max(0, t - kStagesK); x < t; ++x) {     // nothing is in flight when the CTA ends
+      const int k = x % kStagesK;
+      if (through_raw >> k & 1) ptx::mbar_wait_bounded(&sh.raw[k], ((raw_phase >> k) & 1) ^ 1);
+      else ptx::mbar_wait_bounded(&sh.full[k], (x / kStagesK) & 1);
+    }
+    __syncwarp();
+  } else if (warp == kMenderWarp) {
+    // queries behind the sequence's end: dV and dK sum over them
+    KeyWalk w(n_items);
+    uint32_t raw_phase = 0;
+    for (int t = 0; w.next(p); ++t) {
+      if ((w.i + 1) * kQTile <= w.T) continue;
+      const int s = t % kStagesK, n = w.T - w.i * kQTile;
+      if (!wait(&sh.raw[s], (raw_phase >> s) & 1)) break;
+      raw_phase ^= 1u << s;
+      for (int c = 0; c < 5; ++c)
+        for (int x = n * 8 + lane; x < kQTile * 8; x += 32)
+          *reinterpret_cast<uint4*>(stage + s * kStageK + c * kQChunk + x * 16) = make_uint4(0, 0, 0, 0);
+      ptx::fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(&sh.full[s]);
+    }
+  } else if (warp == kItemWarp) {
+    KeyWalk w(n_items);
+    int n = 0;
+    while (w.next(p)) {
+      if (!w.first) continue;
+      if (n > 0 && !wait(&sh.kv_empty, (n - 1) & 1)) break;
+      if (umma::elect_one()) {
+        const int y = (int)((int64_t)w.l * p.rows + w.row0 + w.j0);
+        ptx::mbar_expect_tx(&sh.kv_full, kQBytes + kVBytes);
+        for (int c = 0; c < 2; ++c) ptx::tma_load_3d(sK + c * kLatChunk, &maps.kv, 64 * c, w.h, y, &sh.kv_full);
+        ptx::tma_load_2d(sK + 2 * kLatChunk, &maps.kr, 0, y, &sh.kv_full);
+        for (int c = 0; c < 2; ++c) ptx::tma_load_3d(sV + c * kLatChunk, &maps.kv, kLatNope + 64 * c, w.h, y, &sh.kv_full);
+      }
+      __syncwarp();
+      ++n;
+    }
+    if (n > 0) ptx::mbar_wait_bounded(&sh.kv_full, (n - 1) & 1);
+    __syncwarp();
+  } else if (warp == kMmaWarp) {
+    constexpr uint32_t idesc = umma::instr_desc(kLatTile, kQTile, false), idesc_v = umma::instr_desc(kLatTile, kLatV, true),
+                       idesc_k = umma::instr_desc(kLatTile, 192, true);
+    const uint64_t hi = (uint64_t)umma::smem_desc_sw128(0, 0, 1024) & 0xffffffff00000000ull;
+    const uint32_t k_lo = (ptx::smem_u32(sK) >> 4) | 1u << 16, v_lo = (ptx::smem_u32(sV) >> 4) | 1u << 16, st_lo = ptx::smem_u32(stage) >> 4;
+    const int steps_r = p.dr / 16;
+    KeyWalk cur(n_items), nxt(n_items);
+    int n_k = 0, s_cur = 0, s_nxt = 0, ph_nxt = 0;
+    bool ok = true;
+    auto scores = [&](const KeyWalk& w, int t) {
+      if (w.first) ok = ok && wait(&sh.kv_full, n_k++ & 1);
+      ok = ok && wait(&sh.full[s_nxt], ph_nxt) && (t == 0 || wait(&sh.sp_free, (t - 1) & 1));
+      if (!ok) return;
+      umma::fence_after_sync();
+      const bool last = w.last();
+      if (umma::elect_one()) {
+        const uint32_t b = (st_lo + s_nxt * (kStageK >> 4)) | 1u << 16;
+#pragma unroll
+        for (int k = 0; k < 12; ++k)
+          if (k < 8 || k - 8 < steps_r)
+            umma::mma_bf16(tmem + kS, hi | (k_lo + (((k >> 2) * kLatChunk + (k & 3) * 32) >> 4)), hi | (b + (((k >> 2) * kQChunk + (k & 3) * 32) >> 4)), idesc,
+                           k > 0 ? 1u : 0u);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          umma::mma_bf16(tmem + kDp, hi | (v_lo + (((k >> 2) * kLatChunk + (k & 3) * 32) >> 4)),
+                         hi | (b + (((3 + (k >> 2)) * kQChunk + (k & 3) * 32) >> 4)), idesc, k > 0 ? 1u : 0u);
+        umma::commit(&sh.sp_full);
+        if (last) umma::commit(&sh.kv_empty);
+      }
+      __syncwarp();
+      if (++s_nxt == kStagesK) { s_nxt = 0; ph_nxt ^= 1; }
+    };
+    auto sums = [&](const KeyWalk& w, int t) {
+      ok = ok && wait(&sh.z_full, t & 1);
+      if (!ok) return;
+      umma::fence_after_sync();
+      const bool first = w.first, last = w.last();
+      if (umma::elect_one()) {
+        const uint32_t b = (st_lo + s_cur * (kStageK >> 4)) | (uint32_t)(kQChunk >> 4) << 16;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          umma::mma_bf16_a_tmem(tmem + kDv, tmem + kP + 8 * k, hi | (b + ((3 * kQChunk + k * 2048) >> 4)), idesc_v, (!first || k > 0) ? 1u : 0u);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          umma::mma_bf16_a_tmem(tmem + kDk, tmem + kZ + 8 * k, hi | (b + ((k * 2048) >> 4)), idesc_k, (!first || k > 0) ? 1u : 0u);
+        umma::commit(&sh.empty[s_cur]);
+        umma::commit(&sh.z_empty);
+        if (last) umma::commit(&sh.done);
+      }
+      __syncwarp();
+      if (++s_cur == kStagesK) s_cur = 0;
+    };
+    bool more = nxt.next(p);
+    if (more) scores(nxt, 0);
+    for (int t = 0; ok && more; ++t) {
+      cur = nxt;
+      more = nxt.next(p);
+      if (more && !nxt.first) scores(nxt, t + 1);
+      if (ok) sums(cur, t);
+      if (ok && more && nxt.first) scores(nxt, t + 1);
+    }
+    if (umma::elect_one()) umma::commit(&sh.drain);
+    __syncwarp();
+    ptx::mbar_wait_bounded(&sh.drain, 0);
+    __syncwarp();
+  } else {
+    const int half = warp >> 2, row = 32 * (warp & 3) + lane;
+    const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
+    KeyWalk w(n_items);
+    int lo = 0, hi = 0, n_done = 0;                      // queries that see this thread's key: lo .. hi - 1
+    const float* lse = nullptr;
+    const float* delta = nullptr;
+    for (int t = 0; w.next(p); ++t) {
+      const int j = w.j0 + row;
+      if (w.first) {
+        lo = j;
+        hi = j < w.T ? w.T : 0;
+        if (p.gone && j < w.T) hi = min(hi, p.gone[((int64_t)w.b * p.G + list_of(p.lists, w.l, 0, 1)) * p.gone_cap + j]);
+        const int64_t at = ((int64_t)w.l * p.H + w.h) * p.rows + w.row0;
+        lse = p.lse + at;
+        delta = p.delta + at;
+      }
+      const int t0 = w.i * kQTile + 32 * half;
+      {
+        const int t_q = t0 + lane;
+        sh.rows[warp][t & 1][lane] = t_q < w.T ? make_float2(lse[t_q] * 1.4426950408889634f, delta[t_q]) : make_float2(0.f, 0.f);
+        __syncwarp();
+      }
+      if (!wait(&sh.sp_full, t & 1)) break;
+      umma::fence_after_sync();
+      uint32_t z[32], d[32];
+      umma::tmem_ld32(lanes + kS + 32 * half, z);
+      umma::tmem_ld32(lanes + kDp + 32 * half, d);
+      umma::tmem_ld_wait();
+      umma::fence_before_sync();
+      ptx::mbar_arrive(&sh.sp_free);
+      const int c_lo = max(lo - t0, 0);
+      const uint32_t width = (uint32_t)max(hi - t0 - c_lo, 0);
+      uint32_t pp[16], pz[16];
+#pragma unroll
+      for (int c = 0; c < 32; c += 2) {
+        const float4 r = *reinterpret_cast<const float4*>(&sh.rows[warp][t & 1][c]);
+        float e0 = ptx::ex2_approx(fmaf(__uint_as_float(z[c]), p.scale_log2, -r.x)), e1 = ptx::ex2_approx(fmaf(__uint_as_float(z[c + 1]), p.scale_log2, -r.z));
+        const bool s0 = (uint32_t)(c - c_lo) < width, s1 = (uint32_t)(c + 1 - c_lo) < width;
+        e0 = s0 ? e0 : 0.f;
+        e1 = s1 ? e1 : 0.f;
+        pp[c >> 1] = ptx::pack_bf16x2(e0, e1);
+        pz[c >> 1] = ptx::pack_bf16x2(s0 ? e0 * (__uint_as_float(d[c]) - r.y) : 0.f, s1 ? e1 * (__uint_as_float(d[c + 1]) - r.w) : 0.f);
+      }
+      if (t > 0 && !wait(&sh.z_empty, (t - 1) & 1)) break;
+      umma::tmem_st8(lanes + kP + 16 * half, pp);
+      umma::tmem_st8(lanes + kP + 16 * half + 8, pp + 8);
+      umma::tmem_st8(lanes + kZ + 16 * half, pz);
+      umma::tmem_st8(lanes + kZ + 16 * half + 8, pz + 8);
+      umma::tmem_st_wait();
+      umma::fence_before_sync();
+      ptx::mbar_arrive(&sh.z_full);
+      if (!w.last()) continue;
+      if (!wait(&sh.done, n_done++ & 1)) break;
+      umma::fence_after_sync();
+      const bool mine = j < w.T;
+      __nv_bfloat16* dst = p.gkv + (((int64_t)w.l * p.rows + w.row0 + j) * p.H + w.h) * (kLatNope + kLatV);
+      if (half == 0) {
+        store_bf16(lanes + kDk, kLatNope, p.scale, dst, mine);
+      } else {
+        store_bf16(lanes + kDv, kLatV, 1.f, dst + kLatNope, mine);
+        float* part = p.dkr_part + (((int64_t)w.l * p.H + w.h) * p.rows + w.row0 + j) * p.dr;
+#pragma unroll 1
+        for (int c0 = 0; c0 < p.dr; c0 += 16) {
+          uint32_t o[16];
+          umma::tmem_ld16(lanes + kDk + kLatNope + c0, o);
+          umma::tmem_ld_wait();
+          if (mine) {
+#pragma unroll
+            for (int c = 0; c < 16; c += 4)
+              *reinterpret_cast<float4*>(part + c0 + c) = make_float4(__uint_as_float(o[c]) * p.scale, __uint_as_float(o[c + 1]) * p.scale,
+                                                                      __uint_as_float(o[c + 2]) * p.scale, __uint_as_float(o[c + 3]) * p.scale);
+          }
+        }
+      }
+      umma::fence_before_sync();
+    }
+  }
+  umma::fence_before_sync();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    umma::fence_after_sync();
+    umma::tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+// ------------------------------------------------------------------------------------------- the heads' shares of the rotary keys
+
+__global__ void __launch_bounds__(256) latent_grad_rope_kernel(LatentReplayParams p) {
+  const int b = blockIdx.y % p.B, l = blockIdx.y / p.B, per = p.dr / 4;
+  int64_t row0;
+  ptx::grid_dep_wait();
+  const int T = latent_seq(p, b, row0);
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t t = x / per;
+  const int c = 4 * (int)(x % per);
+  if (t >= T) return;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  const float* part = p.dkr_part + ((int64_t)l * p.H * p.rows + row0 + t) * p.dr + c;
+#pragma unroll 4
+  for (int h = 0; h < p.H; ++h) {
+    const float4 v = *reinterpret_cast<const float4*>(part + (int64_t)h * p.rows * p.dr);
+    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  }
+  *reinterpret_cast<uint2*>(p.gkr + ((int64_t)l * p.rows + row0 + t) * p.dr + c) = make_uint2(ptx::pack_bf16x2(s.x, s.y), ptx::pack_bf16x2(s.z, s.w));
+}
+
+}  // namespace
+
+int launch_latent_bwd(const LatentReplayParams& p, cudaStream_t stream) {
+  const int64_t items = ((int64_t)p.max_len + kLatTile - 1) / kLatTile * p.L * p.B * p.H;
+  if (items > 0x7fffff00LL) return NGC_ERR_UNSUPPORTED;
+  const int64_t rows = (int64_t)p.L * p.rows;
+  Maps mq, mk;                                   // boxes of 128 and of 64 rows
+  if (!make_token_map(&mq.q, p.q, kLatNope + p.dr, p.H, rows, kLatTile) || !make_token_map(&mq.kv, p.kv, kLatNope + kLatV, p.H, rows, kLatTile) ||
+      !make_rows_map(&mq.kr, p.kr, rows, kLatTile, p.dr) || !make_token_map(&mq.go, p.go, kLatV, p.H, rows, kLatTile))
+    return NGC_ERR_UNSUPPORTED;
+  mk = mq;
+  if (!make_token_map(&mk.q, p.q, kLatNope + p.dr, p.H, rows, kQTile) || !make_token_map(&mk.go, p.go, kLatV, p.H, rows, kQTile))
+    return NGC_ERR_UNSUPPORTED;
+  static PerDeviceOnce once;
+  static int sms[kMaxDevices] = {0};
+  int dev = -1;
+  const int rc = once.run([] {
+    int cur = -1;
+    cudaError_t e = cudaGetDevice(&cur);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms[cur], cudaDevAttrMultiProcessorCount, cur);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(latent_grad_q_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemQ);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(latent_grad_kv_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemK);
+    return e;
+  }, &dev);
+  if (rc != NGC_OK) return rc;
+  const int grid = (int)(items < sms[dev] ? items : sms[dev]);
+  NGC_CUDA_TRY(launch_pdl(latent_grad_kv_kernel, dim3(grid), dim3(kThreads), kSmemK, stream, mk, p, (int)items));
+  NGC_CUDA_TRY(launch_pdl(latent_grad_q_kernel, dim3(grid), dim3(kThreads), kSmemQ, stream, mq, p, (int)items));
+  const dim3 g((unsigned)(((int64_t)p.max_len * (p.dr / 4) + 255) / 256), p.L * p.B);
+  NGC_CUDA_TRY(launch_pdl(latent_grad_rope_kernel, g, dim3(256), 0, stream, p));
+  return launch_status();
+}
+
+}  // namespace ngc

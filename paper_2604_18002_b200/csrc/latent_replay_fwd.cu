@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
     // ------------------------------------------------------------------ keys and values
     // Tile t (over all items) has its keys in slots 5 t .. 5 t + 2 and its values in 5 t + 3, 5 t + 4 (mod 8): keys of tile t fit
     // when the values of t - 2 are used up, values of t when the keys of t - 1 are.
-    QueryWalk w(n_items), v(n_items);
+    QueryWalk<2> w(n_items), v(n_items);
     int t = 0, tv = 0, n_raw[2] = {0, 0};
     uint32_t v_through = 0;                              // bit b: the last values of parity b went through raw
     bool ok = true, more = w.next(p);
@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
     __syncwarp();
   } else if (warp == kMenderWarp) {
     // ------------------------------------------------------------------ values behind a sequence's end
-    QueryWalk w(n_items);
+    QueryWalk<2> w(n_items);
     uint32_t phase = 0;
     for (int t = 0; w.next(p); ++t) {
       if ((w.i + 1) * kLatTile <= w.T) continue;
@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
     }
   } else if (warp == kQWarp) {
     // ------------------------------------------------------------------ queries
-    QueryWalk w(n_items);
+    QueryWalk<2> w(n_items);
     int na = 0, nb = 0;                                  // blocks loaded
     bool ok = true;
     while (ok && w.next(p)) {
@@ -162,11 +162,11 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
     const uint64_t hi = (uint64_t)umma::smem_desc_sw128(0, 0, 1024) & 0xffffffff00000000ull;
     const uint32_t q_lo = (ptx::smem_u32(sQ) >> 4) | 1u << 16, ring_lo = ptx::smem_u32(ring) >> 4;
     const int steps_r = p.dr / 16;
-    QueryWalk cur(n_items), nxt(n_items);
+    QueryWalk<2> cur(n_items), nxt(n_items);
     int n_q[2] = {0, 0}, n_p[2] = {0, 0};                // query blocks begun, P tiles used
     bool ok = true;
     // scores of block x for tile t (walk w); commits what that makes free
-    auto scores = [&](const QueryWalk& w, int t, int x) {
+    auto scores = [&](const QueryWalk<2>& w, int t, int x) {
       if (w.first) {
         ok = ok && wait(&sh.q_full[x], n_q[x] & 1);
         ++n_q[x];
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
       __syncwarp();
     };
     // O += P V of block x for tile t
-    auto sums = [&](const QueryWalk& w, int t, int x) {
+    auto sums = [&](const QueryWalk<2>& w, int t, int x) {
       ok = ok && wait(&sh.v_full[t & 1], (t >> 1) & 1) && wait(&sh.p_full[x], n_p[x] & 1);
       if (!ok) return;
       ++n_p[x];
@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
     const int x = warp >> 2, row = 32 * (warp & 3) + lane;
     const uint32_t lane_base = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t s_addr = tmem + lane_base + 128u * x, o_addr = tmem + lane_base + 256u + 128u * x;
-    QueryWalk w(n_items);
+    QueryWalk<2> w(n_items);
     int n_s = 0, n_o = 0;                                // score tiles and items of this block so far
     float m_use = -INFINITY, l_run = 0.f;
     bool begun = false;                                  // this block has had a tile of the item

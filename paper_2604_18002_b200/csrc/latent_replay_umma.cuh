@@ -23,9 +23,9 @@ inline bool make_token_map(CUtensorMap* map, const void* base, int width, int he
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Blocks of 256 queries of one head, the longest first, dealt out to the CTAs in turn; and for each the tiles of 128 keys that any
-// of its queries sees.  Every warp of a CTA walks alike (all lanes together).
-struct QueryWalk {
+// Items of one or two blocks (A, B) of 128 queries of one head, the longest first, dealt out to the CTAs in turn; and for each the
+// tiles of 128 keys that any of its queries sees.  Every warp of a CTA walks alike (all lanes together).
+template <int BLOCKS> struct QueryWalk {
   int it, n_items;              // next item
   int l, b, h, q0, T, n;        // the current one; its key tiles are 0 .. n - 1
   int64_t row0;                 // first row of the sequence, within a layer
@@ -35,7 +35,7 @@ struct QueryWalk {
   bool first;                   // the current tile is the item's first
 
   __device__ __forceinline__ QueryWalk(int items) : it(blockIdx.x), n_items(items), n(0), i(0), window(0), live(0), plain_a(0), plain_b(0) {}
-  __device__ __forceinline__ bool has_b() const { return q0 + kLatTile < T; }
+  __device__ __forceinline__ bool has_b() const { return BLOCKS == 2 && q0 + kLatTile < T; }
   __device__ __forceinline__ bool for_a() const { return i * kLatTile <= q0; }
   __device__ __forceinline__ bool last_a() const { return i * kLatTile == q0; }
   __device__ __forceinline__ bool last() const { return i == n - 1; }
@@ -63,7 +63,7 @@ struct QueryWalk {
         const int per = p.L * p.B * p.H, m = n_items / per - 1 - it / per, x = it % per;
         it += gridDim.x;
         h = x % p.H; b = x / p.H % p.B; l = x / p.H / p.B;
-        q0 = m * 2 * kLatTile;
+        q0 = m * BLOCKS * kLatTile;
         T = latent_seq(p, b, row0);
         if (q0 < T) break;
       }
@@ -72,6 +72,38 @@ struct QueryWalk {
       window = 0;
       load_window(p);
       first = true;
+    }
+  }
+};
+
+// Items of 128 keys of one head, the first (which most queries see) first; and for each the tiles of 64 queries from its own first
+// key to the last query that sees one of them.
+struct KeyWalk {
+  static constexpr int kQ = 64;
+  int it, n_items;
+  int l, b, h, j0, T, i, n;     // current query tile, and the one behind the last
+  int64_t row0;
+  bool first;
+
+  __device__ __forceinline__ KeyWalk(int items) : it(blockIdx.x), n_items(items), i(-1), n(0) {}
+  __device__ __forceinline__ bool last() const { return i == n - 1; }
+  __device__ __forceinline__ bool next(const LatentReplayParams& p) {
+    first = false;
+    if (++i < n) return true;
+    for (;;) {
+      if (it >= n_items) return false;
+      const int per = p.L * p.B * p.H, x = it % per;
+      j0 = it / per * kLatTile;
+      it += gridDim.x;
+      h = x % p.H; b = x / p.H % p.B; l = x / p.H / p.B;
+      T = latent_seq(p, b, row0);
+      if (j0 >= T) continue;
+      int end = T;
+      if (p.tile_gone) end = min(T, p.tile_gone[((int64_t)b * p.G + list_of(p.lists, l, 0, 1)) * (p.gone_cap / kLatTile) + j0 / kLatTile].y);
+      i = j0 / kQ;
+      n = (end + kQ - 1) / kQ;
+      first = true;
+      if (i < n) return true;                            // (a key sees to its own query at least)
     }
   }
 };
