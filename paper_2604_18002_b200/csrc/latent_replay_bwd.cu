@@ -20,7 +20,7 @@
 namespace ngc {
 namespace {
 
-constexpr int kMmaWarp = 8, kProducerWarp = 9, kMenderWarp = 10, kItemWarp = 11;
+constexpr int kMmaWarp = 8, kProducerWarp = 9, kMenderWarp = 10, kPlannerWarp = 11;
 constexpr int kThreads = 12 * 32;
 constexpr uint32_t kTmemCols = 512;
 constexpr int kQBytes = 3 * kLatChunk, kVBytes = 2 * kLatChunk;          // 128 rows of 192 and of 128 channels
@@ -53,9 +53,10 @@ struct SharedQ {
   uint64_t k_full[2], k_raw[2], k_empty[2], v_full, v_empty, q_full, q_empty, sp_full, sp_free, z_full, z_empty, dq_done, drain;
   uint32_t tmem;
   int abort;
+  PlanRing ring;
 };
 
-__global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid_constant__ Maps maps, LatentReplayParams p, int n_items) {
+__global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid_constant__ Maps maps, LatentReplayParams p) {
   extern __shared__ uint8_t smem_dyn[];
   __shared__ SharedQ sh;
   uint8_t* sQ = (uint8_t*)(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);
@@ -64,7 +65,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
   uint8_t* sV = sK + 2 * kQBytes;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (warp == 0) {
-    if (lane < 2) { ptx::mbar_init(&sh.k_full[lane], 1); ptx::mbar_init(&sh.k_raw[lane], 1); ptx::mbar_init(&sh.k_empty[lane], 1); }
+    if (lane < 2) { ptx::mbar_init(&sh.k_full[lane], 1); ptx::mbar_init(&sh.k_raw[lane], 1); ptx::mbar_init(&sh.k_empty[lane], 1); sh.ring.init(lane); }
     if (lane == 2) {
       ptx::mbar_init(&sh.v_full, 1); ptx::mbar_init(&sh.v_empty, 1); ptx::mbar_init(&sh.q_full, 1); ptx::mbar_init(&sh.q_empty, 1);
       ptx::mbar_init(&sh.sp_full, 1); ptx::mbar_init(&sh.sp_free, 256); ptx::mbar_init(&sh.z_full, 256); ptx::mbar_init(&sh.z_empty, 1);
@@ -82,14 +83,15 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
   const uint32_t tmem = sh.tmem;
   constexpr uint32_t kS = 0, kP = 128, kO = 256, kZ = 448;               // columns of S, dP, dQ, dZ
   ptx::grid_dep_wait();
-  auto wait = [&](uint64_t* bar, uint32_t parity) { return umma::warp_wait(bar, parity, &sh.abort, p.dev_status); };
+  const WalkEnv env{p, &sh.ring, &sh.abort};
+  auto wait = [&](uint64_t* bar, uint32_t parity) { return env.wait(bar, parity); };
 
   if (warp == kProducerWarp) {
-    QueryWalk<1> w(n_items);
+    QueryWalk<1> w;
     int t = 0, n_raw[2] = {0, 0};
     uint32_t through_raw = 0;
     bool ok = true;
-    while (ok && w.next(p)) {
+    while (ok && w.next(env)) {
       const int y = (int)((int64_t)w.l * p.rows + w.row0 + w.i * kLatTile), s = t & 1;
       const bool tail = (w.i + 1) * kLatTile > w.T;
       if (t > 1) ok = wait(&sh.k_empty[s], ((t >> 1) - 1) & 1);
@@ -122,9 +124,9 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
     __syncwarp();
   } else if (warp == kMenderWarp) {
     // keys behind the sequence's end: dQ sums over them
-    QueryWalk<1> w(n_items);
+    QueryWalk<1> w;
     uint32_t phase = 0;
-    for (int t = 0; w.next(p); ++t) {
+    for (int t = 0; w.next(env); ++t) {
       if ((w.i + 1) * kLatTile <= w.T) continue;
       const int s = t & 1, n = w.T - w.i * kLatTile;
       if (!wait(&sh.k_raw[s], (phase >> s) & 1)) break;
@@ -136,12 +138,10 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&sh.k_full[s]);
     }
-  } else if (warp == kItemWarp) {
-    QueryWalk<1> w(n_items);
+  } else if (warp == kPlannerWarp) {
     int n = 0;
-    while (w.next(p)) {
-      if (!w.first) continue;
-      if (n > 0 && !wait(&sh.q_empty, (n - 1) & 1)) break;
+    run_planner<QueryWalk<1>>(env, kLatTile, true, [&](const QueryWalk<1>& w, int k) {
+      if (k > 0 && !wait(&sh.q_empty, (k - 1) & 1)) return false;
       if (umma::elect_one()) {
         const int y = (int)((int64_t)w.l * p.rows + w.row0 + w.q0);
         ptx::mbar_expect_tx(&sh.q_full, kQBytes + kVBytes);
@@ -150,7 +150,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
       }
       __syncwarp();
       ++n;
-    }
+      return true;
+    });
     if (n > 0) ptx::mbar_wait_bounded(&sh.q_full, (n - 1) & 1);
     __syncwarp();
   } else if (warp == kMmaWarp) {
@@ -159,7 +160,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
     const uint32_t q_lo = (ptx::smem_u32(sQ) >> 4) | 1u << 16, g_lo = (ptx::smem_u32(sG) >> 4) | 1u << 16, v_lo = (ptx::smem_u32(sV) >> 4) | 1u << 16,
                    k_lo = ptx::smem_u32(sK) >> 4;
     const int steps_r = p.dr / 16;
-    QueryWalk<1> cur(n_items), nxt(n_items);
+    QueryWalk<1> cur, nxt;
     int n_q = 0;
     bool ok = true;
     auto scores = [&](const QueryWalk<1>& w, int t) {
@@ -209,11 +210,11 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
       }
       __syncwarp();
     };
-    bool more = nxt.next(p);
+    bool more = nxt.next(env);
     if (more) scores(nxt, 0);
     for (int t = 0; ok && more; ++t) {
       cur = nxt;
-      more = nxt.next(p);
+      more = nxt.next(env);
       // the next tile's scores first; at an item's end the sums, since the next queries are still on their way
       if (more && !nxt.first) scores(nxt, t + 1);
       if (ok) sums(cur, t);
@@ -226,16 +227,24 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
   } else {
     const int half = warp >> 2, row = 32 * (warp & 3) + lane;
     const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
-    QueryWalk<1> w(n_items);
+    QueryWalk<1> w;
     float lse2 = 0.f, delta = 0.f;
     int n_items_done = 0;
-    for (int t = 0; w.next(p); ++t) {
+    for (int t = 0; w.next(env); ++t) {
       const int t_q = w.q0 + row;
       const bool mine = t_q < w.T;
       if (w.first) {
         const int64_t at = ((int64_t)w.l * p.H + w.h) * p.rows + w.row0 + t_q;
         lse2 = mine ? p.lse[at] * 1.4426950408889634f : 0.f;
         delta = mine ? p.delta[at] : 0.f;
+      }
+      const int j0 = w.i * kLatTile + 64 * half;
+      const bool plain = !w.tiles || (w.plain_a >> (w.i - w.window) & 1);
+      int g[2];                                          // (asked for before the wait: the answer takes as long)
+      if (!plain) {
+        const int32_t* gone = p.gone + ((int64_t)w.b * p.G + list_of(p.lists, w.l, 0, 1)) * p.gone_cap + j0 + lane;
+        g[0] = gone[0];
+        g[1] = gone[32];
       }
       if (!wait(&sh.sp_full, t & 1)) break;
       umma::fence_after_sync();
@@ -247,9 +256,6 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
       umma::tmem_ld_wait();
       umma::fence_before_sync();
       ptx::mbar_arrive(&sh.sp_free);
-      const int j0 = w.i * kLatTile + 64 * half;
-      const bool plain = !w.tiles || (w.plain_a >> (w.i - w.window) & 1);
-      const int32_t* gone = plain ? nullptr : p.gone + ((int64_t)w.b * p.G + list_of(p.lists, w.l, 0, 1)) * p.gone_cap + j0;
       uint32_t pk[32];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -257,14 +263,13 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
         const int behind = t_q - (j0 + 32 * k);          // keys behind the query do not count
         if (behind < 31) seen = behind < 0 ? 0u : (2u << behind) - 1u;
         if (!plain) {
-          const int g = gone[32 * k + lane];
-          const uint32_t lo = __ballot_sync(0xffffffffu, g > w.q0 + kLatTile - 1);
-          if (lo == __ballot_sync(0xffffffffu, g > w.q0)) {
+          const uint32_t lo = __ballot_sync(0xffffffffu, g[k] > w.q0 + kLatTile - 1);
+          if (lo == __ballot_sync(0xffffffffu, g[k] > w.q0)) {
             seen &= lo;
           } else {
             uint32_t m = 0;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) m |= __shfl_sync(0xffffffffu, g, j) > t_q ? 1u << j : 0u;
+            for (int j = 0; j < 32; ++j) m |= __shfl_sync(0xffffffffu, g[k], j) > t_q ? 1u << j : 0u;
             seen &= m;
           }
         }
@@ -314,10 +319,11 @@ struct SharedK {
   uint64_t full[kStagesK], raw[kStagesK], empty[kStagesK], kv_full, kv_empty, sp_full, sp_free, z_full, z_empty, done, drain;
   uint32_t tmem;
   int abort;
+  PlanRing ring;
   float2 rows[8][2][32];                       // per warp, two buffers: (lse in log2 units, D) of its columns' queries
 };
 
-__global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __grid_constant__ Maps maps, LatentReplayParams p, int n_items) {
+__global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __grid_constant__ Maps maps, LatentReplayParams p) {
   extern __shared__ uint8_t smem_dyn[];
   __shared__ SharedK sh;
   uint8_t* sK = (uint8_t*)(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);
@@ -326,6 +332,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (warp == 0) {
     if (lane < kStagesK) { ptx::mbar_init(&sh.full[lane], 1); ptx::mbar_init(&sh.raw[lane], 1); ptx::mbar_init(&sh.empty[lane], 1); }
+    if (lane < 2) sh.ring.init(lane);
     if (lane == 31) {
       ptx::mbar_init(&sh.kv_full, 1); ptx::mbar_init(&sh.kv_empty, 1); ptx::mbar_init(&sh.sp_full, 1); ptx::mbar_init(&sh.sp_free, 256);
       ptx::mbar_init(&sh.z_full, 256); ptx::mbar_init(&sh.z_empty, 1); ptx::mbar_init(&sh.done, 1); ptx::mbar_init(&sh.drain, 1);
@@ -342,13 +349,14 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
   const uint32_t tmem = sh.tmem;
   constexpr uint32_t kDv = 0, kDk = 128, kS = 320, kDp = 384, kP = 448, kZ = 480;        // columns
   ptx::grid_dep_wait();
-  auto wait = [&](uint64_t* bar, uint32_t parity) { return umma::warp_wait(bar, parity, &sh.abort, p.dev_status); };
+  const WalkEnv env{p, &sh.ring, &sh.abort};
+  auto wait = [&](uint64_t* bar, uint32_t parity) { return env.wait(bar, parity); };
 
   if (warp == kProducerWarp) {
-    KeyWalk w(n_items);
+    KeyWalk w;
     int t = 0, s = 0, phase = 0;
     uint32_t through_raw = 0, raw_phase = 0;
-    while (w.next(p)) {
+    while (w.next(env)) {
       if (t >= kStagesK && !wait(&sh.empty[s], phase ^ 1)) break;
       const bool tail = (w.i + 1) * kQTile > w.T;
       const int y = (int)((int64_t)w.l * p.rows + w.row0 + w.i * kQTile);
@@ -373,9 +381,9 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
     __syncwarp();
   } else if (warp == kMenderWarp) {
     // queries behind the sequence's end: dV and dK sum over them
-    KeyWalk w(n_items);
+    KeyWalk w;
     uint32_t raw_phase = 0;
-    for (int t = 0; w.next(p); ++t) {
+    for (int t = 0; w.next(env); ++t) {
       if ((w.i + 1) * kQTile <= w.T) continue;
       const int s = t % kStagesK, n = w.T - w.i * kQTile;
       if (!wait(&sh.raw[s], (raw_phase >> s) & 1)) break;
@@ -387,12 +395,10 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&sh.full[s]);
     }
-  } else if (warp == kItemWarp) {
-    KeyWalk w(n_items);
+  } else if (warp == kPlannerWarp) {
     int n = 0;
-    while (w.next(p)) {
-      if (!w.first) continue;
-      if (n > 0 && !wait(&sh.kv_empty, (n - 1) & 1)) break;
+    run_planner<KeyWalk>(env, kLatTile, false, [&](const KeyWalk& w, int k) {
+      if (k > 0 && !wait(&sh.kv_empty, (k - 1) & 1)) return false;
       if (umma::elect_one()) {
         const int y = (int)((int64_t)w.l * p.rows + w.row0 + w.j0);
         ptx::mbar_expect_tx(&sh.kv_full, kQBytes + kVBytes);
@@ -402,7 +408,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
       }
       __syncwarp();
       ++n;
-    }
+      return true;
+    });
     if (n > 0) ptx::mbar_wait_bounded(&sh.kv_full, (n - 1) & 1);
     __syncwarp();
   } else if (warp == kMmaWarp) {
@@ -411,7 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
     const uint64_t hi = (uint64_t)umma::smem_desc_sw128(0, 0, 1024) & 0xffffffff00000000ull;
     const uint32_t k_lo = (ptx::smem_u32(sK) >> 4) | 1u << 16, v_lo = (ptx::smem_u32(sV) >> 4) | 1u << 16, st_lo = ptx::smem_u32(stage) >> 4;
     const int steps_r = p.dr / 16;
-    KeyWalk cur(n_items), nxt(n_items);
+    KeyWalk cur, nxt;
     int n_k = 0, s_cur = 0, s_nxt = 0, ph_nxt = 0;
     bool ok = true;
     auto scores = [&](const KeyWalk& w, int t) {
@@ -457,11 +464,11 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
       __syncwarp();
       if (++s_cur == kStagesK) s_cur = 0;
     };
-    bool more = nxt.next(p);
+    bool more = nxt.next(env);
     if (more) scores(nxt, 0);
     for (int t = 0; ok && more; ++t) {
       cur = nxt;
-      more = nxt.next(p);
+      more = nxt.next(env);
       if (more && !nxt.first) scores(nxt, t + 1);
       if (ok) sums(cur, t);
       if (ok && more && nxt.first) scores(nxt, t + 1);
@@ -473,11 +480,12 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
   } else {
     const int half = warp >> 2, row = 32 * (warp & 3) + lane;
     const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
-    KeyWalk w(n_items);
+    KeyWalk w;
     int lo = 0, hi = 0, n_done = 0;                      // queries that see this thread's key: lo .. hi - 1
     const float* lse = nullptr;
     const float* delta = nullptr;
-    for (int t = 0; w.next(p); ++t) {
+    float2 ahead = make_float2(0.f, 0.f);
+    for (int t = 0; w.next(env); ++t) {
       const int j = w.j0 + row;
       if (w.first) {
         lo = j;
@@ -488,11 +496,11 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
         delta = p.delta + at;
       }
       const int t0 = w.i * kQTile + 32 * half;
-      {
-        const int t_q = t0 + lane;
-        sh.rows[warp][t & 1][lane] = t_q < w.T ? make_float2(lse[t_q] * 1.4426950408889634f, delta[t_q]) : make_float2(0.f, 0.f);
-        __syncwarp();
-      }
+      auto row_of = [&](int t_q) { return t_q < w.T ? make_float2(lse[t_q] * 1.4426950408889634f, delta[t_q]) : make_float2(0.f, 0.f); };
+      if (w.first) ahead = row_of(t0 + lane);
+      sh.rows[warp][t & 1][lane] = ahead;
+      __syncwarp();
+      if (!w.last()) ahead = row_of(t0 + kQTile + lane);     // the next tile's, a tile early
       if (!wait(&sh.sp_full, t & 1)) break;
       umma::fence_after_sync();
       uint32_t z[32], d[32];
@@ -603,8 +611,8 @@ int launch_latent_bwd(const LatentReplayParams& p, cudaStream_t stream) {
   }, &dev);
   if (rc != NGC_OK) return rc;
   const int grid = (int)(items < sms[dev] ? items : sms[dev]);
-  NGC_CUDA_TRY(launch_pdl(latent_grad_kv_kernel, dim3(grid), dim3(kThreads), kSmemK, stream, mk, p, (int)items));
-  NGC_CUDA_TRY(launch_pdl(latent_grad_q_kernel, dim3(grid), dim3(kThreads), kSmemQ, stream, mq, p, (int)items));
+  NGC_CUDA_TRY(launch_pdl(latent_grad_kv_kernel, dim3(grid), dim3(kThreads), kSmemK, stream, mk, p));
+  NGC_CUDA_TRY(launch_pdl(latent_grad_q_kernel, dim3(grid), dim3(kThreads), kSmemQ, stream, mq, p));
   const dim3 g((unsigned)(((int64_t)p.max_len * (p.dr / 4) + 255) / 256), p.L * p.B);
   NGC_CUDA_TRY(launch_pdl(latent_grad_rope_kernel, g, dim3(256), 0, stream, p));
   return launch_status();

@@ -6,7 +6,8 @@
 // passed over, and most of the others need no look at single keys.  Roles, which meet at mbarriers only:
 //   producer warp     K and V chunks of 128 rows x 64 channels by TMA into a ring of eight 16 KB slots, K of tile i + 1 before V of
 //                     tile i: K makes room as soon as both blocks' scores are done
-//   Q warp            the queries of the next item when the last scores of this one are done, block by block
+//   planner warp      what the other roles need to know of the items, up to two ahead, and the queries of the next item when the
+//                     last scores of this one are done, block by block
 //   mender warp       values behind a sequence's end: zeros (they belong to others; a NaN times a zero weight is NaN)
 //   MMA warp          P V of block A, S of its next tile, P V of block B, S of its next tile: one block's softmax runs under
 //                     the other's products
@@ -23,7 +24,7 @@ namespace ngc {
 namespace {
 
 constexpr int kSlots = 8;
-constexpr int kMmaWarp = 8, kProducerWarp = 9, kMenderWarp = 10, kQWarp = 11;
+constexpr int kMmaWarp = 8, kProducerWarp = 9, kMenderWarp = 10, kPlannerWarp = 11;
 constexpr int kThreads = 12 * 32;
 constexpr int kQBlock = 3 * kLatChunk;         // 128 queries, 192 channels
 constexpr int kSmemBytes = 2 * kQBlock + kSlots * kLatChunk + 1024;
@@ -37,9 +38,10 @@ struct Shared {
   uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_done[2], drain;
   uint32_t tmem;
   int abort;
+  PlanRing ring;
 };
 
-__global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_constant__ Maps maps, LatentReplayParams p, int n_items) {
+__global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_constant__ Maps maps, LatentReplayParams p) {
   extern __shared__ uint8_t smem_dyn[];
   __shared__ Shared sh;
   uint8_t* sQ = (uint8_t*)(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);     // [2 blocks][3 chunks]
@@ -52,6 +54,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
       ptx::mbar_init(&sh.v_full[lane], 1); ptx::mbar_init(&sh.v_raw[lane], 1); ptx::mbar_init(&sh.v_empty[lane], 1);
       ptx::mbar_init(&sh.q_full[lane], 1); ptx::mbar_init(&sh.q_empty[lane], 1);
       ptx::mbar_init(&sh.s_full[lane], 1); ptx::mbar_init(&sh.p_full[lane], 128); ptx::mbar_init(&sh.o_done[lane], 1);
+      sh.ring.init(lane);
     }
     if (lane == 2) { ptx::mbar_init(&sh.drain, 1); sh.abort = 0; }
     ptx::fence_barrier_init();
@@ -64,18 +67,18 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
   umma::fence_after_sync();
   const uint32_t tmem = sh.tmem;
   ptx::grid_dep_wait();
-  auto wait = [&](uint64_t* bar, uint32_t parity) { return umma::warp_wait(bar, parity, &sh.abort, p.dev_status); };
+  const WalkEnv env{p, &sh.ring, &sh.abort};
+  auto wait = [&](uint64_t* bar, uint32_t parity) { return env.wait(bar, parity); };
 
   if (warp == kProducerWarp) {
     // ------------------------------------------------------------------ keys and values
     // Tile t (over all items) has its keys in slots 5 t .. 5 t + 2 and its values in 5 t + 3, 5 t + 4 (mod 8): keys of tile t fit
     // when the values of t - 2 are used up, values of t when the keys of t - 1 are.
-    QueryWalk<2> w(n_items), v(n_items);
+    QueryWalk<2> w, v;                                   // v: the tile before
     int t = 0, tv = 0, n_raw[2] = {0, 0};
     uint32_t v_through = 0;                              // bit b: the last values of parity b went through raw
-    bool ok = true, more = w.next(p);
+    bool ok = true, more = w.next(env);
     auto values = [&]() {                                // of tile tv
-      v.next(p);
       if (tv > 0) ok = wait(&sh.k_empty[(tv - 1) & 1], ((tv - 1) >> 1) & 1);
       if (!ok) return;
       const int64_t y = (int64_t)v.l * p.rows + v.row0 + v.i * kLatTile;
@@ -102,8 +105,9 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
       }
       __syncwarp();
       ++t;
-      more = w.next(p);
       if (t > 1) values();                               // of the tile before
+      v = w;
+      more = ok && w.next(env);
     }
     if (ok && t > tv) values();
     // nothing is in flight when the CTA ends
@@ -115,9 +119,9 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
     __syncwarp();
   } else if (warp == kMenderWarp) {
     // ------------------------------------------------------------------ values behind a sequence's end
-    QueryWalk<2> w(n_items);
+    QueryWalk<2> w;
     uint32_t phase = 0;
-    for (int t = 0; w.next(p); ++t) {
+    for (int t = 0; w.next(env); ++t) {
       if ((w.i + 1) * kLatTile <= w.T) continue;
       if (!wait(&sh.v_raw[t & 1], (phase >> (t & 1)) & 1)) break;
       phase ^= 1u << (t & 1);
@@ -130,19 +134,15 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&sh.v_full[t & 1]);
     }
-  } else if (warp == kQWarp) {
-    // ------------------------------------------------------------------ queries
-    QueryWalk<2> w(n_items);
+  } else if (warp == kPlannerWarp) {
+    // ------------------------------------------------------------------ plans and queries of the items
     int na = 0, nb = 0;                                  // blocks loaded
-    bool ok = true;
-    while (ok && w.next(p)) {
-      if (!w.first) continue;
+    run_planner<QueryWalk<2>>(env, 2 * kLatTile, true, [&](const QueryWalk<2>& w, int) {
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         int& n = x ? nb : na;
         if (x && !w.has_b()) break;
-        ok = ok && (n == 0 || wait(&sh.q_empty[x], (n - 1) & 1));
-        if (!ok) break;
+        if (n > 0 && !wait(&sh.q_empty[x], (n - 1) & 1)) return false;
         if (umma::elect_one()) {
           const int y = (int)((int64_t)w.l * p.rows + w.row0 + w.q0 + x * kLatTile);
           ptx::mbar_expect_tx(&sh.q_full[x], kQBlock);
@@ -151,7 +151,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
         __syncwarp();
         ++n;
       }
-    }
+      return true;
+    });
     if (na > 0) ptx::mbar_wait_bounded(&sh.q_full[0], (na - 1) & 1);
     if (nb > 0) ptx::mbar_wait_bounded(&sh.q_full[1], (nb - 1) & 1);
     __syncwarp();
@@ -162,7 +163,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
     const uint64_t hi = (uint64_t)umma::smem_desc_sw128(0, 0, 1024) & 0xffffffff00000000ull;
     const uint32_t q_lo = (ptx::smem_u32(sQ) >> 4) | 1u << 16, ring_lo = ptx::smem_u32(ring) >> 4;
     const int steps_r = p.dr / 16;
-    QueryWalk<2> cur(n_items), nxt(n_items);
+    QueryWalk<2> cur, nxt;
     int n_q[2] = {0, 0}, n_p[2] = {0, 0};                // query blocks begun, P tiles used
     bool ok = true;
     // scores of block x for tile t (walk w); commits what that makes free
@@ -219,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
       }
       __syncwarp();
     };
-    bool more = nxt.next(p);
+    bool more = nxt.next(env);
     int t = 0;
     if (more) {
       if (nxt.for_a()) scores(nxt, 0, 0);
@@ -227,7 +228,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
     }
     while (ok && more) {
       cur = nxt;
-      more = nxt.next(p);
+      more = nxt.next(env);
       if (cur.for_a()) sums(cur, t, 0);
       if (ok && more && nxt.for_a()) scores(nxt, t + 1, 0);
       if (ok && cur.has_b()) sums(cur, t, 1);
@@ -243,13 +244,20 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
     const int x = warp >> 2, row = 32 * (warp & 3) + lane;
     const uint32_t lane_base = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t s_addr = tmem + lane_base + 128u * x, o_addr = tmem + lane_base + 256u + 128u * x;
-    QueryWalk<2> w(n_items);
+    QueryWalk<2> w;
     int n_s = 0, n_o = 0;                                // score tiles and items of this block so far
     float m_use = -INFINITY, l_run = 0.f;
     bool begun = false;                                  // this block has had a tile of the item
-    while (w.next(p)) {
+    while (w.next(env)) {
       if (w.first) { m_use = -INFINITY; l_run = 0.f; begun = false; }
       if (x ? !w.has_b() : !w.for_a()) continue;
+      const bool plain = !w.tiles || ((x ? w.plain_b : w.plain_a) >> (w.i - w.window) & 1);
+      int g[4];                                          // (asked for before the wait: the answer takes as long)
+      if (!plain) {
+        const int32_t* gone = p.gone + ((int64_t)w.b * p.G + list_of(p.lists, w.l, 0, 1)) * p.gone_cap + w.i * kLatTile + lane;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) g[k] = gone[32 * k];
+      }
       if (!wait(&sh.s_full[x], n_s & 1)) break;
       ++n_s;
       umma::fence_after_sync();
@@ -265,21 +273,19 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
           for (int j = 0; j < 32; ++j)
             if (j0 + 32 * k + j > t_q) z[k][j] = 0xff800000u;
       }
-      if (w.tiles && !((x ? w.plain_b : w.plain_a) >> (w.i - w.window) & 1)) {
+      if (!plain) {
         // keys that have gone: the same for all queries of the block where no round falls between its first and last
-        const int32_t* gone = p.gone + ((int64_t)w.b * p.G + list_of(p.lists, w.l, 0, 1)) * p.gone_cap + j0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const int g = gone[32 * k + lane];
-          const uint32_t seen = __ballot_sync(0xffffffffu, g > q_lo + kLatTile - 1);
-          if (seen == __ballot_sync(0xffffffffu, g > q_lo)) {
+          const uint32_t seen = __ballot_sync(0xffffffffu, g[k] > q_lo + kLatTile - 1);
+          if (seen == __ballot_sync(0xffffffffu, g[k] > q_lo)) {
 #pragma unroll
             for (int j = 0; j < 32; ++j)
               if (!(seen >> j & 1)) z[k][j] = 0xff800000u;
           } else {
 #pragma unroll
             for (int j = 0; j < 32; ++j)
-              if (__shfl_sync(0xffffffffu, g, j) <= t_q) z[k][j] = 0xff800000u;
+              if (__shfl_sync(0xffffffffu, g[k], j) <= t_q) z[k][j] = 0xff800000u;
           }
         }
       }
@@ -400,7 +406,7 @@ int launch_latent_fwd(const LatentReplayParams& p, cudaStream_t stream) {
   }, &dev);
   if (rc != NGC_OK) return rc;
   const int grid = (int)(items < sms[dev] ? items : sms[dev]);
-  NGC_CUDA_TRY(launch_pdl(latent_fwd_kernel, dim3(grid), dim3(kThreads), kSmemBytes, stream, maps, p, (int)items));
+  NGC_CUDA_TRY(launch_pdl(latent_fwd_kernel, dim3(grid), dim3(kThreads), kSmemBytes, stream, maps, p));
   return launch_status();
 }
 

@@ -23,23 +23,96 @@ inline bool make_token_map(CUtensorMap* map, const void* base, int width, int he
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Items of one or two blocks (A, B) of 128 queries of one head, the longest first, dealt out to the CTAs in turn; and for each the
-// tiles of 128 keys that any of its queries sees.  Every warp of a CTA walks alike (all lanes together).
+// Deals the items of a call out to its CTAs: blocks of `size` tokens of every (sequence, head, layer), level by level (all first
+// blocks, all second ones, ...; or from the last level down), so that the long ones come first; and in turn from the first CTA to the
+// last and back, so that who gets a longer one gets a shorter one next.  Only blocks that exist are counted.  All lanes of a warp
+// together.
+struct Deal {
+  int size, pass, m, before, count;            // level, items before it, sequences that have it
+  bool down;
+  __device__ __forceinline__ Deal(const LatentReplayParams& p, int block, bool from_last) : size(block), pass(0), m(0), before(0), count(0), down(from_last) {
+    if (down) {
+      int longest = 0;
+      for (int b0 = 0; b0 < p.B; b0 += 32) longest = max(longest, length(p, b0 + (threadIdx.x & 31)));
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
+      m = (longest + size - 1) / size - 1;
+    }
+    count = m >= 0 ? sequences(p) : 0;
+  }
+  static __device__ __forceinline__ int length(const LatentReplayParams& p, int b) {
+    int64_t row0;
+    return b < p.B ? latent_seq(p, b, row0) : 0;
+  }
+  __device__ __forceinline__ int sequences(const LatentReplayParams& p) const {
+    int n = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 32) n += __popc(__ballot_sync(0xffffffffu, length(p, b0 + (threadIdx.x & 31)) > (int64_t)m * size));
+    return n;
+  }
+  // The next item of this CTA: block m of a sequence.
+  __device__ __forceinline__ bool next(const LatentReplayParams& p, int& l, int& b, int& h) {
+    const int k = pass * (int)gridDim.x + ((pass & 1) ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x), per = p.L * p.H;
+    while (count > 0 && k - before >= count * per) {
+      before += count * per;
+      m += down ? -1 : 1;
+      count = m >= 0 ? sequences(p) : 0;
+    }
+    if (count == 0) return false;                        // (levels only end behind the last one)
+    ++pass;
+    int x = k - before;
+    h = x % p.H;
+    x /= p.H;
+    l = x / count;
+    x %= count;
+    for (int b0 = 0;; b0 += 32) {
+      const uint32_t has = __ballot_sync(0xffffffffu, length(p, b0 + (threadIdx.x & 31)) > (int64_t)m * size);
+      const int n = __popc(has);
+      if (x < n) { b = b0 + (int)__fns(has, 0, x + 1); return true; }
+      x -= n;
+    }
+  }
+};
+
+// An item's description, made by the planner warp (which also loads what stays in shared memory throughout the item) up to two items
+// ahead, so that no other role meets the chain of reads behind it.
+struct ReplayPlan {
+  int valid, l, b, h, x0, T, n;                // first token of the item's block; query walks: key tiles, key walks: query tiles
+  uint32_t live, plain_a, plain_b;             // query walks: see there, of the first 32 tiles
+  int64_t row0;                                // first row of the sequence, within a layer
+};
+struct PlanRing {
+  uint64_t full[2], empty[2];
+  ReplayPlan plan[2];
+  static constexpr int kReaders = 11;          // producer, mender, MMA, eight softmax warps
+  __device__ __forceinline__ void init(int i) { ptx::mbar_init(&full[i], 1); ptx::mbar_init(&empty[i], kReaders); }
+};
+// What every walk needs of a launch.
+struct WalkEnv {
+  const LatentReplayParams& p;
+  PlanRing* ring;
+  int* abort;
+  __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) const { return umma::warp_wait(bar, parity, abort, p.dev_status); }
+  __device__ __forceinline__ const int2* tiles(int l, int b) const {
+    return p.tile_gone ? p.tile_gone + ((int64_t)b * p.G + list_of(p.lists, l, 0, 1)) * (p.gone_cap / kLatTile) : nullptr;
+  }
+};
+
+// Items of one or two blocks (A, B) of 128 queries of one head; and for each the tiles of 128 keys that any of its queries sees.
 template <int BLOCKS> struct QueryWalk {
-  int it, n_items;              // next item
-  int l, b, h, q0, T, n;        // the current one; its key tiles are 0 .. n - 1
-  int64_t row0;                 // first row of the sequence, within a layer
+  int k;                        // items so far
+  int l, b, h, q0, T, n;        // the current item; its key tiles are 0 .. n - 1
+  int64_t row0;
   const int2* tiles;            // of its list, or null
   int i, window;                // current tile, first tile of the window
   uint32_t live, plain_a, plain_b;             // of the window: tiles that a query sees; ones without a key that goes before query block A's (B's) last
   bool first;                   // the current tile is the item's first
 
-  __device__ __forceinline__ QueryWalk(int items) : it(blockIdx.x), n_items(items), n(0), i(0), window(0), live(0), plain_a(0), plain_b(0) {}
+  __device__ __forceinline__ QueryWalk() : k(0), n(0), i(0), window(0), live(0), plain_a(0), plain_b(0) {}
   __device__ __forceinline__ bool has_b() const { return BLOCKS == 2 && q0 + kLatTile < T; }
   __device__ __forceinline__ bool for_a() const { return i * kLatTile <= q0; }
   __device__ __forceinline__ bool last_a() const { return i * kLatTile == q0; }
   __device__ __forceinline__ bool last() const { return i == n - 1; }
-  __device__ __forceinline__ void load_window(const LatentReplayParams& p) {
+  __device__ __forceinline__ void load_window() {
     const int t = window + (threadIdx.x & 31);
     int2 g = make_int2(kNeverGone, kNeverGone);
     if (tiles && t < n) g = tiles[t];
@@ -47,65 +120,100 @@ template <int BLOCKS> struct QueryWalk {
     plain_a = __ballot_sync(0xffffffffu, g.x > q0 + kLatTile - 1);
     plain_b = __ballot_sync(0xffffffffu, g.x > q0 + 2 * kLatTile - 1);
   }
-  __device__ __forceinline__ bool next(const LatentReplayParams& p) {
+  // The planner's part.
+  __device__ __forceinline__ bool plan(const WalkEnv& e, Deal& deal) {
+    if (!deal.next(e.p, l, b, h)) return false;
+    q0 = deal.m * BLOCKS * kLatTile;
+    T = latent_seq(e.p, b, row0);
+    n = q0 / kLatTile + 1 + (has_b() ? 1 : 0);
+    tiles = e.tiles(l, b);
+    window = 0;
+    load_window();
+    return true;
+  }
+  __device__ __forceinline__ void publish(ReplayPlan& r) const {
+    r.l = l; r.b = b; r.h = h; r.x0 = q0; r.T = T; r.n = n; r.row0 = row0; r.live = live; r.plain_a = plain_a; r.plain_b = plain_b;
+  }
+  // The other roles'.
+  __device__ __forceinline__ bool next(const WalkEnv& e) {
     first = false;
-    for (;;) {
-      while (live == 0 && window + 32 < n) { window += 32; load_window(p); }
-      if (live != 0) {
-        const int k = __ffs(live) - 1;
-        live &= live - 1;
-        i = window + k;
-        return true;
-      }
-      // the next item
-      for (;;) {
-        if (it >= n_items) return false;
-        const int per = p.L * p.B * p.H, m = n_items / per - 1 - it / per, x = it % per;
-        it += gridDim.x;
-        h = x % p.H; b = x / p.H % p.B; l = x / p.H / p.B;
-        q0 = m * BLOCKS * kLatTile;
-        T = latent_seq(p, b, row0);
-        if (q0 < T) break;
-      }
-      n = q0 / kLatTile + 1 + (has_b() ? 1 : 0);
-      tiles = p.tile_gone ? p.tile_gone + ((int64_t)b * p.G + list_of(p.lists, l, 0, 1)) * (p.gone_cap / kLatTile) : nullptr;
+    while (live == 0 && window + 32 < n) { window += 32; load_window(); }
+    if (live == 0) {
+      const int slot = k & 1;
+      if (!e.wait(&e.ring->full[slot], (k >> 1) & 1)) return false;
+      ++k;
+      const ReplayPlan& r = e.ring->plan[slot];
+      const bool valid = r.valid;
+      l = r.l; b = r.b; h = r.h; q0 = r.x0; T = r.T; n = r.n; row0 = r.row0; live = r.live; plain_a = r.plain_a; plain_b = r.plain_b;
+      __syncwarp();
+      if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(&e.ring->empty[slot]);
+      if (!valid) return false;
+      tiles = e.tiles(l, b);
       window = 0;
-      load_window(p);
       first = true;
+      while (live == 0 && window + 32 < n) { window += 32; load_window(); }        // (a query sees its own key: one tile is live)
     }
+    const int at = __ffs(live) - 1;
+    live &= live - 1;
+    i = window + at;
+    return true;
   }
 };
 
-// Items of 128 keys of one head, the first (which most queries see) first; and for each the tiles of 64 queries from its own first
-// key to the last query that sees one of them.
+// Items of 128 keys of one head; and for each the tiles of 64 queries from its own first key to the last query that sees one of
+// them.
 struct KeyWalk {
   static constexpr int kQ = 64;
-  int it, n_items;
+  int k;
   int l, b, h, j0, T, i, n;     // current query tile, and the one behind the last
   int64_t row0;
   bool first;
 
-  __device__ __forceinline__ KeyWalk(int items) : it(blockIdx.x), n_items(items), i(-1), n(0) {}
+  __device__ __forceinline__ KeyWalk() : k(0), i(-1), n(0) {}
   __device__ __forceinline__ bool last() const { return i == n - 1; }
-  __device__ __forceinline__ bool next(const LatentReplayParams& p) {
+  __device__ __forceinline__ bool plan(const WalkEnv& e, Deal& deal) {
+    if (!deal.next(e.p, l, b, h)) return false;
+    j0 = deal.m * kLatTile;
+    T = latent_seq(e.p, b, row0);
+    const int2* tiles = e.tiles(l, b);
+    const int end = tiles ? min(T, tiles[j0 / kLatTile].y) : T;
+    n = (end + kQ - 1) / kQ;                             // (a key sees to its own query at least: one tile or more)
+    return true;
+  }
+  __device__ __forceinline__ void publish(ReplayPlan& r) const { r.l = l; r.b = b; r.h = h; r.x0 = j0; r.T = T; r.n = n; r.row0 = row0; }
+  __device__ __forceinline__ bool next(const WalkEnv& e) {
     first = false;
     if (++i < n) return true;
-    for (;;) {
-      if (it >= n_items) return false;
-      const int per = p.L * p.B * p.H, x = it % per;
-      j0 = it / per * kLatTile;
-      it += gridDim.x;
-      h = x % p.H; b = x / p.H % p.B; l = x / p.H / p.B;
-      T = latent_seq(p, b, row0);
-      if (j0 >= T) continue;
-      int end = T;
-      if (p.tile_gone) end = min(T, p.tile_gone[((int64_t)b * p.G + list_of(p.lists, l, 0, 1)) * (p.gone_cap / kLatTile) + j0 / kLatTile].y);
-      i = j0 / kQ;
-      n = (end + kQ - 1) / kQ;
-      first = true;
-      if (i < n) return true;                            // (a key sees to its own query at least)
-    }
+    const int slot = k & 1;
+    if (!e.wait(&e.ring->full[slot], (k >> 1) & 1)) return false;
+    ++k;
+    const ReplayPlan& r = e.ring->plan[slot];
+    const bool valid = r.valid;
+    l = r.l; b = r.b; h = r.h; j0 = r.x0; T = r.T; n = r.n; row0 = r.row0;
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(&e.ring->empty[slot]);
+    i = j0 / kQ;
+    first = true;
+    return valid;
   }
 };
+
+// The planner warp: plans item after item and calls load(walk, number of the item) for each; false ends it.
+template <typename Walk, typename Load> __device__ __forceinline__ void run_planner(const WalkEnv& e, int block, bool from_last, Load&& load) {
+  Deal deal(e.p, block, from_last);
+  Walk w;
+  for (int k = 0;; ++k) {
+    const int slot = k & 1;
+    const bool valid = w.plan(e, deal);
+    if (k > 1 && !e.wait(&e.ring->empty[slot], ((k >> 1) - 1) & 1)) return;
+    if ((threadIdx.x & 31) == 0) {
+      if (valid) w.publish(e.ring->plan[slot]);
+      e.ring->plan[slot].valid = valid;
+      ptx::mbar_arrive(&e.ring->full[slot]);
+    }
+    __syncwarp();
+    if (!valid || !load(w, k)) return;
+  }
+}
 
 }  // namespace ngc
