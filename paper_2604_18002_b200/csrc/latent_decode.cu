@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(cta_threads(NH), 1) latent_decode_kernel(const
     if (lane < p.stages) { ptx::mbar_init(&sh.r_full[lane], kTile / p.page); ptx::mbar_init(&sh.r_empty[lane], 1); }
     if (lane == 31) {
       ptx::mbar_init(&sh.s_full[0], 1); ptx::mbar_init(&sh.s_full[1], 1);
-      ptx::mbar_init(&sh.p_full, kSoft * 32);
+      ptx::mbar_init(&sh.p_full, kSoft);
       ptx::mbar_init(&sh.o_done, 1);
       ptx::mbar_init(&sh.q_full, 1); ptx::mbar_init(&sh.q_empty, 1); ptx::mbar_init(&sh.drain, 1);
       sh.abort = 0; sh.u0 = 0; sh.t0 = 0; sh.len0 = 0;
@@ -532,7 +532,8 @@ __global__ void __launch_bounds__(cta_threads(NH), 1) latent_decode_kernel(const
           stmatrix_x4_trans(st_addr + k * 16 * 128, pk[4 * k], pk[4 * k + 1], pk[4 * k + 2], pk[4 * k + 3]);
         ptx::fence_proxy_async();
         umma::fence_before_sync();
-        ptx::mbar_arrive(&sh.p_full);
+        __syncwarp();                                    // (one arrival per warp: they are taken one by one)
+        if (lane == 0) ptx::mbar_arrive(&sh.p_full);
       }
       if (gone) break;
       // ---- end of the part: sums of weights over all tokens, then the rows leave

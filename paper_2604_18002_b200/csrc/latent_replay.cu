@@ -7,62 +7,100 @@ namespace ngc {
 namespace {
 
 // When each token was evicted.  Kept lists of all rounds become one number per token: the sequence length at the first
-// round that fired after the token was there and did not keep it.  (Entries are marked with the last round that names
-// them; a token named by none goes at the first round that it was there for.)  One CTA per (list, sequence).
-__global__ void __launch_bounds__(1024) latent_gone_kernel(LatentReplayParams p) {
-  const int gi = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+// round that fired after the token was there and did not keep it.  (Tokens are marked with the last round that names
+// them; a token named by none goes at the first round that it was there for.)  A CTA takes kSpan tokens of a (sequence, list) and
+// looks through all rounds' lists for them: their entries are read many times over, from L2, but all at once.  Bound by latency:
+// 13 us with one CTA per list.
+constexpr int kSpan = 1024;
+__global__ void __launch_bounds__(kSpan) latent_gone_kernel(LatentReplayParams p) {
+  __shared__ int mark[kSpan];
+  const int gi = blockIdx.y % p.G, b = blockIdx.y / p.G, tid = threadIdx.x, t0 = blockIdx.x * kSpan, t = t0 + tid;
+  ptx::grid_dep_launch();
+  ptx::grid_dep_wait();
   int64_t row0;
   const int T = latent_seq(p, b, row0);
+  if (t0 >= T) return;
   const int64_t list = (int64_t)b * p.G + gi;
-  int32_t* gone = p.gone + list * p.gone_cap;
-  int2* tiles = p.tile_gone + list * (p.gone_cap / kLatTile);
-  const int T_up = (T + kLatTile - 1) / kLatTile * kLatTile;
-  for (int t = tid; t < T_up; t += 1024) gone[t] = -1;
+  mark[tid] = -1;
   __syncthreads();
+  const bool report = blockIdx.x == 0;
   for (int r = 0; r < p.n_rounds; ++r) {
     const int64_t at = ((int64_t)r * p.B + b) * p.G + gi;
-    const int n = p.alive_count[at], fired = min(p.total_before[r * p.B + b], T);
-    if (n < 0 || n > p.kt_max) {
-      // (a list that failed has count -1 from its round on: that its rollout went on all the same is what is reported)
-      if (tid == 0 && p.total_before[r * p.B + b] < T) set_dev_status(p.dev_status, NGC_DEV_BAD_KEPT);
+    const int n = p.alive_count[at], fired = p.total_before[r * p.B + b];
+    if (fired >= T) break;                             // no query of the sequence comes after this round
+    if (n < 0 || n > p.kt_max) {                       // (a list that failed has count -1 from its round on)
+      if (report && tid == 0) set_dev_status(p.dev_status, NGC_DEV_BAD_KEPT);
       continue;
     }
-    if (p.total_before[r * p.B + b] >= T) break;       // no query of the sequence comes after this round
-    for (int i = tid; i < n; i += 1024) {
-      const int t = p.alive_pos[at * p.kt_max + i];
-      if (t < 0 || t >= fired) set_dev_status(p.dev_status, NGC_DEV_BAD_KEPT);
-      else atomicMax(&gone[t], r);
+    for (int i = tid; i < n; i += kSpan) {
+      const int x = p.alive_pos[at * p.kt_max + i];
+      if (x < 0 || x >= fired) {
+        if (report) set_dev_status(p.dev_status, NGC_DEV_BAD_KEPT);
+      } else if (x >= t0 && x < t0 + kSpan) {
+        atomicMax(&mark[x - t0], r);
+      }
     }
   }
   __syncthreads();
-  for (int t = tid; t < T_up; t += 1024) {
-    int r = gone[t] + 1;                               // the first round that does not name it ...
-    while (r < p.n_rounds && p.total_before[r * p.B + b] <= t) ++r;      // ... among those that it was there for
-    gone[t] = t >= T ? 0 : (r < p.n_rounds ? p.total_before[r * p.B + b] : kNeverGone);
-  }
+  int r = mark[tid] + 1;                               // the first round that does not name it ...
+  while (r < p.n_rounds && p.total_before[r * p.B + b] <= t) ++r;        // ... among those that it was there for
+  const int gone = t >= T ? 0 : (r < p.n_rounds ? p.total_before[r * p.B + b] : kNeverGone);
+  if (t < p.gone_cap) p.gone[list * p.gone_cap + t] = gone;
+  int lo = t < T ? gone : kNeverGone, hi = gone;
+  for (int o = 16; o > 0; o >>= 1) { lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o)); hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o)); }
   __syncthreads();
-  for (int i = tid >> 5; i < T_up / kLatTile; i += 32) {
-    int lo = kNeverGone, hi = 0;
-    for (int t = i * kLatTile + (tid & 31); t < min((i + 1) * kLatTile, T); t += 32) { lo = min(lo, gone[t]); hi = max(hi, gone[t]); }
-    for (int o = 16; o > 0; o >>= 1) { lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o)); hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o)); }
-    if ((tid & 31) == 0) tiles[i] = make_int2(lo, hi);
+  int2* warps = reinterpret_cast<int2*>(mark);
+  if ((tid & 31) == 0) warps[tid >> 5] = make_int2(lo, hi);
+  __syncthreads();
+  if (tid < kSpan / kLatTile && t0 + tid * kLatTile < T) {
+    int2 x = warps[4 * tid];
+    for (int k = 1; k < 4; ++k) { x.x = min(x.x, warps[4 * tid + k].x); x.y = max(x.y, warps[4 * tid + k].y); }
+    p.tile_gone[list * (p.gone_cap / kLatTile) + t0 / kLatTile + tid] = x;
   }
 }
 
-__device__ __forceinline__ float at(const __nv_bfloat16* x) { return __bfloat162float(*x); }
-
-// delta = sum over channels of out * grad_out: 16 lanes per (token, head).
-__global__ void __launch_bounds__(256) latent_delta_kernel(LatentReplayParams p) {
-  const int lane = threadIdx.x & 31, h = blockIdx.y, b = blockIdx.z % p.B, l = blockIdx.z / p.B;
-  int64_t row0;
-  const int T = latent_seq(p, b, row0), t = blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (t >= T) return;
-  const int64_t x = (((int64_t)l * p.rows + row0 + t) * p.H + h) * 128;
+// delta = sum over channels of out * grad_out: 16 lanes per (token, head), 8 channels each.  Bound by HBM: both are read once.
+__device__ __forceinline__ float dot8(uint4 a, const float* o) {
+  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
   float s = 0.f;
-  for (int i = 0; i < 4; ++i)
-    s += at(p.go + x + 32 * i + lane) * (p.out_bf16 ? at((const __nv_bfloat16*)p.out + x + 32 * i + lane) : ((const float*)p.out)[x + 32 * i + lane]);
-  s = warp_sum(s);
-  if (lane == 0) p.delta[((int64_t)l * p.H + h) * p.rows + row0 + t] = s;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s += __uint_as_float(w[i] << 16) * o[2 * i] + __uint_as_float(w[i] & 0xffff0000u) * o[2 * i + 1];
+  return s;
+}
+__global__ void __launch_bounds__(256) latent_delta_kernel(LatentReplayParams p) {
+  const int c = 8 * (threadIdx.x & 15), b = blockIdx.y % p.B, l = blockIdx.y / p.B;
+  ptx::grid_dep_launch();
+  ptx::grid_dep_wait();
+  int64_t row0;
+  const int64_t T = latent_seq(p, b, row0), x0 = (int64_t)blockIdx.x * 64 + (threadIdx.x >> 4);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {                        // (token, head) pairs in the order of memory
+    const int64_t x = x0 + 16 * k, t = x / p.H;
+    const int h = (int)(x - t * p.H);
+    float s = 0.f;
+    if (t < T) {
+      const int64_t at = (((int64_t)l * p.rows + row0) * p.H + x) * kLatV + c;
+      const uint4 g = *reinterpret_cast<const uint4*>(p.go + at);
+      float o[8];
+      if (p.out_bf16) {
+        const uint4 v = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)p.out + at);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { o[2 * i] = __uint_as_float(w[i] << 16); o[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+      } else {
+        const float4 v0 = *reinterpret_cast<const float4*>((const float*)p.out + at), v1 = *reinterpret_cast<const float4*>((const float*)p.out + at + 4);
+        o[0] = v0.x; o[1] = v0.y; o[2] = v0.z; o[3] = v0.w; o[4] = v1.x; o[5] = v1.y; o[6] = v1.z; o[7] = v1.w;
+      }
+      s = dot8(g, o);
+    }
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (c == 0 && t < T) p.delta[((int64_t)l * p.H + h) * p.rows + row0 + t] = s;
+  }
+}
+
+cudaError_t launch_gone(const LatentReplayParams& p, cudaStream_t stream) {
+  return launch_pdl(latent_gone_kernel, dim3((p.max_len + kSpan - 1) / kSpan, p.G * p.B), dim3(kSpan), 0, stream, p);
 }
 
 bool valid_seqs(const ngc_latent_seqs* s) {
@@ -96,7 +134,7 @@ int prepare(const ngc_latent_seqs* s, const void* q, const void* kv, const void*
       !aligned16(kv) || !aligned16(k_rope))
     return NGC_ERR_INVALID_ARG;
   if (s->dtype != NGC_BF16 || s->d_nope != kLatNope || s->d_v != kLatV || s->d_rope % 16 != 0 || s->d_rope > 64 ||
-      s->rows * s->L > 0x7fffffffLL || s->max_len > 0x7fffff00 || (int64_t)s->L * s->B > 65535 || s->H > 65535)
+      s->rows * s->L > 0x7fffffffLL || s->max_len > 0x7fffff00 || (int64_t)s->L * s->B > 65535)
     return NGC_ERR_UNSUPPORTED;
   const Space w = space_of(s, lists, n_rounds, backward);
   if (w.all > 0 && (!ws || ws_bytes < w.all || ((uintptr_t)ws & 255))) return NGC_ERR_WORKSPACE;
@@ -131,7 +169,7 @@ extern "C" int ngc_latent_replay_attn(const ngc_latent_seqs* s, const void* q, c
   if (!out || !aligned16(out)) return NGC_ERR_INVALID_ARG;
   if (s->rows == 0 || s->max_len == 0) return NGC_OK;
   p.out = out; p.lse = lse;
-  if (n_rounds > 0) latent_gone_kernel<<<dim3(p.G, p.B), 1024, 0, stream>>>(p);
+  if (n_rounds > 0) NGC_CUDA_TRY(launch_gone(p, stream));
   return launch_latent_fwd(p, stream);
 }
 
@@ -150,7 +188,7 @@ extern "C" int ngc_latent_replay_attn_backward(const ngc_latent_seqs* s, const v
   if (s->rows == 0 || s->max_len == 0) return NGC_OK;
   p.out = const_cast<void*>(out); p.lse = const_cast<float*>(lse); p.go = (const __nv_bfloat16*)grad_out;
   p.gq = (__nv_bfloat16*)grad_q; p.gkv = (__nv_bfloat16*)grad_kv; p.gkr = (__nv_bfloat16*)grad_k_rope;
-  if (n_rounds > 0) latent_gone_kernel<<<dim3(p.G, p.B), 1024, 0, stream>>>(p);
-  latent_delta_kernel<<<dim3((p.max_len + 7) / 8, p.H, p.L * p.B), 256, 0, stream>>>(p);
+  if (n_rounds > 0) NGC_CUDA_TRY(launch_gone(p, stream));
+  NGC_CUDA_TRY(launch_pdl(latent_delta_kernel, dim3((unsigned)(((int64_t)p.max_len * p.H + 63) / 64), p.L * p.B), dim3(256), 0, stream, p));
   return launch_latent_bwd(p, stream);
 }

@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
     if (lane < 2) { ptx::mbar_init(&sh.k_full[lane], 1); ptx::mbar_init(&sh.k_raw[lane], 1); ptx::mbar_init(&sh.k_empty[lane], 1); sh.ring.init(lane); }
     if (lane == 2) {
       ptx::mbar_init(&sh.v_full, 1); ptx::mbar_init(&sh.v_empty, 1); ptx::mbar_init(&sh.q_full, 1); ptx::mbar_init(&sh.q_empty, 1);
-      ptx::mbar_init(&sh.sp_full, 1); ptx::mbar_init(&sh.sp_free, 256); ptx::mbar_init(&sh.z_full, 256); ptx::mbar_init(&sh.z_empty, 1);
+      ptx::mbar_init(&sh.sp_full, 1); ptx::mbar_init(&sh.sp_free, 8); ptx::mbar_init(&sh.z_full, 8); ptx::mbar_init(&sh.z_empty, 1);
       ptx::mbar_init(&sh.dq_done, 1); ptx::mbar_init(&sh.drain, 1);
       sh.abort = 0;
     }
@@ -255,7 +255,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
       for (int k = 0; k < 2; ++k) umma::tmem_ld32(lanes + kP + 64 * half + 32 * k, d[k]);
       umma::tmem_ld_wait();
       umma::fence_before_sync();
-      ptx::mbar_arrive(&sh.sp_free);
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(&sh.sp_free);
       uint32_t pk[32];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -288,7 +289,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
       umma::tmem_st32(lanes + kZ + 32 * half, pk);
       umma::tmem_st_wait();
       umma::fence_before_sync();
-      ptx::mbar_arrive(&sh.z_full);
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(&sh.z_full);
       if (!w.last()) continue;
       if (!wait(&sh.dq_done, n_items_done++ & 1)) break;
       umma::fence_after_sync();
@@ -334,8 +336,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
     if (lane < kStagesK) { ptx::mbar_init(&sh.full[lane], 1); ptx::mbar_init(&sh.raw[lane], 1); ptx::mbar_init(&sh.empty[lane], 1); }
     if (lane < 2) sh.ring.init(lane);
     if (lane == 31) {
-      ptx::mbar_init(&sh.kv_full, 1); ptx::mbar_init(&sh.kv_empty, 1); ptx::mbar_init(&sh.sp_full, 1); ptx::mbar_init(&sh.sp_free, 256);
-      ptx::mbar_init(&sh.z_full, 256); ptx::mbar_init(&sh.z_empty, 1); ptx::mbar_init(&sh.done, 1); ptx::mbar_init(&sh.drain, 1);
+      ptx::mbar_init(&sh.kv_full, 1); ptx::mbar_init(&sh.kv_empty, 1); ptx::mbar_init(&sh.sp_full, 1); ptx::mbar_init(&sh.sp_free, 8);
+      ptx::mbar_init(&sh.z_full, 8); ptx::mbar_init(&sh.z_empty, 1); ptx::mbar_init(&sh.done, 1); ptx::mbar_init(&sh.drain, 1);
       sh.abort = 0;
     }
     ptx::fence_barrier_init();
@@ -508,7 +510,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
       umma::tmem_ld32(lanes + kDp + 32 * half, d);
       umma::tmem_ld_wait();
       umma::fence_before_sync();
-      ptx::mbar_arrive(&sh.sp_free);
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(&sh.sp_free);
       const int c_lo = max(lo - t0, 0);
       const uint32_t width = (uint32_t)max(hi - t0 - c_lo, 0);
       uint32_t pp[16], pz[16];
@@ -529,7 +532,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
       umma::tmem_st8(lanes + kZ + 16 * half + 8, pz + 8);
       umma::tmem_st_wait();
       umma::fence_before_sync();
-      ptx::mbar_arrive(&sh.z_full);
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(&sh.z_full);
       if (!w.last()) continue;
       if (!wait(&sh.done, n_done++ & 1)) break;
       umma::fence_after_sync();

@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
       ptx::mbar_init(&sh.k_full[lane], 1); ptx::mbar_init(&sh.k_empty[lane], 1);
       ptx::mbar_init(&sh.v_full[lane], 1); ptx::mbar_init(&sh.v_raw[lane], 1); ptx::mbar_init(&sh.v_empty[lane], 1);
       ptx::mbar_init(&sh.q_full[lane], 1); ptx::mbar_init(&sh.q_empty[lane], 1);
-      ptx::mbar_init(&sh.s_full[lane], 1); ptx::mbar_init(&sh.p_full[lane], 128); ptx::mbar_init(&sh.o_done[lane], 1);
+      ptx::mbar_init(&sh.s_full[lane], 1); ptx::mbar_init(&sh.p_full[lane], 4); ptx::mbar_init(&sh.o_done[lane], 1);
       sh.ring.init(lane);
     }
     if (lane == 2) { ptx::mbar_init(&sh.drain, 1); sh.abort = 0; }
@@ -340,7 +340,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
       }
       umma::tmem_st_wait();
       umma::fence_before_sync();
-      ptx::mbar_arrive(&sh.p_full[x]);
+      __syncwarp();                                      // (one arrival per warp: they are taken one by one)
+      if (lane == 0) ptx::mbar_arrive(&sh.p_full[x]);
       if (!(x ? w.last() : w.last_a())) continue;
       // ---- the block's last tile: its rows leave
       if (!wait(&sh.o_done[x], n_o & 1)) break;
