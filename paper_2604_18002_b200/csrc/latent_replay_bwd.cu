@@ -65,7 +65,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
   uint8_t* sV = sK + 2 * kQBytes;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (warp == 0) {
-    if (lane < 2) { ptx::mbar_init(&sh.k_full[lane], 1); ptx::mbar_init(&sh.k_raw[lane], 1); ptx::mbar_init(&sh.k_empty[lane], 1); sh.ring.init(lane); }
+    if (lane < 2) { ptx::mbar_init(&sh.k_full[lane], 1); ptx::mbar_init(&sh.k_raw[lane], 1); ptx::mbar_init(&sh.k_empty[lane], 1); }
+    if (lane < kPlans) sh.ring.init(lane);
     if (lane == 2) {
       ptx::mbar_init(&sh.v_full, 1); ptx::mbar_init(&sh.v_empty, 1); ptx::mbar_init(&sh.q_full, 1); ptx::mbar_init(&sh.q_empty, 1);
       ptx::mbar_init(&sh.sp_full, 1); ptx::mbar_init(&sh.sp_free, 8); ptx::mbar_init(&sh.z_full, 8); ptx::mbar_init(&sh.z_empty, 1);
@@ -160,67 +161,58 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
     const uint32_t q_lo = (ptx::smem_u32(sQ) >> 4) | 1u << 16, g_lo = (ptx::smem_u32(sG) >> 4) | 1u << 16, v_lo = (ptx::smem_u32(sV) >> 4) | 1u << 16,
                    k_lo = ptx::smem_u32(sK) >> 4;
     const int steps_r = p.dr / 16;
-    QueryWalk<1> cur, nxt;
-    int n_q = 0;
-    bool ok = true;
-    auto scores = [&](const QueryWalk<1>& w, int t) {
-      if (w.first) ok = ok && wait(&sh.q_full, n_q++ & 1);
-      ok = ok && (t == 0 || wait(&sh.sp_free, (t - 1) & 1)) && wait(&sh.k_full[t & 1], (t >> 1) & 1);
-      if (!ok) return;
-      umma::fence_after_sync();
-      if (umma::elect_one()) {
-        const uint32_t b = (k_lo + (t & 1) * (kQBytes >> 4)) | 1u << 16;
+    // One thread issues everything: scores of the next tile before the sums of this one; at an item's end the other way round, since
+    // the next queries are still on their way.
+    if (umma::elect_one()) {
+      QueryWalk<1> nxt;
+      uint32_t flags = 0;                                // of the two tiles between scores and sums: first, last of an item
+      int n_q = 0, ts = 0, tz = 0;                       // query blocks begun, tiles whose scores, whose sums are issued
+      bool ok = true, more = nxt.next<true>(env);
+      while (ok && (more || tz < ts)) {
+        if (more && (ts == tz || (ts == tz + 1 && !nxt.first))) {
+          if (nxt.first) ok = env.wait_alone(&sh.q_full, n_q++ & 1);
+          ok = ok && env.wait_alone(&sh.k_full[ts & 1], (ts >> 1) & 1) && (ts == 0 || env.wait_alone(&sh.sp_free, (ts - 1) & 1));
+          if (!ok) break;
+          umma::fence_after_sync();
+          const uint32_t b = (k_lo + (ts & 1) * (kQBytes >> 4)) | 1u << 16;
 #pragma unroll
-        for (int k = 0; k < 12; ++k)
-          if (k < 8 || k - 8 < steps_r) {
+          for (int k = 0; k < 12; ++k)
+            if (k < 8 || k - 8 < steps_r) {
+              const uint32_t o = ((k >> 2) * kLatChunk + (k & 3) * 32) >> 4;
+              umma::mma_bf16(tmem + kS, hi | (q_lo + o), hi | (b + o), idesc, k > 0 ? 1u : 0u);
+            }
+          ok = env.wait_alone(&sh.v_full, ts & 1);
+          if (!ok) break;
+          umma::fence_after_sync();
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
             const uint32_t o = ((k >> 2) * kLatChunk + (k & 3) * 32) >> 4;
-            umma::mma_bf16(tmem + kS, hi | (q_lo + o), hi | (b + o), idesc, k > 0 ? 1u : 0u);
+            umma::mma_bf16(tmem + kP, hi | (g_lo + o), hi | (v_lo + o), idesc, k > 0 ? 1u : 0u);
           }
-      }
-      __syncwarp();
-      ok = wait(&sh.v_full, t & 1);
-      if (!ok) return;
-      umma::fence_after_sync();
-      const bool last = w.last();
-      if (umma::elect_one()) {
+          umma::commit(&sh.sp_full);
+          umma::commit(&sh.v_empty);
+          if (nxt.last()) umma::commit(&sh.q_empty);
+          flags |= (uint32_t)((nxt.first ? 1 : 0) | (nxt.last() ? 2 : 0)) << (2 * (ts & 1));
+          ++ts;
+          more = nxt.next<true>(env);
+        } else {
+          ok = env.wait_alone(&sh.z_full, tz & 1);
+          if (!ok) break;
+          umma::fence_after_sync();
+          const bool first = flags >> (2 * (tz & 1)) & 1, last = flags >> (2 * (tz & 1)) & 2;
+          flags &= ~(3u << (2 * (tz & 1)));
+          const uint32_t b = (k_lo + (tz & 1) * (kQBytes >> 4)) | (uint32_t)(kLatChunk >> 4) << 16;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint32_t o = ((k >> 2) * kLatChunk + (k & 3) * 32) >> 4;
-          umma::mma_bf16(tmem + kP, hi | (g_lo + o), hi | (v_lo + o), idesc, k > 0 ? 1u : 0u);
+          for (int k = 0; k < 8; ++k)
+            umma::mma_bf16_a_tmem(tmem + kO, tmem + kZ + 8 * k, hi | (b + ((k * 2048) >> 4)), idesc_q, (!first || k > 0) ? 1u : 0u);
+          umma::commit(&sh.k_empty[tz & 1]);
+          umma::commit(&sh.z_empty);
+          if (last) umma::commit(&sh.dq_done);
+          ++tz;
         }
-        umma::commit(&sh.sp_full);
-        umma::commit(&sh.v_empty);
-        if (last) umma::commit(&sh.q_empty);
       }
-      __syncwarp();
-    };
-    auto sums = [&](const QueryWalk<1>& w, int t) {
-      ok = ok && wait(&sh.z_full, t & 1);
-      if (!ok) return;
-      umma::fence_after_sync();
-      const bool first = w.first, last = w.last();
-      if (umma::elect_one()) {
-        const uint32_t b = (k_lo + (t & 1) * (kQBytes >> 4)) | (uint32_t)(kLatChunk >> 4) << 16;
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          umma::mma_bf16_a_tmem(tmem + kO, tmem + kZ + 8 * k, hi | (b + ((k * 2048) >> 4)), idesc_q, (!first || k > 0) ? 1u : 0u);
-        umma::commit(&sh.k_empty[t & 1]);
-        umma::commit(&sh.z_empty);
-        if (last) umma::commit(&sh.dq_done);
-      }
-      __syncwarp();
-    };
-    bool more = nxt.next(env);
-    if (more) scores(nxt, 0);
-    for (int t = 0; ok && more; ++t) {
-      cur = nxt;
-      more = nxt.next(env);
-      // the next tile's scores first; at an item's end the sums, since the next queries are still on their way
-      if (more && !nxt.first) scores(nxt, t + 1);
-      if (ok) sums(cur, t);
-      if (ok && more && nxt.first) scores(nxt, t + 1);
+      umma::commit(&sh.drain);
     }
-    if (umma::elect_one()) umma::commit(&sh.drain);
     __syncwarp();
     ptx::mbar_wait_bounded(&sh.drain, 0);
     __syncwarp();
@@ -334,7 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (warp == 0) {
     if (lane < kStagesK) { ptx::mbar_init(&sh.full[lane], 1); ptx::mbar_init(&sh.raw[lane], 1); ptx::mbar_init(&sh.empty[lane], 1); }
-    if (lane < 2) sh.ring.init(lane);
+    if (lane < kPlans) sh.ring.init(lane);
     if (lane == 31) {
       ptx::mbar_init(&sh.kv_full, 1); ptx::mbar_init(&sh.kv_empty, 1); ptx::mbar_init(&sh.sp_full, 1); ptx::mbar_init(&sh.sp_free, 8);
       ptx::mbar_init(&sh.z_full, 8); ptx::mbar_init(&sh.z_empty, 1); ptx::mbar_init(&sh.done, 1); ptx::mbar_init(&sh.drain, 1);
@@ -420,38 +412,39 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
     const uint64_t hi = (uint64_t)umma::smem_desc_sw128(0, 0, 1024) & 0xffffffff00000000ull;
     const uint32_t k_lo = (ptx::smem_u32(sK) >> 4) | 1u << 16, v_lo = (ptx::smem_u32(sV) >> 4) | 1u << 16, st_lo = ptx::smem_u32(stage) >> 4;
     const int steps_r = p.dr / 16;
-    KeyWalk cur, nxt;
-    int n_k = 0, s_cur = 0, s_nxt = 0, ph_nxt = 0;
-    bool ok = true;
-    auto scores = [&](const KeyWalk& w, int t) {
-      if (w.first) ok = ok && wait(&sh.kv_full, n_k++ & 1);
-      ok = ok && wait(&sh.full[s_nxt], ph_nxt) && (t == 0 || wait(&sh.sp_free, (t - 1) & 1));
-      if (!ok) return;
-      umma::fence_after_sync();
-      const bool last = w.last();
-      if (umma::elect_one()) {
+    if (umma::elect_one()) {
+    KeyWalk nxt;
+    uint32_t flags = 0;                                  // of the two tiles between scores and sums: first, last of an item
+    int n_k = 0, ts = 0, tz = 0, s_nxt = 0, ph_nxt = 0, s_cur = 0;
+    bool ok = true, more = nxt.next<true>(env);
+    while (ok && (more || tz < ts)) {
+      if (more && (ts == tz || (ts == tz + 1 && !nxt.first))) {
+        if (nxt.first) ok = env.wait_alone(&sh.kv_full, n_k++ & 1);
+        ok = ok && env.wait_alone(&sh.full[s_nxt], ph_nxt) && (ts == 0 || env.wait_alone(&sh.sp_free, (ts - 1) & 1));
+        if (!ok) break;
+        umma::fence_after_sync();
         const uint32_t b = (st_lo + s_nxt * (kStageK >> 4)) | 1u << 16;
 #pragma unroll
         for (int k = 0; k < 12; ++k)
           if (k < 8 || k - 8 < steps_r)
-            umma::mma_bf16(tmem + kS, hi | (k_lo + (((k >> 2) * kLatChunk + (k & 3) * 32) >> 4)), hi | (b + (((k >> 2) * kQChunk + (k & 3) * 32) >> 4)), idesc,
-                           k > 0 ? 1u : 0u);
+            umma::mma_bf16(tmem + kS, hi | (k_lo + (((k >> 2) * kLatChunk + (k & 3) * 32) >> 4)), hi | (b + (((k >> 2) * kQChunk + (k & 3) * 32) >> 4)),
+                           idesc, k > 0 ? 1u : 0u);
 #pragma unroll
         for (int k = 0; k < 8; ++k)
           umma::mma_bf16(tmem + kDp, hi | (v_lo + (((k >> 2) * kLatChunk + (k & 3) * 32) >> 4)),
                          hi | (b + (((3 + (k >> 2)) * kQChunk + (k & 3) * 32) >> 4)), idesc, k > 0 ? 1u : 0u);
         umma::commit(&sh.sp_full);
-        if (last) umma::commit(&sh.kv_empty);
-      }
-      __syncwarp();
-      if (++s_nxt == kStagesK) { s_nxt = 0; ph_nxt ^= 1; }
-    };
-    auto sums = [&](const KeyWalk& w, int t) {
-      ok = ok && wait(&sh.z_full, t & 1);
-      if (!ok) return;
-      umma::fence_after_sync();
-      const bool first = w.first, last = w.last();
-      if (umma::elect_one()) {
+        if (nxt.last()) umma::commit(&sh.kv_empty);
+        if (++s_nxt == kStagesK) { s_nxt = 0; ph_nxt ^= 1; }
+        flags |= (uint32_t)((nxt.first ? 1 : 0) | (nxt.last() ? 2 : 0)) << (2 * (ts & 1));
+        ++ts;
+        more = nxt.next<true>(env);
+      } else {
+        ok = env.wait_alone(&sh.z_full, tz & 1);
+        if (!ok) break;
+        umma::fence_after_sync();
+        const bool first = flags >> (2 * (tz & 1)) & 1, last = flags >> (2 * (tz & 1)) & 2;
+        flags &= ~(3u << (2 * (tz & 1)));
         const uint32_t b = (st_lo + s_cur * (kStageK >> 4)) | (uint32_t)(kQChunk >> 4) << 16;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
@@ -462,20 +455,12 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
         umma::commit(&sh.empty[s_cur]);
         umma::commit(&sh.z_empty);
         if (last) umma::commit(&sh.done);
+        if (++s_cur == kStagesK) s_cur = 0;
+        ++tz;
       }
-      __syncwarp();
-      if (++s_cur == kStagesK) s_cur = 0;
-    };
-    bool more = nxt.next(env);
-    if (more) scores(nxt, 0);
-    for (int t = 0; ok && more; ++t) {
-      cur = nxt;
-      more = nxt.next(env);
-      if (more && !nxt.first) scores(nxt, t + 1);
-      if (ok) sums(cur, t);
-      if (ok && more && nxt.first) scores(nxt, t + 1);
     }
-    if (umma::elect_one()) umma::commit(&sh.drain);
+    umma::commit(&sh.drain);
+    }
     __syncwarp();
     ptx::mbar_wait_bounded(&sh.drain, 0);
     __syncwarp();

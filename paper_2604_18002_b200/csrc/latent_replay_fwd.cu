@@ -54,8 +54,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
       ptx::mbar_init(&sh.v_full[lane], 1); ptx::mbar_init(&sh.v_raw[lane], 1); ptx::mbar_init(&sh.v_empty[lane], 1);
       ptx::mbar_init(&sh.q_full[lane], 1); ptx::mbar_init(&sh.q_empty[lane], 1);
       ptx::mbar_init(&sh.s_full[lane], 1); ptx::mbar_init(&sh.p_full[lane], 4); ptx::mbar_init(&sh.o_done[lane], 1);
-      sh.ring.init(lane);
     }
+    if (lane < kPlans) sh.ring.init(lane);
     if (lane == 2) { ptx::mbar_init(&sh.drain, 1); sh.abort = 0; }
     ptx::fence_barrier_init();
   } else if (warp == kProducerWarp && lane == 0) {
@@ -163,79 +163,76 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
     const uint64_t hi = (uint64_t)umma::smem_desc_sw128(0, 0, 1024) & 0xffffffff00000000ull;
     const uint32_t q_lo = (ptx::smem_u32(sQ) >> 4) | 1u << 16, ring_lo = ptx::smem_u32(ring) >> 4;
     const int steps_r = p.dr / 16;
-    QueryWalk<2> cur, nxt;
-    int n_q[2] = {0, 0}, n_p[2] = {0, 0};                // query blocks begun, P tiles used
-    bool ok = true;
-    // scores of block x for tile t (walk w); commits what that makes free
-    auto scores = [&](const QueryWalk<2>& w, int t, int x) {
-      if (w.first) {
-        ok = ok && wait(&sh.q_full[x], n_q[x] & 1);
-        ++n_q[x];
-      }
-      ok = ok && wait(&sh.k_full[t & 1], (t >> 1) & 1);
-      if (!ok) return;
-      umma::fence_after_sync();
-      const bool last = x ? w.last() : w.last_a(), k_done = x || !w.has_b() ;
-      const uint32_t k0 = ring_lo + ((5 * t) & 7) * (kLatChunk >> 4), k1 = ring_lo + ((5 * t + 1) & 7) * (kLatChunk >> 4),
-                     k2 = ring_lo + ((5 * t + 2) & 7) * (kLatChunk >> 4);
-      if (umma::elect_one()) {
-        const uint32_t a = q_lo + x * (kQBlock >> 4), d = tmem + 128u * x;
+    // One thread does it all: what a whole warp takes to wait, elect and meet again adds up (the gradient's kernel for keys: 723
+    // -> 671 us for rollouts of 8192 tokens).
+    if (umma::elect_one()) {
+    struct { bool a, b, first, last_a, last_b; } cur = {false, false, false, false, false};
+    QueryWalk<2> nxt;
+    uint32_t q_phase = 0, p_phase = 0;                   // bit x: parity of block x's next queries, next weights
+    bool ok = true, have = false, more = nxt.next<true>(env);
+    for (int t = -1; ok && (have || more); ++t) {
+#pragma unroll 1
+      for (int x = 0; x < 2; ++x) {
+        if (have && (x ? cur.b : cur.a)) {
+          // O += P V of block x for tile t
+          ok = env.wait_alone(&sh.v_full[t & 1], (t >> 1) & 1) && env.wait_alone(&sh.p_full[x], (p_phase >> x) & 1);
+          if (!ok) break;
+          p_phase ^= 1u << x;
+          umma::fence_after_sync();
+          const int s0 = (5 * t + 3) & 7;
+          const uint32_t pa = tmem + 128u * x, d = tmem + 256u + 128u * x, v0 = ring_lo + s0 * (kLatChunk >> 4);
+          {
+            if (s0 < 7) {
+              const uint32_t b = v0 | (uint32_t)(kLatChunk >> 4) << 16;
 #pragma unroll
-        for (int c = 0; c < 3; ++c) {
-          const uint32_t b = (c == 0 ? k0 : c == 1 ? k1 : k2) | 1u << 16;
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (c < 2 || k < steps_r) umma::mma_bf16(d, hi | (a + ((c * kLatChunk + k * 32) >> 4)), hi | (b + 2 * k), idesc_s, (c > 0 || k > 0) ? 1u : 0u);
-        }
-        umma::commit(&sh.s_full[x]);
-        if (last) umma::commit(&sh.q_empty[x]);
-        if (k_done) umma::commit(&sh.k_empty[t & 1]);
-      }
-      __syncwarp();
-    };
-    // O += P V of block x for tile t
-    auto sums = [&](const QueryWalk<2>& w, int t, int x) {
-      ok = ok && wait(&sh.v_full[t & 1], (t >> 1) & 1) && wait(&sh.p_full[x], n_p[x] & 1);
-      if (!ok) return;
-      ++n_p[x];
-      umma::fence_after_sync();
-      const int s0 = (5 * t + 3) & 7;
-      const bool last = x ? w.last() : w.last_a(), first = w.first, v_done = x || !w.has_b();
-      if (umma::elect_one()) {
-        const uint32_t pa = tmem + 128u * x, d = tmem + 256u + 128u * x;
-        const uint32_t v0 = ring_lo + s0 * (kLatChunk >> 4);
-        if (s0 < 7) {
-          const uint32_t b = v0 | (uint32_t)(kLatChunk >> 4) << 16;
-#pragma unroll
-          for (int k = 0; k < 8; ++k) umma::mma_bf16_a_tmem(d, pa + 8 * k, hi | (b + ((k * 2048) >> 4)), idesc_o, (!first || k > 0) ? 1u : 0u);
-        } else {                                         // the two chunks lie at the ring's two ends
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            umma::mma_bf16_a_tmem(d, pa + 8 * k, hi | ((v0 | 1u << 16) + ((k * 2048) >> 4)), idesc_half, (!first || k > 0) ? 1u : 0u);
-            umma::mma_bf16_a_tmem(d + 64, pa + 8 * k, hi | ((ring_lo | 1u << 16) + ((k * 2048) >> 4)), idesc_half, (!first || k > 0) ? 1u : 0u);
+              for (int k = 0; k < 8; ++k) umma::mma_bf16_a_tmem(d, pa + 8 * k, hi | (b + ((k * 2048) >> 4)), idesc_o, (!cur.first || k > 0) ? 1u : 0u);
+            } else {                                     // the two chunks lie at the ring's two ends
+#pragma unroll 1
+              for (int k = 0; k < 8; ++k) {
+                umma::mma_bf16_a_tmem(d, pa + 8 * k, hi | ((v0 | 1u << 16) + ((k * 2048) >> 4)), idesc_half, (!cur.first || k > 0) ? 1u : 0u);
+                umma::mma_bf16_a_tmem(d + 64, pa + 8 * k, hi | ((ring_lo | 1u << 16) + ((k * 2048) >> 4)), idesc_half, (!cur.first || k > 0) ? 1u : 0u);
+              }
+            }
+            if (x ? cur.last_b : cur.last_a) umma::commit(&sh.o_done[x]);
+            if (x || !cur.b) umma::commit(&sh.v_empty[t & 1]);
           }
         }
-        if (last) umma::commit(&sh.o_done[x]);
-        if (v_done) umma::commit(&sh.v_empty[t & 1]);
+        if (more && (x ? nxt.has_b() : nxt.for_a())) {
+          // scores of block x for tile t + 1
+          const int tn = t + 1;
+          if (nxt.first) {
+            ok = env.wait_alone(&sh.q_full[x], (q_phase >> x) & 1);
+            q_phase ^= 1u << x;
+          }
+          ok = ok && env.wait_alone(&sh.k_full[tn & 1], (tn >> 1) & 1);
+          if (!ok) break;
+          umma::fence_after_sync();
+          const bool last = x ? nxt.last() : nxt.last_a(), k_done = x || !nxt.has_b();
+          const uint32_t k0 = ring_lo + ((5 * tn) & 7) * (kLatChunk >> 4), k1 = ring_lo + ((5 * tn + 1) & 7) * (kLatChunk >> 4),
+                         k2 = ring_lo + ((5 * tn + 2) & 7) * (kLatChunk >> 4);
+          const uint32_t a = q_lo + x * (kQBlock >> 4), d = tmem + 128u * x;
+          {
+#pragma unroll
+            for (int c = 0; c < 3; ++c) {
+              const uint32_t b = (c == 0 ? k0 : c == 1 ? k1 : k2) | 1u << 16;
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                if (c < 2 || k < steps_r) umma::mma_bf16(d, hi | (a + ((c * kLatChunk + k * 32) >> 4)), hi | (b + 2 * k), idesc_s, (c > 0 || k > 0) ? 1u : 0u);
+            }
+            umma::commit(&sh.s_full[x]);
+            if (last) umma::commit(&sh.q_empty[x]);
+            if (k_done) umma::commit(&sh.k_empty[tn & 1]);
+          }
+        }
       }
-      __syncwarp();
-    };
-    bool more = nxt.next(env);
-    int t = 0;
-    if (more) {
-      if (nxt.for_a()) scores(nxt, 0, 0);
-      if (ok && nxt.has_b()) scores(nxt, 0, 1);
+      have = more;
+      if (more) {
+        cur.a = nxt.for_a(); cur.b = nxt.has_b(); cur.first = nxt.first; cur.last_a = nxt.last_a(); cur.last_b = nxt.last();
+        more = nxt.next<true>(env);
+      }
     }
-    while (ok && more) {
-      cur = nxt;
-      more = nxt.next(env);
-      if (cur.for_a()) sums(cur, t, 0);
-      if (ok && more && nxt.for_a()) scores(nxt, t + 1, 0);
-      if (ok && cur.has_b()) sums(cur, t, 1);
-      if (ok && more && nxt.has_b()) scores(nxt, t + 1, 1);
-      ++t;
+    umma::commit(&sh.drain);                             // everything issued has completed before tensor memory is released
     }
-    if (umma::elect_one()) umma::commit(&sh.drain);      // everything issued has completed before tensor memory is released
     __syncwarp();
     ptx::mbar_wait_bounded(&sh.drain, 0);
     __syncwarp();

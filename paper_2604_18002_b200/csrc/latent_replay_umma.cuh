@@ -73,16 +73,17 @@ struct Deal {
   }
 };
 
-// An item's description, made by the planner warp (which also loads what stays in shared memory throughout the item) up to two items
+// An item's description, made by the planner warp (which also loads what stays in shared memory throughout the item) some items
 // ahead, so that no other role meets the chain of reads behind it.
+constexpr int kPlans = 4, kPlanWindows = 8;
 struct ReplayPlan {
   int valid, l, b, h, x0, T, n;                // first token of the item's block; query walks: key tiles, key walks: query tiles
-  uint32_t live, plain_a, plain_b;             // query walks: see there, of the first 32 tiles
+  uint32_t live[kPlanWindows], plain_a[kPlanWindows], plain_b[kPlanWindows];     // query walks: see there, of the first 256 tiles
   int64_t row0;                                // first row of the sequence, within a layer
 };
 struct PlanRing {
-  uint64_t full[2], empty[2];
-  ReplayPlan plan[2];
+  uint64_t full[kPlans], empty[kPlans];
+  ReplayPlan plan[kPlans];
   static constexpr int kReaders = 11;          // producer, mender, MMA, eight softmax warps
   __device__ __forceinline__ void init(int i) { ptx::mbar_init(&full[i], 1); ptx::mbar_init(&empty[i], kReaders); }
 };
@@ -92,6 +93,21 @@ struct WalkEnv {
   PlanRing* ring;
   int* abort;
   __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) const { return umma::warp_wait(bar, parity, abort, p.dev_status); }
+  __device__ __forceinline__ bool wait_alone(uint64_t* bar, uint32_t parity) const { return umma::wait_or_abort(bar, parity, abort, p.dev_status); }
+  // Plan of item k: wait for it, and give it back (by a warp, or by one thread that stands for its warp).
+  template <bool ALONE> __device__ __forceinline__ bool obtain(int k) const {
+    uint64_t* bar = &ring->full[k % kPlans];
+    return ALONE ? wait_alone(bar, (k / kPlans) & 1) : wait(bar, (k / kPlans) & 1);
+  }
+  template <bool ALONE> __device__ __forceinline__ void release(int k) const {
+    if (!ALONE) __syncwarp();
+    if (ALONE || (threadIdx.x & 31) == 0) ptx::mbar_arrive(&ring->empty[k % kPlans]);
+  }
+  // For both of two barriers: half of the lanes look at one, half at the other.
+  __device__ __forceinline__ bool wait(uint64_t* bar0, uint32_t parity0, uint64_t* bar1, uint32_t parity1) const {
+    const bool odd = threadIdx.x & 1;
+    return umma::warp_wait(odd ? bar1 : bar0, odd ? parity1 : parity0, abort, p.dev_status);
+  }
   __device__ __forceinline__ const int2* tiles(int l, int b) const {
     return p.tile_gone ? p.tile_gone + ((int64_t)b * p.G + list_of(p.lists, l, 0, 1)) * (p.gone_cap / kLatTile) : nullptr;
   }
@@ -112,13 +128,24 @@ template <int BLOCKS> struct QueryWalk {
   __device__ __forceinline__ bool for_a() const { return i * kLatTile <= q0; }
   __device__ __forceinline__ bool last_a() const { return i * kLatTile == q0; }
   __device__ __forceinline__ bool last() const { return i == n - 1; }
-  __device__ __forceinline__ void load_window() {
-    const int t = window + (threadIdx.x & 31);
-    int2 g = make_int2(kNeverGone, kNeverGone);
-    if (tiles && t < n) g = tiles[t];
-    live = __ballot_sync(0xffffffffu, t < n && g.y > q0);
-    plain_a = __ballot_sync(0xffffffffu, g.x > q0 + kLatTile - 1);
-    plain_b = __ballot_sync(0xffffffffu, g.x > q0 + 2 * kLatTile - 1);
+  // Masks of the window: by all lanes, or (ALONE) by one thread.
+  template <bool ALONE> __device__ __forceinline__ void load_window() {
+    if (ALONE) {
+      live = plain_a = plain_b = 0;
+      for (int t = window; t < min(window + 32, n); ++t) {
+        const int2 g = tiles ? tiles[t] : make_int2(kNeverGone, kNeverGone);
+        live |= (uint32_t)(g.y > q0) << (t - window);
+        plain_a |= (uint32_t)(g.x > q0 + kLatTile - 1) << (t - window);
+        plain_b |= (uint32_t)(g.x > q0 + 2 * kLatTile - 1) << (t - window);
+      }
+    } else {
+      const int t = window + (threadIdx.x & 31);
+      int2 g = make_int2(kNeverGone, kNeverGone);
+      if (tiles && t < n) g = tiles[t];
+      live = __ballot_sync(0xffffffffu, t < n && g.y > q0);
+      plain_a = __ballot_sync(0xffffffffu, g.x > q0 + kLatTile - 1);
+      plain_b = __ballot_sync(0xffffffffu, g.x > q0 + 2 * kLatTile - 1);
+    }
   }
   // The planner's part.
   __device__ __forceinline__ bool plan(const WalkEnv& e, Deal& deal) {
@@ -127,36 +154,48 @@ template <int BLOCKS> struct QueryWalk {
     T = latent_seq(e.p, b, row0);
     n = q0 / kLatTile + 1 + (has_b() ? 1 : 0);
     tiles = e.tiles(l, b);
-    window = 0;
-    load_window();
     return true;
   }
-  __device__ __forceinline__ void publish(ReplayPlan& r) const {
-    r.l = l; r.b = b; r.h = h; r.x0 = q0; r.T = T; r.n = n; r.row0 = row0; r.live = live; r.plain_a = plain_a; r.plain_b = plain_b;
+  __device__ __forceinline__ void publish(ReplayPlan& r) {
+    const bool one = (threadIdx.x & 31) == 0;
+    if (one) { r.l = l; r.b = b; r.h = h; r.x0 = q0; r.T = T; r.n = n; r.row0 = row0; }
+    for (int w = 0; w < kPlanWindows && 32 * w < n; ++w) {
+      window = 32 * w;
+      load_window<false>();
+      if (one) { r.live[w] = live; r.plain_a[w] = plain_a; r.plain_b[w] = plain_b; }
+    }
   }
-  // The other roles'.
-  __device__ __forceinline__ bool next(const WalkEnv& e) {
+  // The other roles', by all lanes of a warp or by one thread alone.  (An item's plan is held until its last tile has been passed.)
+  template <bool ALONE = false> __device__ __forceinline__ bool next(const WalkEnv& e) {
     first = false;
-    while (live == 0 && window + 32 < n) { window += 32; load_window(); }
+    if (live == 0) advance<ALONE>(e);
     if (live == 0) {
-      const int slot = k & 1;
-      if (!e.wait(&e.ring->full[slot], (k >> 1) & 1)) return false;
+      if (k > 0) e.release<ALONE>(k - 1);
+      if (!e.obtain<ALONE>(k)) return false;
+      const ReplayPlan& r = e.ring->plan[k % kPlans];
       ++k;
-      const ReplayPlan& r = e.ring->plan[slot];
-      const bool valid = r.valid;
-      l = r.l; b = r.b; h = r.h; q0 = r.x0; T = r.T; n = r.n; row0 = r.row0; live = r.live; plain_a = r.plain_a; plain_b = r.plain_b;
-      __syncwarp();
-      if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(&e.ring->empty[slot]);
-      if (!valid) return false;
+      if (!r.valid) return false;
+      l = r.l; b = r.b; h = r.h; q0 = r.x0; T = r.T; n = r.n; row0 = r.row0; live = r.live[0]; plain_a = r.plain_a[0]; plain_b = r.plain_b[0];
       tiles = e.tiles(l, b);
       window = 0;
       first = true;
-      while (live == 0 && window + 32 < n) { window += 32; load_window(); }        // (a query sees its own key: one tile is live)
+      if (live == 0) advance<ALONE>(e);                  // (a query sees its own key: one tile is live)
     }
     const int at = __ffs(live) - 1;
     live &= live - 1;
     i = window + at;
     return true;
+  }
+  template <bool ALONE> __device__ __forceinline__ void advance(const WalkEnv& e) {
+    while (live == 0 && window + 32 < n) {
+      window += 32;
+      if (window < 32 * kPlanWindows) {
+        const ReplayPlan& r = e.ring->plan[(k - 1) % kPlans];
+        live = r.live[window / 32]; plain_a = r.plain_a[window / 32]; plain_b = r.plain_b[window / 32];
+      } else {
+        load_window<ALONE>();
+      }
+    }
   }
 };
 
@@ -180,21 +219,21 @@ struct KeyWalk {
     n = (end + kQ - 1) / kQ;                             // (a key sees to its own query at least: one tile or more)
     return true;
   }
-  __device__ __forceinline__ void publish(ReplayPlan& r) const { r.l = l; r.b = b; r.h = h; r.x0 = j0; r.T = T; r.n = n; r.row0 = row0; }
-  __device__ __forceinline__ bool next(const WalkEnv& e) {
+  __device__ __forceinline__ void publish(ReplayPlan& r) const {
+    if ((threadIdx.x & 31) == 0) { r.l = l; r.b = b; r.h = h; r.x0 = j0; r.T = T; r.n = n; r.row0 = row0; }
+  }
+  template <bool ALONE = false> __device__ __forceinline__ bool next(const WalkEnv& e) {
     first = false;
     if (++i < n) return true;
-    const int slot = k & 1;
-    if (!e.wait(&e.ring->full[slot], (k >> 1) & 1)) return false;
+    if (k > 0) e.release<ALONE>(k - 1);
+    if (!e.obtain<ALONE>(k)) return false;
+    const ReplayPlan& r = e.ring->plan[k % kPlans];
     ++k;
-    const ReplayPlan& r = e.ring->plan[slot];
-    const bool valid = r.valid;
+    if (!r.valid) return false;
     l = r.l; b = r.b; h = r.h; j0 = r.x0; T = r.T; n = r.n; row0 = r.row0;
-    __syncwarp();
-    if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(&e.ring->empty[slot]);
     i = j0 / kQ;
     first = true;
-    return valid;
+    return true;
   }
 };
 
@@ -203,11 +242,11 @@ template <typename Walk, typename Load> __device__ __forceinline__ void run_plan
   Deal deal(e.p, block, from_last);
   Walk w;
   for (int k = 0;; ++k) {
-    const int slot = k & 1;
+    const int slot = k % kPlans;
     const bool valid = w.plan(e, deal);
-    if (k > 1 && !e.wait(&e.ring->empty[slot], ((k >> 1) - 1) & 1)) return;
+    if (k >= kPlans && !e.wait(&e.ring->empty[slot], (k / kPlans - 1) & 1)) return;
+    if (valid) w.publish(e.ring->plan[slot]);
     if ((threadIdx.x & 31) == 0) {
-      if (valid) w.publish(e.ring->plan[slot]);
       e.ring->plan[slot].valid = valid;
       ptx::mbar_arrive(&e.ring->full[slot]);
     }
