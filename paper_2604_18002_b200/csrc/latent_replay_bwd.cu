@@ -161,18 +161,18 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
     const uint32_t q_lo = (ptx::smem_u32(sQ) >> 4) | 1u << 16, g_lo = (ptx::smem_u32(sG) >> 4) | 1u << 16, v_lo = (ptx::smem_u32(sV) >> 4) | 1u << 16,
                    k_lo = ptx::smem_u32(sK) >> 4;
     const int steps_r = p.dr / 16;
-    // One thread issues everything: scores of the next tile before the sums of this one; at an item's end the other way round, since
-    // the next queries are still on their way.
+    // One thread issues everything, whatever is ready: S of the next tile, its dP, the sums of this one.  (In a fixed order sums waited
+    // for scores whose keys waited for the sums to make room: XX us.)
     if (umma::elect_one()) {
       QueryWalk<1> nxt;
+      Patience patience;
       uint32_t flags = 0;                                // of the two tiles between scores and sums: first, last of an item
       int n_q = 0, ts = 0, tz = 0;                       // query blocks begun, tiles whose scores, whose sums are issued
-      bool ok = true, more = nxt.next<true>(env);
-      while (ok && (more || tz < ts)) {
-        if (more && (ts == tz || (ts == tz + 1 && !nxt.first))) {
-          if (nxt.first) ok = env.wait_alone(&sh.q_full, n_q++ & 1);
-          ok = ok && env.wait_alone(&sh.k_full[ts & 1], (ts >> 1) & 1) && (ts == 0 || env.wait_alone(&sh.sp_free, (ts - 1) & 1));
-          if (!ok) break;
+      bool s_done = false, more = nxt.next<true>(env);   // s_done: S of tile ts is issued, dP is not
+      while (more || tz < ts) {
+        bool moved = false;
+        if (more && !s_done && ts <= tz + 1 && ptx::mbar_test_wait(&sh.k_full[ts & 1], (ts >> 1) & 1) &&
+            (ts == 0 || ptx::mbar_test_wait(&sh.sp_free, (ts - 1) & 1)) && (!nxt.first || ptx::mbar_test_wait(&sh.q_full, n_q & 1))) {
           umma::fence_after_sync();
           const uint32_t b = (k_lo + (ts & 1) * (kQBytes >> 4)) | 1u << 16;
 #pragma unroll
@@ -181,8 +181,10 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
               const uint32_t o = ((k >> 2) * kLatChunk + (k & 3) * 32) >> 4;
               umma::mma_bf16(tmem + kS, hi | (q_lo + o), hi | (b + o), idesc, k > 0 ? 1u : 0u);
             }
-          ok = env.wait_alone(&sh.v_full, ts & 1);
-          if (!ok) break;
+          n_q += nxt.first;
+          s_done = moved = true;
+        }
+        if (s_done && ptx::mbar_test_wait(&sh.v_full, ts & 1)) {
           umma::fence_after_sync();
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
@@ -194,10 +196,11 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
           if (nxt.last()) umma::commit(&sh.q_empty);
           flags |= (uint32_t)((nxt.first ? 1 : 0) | (nxt.last() ? 2 : 0)) << (2 * (ts & 1));
           ++ts;
+          s_done = false;
+          moved = true;
           more = nxt.next<true>(env);
-        } else {
-          ok = env.wait_alone(&sh.z_full, tz & 1);
-          if (!ok) break;
+        }
+        if (tz < ts && ptx::mbar_test_wait(&sh.z_full, tz & 1)) {
           umma::fence_after_sync();
           const bool first = flags >> (2 * (tz & 1)) & 1, last = flags >> (2 * (tz & 1)) & 2;
           flags &= ~(3u << (2 * (tz & 1)));
@@ -209,7 +212,10 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
           umma::commit(&sh.z_empty);
           if (last) umma::commit(&sh.dq_done);
           ++tz;
+          moved = true;
         }
+        if (moved) patience.moved();
+        else if (!patience.more(&sh.abort, p.dev_status)) break;
       }
       umma::commit(&sh.drain);
     }
@@ -413,53 +419,57 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
     const uint32_t k_lo = (ptx::smem_u32(sK) >> 4) | 1u << 16, v_lo = (ptx::smem_u32(sV) >> 4) | 1u << 16, st_lo = ptx::smem_u32(stage) >> 4;
     const int steps_r = p.dr / 16;
     if (umma::elect_one()) {
-    KeyWalk nxt;
-    uint32_t flags = 0;                                  // of the two tiles between scores and sums: first, last of an item
-    int n_k = 0, ts = 0, tz = 0, s_nxt = 0, ph_nxt = 0, s_cur = 0;
-    bool ok = true, more = nxt.next<true>(env);
-    while (ok && (more || tz < ts)) {
-      if (more && (ts == tz || (ts == tz + 1 && !nxt.first))) {
-        if (nxt.first) ok = env.wait_alone(&sh.kv_full, n_k++ & 1);
-        ok = ok && env.wait_alone(&sh.full[s_nxt], ph_nxt) && (ts == 0 || env.wait_alone(&sh.sp_free, (ts - 1) & 1));
-        if (!ok) break;
-        umma::fence_after_sync();
-        const uint32_t b = (st_lo + s_nxt * (kStageK >> 4)) | 1u << 16;
+      KeyWalk nxt;
+      Patience patience;
+      uint32_t flags = 0;                                // of the two tiles between scores and sums: first, last of an item
+      int n_k = 0, ts = 0, tz = 0, s_nxt = 0, ph_nxt = 0, s_cur = 0;
+      bool more = nxt.next<true>(env);
+      while (more || tz < ts) {
+        bool moved = false;
+        if (more && ts <= tz + 1 && ptx::mbar_test_wait(&sh.full[s_nxt], ph_nxt) && (ts == 0 || ptx::mbar_test_wait(&sh.sp_free, (ts - 1) & 1)) &&
+            (!nxt.first || ptx::mbar_test_wait(&sh.kv_full, n_k & 1))) {
+          umma::fence_after_sync();
+          const uint32_t b = (st_lo + s_nxt * (kStageK >> 4)) | 1u << 16;
 #pragma unroll
-        for (int k = 0; k < 12; ++k)
-          if (k < 8 || k - 8 < steps_r)
-            umma::mma_bf16(tmem + kS, hi | (k_lo + (((k >> 2) * kLatChunk + (k & 3) * 32) >> 4)), hi | (b + (((k >> 2) * kQChunk + (k & 3) * 32) >> 4)),
-                           idesc, k > 0 ? 1u : 0u);
+          for (int k = 0; k < 12; ++k)
+            if (k < 8 || k - 8 < steps_r)
+              umma::mma_bf16(tmem + kS, hi | (k_lo + (((k >> 2) * kLatChunk + (k & 3) * 32) >> 4)), hi | (b + (((k >> 2) * kQChunk + (k & 3) * 32) >> 4)),
+                             idesc, k > 0 ? 1u : 0u);
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          umma::mma_bf16(tmem + kDp, hi | (v_lo + (((k >> 2) * kLatChunk + (k & 3) * 32) >> 4)),
-                         hi | (b + (((3 + (k >> 2)) * kQChunk + (k & 3) * 32) >> 4)), idesc, k > 0 ? 1u : 0u);
-        umma::commit(&sh.sp_full);
-        if (nxt.last()) umma::commit(&sh.kv_empty);
-        if (++s_nxt == kStagesK) { s_nxt = 0; ph_nxt ^= 1; }
-        flags |= (uint32_t)((nxt.first ? 1 : 0) | (nxt.last() ? 2 : 0)) << (2 * (ts & 1));
-        ++ts;
-        more = nxt.next<true>(env);
-      } else {
-        ok = env.wait_alone(&sh.z_full, tz & 1);
-        if (!ok) break;
-        umma::fence_after_sync();
-        const bool first = flags >> (2 * (tz & 1)) & 1, last = flags >> (2 * (tz & 1)) & 2;
-        flags &= ~(3u << (2 * (tz & 1)));
-        const uint32_t b = (st_lo + s_cur * (kStageK >> 4)) | (uint32_t)(kQChunk >> 4) << 16;
+          for (int k = 0; k < 8; ++k)
+            umma::mma_bf16(tmem + kDp, hi | (v_lo + (((k >> 2) * kLatChunk + (k & 3) * 32) >> 4)),
+                           hi | (b + (((3 + (k >> 2)) * kQChunk + (k & 3) * 32) >> 4)), idesc, k > 0 ? 1u : 0u);
+          umma::commit(&sh.sp_full);
+          if (nxt.last()) umma::commit(&sh.kv_empty);
+          n_k += nxt.first;
+          if (++s_nxt == kStagesK) { s_nxt = 0; ph_nxt ^= 1; }
+          flags |= (uint32_t)((nxt.first ? 1 : 0) | (nxt.last() ? 2 : 0)) << (2 * (ts & 1));
+          ++ts;
+          moved = true;
+          more = nxt.next<true>(env);
+        }
+        if (tz < ts && ptx::mbar_test_wait(&sh.z_full, tz & 1)) {
+          umma::fence_after_sync();
+          const bool first = flags >> (2 * (tz & 1)) & 1, last = flags >> (2 * (tz & 1)) & 2;
+          flags &= ~(3u << (2 * (tz & 1)));
+          const uint32_t b = (st_lo + s_cur * (kStageK >> 4)) | (uint32_t)(kQChunk >> 4) << 16;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          umma::mma_bf16_a_tmem(tmem + kDv, tmem + kP + 8 * k, hi | (b + ((3 * kQChunk + k * 2048) >> 4)), idesc_v, (!first || k > 0) ? 1u : 0u);
+          for (int k = 0; k < 4; ++k)
+            umma::mma_bf16_a_tmem(tmem + kDv, tmem + kP + 8 * k, hi | (b + ((3 * kQChunk + k * 2048) >> 4)), idesc_v, (!first || k > 0) ? 1u : 0u);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          umma::mma_bf16_a_tmem(tmem + kDk, tmem + kZ + 8 * k, hi | (b + ((k * 2048) >> 4)), idesc_k, (!first || k > 0) ? 1u : 0u);
-        umma::commit(&sh.empty[s_cur]);
-        umma::commit(&sh.z_empty);
-        if (last) umma::commit(&sh.done);
-        if (++s_cur == kStagesK) s_cur = 0;
-        ++tz;
+          for (int k = 0; k < 4; ++k)
+            umma::mma_bf16_a_tmem(tmem + kDk, tmem + kZ + 8 * k, hi | (b + ((k * 2048) >> 4)), idesc_k, (!first || k > 0) ? 1u : 0u);
+          umma::commit(&sh.empty[s_cur]);
+          umma::commit(&sh.z_empty);
+          if (last) umma::commit(&sh.done);
+          if (++s_cur == kStagesK) s_cur = 0;
+          ++tz;
+          moved = true;
+        }
+        if (moved) patience.moved();
+        else if (!patience.more(&sh.abort, p.dev_status)) break;
       }
-    }
-    umma::commit(&sh.drain);
+      umma::commit(&sh.drain);
     }
     __syncwarp();
     ptx::mbar_wait_bounded(&sh.drain, 0);
