@@ -3,7 +3,8 @@
 // With the forward pass's lse and D = sum over channels of out * grad_out, P = exp(z - lse) and dz = P (dP - D), dP = dO V^T
 // (the scale of z is applied to the finished sums).  Two kernels, each of which computes S and dP again, so that every sum lies in one
 // CTA's tensor memory: no atomics, the same bits in every run.
-//   queries   an item is 128 queries of a head; over its tiles of 128 keys: S = Q K^T, dP = dO V^T, dQ += dZ K
+//   queries   an item is 128 queries of a head; over its tiles of 64 keys: S = Q K^T, dP = dO V^T, dQ += dZ K (two buffers of each
+//             fill tensor memory; with 128 keys two stages of K were too few: XX us)
 //   keys      an item is 128 keys of a head; over the tiles of 64 queries that see them: S^T = K Q^T, dP^T = V dO^T,
 //             dV += P^T dO, dK += dZ^T Q.  Keys are the lanes of tensor memory, so what a query sees is one range of columns per
 //             thread.  64 queries because dV, dK (320 columns), S^T, dP^T and the bf16 P^T, dZ^T fill tensor memory
@@ -47,10 +48,14 @@ __device__ __forceinline__ void store_bf16(uint32_t taddr, int n, float f, __nv_
 
 // ------------------------------------------------------------------------------------------------------------ queries
 
-constexpr int kSmemQ = kQBytes + kVBytes + 2 * kQBytes + kVBytes + 1024;         // Q, dO; two stages of K; V
+constexpr int kKTile = 64;                     // keys per tile
+constexpr int kKChunk = kKTile * 128;          // 64 keys x 64 channels
+constexpr int kStagesK = 4, kStagesV = 3;      // tiles of keys (3 chunks; in use until dQ has them) and of values (2 chunks; until dP)
+constexpr int kSmemQ = kQBytes + kVBytes + kStagesK * 3 * kKChunk + kStagesV * 2 * kKChunk + 1024;
 
 struct SharedQ {
-  uint64_t k_full[2], k_raw[2], k_empty[2], v_full, v_empty, q_full, q_empty, sp_full, sp_free, z_full, z_empty, dq_done, drain;
+  uint64_t k_full[kStagesK], k_raw[kStagesK], k_empty[kStagesK], v_empty[kStagesV];
+  uint64_t sp_full, sp_free, z_full, z_empty, q_full, q_empty, a_full, dq_done, drain;
   uint32_t tmem;
   int abort;
   PlanRing ring;
@@ -61,15 +66,16 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
   __shared__ SharedQ sh;
   uint8_t* sQ = (uint8_t*)(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);
   uint8_t* sG = sQ + kQBytes;
-  uint8_t* sK = sG + kVBytes;                            // [2]
-  uint8_t* sV = sK + 2 * kQBytes;
+  uint8_t* sK = sG + kVBytes;
+  uint8_t* sV = sK + kStagesK * 3 * kKChunk;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (warp == 0) {
-    if (lane < 2) { ptx::mbar_init(&sh.k_full[lane], 1); ptx::mbar_init(&sh.k_raw[lane], 1); ptx::mbar_init(&sh.k_empty[lane], 1); }
+    if (lane < kStagesK) { ptx::mbar_init(&sh.k_full[lane], 2); ptx::mbar_init(&sh.k_raw[lane], 1); ptx::mbar_init(&sh.k_empty[lane], 1); }
+    if (lane < kStagesV) ptx::mbar_init(&sh.v_empty[lane], 1);
     if (lane < kPlans) sh.ring.init(lane);
-    if (lane == 2) {
-      ptx::mbar_init(&sh.v_full, 1); ptx::mbar_init(&sh.v_empty, 1); ptx::mbar_init(&sh.q_full, 1); ptx::mbar_init(&sh.q_empty, 1);
+    if (lane == 31) {
       ptx::mbar_init(&sh.sp_full, 1); ptx::mbar_init(&sh.sp_free, 8); ptx::mbar_init(&sh.z_full, 8); ptx::mbar_init(&sh.z_empty, 1);
+      ptx::mbar_init(&sh.q_full, 1); ptx::mbar_init(&sh.q_empty, 8); ptx::mbar_init(&sh.a_full, 8);
       ptx::mbar_init(&sh.dq_done, 1); ptx::mbar_init(&sh.drain, 1);
       sh.abort = 0;
     }
@@ -82,66 +88,68 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
   __syncthreads();
   umma::fence_after_sync();
   const uint32_t tmem = sh.tmem;
-  constexpr uint32_t kS = 0, kP = 128, kO = 256, kZ = 448;               // columns of S, dP, dQ, dZ
+  constexpr uint32_t kO = 0, kQa = 192, kGa = 288, kS = 352, kP = 416, kZ = 480;         // columns of dQ, Q, dO, S, dP, dZ
   ptx::grid_dep_wait();
   const WalkEnv env{p, &sh.ring, &sh.abort};
   auto wait = [&](uint64_t* bar, uint32_t parity) { return env.wait(bar, parity); };
 
   if (warp == kProducerWarp) {
-    QueryWalk<1> w;
-    int t = 0, n_raw[2] = {0, 0};
-    uint32_t through_raw = 0;
-    bool ok = true;
-    while (ok && w.next(env)) {
-      const int y = (int)((int64_t)w.l * p.rows + w.row0 + w.i * kLatTile), s = t & 1;
-      const bool tail = (w.i + 1) * kLatTile > w.T;
-      if (t > 1) ok = wait(&sh.k_empty[s], ((t >> 1) - 1) & 1);
-      if (!ok) break;
+    HalfWalk w;
+    int tk = 0, sk = 0, sv = 0, pk = 0, pv = 0;          // tiles loaded, stages, parities of their uses
+    bool given_up = false;
+    uint32_t through_raw = 0, raw_phase = 0;
+    while (w.next(env)) {
+      const int y = (int)((int64_t)w.w.l * p.rows + w.w.row0 + w.k0), h = w.w.h;
+      const bool tail = w.k0 + kKTile > w.w.T;
+      if (tk >= kStagesK && !wait(&sh.k_empty[sk], pk ^ 1)) break;
       if (umma::elect_one()) {
-        uint64_t* bar = tail ? &sh.k_raw[s] : &sh.k_full[s];
-        ptx::mbar_expect_tx(bar, kQBytes);
-        for (int c = 0; c < 2; ++c) ptx::tma_load_3d(sK + s * kQBytes + c * kLatChunk, &maps.kv, 64 * c, w.h, y, bar);
-        ptx::tma_load_2d(sK + s * kQBytes + 2 * kLatChunk, &maps.kr, 0, y, bar);
+        uint64_t* bar = tail ? &sh.k_raw[sk] : &sh.k_full[sk];           // (k_full: one arrival for K, one for V)
+        uint8_t* dst = sK + sk * 3 * kKChunk;
+        ptx::mbar_expect_tx(bar, 3 * kKChunk);
+        for (int c = 0; c < 2; ++c) ptx::tma_load_3d(dst + c * kKChunk, &maps.kv, 64 * c, h, y, bar);
+        ptx::tma_load_2d(dst + 2 * kKChunk, &maps.kr, 0, y, bar);
       }
       __syncwarp();
-      through_raw = tail ? through_raw | 1u << s : through_raw & ~(1u << s);
-      n_raw[0] += tail && !s; n_raw[1] += tail && s;
-      if (t > 0) ok = wait(&sh.v_empty, (t - 1) & 1);
-      ++t;
-      if (!ok) { --t; break; }
+      through_raw = tail ? through_raw | 1u << sk : through_raw & ~(1u << sk);
+      if (tail) raw_phase ^= 1u << sk;
+      if (tk >= kStagesV && !wait(&sh.v_empty[sv], pv ^ 1)) { given_up = true; break; }
       if (umma::elect_one()) {
-        ptx::mbar_expect_tx(&sh.v_full, kVBytes);
-        for (int c = 0; c < 2; ++c) ptx::tma_load_3d(sV + c * kLatChunk, &maps.kv, kLatNope + 64 * c, w.h, y, &sh.v_full);
+        ptx::mbar_expect_tx(&sh.k_full[sk], 2 * kKChunk);
+        for (int c = 0; c < 2; ++c) ptx::tma_load_3d(sV + (2 * sv + c) * kKChunk, &maps.kv, kLatNope + 64 * c, h, y, &sh.k_full[sk]);
       }
       __syncwarp();
+      ++tk;
+      if (++sk == kStagesK) { sk = 0; pk ^= 1; }
+      if (++sv == kStagesV) { sv = 0; pv ^= 1; }
     }
-    // nothing is in flight when the CTA ends (after a wait that ran out: K of tile t may be, V of it is not)
-    const int tk = ok ? t : t + 1;
-    for (int x = max(0, tk - 2); x < tk; ++x) {
-      if (through_raw >> (x & 1) & 1) ptx::mbar_wait_bounded(&sh.k_raw[x & 1], (n_raw[x & 1] - 1) & 1);
-      else ptx::mbar_wait_bounded(&sh.k_full[x & 1], (x >> 1) & 1);
+    // nothing is in flight when the CTA ends (a tile given up half way: its keys, which have a second or so to come)
+    for (int x = max(0, tk - kStagesK); x < tk; ++x) {
+      const int s = x % kStagesK;
+      if (through_raw >> s & 1) ptx::mbar_wait_bounded(&sh.k_raw[s], ((raw_phase >> s) & 1) ^ 1);
+      ptx::mbar_wait_bounded(&sh.k_full[s], (x / kStagesK) & 1);
     }
-    if (t > 0) ptx::mbar_wait_bounded(&sh.v_full, (t - 1) & 1);
+    if (given_up) ptx::mbar_wait_bounded(through_raw >> sk & 1 ? &sh.k_raw[sk] : &sh.k_full[sk], through_raw >> sk & 1 ? ((raw_phase >> sk) & 1) ^ 1 : pk);
     __syncwarp();
   } else if (warp == kMenderWarp) {
     // keys behind the sequence's end: dQ sums over them
-    QueryWalk<1> w;
+    HalfWalk w;
     uint32_t phase = 0;
     for (int t = 0; w.next(env); ++t) {
-      if ((w.i + 1) * kLatTile <= w.T) continue;
-      const int s = t & 1, n = w.T - w.i * kLatTile;
+      const int s = t % kStagesK, n = w.w.T - w.k0;
+      if (n >= kKTile) continue;
       if (!wait(&sh.k_raw[s], (phase >> s) & 1)) break;
       phase ^= 1u << s;
       for (int c = 0; c < 3; ++c)
-        for (int x = n * 8 + lane; x < kLatTile * 8; x += 32)
-          *reinterpret_cast<uint4*>(sK + s * kQBytes + c * kLatChunk + x * 16) = make_uint4(0, 0, 0, 0);
+        for (int x = n * 8 + lane; x < kKTile * 8; x += 32)
+          *reinterpret_cast<uint4*>(sK + (3 * s + c) * kKChunk + x * 16) = make_uint4(0, 0, 0, 0);
       ptx::fence_proxy_async();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&sh.k_full[s]);
     }
   } else if (warp == kPlannerWarp) {
     int n = 0;
-    run_planner<QueryWalk<1>>(env, kLatTile, true, [&](const QueryWalk<1>& w, int k) {
+    run_planner<HalfWalk>(env, kLatTile, true, [&](const HalfWalk& x, int k) {
+      const QueryWalk<1>& w = x.w;
       if (k > 0 && !wait(&sh.q_empty, (k - 1) & 1)) return false;
       if (umma::elect_one()) {
         const int y = (int)((int64_t)w.l * p.rows + w.row0 + w.q0);
@@ -156,66 +164,54 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
     if (n > 0) ptx::mbar_wait_bounded(&sh.q_full, (n - 1) & 1);
     __syncwarp();
   } else if (warp == kMmaWarp) {
-    constexpr uint32_t idesc = umma::instr_desc(kLatTile, kLatTile, false), idesc_q = umma::instr_desc(kLatTile, 192, true);
+    constexpr uint32_t idesc = umma::instr_desc(kLatTile, kKTile, false), idesc_q = umma::instr_desc(kLatTile, 192, true);
     const uint64_t hi = (uint64_t)umma::smem_desc_sw128(0, 0, 1024) & 0xffffffff00000000ull;
-    const uint32_t q_lo = (ptx::smem_u32(sQ) >> 4) | 1u << 16, g_lo = (ptx::smem_u32(sG) >> 4) | 1u << 16, v_lo = (ptx::smem_u32(sV) >> 4) | 1u << 16,
+    const uint32_t v_lo = (ptx::smem_u32(sV) >> 4) | 1u << 16,
                    k_lo = ptx::smem_u32(sK) >> 4;
     const int steps_r = p.dr / 16;
-    // One thread issues everything, whatever is ready: S of the next tile, its dP, the sums of this one.  (In a fixed order sums waited
-    // for scores whose keys waited for the sums to make room: XX us.)
+    // One thread issues everything: scores of the next tile before the sums of this one; at an item's end the other way round, since
+    // the next queries are still on their way.
     if (umma::elect_one()) {
-      QueryWalk<1> nxt;
-      Patience patience;
-      uint32_t flags = 0;                                // of the two tiles between scores and sums: first, last of an item
-      int n_q = 0, ts = 0, tz = 0;                       // query blocks begun, tiles whose scores, whose sums are issued
-      bool s_done = false, more = nxt.next<true>(env);   // s_done: S of tile ts is issued, dP is not
+      HalfWalk nxt;
+      uint32_t flags = 0;                                // two bits for each of the tiles between scores and sums: first, last of an item
+      int n_q = 0, ts = 0, tz = 0, sk = 0, pk = 0, sv = 0, sz = 0;       // query blocks begun, tiles whose scores, whose sums are issued; stages
+      bool more = nxt.next<true>(env);
       while (more || tz < ts) {
-        bool moved = false;
-        if (more && !s_done && ts <= tz + 1 && ptx::mbar_test_wait(&sh.k_full[ts & 1], (ts >> 1) & 1) &&
-            (ts == 0 || ptx::mbar_test_wait(&sh.sp_free, (ts - 1) & 1)) && (!nxt.first || ptx::mbar_test_wait(&sh.q_full, n_q & 1))) {
+        if (more && ts <= tz + 1 && !(nxt.first && tz < ts)) {
+          if (nxt.first && !env.wait_alone(&sh.a_full, n_q++ & 1)) break;
+          if (!env.wait_alone(&sh.k_full[sk], pk) || (ts > 0 && !env.wait_alone(&sh.sp_free, (ts - 1) & 1))) break;
           umma::fence_after_sync();
-          const uint32_t b = (k_lo + (ts & 1) * (kQBytes >> 4)) | 1u << 16;
+          const uint32_t b = (k_lo + sk * (3 * kKChunk >> 4)) | 1u << 16, v = v_lo + sv * (2 * kKChunk >> 4);
 #pragma unroll
           for (int k = 0; k < 12; ++k)
-            if (k < 8 || k - 8 < steps_r) {
-              const uint32_t o = ((k >> 2) * kLatChunk + (k & 3) * 32) >> 4;
-              umma::mma_bf16(tmem + kS, hi | (q_lo + o), hi | (b + o), idesc, k > 0 ? 1u : 0u);
-            }
-          n_q += nxt.first;
-          s_done = moved = true;
-        }
-        if (s_done && ptx::mbar_test_wait(&sh.v_full, ts & 1)) {
-          umma::fence_after_sync();
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const uint32_t o = ((k >> 2) * kLatChunk + (k & 3) * 32) >> 4;
-            umma::mma_bf16(tmem + kP, hi | (g_lo + o), hi | (v_lo + o), idesc, k > 0 ? 1u : 0u);
-          }
-          umma::commit(&sh.sp_full);
-          umma::commit(&sh.v_empty);
-          if (nxt.last()) umma::commit(&sh.q_empty);
-          flags |= (uint32_t)((nxt.first ? 1 : 0) | (nxt.last() ? 2 : 0)) << (2 * (ts & 1));
-          ++ts;
-          s_done = false;
-          moved = true;
-          more = nxt.next<true>(env);
-        }
-        if (tz < ts && ptx::mbar_test_wait(&sh.z_full, tz & 1)) {
-          umma::fence_after_sync();
-          const bool first = flags >> (2 * (tz & 1)) & 1, last = flags >> (2 * (tz & 1)) & 2;
-          flags &= ~(3u << (2 * (tz & 1)));
-          const uint32_t b = (k_lo + (tz & 1) * (kQBytes >> 4)) | (uint32_t)(kLatChunk >> 4) << 16;
+            if (k < 8 || k - 8 < steps_r)
+              umma::mma_bf16_a_tmem(tmem + kS, tmem + kQa + 8 * k, hi | (b + (((k >> 2) * kKChunk + (k & 3) * 32) >> 4)), idesc, k > 0 ? 1u : 0u);
 #pragma unroll
           for (int k = 0; k < 8; ++k)
+            umma::mma_bf16_a_tmem(tmem + kP, tmem + kGa + 8 * k, hi | (v + (((k >> 2) * kKChunk + (k & 3) * 32) >> 4)), idesc, k > 0 ? 1u : 0u);
+          umma::commit(&sh.sp_full);
+          umma::commit(&sh.v_empty[sv]);
+          flags |= (uint32_t)((nxt.first ? 1 : 0) | (nxt.last ? 2 : 0)) << (2 * (ts & 1));
+          ++ts;
+          if (++sk == kStagesK) { sk = 0; pk ^= 1; }
+          if (++sv == kStagesV) sv = 0;
+          more = nxt.next<true>(env);
+        } else {
+          const int z = tz & 1;
+          if (!env.wait_alone(&sh.z_full, z)) break;
+          umma::fence_after_sync();
+          const bool first = flags >> (2 * z) & 1, last = flags >> (2 * z) & 2;
+          flags &= ~(3u << (2 * z));
+          const uint32_t b = (k_lo + sz * (3 * kKChunk >> 4)) | (uint32_t)(kKChunk >> 4) << 16;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
             umma::mma_bf16_a_tmem(tmem + kO, tmem + kZ + 8 * k, hi | (b + ((k * 2048) >> 4)), idesc_q, (!first || k > 0) ? 1u : 0u);
-          umma::commit(&sh.k_empty[tz & 1]);
+          umma::commit(&sh.k_empty[sz]);
           umma::commit(&sh.z_empty);
           if (last) umma::commit(&sh.dq_done);
           ++tz;
-          moved = true;
+          if (++sz == kStagesK) sz = 0;
         }
-        if (moved) patience.moved();
-        else if (!patience.more(&sh.abort, p.dev_status)) break;
       }
       umma::commit(&sh.drain);
     }
@@ -225,71 +221,84 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
   } else {
     const int half = warp >> 2, row = 32 * (warp & 3) + lane;
     const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
-    QueryWalk<1> w;
+    HalfWalk x;
+    const QueryWalk<1>& w = x.w;
     float lse2 = 0.f, delta = 0.f;
     int n_items_done = 0;
-    for (int t = 0; w.next(env); ++t) {
+    for (int t = 0; x.next(env); ++t) {
       const int t_q = w.q0 + row;
       const bool mine = t_q < w.T;
-      if (w.first) {
+      if (x.first) {
         const int64_t at = ((int64_t)w.l * p.H + w.h) * p.rows + w.row0 + t_q;
         lse2 = mine ? p.lse[at] * 1.4426950408889634f : 0.f;
         delta = mine ? p.delta[at] : 0.f;
+        // this query's channels from shared into tensor memory (the item before is done with its own: its last scores are here);
+        // the products then read shared memory for keys and values alone
+        if (!wait(&sh.q_full, n_items_done & 1)) break;
+        auto copy = [&](const uint8_t* src, int piece0, int pieces, uint32_t dst) {      // 16-byte pieces of a row of 128-byte chunks
+          for (int c = 0; c < pieces; c += 2) {
+            uint32_t v[8];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int q = piece0 + c + e;
+              *reinterpret_cast<uint4*>(v + 4 * e) = *reinterpret_cast<const uint4*>(src + (q >> 3) * kLatChunk + row * 128 + (((q & 7) ^ (row & 7)) << 4));
+            }
+            umma::tmem_st8(lanes + dst + 4 * (piece0 + c), v);
+          }
+        };
+        copy(sQ, 12 * half, 12, kQa);
+        copy(sG, 8 * half, 8, kGa);
+        umma::tmem_st_wait();
+        umma::fence_before_sync();
+        __syncwarp();
+        if (lane == 0) { ptx::mbar_arrive(&sh.a_full); ptx::mbar_arrive(&sh.q_empty); }
       }
-      const int j0 = w.i * kLatTile + 64 * half;
+      const int j0 = x.k0 + 32 * half;
       const bool plain = !w.tiles || (w.plain_a >> (w.i - w.window) & 1);
-      int g[2];                                          // (asked for before the wait: the answer takes as long)
-      if (!plain) {
-        const int32_t* gone = p.gone + ((int64_t)w.b * p.G + list_of(p.lists, w.l, 0, 1)) * p.gone_cap + j0 + lane;
-        g[0] = gone[0];
-        g[1] = gone[32];
-      }
+      // (asked for before the wait: the answer takes as long)
+      const int g = plain ? 0 : p.gone[((int64_t)w.b * p.G + list_of(p.lists, w.l, 0, 1)) * p.gone_cap + j0 + lane];
       if (!wait(&sh.sp_full, t & 1)) break;
       umma::fence_after_sync();
-      uint32_t z[2][32], d[2][32];
-#pragma unroll
-      for (int k = 0; k < 2; ++k) umma::tmem_ld32(lanes + kS + 64 * half + 32 * k, z[k]);
-#pragma unroll
-      for (int k = 0; k < 2; ++k) umma::tmem_ld32(lanes + kP + 64 * half + 32 * k, d[k]);
+      uint32_t z[32], d[32];
+      umma::tmem_ld32(lanes + kS + 32 * half, z);
+      umma::tmem_ld32(lanes + kP + 32 * half, d);
       umma::tmem_ld_wait();
       umma::fence_before_sync();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&sh.sp_free);
-      uint32_t pk[32];
+      uint32_t seen = 0xffffffffu;                       // bit j: this query sees key j0 + j
+      const int behind = t_q - j0;                       // keys behind the query do not count
+      if (behind < 31) seen = behind < 0 ? 0u : (2u << behind) - 1u;
+      if (!plain) {
+        const uint32_t lo = __ballot_sync(0xffffffffu, g > w.q0 + kLatTile - 1);
+        if (lo == __ballot_sync(0xffffffffu, g > w.q0)) {
+          seen &= lo;
+        } else {
+          uint32_t m = 0;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        uint32_t seen = 0xffffffffu;                     // bit j: this query sees key j0 + 32 k + j
-        const int behind = t_q - (j0 + 32 * k);          // keys behind the query do not count
-        if (behind < 31) seen = behind < 0 ? 0u : (2u << behind) - 1u;
-        if (!plain) {
-          const uint32_t lo = __ballot_sync(0xffffffffu, g[k] > w.q0 + kLatTile - 1);
-          if (lo == __ballot_sync(0xffffffffu, g[k] > w.q0)) {
-            seen &= lo;
-          } else {
-            uint32_t m = 0;
-#pragma unroll
-            for (int j = 0; j < 32; ++j) m |= __shfl_sync(0xffffffffu, g[k], j) > t_q ? 1u << j : 0u;
-            seen &= m;
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < 32; j += 2) {
-          float e[2];
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const float pr = ptx::ex2_approx(fmaf(__uint_as_float(z[k][j + c]), p.scale_log2, -lse2));
-            e[c] = (seen >> (j + c) & 1) ? pr * (__uint_as_float(d[k][j + c]) - delta) : 0.f;
-          }
-          pk[16 * k + (j >> 1)] = ptx::pack_bf16x2(e[0], e[1]);
+          for (int j = 0; j < 32; ++j) m |= __shfl_sync(0xffffffffu, g, j) > t_q ? 1u << j : 0u;
+          seen &= m;
         }
       }
+      uint32_t pk[16];
+#pragma unroll
+      for (int j = 0; j < 32; j += 2) {
+        float e[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const float pr = ptx::ex2_approx(fmaf(__uint_as_float(z[j + c]), p.scale_log2, -lse2));
+          e[c] = (seen >> (j + c) & 1) ? pr * (__uint_as_float(d[j + c]) - delta) : 0.f;
+        }
+        pk[j >> 1] = ptx::pack_bf16x2(e[0], e[1]);
+      }
       if (t > 0 && !wait(&sh.z_empty, (t - 1) & 1)) break;
-      umma::tmem_st32(lanes + kZ + 32 * half, pk);
+      umma::tmem_st8(lanes + kZ + 16 * half, pk);
+      umma::tmem_st8(lanes + kZ + 16 * half + 8, pk + 8);
       umma::tmem_st_wait();
       umma::fence_before_sync();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&sh.z_full);
-      if (!w.last()) continue;
+      if (!x.last) continue;
       if (!wait(&sh.dq_done, n_items_done++ & 1)) break;
       umma::fence_after_sync();
       __nv_bfloat16* dst = p.gq + (((int64_t)w.l * p.rows + w.row0 + t_q) * p.H + w.h) * (kLatNope + p.dr);
@@ -311,12 +320,12 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
 
 constexpr int kQTile = KeyWalk::kQ;
 constexpr int kQChunk = kQTile * 128;          // 64 queries x 64 channels
-constexpr int kStageK = 5 * kQChunk;           // Q: 3 chunks, dO: 2
-constexpr int kStagesK = 3;
-constexpr int kSmemK = kQBytes + kVBytes + kStagesK * kStageK + 1024;
+constexpr int kStageBytes = 5 * kQChunk;           // Q: 3 chunks, dO: 2
+constexpr int kStages = 3;
+constexpr int kSmemK = kQBytes + kVBytes + kStages * kStageBytes + 1024;
 
 struct SharedK {
-  uint64_t full[kStagesK], raw[kStagesK], empty[kStagesK], kv_full, kv_empty, sp_full, sp_free, z_full, z_empty, done, drain;
+  uint64_t full[kStages], raw[kStages], empty[kStages], kv_full, kv_empty, sp_full, sp_free, z_full, z_empty, done, drain;
   uint32_t tmem;
   int abort;
   PlanRing ring;
@@ -331,7 +340,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
   uint8_t* stage = sV + kVBytes;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (warp == 0) {
-    if (lane < kStagesK) { ptx::mbar_init(&sh.full[lane], 1); ptx::mbar_init(&sh.raw[lane], 1); ptx::mbar_init(&sh.empty[lane], 1); }
+    if (lane < kStages) { ptx::mbar_init(&sh.full[lane], 1); ptx::mbar_init(&sh.raw[lane], 1); ptx::mbar_init(&sh.empty[lane], 1); }
     if (lane < kPlans) sh.ring.init(lane);
     if (lane == 31) {
       ptx::mbar_init(&sh.kv_full, 1); ptx::mbar_init(&sh.kv_empty, 1); ptx::mbar_init(&sh.sp_full, 1); ptx::mbar_init(&sh.sp_free, 8);
@@ -357,13 +366,13 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
     int t = 0, s = 0, phase = 0;
     uint32_t through_raw = 0, raw_phase = 0;
     while (w.next(env)) {
-      if (t >= kStagesK && !wait(&sh.empty[s], phase ^ 1)) break;
+      if (t >= kStages && !wait(&sh.empty[s], phase ^ 1)) break;
       const bool tail = (w.i + 1) * kQTile > w.T;
       const int y = (int)((int64_t)w.l * p.rows + w.row0 + w.i * kQTile);
       if (umma::elect_one()) {
         uint64_t* bar = tail ? &sh.raw[s] : &sh.full[s];
-        uint8_t* dst = stage + s * kStageK;
-        ptx::mbar_expect_tx(bar, kStageK);
+        uint8_t* dst = stage + s * kStageBytes;
+        ptx::mbar_expect_tx(bar, kStageBytes);
         for (int c = 0; c < 3; ++c) ptx::tma_load_3d(dst + c * kQChunk, &maps.q, 64 * c, w.h, y, bar);
         for (int c = 0; c < 2; ++c) ptx::tma_load_3d(dst + (3 + c) * kQChunk, &maps.go, 64 * c, w.h, y, bar);
       }
@@ -371,12 +380,12 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
       through_raw = tail ? through_raw | 1u << s : through_raw & ~(1u << s);
       if (tail) raw_phase ^= 1u << s;
       ++t;
-      if (++s == kStagesK) { s = 0; phase ^= 1; }
+      if (++s == kStages) { s = 0; phase ^= 1; }
     }
-    for (int x = max(0, t - kStagesK); x < t; ++x) {     // nothing is in flight when the CTA ends
-      const int k = x % kStagesK;
+    for (int x = max(0, t - kStages); x < t; ++x) {     // nothing is in flight when the CTA ends
+      const int k = x % kStages;
       if (through_raw >> k & 1) ptx::mbar_wait_bounded(&sh.raw[k], ((raw_phase >> k) & 1) ^ 1);
-      else ptx::mbar_wait_bounded(&sh.full[k], (x / kStagesK) & 1);
+      else ptx::mbar_wait_bounded(&sh.full[k], (x / kStages) & 1);
     }
     __syncwarp();
   } else if (warp == kMenderWarp) {
@@ -385,12 +394,12 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
     uint32_t raw_phase = 0;
     for (int t = 0; w.next(env); ++t) {
       if ((w.i + 1) * kQTile <= w.T) continue;
-      const int s = t % kStagesK, n = w.T - w.i * kQTile;
+      const int s = t % kStages, n = w.T - w.i * kQTile;
       if (!wait(&sh.raw[s], (raw_phase >> s) & 1)) break;
       raw_phase ^= 1u << s;
       for (int c = 0; c < 5; ++c)
         for (int x = n * 8 + lane; x < kQTile * 8; x += 32)
-          *reinterpret_cast<uint4*>(stage + s * kStageK + c * kQChunk + x * 16) = make_uint4(0, 0, 0, 0);
+          *reinterpret_cast<uint4*>(stage + s * kStageBytes + c * kQChunk + x * 16) = make_uint4(0, 0, 0, 0);
       ptx::fence_proxy_async();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&sh.full[s]);
@@ -429,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
         if (more && ts <= tz + 1 && ptx::mbar_test_wait(&sh.full[s_nxt], ph_nxt) && (ts == 0 || ptx::mbar_test_wait(&sh.sp_free, (ts - 1) & 1)) &&
             (!nxt.first || ptx::mbar_test_wait(&sh.kv_full, n_k & 1))) {
           umma::fence_after_sync();
-          const uint32_t b = (st_lo + s_nxt * (kStageK >> 4)) | 1u << 16;
+          const uint32_t b = (st_lo + s_nxt * (kStageBytes >> 4)) | 1u << 16;
 #pragma unroll
           for (int k = 0; k < 12; ++k)
             if (k < 8 || k - 8 < steps_r)
@@ -442,7 +451,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
           umma::commit(&sh.sp_full);
           if (nxt.last()) umma::commit(&sh.kv_empty);
           n_k += nxt.first;
-          if (++s_nxt == kStagesK) { s_nxt = 0; ph_nxt ^= 1; }
+          if (++s_nxt == kStages) { s_nxt = 0; ph_nxt ^= 1; }
           flags |= (uint32_t)((nxt.first ? 1 : 0) | (nxt.last() ? 2 : 0)) << (2 * (ts & 1));
           ++ts;
           moved = true;
@@ -452,7 +461,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
           umma::fence_after_sync();
           const bool first = flags >> (2 * (tz & 1)) & 1, last = flags >> (2 * (tz & 1)) & 2;
           flags &= ~(3u << (2 * (tz & 1)));
-          const uint32_t b = (st_lo + s_cur * (kStageK >> 4)) | (uint32_t)(kQChunk >> 4) << 16;
+          const uint32_t b = (st_lo + s_cur * (kStageBytes >> 4)) | (uint32_t)(kQChunk >> 4) << 16;
 #pragma unroll
           for (int k = 0; k < 4; ++k)
             umma::mma_bf16_a_tmem(tmem + kDv, tmem + kP + 8 * k, hi | (b + ((3 * kQChunk + k * 2048) >> 4)), idesc_v, (!first || k > 0) ? 1u : 0u);
@@ -462,7 +471,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
           umma::commit(&sh.empty[s_cur]);
           umma::commit(&sh.z_empty);
           if (last) umma::commit(&sh.done);
-          if (++s_cur == kStagesK) s_cur = 0;
+          if (++s_cur == kStages) s_cur = 0;
           ++tz;
           moved = true;
         }
@@ -590,12 +599,13 @@ int launch_latent_bwd(const LatentReplayParams& p, cudaStream_t stream) {
   const int64_t items = ((int64_t)p.max_len + kLatTile - 1) / kLatTile * p.L * p.B * p.H;
   if (items > 0x7fffff00LL) return NGC_ERR_UNSUPPORTED;
   const int64_t rows = (int64_t)p.L * p.rows;
-  Maps mq, mk;                                   // boxes of 128 and of 64 rows
+  Maps mq, mk;
   if (!make_token_map(&mq.q, p.q, kLatNope + p.dr, p.H, rows, kLatTile) || !make_token_map(&mq.kv, p.kv, kLatNope + kLatV, p.H, rows, kLatTile) ||
       !make_rows_map(&mq.kr, p.kr, rows, kLatTile, p.dr) || !make_token_map(&mq.go, p.go, kLatV, p.H, rows, kLatTile))
     return NGC_ERR_UNSUPPORTED;
-  mk = mq;
-  if (!make_token_map(&mk.q, p.q, kLatNope + p.dr, p.H, rows, kQTile) || !make_token_map(&mk.go, p.go, kLatV, p.H, rows, kQTile))
+  mk = mq;                                       // what is loaded once per item in boxes of 128 rows, tiles of 64
+  if (!make_token_map(&mq.kv, p.kv, kLatNope + kLatV, p.H, rows, kKTile) || !make_rows_map(&mq.kr, p.kr, rows, kKTile, p.dr) ||
+      !make_token_map(&mk.q, p.q, kLatNope + p.dr, p.H, rows, kQTile) || !make_token_map(&mk.go, p.go, kLatV, p.H, rows, kQTile))
     return NGC_ERR_UNSUPPORTED;
   static PerDeviceOnce once;
   static int sms[kMaxDevices] = {0};

@@ -216,6 +216,27 @@ template <int BLOCKS> struct QueryWalk {
   }
 };
 
+// The same by tiles of 64 keys, one block of queries per item.
+struct HalfWalk {
+  QueryWalk<1> w;
+  int k0;                       // first key
+  bool begun, upper, first, last;
+
+  __device__ __forceinline__ HalfWalk() : begun(false), upper(false) {}
+  __device__ __forceinline__ bool has_upper() const { return w.i * kLatTile + 64 < min(w.T, w.q0 + kLatTile); }
+  __device__ __forceinline__ bool plan(const WalkEnv& e, Deal& deal) { return w.plan(e, deal); }
+  __device__ __forceinline__ void publish(ReplayPlan& r) { w.publish(r); }
+  template <bool ALONE = false> __device__ __forceinline__ bool next(const WalkEnv& e) {
+    upper = begun && !upper && has_upper();
+    if (!upper && !w.next<ALONE>(e)) return false;
+    begun = true;
+    k0 = w.i * kLatTile + (upper ? 64 : 0);
+    first = w.first && !upper;
+    last = w.last() && (upper || !has_upper());
+    return true;
+  }
+};
+
 // Items of 128 keys of one head; and for each the tiles of 64 queries from its own first key to the last query that sees one of
 // them.
 struct KeyWalk {
