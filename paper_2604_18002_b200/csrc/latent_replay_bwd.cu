@@ -175,9 +175,9 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
       HalfWalk nxt;
       uint32_t flags = 0;                                // two bits for each of the tiles between scores and sums: first, last of an item
       int n_q = 0, ts = 0, tz = 0, sk = 0, pk = 0, sv = 0, sz = 0;       // query blocks begun, tiles whose scores, whose sums are issued; stages
-      bool more = nxt.next<true>(env);
+      bool more = nxt.next<true>(env), fresh = true;     // fresh: nxt's scores are not issued yet
       while (more || tz < ts) {
-        if (more && ts <= tz + 1 && !(nxt.first && tz < ts)) {
+        if (more && !(nxt.first && tz < ts)) {
           if (nxt.first && !env.wait_alone(&sh.a_full, n_q++ & 1)) break;
           if (!env.wait_alone(&sh.k_full[sk], pk) || (ts > 0 && !env.wait_alone(&sh.sp_free, (ts - 1) & 1))) break;
           umma::fence_after_sync();
@@ -195,8 +195,9 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
           ++ts;
           if (++sk == kStagesK) { sk = 0; pk ^= 1; }
           if (++sv == kStagesV) sv = 0;
-          more = nxt.next<true>(env);
-        } else {
+          fresh = false;
+        }
+        if (tz + 1 < ts || (tz < ts && (!more || fresh))) {              // sums of the tile before, or of the last
           const int z = tz & 1;
           if (!env.wait_alone(&sh.z_full, z)) break;
           umma::fence_after_sync();
@@ -211,6 +212,10 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_q_kernel(const __grid
           if (last) umma::commit(&sh.dq_done);
           ++tz;
           if (++sz == kStagesK) sz = 0;
+        }
+        if (!fresh) {                                    // (while the products run: the thread's own instructions take long)
+          more = more && nxt.next<true>(env);
+          fresh = true;
         }
       }
       umma::commit(&sh.drain);

@@ -110,7 +110,7 @@ struct WalkEnv {
   PlanRing* ring;
   int* abort;
   __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) const { return umma::warp_wait(bar, parity, abort, p.dev_status); }
-  __device__ __forceinline__ bool wait_alone(uint64_t* bar, uint32_t parity) const { return umma::wait_or_abort(bar, parity, abort, p.dev_status); }
+  __device__ __forceinline__ bool wait_alone(uint64_t* bar, uint32_t parity) const { return umma::wait_quick(bar, parity, abort, p.dev_status); }
   // Plan of item k: wait for it, and give it back (by a warp, or by one thread that stands for its warp).
   template <bool ALONE> __device__ __forceinline__ bool obtain(int k) const {
     uint64_t* bar = &ring->full[k % kPlans];

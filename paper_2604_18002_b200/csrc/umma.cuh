@@ -155,6 +155,14 @@ __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, in
     }
   }
 }
+// The same for a thread whose every instruction counts (one that issues MMAs beside busy warps): the first look is all that is
+// inlined.
+static __device__ __noinline__ bool wait_long(uint64_t* bar, uint32_t parity, int* abort, int32_t* dev_status) {
+  return wait_or_abort(bar, parity, abort, dev_status);
+}
+__device__ __forceinline__ bool wait_quick(uint64_t* bar, uint32_t parity, int* abort, int32_t* dev_status) {
+  return ptx::mbar_try_wait(bar, parity) || wait_long(bar, parity, abort, dev_status);
+}
 // The same for a whole warp: every lane gets the same answer.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int* abort, int32_t* dev_status) {
   return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort, dev_status));
