@@ -327,102 +327,75 @@ __global__ void __launch_bounds__(cta_threads(NH), 1) latent_decode_kernel(const
     __syncwarp();
   } else if (warp == kMmaWarp) {
     // ------------------------------------------------------------------ products
-    // (One elected thread issues: the compiler then keeps descriptors in uniform registers; with `lane == 0` a product took 90
-    // cycles to issue and the CTA 4500 per tile.)
-    if (n_tiles > 0) {
+    // One elected thread does it all: the compiler keeps descriptors in uniform registers then (with `lane == 0` a product took 90
+    // cycles to issue and the CTA 4500 per tile), and nothing is spent on meeting the warp again.
+    if (n_tiles > 0 && umma::elect_one()) {
       constexpr uint32_t idesc_s = umma::instr_desc(64, NH, false);
       constexpr uint32_t idesc_o = umma::instr_desc(128, NH, false, true);
       const uint64_t hi = (uint64_t)umma::smem_desc_sw128(0, 0, 1024) & 0xffffffff00000000ull;
       const uint32_t k_lo = ptx::smem_u32(sK) >> 4, q_lo = (ptx::smem_u32(sQ) >> 4) | 1u << 16, p_lo = (ptx::smem_u32(sP) >> 4) | 1u << 16;
       const int steps_r = p.dr / 16;
       Walk ws(sh), wp(sh);                               // the parts that scores and sums are at
+      umma::Patience patience;
       int s_at = 0, p_at = 0, n_q = 0;                   // tile within the walk's part; units begun
       ws.t_end = ws.t_begin = wp.t_end = wp.t_begin = 0;
-      // The warp looks at what is there, a tile for the next scores or weights for the next sums, and issues that: sums that
-      // waited behind the scores of a tile still on its way would hold their own tile's stage meanwhile.
+      // It looks at what is there, weights for the next sums or a tile for the next scores, and issues that: sums that waited
+      // behind the scores of a tile still on its way would hold their own tile's stage meanwhile.
       int s_next = 0, p_next = 0;
       Ring sp(p.stages), pp(p.stages);                   // the stages that scores and sums are at
-      uint64_t t0 = 0;
-      for (uint32_t spins = 0; p_next < n_tiles;) {
+      bool ok = true;
+      while (ok && p_next < n_tiles) {
         bool moved = false;
-        if (s_next < n_tiles && s_at == ws.t_end) { ws.next(p); s_at = ws.t_begin; ++n_q; }
-        // one look at everything that could be waited for, a barrier per lane: the next tile's pairs, its rotary part, the queries,
-        // the next weights
-        uint64_t* bar = &sh.p_full;
-        uint32_t parity = p_next & 1;
-        if (lane < kM) {
-          bar = &sh.full[sp.slot * kM + lane];
-          parity = sp.phase;
-        } else if (lane == kM) { bar = &sh.r_full[sp.slot]; parity = sp.phase; }
-        else if (lane == kM + 1) { bar = &sh.q_full; parity = (n_q - 1) & 1; }
-        const uint32_t seen = __ballot_sync(0xffffffffu, ptx::mbar_test_wait(bar, parity));
-        if (p_next < s_next && (seen >> 31)) {
+        if (p_next < s_next && ptx::mbar_test_wait(&sh.p_full, p_next & 1)) {
           umma::fence_after_sync();
           bool fresh = false;
           if (p_at == wp.t_end) { wp.next(p); p_at = wp.t_begin; fresh = true; }
           const uint32_t a_lo = (k_lo + pp.slot * (kStage >> 4)) | (uint32_t)(kBox >> 4) << 16;
-          if (umma::elect_one()) {
 #pragma unroll
-            for (int m = 0; m < kM; ++m) {
+          for (int m = 0; m < kM; ++m) {
 #pragma unroll
-              for (int kk = 0; kk < 4; ++kk)
-                umma::mma_bf16(tmem + (uint32_t)(m * NH), hi | (a_lo + ((m * kPair + kk * 2048) >> 4)), hi | (p_lo + 2 * kk), idesc_o,
-                               (!fresh || kk > 0) ? 1u : 0u);
-              umma::commit(&sh.empty[pp.slot * kM + m]);
-            }
-            umma::commit(&sh.o_done);
+            for (int kk = 0; kk < 4; ++kk)
+              umma::mma_bf16(tmem + (uint32_t)(m * NH), hi | (a_lo + ((m * kPair + kk * 2048) >> 4)), hi | (p_lo + 2 * kk), idesc_o,
+                             (!fresh || kk > 0) ? 1u : 0u);
+            umma::commit(&sh.empty[pp.slot * kM + m]);
           }
-          __syncwarp();
+          umma::commit(&sh.o_done);
           pp.next();
           ++p_at;
           ++p_next;
           moved = true;
         }
-        // scores from the first channels' arrival on, while the others are on their way (the scores' buffer held those of
-        // s_next - 2, read before their weights were published)
-        constexpr uint32_t kFirst = 1u | 1u << (kM + 1);
-        if (s_next < n_tiles && s_next <= p_next + 1 && (seen & kFirst) == kFirst) {
-          const uint32_t d = s_tmem + (uint32_t)((s_next & 1) * NH);
-          const uint32_t a_lo = (k_lo + sp.slot * (kStage >> 4)) | 1u << 16;
-          bool ok = true;
-          ++s_at;
+        if (s_next < n_tiles && s_next <= p_next + 1) {  // (the scores' buffer held those of s_next - 2, read before their weights were published)
+          if (s_at == ws.t_end) { ws.next(p); s_at = ws.t_begin; ++n_q; }
+          if (ptx::mbar_test_wait(&sh.full[sp.slot * kM], sp.phase) && ptx::mbar_test_wait(&sh.q_full, (n_q - 1) & 1)) {
+            // the first channels are there, the others on their way
+            const uint32_t d = s_tmem + (uint32_t)((s_next & 1) * NH);
+            const uint32_t a_lo = (k_lo + sp.slot * (kStage >> 4)) | 1u << 16;
+            ++s_at;
 #pragma unroll
-          for (int m = 0; m <= kM; ++m) {                // the rotary part last
-            ok = ok && ((seen >> m & 1) || umma::warp_wait(m < kM ? &sh.full[sp.slot * kM + m] : &sh.r_full[sp.slot], sp.phase, &sh.abort, p.dev_status));
-            umma::fence_after_sync();
-            if (ok && umma::elect_one()) {
+            for (int m = 0; m <= kM; ++m) {              // the rotary part last
+              if (m > 0) ok = ok && umma::wait_quick(m < kM ? &sh.full[sp.slot * kM + m] : &sh.r_full[sp.slot], sp.phase, &sh.abort, p.dev_status);
+              if (!ok) break;
+              umma::fence_after_sync();
 #pragma unroll
               for (int k = 0; k < (m < kM ? 8 : 4); ++k)
                 if (m < kM || k < steps_r)
                   umma::mma_bf16(d, hi | (a_lo + ((m * kPair + (k >> 2) * kBox + (k & 3) * 32) >> 4)),
                                  hi | (q_lo + (((2 * m + (k >> 2)) * NH * 128 + (k & 3) * 32) >> 4)), idesc_s, (m > 0 || k > 0) ? 1u : 0u);
-              if (m == kM) {
-                umma::commit(&sh.s_full[s_next & 1]);
-                umma::commit(&sh.r_empty[sp.slot]);
-                if (s_at == ws.t_end) umma::commit(&sh.q_empty);
-              }
             }
-            __syncwarp();
-          }
-          if (!ok) break;
-          sp.next();
-          ++s_next;
-          moved = true;
-        }
-        if (moved) { t0 = 0; continue; }
-        if ((++spins & 255u) == 0) {
-          const uint64_t now = ptx::globaltimer_ns();
-          if (t0 == 0) t0 = now;
-          const bool late = now - t0 > ptx::kWaitLimitNs;
-          if (__any_sync(0xffffffffu, late || *(volatile int*)&sh.abort)) {
-            if (late) set_dev_status(p.dev_status, NGC_DEV_TIMEOUT);
-            *(volatile int*)&sh.abort = 1;
-            break;
+            if (!ok) break;
+            umma::commit(&sh.s_full[s_next & 1]);
+            umma::commit(&sh.r_empty[sp.slot]);
+            if (s_at == ws.t_end) umma::commit(&sh.q_empty);
+            sp.next();
+            ++s_next;
+            moved = true;
           }
         }
+        if (moved) patience.moved();
+        else ok = patience.more(&sh.abort, p.dev_status);
       }
-      if (umma::elect_one()) umma::commit(&sh.drain);    // everything issued has completed before tensor memory is released
-      __syncwarp();
+      umma::commit(&sh.drain);                           // everything issued has completed before tensor memory is released
       ptx::mbar_wait_bounded(&sh.drain, 0);
     }
     __syncwarp();

@@ -434,7 +434,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
     const int steps_r = p.dr / 16;
     if (umma::elect_one()) {
       KeyWalk nxt;
-      Patience patience;
+      umma::Patience patience;
       uint32_t flags = 0;                                // of the two tiles between scores and sums: first, last of an item
       int n_k = 0, ts = 0, tz = 0, s_nxt = 0, ph_nxt = 0, s_cur = 0;
       bool more = nxt.next<true>(env);

@@ -87,23 +87,6 @@ struct PlanRing {
   static constexpr int kReaders = 11;          // producer, mender, MMA, eight softmax warps
   __device__ __forceinline__ void init(int i) { ptx::mbar_init(&full[i], 1); ptx::mbar_init(&empty[i], kReaders); }
 };
-// The limit of a thread's turns round a loop in which it looks at barriers without waiting at any.
-struct Patience {
-  uint32_t turns = 0;
-  uint64_t since = 0;
-  __device__ __forceinline__ void moved() { since = 0; }
-  // One more turn without anything to do; false when it is time to leave.
-  __device__ __forceinline__ bool more(int* abort, int32_t* dev_status) {
-    if ((++turns & 255u) != 0) return true;
-    if (*(volatile int*)abort) return false;
-    const uint64_t now = ptx::globaltimer_ns();
-    if (since == 0) since = now;
-    if (now - since <= ptx::kWaitLimitNs) return true;
-    *(volatile int*)abort = 1;
-    set_dev_status(dev_status, NGC_DEV_TIMEOUT);
-    return false;
-  }
-};
 // What every walk needs of a launch.
 struct WalkEnv {
   const LatentReplayParams& p;

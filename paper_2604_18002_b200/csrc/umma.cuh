@@ -163,7 +163,24 @@ static __device__ __noinline__ bool wait_long(uint64_t* bar, uint32_t parity, in
 __device__ __forceinline__ bool wait_quick(uint64_t* bar, uint32_t parity, int* abort, int32_t* dev_status) {
   return ptx::mbar_try_wait(bar, parity) || wait_long(bar, parity, abort, dev_status);
 }
-// The same for a whole warp: every lane gets the same answer.
+// The limit of a thread's turns round a loop in which it looks at barriers without waiting at any.
+struct Patience {
+  uint32_t turns = 0;
+  uint64_t since = 0;
+  __device__ __forceinline__ void moved() { since = 0; }
+  // One more turn without anything to do; false when it is time to leave.
+  __device__ __forceinline__ bool more(int* abort, int32_t* dev_status) {
+    if ((++turns & 255u) != 0) return true;
+    if (*(volatile int*)abort) return false;
+    const uint64_t now = ptx::globaltimer_ns();
+    if (since == 0) since = now;
+    if (now - since <= ptx::kWaitLimitNs) return true;
+    *(volatile int*)abort = 1;
+    set_dev_status(dev_status, NGC_DEV_TIMEOUT);
+    return false;
+  }
+};
+// Bounded wait of a whole warp: every lane gets the same answer.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int* abort, int32_t* dev_status) {
   return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort, dev_status));
 }
