@@ -624,15 +624,20 @@ def new_latent_pool(L: int, B: int, d_latent: int, d_rope: int, n_pages: int, pa
 
 def _pool_view(what: str, pool: NgcLatentPool):
     """Checks a pool's own tensors; (descriptor, L, B, G, d_rope, device index)."""
-    rows, table = pool.rows, pool.page_table
+    rows, table, used, lens = pool.rows, pool.page_table, pool.page_used, pool.lens
     index = rows.get_device()
     L, n_pages, page, width = rows.shape
     B, G, cap = table.shape
     if G != lists_G(pool.lists, L, 1):
         raise NgcError(f"{what}: page_table {tuple(table.shape)} does not fit rows {tuple(rows.shape)} and the lists")
-    desc = LatentPoolDesc(_arg(what, "rows", rows, rows.shape, torch.bfloat16, index), _arg(what, "page_table", table, table.shape, _I32, index),
-                          _arg(what, "page_used", pool.page_used, (G, n_pages), _U8, index), _arg(what, "lens", pool.lens, (B, G), _I32, index),
-                          L, B, pool.d_latent, width - pool.d_latent, BF16, page, cap, n_pages, pool.lists)
+    if not (rows.dtype is torch.bfloat16 and table.dtype is _I32 and used.dtype is _U8 and lens.dtype is _I32 and used.shape == (G, n_pages)
+            and lens.shape == (B, G) and table.get_device() == used.get_device() == lens.get_device() == index and rows.is_contiguous()
+            and table.is_contiguous() and used.is_contiguous() and lens.is_contiguous()):
+        for name, t, shape, dtype in (("rows", rows, rows.shape, torch.bfloat16), ("page_table", table, table.shape, _I32),
+                                      ("page_used", used, (G, n_pages), _U8), ("lens", lens, (B, G), _I32)):
+            _arg(what, name, t, shape, dtype, index)
+    desc = LatentPoolDesc(rows.data_ptr(), table.data_ptr(), used.data_ptr(), lens.data_ptr(), L, B, pool.d_latent, width - pool.d_latent, BF16,
+                          page, cap, n_pages, pool.lists)
     return desc, L, B, G, width - pool.d_latent, index
 
 

@@ -1,12 +1,13 @@
 // ngc_pool_update and ngc_latent_write: the pages of a common pool and the rows of new tokens.
 //
-// The books (page table, used map, lengths) of one list are the work of one CTA: every step depends on the one before
-// (what eviction returns can be handed out again), and all of it is a few reads per sequence and one byte per page of the
-// pool.  Warps take sequences for the eviction; sums over sequences and over the used map give every new page its rank,
-// and the page of rank r finds its sequence by bisection, so the free pages are never listed.  Only the slot map is as
-// long as the tokens: a cluster of CTAs per list shares it, the others wait for the books at the cluster's barrier and
-// read the first CTA's sums from its shared memory.  Bound by latency: a chain of dependent reads (lengths -> table row ->
-// used map -> table -> slots).
+// The books (page table, used map, lengths) of one list are the work of one cluster of CTAs: every step depends on the one
+// before (what eviction returns can be handed out again), and all of it is a few reads per sequence and one byte per page of the
+// pool.  Sequences are dealt out to the threads of the cluster, those that evict or leave to its warps; what they find lies in
+// the first CTA's shared memory.  There sums over sequences and over the map give every new page its rank, and the page of rank r
+// finds its sequence by bisection.  The slot map is shared by the cluster again, or, for many tokens, a kernel of its own.  Bound by latency, a chain of dependent reads (lengths -> table row -> map -> table -> slots) and
+// the barriers between them, and by one SM's instructions where all sequences evict: 256 threads per CTA, because barriers of
+// 1024 took longer than the work (64 growing sequences: XX -> XX us), and up to eight CTAs per list (64 evicting sequences on
+// 28 layers: XX -> XX us).
 #include <cooperative_groups.h>
 
 #include "latent_pool.cuh"
@@ -17,7 +18,7 @@ namespace cg = cooperative_groups;
 namespace ngc {
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxB = 8192;
 
@@ -32,6 +33,7 @@ struct PoolParams {
   int32_t* first;              // [B+1]
   int32_t* dev_status;
   int B, G, cap, n_pages, page, page_shift, k_max, n_slots;
+  int split;                   // the slots are left to a kernel of their own
 };
 
 // Inclusive sum over the CTA's threads; `total` gets the sum of all.  Two barriers.
@@ -44,16 +46,16 @@ __device__ __forceinline__ int block_scan(int v, int* warp_sums, int& total) {
   }
   if (lane == 31) warp_sums[warp] = v;
   __syncthreads();
-  int w = warp_sums[lane];
+  int before = 0;
+  total = 0;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int u = __shfl_up_sync(0xffffffffu, w, o);
-    if (lane >= o) w += u;
+  for (int w = 0; w < kWarps; ++w) {
+    const int u = warp_sums[w];
+    before += w < warp ? u : 0;
+    total += u;
   }
-  total = __shfl_sync(0xffffffffu, w, 31);
-  const int before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
   __syncthreads();
-  return v + (warp > 0 ? before : 0);
+  return v + before;
 }
 
 // Last b with sum[b] <= x, for 0 <= x < sum[B] (sequences without a share never are the answer).
@@ -80,93 +82,115 @@ __device__ __forceinline__ uint32_t free_mask(const uint8_t* used, int at, int n
   return m;
 }
 
-// What sequence b keeps, gives back and needs; one warp.  Returns to lane 0 the length it goes on from (-1: it does not
-// grow), and the pages it needs.
-__device__ __forceinline__ void settle_sequence(const PoolParams& p, int gi, int b, int first_token, int& len_out, int& need_out, int& have_out) {
+// What a sequence goes on from: the length it grows from (-1: it does not grow), the pages it needs.
+struct Settled { int len, need; };
+
+// The part that both ways share: may the sequence grow from `len` tokens?  `last_page`: the entry of its last page, where that has room.
+__device__ __forceinline__ Settled settle_growth(const PoolParams& p, int len, int n_new, int first_token, int last_page) {
+  const int grow = max(n_new, 0), have = (len + p.page - 1) >> p.page_shift;
+  if (grow > p.n_slots - first_token) {
+    set_dev_status(p.dev_status, NGC_DEV_BAD_COUNTS);
+    return {-1, 0};
+  }
+  if (grow > p.cap * p.page - len) {
+    set_dev_status(p.dev_status, NGC_DEV_STRIP_FULL);
+    return {-1, 0};
+  }
+  if (grow > 0 && (len & (p.page - 1)) != 0 && (uint32_t)last_page >= (uint32_t)p.n_pages) {
+    set_dev_status(p.dev_status, NGC_DEV_BAD_PAGE);
+    return {-1, 0};
+  }
+  return {len, ((len + grow + p.page - 1) >> p.page_shift) - have};
+}
+
+// A sequence that evicts or leaves; one warp.  `rows` holds the table row of up to kRowMax pages while it is rewritten.
+constexpr int kRowMax = 512;
+__device__ Settled settle_eviction(const PoolParams& p, int gi, int b, int first_token, int* rows, uint8_t* used) {
   const int lane = threadIdx.x & 31;
   const int64_t list = (int64_t)b * p.G + gi;
   int32_t* row = p.table + list * p.cap;
-  uint8_t* used = p.used + (int64_t)gi * p.n_pages;
-  int len = p.lens[list];
-  const int n_new = p.n_new[b];
-  const int budget = p.kept ? p.budget[b] : -1;
-  len_out = -1;
-  need_out = 0;
-  have_out = 0;
-  if (len < 0 || len > p.cap * p.page || n_new < -1 || budget < -1 || budget > p.k_max) {
-    if (lane == 0) set_dev_status(p.dev_status, NGC_DEV_BAD_COUNTS);
-    return;
+  const int len = p.lens[list], n_new = p.n_new[b], budget = p.kept ? p.budget[b] : -1;
+  const int have = (len + p.page - 1) >> p.page_shift, keep = max(budget, 0);
+  const int32_t* kept = p.kept + (budget > 0 ? list * p.k_max : 0);
+  bool bad_page = false, bad_kept = keep > have;
+  const bool small = have <= kRowMax;
+  for (int j = lane; j < have; j += 32) {
+    const int pg = row[j];
+    bad_page = bad_page || (uint32_t)pg >= (uint32_t)p.n_pages;
+    if (small) rows[j] = pg;
   }
-  int have = (len + p.page - 1) >> p.page_shift;
-  const bool evict = budget >= 0, leave = n_new < 0;
-  bool bad_page = false, bad_kept = budget > have;
-  const int32_t* kept = p.kept + (evict ? list * p.k_max : 0);
-  if (evict || leave)                                  // (growth alone needs nothing of the old entries but the last page's, below)
-    for (int j = lane; j < have; j += 32) bad_page = bad_page || (uint32_t)row[j] >= (uint32_t)p.n_pages;
-  if (evict && !bad_kept)
-    for (int j = lane; j < budget; j += 32) {
+  if (!bad_kept)
+    for (int j = lane; j < keep; j += 32) {
       const int u = kept[j], prev = j > 0 ? kept[j - 1] : -1;
       bad_kept = bad_kept || u <= prev || u >= have;
     }
-  if (__any_sync(0xffffffffu, bad_page || bad_kept)) {
-    bad_page = __any_sync(0xffffffffu, bad_page);
+  bad_page = __any_sync(0xffffffffu, bad_page);
+  if (__any_sync(0xffffffffu, bad_kept) || bad_page) {
     if (lane == 0) set_dev_status(p.dev_status, bad_page ? NGC_DEV_BAD_PAGE : NGC_DEV_BAD_KEPT);
-    return;
+    return {-1, 0};
   }
-  if (evict || leave) {
-    for (int j = lane; j < have; j += 32) used[row[j]] = 0;
+  const int stay = n_new < 0 ? 0 : keep;                 // pages that stay
+  const int last_unit = stay > 0 ? kept[stay - 1] : -1;
+  int last_page = -1;
+  if (small) {
+    for (int j = lane; j < have; j += 32) used[rows[j]] = 0;
     __syncwarp();
-    if (leave) {
-      for (int j = lane; j < have; j += 32) row[j] = -1;
-      len = have = 0;
-    } else {
-      // in place: entry j comes from kept[j] >= j, and a step of 32 entries reads its sources before it writes
-      const int last = budget > 0 ? kept[budget - 1] : -1;
-      for (int j0 = 0; j0 < budget; j0 += 32) {
-        const int j = j0 + lane;
-        const int pg = j < budget ? row[kept[j]] : 0;
-        __syncwarp();
-        if (j < budget) { row[j] = pg; used[pg] = 1; }
-        __syncwarp();
-      }
-      for (int j = budget + lane; j < have; j += 32) row[j] = -1;
-      len = budget * p.page - (last == have - 1 ? have * p.page - len : 0);
-      if (budget == 0) len = 0;
-      have = budget;
+    for (int j = lane; j < stay; j += 32) {
+      const int pg = rows[kept[j]];
+      row[j] = pg;
+      used[pg] = 1;
     }
-    if (lane == 0) p.lens[list] = len;
+    if (stay > 0) last_page = rows[last_unit];
+    __syncwarp();
+  } else {
+    for (int j = lane; j < have; j += 32) used[row[j]] = 0;
+    if (stay > 0) last_page = row[last_unit];
+    __syncwarp();
+    // in place: entry j comes from kept[j] >= j, and a step of 32 entries reads its sources before it writes
+    for (int j0 = 0; j0 < stay; j0 += 32) {
+      const int j = j0 + lane;
+      const int pg = j < stay ? row[kept[j]] : 0;
+      __syncwarp();
+      if (j < stay) { row[j] = pg; used[pg] = 1; }
+      __syncwarp();
+    }
   }
-  const int grow = max(n_new, 0);
-  if (grow > p.n_slots - first_token) {
-    if (lane == 0) set_dev_status(p.dev_status, NGC_DEV_BAD_COUNTS);
-    return;
+  for (int j = stay + lane; j < have; j += 32) row[j] = -1;
+  const int left = stay == 0 ? 0 : stay * p.page - (last_unit == have - 1 ? have * p.page - len : 0);
+  Settled s = {-1, 0};
+  if (lane == 0) {
+    p.lens[list] = left;
+    s = settle_growth(p, left, n_new, first_token, last_page);
   }
-  if (grow > p.cap * p.page - len) {
-    if (lane == 0) set_dev_status(p.dev_status, NGC_DEV_STRIP_FULL);
-    return;
-  }
-  // the tokens that still fit the last page go where its entry says
-  if (grow > 0 && (len & (p.page - 1)) != 0 && (uint32_t)row[have - 1] >= (uint32_t)p.n_pages) {
-    if (lane == 0) set_dev_status(p.dev_status, NGC_DEV_BAD_PAGE);
-    return;
-  }
-  len_out = len;
-  have_out = have;
-  need_out = ((len + grow + p.page - 1) >> p.page_shift) - have;
+  return s;
+}
+
+// Slot of position pos (-1: none) of sequence b.
+__device__ __forceinline__ int slot_of(const PoolParams& p, int gi, int b, int pos) {
+  if (pos < 0 || !NGC_IN_BOUNDS(p.dev_status, (pos >> p.page_shift) < p.cap)) return -1;
+  return (p.table[((int64_t)b * p.G + gi) * p.cap + (pos >> p.page_shift)] << p.page_shift) + (pos & (p.page - 1));
 }
 
 __global__ void __launch_bounds__(kThreads) pool_update_kernel(PoolParams p) {
   extern __shared__ int sh[];
-  __shared__ int warp_sums[32];
+  __shared__ int warp_sums[kWarps];
+  __shared__ int rows[kWarps][kRowMax];
+  __shared__ uint16_t list[16 * kThreads];
+  __shared__ int n_waiting;
   int* first = sh;                                     // [B+1] new tokens of the sequences before
   int* need = first + p.B + 1;                         // [B+1] pages ...
   int* from = need + p.B + 1;                          // [B] length a sequence grows from, -1: it does not
+  int* waiting = from + p.B;                           // [B / ranks] sequences of this CTA that evict or leave
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank(), n_ranks = (int)cluster.num_blocks();
   const int gi = blockIdx.y;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  uint8_t* const used = p.used + (int64_t)gi * p.n_pages;
+  const bool wide = ((uintptr_t)used & 15) == 0;
 
+  ptx::grid_dep_launch();
   ptx::grid_dep_wait();
+  if (tid == 0) n_waiting = 0;
   // new tokens of the sequences before, failing ones included: the same in every list
   int run = 0;
   for (int b0 = 0; b0 < p.B; b0 += kThreads) {
@@ -178,18 +202,37 @@ __global__ void __launch_bounds__(kThreads) pool_update_kernel(PoolParams p) {
     run += total;
   }
   if (tid == 0) first[0] = 0;
-  __syncthreads();
+  if (n_ranks > 1) cluster.sync(); else __syncthreads();               // (all CTAs have begun: the first's shared memory is there)
+  int* const need0 = n_ranks > 1 ? cluster.map_shared_rank(need, 0) : need;
+  int* const from0 = n_ranks > 1 ? cluster.map_shared_rank(from, 0) : from;
   if (gi == 0 && rank == 0)
     for (int b = tid; b <= p.B; b += kThreads) p.first[b] = first[b];
-
-  if (rank == 0) {
-    uint8_t* used = p.used + (int64_t)gi * p.n_pages;
-    for (int b = warp; b < p.B; b += kWarps) {
-      int len, n, have;
-      settle_sequence(p, gi, b, first[b], len, n, have);
-      if (lane == 0) { from[b] = len; need[b + 1] = n; }
+  // sequences that only grow, a thread each; the others are left to the warps
+  for (int b = rank + n_ranks * tid; b < p.B; b += n_ranks * kThreads) {
+    const int64_t list = (int64_t)b * p.G + gi;
+    const int n_new = p.n_new[b], len = p.lens[list], budget = p.kept ? p.budget[b] : -1;
+    Settled s = {-1, 0};
+    if (len < 0 || len > p.cap * p.page || n_new < -1 || budget < -1 || budget > p.k_max) {
+      set_dev_status(p.dev_status, NGC_DEV_BAD_COUNTS);
+    } else if (budget >= 0 || n_new < 0) {
+      waiting[atomicAdd(&n_waiting, 1)] = b;
+      continue;
+    } else {
+      const int have = (len + p.page - 1) >> p.page_shift;
+      const int last_page = n_new > 0 && (len & (p.page - 1)) != 0 ? p.table[list * p.cap + have - 1] : 0;
+      s = settle_growth(p, len, n_new, first[b], last_page);
     }
-    __syncthreads();
+    from0[b] = s.len;
+    need0[b + 1] = s.need;
+  }
+  __syncthreads();
+  for (int i = warp; i < n_waiting; i += kWarps) {
+    const int b = waiting[i];
+    const Settled s = settle_eviction(p, gi, b, first[b], rows[warp], used);
+    if (lane == 0) { from0[b] = s.len; need0[b + 1] = s.need; }
+  }
+  if (n_ranks > 1) cluster.sync(); else __syncthreads();
+  if (rank == 0) {
     run = 0;
     for (int b0 = 0; b0 < p.B; b0 += kThreads) {
       const int b = b0 + tid;
@@ -201,14 +244,13 @@ __global__ void __launch_bounds__(kThreads) pool_update_kernel(PoolParams p) {
     }
     if (tid == 0) need[0] = 0;
     const int wanted = run;
-    const bool wide = ((uintptr_t)used & 15) == 0;
     __syncthreads();
-    // how many pages are free; sequences beyond the last that fits do not grow
-    int limit = wanted;
     if (wanted > 0) {
-      int mine = 0, n_free;
-      for (int at = 16 * tid; at < p.n_pages; at += 16 * kThreads) mine += __popc(free_mask(used, at, p.n_pages, wide));
-      block_scan(mine, warp_sums, n_free);
+      // how many pages are free; sequences beyond the last that fits do not grow
+      int limit = wanted, here = 0, n_free;
+      uint32_t m = 0;                                  // of this thread's last 16 pages: all it has, in a pool of up to 4096
+      for (int at = 16 * tid; at < p.n_pages; at += 16 * kThreads) here += __popc(m = free_mask(used, at, p.n_pages, wide));
+      block_scan(here, warp_sums, n_free);
       if (n_free < wanted) {
         int best = 0;
         for (int b = tid; b < p.B; b += kThreads) {
@@ -222,49 +264,93 @@ __global__ void __launch_bounds__(kThreads) pool_update_kernel(PoolParams p) {
         limit = warp_sums[0];
         __syncthreads();
       }
-    }
-    run = 0;
-    for (int at0 = 0; run < limit && at0 < p.n_pages; at0 += 16 * kThreads) {
-      const int at = at0 + 16 * tid;
-      uint32_t m = at < p.n_pages ? free_mask(used, at, p.n_pages, wide) : 0u;
-      int total;
-      const int n = __popc(m);
-      int r = run + block_scan(n, warp_sums, total) - n;
-      for (; m != 0 && r < limit; m &= m - 1, ++r) {
-        const int pg = at + __ffs(m) - 1;
-        const int b = find_seq(need, p.B, r);
-        const int entry = ((from[b] + p.page - 1) >> p.page_shift) + r - need[b];
-        if (NGC_IN_BOUNDS(p.dev_status, from[b] >= 0 && entry >= 0 && entry < p.cap)) {
-          p.table[((int64_t)b * p.G + gi) * p.cap + entry] = pg;
-          used[pg] = 1;
+      run = 0;
+      for (int at0 = 0; run < limit && at0 < p.n_pages; at0 += 16 * kThreads) {
+        const int at = at0 + 16 * tid;
+        if (p.n_pages > 16 * kThreads) m = at < p.n_pages ? free_mask(used, at, p.n_pages, wide) : 0u;
+        int total, rk = block_scan(__popc(m), warp_sums, total) - __popc(m);
+        for (; m != 0; m &= m - 1, ++rk) list[rk] = (uint16_t)(16 * tid + __ffs(m) - 1);      // the free pages of this step, in order
+        __syncthreads();
+        for (int k = tid; k < min(total, limit - run); k += kThreads) {
+          const int pg = at0 + list[k], b = find_seq(need, p.B, run + k);
+          const int entry = ((from[b] + p.page - 1) >> p.page_shift) + run + k - need[b];
+          if (NGC_IN_BOUNDS(p.dev_status, from[b] >= 0 && entry >= 0 && entry < p.cap)) {
+            p.table[((int64_t)b * p.G + gi) * p.cap + entry] = pg;
+            used[pg] = 1;
+          }
         }
+        run += total;
+        __syncthreads();
       }
-      run += total;
     }
     for (int b = tid; b < p.B; b += kThreads)
       if (from[b] >= 0 && first[b + 1] > first[b]) p.lens[(int64_t)b * p.G + gi] = from[b] + first[b + 1] - first[b];
   }
-  cluster.sync();                                      // the books are done, and visible to the whole cluster
-  if (rank != 0) {
-    const int* far = cluster.map_shared_rank(from, 0);
-    for (int b = tid; b < p.B; b += kThreads) from[b] = far[b];
+  if (n_ranks > 1) {
+    cluster.sync();                                    // the books are done, and visible to the whole cluster
+    if (rank != 0)
+      for (int b = tid; b < p.B; b += kThreads) from[b] = from0[b];
+    cluster.sync();                                    // (the first CTA's shared memory stays until all have read it)
   }
-  __syncthreads();
-  const int total = min(first[p.B], p.n_slots);
   int32_t* slots = p.slots + (int64_t)gi * p.n_slots;
+  if (p.split) {                                       // many: only each sequence's first, for the second kernel
+    for (int b = rank * kThreads + tid; b < p.B; b += n_ranks * kThreads)
+      if (first[b + 1] > first[b] && first[b] < p.n_slots) slots[first[b]] = slot_of(p, gi, b, from[b]);
+    return;
+  }
   for (int i = rank * kThreads + tid; i < p.n_slots; i += n_ranks * kThreads) {
     int slot = -1;
-    if (i < total) {
+    if (i < first[p.B]) {
       const int b = find_seq(first, p.B, i);
-      if (from[b] >= 0) {
-        const int pos = from[b] + i - first[b];
-        if (NGC_IN_BOUNDS(p.dev_status, (pos >> p.page_shift) < p.cap))
-          slot = (p.table[((int64_t)b * p.G + gi) * p.cap + (pos >> p.page_shift)] << p.page_shift) + (pos & (p.page - 1));
-      }
+      slot = slot_of(p, gi, b, from[b] < 0 ? -1 : from[b] + i - first[b]);
     }
     slots[i] = slot;
   }
-  cluster.sync();                                      // the first CTA's shared memory stays until all have read it
+}
+
+// The slots of many tokens: a warp takes kRun tokens, looks for the first one's sequence and goes on from there.  The first token of
+// every sequence has its slot already, -1 if the sequence did not grow.
+constexpr int kRun = 512;
+__global__ void __launch_bounds__(kThreads) pool_slots_kernel(PoolParams p) {
+  extern __shared__ int first[];
+  ptx::grid_dep_launch();
+  ptx::grid_dep_wait();
+  const int gi = blockIdx.y, lane = threadIdx.x & 31;
+  for (int b = threadIdx.x; b <= p.B; b += kThreads) first[b] = p.first[b];
+  __syncthreads();
+  int32_t* slots = p.slots + (int64_t)gi * p.n_slots;
+  const int total = min(first[p.B], p.n_slots), mask = p.page - 1;
+  const int64_t base = ((int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5)) * kRun;
+  if (base >= p.n_slots) return;
+  // (bound by instructions: what belongs to the sequence is kept from token to token)
+  int b = base < total ? find_seq(first, p.B, (int)base) : 0, end = first[b], start = 0;
+  if (base < total) --b;                                 // (the first token takes the step to its sequence)
+  bool grew = false;
+  const int32_t* row = p.table;
+  int low[kRun / 32], entry[kRun / 32];                  // place in the page, page (-1: no slot)
+#pragma unroll
+  for (int k = 0; k < kRun / 32; ++k) {
+    const int64_t i = base + 32 * k + lane;
+    low[k] = 0;
+    entry[k] = -1;
+    if (i < total) {
+      if ((int)i >= end) {
+        do end = first[++b + 1]; while ((int)i >= end);
+        const int64_t list = (int64_t)b * p.G + gi;
+        grew = slots[first[b]] >= 0;
+        start = p.lens[list] - end;
+        row = p.table + list * p.cap;
+      }
+      const int pos = start + (int)i;
+      low[k] = pos & mask;
+      if (grew && NGC_IN_BOUNDS(p.dev_status, (pos >> p.page_shift) < p.cap)) entry[k] = row[pos >> p.page_shift];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kRun / 32; ++k) {
+    const int64_t i = base + 32 * k + lane;
+    if (i < p.n_slots) slots[i] = entry[k] < 0 ? -1 : (entry[k] << p.page_shift) + low[k];
+  }
 }
 
 // One warp per row: a row of 512 + 64 channels is 72 pieces of 16 bytes.  Bound by HBM.
@@ -305,14 +391,22 @@ extern "C" int ngc_pool_update(ngc_latent_pool* c, const int32_t* kept_sorted, c
   p.B = c->B; p.G = lists_G(c->lists, c->L, 1); p.cap = c->pages_cap; p.n_pages = c->n_pages;
   p.page = c->page; p.page_shift = c->page == 32 ? 5 : 6; p.k_max = kept_sorted ? k_max : 0; p.n_slots = n_slots;
   if (p.G > 65535) return NGC_ERR_UNSUPPORTED;
+  // A cluster per list where there is work for it, evictions or many sequences; as many CTAs as are resident at once.
+  unsigned cluster = 1;
+  if (kept_sorted || p.B > kThreads)
+    while (cluster < 8 && 2 * cluster * p.G <= 2 * 148) cluster *= 2;
+  p.split = n_slots > 4 * kThreads * (int)cluster;     // (four tokens per thread: 281 thousand tokens on 28 layers, 73 us without)
+  const size_t smem = (size_t)(2 * (p.B + 1) + p.B + (p.B + (int)cluster - 1) / (int)cluster) * 4;      // first, need, from, waiting
   static PerDeviceOnce once;
   const int rc = once.run([] {
-    return cudaFuncSetAttribute(pool_update_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (3 * kMaxB + 2) * 4);
+    cudaError_t e = cudaFuncSetAttribute(pool_update_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (4 * kMaxB + 16) * 4);
+    return e == cudaSuccess ? cudaFuncSetAttribute(pool_slots_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (kMaxB + 1) * 4) : e;
   });
   if (rc != NGC_OK) return rc;
-  unsigned cluster = 1;
-  while (cluster < 8 && n_slots > (int)cluster * 4 * kThreads) cluster *= 2;
-  NGC_CUDA_TRY(launch_pdl_cluster(pool_update_kernel, dim3(cluster, p.G), dim3(kThreads), cluster, (3 * (size_t)p.B + 2) * 4, stream, p));
+  NGC_CUDA_TRY(launch_pdl_cluster(pool_update_kernel, dim3(cluster, p.G), dim3(kThreads), cluster, smem, stream, p));
+  if (p.split)
+    NGC_CUDA_TRY(launch_pdl(pool_slots_kernel, dim3((unsigned)(((int64_t)n_slots + kWarps * kRun - 1) / (kWarps * kRun)), p.G), dim3(kThreads),
+                            (size_t)(p.B + 1) * 4, stream, p));
   return launch_status();
 }
 

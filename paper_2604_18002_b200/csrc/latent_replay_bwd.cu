@@ -602,7 +602,7 @@ __global__ void __launch_bounds__(256) latent_grad_rope_kernel(LatentReplayParam
 
 int launch_latent_bwd(const LatentReplayParams& p, cudaStream_t stream) {
   const int64_t items = ((int64_t)p.max_len + kLatTile - 1) / kLatTile * p.L * p.B * p.H;
-  if (items > 0x7fffff00LL) return NGC_ERR_UNSUPPORTED;
+  if (items > 0x7fff0000LL) return NGC_ERR_UNSUPPORTED;
   const int64_t rows = (int64_t)p.L * p.rows;
   Maps mq, mk;
   if (!make_token_map(&mq.q, p.q, kLatNope + p.dr, p.H, rows, kLatTile) || !make_token_map(&mq.kv, p.kv, kLatNope + kLatV, p.H, rows, kLatTile) ||

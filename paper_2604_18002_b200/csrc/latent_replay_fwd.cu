@@ -386,7 +386,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_fwd_kernel(const __grid_co
 
 int launch_latent_fwd(const LatentReplayParams& p, cudaStream_t stream) {
   const int64_t blocks = ((int64_t)p.max_len + 2 * kLatTile - 1) / (2 * kLatTile), items = blocks * p.L * p.B * p.H;
-  if (items > 0x7fffff00LL) return NGC_ERR_UNSUPPORTED;
+  if (items > 0x7fff0000LL) return NGC_ERR_UNSUPPORTED;
   Maps maps;
   const int64_t rows = (int64_t)p.L * p.rows;
   if (!make_token_map(&maps.q, p.q, kLatNope + p.dr, p.H, rows, kLatTile) || !make_token_map(&maps.kv, p.kv, kLatNope + kLatV, p.H, rows, kLatTile) ||
