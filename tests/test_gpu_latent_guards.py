@@ -270,7 +270,7 @@ def test_eviction_of_rows_longer_than_a_warps_buffer():
     for s in range(B):
         for g in range(2):
             last = [have[s, g] - 1] if (s, g) == (0, 0) else []              # a short last page stays last
-            kept[s, g, : budget[s]] = np.sort(list(rng.permutation(have[s, g] - 1)[: budget[s] - len(last)]) + last)
+            kept[s, g, : budget[s]] = np.sort(list(rng.permutation(max(have[s, g] - 1, 1))[: budget[s] - len(last)]) + last)
     assert run_update(pool, [1, 40, 3], 50, kept, budget) == set()
 
 
