@@ -53,9 +53,9 @@ __global__ void __launch_bounds__(kSpan) latent_gone_kernel(LatentReplayParams p
   if ((tid & 31) == 0) warps[tid >> 5] = make_int2(lo, hi);
   __syncthreads();
   if (tid < kSpan / kLatTile && t0 + tid * kLatTile < T) {
-    int2 x = warps[4 * tid];
-    for (int k = 1; k < 4; ++k) { x.x = min(x.x, warps[4 * tid + k].x); x.y = max(x.y, warps[4 * tid + k].y); }
-    p.tile_gone[list * (p.gone_cap / kLatTile) + t0 / kLatTile + tid] = x;
+    const int2* w = warps + 4 * tid;
+    p.tile_gone[list * (p.gone_cap / kLatTile) + t0 / kLatTile + tid] =
+        make_int4(min(w[0].x, w[1].x), max(w[0].y, w[1].y), min(w[2].x, w[3].x), max(w[2].y, w[3].y));
   }
 }
 
@@ -116,7 +116,7 @@ Space space_of(const ngc_latent_seqs* s, int lists, int n_rounds, int backward) 
   size_t at = 0;
   if (n_rounds > 0) {
     w.gone = at; at += align256(BG * gone_cap(s) * 4);
-    w.tiles = at; at += align256(BG * (gone_cap(s) / kLatTile) * 8);
+    w.tiles = at; at += align256(BG * (gone_cap(s) / kLatTile) * 16);
   }
   if (backward) {
     w.delta = at; at += align256((size_t)s->L * s->H * s->rows * 4);
@@ -143,7 +143,7 @@ int prepare(const ngc_latent_seqs* s, const void* q, const void* kv, const void*
   p->seq_off = s->seq_off; p->lens = s->lens; p->rows = s->rows;
   p->q = (const __nv_bfloat16*)q; p->kv = (const __nv_bfloat16*)kv; p->kr = (const __nv_bfloat16*)k_rope;
   p->alive_pos = alive_pos; p->alive_count = alive_count; p->total_before = total_before;
-  if (n_rounds > 0) { p->gone = (int32_t*)(base + w.gone); p->tile_gone = (int2*)(base + w.tiles); }
+  if (n_rounds > 0) { p->gone = (int32_t*)(base + w.gone); p->tile_gone = (int4*)(base + w.tiles); }
   if (backward) { p->delta = (float*)(base + w.delta); p->dkr_part = (float*)(base + w.dkr); }
   p->L = s->L; p->B = s->B; p->H = s->H; p->G = lists_G(lists, s->L, 1); p->dr = s->d_rope; p->lists = lists; p->n_rounds = n_rounds;
   p->kt_max = kt_max; p->max_len = s->max_len; p->gone_cap = gone_cap(s); p->out_bf16 = out_dtype == NGC_BF16;

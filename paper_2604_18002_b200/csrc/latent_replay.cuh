@@ -23,7 +23,7 @@ struct LatentReplayParams {
   const int32_t* alive_count;
   const int32_t* total_before;
   int32_t* gone;                // [B][G][gone_cap] sequence length at the round that evicted each token; null: no rounds
-  int2* tile_gone;              // [B][G][gone_cap / 128] smallest and largest of a tile of 128 tokens
+  int4* tile_gone;              // [B][G][gone_cap / 128] of a tile of 128 tokens: smallest and largest of its first 64, of its others
   void* out;                    // [L][rows][H][128]
   float* lse;                   // [L][H][rows] or null
   const __nv_bfloat16* go;      // gradient of out

@@ -78,7 +78,7 @@ struct Deal {
 constexpr int kPlans = 4, kPlanWindows = 8;
 struct ReplayPlan {
   int valid, l, b, h, x0, T, n;                // first token of the item's block; query walks: key tiles, key walks: query tiles
-  uint32_t live[kPlanWindows], plain_a[kPlanWindows], plain_b[kPlanWindows];     // query walks: see there, of the first 256 tiles
+  uint32_t lower[kPlanWindows], upper[kPlanWindows], plain_a[kPlanWindows], plain_b[kPlanWindows];       // query walks: see there, of the first 256 tiles
   int64_t row0;                                // first row of the sequence, within a layer
 };
 struct PlanRing {
@@ -108,7 +108,7 @@ struct WalkEnv {
     const bool odd = threadIdx.x & 1;
     return umma::warp_wait(odd ? bar1 : bar0, odd ? parity1 : parity0, abort, p.dev_status);
   }
-  __device__ __forceinline__ const int2* tiles(int l, int b) const {
+  __device__ __forceinline__ const int4* tiles(int l, int b) const {
     return p.tile_gone ? p.tile_gone + ((int64_t)b * p.G + list_of(p.lists, l, 0, 1)) * (p.gone_cap / kLatTile) : nullptr;
   }
 };
@@ -118,34 +118,41 @@ template <int BLOCKS> struct QueryWalk {
   int k;                        // items so far
   int l, b, h, q0, T, n;        // the current item; its key tiles are 0 .. n - 1
   int64_t row0;
-  const int2* tiles;            // of its list, or null
+  const int4* tiles;            // of its list, or null
   int i, window;                // current tile, first tile of the window
-  uint32_t live, plain_a, plain_b;             // of the window: tiles that a query sees; ones without a key that goes before query block A's (B's) last
+  uint32_t live, lower, upper;                 // of the window: tiles still to come that a query sees; of those, whether it sees the first 64 keys, the others
+  uint32_t plain_a, plain_b;                   // ones without a key that goes before query block A's (B's) last
   bool first;                   // the current tile is the item's first
 
-  __device__ __forceinline__ QueryWalk() : k(0), n(0), i(0), window(0), live(0), plain_a(0), plain_b(0) {}
+  __device__ __forceinline__ QueryWalk() : k(0), n(0), i(0), window(0), live(0), lower(0), upper(0), plain_a(0), plain_b(0) {}
   __device__ __forceinline__ bool has_b() const { return BLOCKS == 2 && q0 + kLatTile < T; }
   __device__ __forceinline__ bool for_a() const { return i * kLatTile <= q0; }
   __device__ __forceinline__ bool last_a() const { return i * kLatTile == q0; }
   __device__ __forceinline__ bool last() const { return i == n - 1; }
   // Masks of the window: by all lanes, or (ALONE) by one thread.
   template <bool ALONE> __device__ __forceinline__ void load_window() {
+    auto look = [&](int t, bool& lo, bool& up, bool& pa, bool& pb) {
+      int4 g = make_int4(kNeverGone, kNeverGone, kNeverGone, kNeverGone);
+      if (tiles && t < n) g = tiles[t];
+      lo = t < n && g.y > q0;
+      up = t < n && g.w > q0 && t * kLatTile + 64 < T;
+      pa = min(g.x, g.z) > q0 + kLatTile - 1;
+      pb = min(g.x, g.z) > q0 + 2 * kLatTile - 1;
+    };
+    bool lo, up, pa, pb;
     if (ALONE) {
-      live = plain_a = plain_b = 0;
+      lower = upper = plain_a = plain_b = 0;
       for (int t = window; t < min(window + 32, n); ++t) {
-        const int2 g = tiles ? tiles[t] : make_int2(kNeverGone, kNeverGone);
-        live |= (uint32_t)(g.y > q0) << (t - window);
-        plain_a |= (uint32_t)(g.x > q0 + kLatTile - 1) << (t - window);
-        plain_b |= (uint32_t)(g.x > q0 + 2 * kLatTile - 1) << (t - window);
+        look(t, lo, up, pa, pb);
+        lower |= (uint32_t)lo << (t - window); upper |= (uint32_t)up << (t - window);
+        plain_a |= (uint32_t)pa << (t - window); plain_b |= (uint32_t)pb << (t - window);
       }
     } else {
-      const int t = window + (threadIdx.x & 31);
-      int2 g = make_int2(kNeverGone, kNeverGone);
-      if (tiles && t < n) g = tiles[t];
-      live = __ballot_sync(0xffffffffu, t < n && g.y > q0);
-      plain_a = __ballot_sync(0xffffffffu, g.x > q0 + kLatTile - 1);
-      plain_b = __ballot_sync(0xffffffffu, g.x > q0 + 2 * kLatTile - 1);
+      look(window + (threadIdx.x & 31), lo, up, pa, pb);
+      lower = __ballot_sync(0xffffffffu, lo); upper = __ballot_sync(0xffffffffu, up);
+      plain_a = __ballot_sync(0xffffffffu, pa); plain_b = __ballot_sync(0xffffffffu, pb);
     }
+    live = lower | upper;
   }
   // The planner's part.
   __device__ __forceinline__ bool plan(const WalkEnv& e, Deal& deal) {
@@ -162,7 +169,7 @@ template <int BLOCKS> struct QueryWalk {
     for (int w = 0; w < kPlanWindows && 32 * w < n; ++w) {
       window = 32 * w;
       load_window<false>();
-      if (one) { r.live[w] = live; r.plain_a[w] = plain_a; r.plain_b[w] = plain_b; }
+      if (one) { r.lower[w] = lower; r.upper[w] = upper; r.plain_a[w] = plain_a; r.plain_b[w] = plain_b; }
     }
   }
   // The other roles', by all lanes of a warp or by one thread alone.  (An item's plan is held until its last tile has been passed.)
@@ -175,7 +182,7 @@ template <int BLOCKS> struct QueryWalk {
       const ReplayPlan& r = e.ring->plan[k % kPlans];
       ++k;
       if (!r.valid) return false;
-      l = r.l; b = r.b; h = r.h; q0 = r.x0; T = r.T; n = r.n; row0 = r.row0; live = r.live[0]; plain_a = r.plain_a[0]; plain_b = r.plain_b[0];
+      l = r.l; b = r.b; h = r.h; q0 = r.x0; T = r.T; n = r.n; row0 = r.row0; take(r, 0);
       tiles = e.tiles(l, b);
       window = 0;
       first = true;
@@ -186,12 +193,18 @@ template <int BLOCKS> struct QueryWalk {
     i = window + at;
     return true;
   }
+  __device__ __forceinline__ void take(const ReplayPlan& r, int w) {
+    lower = r.lower[w]; upper = r.upper[w]; plain_a = r.plain_a[w]; plain_b = r.plain_b[w];
+    live = lower | upper;
+  }
+  // Which halves of the current tile are seen: bit 0 the first 64 keys, bit 1 the others.
+  __device__ __forceinline__ int halves() const { return (lower >> (i - window) & 1) | (upper >> (i - window) & 1) << 1; }
   template <bool ALONE> __device__ __forceinline__ void advance(const WalkEnv& e) {
     while (live == 0 && window + 32 < n) {
       window += 32;
       if (window < 32 * kPlanWindows) {
         const ReplayPlan& r = e.ring->plan[(k - 1) % kPlans];
-        live = r.live[window / 32]; plain_a = r.plain_a[window / 32]; plain_b = r.plain_b[window / 32];
+        take(r, window / 32);
       } else {
         load_window<ALONE>();
       }
@@ -202,20 +215,24 @@ template <int BLOCKS> struct QueryWalk {
 // The same by tiles of 64 keys, one block of queries per item.
 struct HalfWalk {
   QueryWalk<1> w;
-  int k0;                       // first key
-  bool begun, upper, first, last;
+  int k0, pending;              // first key; halves of w's tile still to come
+  bool fresh, first, last;      // fresh: no tile of the item has been taken
 
-  __device__ __forceinline__ HalfWalk() : begun(false), upper(false) {}
-  __device__ __forceinline__ bool has_upper() const { return w.i * kLatTile + 64 < min(w.T, w.q0 + kLatTile); }
+  __device__ __forceinline__ HalfWalk() : pending(0), fresh(false) {}
   __device__ __forceinline__ bool plan(const WalkEnv& e, Deal& deal) { return w.plan(e, deal); }
   __device__ __forceinline__ void publish(ReplayPlan& r) { w.publish(r); }
   template <bool ALONE = false> __device__ __forceinline__ bool next(const WalkEnv& e) {
-    upper = begun && !upper && has_upper();
-    if (!upper && !w.next<ALONE>(e)) return false;
-    begun = true;
-    k0 = w.i * kLatTile + (upper ? 64 : 0);
-    first = w.first && !upper;
-    last = w.last() && (upper || !has_upper());
+    if (pending == 0) {
+      if (!w.next<ALONE>(e)) return false;
+      pending = w.halves();
+      fresh = fresh || w.first;
+    }
+    const bool up = !(pending & 1);
+    pending &= pending - 1;
+    k0 = w.i * kLatTile + (up ? 64 : 0);
+    first = fresh;
+    fresh = false;
+    last = w.last() && pending == 0;
     return true;
   }
 };
@@ -235,8 +252,8 @@ struct KeyWalk {
     if (!deal.next(e.p, l, b, h)) return false;
     j0 = deal.m * kLatTile;
     T = latent_seq(e.p, b, row0);
-    const int2* tiles = e.tiles(l, b);
-    const int end = tiles ? min(T, tiles[j0 / kLatTile].y) : T;
+    const int4* tiles = e.tiles(l, b);
+    const int end = tiles ? min(T, max(tiles[j0 / kLatTile].y, tiles[j0 / kLatTile].w)) : T;
     n = (end + kQ - 1) / kQ;                             // (a key sees to its own query at least: one tile or more)
     return true;
   }
