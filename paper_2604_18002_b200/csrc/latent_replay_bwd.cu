@@ -3,15 +3,23 @@
 // With the forward pass's lse and D = sum over channels of out * grad_out, P = exp(z - lse) and dz = P (dP - D), dP = dO V^T
 // (the scale of z is applied to the finished sums).  Two kernels, each of which computes S and dP again, so that every sum lies in one
 // CTA's tensor memory: no atomics, the same bits in every run.
-//   queries   an item is 128 queries of a head; over its tiles of 64 keys: S = Q K^T, dP = dO V^T, dQ += dZ K (two buffers of each
-//             fill tensor memory; with 128 keys two stages of K were too few: XX us)
+//   queries   an item is 128 queries of a head; over its tiles of 64 keys: S = Q K^T, dP = dO V^T, dQ += dZ K.  Q and dO are copied to
+//             tensor memory once per item and are A operands there, so the products read shared memory for keys and values alone, and
+//             four tiles of K and three of V fit (tiles of 128 keys left room for two: rollouts of 8192 tokens 1126 -> 1151 us).
+//             Tiles of 64 keys that no query of the item sees are passed over
 //   keys      an item is 128 keys of a head; over the tiles of 64 queries that see them: S^T = K Q^T, dP^T = V dO^T,
 //             dV += P^T dO, dK += dZ^T Q.  Keys are the lanes of tensor memory, so what a query sees is one range of columns per
 //             thread.  64 queries because dV, dK (320 columns), S^T, dP^T and the bf16 P^T, dZ^T fill tensor memory
 // P and dZ are A operands in tensor memory, in columns of their own: the scores of the next tile are computed while the softmax
 // warps work on this one.  The head's share of the rotary keys' gradient goes to the workspace in fp32; a last kernel sums the heads
 // in order.  Roles as in the forward pass: producers by TMA, a mender (rows behind a sequence's end are zeroed where they are
-// summed over), the MMA warp, eight softmax warps (two per quarter of the lanes, half of the columns each).
+// summed over), one thread that issues all products, eight softmax warps (two per quarter of the lanes, half of the columns each; 16 warps
+// changed nothing: 1016 -> 1012 us for the queries', 1028 for the keys').
+//
+// Bound by the tensor pipe and the hand-overs around it: causal, 4096 tokens of 16 heads, batch 2, the keys' kernel takes 342 us with the
+// tensor pipe 73 % busy (a product of 128 x 64 reads its A operand, keys or values, from shared memory again for every tile, and dV,
+// dK, S and dP leave tensor memory no room for it), the queries' 275 us with 57 % (S and dP have one buffer: dQ, Q and dO fill the
+// rest).  8192 tokens: 2180 us, 820 TFLOP/s of the five products that the gradient needs; seven are computed.
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -579,6 +587,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_grad_kv_kernel(const __gri
 
 // ------------------------------------------------------------------------------------------- the heads' shares of the rotary keys
 
+// Four channels of a token per thread, heads in order.  Bound by HBM: 60 MB in 12 us for 14.7 thousand tokens of 16 heads (5 TB/s).
 __global__ void __launch_bounds__(256) latent_grad_rope_kernel(LatentReplayParams p) {
   const int b = blockIdx.y % p.B, l = blockIdx.y / p.B, per = p.dr / 4;
   int64_t row0;
