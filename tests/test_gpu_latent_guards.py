@@ -8,7 +8,7 @@ import test_gpu_latent as t_lat
 from helpers import ngc, status_value
 from oracle import latent as ora
 from test_gpu_debug_build import debug_library      # noqa: F401
-from test_gpu_latent import Replay, assert_within, bf16, f32, history, host, normal, random_pool, run_decode, run_update
+from test_gpu_latent import Replay, assert_within, bf16, device_history, f32, history, host, normal, random_pool, run_decode, run_update
 
 pytestmark = pytest.mark.gpu
 
@@ -228,6 +228,31 @@ def test_replay_of_random_shapes(seed):
     lens[0] += 1
     rounds = None if seed % 3 == 0 else [(f, float(rng.uniform(0, 1))) for f in np.sort(rng.uniform(0.05, 1, int(rng.integers(1, 6))))]
     r = Replay(L, B, H, dr, lens, int(rng.integers(0, 3)), 300 + seed, rounds, int(rng.integers(0, 3)), int(rng.choice([1, 4, 32])))
+    r.forward(f32 if seed % 2 else bf16)
+    r.backward()
+    assert status_value(r.st) == 0
+    r.check_forward()
+    r.check_backward()
+
+
+@pytest.mark.parametrize("seed", range(3))
+def test_histories_that_leave_halves_of_tiles(seed):
+    """Rounds that keep or drop 64 keys at a time, at moments inside a block of queries: tiles of which only the first half is left,
+    only the second, a few keys of one, none; more items than SMs."""
+    rng = np.random.default_rng(400 + seed)
+    lens, H = [1400, 1337, 1281, 1410], 8
+    r = Replay(1, len(lens), H, 64, lens, 1, 410 + seed, [(0.5, 0.5)])
+    r.hist = []
+    for n in lens:
+        alive, at, rounds = np.zeros(0, np.int64), 0, []
+        for fired in (655, 700 + 7 * seed, 1024, 1279):
+            alive = np.concatenate([alive, np.arange(at, fired)])
+            at = fired
+            share = rng.choice([0.0, 0.0, 1.0, 1.0, 0.05], fired // 64 + 1)           # of every 64 keys
+            alive = alive[rng.random(len(alive)) < share[alive // 64]]
+            rounds.append((fired, alive))
+        r.hist.append([rounds])
+    r.alive = device_history(r.hist, len(lens), 1)
     r.forward(f32 if seed % 2 else bf16)
     r.backward()
     assert status_value(r.st) == 0
