@@ -620,12 +620,12 @@ typedef struct {
  * in order of sequences.  Token t of sequence b's new ones is number first[b] + t.
  *   n_new [B];  kept_sorted [B][G][k_max] as written by ngc_sample_evict, budget [B], or both NULL
  *   slots [G][n_slots] out: page * (tokens per page) + place in the page of every new token; -1 from first[B] on
- *   first [B+1] out: new tokens of the sequences before
+ *   first [B+1] out: new tokens of the sequences before (2^30 - 1 where there are more)
  * Per list, a sequence with counts that are none (NGC_DEV_BAD_COUNTS: also more
  * new tokens than n_slots holds), a bad kept list (NGC_DEV_BAD_KEPT) or page-table entry
  * (NGC_DEV_BAD_PAGE) is left as it was; one that outgrows pages_cap
  * (NGC_DEV_STRIP_FULL) or the free pages (NGC_DEV_POOL_FULL) evicts but does
- * not grow.  Their new tokens get slot -1.  B <= 8192.
+ * not grow.  Their new tokens get slot -1.  B <= 8192, n_slots < 2^30.
  */
 int ngc_pool_update(ngc_latent_pool* c, const int32_t* kept_sorted, const int32_t* budget, int k_max, const int32_t* n_new,
                     int32_t* slots, int n_slots, int32_t* first, int32_t* dev_status, ngc_stream stream);

@@ -21,7 +21,7 @@ def pool_update(table, used, lens, page, n_new, n_slots, kept=None, budget=None)
     table, used, lens = table.copy(), used.copy(), lens.copy()
     B, G, cap = table.shape
     n_pages = used.shape[1]
-    first = np.concatenate([[0], np.cumsum(np.maximum(n_new, 0))]).astype(np.int32)
+    first = np.concatenate([[0], np.minimum(np.cumsum(np.maximum(n_new, 0).astype(np.int64)), 2 ** 30 - 1)]).astype(np.int32)
     slots = np.full((G, n_slots), -1, np.int32)
     problems = set()
     for g in range(G):

@@ -37,13 +37,16 @@ struct PoolParams {
   int split;                   // the slots are left to a kernel of their own
 };
 
-// Inclusive sum over the CTA's threads; `total` gets the sum of all.  Two barriers.
+// Inclusive sum over the CTA's threads; `total` gets the sum of all.  Two barriers.  Sums stop at kMost, so counts that are no
+// counts cannot wrap around and pass for small ones: what lies behind them has no slot.
+constexpr int kMost = 0x3fffffff;
+__device__ __forceinline__ int add(int a, int b) { return min(a + b, kMost); }                 // of 0 .. kMost
 __device__ __forceinline__ int block_scan(int v, int* warp_sums, int& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int u = __shfl_up_sync(0xffffffffu, v, o);
-    if (lane >= o) v += u;
+    if (lane >= o) v = add(v, u);
   }
   if (lane == 31) warp_sums[warp] = v;
   __syncthreads();
@@ -52,11 +55,11 @@ __device__ __forceinline__ int block_scan(int v, int* warp_sums, int& total) {
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) {
     const int u = warp_sums[w];
-    before += w < warp ? u : 0;
-    total += u;
+    before = add(before, w < warp ? u : 0);
+    total = add(total, u);
   }
   __syncthreads();
-  return v + before;
+  return add(v, before);
 }
 
 // Last b with sum[b] <= x, for 0 <= x < sum[B] (sequences without a share never are the answer).
@@ -196,11 +199,11 @@ __global__ void __launch_bounds__(kThreads) pool_update_kernel(PoolParams p) {
   int run = 0;
   for (int b0 = 0; b0 < p.B; b0 += kThreads) {
     const int b = b0 + tid;
-    const int n = b < p.B ? max(p.n_new[b], 0) : 0;
+    const int n = b < p.B ? min(max(p.n_new[b], 0), kMost) : 0;
     int total;
     const int incl = block_scan(n, warp_sums, total);
-    if (b < p.B) first[b + 1] = run + incl;
-    run += total;
+    if (b < p.B) first[b + 1] = add(run, incl);
+    run = add(run, total);
   }
   if (tid == 0) first[0] = 0;
   if (n_ranks > 1) cluster.sync(); else __syncthreads();               // (all CTAs have begun: the first's shared memory is there)
@@ -386,7 +389,7 @@ extern "C" int ngc_pool_update(ngc_latent_pool* c, const int32_t* kept_sorted, c
   if (!valid_latent_pool(c) || !n_new || !slots || n_slots < 1 || !first || (kept_sorted == nullptr) != (budget == nullptr) ||
       (kept_sorted && k_max < 1))
     return NGC_ERR_INVALID_ARG;
-  if (c->B > kMaxB) return NGC_ERR_UNSUPPORTED;
+  if (c->B > kMaxB || n_slots > kMost) return NGC_ERR_UNSUPPORTED;
   PoolParams p;
   p.table = c->page_table; p.used = c->page_used; p.lens = c->lens;
   p.kept = kept_sorted; p.budget = budget; p.n_new = n_new; p.slots = slots; p.first = first; p.dev_status = dev_status;

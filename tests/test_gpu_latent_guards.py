@@ -306,6 +306,19 @@ def test_slots_of_many_tokens_with_sequences_that_do_not_grow(n_new, n_slots):
     assert run_update(pool, [1, -1, -1, 200, 0, 3000], n_slots) <= {ora.POOL_FULL, ora.STRIP_FULL}
 
 
+@pytest.mark.parametrize("n_slots", [40, 9000])
+def test_counts_whose_sum_passes_32_bits_get_no_slots(n_slots):
+    big = 2 ** 31 - 1
+    for n_new in ([big, big, 5, 3, 0, 7], [4, big, big, 5, 3, -1], [2 ** 30, 2 ** 30, 2 ** 30, 2 ** 30, 5, 3], [big] * 6):
+        pool = random_pool(2, 6, 32, 8, 60, [[50, 40], [64, 64], [10, 33], [0, 0], [96, 90], [33, 33]], 1, 7)
+        assert run_update(pool, n_new, n_slots) <= {ora.BAD_COUNTS}
+    B = 700                                                                    # more than a pass over the sequences takes
+    pool = random_pool(2, B, 32, 2, 1500, np.full((B, 2), 20), 1, 8)
+    n_new = np.ones(B, np.int64)
+    n_new[100:400] = big
+    assert run_update(pool, n_new, n_slots) == {ora.BAD_COUNTS}
+
+
 # ------------------------------------------------------------------ numbers
 
 def test_nan_and_infinities_in_alive_rows_stay_with_their_sequence_and_heads():

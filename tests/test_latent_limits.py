@@ -46,6 +46,7 @@ def test_arguments_of_pool_update_and_write_are_refused(ngc):
                                                              (None, None, 0, 16, 16, 0, 16), (None, None, 0, 16, 16, 4, None)]:
         assert lib.ngc_pool_update(c, kept, budget, k_max, n_new, slots, n_slots, first, None, None) == -1
     assert lib.ngc_pool_update(C.byref(pool(ngc, B=8193)), None, None, 0, 16, 16, 4, 16, None, None) == -2
+    assert lib.ngc_pool_update(c, None, None, 0, 16, 16, 2 ** 30, 16, None, None) == -2
     for args in [(None, 4, 16, 16, 0, 1), (16, 0, 16, 16, 0, 1), (16, 4, None, 16, 0, 1), (16, 4, 16, None, 0, 1), (16, 4, 16, 16, 1, 1), (16, 4, 16, 16, -1, 1),
                  (16, 4, 16, 16, 0, 3), (16, 4, 24, 16, 0, 1), (16, 4, 16, 20, 0, 1)]:
         assert lib.ngc_latent_write(c, *args, None, None) == -1
