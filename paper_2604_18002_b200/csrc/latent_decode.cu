@@ -14,7 +14,8 @@
 //   producers (2 warps)   the tile's rows by TMA, a box of 64 channels per page, into a ring of stages; a warp per page of a tile
 //   mender (1 warp)       rows behind a unit's last token: zeros (they may hold anything; a NaN times a zero weight is NaN)
 //   queries (1 thread)    the heads' queries of the next unit, when the last unit's scores are done
-//   MMA (1 thread)        whatever is ready: S^T of the next tile, which runs under the softmax of this one, or this one's sums
+//   scores (1 thread)     S^T of the next tile, pair of 128 channels by pair as they come; it runs under the softmax of this one
+//   sums (1 thread)       O^T; a pair of channels whose products are done makes room for the next tile but one's
 //   softmax (4 or 8 warps) 16 tokens each.  A thread holds two tokens of four heads; weights go to shared memory
 //                         by transposing matrix stores, as the K-major B operand.  The maximum that the exponentials refer to
 //                         moves only when a score exceeds it by 2^8 (exact in bf16 and fp32), which is one vote per tile.
@@ -22,8 +23,9 @@
 //
 // 64 sequences of 1024 to 4096 tokens, 16 heads of 512 + 64 channels, one layer: 52 us with the second kernel, 3.7 TB/s; beginning,
 // first tile and joining are most of the 13 us that a call of one sequence takes.  24 sequences of 2048 to 8192, 128 heads, two
-// layers: 126 us, 543 TFLOP/s: the queries of 64 heads leave shared memory room for two tiles, so loads, scores, softmax and sums of
-// a tile (3 to 4 us) overlap with those of one other, and every row is fetched from L2 by both groups of heads.
+// layers: 125 us, 548 TFLOP/s: the queries of 64 heads leave shared memory room for two tiles.  A tile holds its place for some 5500 cycles:
+// 1700 until its first rows are there, 1400 until the last, 1850 of softmax and its hand-overs, 800 of sums; with every row in L2 the
+// call takes 108 us.
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -40,10 +42,10 @@ constexpr int kBox = kTile * 128;              // 64 tokens x 64 channels
 constexpr int kPair = 2 * kBox;                // 128 channels of the latent part: what arrives, is used and makes room together
 constexpr int kMaxPairs = 9, kMaxStages = 4;  // in shared memory, at most
 // Warps: softmax, four for 16 heads, else eight (a warp reaches a quarter of tensor memory's lanes; 16 for 64 heads: 147 -> 157 us
-// for 24 sequences of two layers, 128 heads), then one each for the MMAs, the first and
-// the second page of a tile, the mender, the queries.
+// for 24 sequences of two layers, 128 heads), then one each for the scores, the first and
+// the second page of a tile, the mender, the queries, the sums (scores and sums issued by one thread as they came: 1 to 2 % slower).
 __host__ __device__ constexpr int softmax_warps(int nh) { return nh < 32 ? 4 : 8; }
-__host__ __device__ constexpr int cta_threads(int nh) { return (softmax_warps(nh) + 5) * 32; }
+__host__ __device__ constexpr int cta_threads(int nh) { return (softmax_warps(nh) + 6) * 32; }
 constexpr int kSmemLimit = 227 * 1024;
 constexpr int kStaticReserve = 2048;           // barriers and exchange buffers (static shared memory)
 constexpr float kLazy = 8.f;
@@ -66,7 +68,7 @@ struct Maps { CUtensorMap rows, ql, qr; };
 
 template <int NH> struct Shared {
   uint64_t full[kMaxPairs], empty[kMaxPairs], raw[kMaxPairs], r_full[kMaxStages], r_empty[kMaxStages];
-  uint64_t s_full[2], p_full, o_done, q_full, q_empty, drain;
+  uint64_t s_full[2], s_free[2], p_full, o_done, q_full, q_empty, drain;
   uint32_t tmem;
   int abort;
   int u0, t0, len0, g0, n_tiles, total;        // where this CTA's piece begins, how many tiles it has, tiles of the call
@@ -143,7 +145,7 @@ template <int N> __device__ __forceinline__ void softmax_sync() { asm volatile("
 template <int NH, int DC>
 __global__ void __launch_bounds__(cta_threads(NH), 1) latent_decode_kernel(const __grid_constant__ Maps maps, LatentDecodeParams p) {
   constexpr int kSoft = softmax_warps(NH), kThreads = cta_threads(NH);
-  constexpr int kMmaWarp = kSoft, kProducerWarp = kSoft + 1, kMenderWarp = kSoft + 3, kQueryWarp = kSoft + 4;
+  constexpr int kScoreWarp = kSoft, kProducerWarp = kSoft + 1, kMenderWarp = kSoft + 3, kQueryWarp = kSoft + 4, kSumWarp = kSoft + 5;
   extern __shared__ uint8_t smem_dyn[];
   __shared__ Shared<NH> sh;
   uint8_t* sQ = (uint8_t*)(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);     // [chunks][NH rows x 128 B]
@@ -161,16 +163,17 @@ __global__ void __launch_bounds__(cta_threads(NH), 1) latent_decode_kernel(const
     if (lane < p.stages) { ptx::mbar_init(&sh.r_full[lane], kTile / p.page); ptx::mbar_init(&sh.r_empty[lane], 1); }
     if (lane == 31) {
       ptx::mbar_init(&sh.s_full[0], 1); ptx::mbar_init(&sh.s_full[1], 1);
+      ptx::mbar_init(&sh.s_free[0], kSoft); ptx::mbar_init(&sh.s_free[1], kSoft);
       ptx::mbar_init(&sh.p_full, kSoft);
       ptx::mbar_init(&sh.o_done, 1);
-      ptx::mbar_init(&sh.q_full, 1); ptx::mbar_init(&sh.q_empty, 1); ptx::mbar_init(&sh.drain, 1);
+      ptx::mbar_init(&sh.q_full, 1); ptx::mbar_init(&sh.q_empty, 1); ptx::mbar_init(&sh.drain, 2);
       sh.abort = 0; sh.u0 = 0; sh.t0 = 0; sh.len0 = 0;
     }
     ptx::fence_barrier_init();
   } else if (warp == kProducerWarp && lane == 0) {
     ptx::prefetch_tensormap(&maps.rows); ptx::prefetch_tensormap(&maps.ql); ptx::prefetch_tensormap(&maps.qr);
   }
-  if (warp == kMmaWarp) umma::tmem_alloc(&sh.tmem, kCols);
+  if (warp == kScoreWarp) umma::tmem_alloc(&sh.tmem, kCols);
   ptx::grid_dep_wait();
   // ---- the line of tiles, and where this piece begins: every thread sums a run of units
   {
@@ -328,77 +331,76 @@ __global__ void __launch_bounds__(cta_threads(NH), 1) latent_decode_kernel(const
     }
     if (k > 0) ptx::mbar_wait_bounded(&sh.q_full, (k - 1) & 1);
     __syncwarp();
-  } else if (warp == kMmaWarp) {
-    // ------------------------------------------------------------------ products
-    // One elected thread does it all: the compiler keeps descriptors in uniform registers then (with `lane == 0` a product took 90
+  } else if (warp == kScoreWarp) {
+    // ------------------------------------------------------------------ scores
+    // One elected thread issues them: the compiler keeps descriptors in uniform registers then (with `lane == 0` a product took 90
     // cycles to issue and the CTA 4500 per tile), and nothing is spent on meeting the warp again.
     if (n_tiles > 0 && umma::elect_one()) {
-      constexpr uint32_t idesc_s = umma::instr_desc(64, NH, false);
-      constexpr uint32_t idesc_o = umma::instr_desc(128, NH, false, true);
+      constexpr uint32_t idesc = umma::instr_desc(64, NH, false);
       const uint64_t hi = (uint64_t)umma::smem_desc_sw128(0, 0, 1024) & 0xffffffff00000000ull;
-      const uint32_t k_lo = ptx::smem_u32(sK) >> 4, q_lo = (ptx::smem_u32(sQ) >> 4) | 1u << 16, p_lo = (ptx::smem_u32(sP) >> 4) | 1u << 16;
+      const uint32_t k_lo = (ptx::smem_u32(sK) >> 4) | 1u << 16, q_lo = (ptx::smem_u32(sQ) >> 4) | 1u << 16;
       const int steps_r = p.dr / 16;
-      Walk ws(sh), wp(sh);                               // the parts that scores and sums are at
-      umma::Patience patience;
-      int s_at = 0, p_at = 0, n_q = 0;                   // tile within the walk's part; units begun
-      ws.t_end = ws.t_begin = wp.t_end = wp.t_begin = 0;
-      // It looks at what is there, weights for the next sums or a tile for the next scores, and issues that: sums that waited
-      // behind the scores of a tile still on its way would hold their own tile's stage meanwhile.
-      int s_next = 0, p_next = 0;
-      Ring sp(p.stages), pp(p.stages);                   // the stages that scores and sums are at
+      auto wait = [&](uint64_t* bar, uint32_t parity) { return umma::wait_quick(bar, parity, &sh.abort, p.dev_status); };
+      Walk w(sh);
+      Ring at(p.stages);
+      int t = 0, n_q = 0;                                // tiles, units begun
       bool ok = true;
-      while (ok && p_next < n_tiles) {
-        bool moved = false;
-        if (p_next < s_next && ptx::mbar_test_wait(&sh.p_full, p_next & 1)) {
+      while (ok && w.next(p)) {
+        ok = wait(&sh.q_full, n_q++ & 1);
+        for (int i = w.t_begin; ok && i < w.t_end; ++i, ++t) {
+          ok = t < 2 || wait(&sh.s_free[t & 1], ((t >> 1) - 1) & 1);
+          const uint32_t d = s_tmem + (uint32_t)((t & 1) * NH), a_lo = k_lo + at.slot * (kStage >> 4);
+#pragma unroll
+          for (int m = 0; m <= kM; ++m) {                // pairs of channels as they come, the rotary part last
+            ok = ok && wait(m < kM ? &sh.full[at.slot * kM + m] : &sh.r_full[at.slot], at.phase);
+            if (!ok) break;
+            umma::fence_after_sync();
+#pragma unroll
+            for (int k = 0; k < (m < kM ? 8 : 4); ++k)
+              if (m < kM || k < steps_r)
+                umma::mma_bf16(d, hi | (a_lo + ((m * kPair + (k >> 2) * kBox + (k & 3) * 32) >> 4)),
+                               hi | (q_lo + (((2 * m + (k >> 2)) * NH * 128 + (k & 3) * 32) >> 4)), idesc, (m > 0 || k > 0) ? 1u : 0u);
+          }
+          if (!ok) break;
+          umma::commit(&sh.s_full[t & 1]);
+          umma::commit(&sh.r_empty[at.slot]);
+          if (i + 1 == w.t_end) umma::commit(&sh.q_empty);
+          at.next();
+        }
+      }
+      umma::commit(&sh.drain);                           // everything issued has completed before tensor memory is released
+      ptx::mbar_wait_bounded(&sh.drain, 0);
+    }
+    __syncwarp();
+  } else if (warp == kSumWarp) {
+    // ------------------------------------------------------------------ sums
+    if (n_tiles > 0 && umma::elect_one()) {
+      constexpr uint32_t idesc = umma::instr_desc(128, NH, false, true);
+      const uint64_t hi = (uint64_t)umma::smem_desc_sw128(0, 0, 1024) & 0xffffffff00000000ull;
+      const uint32_t k_lo = (ptx::smem_u32(sK) >> 4) | (uint32_t)(kBox >> 4) << 16, p_lo = (ptx::smem_u32(sP) >> 4) | 1u << 16;
+      Walk w(sh);
+      Ring at(p.stages);
+      int t = 0;
+      bool ok = true;
+      while (ok && w.next(p))
+        for (int i = w.t_begin; ok && i < w.t_end; ++i, ++t) {
+          ok = umma::wait_quick(&sh.p_full, t & 1, &sh.abort, p.dev_status);
+          if (!ok) break;
           umma::fence_after_sync();
-          bool fresh = false;
-          if (p_at == wp.t_end) { wp.next(p); p_at = wp.t_begin; fresh = true; }
-          const uint32_t a_lo = (k_lo + pp.slot * (kStage >> 4)) | (uint32_t)(kBox >> 4) << 16;
+          const uint32_t a_lo = k_lo + at.slot * (kStage >> 4);
+          const bool fresh = i == w.t_begin;
 #pragma unroll
           for (int m = 0; m < kM; ++m) {
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
-              umma::mma_bf16(tmem + (uint32_t)(m * NH), hi | (a_lo + ((m * kPair + kk * 2048) >> 4)), hi | (p_lo + 2 * kk), idesc_o,
+              umma::mma_bf16(tmem + (uint32_t)(m * NH), hi | (a_lo + ((m * kPair + kk * 2048) >> 4)), hi | (p_lo + 2 * kk), idesc,
                              (!fresh || kk > 0) ? 1u : 0u);
-            umma::commit(&sh.empty[pp.slot * kM + m]);
+            umma::commit(&sh.empty[at.slot * kM + m]);
           }
           umma::commit(&sh.o_done);
-          pp.next();
-          ++p_at;
-          ++p_next;
-          moved = true;
+          at.next();
         }
-        if (s_next < n_tiles && s_next <= p_next + 1) {  // (the scores' buffer held those of s_next - 2, read before their weights were published)
-          if (s_at == ws.t_end) { ws.next(p); s_at = ws.t_begin; ++n_q; }
-          if (ptx::mbar_test_wait(&sh.full[sp.slot * kM], sp.phase) && ptx::mbar_test_wait(&sh.q_full, (n_q - 1) & 1)) {
-            // the first channels are there, the others on their way
-            const uint32_t d = s_tmem + (uint32_t)((s_next & 1) * NH);
-            const uint32_t a_lo = (k_lo + sp.slot * (kStage >> 4)) | 1u << 16;
-            ++s_at;
-#pragma unroll
-            for (int m = 0; m <= kM; ++m) {              // the rotary part last
-              if (m > 0) ok = ok && umma::wait_quick(m < kM ? &sh.full[sp.slot * kM + m] : &sh.r_full[sp.slot], sp.phase, &sh.abort, p.dev_status);
-              if (!ok) break;
-              umma::fence_after_sync();
-#pragma unroll
-              for (int k = 0; k < (m < kM ? 8 : 4); ++k)
-                if (m < kM || k < steps_r)
-                  umma::mma_bf16(d, hi | (a_lo + ((m * kPair + (k >> 2) * kBox + (k & 3) * 32) >> 4)),
-                                 hi | (q_lo + (((2 * m + (k >> 2)) * NH * 128 + (k & 3) * 32) >> 4)), idesc_s, (m > 0 || k > 0) ? 1u : 0u);
-            }
-            if (!ok) break;
-            umma::commit(&sh.s_full[s_next & 1]);
-            umma::commit(&sh.r_empty[sp.slot]);
-            if (s_at == ws.t_end) umma::commit(&sh.q_empty);
-            sp.next();
-            ++s_next;
-            moved = true;
-          }
-        }
-        if (moved) patience.moved();
-        else ok = patience.more(&sh.abort, p.dev_status);
-      }
-      umma::commit(&sh.drain);                           // everything issued has completed before tensor memory is released
+      umma::commit(&sh.drain);
       ptx::mbar_wait_bounded(&sh.drain, 0);
     }
     __syncwarp();
@@ -434,6 +436,9 @@ __global__ void __launch_bounds__(cta_threads(NH), 1) latent_decode_kernel(const
 #pragma unroll
         for (int k = 0; k < kBlocks; ++k) ld_frags(s_tmem + lane_base + (uint32_t)((t & 1) * NH + col0 + 16 * k), z + 8 * k);
         umma::tmem_ld_wait();
+        umma::fence_before_sync();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&sh.s_free[t & 1]);
         const int n = w.len - i * kTile;
         if (n < kTile) {
 #pragma unroll
@@ -572,7 +577,7 @@ __global__ void __launch_bounds__(cta_threads(NH), 1) latent_decode_kernel(const
   // ---- every role has left its loops; nothing of this CTA is in flight any more
   umma::fence_before_sync();
   __syncthreads();
-  if (warp == kMmaWarp) {
+  if (warp == kScoreWarp) {
     umma::fence_after_sync();
     umma::tmem_dealloc(tmem, kCols);
   }
