@@ -583,64 +583,112 @@ __global__ void __launch_bounds__(cta_threads(NH), 1) latent_decode_kernel(const
   }
 }
 
-// Joins the parts of the unit that begins in piece blockIdx.x and goes on behind it.  A CTA of 128 threads takes four
-// heads: each warp works out the weights of one head's parts, then a thread sums four channels of all four.  Bound by latency, plan ->
-// maxima -> sums, so the CTAs are small enough to be resident all at once.
-constexpr int kJoin = 4;
+// Joins the parts of units that lie in several pieces.  Bound by latency, plan -> maxima and sums of the parts -> result, so the CTAs are
+// small enough to be resident all at once.  The first p.pieces x H / 4 take a unit in few parts each, the one that begins in their piece,
+// and four heads of it: a warp works out the weights of one head's parts, then a thread sums four channels of all four.  The others take
+// the heads of units in many parts, 128 channels at a time, a quarter of the parts to each warp (one sequence of 8192 tokens, 128 parts: the
+// call takes 25 us, 82 where a thread adds up all of them).
+constexpr int kJoin = 4, kManyParts = 12, kAhead = 4, kJoinExtra = 8 * kMaxCtas;
+__device__ __forceinline__ int64_t part_of(const LatentDecodeParams& p, int i0, int i, int h) {
+  return ((int64_t)(i0 + i) * 2 + (i == 0 ? 1 : 0)) * p.heads_pad + h;
+}
+// One warp: what part i of head h counts, for all of the unit's n parts.
+__device__ __forceinline__ void join_weights(const LatentDecodeParams& p, int i0, int n, int h, float* weight) {
+  constexpr int kRounds = (kMaxCtas + 31) / 32;
+  const int lane = threadIdx.x & 31;
+  float2 ml[kRounds];
+  float m = -INFINITY, total = 0.f;
+#pragma unroll
+  for (int k = 0; k < kRounds; ++k) {
+    ml[k] = 32 * k + lane < n ? p.part_ml[part_of(p, i0, 32 * k + lane, h)] : make_float2(-INFINITY, 0.f);
+    m = fmaxf(m, ml[k].x);
+  }
+  m = warp_max(m);
+  if (m == -INFINITY) m = 0.f;
+#pragma unroll
+  for (int k = 0; k < kRounds; ++k) {
+    ml[k].x = ptx::ex2_approx(ml[k].x - m);
+    total += ml[k].y * ml[k].x;
+  }
+  const float inv = 1.f / warp_sum(total);
+#pragma unroll
+  for (int k = 0; k < kRounds; ++k)
+    if (32 * k + lane < n) weight[32 * k + lane] = ml[k].x * inv;
+}
+__device__ __forceinline__ void join_store(const LatentDecodeParams& p, int unit, int h, int c, const float4& o) {
+  const int64_t at = (((int64_t)p.layer_begin * p.B + unit) * p.H + h) * p.dc + c;
+  if (p.out_bf16)
+    *reinterpret_cast<uint2*>((__nv_bfloat16*)p.out + at) = make_uint2(ptx::pack_bf16x2(o.x, o.y), ptx::pack_bf16x2(o.z, o.w));
+  else
+    *reinterpret_cast<float4*>((float*)p.out + at) = o;
+}
+__device__ __forceinline__ void add_part(float4& o, const float4& v, float f) { o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f; }
+
 __global__ void __launch_bounds__(128) latent_join_kernel(LatentDecodeParams p) {
   __shared__ float weight[kJoin][kMaxCtas];
+  __shared__ float4 sums[4][32];
+  __shared__ int3 units[kMaxCtas / (kManyParts - 1) + 1];                // unit, first piece, parts
+  __shared__ int n_units;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, few = p.pieces * ((p.H + kJoin - 1) / kJoin);
   ptx::grid_dep_launch();
   ptx::grid_dep_wait();
-  const int i0 = blockIdx.x;
-  const int2 plan = p.plan[i0];
-  if (plan.x < 0) return;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = plan.y - i0 + 1, h0 = kJoin * blockIdx.y;
-  auto slot = [&](int i, int h) { return ((int64_t)(i0 + i) * 2 + (i == 0 ? 1 : 0)) * p.heads_pad + h; };
-  if (h0 + warp < p.H) {                                 // a warp per head: lanes take parts
-    float2 ml[(kMaxCtas + 31) / 32];
-    float m = -INFINITY, total = 0.f;
+  if ((int)blockIdx.x < few) {
+    const int i0 = blockIdx.x % p.pieces, h0 = kJoin * (blockIdx.x / p.pieces), c = 4 * threadIdx.x;
+    const int2 plan = p.plan[i0];
+    const int n = plan.y - i0 + 1;
+    if (plan.x < 0 || n >= kManyParts) return;
+    if (h0 + warp < p.H) join_weights(p, i0, n, h0 + warp, weight[warp]);
+    __syncthreads();
+    if (c >= p.dc) return;
+    float4 o[kJoin];
 #pragma unroll
-    for (int k = 0; k < (kMaxCtas + 31) / 32; ++k) {
-      ml[k] = 32 * k + lane < n ? p.part_ml[slot(32 * k + lane, h0 + warp)] : make_float2(-INFINITY, 0.f);
-      m = fmaxf(m, ml[k].x);
+    for (int k = 0; k < kJoin; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+    for (int i = 0; i < n; ++i)
+#pragma unroll
+      for (int k = 0; k < kJoin; ++k)
+        if (h0 + k < p.H) add_part(o[k], *reinterpret_cast<const float4*>(p.part_o + part_of(p, i0, i, h0 + k) * p.dc + c), weight[k][i]);
+#pragma unroll
+    for (int k = 0; k < kJoin; ++k)
+      if (h0 + k < p.H) join_store(p, plan.x, h0 + k, c, o[k]);
+    return;
+  }
+  if (warp == 0) {
+    int at = 0;
+    for (int k = 0; k < p.pieces; k += 32) {
+      const int2 plan = k + lane < p.pieces ? p.plan[k + lane] : make_int2(-1, -1);
+      const bool many = plan.x >= 0 && plan.y - (k + lane) + 1 >= kManyParts;
+      const uint32_t all = __ballot_sync(0xffffffffu, many);
+      if (many) units[at + __popc(all & ((1u << lane) - 1))] = make_int3(plan.x, k + lane, plan.y - (k + lane) + 1);
+      at += __popc(all);
     }
-    m = warp_max(m);
-    if (m == -INFINITY) m = 0.f;
-#pragma unroll
-    for (int k = 0; k < (kMaxCtas + 31) / 32; ++k) {
-      ml[k].x = ptx::ex2_approx(ml[k].x - m);
-      total += ml[k].y * ml[k].x;
-    }
-    const float inv = 1.f / warp_sum(total);
-#pragma unroll
-    for (int k = 0; k < (kMaxCtas + 31) / 32; ++k)
-      if (32 * k + lane < n) weight[warp][32 * k + lane] = ml[k].x * inv;
+    if (lane == 0) n_units = at;
   }
   __syncthreads();
-  const int c = 4 * threadIdx.x;
-  if (c >= p.dc) return;
-  float4 o[kJoin];
+  const int slices = p.dc / 128;
+  for (int item = blockIdx.x - few; item < n_units * p.H * slices; item += gridDim.x - few) {
+    const int c = 128 * (item % slices) + 4 * lane, h = item / slices % p.H, i0 = units[item / slices / p.H].y, n = units[item / slices / p.H].z;
+    float4 v[kAhead], o = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto part = [&](int i) { return *reinterpret_cast<const float4*>(p.part_o + part_of(p, i0, i, h) * p.dc + c); };
 #pragma unroll
-  for (int k = 0; k < kJoin; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-  for (int i = 0; i < n; ++i)
+    for (int k = 0; k < kAhead; ++k)                     // (asked for along with the maxima)
+      if (warp + 4 * k < n) v[k] = part(warp + 4 * k);
+    join_weights(p, i0, n, h, weight[warp]);
+    __syncwarp();
+    for (int i = warp; i < n; i += 4 * kAhead)
 #pragma unroll
-    for (int k = 0; k < kJoin; ++k) {
-      if (h0 + k < p.H) {
-        const float4 v = *reinterpret_cast<const float4*>(p.part_o + slot(i, h0 + k) * p.dc + c);
-        const float f = weight[k][i];
-        o[k].x += v.x * f; o[k].y += v.y * f; o[k].z += v.z * f; o[k].w += v.w * f;
+      for (int k = 0; k < kAhead; ++k) {
+        if (i + 4 * k < n) add_part(o, v[k], weight[warp][i + 4 * k]);
+        if (i + 4 * (k + kAhead) < n) v[k] = part(i + 4 * (k + kAhead));
       }
-    }
+    sums[warp][lane] = o;
+    __syncthreads();
+    if (warp == 0) {
 #pragma unroll
-  for (int k = 0; k < kJoin; ++k) {
-    const int h = h0 + k;
-    const int64_t at = (((int64_t)p.layer_begin * p.B + plan.x) * p.H + h) * p.dc + c;
-    if (h >= p.H) break;
-    if (p.out_bf16)
-      *reinterpret_cast<uint2*>((__nv_bfloat16*)p.out + at) = make_uint2(ptx::pack_bf16x2(o[k].x, o[k].y), ptx::pack_bf16x2(o[k].z, o[k].w));
-    else
-      *reinterpret_cast<float4*>((float*)p.out + at) = o[k];
+      for (int w = 1; w < 4; ++w) add_part(o, sums[w][lane], 1.f);
+      join_store(p, units[item / slices / p.H].x, h, c, o);
+    }
+    __syncthreads();                                     // (before the next item's weights and sums)
   }
 }
 
@@ -685,7 +733,7 @@ template <int NH, int DC> int launch(const Maps& maps, LatentDecodeParams& p, cu
   if (rc != NGC_OK) return rc;
   // (all of it, however little the ring takes: two CTAs of an SM would fight for its tensor memory)
   NGC_CUDA_TRY(launch_pdl(latent_decode_kernel<NH, DC>, dim3(p.pieces * p.groups), dim3(cta_threads(NH)), kSmemLimit - kStaticReserve, stream, maps, p));
-  NGC_CUDA_TRY(launch_pdl(latent_join_kernel, dim3(p.pieces, (p.H + kJoin - 1) / kJoin), dim3(128), 0, stream, p));
+  NGC_CUDA_TRY(launch_pdl(latent_join_kernel, dim3(p.pieces * ((p.H + kJoin - 1) / kJoin) + kJoinExtra), dim3(128), 0, stream, p));
   return launch_status();
 }
 

@@ -205,6 +205,17 @@ def test_decode_of_more_units_than_threads():
     assert_within(out, want, bound)
 
 
+@pytest.mark.parametrize("H,dc,lens", [(16, 512, [64 * 11]), (5, 128, [64 * 12]), (17, 384, [64 * 13 - 1, 0]), (3, 256, [64 * 148 + 5]), (16, 512, [20001, 3, 0, 5000]),
+                                       (128, 512, [4000, 1, 700, 2600]), (64, 128, [9000, 9000, 30, 9000, 64])])
+def test_decode_of_sequences_in_few_and_in_many_parts(H, dc, lens):
+    pool = random_pool(1, len(lens), 64, -(-max(lens) // 64), sum(-(-n // 64) for n in lens) + 1, lens, 0, 31, dc, 64)
+    for out_dtype in (bf16, f32):
+        ql, qr, out, st = run_decode(pool, H, 0.1, out_dtype)
+        want, bound = ora.decode(host(pool.rows), host(pool.page_table), host(pool.lens), host(ql), host(qr), 0.1, 0, out_dtype is bf16)
+        assert status_value(st) == 0
+        assert_within(out, want, bound)
+
+
 @pytest.mark.parametrize("seed", range(8))
 def test_decode_of_random_shapes(seed):
     rng = np.random.default_rng(100 + seed)
