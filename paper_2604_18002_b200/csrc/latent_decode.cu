@@ -21,9 +21,9 @@
 //                         moves only when a score exceeds it by 2^8 (exact in bf16 and fp32), which is one vote per tile.
 // Every wait is bounded; one that runs out makes all roles leave and is reported.
 //
-// 64 sequences of 1024 to 4096 tokens, 16 heads of 512 + 64 channels, one layer: 52 us with the second kernel, 3.7 TB/s; beginning,
+// 64 sequences of 1024 to 4096 tokens, 16 heads of 512 + 64 channels, one layer: 49 us with the second kernel, 3.9 TB/s; beginning,
 // first tile and joining are most of the 13 us that a call of one sequence takes.  24 sequences of 2048 to 8192, 128 heads, two
-// layers: 125 us, 548 TFLOP/s: the queries of 64 heads leave shared memory room for two tiles.  A tile holds its place for some 5500 cycles:
+// layers: 123 us, 555 TFLOP/s: the queries of 64 heads leave shared memory room for two tiles.  A tile holds its place for some 5500 cycles:
 // 1700 until its first rows are there, 1400 until the last, 1850 of softmax and its hand-overs, 800 of sums; with every row in L2 the
 // call takes 108 us.
 #include <cuda.h>
@@ -587,8 +587,9 @@ __global__ void __launch_bounds__(cta_threads(NH), 1) latent_decode_kernel(const
 // small enough to be resident all at once.  The first p.pieces x H / 4 take a unit in few parts each, the one that begins in their piece,
 // and four heads of it: a warp works out the weights of one head's parts, then a thread sums four channels of all four.  The others take
 // the heads of units in many parts, 128 channels at a time, a quarter of the parts to each warp (one sequence of 8192 tokens, 128 parts: the
-// call takes 25 us, 82 where a thread adds up all of them).
-constexpr int kJoin = 4, kManyParts = 12, kAhead = 4, kJoinExtra = 8 * kMaxCtas;
+// call takes 25 us, 82 where a thread adds up all of them).  Many are 8 or more: with 6, 16 sequences of 128 heads take 51 us instead of 45,
+// with 12, 16 sequences of 16 heads 37 instead of 33.
+constexpr int kJoin = 4, kManyParts = 8, kAhead = 4, kJoinExtra = 8 * kMaxCtas;
 __device__ __forceinline__ int64_t part_of(const LatentDecodeParams& p, int i0, int i, int h) {
   return ((int64_t)(i0 + i) * 2 + (i == 0 ? 1 : 0)) * p.heads_pad + h;
 }
