@@ -150,6 +150,7 @@ class NgcLatentRollout:
         self.first = torch.empty((B + 1,), dtype=torch.int32, device=device)
         self.kept_order = torch.empty((B, self.G, pages_cap), dtype=torch.int32, device=device)
         self.kept_sorted = torch.empty_like(self.kept_order)
+        self.counts = None         # (n, n_protect, budget) of the last round's draw
         self.status = ngc.new_status(device)
         self.ws_sample = ngc.alloc_workspace(ngc.workspace_bytes(ngc.OP_SAMPLE, None, self.G, pages_cap, pages_cap, B=B), device)
         self.ws_decode = ngc.alloc_workspace(ngc.latent_decode_workspace_bytes(self.pool, H), device)
@@ -161,9 +162,14 @@ class NgcLatentRollout:
     def evict(self, logits: torch.Tensor, n: torch.Tensor, n_protect: Optional[torch.Tensor], budget: torch.Tensor, seed: int, rnd: int,
               n_new: torch.Tensor, greedy: int = 0):
         """An eviction round over whole pages and the next tokens' pages in one: draws ``budget[b]`` of ``n[b]`` pages by ``logits``
-        [B][G][pages_cap] fp32.  (With a length per list, lists may be a page short of ``n``: give the missing unit the logit -inf.)"""
-        ngc.ngc_sample_evict(logits, n, n_protect, budget, seed, rnd, self.kept_order, self.kept_sorted, None, greedy=greedy,
-                             list_base=self.list_base, ws=self.ws_sample, status=self.status)
+        [B][G][pages_cap] fp32.  (With a length per list, lists may be a page short of ``n``: give the missing unit the logit -inf, and
+        a budget that leaves it undrawn.)  ``budget[b]`` -1 leaves rollout b out: it keeps all it has, whatever its counts and logits
+        hold.  ``counts`` are then the draw's own (n, n_protect, budget), zeros for those left out, as ngc_evict_logprob takes them;
+        in a history for ngc_replay_visibility a rollout's rounds are those that it took part in."""
+        left_out = budget == -1
+        self.counts = tuple(None if x is None else x.masked_fill(left_out, 0) for x in (n, n_protect, budget))
+        ngc.ngc_sample_evict(logits, *self.counts, seed, rnd, self.kept_order, self.kept_sorted, None, greedy=greedy, list_base=self.list_base,
+                             ws=self.ws_sample, status=self.status)
         ngc.ngc_pool_update(self.pool, n_new, self.slots, self.first, kept_sorted=self.kept_sorted, budget=budget, status=self.status)
 
     def write(self, latent: torch.Tensor, rope: torch.Tensor, layer_begin: int = 0, layer_end: Optional[int] = None):
