@@ -141,12 +141,13 @@ class NgcLatentRollout:
     ``decode``; an eviction round is ``evict`` in the place of ``update``."""
 
     def __init__(self, L, B, H, d_latent, d_rope, n_pages, pages_cap, max_new, scale, page=64, lists=ngc.LISTS_SHARED, list_base=0, device="cuda"):
-        """``max_new``: new tokens of all rollouts that one ``update`` may bring; ``scale``: of the scores (one over the root of the
-        expanded key's width)."""
+        """``max_new``: new tokens of all rollouts that one ``update`` may bring (admitted prompts); ``scale``: of the scores (one over the
+        root of the expanded key's width)."""
         self.L, self.B, self.H, self.lists, self.scale, self.list_base, self.device = L, B, H, lists, scale, list_base, device
         self.G = ngc.lists_G(lists, L, 1)
         self.pool = ngc.new_latent_pool(L, B, d_latent, d_rope, n_pages, pages_cap, page, lists, device)
-        self.slots = torch.empty((self.G, max_new), dtype=torch.int32, device=device)
+        self._all_slots = torch.empty((self.G * max_new,), dtype=torch.int32, device=device)
+        self.slots = self._all_slots.view(self.G, max_new)
         self.first = torch.empty((B + 1,), dtype=torch.int32, device=device)
         self.kept_order = torch.empty((B, self.G, pages_cap), dtype=torch.int32, device=device)
         self.kept_sorted = torch.empty_like(self.kept_order)
@@ -155,17 +156,29 @@ class NgcLatentRollout:
         self.ws_sample = ngc.alloc_workspace(ngc.workspace_bytes(ngc.OP_SAMPLE, None, self.G, pages_cap, pages_cap, B=B), device)
         self.ws_decode = ngc.alloc_workspace(ngc.latent_decode_workspace_bytes(self.pool, H), device)
 
-    def update(self, n_new: torch.Tensor):
-        """Pages and ``slots`` for ``n_new[b]`` new tokens per rollout (int32 [B]; -1: the rollout is finished)."""
+    def _take_slots(self, n_slots: Optional[int]):
+        most = self._all_slots.numel() // self.G
+        n = most if n_slots is None else n_slots
+        if not 1 <= n <= most:
+            raise ngc.NgcError(f"n_slots must be 1 .. {most} (max_new), got {n}")
+        if n != self.slots.shape[1]:
+            self.slots = self._all_slots[: self.G * n].view(self.G, n)
+
+    def update(self, n_new: torch.Tensor, n_slots: Optional[int] = None):
+        """Pages and ``slots`` for ``n_new[b]`` new tokens per rollout (int32 [B]; -1: the rollout is finished).  ``n_slots`` (``max_new``
+        if None): how many tokens this call may bring, B for a decode step; the slots and the rows of ``write`` are as many, and
+        what a step costs goes by it."""
+        self._take_slots(n_slots)
         ngc.ngc_pool_update(self.pool, n_new, self.slots, self.first, status=self.status)
 
     def evict(self, logits: torch.Tensor, n: torch.Tensor, n_protect: Optional[torch.Tensor], budget: torch.Tensor, seed: int, rnd: int,
-              n_new: torch.Tensor, greedy: int = 0):
+              n_new: torch.Tensor, greedy: int = 0, n_slots: Optional[int] = None):
         """An eviction round over whole pages and the next tokens' pages in one: draws ``budget[b]`` of ``n[b]`` pages by ``logits``
         [B][G][pages_cap] fp32.  (With a length per list, lists may be a page short of ``n``: give the missing unit the logit -inf, and
         a budget that leaves it undrawn.)  ``budget[b]`` -1 leaves rollout b out: it keeps all it has, whatever its counts and logits
         hold.  ``counts`` are then the draw's own (n, n_protect, budget), zeros for those left out, as ngc_evict_logprob takes them;
-        in a history for ngc_replay_visibility a rollout's rounds are those that it took part in."""
+        in a history for ngc_replay_visibility a rollout's rounds are those that it took part in.  ``n_slots`` as for ``update``."""
+        self._take_slots(n_slots)
         left_out = budget == -1
         self.counts = tuple(None if x is None else x.masked_fill(left_out, 0) for x in (n, n_protect, budget))
         ngc.ngc_sample_evict(logits, *self.counts, seed, rnd, self.kept_order, self.kept_sorted, None, greedy=greedy, list_base=self.list_base,
@@ -173,7 +186,8 @@ class NgcLatentRollout:
         ngc.ngc_pool_update(self.pool, n_new, self.slots, self.first, kept_sorted=self.kept_sorted, budget=budget, status=self.status)
 
     def write(self, latent: torch.Tensor, rope: torch.Tensor, layer_begin: int = 0, layer_end: Optional[int] = None):
-        """Rows of the new tokens, in the order of ``first``: latent [L][max_new][d_latent], rope [L][max_new][d_rope]."""
+        """Rows of the new tokens, in the order of ``first``: latent [L][n_slots][d_latent], rope [L][n_slots][d_rope], n_slots those of the
+        last ``update`` or ``evict``."""
         ngc.ngc_latent_write(self.pool, self.slots, latent, rope, layer_begin, layer_end, status=self.status)
 
     def decode(self, q_latent: torch.Tensor, q_rope: torch.Tensor, out: torch.Tensor, layer_begin: int = 0, layer_end: Optional[int] = None):
