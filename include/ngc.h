@@ -617,15 +617,18 @@ typedef struct {
  *   n_new[b] >= 0:   the sequence grows by n_new[b] tokens;  n_new[b] = -1: it is finished, its pages return to the pool, its
  *                    length becomes 0
  * All returns come before all growth; growth takes the lowest free page numbers
- * in order of sequences.  Token t of sequence b's new ones is number first[b] + t.
+ * in order of sequences.  Where they are too few, each sequence that still fits beside the ones before it grows: one that does
+ * not keeps no pages from those after it.  Token t of sequence b's new ones is number first[b] + t.
  *   n_new [B];  kept_sorted [B][G][k_max] as written by ngc_sample_evict, budget [B], or both NULL
  *   slots [G][n_slots] out: page * (tokens per page) + place in the page of every new token; -1 from first[B] on
  *   first [B+1] out: new tokens of the sequences before (2^30 - 1 where there are more)
  * Per list, a sequence with counts that are none (NGC_DEV_BAD_COUNTS: also more
  * new tokens than n_slots holds), a bad kept list (NGC_DEV_BAD_KEPT) or page-table entry
  * (NGC_DEV_BAD_PAGE) is left as it was; one that outgrows pages_cap
- * (NGC_DEV_STRIP_FULL) or the free pages (NGC_DEV_POOL_FULL) evicts but does
- * not grow.  Their new tokens get slot -1.  B <= 8192, n_slots < 2^30.
+ * (NGC_DEV_STRIP_FULL) or what is free when its turn comes (NGC_DEV_POOL_FULL) evicts but does
+ * not grow.  Their new tokens get slot -1.  So after a report a sequence may have grown on some lists and not on others (its lens
+ * differ by n_new[b]); calling again would grow the former twice.  n_new[b] = -1 takes it back on all lists, and it can be admitted anew.
+ * B <= 8192, n_slots < 2^30.
  */
 int ngc_pool_update(ngc_latent_pool* c, const int32_t* kept_sorted, const int32_t* budget, int k_max, const int32_t* n_new,
                     int32_t* slots, int n_slots, int32_t* first, int32_t* dev_status, ngc_stream stream);

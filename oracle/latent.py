@@ -70,10 +70,10 @@ def pool_update(table, used, lens, page, n_new, n_slots, kept=None, budget=None)
         at = 0
         for b, length, n in grows:
             have, need = -(-length // page), -(-(length + n) // page)
-            at += need - have
-            if need > have and at > len(free):                   # (it and all after it that need pages: none is skipped over)
+            if need - have > len(free) - at:                     # (those after it that need less may fit)
                 problems.add(POOL_FULL)
                 continue
+            at += need - have
             for j in range(have, need):
                 x = free[at - need + j]
                 table[b, g, j] = x

@@ -169,6 +169,36 @@ __device__ Settled settle_eviction(const PoolParams& p, int gi, int b, int first
   return s;
 }
 
+// Who grows where pages are short: in order of sequences each that fits beside those before it, so that one too large does not keep
+// the pages from the others.  need[b + 1] are the sums of the pages wanted, and become those of the pages granted.  One warp, 32
+// sequences at a time: what is more than all that is left is refused at once, then the first of the others that does not fit, until all do.
+__device__ void grant_growth(const PoolParams& p, int* need, int* from, int n_free) {
+  const int lane = threadIdx.x & 31;
+  int wanted = 0, granted = 0;                         // of the sequences before these 32
+  for (int b0 = 0; b0 < p.B; b0 += 32) {
+    const int b = b0 + lane, sum = need[min(b, p.B - 1) + 1];
+    int before = __shfl_up_sync(0xffffffffu, sum, 1);
+    if (lane == 0) before = wanted;
+    wanted = __shfl_sync(0xffffffffu, sum, 31);
+    const int mine = b < p.B ? sum - before : 0;
+    bool refused = mine > n_free - granted;
+    for (;;) {
+      int incl = refused ? 0 : mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += v; }
+      const uint32_t over = __ballot_sync(0xffffffffu, !refused && mine > 0 && incl > n_free - granted);
+      if (over == 0) {
+        if (b < p.B) need[b + 1] = granted + incl;
+        granted += __shfl_sync(0xffffffffu, incl, 31);
+        break;
+      }
+      const int first = __ffs(over) - 1, left = n_free - granted - __shfl_sync(0xffffffffu, incl - mine, first);
+      refused = refused || (lane >= first && mine > left);
+    }
+    if (refused) { from[b] = -1; set_dev_status(p.dev_status, NGC_DEV_POOL_FULL); }
+  }
+}
+
 // Slot of position pos (-1: none) of sequence b.
 __device__ __forceinline__ int slot_of(const PoolParams& p, int gi, int b, int pos) {
   if (pos < 0 || !NGC_IN_BOUNDS(p.dev_status, (pos >> p.page_shift) < p.cap)) return -1;
@@ -250,23 +280,15 @@ __global__ void __launch_bounds__(kThreads) pool_update_kernel(PoolParams p) {
     const int wanted = run;
     __syncthreads();
     if (wanted > 0) {
-      // how many pages are free; sequences beyond the last that fits do not grow
+      // how many pages are free; where they are too few, not all sequences grow
       int limit = wanted, here = 0, n_free;
       uint32_t m = 0;                                  // of this thread's last 16 pages: all it has, in a pool of up to 4096
       for (int at = 16 * tid; at < p.n_pages; at += 16 * kThreads) here += __popc(m = free_mask(used, at, p.n_pages, wide));
       block_scan(here, warp_sums, n_free);
       if (n_free < wanted) {
-        int best = 0;
-        for (int b = tid; b < p.B; b += kThreads) {
-          if (need[b + 1] <= n_free) best = max(best, need[b + 1]);
-          else if (need[b + 1] > need[b]) { from[b] = -1; set_dev_status(p.dev_status, NGC_DEV_POOL_FULL); }
-        }
-        if (tid == 0) warp_sums[0] = 0;
+        if (warp == 0) grant_growth(p, need, from, n_free);
         __syncthreads();
-        atomicMax(&warp_sums[0], best);
-        __syncthreads();
-        limit = warp_sums[0];
-        __syncthreads();
+        limit = need[p.B];
       }
       run = 0;
       for (int at0 = 0; run < limit && at0 < p.n_pages; at0 += 16 * kThreads) {
