@@ -29,7 +29,8 @@ def pool_update(table, used, lens, page, n_new, n_slots, kept=None, budget=None)
         for b in range(B):
             n, keep = int(n_new[b]), -1 if kept is None else int(budget[b])
             length = int(lens[b, g])
-            if not 0 <= length <= cap * page or n < -1 or keep < -1 or (kept is not None and keep > kept.shape[2]):
+            if (not 0 <= length <= cap * page or n < -1 or n > max(n_slots - int(first[b]), 0) or keep < -1
+                    or (kept is not None and keep > kept.shape[2])):
                 problems.add(BAD_COUNTS)
                 continue
             have = -(-length // page)
@@ -58,9 +59,7 @@ def pool_update(table, used, lens, page, n_new, n_slots, kept=None, budget=None)
                 length = tokens
                 lens[b, g] = length
             n = max(n, 0)
-            if n > n_slots - first[b]:
-                problems.add(BAD_COUNTS)
-            elif n > cap * page - length:
+            if n > cap * page - length:
                 problems.add(STRIP_FULL)
             elif n > 0 and length % page and not 0 <= table[b, g, length // page] < n_pages:
                 problems.add(BAD_PAGE)

@@ -90,12 +90,8 @@ __device__ __forceinline__ uint32_t free_mask(const uint8_t* used, int at, int n
 struct Settled { int len, need; };
 
 // The part that both ways share: may the sequence grow from `len` tokens?  `last_page`: the entry of its last page, where that has room.
-__device__ __forceinline__ Settled settle_growth(const PoolParams& p, int len, int n_new, int first_token, int last_page) {
+__device__ __forceinline__ Settled settle_growth(const PoolParams& p, int len, int n_new, int last_page) {
   const int grow = max(n_new, 0), have = (len + p.page - 1) >> p.page_shift;
-  if (grow > p.n_slots - first_token) {
-    set_dev_status(p.dev_status, NGC_DEV_BAD_COUNTS);
-    return {-1, 0};
-  }
   if (grow > p.cap * p.page - len) {
     set_dev_status(p.dev_status, NGC_DEV_STRIP_FULL);
     return {-1, 0};
@@ -109,7 +105,7 @@ __device__ __forceinline__ Settled settle_growth(const PoolParams& p, int len, i
 
 // A sequence that evicts or leaves; one warp.  `rows` holds the table row of up to kRowMax pages while it is rewritten.
 constexpr int kRowMax = 512;
-__device__ Settled settle_eviction(const PoolParams& p, int gi, int b, int first_token, int* rows, uint8_t* used) {
+__device__ Settled settle_eviction(const PoolParams& p, int gi, int b, int* rows, uint8_t* used) {
   const int lane = threadIdx.x & 31;
   const int64_t list = (int64_t)b * p.G + gi;
   int32_t* row = p.table + list * p.cap;
@@ -164,7 +160,7 @@ __device__ Settled settle_eviction(const PoolParams& p, int gi, int b, int first
   Settled s = {-1, 0};
   if (lane == 0) {
     p.lens[list] = left;
-    s = settle_growth(p, left, n_new, first_token, last_page);
+    s = settle_growth(p, left, n_new, last_page);
   }
   return s;
 }
@@ -246,7 +242,8 @@ __global__ void __launch_bounds__(kThreads) pool_update_kernel(PoolParams p) {
     const int64_t list = (int64_t)b * p.G + gi;
     const int n_new = p.n_new[b], len = p.lens[list], budget = p.kept ? p.budget[b] : -1;
     Settled s = {-1, 0};
-    if (len < 0 || len > p.cap * p.page || n_new < -1 || budget < -1 || budget > p.k_max) {
+    // (new tokens without slots count as no counts, before anything of the sequence is changed)
+    if (len < 0 || len > p.cap * p.page || n_new < -1 || n_new > max(p.n_slots - first[b], 0) || budget < -1 || budget > p.k_max) {
       set_dev_status(p.dev_status, NGC_DEV_BAD_COUNTS);
     } else if (budget >= 0 || n_new < 0) {
       waiting[atomicAdd(&n_waiting, 1)] = b;
@@ -254,7 +251,7 @@ __global__ void __launch_bounds__(kThreads) pool_update_kernel(PoolParams p) {
     } else {
       const int have = (len + p.page - 1) >> p.page_shift;
       const int last_page = n_new > 0 && (len & (p.page - 1)) != 0 ? p.table[list * p.cap + have - 1] : 0;
-      s = settle_growth(p, len, n_new, first[b], last_page);
+      s = settle_growth(p, len, n_new, last_page);
     }
     from0[b] = s.len;
     need0[b + 1] = s.need;
@@ -262,7 +259,7 @@ __global__ void __launch_bounds__(kThreads) pool_update_kernel(PoolParams p) {
   __syncthreads();
   for (int i = warp; i < n_waiting; i += kWarps) {
     const int b = waiting[i];
-    const Settled s = settle_eviction(p, gi, b, first[b], rows[warp], used);
+    const Settled s = settle_eviction(p, gi, b, rows[warp], used);
     if (lane == 0) { from0[b] = s.len; need0[b + 1] = s.need; }
   }
   if (n_ranks > 1) cluster.sync(); else __syncthreads();

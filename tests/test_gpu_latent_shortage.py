@@ -45,3 +45,17 @@ def test_a_sequence_that_grew_on_some_lists_only_can_be_finished_and_admitted_an
     assert host(pool.lens)[2].tolist() == [0, 0]
     assert run_update(pool, [0, 0, 5 * page], 5 * page) == set()
     assert host(pool.lens).tolist() == [[65, 65], [96, 128], [5 * page, 5 * page]]
+
+
+@pytest.mark.parametrize("n_slots", [60, 5000])
+def test_a_sequence_with_more_new_tokens_than_slots_does_not_evict_either(n_slots):
+    """It is left as it was, pages and length, in a round too; those behind it that end or only evict are served."""
+    page = 32
+    pool = random_pool(2, 5, page, 6, 40, [[64, 60], [100, 96], [128, 128], [70, 70], [33, 33]], 1, 6)
+    before = [host(x).copy() for x in (pool.page_table, pool.lens)]
+    budget = np.array([1, 2, 2, 1, 1])
+    kept = np.full((5, 2, 2), -1)
+    kept[0, :, 0], kept[1], kept[2], kept[3, :, 0], kept[4, :, 0] = 1, [0, 2], [1, 3], 2, 0
+    assert run_update(pool, [20, n_slots, 0, -1, 5], n_slots, kept, budget) == {ora.BAD_COUNTS}
+    assert (host(pool.page_table)[1] == before[0][1]).all() and (host(pool.lens)[1] == before[1][1]).all()
+    assert host(pool.lens)[[0, 2, 3, 4]].tolist() == [[52, 48], [64, 64], [0, 0], [33, 33]]      # (the last one's 5 tokens have no slots either)

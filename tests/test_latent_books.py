@@ -30,3 +30,11 @@ def test_shortage_is_each_lists_own_and_can_be_undone():
     assert problems == {ora.POOL_FULL} and lens.tolist() == [[64, 64], [160, 32]] and (slots[0] >= 0).all() and (slots[1] == -1).all()
     table, used, lens, slots, first, problems = ora.pool_update(table, used, lens, 32, np.array([0, -1]), 1)
     assert problems == set() and lens.tolist() == [[64, 64], [0, 0]] and used.sum(1).tolist() == [2, 2]
+
+
+def test_more_new_tokens_than_slots_leave_a_sequence_as_it_was():
+    s = state([[64], [64], [40]], 32, 8, 20)
+    kept, budget = np.array([[[1]], [[0]], [[1]]]), np.array([1, 1, 1])
+    table, used, lens, slots, first, problems = ora.pool_update(*s, 32, np.array([5, 60, -1]), 60, kept, budget)
+    assert problems == {ora.BAD_COUNTS} and lens.tolist() == [[37], [64], [0]]
+    assert table[1, 0, :3].tolist() == [2, 3, -1] and (slots[0, 5:] == -1).all()
