@@ -29,11 +29,14 @@ inline bool make_token_map(CUtensorMap* map, const void* base, int width, int he
 // together.
 struct Deal {
   int size, pass, m, before, count;            // level, items before it, sequences that have it
+  int at, seen;                                // the 32 sequences that the last item came from, sequences of the level before them
   bool down;
-  __device__ __forceinline__ Deal(const LatentReplayParams& p, int block, bool from_last) : size(block), pass(0), m(0), before(0), count(0), down(from_last) {
+  __device__ __forceinline__ Deal(const LatentReplayParams& p, int block, bool from_last)
+      : size(block), pass(0), m(0), before(0), count(0), at(0), seen(0), down(from_last) {
     if (down) {
       int longest = 0;
-      for (int b0 = 0; b0 < p.B; b0 += 32) longest = max(longest, length(p, b0 + (threadIdx.x & 31)));
+      int64_t row0;
+      for (int b = threadIdx.x & 31; b < p.B; b += 32) longest = max(longest, latent_seq(p, b, row0));
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
       m = (longest + size - 1) / size - 1;
@@ -46,16 +49,19 @@ struct Deal {
   }
   __device__ __forceinline__ int sequences(const LatentReplayParams& p) const {
     int n = 0;
+#pragma unroll 1                                         // (unrolled: rollouts of 8192 tokens forward 289 -> 295 to 299 us, the other roles' code moves)
     for (int b0 = 0; b0 < p.B; b0 += 32) n += __popc(__ballot_sync(0xffffffffu, length(p, b0 + (threadIdx.x & 31)) > (int64_t)m * size));
     return n;
   }
-  // The next item of this CTA: block m of a sequence.
+  // The next item of this CTA: block m of a sequence.  Sequences come in order within a level and layer, so the search goes on where
+  // the last one ended (from the first sequence on for every item: 8192 of 32 tokens 57 instead of 5.2 ms forward, 115 instead of 7.5 back).
   __device__ __forceinline__ bool next(const LatentReplayParams& p, int& l, int& b, int& h) {
     const int k = pass * (int)gridDim.x + ((pass & 1) ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x), per = p.L * p.H;
     while (count > 0 && k - before >= count * per) {
       before += count * per;
       m += down ? -1 : 1;
       count = m >= 0 ? sequences(p) : 0;
+      at = seen = 0;
     }
     if (count == 0) return false;                        // (levels only end behind the last one)
     ++pass;
@@ -64,11 +70,12 @@ struct Deal {
     x /= p.H;
     l = x / count;
     x %= count;
-    for (int b0 = 0;; b0 += 32) {
-      const uint32_t has = __ballot_sync(0xffffffffu, length(p, b0 + (threadIdx.x & 31)) > (int64_t)m * size);
+    if (x < seen) at = seen = 0;                         // (the next layer)
+    for (;; at += 32) {
+      const uint32_t has = __ballot_sync(0xffffffffu, length(p, at + (threadIdx.x & 31)) > (int64_t)m * size);
       const int n = __popc(has);
-      if (x < n) { b = b0 + (int)__fns(has, 0, x + 1); return true; }
-      x -= n;
+      if (x - seen < n) { b = at + (int)__fns(has, 0, x - seen + 1); return true; }
+      seen += n;
     }
   }
 };
