@@ -1,5 +1,5 @@
 """Latent attention where single keys and far masks decide: weights that sit on one key at the edges of tiles, pages and pieces of long
-sequences, gradients behind the 256th tile of keys, batches of thousands of short sequences."""
+sequences, gradients behind the 256th tile of keys."""
 import numpy as np
 import pytest
 import torch
@@ -105,17 +105,3 @@ def test_gradients_behind_the_plans_masks(T, rounds):
     got = [r.out[0, -n:, 0], r.grads[0][0, -n:, 0], r.grads[1][0, -n:, 0, :128], r.grads[1][0, -n:, 0, 128:], r.grads[2][0, -n:]]
     for name, g, (want, bound) in zip(("out", "grad q", "grad k", "grad v", "grad k_rope"), got, last_queries(r, n, rounds)):
         assert_within(g, want, bound, name)
-
-
-@pytest.mark.parametrize("B,H,rounds,longest", [(1500, 2, None, 1), (2111, 1, [(0.5, 0.5)], 1), (1100, 3, [(0.3, 0.4), (0.8, 0.7)], 900)])
-def test_batches_of_many_short_sequences(B, H, rounds, longest):
-    """More sequences than a warp looks over at once, empty ones among them, and a long one at the end."""
-    rng = np.random.default_rng(B)
-    lens = [int(x) for x in rng.integers(0, 40, B)]
-    lens[B // 3], lens[-1], lens[0] = 150, max(longest, lens[-1]), 0
-    r = Replay(1, B, H, 32, lens, 1, 90, rounds)
-    r.forward(bf16)
-    r.check_forward()
-    r.backward()
-    r.check_backward()
-    assert status_value(r.st) == 0
