@@ -81,3 +81,75 @@ def test_a_budget_below_minus_one_is_reported():
     assert status_value(ro.status) == 1
     want = ora.pool_update(*before, 32, np.array([0, 0]), ro.slots.shape[1], host(ro.kept_sorted), np.array([-2, 1]))
     same_books(ro, want)
+
+
+def test_a_ragged_life_of_rounds_becomes_the_training_masks():
+    """Prompts, steps and rounds that leave rollouts out, by the loop; its kept lists through ngc_replay_visibility, and those into the pass
+    over whole sequences: every step's absorbed attention, with the projections applied, is that pass's row of the token."""
+    from paper_2604_18002_b200.rollout import NgcLatentRollout
+    b = ngc()
+    L, B, H, dc, dr, page, cap = 2, 3, 4, 256, 32, 32, 8
+    prompt, steps, scale = [70, 33, 130], 80, (128 + dr) ** -0.5
+    T = [p + steps for p in prompt]
+    rounds_at = {10: [2, -1, 3], 41: [3, 2, -1], 63: [2, 2, 2]}
+    latent, rope = [normal((L, n, dc), 500 + i) for i, n in enumerate(T)], [normal((L, n, dr), 520 + i) for i, n in enumerate(T)]
+    g = torch.Generator().manual_seed(17)
+    U, W = ((torch.randn((L, H, 128, dc), generator=g) / dc ** 0.5).to(bf16) for _ in range(2))
+    qn, qr = [normal((L, n, H, 128), 540 + i) for i, n in enumerate(T)], [normal((L, n, H, dr), 560 + i) for i, n in enumerate(T)]
+    ro = NgcLatentRollout(L, B, H, dc, dr, n_pages=24, pages_cap=cap, max_new=sum(prompt), scale=scale, page=page, lists=b.LISTS_PER_LAYER)
+    ro.update(ints(prompt))
+    ro.write(torch.cat([x[:, :p] for x, p in zip(latent, prompt)], 1).cuda(), torch.cat([x[:, :p] for x, p in zip(rope, prompt)], 1).cuda())
+    got, n_new = [torch.zeros((L, n, H, 128)) for n in T], ints([1] * B)
+    own = [[] for _ in range(B)]                                               # per rollout: (kept, budget, alive before, total before) of its rounds
+    for i in range(steps):
+        now = [p + i for p in prompt]
+        if i in rounds_at:
+            lens = host(ro.pool.lens).copy()
+            units = -(-lens // page)
+            logits = torch.randn((B, L, cap), generator=g)
+            for s in range(B):
+                for l in range(L):
+                    logits[s, l, int(units[s, l]):] = -float("inf")
+            ro.evict(logits.cuda(), ints(units.max(1).tolist()), None, ints(rounds_at[i]), 11, i, n_new, n_slots=B)
+            for s in range(B):
+                if rounds_at[i][s] >= 0:
+                    own[s].append((host(ro.kept_sorted)[s], rounds_at[i][s], lens[s], now[s]))
+        else:
+            ro.update(n_new, B)
+        out = torch.zeros((L, B, H, dc), device="cuda")
+        q = torch.stack([torch.einsum("lhd,lhdc->lhc", qn[s][:, now[s]].float(), U.float()) for s in range(B)], 1).to(bf16).cuda()
+        r = torch.stack([qr[s][:, now[s]] for s in range(B)], 1).cuda()
+        rows = [torch.stack([x[s][:, now[s]] for s in range(B)], 1).cuda() for x in (latent, rope)]
+        for l in range(L):
+            ro.write(*rows, l, l + 1)
+            ro.decode(q, r, out, l, l + 1)
+        for s in range(B):
+            got[s][:, now[s]] = torch.einsum("lhc,lhdc->lhd", out[:, s].cpu(), W.float())
+    ro.check_status()
+    # the histories; rollouts with fewer rounds get ones behind their end, which keep nothing
+    R = max(len(x) for x in own)
+    kept, budget = torch.full((R, B, L, cap), -1, dtype=torch.int32), torch.zeros((R, B), dtype=torch.int32)
+    alive, total = torch.full((R, B, L), 10 ** 6, dtype=torch.int32), torch.full((R, B), 2 ** 30, dtype=torch.int32)
+    assert sorted(len(x) for x in own) == [2, 2, 3]
+    for s in range(B):
+        for k, (ks, n, before, at) in enumerate(own[s]):
+            kept[k, s], budget[k, s], alive[k, s], total[k, s] = torch.as_tensor(ks), n, torch.as_tensor(before), at
+        for k in range(len(own[s]), R):
+            alive[k, s] = torch.as_tensor(host(ro.pool.lens)[s])
+    most = cap * page
+    pos, count, st = torch.empty((R, B, L, cap * page), dtype=torch.int32, device="cuda"), torch.empty((R, B, L), dtype=torch.int32, device="cuda"), b.new_status()
+    b.ngc_replay_visibility(kept.cuda(), budget.cuda(), alive.cuda(), total.cuda(), page, most, pos, count, status=st)
+    assert status_value(st) == 0
+    seqs = b.NgcLatentSeqs(torch.tensor([0] + np.cumsum(T).tolist()).cuda(), ints(T), max(T))
+    kv = torch.cat([torch.cat([torch.einsum("ltc,lhdc->lthd", x.float(), w.float()).to(bf16) for w in (U, W)], -1) for x in latent], 1).cuda()
+    q = torch.cat([torch.cat([a, c], -1) for a, c in zip(qn, qr)], 1).cuda()
+    out = torch.zeros((L, sum(T), H, 128), device="cuda")
+    ws = b.alloc_workspace(b.latent_replay_workspace_bytes(seqs, q, kv, b.LISTS_PER_LAYER, R))
+    b.ngc_latent_replay_attn(seqs, q, kv, torch.cat(rope, 1).cuda(), out, None, pos, count, total.cuda(), lists=b.LISTS_PER_LAYER, ws=ws, status=st)
+    assert status_value(st) == 0
+    for s in range(B):
+        at = sum(T[:s])
+        a, c = got[s][:, prompt[s]:], out[:, at + prompt[s]: at + T[s]].cpu()
+        # roundings on the way: the absorbed query, keys, values and probabilities, each half a step of bf16 (2**-8); scores are sums of
+        # some 300 products of size 1 / 13 with independent roundings, so they move by 0.01 or so, outputs by a few hundredths of their size
+        assert float((a - c).norm() / c.norm()) <= 0.02
