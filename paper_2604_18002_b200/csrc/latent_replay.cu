@@ -130,7 +130,8 @@ Space space_of(const ngc_latent_seqs* s, int lists, int n_rounds, int backward) 
 int prepare(const ngc_latent_seqs* s, const void* q, const void* kv, const void* k_rope, const int32_t* alive_pos, const int32_t* alive_count,
             const int32_t* total_before, int n_rounds, int kt_max, int lists, float scale, int out_dtype, void* ws, size_t ws_bytes,
             int32_t* dev_status, int backward, LatentReplayParams* p) {
-  if (!valid_seqs(s) || !q || !kv || !k_rope || n_rounds < 0 || lists < 0 || lists > 2 || (out_dtype != NGC_F32 && out_dtype != NGC_BF16) ||
+  // (tensors without rows have no address)
+  if (!valid_seqs(s) || (s->rows > 0 && (!q || !kv || !k_rope)) || n_rounds < 0 || lists < 0 || lists > 2 || (out_dtype != NGC_F32 && out_dtype != NGC_BF16) ||
       (n_rounds > 0 && (!alive_pos || !alive_count || !total_before || kt_max < 1)) || !(scale > 0.f && scale <= 2e38f) || !aligned16(q) ||
       !aligned16(kv) || !aligned16(k_rope))
     return NGC_ERR_INVALID_ARG;
@@ -167,8 +168,9 @@ extern "C" int ngc_latent_replay_attn(const ngc_latent_seqs* s, const void* q, c
   LatentReplayParams p;
   const int rc = prepare(s, q, kv, k_rope, alive_pos, alive_count, total_before, n_rounds, kt_max, lists, scale, out_dtype, ws, ws_bytes, dev_status, 0, &p);
   if (rc != NGC_OK) return rc;
+  if (s->rows == 0) return NGC_OK;
   if (!out || !aligned16(out)) return NGC_ERR_INVALID_ARG;
-  if (s->rows == 0 || s->max_len == 0) return NGC_OK;
+  if (s->max_len == 0) return NGC_OK;
   p.out = out; p.lse = lse;
   if (n_rounds > 0) NGC_CUDA_TRY(launch_gone(p, stream));
   return launch_latent_fwd(p, stream);
@@ -183,10 +185,11 @@ extern "C" int ngc_latent_replay_attn_backward(const ngc_latent_seqs* s, const v
   LatentReplayParams p;
   const int rc = prepare(s, q, kv, k_rope, alive_pos, alive_count, total_before, n_rounds, kt_max, lists, scale, out_dtype, ws, ws_bytes, dev_status, 1, &p);
   if (rc != NGC_OK) return rc;
+  if (s->rows == 0) return NGC_OK;
   if (!out || !lse || !grad_out || !grad_q || !grad_kv || !grad_k_rope || !aligned16(out) || !aligned16(grad_out) || !aligned16(grad_q) ||
       !aligned16(grad_kv) || !aligned16(grad_k_rope))
     return NGC_ERR_INVALID_ARG;
-  if (s->rows == 0 || s->max_len == 0) return NGC_OK;
+  if (s->max_len == 0) return NGC_OK;
   p.out = const_cast<void*>(out); p.lse = const_cast<float*>(lse); p.go = (const __nv_bfloat16*)grad_out;
   p.gq = (__nv_bfloat16*)grad_q; p.gkv = (__nv_bfloat16*)grad_kv; p.gkr = (__nv_bfloat16*)grad_k_rope;
   if (n_rounds > 0) NGC_CUDA_TRY(launch_gone(p, stream));
