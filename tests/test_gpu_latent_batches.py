@@ -20,3 +20,22 @@ def test_batches_of_many_short_sequences(B, H, rounds, longest):
     r.backward()
     r.check_backward()
     assert status_value(r.st) == 0
+
+
+@pytest.mark.parametrize("rounds", [None, [(0.3, 0.5), (0.6, 0.5)]])
+def test_a_bound_on_the_lengths_may_be_far_above_them(rounds):
+    r = Replay(1, 3, 2, 64, [300, 1, 170], 2, 95, rounds)
+    r.seqs.max_len = 70001
+    r.forward(bf16)
+    r.check_forward()
+    r.backward()
+    r.check_backward()
+    assert status_value(r.st) == 0
+
+
+def test_a_batch_without_rows():
+    r = Replay(2, 2, 2, 64, [0, 0], 0, 96, None)
+    r.seqs.max_len = 50
+    assert r.forward(bf16)[0].numel() == 0
+    assert all(g.numel() == 0 for g in r.backward())
+    assert status_value(r.st) == 0

@@ -153,3 +153,37 @@ def test_a_ragged_life_of_rounds_becomes_the_training_masks():
         # roundings on the way: the absorbed query, keys, values and probabilities, each half a step of bf16 (2**-8); scores are sums of
         # some 300 products of size 1 / 13 with independent roundings, so they move by 0.01 or so, outputs by a few hundredths of their size
         assert float((a - c).norm() / c.norm()) <= 0.02
+
+
+def test_a_captured_round_follows_its_budgets():
+    """Eviction, books and growth in one graph, replayed with other budgets (rollouts left out change), beside the same calls made one by one."""
+    from paper_2604_18002_b200.rollout import NgcLatentRollout
+    b = ngc()
+    L, B, page, cap = 2, 4, 32, 8
+    ro = [NgcLatentRollout(L, B, 4, 128, 16, n_pages=40, pages_cap=cap, max_new=600, scale=0.1, page=page, lists=b.LISTS_PER_LAYER) for _ in range(2)]
+    n, protect, budget, n_new = ints([0] * B), ints([1] * B), ints([-1] * B), ints([0] * B)
+    logits = torch.zeros((B, L, cap), device="cuda")
+
+    def round_of(k):
+        ro[k].evict(logits, n, protect, budget, 21, 4, n_new, n_slots=300)
+    for k in range(2):
+        ro[k].update(ints([160, 90, 33, 250]))
+        round_of(k)                                                            # (all left out: nothing happens)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        round_of(0)
+    for i, (budgets, new) in enumerate([([3, -1, 1, 5], [1, 100, 1, 0]), ([-1, 2, -1, 2], [70, 1, 64, 3]), ([2, 1, 1, -1], [-1, 5, 0, 90])]):
+        n.copy_(ints((-(-host(ro[1].pool.lens) // page)).min(1).tolist()))
+        budget.copy_(ints(budgets))
+        n_new.copy_(ints(new))
+        logits.copy_(torch.randn((B, L, cap), generator=torch.Generator().manual_seed(i)).cuda())
+        before = books(ro[1])
+        graph.replay()
+        round_of(1)
+        assert torch.equal(ro[0].kept_sorted, ro[1].kept_sorted)
+        want = ora.pool_update(*before, page, np.array(new), 300, host(ro[1].kept_sorted), np.array(budgets))
+        assert want[5] == set()
+        for k in range(2):
+            same_books(ro[k], want, f"round {i}, {'captured' if k == 0 else 'eager'}")
+            ro[k].check_status()
