@@ -6,7 +6,7 @@ import torch
 
 from helpers import ngc, status_value
 from oracle import latent as ora
-from test_gpu_latent import Replay, assert_within, bf16, f32, host, normal, random_pool
+from test_gpu_latent import Replay, assert_within, bf16, f32, host, normal, random_pool, run_decode
 
 pytestmark = pytest.mark.gpu
 
@@ -54,6 +54,26 @@ def test_decode_finds_the_one_key_that_counts(H, dc, dr, page, lens):
     assert status_value(st) == 0
     want, bound = ora.decode(host(pool.rows), table, host(pool.lens), host(ql), host(qr), scale, 0)
     assert_within(out, want, bound)
+
+
+@pytest.mark.parametrize("lens", [[1, 1, 300], [9001, 9001, 70], [70] * 150])
+def test_scores_without_a_number(lens):
+    """A rotary infinity in one key: plus infinity makes the head NaN; minus infinity takes the key out, and where it is the only key, leaves
+    no score at all: NaN too.  Whole units and ones in many parts; the last sequence has none of it."""
+    B, dc, dr, page = len(lens), 128, 16, 64
+    pool = random_pool(1, B, page, -(-max(lens) // page), sum(-(-n // page) for n in lens) + 1, lens, 0, 71, dc, dr)
+    clean, table = host(pool.rows), host(pool.page_table)
+    for s in range(B - 1):
+        t = lens[s] - 1
+        pool.rows[0, table[s, 0, t // page], t % page, dc + 3] = float("inf")
+    ql, qr, out, st = run_decode(pool, 8, 0.1)
+    assert status_value(st) == 0
+    out, up = out[0].cpu(), qr[0, :, :, 3].float() > 0
+    for s in range(B - 1):
+        assert bool(torch.isnan(out[s, up[s]]).all())
+        assert bool((torch.isnan if lens[s] == 1 else torch.isfinite)(out[s, ~up[s]]).all())
+    want, bound = ora.decode(clean, table[-1:], host(pool.lens)[-1:], host(ql)[:, -1:], host(qr)[:, -1:], 0.1, 0)
+    assert_within(out[None, -1:], want, bound)
 
 
 # ------------------------------------------------------------------ expanded form

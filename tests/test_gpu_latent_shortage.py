@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 
 from oracle import latent as ora
+from test_gpu_debug_build import debug_library      # noqa: F401
 from test_gpu_latent import host, random_pool, run_update
 
 pytestmark = pytest.mark.gpu
@@ -59,3 +60,9 @@ def test_a_sequence_with_more_new_tokens_than_slots_does_not_evict_either(n_slot
     assert run_update(pool, [20, n_slots, 0, -1, 5], n_slots, kept, budget) == {ora.BAD_COUNTS}
     assert (host(pool.page_table)[1] == before[0][1]).all() and (host(pool.lens)[1] == before[1][1]).all()
     assert host(pool.lens)[[0, 2, 3, 4]].tolist() == [[52, 48], [64, 64], [0, 0], [33, 33]]      # (the last one's 5 tokens have no slots either)
+
+
+@pytest.mark.parametrize("B,seed", [(33, 2), (300, 3)])
+def test_a_short_pool_on_the_bounds_checking_build(B, seed, debug_library):      # noqa: F811
+    test_who_grows_in_a_short_pool(B, seed)
+    test_a_sequence_with_more_new_tokens_than_slots_does_not_evict_either(60)
