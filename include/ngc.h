@@ -650,7 +650,8 @@ int ngc_latent_write(ngc_latent_pool* c, const int32_t* slots, int n_slots, cons
  *   out      [L][B][H][d_latent] of out_dtype (NGC_F32 or NGC_BF16), 16-byte aligned; an empty sequence gives zeros
  * fp32 scores, softmax and sums; the probabilities are rounded to bf16 for the
  * second product.  Rows of a page behind the length take no part whatever they
- * hold.  A length outside 0 .. pages_cap * page is reported (NGC_DEV_BAD_COUNTS) and the
+ * hold; a head with a score that is NaN or plus infinity, or with none above
+ * minus infinity, gets NaN.  A length outside 0 .. pages_cap * page is reported (NGC_DEV_BAD_COUNTS) and the
  * sequence skipped; a bad page-table entry is reported (NGC_DEV_BAD_PAGE) and the
  * outputs of its sequence are unspecified.  Results are the same in every run; where one lies in its
  * last bits may depend on the call's other lengths (they decide how the work is
@@ -667,7 +668,7 @@ typedef struct {
   const int64_t* seq_off;    /* [B+1], seq_off[0] = 0, seq_off[B] = rows */
   const int32_t* lens;       /* [B] */
   int64_t rows;              /* host copy; L * rows < 2^31 */
-  int32_t L, B, H;
+  int32_t L, B, H;           /* L * B <= 65535 */
   int32_t d_nope, d_v;       /* 128 */
   int32_t d_rope;            /* 16, 32, 48 or 64 */
   int32_t dtype;             /* NGC_BF16 */

@@ -584,7 +584,7 @@ __global__ void __launch_bounds__(cta_threads(NH), 1) latent_decode_kernel(const
 }
 
 // Joins the parts of units that lie in several pieces.  Bound by latency, plan -> maxima and sums of the parts -> result, so the CTAs are
-// small enough to be resident all at once.  The first p.pieces x H / 4 take a unit in few parts each, the one that begins in their piece,
+// small enough to be resident all at once with up to 32 heads (with more up to 3552 on 148 SMs that hold 2368).  The first p.pieces x H / 4 take a unit in few parts each, the one that begins in their piece,
 // and four heads of it: a warp works out the weights of one head's parts, then a thread sums four channels of all four.  The others take
 // the heads of units in many parts, 128 channels at a time, a quarter of the parts to each warp (one sequence of 8192 tokens, 128 parts: the
 // call takes 25 us, 82 where a thread adds up all of them).  Many are 8 or more: with 6, 16 sequences of 128 heads take 51 us instead of 45,

@@ -15,7 +15,7 @@
 //                     moves only when the true one has grown by more than 2^8, so O is rarely rescaled
 // 128-key tiles because a product of 128 x 64 waits for shared memory (Q is read again for every tile).
 // Bound by the tensor pipe: causal, 8192 tokens of 16 heads, batch 2: 588 us, 1169 TFLOP/s; rollouts of 6500 to 8192 tokens with a round
-// every 1024: 292 us, 714 TFLOP/s of visible pairs, the rest are products of half and whole tiles that a round cuts through.
+// every 1024: 287 to 304 us, some 710 TFLOP/s of visible pairs, the rest are products of half and whole tiles that a round cuts through.
 #include <cuda.h>
 #include <cuda_bf16.h>
 

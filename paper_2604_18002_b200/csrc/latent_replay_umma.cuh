@@ -110,11 +110,6 @@ struct WalkEnv {
     if (!ALONE) __syncwarp();
     if (ALONE || (threadIdx.x & 31) == 0) ptx::mbar_arrive(&ring->empty[k % kPlans]);
   }
-  // For both of two barriers: half of the lanes look at one, half at the other.
-  __device__ __forceinline__ bool wait(uint64_t* bar0, uint32_t parity0, uint64_t* bar1, uint32_t parity1) const {
-    const bool odd = threadIdx.x & 1;
-    return umma::warp_wait(odd ? bar1 : bar0, odd ? parity1 : parity0, abort, p.dev_status);
-  }
   __device__ __forceinline__ const int4* tiles(int l, int b) const {
     return p.tile_gone ? p.tile_gone + ((int64_t)b * p.G + list_of(p.lists, l, 0, 1)) * (p.gone_cap / kLatTile) : nullptr;
   }
